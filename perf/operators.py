@@ -4,8 +4,8 @@ A serving loop over compressed latent slots runs these next to each other:
 
   map      block tables and slot maps from request lengths            (mtla_slot_map)
   rope     rotation of the RoPE part of query heads and shared keys   (mtla_rope; inverse = gradient)
-  store    latent rows into the 4-bit pool, and read back             (mtla_pool4_write / mtla_pool4_read)
-  attend   one query per sequence over its 4-bit slots                (mtla_pool4_attend)
+  store    latent rows into the 4-bit pool, and read back             (mtla_qpool_write / mtla_qpool_read)
+  attend   one query per sequence over its 4-bit slots                (mtla_qpool_attend)
 
 A pool page holds 64 slots: [64][r/2] bytes of 4-bit codes (e2m1: sign, two exponent bits, one
 fraction bit; latent 2k in the low half of byte k), [64][r/32] bytes of group scales (the upper
@@ -247,9 +247,9 @@ def prepare(case, seed: int):
                  lse=torch.empty(b, case["heads"], dtype=torch.float32, device="cuda"))
     if own:
         from paper_2505_13544_b200 import binding as M
-        cfg = M.make_pool4_config(n_heads=case["heads"], latent_rank=r, rope_dim=dr, n_pages=n_pages)
+        cfg = M.make_qpool_config(n_heads=case["heads"], latent_rank=r, rope_dim=dr, n_pages=n_pages)
         # The workspace that a serving loop keeps for its batch.
-        state["workspace"] = torch.empty(M.mtla_pool4_workspace_bytes(cfg, b), dtype=torch.uint8, device="cuda")
+        state["workspace"] = torch.empty(M.mtla_qpool_workspace_bytes(cfg, b), dtype=torch.uint8, device="cuda")
     return state
 
 
@@ -414,13 +414,13 @@ def run(state):
         return M.mtla_rope(cfg, [state["q"], state["k"]], state["pos"], first=[case["plain"], 0],
                            out=state["out"], inverse=case["inverse"])
     if op == "store":
-        cfg = M.make_pool4_config(n_heads=1, latent_rank=case["rank"], rope_dim=case["rope"],
+        cfg = M.make_qpool_config(n_heads=1, latent_rank=case["rank"], rope_dim=case["rope"],
                                   n_pages=state["n_pages"])
-        M.mtla_pool4_write(cfg, state["pages"], state["rows"], state["index"])
-        return M.mtla_pool4_read(cfg, state["pages"], state["index"], out=state["out"])
-    cfg = M.make_pool4_config(n_heads=case["heads"], latent_rank=case["rank"], rope_dim=case["rope"],
+        M.mtla_qpool_write(cfg, state["pages"], state["rows"], state["index"])
+        return M.mtla_qpool_read(cfg, state["pages"], state["index"], out=state["out"])
+    cfg = M.make_qpool_config(n_heads=case["heads"], latent_rank=case["rank"], rope_dim=case["rope"],
                               n_pages=state["n_pages"])
-    return list(M.mtla_pool4_attend(cfg, state["pages"], state["table"], state["slots"], state["q"],
+    return list(M.mtla_qpool_attend(cfg, state["pages"], state["table"], state["slots"], state["q"],
                                     scale=state["scale"], out=state["out"], lse=state["lse"],
                                     workspace=state["workspace"]))
 
