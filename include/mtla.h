@@ -289,6 +289,118 @@ size_t mtla_train_workspace_bytes(const mtla_handle* h, int32_t B, int32_t T);
 int mtla_train_backward(mtla_handle* h, const void* x, const void* dy, int32_t B, int32_t T, void* dx,
                         const mtla_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- operators around a paged latent cache held in 4 bits ----
+ *
+ * For serving loops that keep their own requests and page lists: what they run next to a layer's
+ * products when the latent cache is to take about a third of its bf16 bytes.  A step is
+ *     mtla_slot_map      which slot and page every new token goes to,
+ *     mtla_rope          the RoPE parts of its queries and of the shared key (Section 4.3),
+ *     mtla_qpool_write   the slots' running states (Section 4.1) into the pool,
+ *     mtla_qpool_attend  every sequence's query over its slots (absorbed form, Eq. 12 / Eq. 17).
+ * The calls keep no state and allocate nothing.  They run on the GPU that owns their (first)
+ * buffer, whichever GPU is current; all buffers of a call are that GPU's, and `stream` is one of
+ * its streams.  All of them may be captured into CUDA graphs.  Errors are as for the handle calls;
+ * what only the GPU can see (lengths, page numbers, indices) never leads outside the buffers, each
+ * call says what becomes of it. */
+
+/* Block tables and slot maps from request lengths.  Request b holds held[b] tokens and gets
+ * fresh[b] new ones (either may be 0); with stride s (s tokens share a slot) it then has
+ * slots[b] = ceil((held + fresh) / s) slots in pages of 64.  Pages that it does not have yet are
+ * taken from free_pages (device, n_free page numbers) in request order and entered into its row of
+ * `table` (device [B][table_width], read for the pages it has, written only where a page is new).
+ * Outputs (device): starts [B + 1], the requests' first tokens in the flat token list; per token
+ * its request `seq`, its position (0-based, the RoPE angle's), the pool row of its slot (`slot` =
+ * page * 64 + place) and `store`: the same pool row if the token is the last of its chunk or of
+ * this call, else -1, that is the index at which mtla_qpool_write puts the token's running state
+ * (Section 4.1: later tokens of the chunk replace it).  The token arrays have n_tokens entries;
+ * behind the last token seq, slot and store are -1 and position is 0.  taken [1]: pages taken, so
+ * that the next call's list starts there.  A page that is still open must not be shared.
+ * A batch that does not fit (too few free pages, a row wider than the table, more tokens than
+ * n_tokens, a negative or overflowing length) is refused as a whole on the device: taken is -1, all
+ * tokens read as behind the last one, starts is 0, slots[b] = ceil(held / s), the table is left.
+ * B <= 16384. */
+typedef struct {
+  int32_t *starts, *seq, *position;
+  int64_t *slot, *store;
+  int32_t *slots, *taken;
+} mtla_slot_map_out;
+int mtla_slot_map(const int32_t* held, const int32_t* fresh, int32_t B, int32_t stride, int32_t* table,
+                  int32_t table_width, const int32_t* free_pages, int32_t n_free, const mtla_slot_map_out* out,
+                  int32_t n_tokens, void* stream);
+
+/* Rotary positions (Section 4.3) on rope_dim consecutive elements of every head, from `first` on:
+ * pair k of a token at position p turns by p f_k, f_k = theta^(-2k / rope_dim).  Pairs are
+ * neighbours (INTERLEAVED, the layers' own convention) or rope_dim / 2 apart (HALF).  Scaling for
+ * contexts longer than the trained one: LINEAR divides every f_k by `factor`; RAMP does so only for
+ * pairs that turn slowly: with t_k = train_tokens f_k / 2 pi turns and g = (t_k - ramp_low) /
+ * (ramp_high - ramp_low) cut to [0, 1], f_k becomes g f_k + (1 - g) f_k / factor.  Cosine and sine
+ * are multiplied by `magnitude`.  The angle is formed in 64 bits, so that far positions keep it.
+ * inverse != 0 turns back by the same angle (magnitude included): the gradient of the rotation.
+ * Up to four tensors (queries, keys, ...) of the same tokens and type are rotated by one launch;
+ * each is read as [n_tokens][n_heads][width] and written to y of the same shape, elements outside
+ * the part copied.  Strides are in elements, elements of a head are consecutive.  y may be x (in
+ * place: same strides, nothing is copied), otherwise x and y must not overlap; rows of y must not
+ * share elements.  rope_dim even, 2 .. 256; 16-byte accesses are used where sizes, strides
+ * and addresses allow them. */
+enum { MTLA_ROPE_INTERLEAVED = 0, MTLA_ROPE_HALF = 1 };
+enum { MTLA_ROPE_PLAIN = 0, MTLA_ROPE_LINEAR = 1, MTLA_ROPE_RAMP = 2 };
+typedef struct {
+  int32_t rope_dim, layout, scaling;
+  int32_t train_tokens;        /* RAMP: context length of the training */
+  float theta;                 /* 0 selects 10000 */
+  float factor;                /* LINEAR, RAMP; 0 selects 1 */
+  float ramp_low, ramp_high;   /* RAMP: turns over train_tokens at which scaling is full / absent */
+  float magnitude;             /* 0 selects 1 */
+} mtla_rope_config;
+typedef struct {
+  const void* x;
+  void* y;
+  int64_t x_token_stride, x_head_stride, y_token_stride, y_head_stride;
+  int32_t n_heads, width, first;
+} mtla_rope_tensor;
+int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int32_t n_tensors, int32_t dtype,
+              const int32_t* positions, int32_t n_tokens, int32_t inverse, void* stream);
+
+/* The 4-bit pool: n_pages pages of mtla_qpool_page_bytes bytes (device, 16-byte aligned; 0 if the
+ * configuration is invalid), 64 slots each.  A slot's r latents are e2m1 codes (0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives) times a scale per 32 latents; the scale is the smallest number of 4
+ * significant bits, at least 2^-17 apart, whose six-fold reaches the group's largest magnitude, at
+ * most 10240 (larger latents saturate at 61440).  The code is the nearest one, the even one on a
+ * tie.  A group with an infinity or a NaN reads back as NaN.  The d_R RoPE-key elements are kept in
+ * bf16.  A slot takes r / 2 + r / 32 + 2 d_R bytes: 400 at r 512 / d_R 64, against 1152 in bf16.
+ * n_heads 1 .. 32, r a multiple of 64 up to 512, d_R 32 or 64, as for the layers. */
+typedef struct {
+  int32_t n_heads;             /* query heads (attend only; any valid value elsewhere) */
+  int32_t latent_rank, rope_dim;
+  int32_t n_pages;
+} mtla_qpool_config;
+size_t mtla_qpool_page_bytes(const mtla_qpool_config* cfg);
+
+/* Rows of r + d_R elements (the layout of mtla_cache_export; row_stride elements apart, a multiple
+ * of 16 bytes, 16-byte aligned) into the pool rows index[0 .. n-1] (device), and back.  write skips
+ * rows whose index is outside the pool (-1 in a slot map); apart from those no index may occur
+ * twice, since the rows would be stored into each other.  read fills rows of such an index with
+ * zeros; values are exact in both types. */
+int mtla_qpool_write(const mtla_qpool_config* cfg, void* pages, const void* rows, int64_t row_stride,
+                     int32_t dtype, const int64_t* index, int32_t n, void* stream);
+int mtla_qpool_read(const mtla_qpool_config* cfg, const void* pages, const int64_t* index, int32_t n,
+                    void* rows, int64_t row_stride, int32_t dtype, void* stream);
+
+/* One query per sequence over its slots: q device [B][n_heads][r + d_R] (absorbed query and rotated
+ * RoPE query), out device [B][n_heads][r] = softmax(scale q [c ; k]^T) c over the first slots[b]
+ * slots of the pages in row b of `table` (device [B][table_width]); lse (device [B][n_heads], fp32,
+ * may be NULL) receives the natural logarithm of the denominator, for joining with other slots.
+ * dtype is that of q and out; sums, maxima and denominators are fp32.  A sequence without slots
+ * (slots[b] <= 0) gives zeros and minus infinity.  slots[b] past 64 * table_width counts as that
+ * many; slots of a page number outside the pool are left out, and a sequence with no other gives NaN.
+ * workspace: device, 256-byte aligned, mtla_qpool_workspace_bytes(cfg, B) bytes (0 if invalid); its
+ * contents need no preparation, but two calls that may run at the same time need one each (graphs
+ * that may overlap included).  B <= 4096. */
+size_t mtla_qpool_workspace_bytes(const mtla_qpool_config* cfg, int32_t B);
+int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
+                      const int32_t* slots, int32_t B, const void* q, int32_t dtype, float scale, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Bytes of cache in use: B * ceil(tokens/s) * (r + d_R) * sizeof(element)  (Sections 4, 4.3);
  * with per-sequence token counts, the sum over the sequences. */
 size_t mtla_cache_bytes(const mtla_handle* h);

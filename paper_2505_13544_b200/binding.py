@@ -38,7 +38,9 @@ EXPORTED_SYMBOLS = (
     "mtla_clear_error", "mtla_stack_arena_bytes", "mtla_stack_create", "mtla_stack_prefill",
     "mtla_stack_decode_step", "mtla_stack_cache_bytes", "mtla_stack_layer", "mtla_stack_reset",
     "mtla_stack_check", "mtla_stack_launch_count", "mtla_stack_destroy",
-    "mtla_train_workspace_bytes", "mtla_train_backward")
+    "mtla_train_workspace_bytes", "mtla_train_backward", "mtla_slot_map", "mtla_rope",
+    "mtla_qpool_page_bytes", "mtla_qpool_write", "mtla_qpool_read", "mtla_qpool_workspace_bytes",
+    "mtla_qpool_attend")
 
 PAGE_SLOTS = 64
 
@@ -93,6 +95,25 @@ class mtla_stack_config(ctypes.Structure):
     _fields_ = [("n_layers", ctypes.c_int32), ("d_ff", ctypes.c_int32), ("ln_eps", ctypes.c_float)]
 
 
+class mtla_slot_map_out(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("starts", "seq", "position", "slot", "store", "slots", "taken")]
+
+
+class mtla_rope_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rope_dim", "layout", "scaling", "train_tokens")] + [
+        (n, ctypes.c_float) for n in ("theta", "factor", "ramp_low", "ramp_high", "magnitude")]
+
+
+class mtla_rope_tensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("x_token_stride", "x_head_stride", "y_token_stride", "y_head_stride")] + [
+        (n, ctypes.c_int32) for n in ("n_heads", "width", "first")]
+
+
+class mtla_qpool_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_heads", "latent_rank", "rope_dim", "n_pages")]
+
+
 _lib = None
 
 
@@ -106,6 +127,7 @@ def load_library() -> ctypes.CDLL:
     vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
     cfg_p, w_p = ctypes.POINTER(mtla_config), ctypes.POINTER(mtla_weights)
     pg_p, i32_p = ctypes.POINTER(mtla_paging), ctypes.POINTER(ctypes.c_int32)
+    qp_p = ctypes.POINTER(mtla_qpool_config)
     sigs = {
         "mtla_baseline_arena_bytes": (sz, [ctypes.POINTER(mtla_baseline_config)]),
         "mtla_baseline_create": (ctypes.c_int, [ctypes.POINTER(mtla_baseline_config),
@@ -166,6 +188,16 @@ def load_library() -> ctypes.CDLL:
         "mtla_train_backward": (ctypes.c_int, [vp, vp, vp, i32, i32, vp, ctypes.POINTER(mtla_grads), vp,
                                                sz, vp]),
         "mtla_selftest_wait_timeout": (ctypes.c_int, [vp, i32, vp]),
+        "mtla_slot_map": (ctypes.c_int, [vp, vp, i32, i32, vp, i32, vp, i32, ctypes.POINTER(mtla_slot_map_out),
+                                         i32, vp]),
+        "mtla_rope": (ctypes.c_int, [ctypes.POINTER(mtla_rope_config), ctypes.POINTER(mtla_rope_tensor), i32, i32,
+                                     vp, i32, i32, vp]),
+        "mtla_qpool_page_bytes": (sz, [qp_p]),
+        "mtla_qpool_write": (ctypes.c_int, [qp_p, vp, vp, ctypes.c_int64, i32, vp, i32, vp]),
+        "mtla_qpool_read": (ctypes.c_int, [qp_p, vp, vp, i32, vp, ctypes.c_int64, i32, vp]),
+        "mtla_qpool_workspace_bytes": (sz, [qp_p, i32]),
+        "mtla_qpool_attend": (ctypes.c_int, [qp_p, vp, vp, i32, vp, i32, vp, i32, ctypes.c_float, vp, vp, vp, sz,
+                                             vp]),
         "mtla_clear_error": (ctypes.c_int, [vp, vp]),
     }
     for name, (res, args) in sigs.items():
@@ -701,3 +733,195 @@ def mtla_train_backward(h: Handle, x: torch.Tensor, dy: torch.Tensor, stream=Non
                "mtla_train_backward")
         torch.cuda.current_stream().synchronize()     # the workspace is released on return
     return dx, grads
+
+
+# --------------------------------------------------------------------------- 4-bit latent pool
+
+_ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+_ROPE_SCALINGS = {"none": 0, "linear": 1, "ramp": 2}
+
+
+def _stream_of(t: torch.Tensor, stream) -> int:
+    """The given stream, or the current one of the GPU that holds `t`."""
+    return (torch.cuda.current_stream(t.device) if stream is None else stream).cuda_stream
+
+
+def _expect_on(t: torch.Tensor, like: torch.Tensor | None, dtype, shape, name: str) -> int:
+    """data_ptr() of a contiguous CUDA tensor of that type and shape on the GPU of `like`."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise TypeError(f"{name}: expected contiguous {dtype} tensor of shape {tuple(shape)}")
+    if not t.is_cuda or (like is not None and t.device != like.device):
+        raise TypeError(f"{name}: expected a CUDA tensor on the call's GPU")
+    return t.data_ptr()
+
+
+@dataclass
+class SlotMap:
+    """Outputs of mtla_slot_map (see include/mtla.h); keep one to reuse its buffers."""
+    starts: torch.Tensor     # int32 [B + 1]
+    seq: torch.Tensor        # int32 [n_tokens]
+    position: torch.Tensor   # int32 [n_tokens]
+    slot: torch.Tensor       # int64 [n_tokens]
+    store: torch.Tensor      # int64 [n_tokens]
+    slots: torch.Tensor      # int32 [B]
+    taken: torch.Tensor      # int32 [1]
+
+
+def make_slot_map(batch: int, n_tokens: int, device="cuda:0") -> SlotMap:
+    """Buffers for a batch and a number of tokens."""
+    i32 = dict(dtype=torch.int32, device=device)
+    return SlotMap(torch.empty(batch + 1, **i32), torch.empty(n_tokens, **i32), torch.empty(n_tokens, **i32),
+                   torch.empty(n_tokens, dtype=torch.int64, device=device),
+                   torch.empty(n_tokens, dtype=torch.int64, device=device), torch.empty(batch, **i32),
+                   torch.empty(1, **i32))
+
+
+def mtla_slot_map(held: torch.Tensor, fresh: torch.Tensor, free_pages: torch.Tensor, table: torch.Tensor, *,
+                  stride: int, n_tokens: int | None = None, out: SlotMap | None = None, stream=None) -> SlotMap:
+    """held, fresh [B], free_pages [F], table [B][width] (updated in place): int32 on the GPU.
+    n_tokens: entries of the token arrays; taken from `out` if that is given."""
+    if table.dim() != 2 or held.dim() != 1 or free_pages.dim() != 1:
+        raise TypeError("table: expected [B][width]; held and free_pages: one-dimensional")
+    batch, width = table.shape
+    if out is None:
+        if n_tokens is None:
+            raise TypeError("n_tokens: needed when no buffers are given")
+        out = make_slot_map(batch, n_tokens, table.device)
+    n = out.seq.shape[0]
+    if n_tokens is not None and n_tokens != n:
+        raise TypeError("out: its token arrays differ from n_tokens")
+    i32, i64 = torch.int32, torch.int64
+    tp = _expect_on(table, None, i32, (batch, width), "table")
+    o = mtla_slot_map_out(
+        _expect_on(out.starts, table, i32, (batch + 1,), "starts"), _expect_on(out.seq, table, i32, (n,), "seq"),
+        _expect_on(out.position, table, i32, (n,), "position"), _expect_on(out.slot, table, i64, (n,), "slot"),
+        _expect_on(out.store, table, i64, (n,), "store"), _expect_on(out.slots, table, i32, (batch,), "slots"),
+        _expect_on(out.taken, table, i32, (1,), "taken"))
+    _check(load_library().mtla_slot_map(
+        _expect_on(held, table, i32, (batch,), "held"), _expect_on(fresh, table, i32, (batch,), "fresh"), batch,
+        stride, tp, width, _expect_on(free_pages, table, i32, free_pages.shape, "free_pages"), free_pages.shape[0],
+        ctypes.byref(o), n, _stream_of(table, stream)), "mtla_slot_map")
+    return out
+
+
+def make_rope_config(*, rope_dim, layout="interleaved", theta=0.0, scaling="none", factor=0.0, ramp_low=1.0,
+                     ramp_high=32.0, train_tokens=0, magnitude=0.0) -> mtla_rope_config:
+    return mtla_rope_config(rope_dim, _ROPE_LAYOUTS[layout], _ROPE_SCALINGS[scaling], train_tokens, theta, factor,
+                            ramp_low, ramp_high, magnitude)
+
+
+def mtla_rope(cfg: mtla_rope_config, tensors, positions: torch.Tensor, *, first=0, out=None, inverse=False,
+              stream=None) -> list[torch.Tensor]:
+    """Rotates `tensors` (a list of [n_tokens][heads][width], any token and head strides) at
+    positions (int32 [n_tokens]); `first`: start of the rotated part, one for all or one each.
+    out: a list of tensors of the same shapes (the inputs themselves: in place), new ones if None."""
+    count, n_tokens = len(tensors), positions.shape[0]
+    firsts = first if isinstance(first, (list, tuple)) else [first] * count
+    if out is None:
+        out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in tensors]
+    if count < 1 or len(out) != count or len(firsts) != count:
+        raise TypeError("tensors, out and first: expected one entry per tensor")
+    dtype = tensors[0].dtype
+    if dtype not in _DTYPES:
+        raise TypeError(f"tensors: unsupported type {dtype}")
+    pp = _expect_on(positions, tensors[0], torch.int32, (n_tokens,), "positions")
+    arr = (mtla_rope_tensor * count)()
+    for i in range(count):
+        x, y = tensors[i], out[i]
+        for t in (x, y):
+            if t.dim() != 3 or t.dtype != dtype or t.shape != x.shape or t.shape[0] != n_tokens or (
+                    t.stride(2) != 1 and t.shape[2] > 1) or t.device != positions.device:
+                raise TypeError(f"tensor {i}: expected {dtype} [{n_tokens}][heads][width] on the call's GPU, "
+                                "consecutive elements in a head, and an output of the same shape")
+        xs, ys = x.stride(), y.stride()
+        arr[i] = mtla_rope_tensor(x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], x.shape[1], x.shape[2],
+                                  firsts[i])
+    _check(load_library().mtla_rope(ctypes.byref(cfg), arr, count, _DTYPES[dtype], pp, n_tokens, int(inverse),
+                                    _stream_of(positions, stream)), "mtla_rope")
+    return out
+
+
+def make_qpool_config(*, n_heads, latent_rank, rope_dim, n_pages) -> mtla_qpool_config:
+    return mtla_qpool_config(n_heads, latent_rank, rope_dim, n_pages)
+
+
+def mtla_qpool_page_bytes(cfg: mtla_qpool_config) -> int:
+    return load_library().mtla_qpool_page_bytes(ctypes.byref(cfg))
+
+
+def _qpool_pages(cfg: mtla_qpool_config, pages: torch.Tensor) -> int:
+    size = 34 * cfg.latent_rank + 128 * cfg.rope_dim        # mtla_qpool_page_bytes, without the call
+    return _expect_on(pages, None, torch.uint8, (cfg.n_pages, size), "pages")
+
+
+def make_qpool(cfg: mtla_qpool_config, device="cuda:0") -> torch.Tensor:
+    """An uninitialised pool: uint8 [n_pages][page bytes]."""
+    size = mtla_qpool_page_bytes(cfg)
+    if size == 0:
+        raise MTLAError(-2, "mtla_qpool_page_bytes")
+    return torch.empty(cfg.n_pages, size, dtype=torch.uint8, device=device)
+
+
+def _qpool_rows(cfg: mtla_qpool_config, rows: torch.Tensor, pages: torch.Tensor, n: int, name: str) -> int:
+    if (rows.dtype not in _DTYPES or rows.dim() != 2 or rows.shape != (n, cfg.latent_rank + cfg.rope_dim)
+            or rows.stride(1) != 1 or rows.device != pages.device):
+        raise TypeError(f"{name}: expected [{n}][r + d_R], fp32 or bf16, consecutive elements in a row, on the "
+                        "pool's GPU")
+    return rows.data_ptr()
+
+
+def mtla_qpool_write(cfg: mtla_qpool_config, pages: torch.Tensor, rows: torch.Tensor, index: torch.Tensor,
+                     stream=None) -> None:
+    """rows [n][r + d_R] (fp32 or bf16) into pool rows index (int64 [n]; outside the pool: skipped)."""
+    n = index.shape[0]
+    pp, rp = _qpool_pages(cfg, pages), _qpool_rows(cfg, rows, pages, n, "rows")
+    _check(load_library().mtla_qpool_write(ctypes.byref(cfg), pp, rp, rows.stride(0), _DTYPES[rows.dtype],
+                                           _expect_on(index, pages, torch.int64, (n,), "index"), n,
+                                           _stream_of(pages, stream)), "mtla_qpool_write")
+
+
+def mtla_qpool_read(cfg: mtla_qpool_config, pages: torch.Tensor, index: torch.Tensor, *, dtype=torch.bfloat16,
+                    out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Pool rows index (int64 [n]) as [n][r + d_R]; zeros where the index is outside the pool."""
+    n = index.shape[0]
+    pp = _qpool_pages(cfg, pages)
+    if out is None:
+        out = torch.empty(n, cfg.latent_rank + cfg.rope_dim, dtype=dtype, device=pages.device)
+    rp = _qpool_rows(cfg, out, pages, n, "out")
+    _check(load_library().mtla_qpool_read(ctypes.byref(cfg), pp,
+                                          _expect_on(index, pages, torch.int64, (n,), "index"), n, rp,
+                                          out.stride(0), _DTYPES[out.dtype], _stream_of(pages, stream)),
+           "mtla_qpool_read")
+    return out
+
+
+def mtla_qpool_workspace_bytes(cfg: mtla_qpool_config, batch: int) -> int:
+    return load_library().mtla_qpool_workspace_bytes(ctypes.byref(cfg), batch)
+
+
+def mtla_qpool_attend(cfg: mtla_qpool_config, pages: torch.Tensor, table: torch.Tensor, slots: torch.Tensor,
+                      q: torch.Tensor, *, scale: float, out: torch.Tensor | None = None,
+                      lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """q [B][n_heads][r + d_R] over the first slots[b] slots of table row b; returns (out
+    [B][n_heads][r], lse [B][n_heads] fp32).  workspace: uint8, see mtla_qpool_workspace_bytes; a
+    fresh one if None (a loop should keep one)."""
+    if q.dim() != 3 or table.dim() != 2 or q.dtype not in _DTYPES:
+        raise TypeError("q: expected fp32 or bf16 [B][n_heads][r + d_R]; table: expected [B][width]")
+    batch, width = table.shape
+    heads, r = cfg.n_heads, cfg.latent_rank
+    pp = _qpool_pages(cfg, pages)
+    if out is None:
+        out = torch.empty(batch, heads, r, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(batch, heads, dtype=torch.float32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(mtla_qpool_workspace_bytes(cfg, batch), dtype=torch.uint8, device=q.device)
+    _check(load_library().mtla_qpool_attend(
+        ctypes.byref(cfg), pp, _expect_on(table, pages, torch.int32, (batch, width), "table"), width,
+        _expect_on(slots, pages, torch.int32, (batch,), "slots"), batch,
+        _expect_on(q, pages, q.dtype, (batch, heads, r + cfg.rope_dim), "q"), _DTYPES[q.dtype], scale,
+        _expect_on(out, pages, q.dtype, (batch, heads, r), "out"),
+        _expect_on(lse, pages, torch.float32, (batch, heads), "lse"),
+        _expect_on(workspace, pages, torch.uint8, workspace.shape, "workspace"), workspace.numel(),
+        _stream_of(pages, stream)), "mtla_qpool_attend")
+    return out, lse

@@ -1,0 +1,363 @@
+// C ABI of the operators around the 4-bit latent pool (see include/mtla.h): argument checks and
+// launches.  They hold no state: every buffer is the caller's and nothing is allocated.
+#include "mtla.h"
+
+#include <cuda.h>
+#include <math.h>
+
+#include <atomic>
+
+#include "common.cuh"
+#include "qpool_attn.cuh"
+#include "qpool_format.cuh"
+#include "rope_kernel.cuh"
+#include "slot_map_kernel.cuh"
+
+using namespace mtla;
+
+namespace {
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Makes the GPU that owns `p` current for the call and puts the old one back afterwards: a caller
+// may hold tensors on another GPU than the current one.  status() is MTLA_ERR_INVALID_ARG for
+// memory that no GPU can reach.
+class OnDeviceOf {
+ public:
+  explicit OnDeviceOf(const void* p) {
+    cudaPointerAttributes attr;
+    if (cudaPointerGetAttributes(&attr, p) != cudaSuccess || cudaGetDevice(&old_) != cudaSuccess) {
+      cudaGetLastError();
+      status_ = MTLA_ERR_CUDA;
+      return;
+    }
+    if (attr.type != cudaMemoryTypeDevice && attr.type != cudaMemoryTypeManaged) {
+      status_ = MTLA_ERR_INVALID_ARG;
+      return;
+    }
+    device_ = attr.device;
+    if (device_ != old_) {
+      if (cudaSetDevice(device_) != cudaSuccess) { status_ = MTLA_ERR_CUDA; return; }
+      switched_ = true;
+    }
+  }
+  ~OnDeviceOf() { if (switched_) cudaSetDevice(old_); }
+  int status() const { return status_; }
+  int sm_count() const {
+    int n = 0;
+    return cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device_) == cudaSuccess && n > 0 ? n : 1;
+  }
+  int device() const { return device_; }
+
+ private:
+  int old_ = 0, device_ = 0, status_ = MTLA_OK;
+  bool switched_ = false;
+};
+
+int launched() { return cudaGetLastError() == cudaSuccess ? MTLA_OK : MTLA_ERR_CUDA; }
+
+// Raises a kernel's dynamic shared-memory limit to what one CTA may have, once per device.
+template <auto Kernel>
+bool raise_smem(int device) {
+  static std::atomic<uint64_t> done{0};
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (bit && (done.load(std::memory_order_acquire) & bit)) return true;
+  if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024) != cudaSuccess)
+    return false;
+  done.fetch_or(bit, std::memory_order_release);
+  return true;
+}
+
+bool good_pool(const mtla_qpool_config* c) {
+  return c && c->n_heads >= 1 && c->n_heads <= 32 && c->latent_rank >= 64 && c->latent_rank <= 512 &&
+         c->latent_rank % 64 == 0 && (c->rope_dim == 32 || c->rope_dim == 64) && c->n_pages >= 1;
+}
+bool good_dtype(int32_t d) { return d == MTLA_DTYPE_FP32 || d == MTLA_DTYPE_BF16; }
+
+qp::Format format_of(const mtla_qpool_config* c) { return qp::Format{c->latent_rank, c->rope_dim}; }
+
+// ---- rows in and out of the pool
+
+int row_call(const mtla_qpool_config* cfg, const void* pages, const void* rows, int64_t row_stride, int32_t dtype,
+             const int64_t* index, int32_t n, void* stream, bool write) {
+  if (!pages || !rows || !index || n < 0 || !good_dtype(dtype)) return MTLA_ERR_INVALID_ARG;
+  if (!good_pool(cfg)) return MTLA_ERR_UNSUPPORTED_SHAPE;
+  const int width = cfg->latent_rank + cfg->rope_dim, vec = dtype == MTLA_DTYPE_BF16 ? 8 : 4;
+  if (!aligned(pages, 16) || !aligned(rows, 16) || !aligned(index, 8) || row_stride < width || row_stride % vec)
+    return MTLA_ERR_INVALID_ARG;
+  if (n == 0) return MTLA_OK;
+  OnDeviceOf dev(pages);
+  if (dev.status() != MTLA_OK) return dev.status();
+  qp::RowArgs a;
+  a.pages = static_cast<uint8_t*>(const_cast<void*>(pages));
+  a.index = index;
+  a.rows = const_cast<void*>(rows);
+  a.row_stride = row_stride;
+  a.pool_rows = (long long)cfg->n_pages * qp::kPageRows;
+  a.n = n;
+  a.f = format_of(cfg);
+  const long long units = (long long)n * (width / 16);
+  const long long ctas = (units + qp::kRowThreads - 1) / qp::kRowThreads, most = 16ll * dev.sm_count();
+  auto kernel = dtype == MTLA_DTYPE_BF16 ? (write ? qp::qpool_write_kernel<bf16> : qp::qpool_read_kernel<bf16>)
+                                         : (write ? qp::qpool_write_kernel<float> : qp::qpool_read_kernel<float>);
+  kernel<<<(unsigned)(ctas < most ? ctas : most), qp::kRowThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  return launched();
+}
+
+// ---- attention
+
+// CTAs of the attention launch: at most this many per SM fit, and the workspace is sized for it.
+constexpr int kAttnCtasPerSm = 2;
+constexpr int kPlanSms = 148;
+constexpr int kPlanCtas = kAttnCtasPerSm * kPlanSms;
+
+struct AttnPlan { size_t o_part, ml_part, seq_parts, total; };
+AttnPlan plan_attend(const mtla_qpool_config* c, int B) {
+  AttnPlan p;
+  const size_t parts = (size_t)B + kPlanCtas;
+  p.o_part = 0;
+  p.ml_part = align_up(parts * c->n_heads * c->latent_rank * 4, 256);
+  p.seq_parts = p.ml_part + align_up(parts * c->n_heads * 8, 256);
+  p.total = p.seq_parts + align_up((size_t)B * 8, 256);
+  return p;
+}
+
+template <typename T, int MH>
+int launch_attend(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
+  using L = qp::AttnLayout<MH, sizeof(T) == 2 ? 1 : 2>;
+  if (!raise_smem<qp::qpool_attend_kernel<T, MH>>(dev.device())) return MTLA_ERR_CUDA;
+  const int smem = L::bytes(a.f, a.batch);
+  const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
+  const int per_sm = smem <= 112 * 1024 ? kAttnCtasPerSm : 1;
+  const long long most = (long long)a.batch * a.width;
+  const int ctas = (int)(most < (long long)per_sm * sms ? most : (long long)per_sm * sms);
+  if (launch_kernel(qp::qpool_attend_kernel<T, MH>, dim3(ctas), dim3(qp::kAttnThreads), (size_t)smem, st, true, a) !=
+      cudaSuccess) {
+    cudaGetLastError();
+    return MTLA_ERR_CUDA;
+  }
+  const int pieces = ceil_div(a.n_heads * a.f.r, qp::kCombineThreads * 4);
+  if (launch_kernel(qp::qpool_combine_kernel<T>, dim3(pieces, a.batch), dim3(qp::kCombineThreads), (size_t)0, st,
+                    true, a) != cudaSuccess) {
+    cudaGetLastError();
+    return MTLA_ERR_CUDA;
+  }
+  return MTLA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+// ---- slot maps
+
+int mtla_slot_map(const int32_t* held, const int32_t* fresh, int32_t B, int32_t stride, int32_t* table,
+                  int32_t table_width, const int32_t* free_pages, int32_t n_free, const mtla_slot_map_out* out,
+                  int32_t n_tokens, void* stream) {
+  if (!held || !fresh || !table || !out || B < 1 || stride < 1 || table_width < 1 || n_free < 0 || n_tokens < 0 ||
+      (n_free > 0 && !free_pages))
+    return MTLA_ERR_INVALID_ARG;
+  if (!out->starts || !out->slots || !out->taken) return MTLA_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (!out->seq || !out->position || !out->slot || !out->store)) return MTLA_ERR_INVALID_ARG;
+  const void* words[] = {held, fresh, table, free_pages, out->starts, out->slots, out->taken, out->seq, out->position};
+  for (const void* p : words)
+    if (!aligned(p, 4)) return MTLA_ERR_INVALID_ARG;
+  if (!aligned(out->slot, 8) || !aligned(out->store, 8)) return MTLA_ERR_INVALID_ARG;
+  if (B > sm::kMaxBatch) return MTLA_ERR_UNSUPPORTED_SHAPE;
+  OnDeviceOf dev(table);
+  if (dev.status() != MTLA_OK) return dev.status();
+  sm::Args a;
+  a.held = held;
+  a.fresh = fresh;
+  a.table = table;
+  a.free_pages = free_pages;
+  a.starts = out->starts;
+  a.seq = out->seq;
+  a.position = out->position;
+  a.slot = reinterpret_cast<long long*>(out->slot);
+  a.store = reinterpret_cast<long long*>(out->store);
+  a.slots = out->slots;
+  a.taken = out->taken;
+  a.batch = B;
+  a.stride = stride;
+  a.width = table_width;
+  a.n_free = n_free;
+  a.n_tokens = n_tokens;
+  a.vec = aligned(out->seq, 16) && aligned(out->position, 16) && aligned(out->slot, 16) && aligned(out->store, 16);
+  const size_t smem = 2 * ((size_t)B + 1) * 4;
+  if (!raise_smem<sm::slot_map_kernel>(dev.device())) return MTLA_ERR_CUDA;
+  const int work = sm::kThreads * sm::kPerThread;
+  const int ctas = (int)(((long long)n_tokens + work - 1) / work), most = 2 * dev.sm_count();
+  const cudaError_t e = launch_kernel(sm::slot_map_kernel, dim3(ctas < 1 ? 1 : ctas < most ? ctas : most),
+                                      dim3(sm::kThreads), smem, static_cast<cudaStream_t>(stream), true, a);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e == cudaSuccess ? MTLA_OK : MTLA_ERR_CUDA;
+}
+
+// ---- rotary positions
+
+int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int32_t n_tensors, int32_t dtype,
+              const int32_t* positions, int32_t n_tokens, int32_t inverse, void* stream) {
+  if (!cfg || !tensors || !positions || n_tensors < 1 || n_tokens < 0 || !good_dtype(dtype) ||
+      !aligned(positions, 4))
+    return MTLA_ERR_INVALID_ARG;
+  if (n_tensors > rp::kMaxTensors) return MTLA_ERR_UNSUPPORTED_SHAPE;
+  const int d = cfg->rope_dim;
+  if (d < 2 || d % 2 || d / 2 > rp::kMaxPairs) return MTLA_ERR_UNSUPPORTED_SHAPE;
+  if (cfg->layout != MTLA_ROPE_INTERLEAVED && cfg->layout != MTLA_ROPE_HALF) return MTLA_ERR_INVALID_ARG;
+  const double theta = cfg->theta == 0.f ? 10000.0 : (double)cfg->theta;
+  const double factor = cfg->factor == 0.f ? 1.0 : (double)cfg->factor;
+  const float magnitude = cfg->magnitude == 0.f ? 1.f : cfg->magnitude;
+  if (!(theta > 0.0) || !(factor > 0.0) || !isfinite(theta) || !isfinite(factor) || !isfinite(magnitude))
+    return MTLA_ERR_INVALID_ARG;
+  if (cfg->scaling != MTLA_ROPE_PLAIN && cfg->scaling != MTLA_ROPE_LINEAR && cfg->scaling != MTLA_ROPE_RAMP)
+    return MTLA_ERR_INVALID_ARG;
+  if (cfg->scaling == MTLA_ROPE_RAMP &&
+      (cfg->train_tokens < 1 || !(cfg->ramp_high > cfg->ramp_low) || !isfinite(cfg->ramp_low) ||
+       !isfinite(cfg->ramp_high)))
+    return MTLA_ERR_INVALID_ARG;
+
+  rp::Args a;
+  const double two_pi = 6.283185307179586476925286766559;
+  for (int k = 0; k < d / 2; ++k) {
+    double f = pow(theta, -2.0 * k / d);
+    if (cfg->scaling == MTLA_ROPE_LINEAR) {
+      f /= factor;
+    } else if (cfg->scaling == MTLA_ROPE_RAMP) {
+      const double turns = cfg->train_tokens * f / two_pi;
+      double keep = (turns - cfg->ramp_low) / ((double)cfg->ramp_high - cfg->ramp_low);
+      keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+      f = f * keep + f / factor * (1.0 - keep);
+    }
+    a.turns[k] = f / two_pi;
+  }
+  const size_t elem = dtype == MTLA_DTYPE_BF16 ? 2 : 4;
+  const int vec = (int)(16 / elem);
+  const bool half = cfg->layout == MTLA_ROPE_HALF;
+  bool use_vec = d % vec == 0 && (!half || (d / 2) % vec == 0);
+  for (int n = 0; n < n_tensors; ++n) {
+    const mtla_rope_tensor& t = tensors[n];
+    if (!t.x || !t.y || t.n_heads < 1 || t.width < 1 || t.first < 0 || !aligned(t.x, elem) || !aligned(t.y, elem))
+      return MTLA_ERR_INVALID_ARG;
+    if (t.x_token_stride < 0 || t.x_head_stride < 0 || t.y_token_stride < 0 || t.y_head_stride < 0)
+      return MTLA_ERR_INVALID_ARG;
+    if (t.first > t.width - d || (long long)t.n_heads * t.width > (1 << 24)) return MTLA_ERR_UNSUPPORTED_SHAPE;
+    // Rows of the result may not share elements, or their order would decide; in place means the same strides.
+    const bool one = n_tokens <= 1;
+    if ((t.n_heads > 1 && t.y_head_stride < t.width) ||
+        (!one && t.y_token_stride < t.width) ||
+        (!one && t.n_heads > 1 && t.y_token_stride < t.y_head_stride * (t.n_heads - 1) + t.width &&
+         t.y_head_stride < t.y_token_stride * ((long long)n_tokens - 1) + t.width))
+      return MTLA_ERR_INVALID_ARG;
+    if (t.x == t.y && ((!one && t.x_token_stride != t.y_token_stride) ||
+                       (t.n_heads > 1 && t.x_head_stride != t.y_head_stride)))
+      return MTLA_ERR_INVALID_ARG;
+    use_vec = use_vec && t.width % vec == 0 && t.first % vec == 0 && t.x_token_stride % vec == 0 &&
+              t.x_head_stride % vec == 0 && t.y_token_stride % vec == 0 && t.y_head_stride % vec == 0 &&
+              aligned(t.x, 16) && aligned(t.y, 16);
+  }
+  if (n_tokens == 0) return MTLA_OK;
+  long long elements = 0;
+  for (int n = 0; n < n_tensors; ++n) {
+    const mtla_rope_tensor& t = tensors[n];
+    const int v = use_vec ? vec : 1;
+    rp::Tensor& q = a.t[n];
+    q.x = t.x;
+    q.y = t.y;
+    q.x_token = t.x_token_stride;
+    q.x_head = t.x_head_stride;
+    q.y_token = t.y_token_stride;
+    q.y_head = t.y_head_stride;
+    q.heads = t.n_heads;
+    q.width = t.width;
+    q.first = t.first;
+    q.copy_units = (t.width - d) / v;
+    q.units = q.copy_units + (half ? d / 2 / v : (use_vec ? d / v : d / 2));
+    elements += (long long)t.n_heads * t.width;
+  }
+  a.positions = positions;
+  a.magnitude = magnitude;
+  a.n_tensors = n_tensors;
+  a.n_tokens = n_tokens;
+  a.pairs = d / 2;
+  a.inverse = inverse != 0;
+  OnDeviceOf dev(tensors[0].y);
+  if (dev.status() != MTLA_OK) return dev.status();
+  // Tokens per CTA: enough for two 16-byte units per thread, as long as every SM keeps several CTAs.
+  int per = 1;
+  while (per < rp::kMaxTokens && per * elements < 2ll * rp::kThreads * vec &&
+         (n_tokens + 2 * per - 1) / (2 * per) >= 4 * dev.sm_count())
+    per *= 2;
+  a.tokens_per_cta = per;
+  const dim3 grid(ceil_div(n_tokens, per));
+  auto pick = [&](auto bf, auto fp) { return dtype == MTLA_DTYPE_BF16 ? bf : fp; };
+  auto kernel = use_vec ? (half ? pick(rp::rope_kernel<bf16, true, true>, rp::rope_kernel<float, true, true>)
+                                : pick(rp::rope_kernel<bf16, true, false>, rp::rope_kernel<float, true, false>))
+                        : (half ? pick(rp::rope_kernel<bf16, false, true>, rp::rope_kernel<float, false, true>)
+                                : pick(rp::rope_kernel<bf16, false, false>, rp::rope_kernel<float, false, false>));
+  const cudaError_t e =
+      launch_kernel(kernel, grid, dim3(rp::kThreads), (size_t)0, static_cast<cudaStream_t>(stream), true, a);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e == cudaSuccess ? MTLA_OK : MTLA_ERR_CUDA;
+}
+
+// ---- the 4-bit pool
+
+size_t mtla_qpool_page_bytes(const mtla_qpool_config* cfg) {
+  return good_pool(cfg) ? (size_t)format_of(cfg).page_bytes() : 0;
+}
+
+int mtla_qpool_write(const mtla_qpool_config* cfg, void* pages, const void* rows, int64_t row_stride, int32_t dtype,
+                     const int64_t* index, int32_t n, void* stream) {
+  return row_call(cfg, pages, rows, row_stride, dtype, index, n, stream, true);
+}
+
+int mtla_qpool_read(const mtla_qpool_config* cfg, const void* pages, const int64_t* index, int32_t n, void* rows,
+                    int64_t row_stride, int32_t dtype, void* stream) {
+  return row_call(cfg, pages, rows, row_stride, dtype, index, n, stream, false);
+}
+
+size_t mtla_qpool_workspace_bytes(const mtla_qpool_config* cfg, int32_t B) {
+  return good_pool(cfg) && B >= 1 && B <= qp::kMaxBatch ? plan_attend(cfg, B).total : 0;
+}
+
+int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
+                      const int32_t* slots, int32_t B, const void* q, int32_t dtype, float scale, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!pages || !table || !slots || !q || !out || !workspace || B < 1 || table_width < 1 || !good_dtype(dtype) ||
+      !isfinite(scale))
+    return MTLA_ERR_INVALID_ARG;
+  if (!good_pool(cfg) || B > qp::kMaxBatch || (long long)B * table_width > 0x7fffffffll)
+    return MTLA_ERR_UNSUPPORTED_SHAPE;
+  if (!aligned(pages, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256) || !aligned(table, 4) ||
+      !aligned(slots, 4) || !aligned(lse, 4))
+    return MTLA_ERR_INVALID_ARG;
+  const AttnPlan p = plan_attend(cfg, B);
+  if (workspace_bytes < p.total) return MTLA_ERR_ARENA_TOO_SMALL;
+  OnDeviceOf dev(pages);
+  if (dev.status() != MTLA_OK) return dev.status();
+  char* ws = static_cast<char*>(workspace);
+  qp::AttnArgs a;
+  a.pages = static_cast<const uint8_t*>(pages);
+  a.table = table;
+  a.slots = slots;
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.o_part = reinterpret_cast<float*>(ws + p.o_part);
+  a.ml_part = reinterpret_cast<float*>(ws + p.ml_part);
+  a.seq_parts = reinterpret_cast<int2*>(ws + p.seq_parts);
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.n_heads = cfg->n_heads;
+  a.batch = B;
+  a.width = table_width;
+  a.n_pages = cfg->n_pages;
+  a.f = format_of(cfg);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool wide = cfg->n_heads > 16;
+  if (dtype == MTLA_DTYPE_BF16)
+    return wide ? launch_attend<bf16, 2>(a, dev, st) : launch_attend<bf16, 1>(a, dev, st);
+  return wide ? launch_attend<float, 2>(a, dev, st) : launch_attend<float, 1>(a, dev, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,225 @@
+// The 4-bit latent pool: page layout, element format, and the kernels that write and read rows.
+//
+// A page holds 64 slots in three blocks:
+//   codes   [64][r/2] bytes   two e2m1 codes per byte (sign, two exponent bits, one fraction bit:
+//                             0, 0.5, 1, 1.5, 2, 3, 4, 6), latent 2k in the low half of byte k
+//   scales  [64][r/32] bytes  one scale per group of 32 latents: bits 14..7 of a positive half-precision
+//                             number (5 exponent bits, 3 fraction bits), so decoding is a shift
+//   keys    [64][d_R] bf16    the RoPE key, unquantised
+// A latent is code * scale: 2 significant bits times 4, so it is exact in half precision and in
+// bf16, and no product that a kernel forms from it carries a rounding of the cache.  At r 512 /
+// d_R 64 a slot takes 256 + 16 + 128 = 400 bytes against 1152 in bf16.
+//
+// The 16-byte chunk c of row i lies at chunk position c ^ swizzle(i) of its row, so that eight
+// rows' equal chunks fall into different shared-memory banks after a plain copy of the page; the
+// key block's permutation is the one the tensor cores' 128-byte (64-byte) swizzle mode expects.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "sm100_ptx.cuh"
+
+namespace mtla {
+namespace qp {
+
+constexpr int kPageRows = 64;
+constexpr int kGroup = 32;
+constexpr float kScaleMax = 10240.f;   // six steps of it (61440) still fit half precision
+constexpr int kScaleNan = 0xff;
+
+struct Format {
+  int r, dr;
+  __host__ __device__ int code_row() const { return r / 2; }
+  __host__ __device__ int scale_row() const { return r / kGroup; }
+  __host__ __device__ int key_row() const { return 2 * dr; }
+  __host__ __device__ int off_scales() const { return 32 * r; }
+  __host__ __device__ int off_keys() const { return 34 * r; }
+  __host__ __device__ int page_bytes() const { return 34 * r + 128 * dr; }
+  // Chunk permutations (see the head of the file).
+  __host__ __device__ int code_mask() const {
+    const int n = r / kGroup, low = n & -n;
+    return (low < 8 ? low : 8) - 1;
+  }
+  __host__ __device__ int key_swizzle(int row) const { return dr == 64 ? (row & 7) : ((row >> 1) & 3); }
+};
+
+// Eight codes (32 bits) -> four half-precision pairs, in order.
+__device__ __forceinline__ void decode8(uint32_t w, uint32_t (&o)[4]) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
+      : "r"(w));
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// One scale byte in both halves; two scale bytes (lo, hi).
+__device__ __forceinline__ uint32_t scale_pair(uint32_t byte) { return (byte | (byte << 16)) << 7; }
+__device__ __forceinline__ uint32_t scale_pair(uint32_t lo, uint32_t hi) { return (lo | (hi << 16)) << 7; }
+
+// The smallest scale whose six steps reach `top` (a finite magnitude): 6 k q >= top with q the
+// grid's step at that size.  k * q and 6 * k * q are exact, so the two corrections make the
+// approximate quotient's ceiling exact.
+__device__ __forceinline__ float pick_scale(float top) {
+  const float t = top * (1.f / 6.f);
+  const uint32_t e = max(__float_as_uint(t) >> 23, 127u - 14u);         // exponent, at least 2^-14
+  const float q = __uint_as_float((e - 3u) << 23);
+  float k = ceilf(t * __uint_as_float((254u - (e - 3u)) << 23));        // t / q
+  if (6.f * ((k - 1.f) * q) >= top) k -= 1.f;
+  if (6.f * (k * q) < top) k += 1.f;
+  if (k > 16.f) k = 18.f;            // 17 q is off the grid: past 16 q its step is 2 q
+  return fminf(k * q, kScaleMax);
+}
+
+struct RowArgs {
+  uint8_t* pages;
+  const int64_t* index;      // pool row (page * 64 + slot) of every row; outside the pool: skipped
+  void* rows;                // [n][r + d_R], row_stride elements apart
+  long long row_stride;
+  long long pool_rows;
+  int n;
+  Format f;
+};
+
+constexpr int kRowThreads = 256;
+
+// A unit is 16 elements: half a group, so the two threads of a group are neighbours (a row has an
+// even number of units).  Both kernels are bound by the bytes of the wide rows.
+template <typename T>
+__device__ __forceinline__ void load16(const T* p, float (&x)[16]) {
+  constexpr int V = Elem<T>::kVec;
+#pragma unroll
+  for (int i = 0; i < 16 / V; ++i) {
+    float v[V];
+    load_vec(p + i * V, v);
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[i * V + j] = v[j];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store16(T* p, const float (&x)[16]) {
+  constexpr int V = Elem<T>::kVec;
+#pragma unroll
+  for (int i = 0; i < 16 / V; ++i) {
+    float v[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = x[i * V + j];
+    store_vec(p + i * V, v);
+  }
+}
+
+// Rows into the pool.  The code of x at scale s is the nearest one, the even one on a tie, found by
+// comparing |x| with the borders 0.25 s .. 5 s, which are exact in fp32: no quotient, hence no
+// rounding that could move a value across a border.  A group with an infinity or a NaN gets a NaN scale.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) qpool_write_kernel(RowArgs a) {
+  const int units = (a.f.r + a.f.dr) / 16, lat_units = a.f.r / 16;
+  const long long total = (long long)a.n * units;
+  for (long long w = (long long)blockIdx.x * kRowThreads + threadIdx.x; w - (threadIdx.x & 31) < total;
+       w += (long long)gridDim.x * kRowThreads) {
+    const bool in = w < total;
+    const int n = in ? (int)(w / units) : 0, u = in ? (int)(w - (long long)n * units) : 0;
+    const long long at = in ? a.index[n] : -1;
+    const bool keep = at >= 0 && at < a.pool_rows;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    if (keep) load16(static_cast<const T*>(a.rows) + n * a.row_stride + u * 16, x);
+    uint32_t top = 0;                              // magnitudes order like their bits; NaN on top
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    if (!keep) continue;
+    uint8_t* page = a.pages + (at >> 6) * a.f.page_bytes();
+    const int row = (int)(at & 63);
+    if (u < lat_units) {
+      const bool finite = top < 0x7f800000u;
+      const float s = finite ? pick_scale(__uint_as_float(top)) : 0.f;
+      const float b0 = 0.25f * s, b1 = 0.75f * s, b2 = 1.25f * s, b3 = 1.75f * s, b4 = 2.5f * s, b5 = 3.5f * s,
+                  b6 = 5.f * s;
+      uint32_t code[2] = {0u, 0u};
+      if (s > 0.f) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float v = fabsf(x[i]);
+          uint32_t c = (v > b0) + (v >= b1) + (v > b2) + (v >= b3) + (v > b4) + (v >= b5) + (v > b6);
+          c |= (__float_as_uint(x[i]) >> 28) & 8u;
+          code[i >> 3] |= c << (4 * (i & 7));
+        }
+      }
+      const int chunk = (u >> 1) ^ (row & a.f.code_mask());
+      *reinterpret_cast<uint2*>(page + row * a.f.code_row() + chunk * 16 + (u & 1) * 8) = make_uint2(code[0], code[1]);
+      if (!(u & 1))
+        page[a.f.off_scales() + row * a.f.scale_row() + (u >> 1)] =
+            finite ? (uint8_t)(__half_as_ushort(__float2half_rn(s)) >> 7) : (uint8_t)kScaleNan;
+    } else {
+      const int c0 = (u - lat_units) * 2, sw = a.f.key_swizzle(row);
+      uint8_t* keys = page + a.f.off_keys() + row * a.f.key_row();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = x[h * 8 + j];
+        store_vec(reinterpret_cast<bf16*>(keys + ((c0 + h) ^ sw) * 16), v);
+      }
+    }
+  }
+}
+
+// Rows out of the pool, widened to T (exact in both types); zeros where the index is outside the pool.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) qpool_read_kernel(RowArgs a) {
+  const int units = (a.f.r + a.f.dr) / 16, lat_units = a.f.r / 16;
+  const long long total = (long long)a.n * units;
+  for (long long w = (long long)blockIdx.x * kRowThreads + threadIdx.x; w < total;
+       w += (long long)gridDim.x * kRowThreads) {
+    const int n = (int)(w / units), u = (int)(w - (long long)n * units);
+    const long long at = a.index[n];
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    if (at >= 0 && at < a.pool_rows) {
+      const uint8_t* page = a.pages + (at >> 6) * a.f.page_bytes();
+      const int row = (int)(at & 63);
+      if (u < lat_units) {
+        const int chunk = (u >> 1) ^ (row & a.f.code_mask());
+        const uint2 code = *reinterpret_cast<const uint2*>(page + row * a.f.code_row() + chunk * 16 + (u & 1) * 8);
+        const uint32_t s = scale_pair(page[a.f.off_scales() + row * a.f.scale_row() + (u >> 1)]);
+        const uint32_t words[2] = {code.x, code.y};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t o[4];
+          decode8(words[k], o);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t v = mul_h2(o[i], s);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
+            x[k * 8 + 2 * i] = f.x;
+            x[k * 8 + 2 * i + 1] = f.y;
+          }
+        }
+      } else {
+        const int c0 = (u - lat_units) * 2, sw = a.f.key_swizzle(row);
+        const uint8_t* keys = page + a.f.off_keys() + row * a.f.key_row();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[8];
+          load_vec(reinterpret_cast<const bf16*>(keys + ((c0 + h) ^ sw) * 16), v);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[h * 8 + j] = v[j];
+        }
+      }
+    }
+    store16(static_cast<T*>(a.rows) + n * a.row_stride + u * 16, x);
+  }
+}
+
+}  // namespace qp
+}  // namespace mtla

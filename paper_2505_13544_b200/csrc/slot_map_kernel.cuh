@@ -1,0 +1,171 @@
+// Block tables and slot maps from request lengths, on the GPU in one launch.
+//
+// With h_b tokens held and f_b new ones, request b ends with ceil((h_b + f_b) / s) slots and needs
+// ceil(slots / 64) - ceil(ceil(h_b / s) / 64) more pages, which it takes from the free list in
+// request order.  Every CTA forms the two prefix sums (new tokens, new pages) over the whole batch
+// by itself, which costs less than a second launch or a grid-wide wait (a batch is at most a few
+// thousand pairs of integers out of L2), and then fills its share of the token arrays.  The table
+// entries of new pages follow from the prefix sums, so no CTA reads what another writes.
+#pragma once
+
+#include "common.cuh"
+#include "sm100_ptx.cuh"
+
+namespace mtla {
+namespace sm {
+
+constexpr int kThreads = 256;
+constexpr int kMaxBatch = 16384;       // two prefix sums in shared memory
+constexpr int kPage = 64;
+constexpr int kPerThread = 4;          // consecutive tokens of a thread: 16-byte stores
+
+struct Args {
+  const int* held;
+  const int* fresh;
+  int* table;                // [batch][width]
+  const int* free_pages;
+  int *starts, *seq, *position;
+  long long *slot, *store;
+  int *slots, *taken;
+  int batch, stride, width, n_free, n_tokens;
+  int vec;                   // the token arrays are 16-byte aligned
+};
+
+// Pages that hold `tokens` tokens (64-bit: counts go up to 2^31 - 1).
+__device__ __forceinline__ int pages_of(long long tokens, int stride) {
+  return (int)(((tokens + stride - 1) / stride + kPage - 1) / kPage);
+}
+
+__global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
+  extern __shared__ int smem[];
+  int* s_start = smem;                   // [batch + 1] first token of every request
+  int* s_page = smem + a.batch + 1;      // [batch + 1] first new page of every request
+  __shared__ long long warp_tok[kThreads / 32], warp_page[kThreads / 32];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) s_bad = 0;
+  __syncthreads();
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+
+  const int per = ceil_div(a.batch, kThreads);
+  const int lo = min(a.batch, tid * per), hi = min(a.batch, lo + per);
+  long long tok = 0, page = 0;
+  bool bad = false;
+  for (int b = lo; b < hi; ++b) {
+    const long long h = a.held[b], f = a.fresh[b];
+    const bool ok = h >= 0 && f >= 0 && h + f <= 0x7fffffffll;
+    const int have = ok ? pages_of(h, a.stride) : 0;
+    const int want = ok ? pages_of(h + f, a.stride) : 0;
+    bad |= !ok || want > a.width;
+    s_start[b] = ok ? (int)f : 0;        // for now the counts
+    s_page[b] = want - have;
+    tok += ok ? f : 0;
+    page += want - have;
+  }
+  long long tok_in = tok, page_in = page;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long t = __shfl_up_sync(0xffffffffu, tok_in, o), p = __shfl_up_sync(0xffffffffu, page_in, o);
+    if (lane >= o) { tok_in += t; page_in += p; }
+  }
+  if (lane == 31) { warp_tok[warp] = tok_in; warp_page[warp] = page_in; }
+  if (bad) s_bad = 1;
+  __syncthreads();
+  long long tok_at = tok_in - tok, page_at = page_in - page, n_tok = 0, n_page = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) { tok_at += warp_tok[w]; page_at += warp_page[w]; }
+    n_tok += warp_tok[w];
+    n_page += warp_page[w];
+  }
+  // A batch that does not fit is refused as a whole: no page is taken, no token gets a slot.
+  const bool refuse = s_bad || n_tok > a.n_tokens || n_page > a.n_free;
+  for (int b = lo; b < hi; ++b) {
+    const int t = s_start[b], p = s_page[b];
+    s_start[b] = refuse ? 0 : (int)tok_at;
+    s_page[b] = refuse ? 0 : (int)page_at;
+    tok_at += t;
+    page_at += p;
+  }
+  if (tid == 0) {
+    s_start[a.batch] = refuse ? 0 : (int)n_tok;
+    s_page[a.batch] = refuse ? 0 : (int)n_page;
+  }
+  __syncthreads();
+  const int total = s_start[a.batch];
+
+  // Per request: offsets, slot counts, the new entries of its table row (a warp per request).
+  for (int b = blockIdx.x * (kThreads / 32) + warp; b < a.batch; b += gridDim.x * (kThreads / 32)) {
+    const int h = max(a.held[b], 0);
+    const int have = pages_of(h, a.stride), p0 = s_page[b], n_new = s_page[b + 1] - p0;
+    if (lane == 0) {
+      a.starts[b] = s_start[b];
+      a.slots[b] = (int)(((long long)h + (s_start[b + 1] - s_start[b]) + a.stride - 1) / a.stride);
+    }
+    for (int i = lane; i < n_new; i += 32) a.table[(long long)b * a.width + have + i] = a.free_pages[p0 + i];
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    a.starts[a.batch] = total;
+    a.taken[0] = refuse ? -1 : (int)n_page;
+  }
+
+  // Per token.
+  for (long long t0 = ((long long)blockIdx.x * kThreads + tid) * kPerThread; t0 < a.n_tokens;
+       t0 += (long long)gridDim.x * kThreads * kPerThread) {
+    int seq[kPerThread], pos[kPerThread];
+    long long slot[kPerThread], store[kPerThread];
+    int b = 0;
+    if (t0 < total) {                              // the last request that starts at or before t0
+      int lo_b = 0, hi_b = a.batch;
+      while (hi_b - lo_b > 1) {
+        const int mid = (lo_b + hi_b) >> 1;
+        if (s_start[mid] <= t0) lo_b = mid; else hi_b = mid;
+      }
+      b = lo_b;
+    }
+    int held = t0 < total ? a.held[b] : 0, page_of = -1;
+    long long page = 0;
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      const long long t = t0 + i;
+      seq[i] = -1; pos[i] = 0; slot[i] = -1; store[i] = -1;
+      if (t >= total) continue;
+      while (s_start[b + 1] <= t) {                // requests without new tokens are stepped over
+        ++b;
+        held = a.held[b];
+        page_of = -1;
+      }
+      const int p = held + (int)(t - s_start[b]);
+      const int j = p / a.stride;
+      if (page_of != j >> 6) {
+        page_of = j >> 6;
+        const int have = pages_of(held, a.stride);
+        page = page_of < have ? a.table[(long long)b * a.width + page_of] : a.free_pages[s_page[b] + page_of - have];
+      }
+      seq[i] = b;
+      pos[i] = p;
+      slot[i] = page * kPage + (j & 63);
+      const bool last = p - j * a.stride == a.stride - 1 || t + 1 == s_start[b + 1];
+      store[i] = last ? slot[i] : -1;
+    }
+    if (a.vec && t0 + kPerThread <= a.n_tokens) {
+      *reinterpret_cast<int4*>(a.seq + t0) = make_int4(seq[0], seq[1], seq[2], seq[3]);
+      *reinterpret_cast<int4*>(a.position + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      *reinterpret_cast<longlong2*>(a.slot + t0) = make_longlong2(slot[0], slot[1]);
+      *reinterpret_cast<longlong2*>(a.slot + t0 + 2) = make_longlong2(slot[2], slot[3]);
+      *reinterpret_cast<longlong2*>(a.store + t0) = make_longlong2(store[0], store[1]);
+      *reinterpret_cast<longlong2*>(a.store + t0 + 2) = make_longlong2(store[2], store[3]);
+    } else {
+      for (int i = 0; i < kPerThread && t0 + i < a.n_tokens; ++i) {
+        a.seq[t0 + i] = seq[i];
+        a.position[t0 + i] = pos[i];
+        a.slot[t0 + i] = slot[i];
+        a.store[t0 + i] = store[i];
+      }
+    }
+  }
+}
+
+}  // namespace sm
+}  // namespace mtla
