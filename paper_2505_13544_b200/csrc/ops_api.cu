@@ -9,6 +9,7 @@
 
 #include "common.cuh"
 #include "qpool_attn.cuh"
+#include "qpool_attn_tc.cuh"
 #include "qpool_format.cuh"
 #include "rope_kernel.cuh"
 #include "slot_map_kernel.cuh"
@@ -111,38 +112,70 @@ constexpr int kAttnCtasPerSm = 2;
 constexpr int kPlanSms = 148;
 constexpr int kPlanCtas = kAttnCtasPerSm * kPlanSms;
 
-struct AttnPlan { size_t o_part, ml_part, seq_parts, total; };
+struct AttnPlan { size_t o_part, ml_part, seq_parts, q_image, q_unit, error_word, total; };
+int padded_heads(int n) { return n <= 16 ? 16 : 32; }
 AttnPlan plan_attend(const mtla_qpool_config* c, int B) {
   AttnPlan p;
   const size_t parts = (size_t)B + kPlanCtas;
   p.o_part = 0;
   p.ml_part = align_up(parts * c->n_heads * c->latent_rank * 4, 256);
   p.seq_parts = p.ml_part + align_up(parts * c->n_heads * 8, 256);
-  p.total = p.seq_parts + align_up((size_t)B * 8, 256);
+  p.q_image = p.seq_parts + align_up((size_t)B * 8, 256);
+  p.q_unit = p.q_image + align_up((size_t)B * padded_heads(c->n_heads) * 2 * (c->latent_rank + c->rope_dim), 256);
+  p.error_word = p.q_unit + align_up((size_t)B * 32 * 4, 256);
+  p.total = p.error_word + 256;
   return p;
 }
 
+// Launches `kernel` as a dependent of what runs before it on the stream.
+template <typename K, typename... Args>
+int launch_dependent(K* kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+  if (launch_kernel(kernel, grid, dim3(threads), smem, st, true, args...) == cudaSuccess) return MTLA_OK;
+  cudaGetLastError();
+  return MTLA_ERR_CUDA;
+}
+
+template <typename T>
+int launch_combine(const qp::AttnArgs& a, cudaStream_t st) {
+  const int pieces = ceil_div(a.n_heads * a.f.r, qp::kCombineThreads * 4);
+  return launch_dependent(qp::qpool_combine_kernel<T>, dim3(pieces, a.batch), qp::kCombineThreads, 0, st, a);
+}
+
 template <typename T, int MH>
-int launch_attend(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
+int launch_attend(qp::AttnArgs a, const OnDeviceOf& dev, cudaStream_t st) {
   using L = qp::AttnLayout<MH, sizeof(T) == 2 ? 1 : 2>;
   if (!raise_smem<qp::qpool_attend_kernel<T, MH>>(dev.device())) return MTLA_ERR_CUDA;
+  a.error_word = nullptr;                    // this kernel has no wait that could run out
   const int smem = L::bytes(a.f, a.batch);
   const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
   const int per_sm = smem <= 112 * 1024 ? kAttnCtasPerSm : 1;
   const long long most = (long long)a.batch * a.width;
   const int ctas = (int)(most < (long long)per_sm * sms ? most : (long long)per_sm * sms);
-  if (launch_kernel(qp::qpool_attend_kernel<T, MH>, dim3(ctas), dim3(qp::kAttnThreads), (size_t)smem, st, true, a) !=
-      cudaSuccess) {
-    cudaGetLastError();
-    return MTLA_ERR_CUDA;
+  const int status = launch_dependent(qp::qpool_attend_kernel<T, MH>, dim3(ctas), qp::kAttnThreads, smem, st, a);
+  return status == MTLA_OK ? launch_combine<T>(a, st) : status;
+}
+
+template <int NHP, int NB>
+int launch_attend_tc(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
+  if (!raise_smem<qp::qpool_attend_tc_kernel<NHP, NB>>(dev.device())) return MTLA_ERR_CUDA;
+  const qp::tc::Layout l(a.f, NHP, a.batch);
+  const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
+  const long long most = (long long)a.batch * ceil_div(a.width, 2);
+  const int ctas = (int)(most < sms ? most : sms);
+  int status = launch_dependent(qp::qpool_query_kernel<NHP>, dim3(NHP / (qp::kQueryThreads / 32), a.batch),
+                                qp::kQueryThreads, 0, st, a);
+  if (status == MTLA_OK)
+    status = launch_dependent(qp::qpool_attend_tc_kernel<NHP, NB>, dim3(ctas), qp::tc::kThreads, l.total, st, a);
+  return status == MTLA_OK ? launch_combine<bf16>(a, st) : status;
+}
+template <int NHP>
+int launch_attend_tc(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
+  switch (ceil_div(a.f.r, 128)) {
+    case 1: return launch_attend_tc<NHP, 1>(a, dev, st);
+    case 2: return launch_attend_tc<NHP, 2>(a, dev, st);
+    case 3: return launch_attend_tc<NHP, 3>(a, dev, st);
+    default: return launch_attend_tc<NHP, 4>(a, dev, st);
   }
-  const int pieces = ceil_div(a.n_heads * a.f.r, qp::kCombineThreads * 4);
-  if (launch_kernel(qp::qpool_combine_kernel<T>, dim3(pieces, a.batch), dim3(qp::kCombineThreads), (size_t)0, st,
-                    true, a) != cudaSuccess) {
-    cudaGetLastError();
-    return MTLA_ERR_CUDA;
-  }
-  return MTLA_OK;
 }
 
 }  // namespace
@@ -354,7 +387,12 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
   a.n_pages = cfg->n_pages;
   a.f = format_of(cfg);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  a.q_image = reinterpret_cast<uint8_t*>(ws + p.q_image);
+  a.q_unit = reinterpret_cast<float*>(ws + p.q_unit);
+  a.error_word = reinterpret_cast<int*>(ws + p.error_word);
   const bool wide = cfg->n_heads > 16;
+  if (dtype == MTLA_DTYPE_BF16 && B <= qp::tc::kMaxBatch)
+    return wide ? launch_attend_tc<32>(a, dev, st) : launch_attend_tc<16>(a, dev, st);
   if (dtype == MTLA_DTYPE_BF16)
     return wide ? launch_attend<bf16, 2>(a, dev, st) : launch_attend<bf16, 1>(a, dev, st);
   return wide ? launch_attend<float, 2>(a, dev, st) : launch_attend<float, 1>(a, dev, st);

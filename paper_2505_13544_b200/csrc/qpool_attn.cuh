@@ -37,8 +37,11 @@ struct AttnArgs {
   void* out;                 // [batch][n_heads][r]
   float* lse;                // [batch][n_heads] or nullptr
   float* o_part;             // [batch + ctas][n_heads][r]
-  float* ml_part;            // [batch + ctas][n_heads][2]: reference maximum (log2 units), denominator
+  float* ml_part;            // [batch + ctas][n_heads][2]: reference (log2 units) of the sums, denominator
   int2* seq_parts;           // [batch] first part, number of parts (0: finished by one CTA)
+  uint8_t* q_image;          // tensor-core kernel: [batch] queries as its shared memory holds them
+  float* q_unit;             // tensor-core kernel: [batch][32] scale of a head's scores
+  int* error_word;           // tensor-core kernel: a bounded wait gave up
   float scale_log2;          // scale * log2(e)
   int n_heads, batch, width, n_pages;
   Format f;
@@ -112,7 +115,8 @@ __device__ __forceinline__ void decode_pairs(uint32_t w, uint32_t (&o)[4]) {
       : "r"(e), "r"(d));
 }
 
-// Prefix sums of the sequences' tile counts into prefix[0 .. batch]; returns the total.
+// Prefix sums of the sequences' tile counts (PAGES pages each) into prefix[0 .. batch]; returns the total.
+template <int PAGES>
 __device__ inline long long tile_prefix(const AttnArgs& a, int* prefix, int* warp_sums, int threads) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = ceil_div(a.batch, threads);
@@ -120,7 +124,8 @@ __device__ inline long long tile_prefix(const AttnArgs& a, int* prefix, int* war
   int sum = 0;
   for (int b = lo; b < hi; ++b) {
     // A count past the table's width is cut to it; a negative one is no slot at all.
-    const int t = min(max(a.slots[b], 0) / kPageRows + (max(a.slots[b], 0) % kPageRows != 0), a.width);
+    const int n = max(a.slots[b], 0);
+    const int pages = min(n / kPageRows + (n % kPageRows != 0), a.width), t = (pages + PAGES - 1) / PAGES;
     prefix[b + 1] = t;
     sum += t;
   }
@@ -200,7 +205,7 @@ __global__ void __launch_bounds__(kAttnThreads) qpool_attend_kernel(AttnArgs a) 
 
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const long long total = tile_prefix(a, prefix, warp_sums, kAttnThreads);
+  const long long total = tile_prefix<1>(a, prefix, warp_sums, kAttnThreads);
   if (total == 0) return;
   // With fewer tiles than CTAs the rest stays out, so that every share has a tile and the parts of
   // a sequence follow one another without a gap.
@@ -471,7 +476,7 @@ __global__ void __launch_bounds__(kAttnThreads) qpool_attend_kernel(AttnArgs a) 
         if (whole) {
           if (a.lse) a.lse[(long long)b * a.n_heads + tid] = (m_s[tid] - kProbShift + log2f(l_s[tid])) * 0.69314718055994531f;
         } else {
-          a.ml_part[((long long)part * a.n_heads + tid) * 2] = m_s[tid];
+          a.ml_part[((long long)part * a.n_heads + tid) * 2] = m_s[tid] - kProbShift;
           a.ml_part[((long long)part * a.n_heads + tid) * 2 + 1] = l_s[tid];
         }
       }
@@ -489,6 +494,12 @@ __global__ void __launch_bounds__(kCombineThreads) qpool_combine_kernel(AttnArgs
   const int e = (blockIdx.x * kCombineThreads + threadIdx.x) * 4;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
+  if (a.error_word && *a.error_word) {   // a bounded wait gave up: no result that looks like one
+    if (e < a.n_heads * r)
+      for (int i = 0; i < 4; ++i)
+        static_cast<T*>(a.out)[(long long)b * a.n_heads * r + e + i] = Elem<T>::from_float(NAN);
+    return;
+  }
   const bool empty = a.slots[b] <= 0;
   const int2 parts = empty ? make_int2(0, 1) : a.seq_parts[b];
   if (parts.y == 0 || e >= a.n_heads * r) return;
@@ -512,7 +523,7 @@ __global__ void __launch_bounds__(kCombineThreads) qpool_combine_kernel(AttnArgs
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] /= l;
-    lse = (m - kProbShift + log2f(l)) * 0.69314718055994531f;
+    lse = (m + log2f(l)) * 0.69314718055994531f;
   }
   if constexpr (sizeof(T) == 4) {
     store_vec(out, v);
