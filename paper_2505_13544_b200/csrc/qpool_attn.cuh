@@ -100,13 +100,15 @@ __device__ __forceinline__ void cp_async_wait() {
 }
 
 // A thread's register of the transposing load holds codes (4g .. 4g + 3) of slot 2t in its low half
-// and of slot 2t + 1 in its high half.  o[j] = half-precision pair (slot 2t, slot 2t + 1) of latent 4g + j.
+// and of slot 2t + 1 in its high half.  o[j] = half-precision pair (slot 2t, slot 2t + 1) of latent
+// 4g + j.  The pairs are gathered in the upper half with left shifts, which run beside the ALU pipe that
+// the conversions and the selections share.
 __device__ __forceinline__ void decode_pairs(uint32_t w, uint32_t (&o)[4]) {
-  const uint32_t e = (w & 0x0f0fu) | ((w >> 12) & 0xf0f0u);          // latents 0 and 2
-  const uint32_t d = ((w >> 4) & 0x0f0fu) | ((w >> 16) & 0xf0f0u);   // latents 1 and 3
+  const uint32_t e = ((w << 16) & 0x0f0f0000u) | ((w << 4) & 0xf0f00000u);     // latents 0 and 2
+  const uint32_t d = ((w << 12) & 0x0f0f0000u) | (w & 0xf0f00000u);            // latents 1 and 3
   asm("{\n\t.reg .b8 a, b, c, d, x, y;\n\t"
-      "mov.b32 {a, b, x, y}, %4;\n\t"
-      "mov.b32 {c, d, x, y}, %5;\n\t"
+      "mov.b32 {x, y, a, b}, %4;\n\t"
+      "mov.b32 {x, y, c, d}, %5;\n\t"
       "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
       "cvt.rn.f16x2.e2m1x2 %1, c;\n\t"
       "cvt.rn.f16x2.e2m1x2 %2, b;\n\t"

@@ -24,13 +24,13 @@
 // Queries arrive as an image of the B operand that qpool_query_kernel has written (half precision
 // scaled by a power of two per head, swizzled), so that a segment's query is one bulk copy.
 //
-// Roles (28 warps): warps 0-3 score issuers, one per 128 latents, each with its own accumulator
-// (one thread issues a matrix instruction about every hundred cycles, several times slower than
-// these execute); warp 4 producer; warps 5-6 value issuers; warps 8-11 expansion for the scores;
-// warps 12-19 for the values, a page of the tile each four; warps 20-27 softmax and epilogue.
-// The online softmax raises a head's reference only when a tile exceeds it by 2^8, found by a flag that is
-// collected while the probabilities are already being formed.  Probabilities are kept times 2^7:
-// with the 2^8 they stay inside half precision.
+// Roles (28 warps): warps 0-1 score issuers and 2-3 value issuers, one thread each (a thread issues a
+// matrix instruction about every 50 cycles, these execute in 16), warp 4 producer, warps 8-11
+// expansion for the scores, 12-19 for the values (four warps a page of the tile), 20-27 softmax and
+// epilogue.  The hot loops are short on purpose: with five kinds of code on every scheduler, fetching
+// unrolled instructions was the longest stall.
+// The online softmax raises a head's reference only when a tile exceeds it by 2^8.  Probabilities
+// are kept times 2^7: with the 2^8 they stay inside half precision.
 //
 // Every wait is bounded; after a time-out the roles unwind and qpool_combine_kernel answers with NaN.
 #pragma once
@@ -45,15 +45,22 @@ constexpr int kTile = 128;                  // slots per tile: two pages
 constexpr int kThreads = 896;
 constexpr int kStages = 3;
 constexpr int kMaxBatch = 1022;             // prefix sums kept in shared memory
-constexpr int kProducerWarp = 4, kFirstValueIssuer = 5, kValueIssuers = 2;
+constexpr int kProducerWarp = 4, kScoreIssuer0 = 0, kValueIssuer0 = 2;
 constexpr int kScoreWarp0 = 8, kScoreWarps = 4, kValueWarp0 = 12, kValueWarps = 8;
-constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256;
-constexpr int kInfo = 8;                    // ring of tile descriptions, deeper than any role's lag
-// TMEM columns: four score accumulators, four output blocks, two operand buffers each.
+constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
+constexpr int kInfo = 16;                   // ring of tile descriptions, deeper than any role's lag
+// TMEM columns: two score accumulators, up to four output blocks of NHP columns, two operand
+// buffers of 64 columns for the scores and what is left, three (32 heads) or four, for the values.
 constexpr int kTmemCols = 512;
-constexpr int kColS = 0, kColO = 128, kColAs = 256, kColAv = 384;
+constexpr int kColS = 0, kColO = 64, kMaxAv = 4;
+__host__ __device__ constexpr int col_as(int nhp) { return kColO + 4 * nhp; }
+__host__ __device__ constexpr int col_av(int nhp) { return col_as(nhp) + 128; }
+__host__ __device__ constexpr int av_buffers(int nhp) { return nhp == 32 ? 3 : 4; }
+static_assert(col_av(32) + 64 * av_buffers(32) <= kTmemCols && col_av(16) + 64 * av_buffers(16) <= kTmemCols,
+              "tensor memory budget");
 constexpr float kShift = 7.f, kRescale = 8.f;
-constexpr int kRegsIssuer = 40, kRegsWorker = 80;
+constexpr float kUnset = 3e38f;             // in the place of -reference: any score then exceeds it
+constexpr int kRegsIssuer = 32, kRegsWorker = 88;
 constexpr int kRegsAtLaunch = 65536 / kThreads / 8 * 8;
 static_assert(256 * kRegsIssuer + (kThreads - 256) * kRegsWorker <= kThreads * kRegsAtLaunch,
               "register re-allocation exceeds the CTA's pool");
@@ -66,17 +73,19 @@ struct TileInfo {
 
 struct Misc {
   unsigned long long raw_full[kStages], raw_empty[kStages], scale_full[kStages];
-  // Operand buffers: "empty" per buffer; "full" per quarter of r and parity of the tile, so that its
-  // one reader sees every phase and the writers, two buffers ahead at most, never lead by two.
-  unsigned long long as_full[2][4], as_empty[2], av_full[2][4], av_empty[2];
+  // Operand buffers.  Both issuers of a product wait for every buffer and hand every buffer back (the
+  // one that reads it through its commit), so that nobody can miss a phase.
+  unsigned long long as_full[2], as_empty[2], av_full[kMaxAv], av_empty[kMaxAv];
   unsigned long long s_full, s_empty, p_full[2], p_empty[2], q_full, q_empty;
-  unsigned long long info_full[kInfo], flag_bar[2], group_sync;
+  unsigned long long info_full[kInfo];
   uint32_t tmem_base;
   int abort_word;
-  int exceed_flag[2];
   int warp_sums[32];
   TileInfo info[kInfo];
-  float m_used[32], unit[32], fac[32];
+  float m_used[32];          // reference maximum (log2 units), minus infinity before the first score
+  alignas(16) float neg_ref[32];   // shift - reference: what a score is offset by
+  alignas(16) float unit[32];      // scale of the head's scores
+  float fac[32];
   float red[8][16];
 };
 static_assert(sizeof(Misc) <= 2048, "misc region too small");
@@ -162,6 +171,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   constexpr uint32_t IDESC_S = make_idesc_f16(128, NHP, 0, 0), IDESC_K = make_idesc_bf16(128, NHP, 0, 0);
   constexpr uint32_t IDESC_V = make_idesc_f16(128, NHP, 0, 1);
   constexpr uint32_t P_BYTES = kTile * NHP * 2, P_SBO = kTile * 16;   // bytes between groups of 8 heads
+  constexpr int ISSUERS = NB > 1 ? 2 : 1;                             // of each product
+  constexpr int AVB = av_buffers(NHP), COL_AS = col_as(NHP), COL_AV = col_av(NHP);
   extern __shared__ uint8_t smem_raw[];
   const Format f = a.f;
   const int r = f.r, dr = f.dr;
@@ -177,29 +188,24 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(bar(misc->raw_full[i]), 1);
-      mbar_init(bar(misc->raw_empty[i]), kScoreWarps + kValueWarps + NB);
+      mbar_init(bar(misc->raw_empty[i]), kScoreWarps + kValueWarps + ISSUERS);
       mbar_init(bar(misc->scale_full[i]), kScoreWarps);
     }
-    for (int i = 0; i < 4; ++i) {
-      for (int j = 0; j < 2; ++j) {
-        mbar_init(bar(misc->as_full[j][i]), kScoreWarps);
-        mbar_init(bar(misc->av_full[j][i]), kValueWarps);
-      }
-    }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(misc->as_empty[i]), 1);
-      mbar_init(bar(misc->av_empty[i]), 1);
-      mbar_init(bar(misc->p_full[i]), kSoftmaxThreads);
-      mbar_init(bar(misc->p_empty[i]), kValueIssuers);
-      mbar_init(bar(misc->flag_bar[i]), kSoftmaxThreads);
-      misc->exceed_flag[i] = 0;
+      mbar_init(bar(misc->as_full[i]), kScoreWarps);
+      mbar_init(bar(misc->as_empty[i]), ISSUERS);
+      mbar_init(bar(misc->p_full[i]), kSoftmaxWarps);
+      mbar_init(bar(misc->p_empty[i]), ISSUERS);
+    }
+    for (int i = 0; i < kMaxAv; ++i) {
+      mbar_init(bar(misc->av_full[i]), kValueWarps);
+      mbar_init(bar(misc->av_empty[i]), ISSUERS);
     }
     for (int i = 0; i < kInfo; ++i) mbar_init(bar(misc->info_full[i]), 1);
-    mbar_init(bar(misc->s_full), NB);
-    mbar_init(bar(misc->s_empty), kSoftmaxThreads);
+    mbar_init(bar(misc->s_full), ISSUERS);
+    mbar_init(bar(misc->s_empty), kSoftmaxWarps);
     mbar_init(bar(misc->q_full), 1);
-    mbar_init(bar(misc->q_empty), NB);
-    mbar_init(bar(misc->group_sync), kSoftmaxThreads);
+    mbar_init(bar(misc->q_empty), ISSUERS);
     misc->abort_word = 0;
     mbar_fence_init();
   }
@@ -220,9 +226,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   }
   const int n_tiles = g1 - g0;
   const uint32_t q_u32 = base + L.off_q, p_u32 = base + L.off_p, st_u32 = base + L.off_st;
-  auto stage_of = [&](int n) { return base + (n % kStages) * L.stage; };
   auto wait = [&](unsigned long long& b, int phase, int code) {
-    return mbar_wait(bar(b), phase & 1, abort_word, a.error_word, code);
+    return mbar_wait_compact(bar(b), phase & 1, abort_word, a.error_word, code);
   };
 
   if (n_tiles == 0) {
@@ -231,13 +236,12 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     reg_dealloc<kRegsIssuer>();
     if (warp == kProducerWarp && lane == 0) {
       // ---------------------------------------------------------------- producer
-      int b = find_seq(prefix, a.batch, g0), seg = 0;
+      int b = find_seq(prefix, a.batch, g0), seg = 0, st = 0, round = 0;
       for (int n = 0; n < n_tiles; ++n) {
         const int g = g0 + n;
         while (prefix[b + 1] <= g) ++b;
         const int tile = g - prefix[b], slots = a.slots[b];
         const bool first = n == 0 || tile == 0, last = n + 1 == n_tiles || g + 1 == prefix[b + 1];
-        const int st = n % kStages;
         int page[2], rows[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -245,7 +249,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           page[i] = have > 0 && t < a.width ? __ldg(a.table + (long long)b * a.width + t) : -1;
           rows[i] = page[i] >= 0 && page[i] < a.n_pages ? min(have, kPageRows) : 0;
         }
-        if (!wait(misc->raw_empty[st], (n / kStages) + 1, 1)) break;
+        if (!wait(misc->raw_empty[st], round + 1, 1)) break;
         TileInfo& info = misc->info[n % kInfo];
         info.b = b;
         info.flags = (first ? 1 : 0) | (last ? 2 : 0);
@@ -256,16 +260,16 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           bytes += rows[i] * (f.code_row() + f.key_row()) + (rows[i] * f.scale_row() + 15) / 16 * 16;
-        const uint32_t full = bar(misc->raw_full[st]), dst = stage_of(n);
+        const uint32_t full = bar(misc->raw_full[st]), dst = base + st * L.stage;
         mbar_arrive_expect_tx(full, bytes);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if (rows[i] == 0) continue;
           const uint8_t* src = a.pages + (long long)page[i] * f.page_bytes();
-          bulk_load(dst + L.keys + i * kPageRows * f.key_row(), src + f.off_keys(), rows[i] * f.key_row(), full);
-          bulk_load(dst + L.codes + i * kPageRows * f.code_row(), src, rows[i] * f.code_row(), full);
           bulk_load(dst + L.scales + i * kPageRows * f.scale_row(), src + f.off_scales(),
                     (rows[i] * f.scale_row() + 15) / 16 * 16, full);
+          bulk_load(dst + L.codes + i * kPageRows * f.code_row(), src, rows[i] * f.code_row(), full);
+          bulk_load(dst + L.keys + i * kPageRows * f.key_row(), src + f.off_keys(), rows[i] * f.key_row(), full);
         }
         if (first) {
           // The segment's queries, once the score products of the segment before are done.
@@ -274,64 +278,91 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           bulk_load(q_u32, a.q_image + (long long)b * L.q_bytes, L.q_bytes, bar(misc->q_full));
           ++seg;
         }
+        if (++st == kStages) { st = 0; ++round; }
       }
-    } else if (warp < NB && lane == 0) {
-      // ---------------------------------------------------------------- score issuer kq
-      const int kq = warp;
-      const uint32_t d = tmem + kColS + kq * 32;
-      const int steps = min(8, (r - kq * 128) / 16);       // k-steps of 16 latents
-      int seg = 0;
-      for (int n = 0; n < n_tiles; ++n) {
-        const int st = n % kStages, k = n * NB + kq, sb = k & 1;
-        if (!wait(misc->raw_full[st], n / kStages, 3)) break;
+    } else if (warp >= kScoreIssuer0 && warp < kScoreIssuer0 + ISSUERS && lane == 0) {
+      // ---------------------------------------------------------------- score issuer j: quarters j, j + 2
+      const int j = warp - kScoreIssuer0;
+      const uint32_t d = tmem + kColS + j * 32;
+      const uint64_t mode = dr == 64 ? kSwizzle128B : kSwizzle64B;
+      const uint32_t key_sbo = 8 * f.key_row();
+      const uint64_t q_desc = make_smem_desc(q_u32, 16, 1024, kSwizzle128B);
+      const uint64_t qk_desc = make_smem_desc(q_u32 + NHP * 2 * r, 16, key_sbo, mode);
+      int seg = 0, st = 0, round = 0;
+      bool ok = true;
+      for (int n = 0; n < n_tiles && ok; ++n) {
+        ok = wait(misc->raw_full[st], round, 3);
+        if (!ok) break;
         const int flags = misc->info[n % kInfo].flags;
         if (flags & 1) {
-          if (!wait(misc->q_full, seg, 4)) break;
+          ok = wait(misc->q_full, seg, 4);
+          if (!ok) break;
           ++seg;
         }
-        if (!wait(misc->s_empty, n + 1, 5)) break;
+        ok = wait(misc->s_empty, n + 1, 5);
+        if (!ok) break;
         tc_fence_after_sync();
         uint32_t acc = 0;
-        // RoPE part: its k-steps are dealt out to the issuers.
-        const uint32_t key = stage_of(n) + L.keys, qk = q_u32 + NHP * 2 * r;
-        const uint64_t mode = dr == 64 ? kSwizzle128B : kSwizzle64B;
-        const uint32_t sbo = 8 * f.key_row();
-        for (int ks = kq; ks < dr / 16; ks += NB) {
-          mma_bf16_ss(d, make_smem_desc(key + ks * 32, 16, sbo, mode), make_smem_desc(qk + ks * 32, 16, sbo, mode),
-                      IDESC_K, acc);
+        // RoPE part: its k-steps alternate between the issuers.
+        const uint64_t key_desc = make_smem_desc(base + st * L.stage + L.keys, 16, key_sbo, mode);
+#pragma unroll 1
+        for (int ks = j; ks < dr / 16; ks += ISSUERS) {
+          mma_bf16_ss(d, key_desc + ks * 2, qk_desc + ks * 2, IDESC_K, acc);
           acc = 1;
         }
-        if (!wait(misc->as_full[n & 1][kq], n >> 1, 6)) break;
-        tc_fence_after_sync();
-        for (int ks = 0; ks < steps; ++ks) {
-          const uint32_t panel = q_u32 + (kq * 2 + (ks >> 2)) * NHP * 128 + (ks & 3) * 32;
-          mma_f16_ts(d, tmem + kColAs + sb * 64 + ks * 8, make_smem_desc(panel, 16, 1024, kSwizzle128B), IDESC_S, acc);
-          acc = 1;
+#pragma unroll 1
+        for (int kq = 0; kq < NB; ++kq) {
+          const int k = n * NB + kq, sb = k & 1;
+          ok = wait(misc->as_full[sb], k >> 1, 6);
+          if (!ok) break;
+          if (ISSUERS == 2 && (kq & 1) != j) {
+            mbar_arrive(bar(misc->as_empty[sb]));
+            continue;
+          }
+          tc_fence_after_sync();
+          const uint32_t at = tmem + COL_AS + sb * 64;
+#pragma unroll 1
+          for (int p = 0; p < 2 && kq * 128 + p * 64 < r; ++p) {
+            const uint64_t panel = q_desc + (uint64_t)((kq * 2 + p) * NHP * 8);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              mma_f16_ts(d, at + p * 32 + ks * 8, panel + ks * 2, IDESC_S, 1u);
+          }
+          mma_commit(bar(misc->as_empty[sb]));
         }
-        mma_commit(bar(misc->as_empty[sb]));
+        if (!ok) break;
         mma_commit(bar(misc->s_full));
         mma_commit(bar(misc->raw_empty[st]));
         if (flags & 2) mma_commit(bar(misc->q_empty));
+        if (++st == kStages) { st = 0; ++round; }
       }
-    } else if (warp >= kFirstValueIssuer && warp < kFirstValueIssuer + kValueIssuers && lane == 0) {
+    } else if (warp >= kValueIssuer0 && warp < kValueIssuer0 + ISSUERS && lane == 0) {
       // ---------------------------------------------------------------- value issuer j: blocks j, j + 2
-      const int j = warp - kFirstValueIssuer;
+      const int j = warp - kValueIssuer0;
+      const uint64_t p_desc = make_smem_desc(p_u32, 128, P_SBO, kSwizzleNone);
+      int vb = 0, round = 0;
       bool ok = true;
       for (int n = 0; n < n_tiles && ok; ++n) {
         ok = wait(misc->p_full[n & 1], n >> 1, 7);
         if (!ok) break;
-        const int flags = misc->info[n % kInfo].flags;      // p_full: written long before by the producer
-        for (int mb = j; mb < NB && ok; mb += kValueIssuers) {
-          const int k = n * NB + mb, vb = k & 1;
-          ok = wait(misc->av_full[n & 1][mb], n >> 1, 8);
+        tc_fence_after_sync();
+        const uint32_t fresh = misc->info[n % kInfo].flags & 1;
+        const uint64_t pd = p_desc + (uint64_t)((n & 1) * (P_BYTES / 16));
+#pragma unroll 1
+        for (int mb = 0; mb < NB; ++mb) {
+          ok = wait(misc->av_full[vb], round, 8);
           if (!ok) break;
-          tc_fence_after_sync();
+          if (ISSUERS == 2 && (mb & 1) != j) {
+            mbar_arrive(bar(misc->av_empty[vb]));
+          } else {
+            tc_fence_after_sync();
+            const uint32_t d = tmem + kColO + mb * NHP, at = tmem + COL_AV + vb * 64;
+            mma_f16_ts(d, at, pd, IDESC_V, fresh ^ 1u);
 #pragma unroll
-          for (int ks = 0; ks < kTile / 16; ++ks)
-            mma_f16_ts(tmem + kColO + mb * 32, tmem + kColAv + vb * 64 + ks * 8,
-                       make_smem_desc(p_u32 + (n & 1) * P_BYTES + ks * 256, 128, P_SBO, kSwizzleNone), IDESC_V,
-                       (flags & 1) && ks == 0 ? 0u : 1u);
-          mma_commit(bar(misc->av_empty[vb]));
+            for (int ks = 1; ks < kTile / 16; ++ks) mma_f16_ts(d, at + ks * 8, pd + ks * 16, IDESC_V, 1u);
+            mma_commit(bar(misc->av_empty[vb]));
+          }
+          if (++vb == AVB) { vb = 0; ++round; }
         }
         if (ok) mma_commit(bar(misc->p_empty[n & 1]));
       }
@@ -339,92 +370,104 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   } else if (warp < kValueWarp0) {
     // ------------------------------------------------------------------ expansion for the scores
     reg_alloc<kRegsWorker>();
-    const int q = warp & 3, slot = q * 32 + lane, half = slot >> 6, row = slot & 63;
+    const int q = warp & 3, slot = q * 32 + lane, row = slot & 63;
     const int cmask = f.code_mask(), chunks = r / kGroup;
-    const uint32_t lane_as = tmem + ((uint32_t)(q * 32) << 16) + kColAs;
+    const uint32_t lane_as = tmem + ((uint32_t)(q * 32) << 16) + COL_AS;
+    const uint32_t twist = (uint32_t)(row & cmask) * 16;
+    int st = 0, round = 0;
     bool ok = true;
     for (int n = 0; n < n_tiles; ++n) {
-      const int st = n % kStages;
-      ok = __all_sync(0xffffffffu, wait(misc->raw_full[st], n / kStages, 9));
+      ok = __all_sync(0xffffffffu, wait(misc->raw_full[st], round, 9));
       if (!ok) break;
       const TileInfo& info = misc->info[n % kInfo];
-      const bool live = row < (half ? info.rows1 : info.rows0);
-      const uint32_t stage = stage_of(n);
-      const uint32_t codes = stage + L.codes + slot * f.code_row(), scales = stage + L.scales + slot * f.scale_row();
-      const uint32_t st_out = st_u32 + st * f.scale_row() * kTile * 2 + slot * 2;
-      // The scales as half precision, a group's 128 slots in a row, for the value warps; zero
-      // where there is no slot, so that whatever its codes are, the product is zero.
-      for (int c = 0; c < chunks; c += 2) {
-        uint32_t two;
-        asm volatile("{\n\t.reg .u16 x;\n\tld.shared.u16 x, [%1];\n\tcvt.u32.u16 %0, x;\n\t}" : "=r"(two) : "r"(scales + c));
-        const uint32_t s0 = live ? (two & 0xffu) << 7 : 0u, s1 = live ? (two >> 8) << 7 : 0u;
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + c * kTile * 2), "h"((uint16_t)s0) : "memory");
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + (c + 1) * kTile * 2), "h"((uint16_t)s1) : "memory");
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(misc->scale_full[st]));
+      const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
+      const uint32_t stage = base + st * L.stage;
+      const uint32_t codes = stage + L.codes + slot * f.code_row();
+      uint32_t scales = stage + L.scales + slot * f.scale_row();
+      // The scales also go out as half precision, a group's 128 slots in a row, for the value warps;
+      // zero where there is no slot, so that whatever its codes are, the product is zero.
+      uint32_t st_out = st_u32 + st * f.scale_row() * kTile * 2 + slot * 2;
+#pragma unroll 1
       for (int kq = 0; kq < NB; ++kq) {
         const int k = n * NB + kq, sb = k & 1;
         ok = __all_sync(0xffffffffu, wait(misc->as_empty[sb], (k >> 1) + 1, 10));
         if (!ok) break;
         tc_fence_after_sync();
+        const int c_end = min(chunks, kq * 4 + 4);
+#pragma unroll 1
+        for (int c = kq * 4; c < c_end; c += 2) {
+          // Two chunks at a time: their loads overlap, and a row of scales is a multiple of 2 bytes.
+          const uint4 w0 = lds128(codes + ((uint32_t)(c * 16) ^ twist));
+          const uint4 w1 = lds128(codes + ((uint32_t)(c * 16 + 16) ^ twist));
+          uint32_t two;
+          asm volatile("{\n\t.reg .u16 x;\n\tld.shared.u16 x, [%1];\n\tcvt.u32.u16 %0, x;\n\t}"
+                       : "=r"(two) : "r"(scales + c));
+          const uint32_t s0 = (two & 0xffu) << 7, s1 = (two >> 8) << 7;
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + c * (kTile * 2)), "h"((uint16_t)(s0 & live)) : "memory");
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + (c + 1) * (kTile * 2)), "h"((uint16_t)(s1 & live))
+                       : "memory");
+          const uint32_t sc0 = s0 | (s0 << 16), sc1 = s1 | (s1 << 16);
+          const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+          const uint32_t at = lane_as + sb * 64 + (c & 3) * 16;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c = kq * 4 + i;
-          if (c >= chunks) break;
-          const uint4 w = lds128(codes + (c ^ (row & cmask)) * 16);
-          const uint32_t sc = scale_pair(lds_u8(scales + c));
-          const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-          uint32_t v[16];
+          for (int p = 0; p < 2; ++p) {
+            uint32_t v[16];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t o[4];
-            decode8(word[j], o);
+            for (int i = 0; i < 4; ++i) {
+              uint32_t o[4];
+              decode8(word[4 * p + i], o);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) v[4 * j + m] = mul_h2(o[m], sc);
+              for (int m = 0; m < 4; ++m) v[4 * i + m] = mul_h2(o[m], p ? sc1 : sc0);
+            }
+            tmem_st_x16(at + p * 16, v);
           }
-          tmem_st_x16(lane_as + sb * 64 + i * 16, v);
         }
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc->as_full[n & 1][kq]));
+        if (lane == 0) mbar_arrive(bar(misc->as_full[sb]));
       }
       if (!ok) break;
-      if (lane == 0) mbar_arrive(bar(misc->raw_empty[st]));
+      if (lane == 0) {
+        mbar_arrive(bar(misc->scale_full[st]));
+        mbar_arrive(bar(misc->raw_empty[st]));
+      }
+      if (++st == kStages) { st = 0; ++round; }
     }
   } else if (warp < kSoftmaxWarp0) {
     // ------------------------------------------------------------------ expansion for the values
     reg_alloc<kRegsWorker>();
     const int q = warp & 3, half = (warp - kValueWarp0) >> 2, t = lane & 3;
     const int cmask = f.code_mask(), chunks = r / kGroup;
-    const uint32_t lane_av = tmem + ((uint32_t)(q * 32) << 16) + kColAv + half * 32;
+    const uint32_t lane_av = tmem + ((uint32_t)(q * 32) << 16) + COL_AV + half * 32;
+    const uint32_t twist = (uint32_t)(lane & cmask) * 16;      // rows lane and lane + 32 twist alike
+    const uint32_t step = 32 * f.code_row();
+    int st = 0, round = 0, vb = 0, av_round = 0;
     bool ok = true;
     for (int n = 0; n < n_tiles; ++n) {
-      const int st = n % kStages;
-      ok = __all_sync(0xffffffffu, wait(misc->raw_full[st], n / kStages, 11) &&
-                                       wait(misc->scale_full[st], n / kStages, 12));
+      ok = __all_sync(0xffffffffu, wait(misc->raw_full[st], round, 11) && wait(misc->scale_full[st], round, 12));
       if (!ok) break;
-      const uint32_t codes = stage_of(n) + L.codes + half * kPageRows * f.code_row();
+      const uint32_t codes = base + st * L.stage + L.codes + (half * kPageRows + lane) * f.code_row();
       const uint32_t sts = st_u32 + st * f.scale_row() * kTile * 2 + (half * kPageRows + 2 * t) * 2;
+#pragma unroll 1
       for (int mb = 0; mb < NB; ++mb) {
-        const int k = n * NB + mb, vb = k & 1, c = mb * 4 + q;
-        ok = __all_sync(0xffffffffu, wait(misc->av_empty[vb], (k >> 1) + 1, 13));
+        const int c = mb * 4 + q;
+        ok = __all_sync(0xffffffffu, wait(misc->av_empty[vb], av_round + 1, 13));
         if (!ok) break;
         tc_fence_after_sync();
         if (c < chunks) {
-#pragma unroll
+          const uint32_t at = codes + ((uint32_t)(c * 16) ^ twist), sc_at = sts + c * (kTile * 2);
+#pragma unroll 1
           for (int h = 0; h < 2; ++h) {
-            const int lr = h * 32 + lane;
             uint32_t w[4], v[4][4];
-            ldsm_x4_trans(codes + lr * f.code_row() + (c ^ (lr & cmask)) * 16, w);
+            ldsm_x4_trans(at + h * step, w);
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
               uint32_t sc;
-              asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sts + (c * kTile + h * 32 + m * 8) * 2));
+              asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sc_at + (h * 32 + m * 8) * 2));
               decode_pairs(w[m], v[m]);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) v[m][j] = mul_h2(v[m][j], sc);
+              for (int i = 0; i < 4; ++i) v[m][i] = mul_h2(v[m][i], sc);
             }
             const uint32_t col = lane_av + vb * 64 + h * 16;
             tmem_st_16x128_x4(col, v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]);
@@ -434,182 +477,187 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc->av_full[n & 1][mb]));
+        if (lane == 0) mbar_arrive(bar(misc->av_full[vb]));
+        if (++vb == AVB) { vb = 0; ++av_round; }
       }
       if (!ok) break;
       if (lane == 0) mbar_arrive(bar(misc->raw_empty[st]));
+      if (++st == kStages) { st = 0; ++round; }
     }
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
     // Two groups of four warps: group gr owns heads [gr * NHH, (gr + 1) * NHH) of the tile's 128
-    // slots, a slot per thread.
+    // slots, a slot per thread.  They leave the loop together (they agree on it once a tile, before
+    // anything that depends on the tile's description), so the hardware barrier always completes.
     reg_alloc<kRegsWorker>();
     constexpr int NHH = NHP / 2;
     const int sw = warp - kSoftmaxWarp0, gr = sw >> 2, q = warp & 3, HO = gr * NHH;
     const int sidx = sw * 32 + lane, slot = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + HO;
     bool ok = true;
-    int sync_phase = 0;
-    auto group_sync = [&]() {
-      mbar_arrive(bar(misc->group_sync));
-      if (ok) ok = wait(misc->group_sync, sync_phase, 14);
-      ++sync_phase;
-    };
+    auto group_sync = [&]() { named_sync<1, kSoftmaxThreads>(); };
     auto ld_cols = [&](uint32_t addr, uint32_t (&v)[16]) {
       if (NHH == 16) tmem_ld_x16(addr, v); else tmem_ld_x8(addr, v);
     };
     auto st_cols = [&](uint32_t addr, const uint32_t (&v)[16]) {
       if (NHH == 16) tmem_st_x16(addr, v); else tmem_st_x8(addr, v);
     };
-    // One value per head over the warp's 32 slots, left in red[sw][i].
-    auto reduce_heads = [&](const float (&v)[NHH], bool is_max) {
+    // One value per head over the warp's 32 slots, left in red[sw][i]: halving exchanges, in each of
+    // which a lane keeps half of its heads and adds the partner's share of them.
+    auto reduce_heads = [&](float (&v)[NHH], bool is_max) {
+      auto join = [&](float x, float y) { return is_max ? fmaxf(x, y) : x + y; };
 #pragma unroll
-      for (int i = 0; i < NHH; ++i) {
-        float x = v[i];
+      for (int n = NHH, o = 16; n > 1; n >>= 1, o >>= 1) {
+        const bool upper = lane & o;
 #pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) {
-          const float y = __shfl_xor_sync(0xffffffffu, x, o);
-          x = is_max ? fmaxf(x, y) : x + y;
+        for (int i = 0; i < n / 2; ++i) {
+          const float keep = upper ? v[i + n / 2] : v[i], give = upper ? v[i] : v[i + n / 2];
+          v[i] = join(keep, __shfl_xor_sync(0xffffffffu, give, o));
         }
-        if (lane == 0) misc->red[sw][i] = x;
       }
+      float x = v[0];                                    // head (lane >> log2(32 / NHH)) of the group
+#pragma unroll
+      for (int o = 16 / NHH; o >= 1; o >>= 1) x = join(x, __shfl_xor_sync(0xffffffffu, x, o));
+      if ((lane & (32 / NHH - 1)) == 0) misc->red[sw][lane / (32 / NHH)] = x;
     };
     auto reduced = [&](int h, bool is_max) {
       const float* x = &misc->red[(h / NHH) * 4][h % NHH];
       return is_max ? fmaxf(fmaxf(x[0], x[16]), fmaxf(x[32], x[48])) : (x[0] + x[16]) + (x[32] + x[48]);
     };
+    uint8_t* const p_row = sm + L.off_p + (HO / 8) * P_SBO + slot * 16;
     float l_acc[NHH];
     for (int n = 0; n < n_tiles; ++n) {
       if (ok) ok = wait(misc->info_full[n % kInfo], n / kInfo, 15);
-      const TileInfo info = misc->info[n % kInfo];
-      const bool seg_first = info.flags & 1, seg_last = info.flags & 2;
-      const bool live = (slot & 63) < (slot < 64 ? info.rows0 : info.rows1);
-      if (seg_first) {
+      if (ok) ok = wait(misc->s_full, n, 16);
+      if (named_sync_or<1, kSoftmaxThreads>(!ok)) break;
+      const int flags = misc->info[n % kInfo].flags;
+      const int rows = slot < 64 ? misc->info[n % kInfo].rows0 : misc->info[n % kInfo].rows1;
+      if (flags & 1) {
         if (sidx < 32) {
           misc->m_used[sidx] = -INFINITY;
-          misc->unit[sidx] = sidx < NHP ? a.q_unit[info.b * 32 + sidx] : 0.f;
+          misc->neg_ref[sidx] = kUnset;
+          misc->unit[sidx] = sidx < NHP ? a.q_unit[misc->info[n % kInfo].b * 32 + sidx] : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < NHH; ++i) l_acc[i] = 0.f;
         group_sync();
       }
       float s[NHH];
-#pragma unroll
-      for (int i = 0; i < NHH; ++i) s[i] = 0.f;
-      if (ok) ok = wait(misc->s_full, n, 16);
-      ok = __all_sync(0xffffffffu, ok);                  // TMEM accesses are whole-warp operations
-      if (ok) {
+      {
+        uint32_t sp[2][16];
         tc_fence_after_sync();
-        uint32_t sp[NB > 1 ? 2 : 1][16];
+        ld_cols(lane_base + kColS, sp[0]);
+        if (ISSUERS == 2) ld_cols(lane_base + kColS + 32, sp[1]);
+        tmem_wait_ld();
 #pragma unroll
-        for (int k = 0; k < NB; k += 2) {
-          ld_cols(lane_base + kColS + k * 32, sp[0]);
-          if (k + 1 < NB) ld_cols(lane_base + kColS + (k + 1) * 32, sp[NB > 1 ? 1 : 0]);
-          tmem_wait_ld();
-#pragma unroll
-          for (int i = 0; i < NHH; ++i) {
-            s[i] += __uint_as_float(sp[0][i]);
-            if (k + 1 < NB) s[i] += __uint_as_float(sp[NB > 1 ? 1 : 0][i]);
-          }
-        }
+        for (int i = 0; i < NHH; ++i)
+          s[i] = ISSUERS == 2 ? __uint_as_float(sp[0][i]) + __uint_as_float(sp[1][i]) : __uint_as_float(sp[0][i]);
         tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(misc->s_empty));
       }
-      mbar_arrive(bar(misc->s_empty));
-      float m_ref[NHH];
-      bool exceed = false;
+      const bool live = (slot & 63) < rows, full = __all_sync(0xffffffffu, live);
+      // x = score - reference + shift in log2 units, kept in place of the raw score.
+      float top = -INFINITY;
+      auto offset_scores = [&](float (&x)[NHH]) {
 #pragma unroll
-      for (int i = 0; i < NHH; ++i) {
-        s[i] = live ? s[i] * misc->unit[HO + i] : -INFINITY;
-        m_ref[i] = misc->m_used[HO + i];
-        exceed |= s[i] > m_ref[i] + kRescale;
-      }
-      if (exceed) misc->exceed_flag[n & 1] = 1;
-      mbar_arrive(bar(misc->flag_bar[n & 1]));
-
-      float psum[NHH];                                   // unrounded probabilities
+        for (int i = 0; i < NHH; i += 4) {
+          const float4 u = *reinterpret_cast<const float4*>(&misc->unit[HO + i]);
+          const float4 o = *reinterpret_cast<const float4*>(&misc->neg_ref[HO + i]);
+          x[i] = fmaf(s[i], u.x, o.x);
+          x[i + 1] = fmaf(s[i + 1], u.y, o.y);
+          x[i + 2] = fmaf(s[i + 2], u.z, o.z);
+          x[i + 3] = fmaf(s[i + 3], u.w, o.w);
+        }
+        if (!full) {                                     // only a sequence's last tile
+#pragma unroll
+          for (int i = 0; i < NHH; ++i) x[i] = live ? x[i] : -INFINITY;
+        }
+      };
       uint32_t pb[NHH / 2];
+      float add[NHH];
+      offset_scores(add);
+#pragma unroll
+      for (int i = 0; i < NHH; ++i) top = fmaxf(top, add[i]);
       auto probabilities = [&]() {
 #pragma unroll
         for (int i = 0; i < NHH; i += 2) {
-          // Nothing visible so far (reference still minus infinity): every term is 0, or NaN.
-          const float r0 = m_ref[i] == -INFINITY ? -kShift : m_ref[i] - kShift;
-          const float r1 = m_ref[i + 1] == -INFINITY ? -kShift : m_ref[i + 1] - kShift;
-          psum[i] = ex2_approx(s[i] - r0);
-          psum[i + 1] = ex2_approx(s[i + 1] - r1);
-          const __half2 x = __floats2half2_rn(psum[i], psum[i + 1]);
+          add[i] = ex2_approx(add[i]);
+          add[i + 1] = ex2_approx(add[i + 1]);
+          const __half2 x = __floats2half2_rn(add[i], add[i + 1]);
           pb[i / 2] = *reinterpret_cast<const uint32_t*>(&x);
         }
       };
       // P as the MN-major, un-swizzled B operand: eight heads of a slot are 16 bytes, eight slots
       // follow one another, groups of eight heads are P_SBO apart.
       auto store_probabilities = [&]() {
-        uint8_t* d = sm + L.off_p + (n & 1) * P_BYTES + (HO / 8) * P_SBO + slot * 16;
 #pragma unroll
         for (int i = 0; i < NHH / 8; ++i)
-          *reinterpret_cast<uint4*>(d + i * P_SBO) = make_uint4(pb[4 * i], pb[4 * i + 1], pb[4 * i + 2], pb[4 * i + 3]);
+          *reinterpret_cast<uint4*>(p_row + (n & 1) * P_BYTES + i * P_SBO) =
+              make_uint4(pb[4 * i], pb[4 * i + 1], pb[4 * i + 2], pb[4 * i + 3]);
       };
-      probabilities();
       if (ok) ok = wait(misc->p_empty[n & 1], (n >> 1) + 1, 17);     // value products of tile n - 2
-      if (ok) store_probabilities();
-      if (ok) ok = wait(misc->flag_bar[n & 1], n >> 1, 18);
-      if (ok && misc->exceed_flag[n & 1]) {
-        // Rare: some reference has to rise (always at a segment's first tile).  Everybody is here:
-        // the flag is read after all arrivals.
-        reduce_heads(s, true);
+      if (named_sync_or<1, kSoftmaxThreads>(top > kShift + kRescale)) {
+        // Rare: some reference has to rise (always at a segment's first tile).
+        {
+          float x[NHH];
+#pragma unroll
+          for (int i = 0; i < NHH; ++i) x[i] = live ? s[i] * misc->unit[HO + i] : -INFINITY;
+          reduce_heads(x, true);
+        }
         group_sync();
-        if (sidx == 0) misc->exceed_flag[n & 1] = 0;
         if (sidx < NHP) {
           const float mt = reduced(sidx, true), m_old = misc->m_used[sidx];
           const float m_new = mt > m_old + kRescale ? mt : m_old;
           misc->m_used[sidx] = m_new;
+          misc->neg_ref[sidx] = m_new == -INFINITY ? kUnset : kShift - m_new;
           misc->fac[sidx] = m_new == m_old ? 1.f : exp2f(m_old - m_new);       // 0 from minus infinity
         }
         group_sync();
 #pragma unroll
-        for (int i = 0; i < NHH; ++i) {
-          m_ref[i] = misc->m_used[HO + i];
-          l_acc[i] *= misc->fac[HO + i];
-        }
-        if (!seg_first) {
+        for (int i = 0; i < NHH; ++i) l_acc[i] *= misc->fac[HO + i];
+        if (!(flags & 1)) {
           // O is scaled to the old references: wait for the previous tile's products, rescale.
           if (ok) ok = wait(misc->p_empty[(n - 1) & 1], (n - 1) >> 1, 19);
-          ok = __all_sync(0xffffffffu, ok);
+          ok = __all_sync(0xffffffffu, ok);              // TMEM accesses are whole-warp operations
           if (ok) {
             tc_fence_after_sync();
+#pragma unroll 1
             for (int mb = 0; mb < NB; ++mb) {
               uint32_t ov[16];
-              ld_cols(lane_base + kColO + mb * 32, ov);
+              ld_cols(lane_base + kColO + mb * NHP, ov);
               tmem_wait_ld();
 #pragma unroll
               for (int i = 0; i < NHH; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * misc->fac[HO + i]);
-              st_cols(lane_base + kColO + mb * 32, ov);
+              st_cols(lane_base + kColO + mb * NHP, ov);
             }
             tmem_wait_st();
           }
         }
-        probabilities();
-        if (ok) store_probabilities();
+        offset_scores(add);
         group_sync();                                    // fac / red may be rewritten
       }
+      probabilities();
+      if (ok) store_probabilities();
 #pragma unroll
-      for (int i = 0; i < NHH; ++i) l_acc[i] += psum[i];
-      if (ok) {
-        fence_proxy_async_smem();
-        tc_fence_before_sync();
-        mbar_arrive(bar(misc->p_full[n & 1]));
-      }
-      if (!seg_last) continue;
+      for (int i = 0; i < NHH; ++i) l_acc[i] += add[i];
+      fence_proxy_async_smem();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(misc->p_full[n & 1]));
+      if (!(flags & 2)) continue;
 
       // ---- end of a segment
-      const int b = info.b, g = g0 + n;
+      const int b = misc->info[n % kInfo].b, g = g0 + n;
       const bool whole = prefix[b] >= g0 && g + 1 == prefix[b + 1];
       const int c0 = share_owner(prefix[b], total, ctas), part = (int)blockIdx.x + b;
       reduce_heads(l_acc, false);
       group_sync();
-      if (sidx < NHP) misc->fac[sidx] = reduced(sidx, false);
+      if (sidx < NHP) misc->fac[sidx] = reduced(sidx, false);     // denominators
       group_sync();
       if (ok && sidx < a.n_heads) {
         const float l = misc->fac[sidx], m = misc->m_used[sidx] - kShift;
+        misc->unit[sidx] = 1.f / l;                      // the units have done their work in this segment
         if (whole) {
           if (a.lse) a.lse[(long long)b * a.n_heads + sidx] = (m + log2f(l)) * 0.69314718055994531f;
         } else {
@@ -619,26 +667,27 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       }
       if (ok && sidx == 0 && g + 1 == prefix[b + 1])
         a.seq_parts[b] = whole ? make_int2(0, 0) : make_int2(c0 + b, (int)blockIdx.x - c0 + 1);
+      group_sync();
       if (ok) ok = wait(misc->p_empty[n & 1], n >> 1, 20);           // the last value products
       ok = __all_sync(0xffffffffu, ok);
       if (ok) {
         tc_fence_after_sync();
         // Lane 8j + g of a quarter holds latent 4g + j.
         const int lat = q * 32 + 4 * (lane & 7) + (lane >> 3);
+        const long long at = (long long)(whole ? b : part) * a.n_heads * r + lat;
+#pragma unroll 1
         for (int mb = 0; mb < NB; ++mb) {
           uint32_t ov[16];
-          ld_cols(lane_base + kColO + mb * 32, ov);
+          ld_cols(lane_base + kColO + mb * NHP, ov);
           tmem_wait_ld();
           if (mb * 128 + lat >= r) continue;
 #pragma unroll
           for (int i = 0; i < NHH; ++i) {
-            if (HO + i >= a.n_heads) continue;
+            if (HO + i >= a.n_heads) break;
+            const long long e = at + (HO + i) * r + mb * 128;
             const float v = __uint_as_float(ov[i]);
-            if (whole)
-              static_cast<bf16*>(a.out)[((long long)b * a.n_heads + HO + i) * r + mb * 128 + lat] =
-                  __float2bfloat16_rn(v / misc->fac[HO + i]);
-            else
-              a.o_part[((long long)part * a.n_heads + HO + i) * r + mb * 128 + lat] = v;
+            if (whole) static_cast<bf16*>(a.out)[e] = __float2bfloat16_rn(v * misc->unit[HO + i]);
+            else a.o_part[e] = v;
           }
         }
         tc_fence_before_sync();

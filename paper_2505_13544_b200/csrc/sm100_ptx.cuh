@@ -83,6 +83,25 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return mbar_wait_for(bar, parity, abort_word, error_word, code, kWaitBudgetNs);
 }
 
+// The same wait as few instructions, for kernels whose roles would otherwise not fit the
+// instruction cache together: one polling loop, the clock read on every 256th poll only.
+__device__ __forceinline__ bool mbar_wait_compact(uint32_t bar, uint32_t parity, volatile int* abort_word,
+                                                  int* error_word, int code) {
+  uint32_t polls = 0, t0 = 0;
+  while (!mbar_try_wait(bar, parity)) {
+    if ((++polls & 255u) == 0u) {
+      const uint32_t now = (uint32_t)(global_timer_ns() >> 20);          // about milliseconds
+      if (polls == 256u) t0 = now;
+      if (*abort_word || now - t0 > (uint32_t)(kWaitBudgetNs >> 20)) {
+        *abort_word = 1;
+        atomicCAS(error_word, 0, code);
+        return false;
+      }
+    }
+  }
+  return true;
+}
+
 // 2^x by the special-function unit (about 2 ulp; flushes denormals): enough for probabilities
 // that are rounded to bf16 straight away.
 __device__ __forceinline__ float ex2_approx(float x) {
@@ -102,6 +121,26 @@ __device__ __forceinline__ void tc_fence_before_sync() {
 }
 __device__ __forceinline__ void tc_fence_after_sync() {
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+
+// Rendezvous of `threads` threads of the CTA on hardware barrier `id`; the second form also tells
+// whether any of them passed a true predicate.  For groups all of whose threads always get there.
+template <int ID, int THREADS>
+__device__ __forceinline__ void named_sync() {
+  asm volatile("barrier.cta.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory");
+}
+template <int ID, int THREADS>
+__device__ __forceinline__ bool named_sync_or(bool p) {
+  int r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n\t"
+      "selp.b32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((int)p), "n"(ID), "n"(THREADS)
+      : "memory");
+  return r != 0;
 }
 
 // Programmatic dependent launch.  grid_launch_dependents lets the next kernel on the stream
