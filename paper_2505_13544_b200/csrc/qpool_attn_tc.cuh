@@ -24,11 +24,11 @@
 // Queries arrive as an image of the B operand that qpool_query_kernel has written (half precision
 // scaled by a power of two per head, swizzled), so that a segment's query is one bulk copy.
 //
-// Roles (28 warps): warps 0-1 score issuers and 2-3 value issuers, one thread each (a thread issues a
-// matrix instruction about every 50 cycles, these execute in 16), warp 4 producer, warps 8-11
-// expansion for the scores, 12-19 for the values (four warps a page of the tile), 20-27 softmax and
-// epilogue.  The hot loops are short on purpose: with five kinds of code on every scheduler, fetching
-// unrolled instructions was the longest stall.
+// Roles (28 warps): warp 0 issues the score products, warp 1 the value products, warp 2 is the
+// producer; warps 4-11 expand for the scores (two groups, a quarter of r each in turn), 12-19 for the
+// values (a page of the tile each four), 20-27 softmax and epilogue.  The hot loops are short on
+// purpose: with five kinds of code on every scheduler, fetching unrolled instructions was the
+// longest stall (107 KB of them: 517 us at 128 x 16384 slots, 61 KB: 362 us).
 // The online softmax raises a head's reference only when a tile exceeds it by 2^8.  Probabilities
 // are kept times 2^7: with the 2^8 they stay inside half precision.
 //
@@ -45,11 +45,11 @@ constexpr int kTile = 128;                  // slots per tile: two pages
 constexpr int kThreads = 896;
 constexpr int kStages = 3;
 constexpr int kMaxBatch = 1022;             // prefix sums kept in shared memory
-constexpr int kProducerWarp = 4, kScoreIssuer0 = 0, kValueIssuer0 = 2;
-constexpr int kScoreWarp0 = 8, kScoreWarps = 4, kValueWarp0 = 12, kValueWarps = 8;
+constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2;
+constexpr int kScoreWarp0 = 4, kScoreWarps = 8, kValueWarp0 = 12, kValueWarps = 8;
 constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
 constexpr int kInfo = 16;                   // ring of tile descriptions, deeper than any role's lag
-// TMEM columns: two score accumulators, up to four output blocks of NHP columns, two operand
+// TMEM columns: two score buffers, up to four output blocks of NHP columns, two operand
 // buffers of 64 columns for the scores and what is left, three (32 heads) or four, for the values.
 constexpr int kTmemCols = 512;
 constexpr int kColS = 0, kColO = 64, kMaxAv = 4;
@@ -60,9 +60,9 @@ static_assert(col_av(32) + 64 * av_buffers(32) <= kTmemCols && col_av(16) + 64 *
               "tensor memory budget");
 constexpr float kShift = 7.f, kRescale = 8.f;
 constexpr float kUnset = 3e38f;             // in the place of -reference: any score then exceeds it
-constexpr int kRegsIssuer = 32, kRegsWorker = 88;
+constexpr int kRegsControl = 40, kRegsWorker = 72;
 constexpr int kRegsAtLaunch = 65536 / kThreads / 8 * 8;
-static_assert(256 * kRegsIssuer + (kThreads - 256) * kRegsWorker <= kThreads * kRegsAtLaunch,
+static_assert(128 * kRegsControl + (kThreads - 128) * kRegsWorker <= kThreads * kRegsAtLaunch,
               "register re-allocation exceeds the CTA's pool");
 
 struct TileInfo {
@@ -73,10 +73,8 @@ struct TileInfo {
 
 struct Misc {
   unsigned long long raw_full[kStages], raw_empty[kStages], scale_full[kStages];
-  // Operand buffers.  Both issuers of a product wait for every buffer and hand every buffer back (the
-  // one that reads it through its commit), so that nobody can miss a phase.
   unsigned long long as_full[2], as_empty[2], av_full[kMaxAv], av_empty[kMaxAv];
-  unsigned long long s_full, s_empty, p_full[2], p_empty[2], q_full, q_empty;
+  unsigned long long s_full[2], s_empty[2], p_full[2], p_empty[2], q_full, q_empty;
   unsigned long long info_full[kInfo];
   uint32_t tmem_base;
   int abort_word;
@@ -171,7 +169,6 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   constexpr uint32_t IDESC_S = make_idesc_f16(128, NHP, 0, 0), IDESC_K = make_idesc_bf16(128, NHP, 0, 0);
   constexpr uint32_t IDESC_V = make_idesc_f16(128, NHP, 0, 1);
   constexpr uint32_t P_BYTES = kTile * NHP * 2, P_SBO = kTile * 16;   // bytes between groups of 8 heads
-  constexpr int ISSUERS = NB > 1 ? 2 : 1;                             // of each product
   constexpr int AVB = av_buffers(NHP), COL_AS = col_as(NHP), COL_AV = col_av(NHP);
   extern __shared__ uint8_t smem_raw[];
   const Format f = a.f;
@@ -182,30 +179,30 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   Misc* misc = reinterpret_cast<Misc*>(sm + L.off_misc);
   int* prefix = reinterpret_cast<int*>(sm + L.off_prefix);
   volatile int* abort_word = &misc->abort_word;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // warp: uniform
   auto bar = [&](unsigned long long& p) { return smem_u32(&p); };
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(bar(misc->raw_full[i]), 1);
-      mbar_init(bar(misc->raw_empty[i]), kScoreWarps + kValueWarps + ISSUERS);
+      mbar_init(bar(misc->raw_empty[i]), kScoreWarps + kValueWarps + 1);
       mbar_init(bar(misc->scale_full[i]), kScoreWarps);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(misc->as_full[i]), kScoreWarps);
-      mbar_init(bar(misc->as_empty[i]), ISSUERS);
+      mbar_init(bar(misc->as_full[i]), kScoreWarps / 2);
+      mbar_init(bar(misc->as_empty[i]), 1);
+      mbar_init(bar(misc->s_full[i]), 1);
+      mbar_init(bar(misc->s_empty[i]), kSoftmaxWarps);
       mbar_init(bar(misc->p_full[i]), kSoftmaxWarps);
-      mbar_init(bar(misc->p_empty[i]), ISSUERS);
+      mbar_init(bar(misc->p_empty[i]), 1);
     }
     for (int i = 0; i < kMaxAv; ++i) {
       mbar_init(bar(misc->av_full[i]), kValueWarps);
-      mbar_init(bar(misc->av_empty[i]), ISSUERS);
+      mbar_init(bar(misc->av_empty[i]), 1);
     }
     for (int i = 0; i < kInfo; ++i) mbar_init(bar(misc->info_full[i]), 1);
-    mbar_init(bar(misc->s_full), ISSUERS);
-    mbar_init(bar(misc->s_empty), kSoftmaxWarps);
     mbar_init(bar(misc->q_full), 1);
-    mbar_init(bar(misc->q_empty), ISSUERS);
+    mbar_init(bar(misc->q_empty), 1);
     misc->abort_word = 0;
     mbar_fence_init();
   }
@@ -229,11 +226,14 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   auto wait = [&](unsigned long long& b, int phase, int code) {
     return mbar_wait_compact(bar(b), phase & 1, abort_word, a.error_word, code);
   };
+  auto wait_warp = [&](unsigned long long& b, int phase, int code) {       // one answer for the warp
+    return __all_sync(0xffffffffu, wait(b, phase, code)) != 0;
+  };
 
   if (n_tiles == 0) {
     // nothing to do; the CTA falls through to the common end
   } else if (warp < kScoreWarp0) {
-    reg_dealloc<kRegsIssuer>();
+    reg_dealloc<kRegsControl>();
     if (warp == kProducerWarp && lane == 0) {
       // ---------------------------------------------------------------- producer
       int b = find_seq(prefix, a.batch, g0), seg = 0, st = 0, round = 0;
@@ -280,10 +280,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         }
         if (++st == kStages) { st = 0; ++round; }
       }
-    } else if (warp >= kScoreIssuer0 && warp < kScoreIssuer0 + ISSUERS && lane == 0) {
-      // ---------------------------------------------------------------- score issuer j: quarters j, j + 2
-      const int j = warp - kScoreIssuer0;
-      const uint32_t d = tmem + kColS + j * 32;
+    } else if (warp == kScoreIssuer) {
+      // ---------------------------------------------------------------- score products (whole warp, uniform)
       const uint64_t mode = dr == 64 ? kSwizzle128B : kSwizzle64B;
       const uint32_t key_sbo = 8 * f.key_row();
       const uint64_t q_desc = make_smem_desc(q_u32, 16, 1024, kSwizzle128B);
@@ -291,94 +289,102 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       int seg = 0, st = 0, round = 0;
       bool ok = true;
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = wait(misc->raw_full[st], round, 3);
+        ok = wait_warp(misc->raw_full[st], round, 3);
         if (!ok) break;
         const int flags = misc->info[n % kInfo].flags;
         if (flags & 1) {
-          ok = wait(misc->q_full, seg, 4);
+          ok = wait_warp(misc->q_full, seg, 4);
           if (!ok) break;
           ++seg;
         }
-        ok = wait(misc->s_empty, n + 1, 5);
+        ok = wait_warp(misc->s_empty[n & 1], (n >> 1) + 1, 5);
         if (!ok) break;
         tc_fence_after_sync();
-        uint32_t acc = 0;
-        // RoPE part: its k-steps alternate between the issuers.
+        const uint32_t d = tmem + kColS + (n & 1) * 32;
         const uint64_t key_desc = make_smem_desc(base + st * L.stage + L.keys, 16, key_sbo, mode);
-#pragma unroll 1
-        for (int ks = j; ks < dr / 16; ks += ISSUERS) {
-          mma_bf16_ss(d, key_desc + ks * 2, qk_desc + ks * 2, IDESC_K, acc);
-          acc = 1;
+        if (elect_one()) {                               // RoPE part: d_R / 16 is 2 or 4
+          mma_bf16_ss(d, key_desc, qk_desc, IDESC_K, 0u);
+          mma_bf16_ss(d, key_desc + 2, qk_desc + 2, IDESC_K, 1u);
+          if (dr == 64) {
+            mma_bf16_ss(d, key_desc + 4, qk_desc + 4, IDESC_K, 1u);
+            mma_bf16_ss(d, key_desc + 6, qk_desc + 6, IDESC_K, 1u);
+          }
         }
+        __syncwarp();
 #pragma unroll 1
         for (int kq = 0; kq < NB; ++kq) {
           const int k = n * NB + kq, sb = k & 1;
-          ok = wait(misc->as_full[sb], k >> 1, 6);
+          ok = wait_warp(misc->as_full[sb], k >> 1, 6);
           if (!ok) break;
-          if (ISSUERS == 2 && (kq & 1) != j) {
-            mbar_arrive(bar(misc->as_empty[sb]));
-            continue;
-          }
           tc_fence_after_sync();
           const uint32_t at = tmem + COL_AS + sb * 64;
-#pragma unroll 1
-          for (int p = 0; p < 2 && kq * 128 + p * 64 < r; ++p) {
-            const uint64_t panel = q_desc + (uint64_t)((kq * 2 + p) * NHP * 8);
+          const uint64_t panel = q_desc + (uint64_t)(kq * 2 * NHP * 8);
+          if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-              mma_f16_ts(d, at + p * 32 + ks * 8, panel + ks * 2, IDESC_S, 1u);
+            for (int ks = 0; ks < 4; ++ks) mma_f16_ts(d, at + ks * 8, panel + ks * 2, IDESC_S, 1u);
+            if (kq * 128 + 64 < r) {
+#pragma unroll
+              for (int ks = 0; ks < 4; ++ks)
+                mma_f16_ts(d, at + 32 + ks * 8, panel + NHP * 8 + ks * 2, IDESC_S, 1u);
+            }
+            mma_commit(bar(misc->as_empty[sb]));
           }
-          mma_commit(bar(misc->as_empty[sb]));
+          __syncwarp();
         }
         if (!ok) break;
-        mma_commit(bar(misc->s_full));
-        mma_commit(bar(misc->raw_empty[st]));
-        if (flags & 2) mma_commit(bar(misc->q_empty));
+        if (elect_one()) {
+          mma_commit(bar(misc->s_full[n & 1]));
+          mma_commit(bar(misc->raw_empty[st]));
+          if (flags & 2) mma_commit(bar(misc->q_empty));
+        }
+        __syncwarp();
         if (++st == kStages) { st = 0; ++round; }
       }
-    } else if (warp >= kValueIssuer0 && warp < kValueIssuer0 + ISSUERS && lane == 0) {
-      // ---------------------------------------------------------------- value issuer j: blocks j, j + 2
-      const int j = warp - kValueIssuer0;
+    } else if (warp == kValueIssuer) {
+      // ---------------------------------------------------------------- value products (whole warp, uniform)
       const uint64_t p_desc = make_smem_desc(p_u32, 128, P_SBO, kSwizzleNone);
       int vb = 0, round = 0;
       bool ok = true;
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = wait(misc->p_full[n & 1], n >> 1, 7);
+        ok = wait_warp(misc->p_full[n & 1], n >> 1, 7);
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t fresh = misc->info[n % kInfo].flags & 1;
         const uint64_t pd = p_desc + (uint64_t)((n & 1) * (P_BYTES / 16));
 #pragma unroll 1
         for (int mb = 0; mb < NB; ++mb) {
-          ok = wait(misc->av_full[vb], round, 8);
+          ok = wait_warp(misc->av_full[vb], round, 8);
           if (!ok) break;
-          if (ISSUERS == 2 && (mb & 1) != j) {
-            mbar_arrive(bar(misc->av_empty[vb]));
-          } else {
-            tc_fence_after_sync();
-            const uint32_t d = tmem + kColO + mb * NHP, at = tmem + COL_AV + vb * 64;
+          tc_fence_after_sync();
+          const uint32_t d = tmem + kColO + mb * NHP, at = tmem + COL_AV + vb * 64;
+          if (elect_one()) {
             mma_f16_ts(d, at, pd, IDESC_V, fresh ^ 1u);
 #pragma unroll
             for (int ks = 1; ks < kTile / 16; ++ks) mma_f16_ts(d, at + ks * 8, pd + ks * 16, IDESC_V, 1u);
             mma_commit(bar(misc->av_empty[vb]));
           }
+          __syncwarp();
           if (++vb == AVB) { vb = 0; ++round; }
         }
-        if (ok) mma_commit(bar(misc->p_empty[n & 1]));
+        if (ok && elect_one()) mma_commit(bar(misc->p_empty[n & 1]));
+        __syncwarp();
       }
     }
   } else if (warp < kValueWarp0) {
     // ------------------------------------------------------------------ expansion for the scores
+    // Two groups of four warps; a group fills every other operand buffer.
     reg_alloc<kRegsWorker>();
-    const int q = warp & 3, slot = q * 32 + lane, row = slot & 63;
+    const int q = warp & 3, grp = (warp - kScoreWarp0) >> 2, slot = q * 32 + lane, row = slot & 63;
     const int cmask = f.code_mask(), chunks = r / kGroup;
-    const uint32_t lane_as = tmem + ((uint32_t)(q * 32) << 16) + COL_AS;
+    const uint32_t lane_as = tmem + ((uint32_t)(q * 32) << 16) + COL_AS + grp * 64;
     const uint32_t twist = (uint32_t)(row & cmask) * 16;
     int st = 0, round = 0;
     bool ok = true;
+    // One warp of a group polls, the others wait in a hardware barrier: polling takes issue slots.
+    auto any_bad = [&](bool bad) { return grp ? named_sync_or<5, 128>(bad) : named_sync_or<2, 128>(bad); };
     for (int n = 0; n < n_tiles; ++n) {
-      ok = __all_sync(0xffffffffu, wait(misc->raw_full[st], round, 9));
-      if (!ok) break;
+      if (q == 0) ok = wait(misc->raw_full[st], round, 9);
+      if (any_bad(!ok)) break;
       const TileInfo& info = misc->info[n % kInfo];
       const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
       const uint32_t stage = base + st * L.stage;
@@ -388,10 +394,13 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       // zero where there is no slot, so that whatever its codes are, the product is zero.
       uint32_t st_out = st_u32 + st * f.scale_row() * kTile * 2 + slot * 2;
 #pragma unroll 1
-      for (int kq = 0; kq < NB; ++kq) {
-        const int k = n * NB + kq, sb = k & 1;
-        ok = __all_sync(0xffffffffu, wait(misc->as_empty[sb], (k >> 1) + 1, 10));
-        if (!ok) break;
+      for (int kq = (n * NB + grp) & 1; kq < NB; kq += 2) {
+        const int k = n * NB + kq;                       // k mod 2 = grp
+        if (q == 0) ok = wait(misc->as_empty[grp], (k >> 1) + 1, 10);
+        if (any_bad(!ok)) {
+          ok = false;
+          break;
+        }
         tc_fence_after_sync();
         const int c_end = min(chunks, kq * 4 + 4);
 #pragma unroll 1
@@ -408,7 +417,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
                        : "memory");
           const uint32_t sc0 = s0 | (s0 << 16), sc1 = s1 | (s1 << 16);
           const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-          const uint32_t at = lane_as + sb * 64 + (c & 3) * 16;
+          const uint32_t at = lane_as + (c & 3) * 16;
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
             uint32_t v[16];
@@ -425,7 +434,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc->as_full[sb]));
+        if (lane == 0) mbar_arrive(bar(misc->as_full[grp]));
       }
       if (!ok) break;
       if (lane == 0) {
@@ -444,16 +453,21 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     const uint32_t step = 32 * f.code_row();
     int st = 0, round = 0, vb = 0, av_round = 0;
     bool ok = true;
+    // One of a page's four warps polls (see above).
+    auto any_bad = [&](bool bad) { return half ? named_sync_or<4, 128>(bad) : named_sync_or<3, 128>(bad); };
     for (int n = 0; n < n_tiles; ++n) {
-      ok = __all_sync(0xffffffffu, wait(misc->raw_full[st], round, 11) && wait(misc->scale_full[st], round, 12));
-      if (!ok) break;
+      if (q == 0) ok = wait(misc->raw_full[st], round, 11) && wait(misc->scale_full[st], round, 12);
+      if (any_bad(!ok)) break;
       const uint32_t codes = base + st * L.stage + L.codes + (half * kPageRows + lane) * f.code_row();
       const uint32_t sts = st_u32 + st * f.scale_row() * kTile * 2 + (half * kPageRows + 2 * t) * 2;
 #pragma unroll 1
       for (int mb = 0; mb < NB; ++mb) {
         const int c = mb * 4 + q;
-        ok = __all_sync(0xffffffffu, wait(misc->av_empty[vb], av_round + 1, 13));
-        if (!ok) break;
+        if (q == 0) ok = wait(misc->av_empty[vb], av_round + 1, 13);
+        if (any_bad(!ok)) {
+          ok = false;
+          break;
+        }
         tc_fence_after_sync();
         if (c < chunks) {
           const uint32_t at = codes + ((uint32_t)(c * 16) ^ twist), sc_at = sts + c * (kTile * 2);
@@ -527,8 +541,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     uint8_t* const p_row = sm + L.off_p + (HO / 8) * P_SBO + slot * 16;
     float l_acc[NHH];
     for (int n = 0; n < n_tiles; ++n) {
-      if (ok) ok = wait(misc->info_full[n % kInfo], n / kInfo, 15);
-      if (ok) ok = wait(misc->s_full, n, 16);
+      if (ok && sw == 0) ok = wait(misc->info_full[n % kInfo], n / kInfo, 15) && wait(misc->s_full[n & 1], n >> 1, 16);
       if (named_sync_or<1, kSoftmaxThreads>(!ok)) break;
       const int flags = misc->info[n % kInfo].flags;
       const int rows = slot < 64 ? misc->info[n % kInfo].rows0 : misc->info[n % kInfo].rows1;
@@ -544,17 +557,15 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       }
       float s[NHH];
       {
-        uint32_t sp[2][16];
+        uint32_t sp[16];
         tc_fence_after_sync();
-        ld_cols(lane_base + kColS, sp[0]);
-        if (ISSUERS == 2) ld_cols(lane_base + kColS + 32, sp[1]);
+        ld_cols(lane_base + kColS + (n & 1) * 32, sp);
         tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < NHH; ++i)
-          s[i] = ISSUERS == 2 ? __uint_as_float(sp[0][i]) + __uint_as_float(sp[1][i]) : __uint_as_float(sp[0][i]);
+        for (int i = 0; i < NHH; ++i) s[i] = __uint_as_float(sp[i]);
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc->s_empty));
+        if (lane == 0) mbar_arrive(bar(misc->s_empty[n & 1]));
       }
       const bool live = (slot & 63) < rows, full = __all_sync(0xffffffffu, live);
       // x = score - reference + shift in log2 units, kept in place of the raw score.
@@ -596,7 +607,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           *reinterpret_cast<uint4*>(p_row + (n & 1) * P_BYTES + i * P_SBO) =
               make_uint4(pb[4 * i], pb[4 * i + 1], pb[4 * i + 2], pb[4 * i + 3]);
       };
-      if (ok) ok = wait(misc->p_empty[n & 1], (n >> 1) + 1, 17);     // value products of tile n - 2
+      if (sw == 0 && ok) ok = wait(misc->p_empty[n & 1], (n >> 1) + 1, 17);    // value products of tile n - 2
       if (named_sync_or<1, kSoftmaxThreads>(top > kShift + kRescale)) {
         // Rare: some reference has to rise (always at a segment's first tile).
         {

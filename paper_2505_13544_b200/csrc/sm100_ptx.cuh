@@ -123,6 +123,15 @@ __device__ __forceinline__ void tc_fence_after_sync() {
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 }
 
+// True in one lane of a converged warp (always the same one).  Matrix instructions issued under it
+// by a warp whose loop is uniform keep their descriptors in uniform registers: about 23 cycles
+// each, against 60 to 80 from a single thread's loop (measured, 128 x 32 x 16).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+  return p != 0;
+}
+
 // Rendezvous of `threads` threads of the CTA on hardware barrier `id`; the second form also tells
 // whether any of them passed a true predicate.  For groups all of whose threads always get there.
 template <int ID, int THREADS>
