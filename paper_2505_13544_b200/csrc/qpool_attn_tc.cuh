@@ -25,14 +25,15 @@
 // scaled by a power of two per head, swizzled), so that a segment's query is one bulk copy.
 //
 // Roles (28 warps): warp 0 issues the score products, warp 1 the value products, warp 2 is the
-// producer; warps 4-11 expand for the scores (two groups, a quarter of r each in turn), 12-19 for the
-// values (a page of the tile each four), 20-27 softmax and epilogue.  The hot loops are short on
-// purpose: with five kinds of code on every scheduler, fetching unrolled instructions was the
-// longest stall (107 KB of them: 517 us at 128 x 16384 slots, 61 KB: 362 us).
+// producer; warps 4-19 expand, in four groups that take turns (see there); warps 20-27 are softmax
+// and epilogue.  The hot loops are short on purpose: with several kinds of code on every scheduler,
+// fetching unrolled instructions was the longest stall (107 KB of them: 517 us at 128 x 16384
+// slots, 61 KB: 362 us).
 // The online softmax raises a head's reference only when a tile exceeds it by 2^8.  Probabilities
 // are kept times 2^7: with the 2^8 they stay inside half precision.
 //
-// Every wait is bounded; after a time-out the roles unwind and qpool_combine_kernel answers with NaN.
+// Every wait is bounded; after a time-out the roles unwind, each when its own next wait runs out, and
+// qpool_combine_kernel answers with NaN.
 #pragma once
 
 #include "qpool_attn.cuh"
@@ -43,16 +44,16 @@ namespace tc {
 
 constexpr int kTile = 128;                  // slots per tile: two pages
 constexpr int kThreads = 896;
-constexpr int kStages = 3;
+constexpr int kMaxStages = 4;
 constexpr int kMaxBatch = 1022;             // prefix sums kept in shared memory
 constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2;
-constexpr int kScoreWarp0 = 4, kScoreWarps = 8, kValueWarp0 = 12, kValueWarps = 8;
+constexpr int kExpandWarp0 = 4, kExpandGroups = 4;
 constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
 constexpr int kInfo = 16;                   // ring of tile descriptions, deeper than any role's lag
 // TMEM columns: two score buffers, up to four output blocks of NHP columns, two operand
 // buffers of 64 columns for the scores and what is left, three (32 heads) or four, for the values.
 constexpr int kTmemCols = 512;
-constexpr int kColS = 0, kColO = 64, kMaxAv = 4;
+constexpr int kColS = 0, kColO = 64;
 __host__ __device__ constexpr int col_as(int nhp) { return kColO + 4 * nhp; }
 __host__ __device__ constexpr int col_av(int nhp) { return col_as(nhp) + 128; }
 __host__ __device__ constexpr int av_buffers(int nhp) { return nhp == 32 ? 3 : 4; }
@@ -60,10 +61,7 @@ static_assert(col_av(32) + 64 * av_buffers(32) <= kTmemCols && col_av(16) + 64 *
               "tensor memory budget");
 constexpr float kShift = 7.f, kRescale = 8.f;
 constexpr float kUnset = 3e38f;             // in the place of -reference: any score then exceeds it
-constexpr int kRegsControl = 40, kRegsWorker = 72;
-constexpr int kRegsAtLaunch = 65536 / kThreads / 8 * 8;
-static_assert(128 * kRegsControl + (kThreads - 128) * kRegsWorker <= kThreads * kRegsAtLaunch,
-              "register re-allocation exceeds the CTA's pool");
+constexpr int kSmemMax = 227 * 1024 - 1024;
 
 struct TileInfo {
   int b;
@@ -72,8 +70,11 @@ struct TileInfo {
 };
 
 struct Misc {
-  unsigned long long raw_full[kStages], raw_empty[kStages], scale_full[kStages];
-  unsigned long long as_full[2], as_empty[2], av_full[kMaxAv], av_empty[kMaxAv];
+  unsigned long long raw_full[kMaxStages], raw_empty[kMaxStages], scale_full[kMaxStages];
+  // Operand units (a quarter of r of one tile) are numbered through; unit k's barriers are those of k
+  // mod 4, its buffer is shared with fewer units.  Who fills unit k waits for the unit that had the
+  // buffer before, and sees every phase of that unit's barrier.
+  unsigned long long as_full[4], as_empty[4], av_full[4], av_empty[4];
   unsigned long long s_full[2], s_empty[2], p_full[2], p_empty[2], q_full, q_empty;
   unsigned long long info_full[kInfo];
   uint32_t tmem_base;
@@ -90,20 +91,27 @@ static_assert(sizeof(Misc) <= 2048, "misc region too small");
 
 struct Layout {
   int codes, scales, keys;                  // offsets in a stage
-  int stage;
+  int stage, stages;
   int off_q, q_bytes, off_p, off_st, off_misc, off_prefix, total;
   __host__ __device__ Layout(const Format& f, int nhp, int batch) {
     keys = 0;                                            // swizzled operand: 1024-byte aligned
     codes = kTile * f.key_row();
     scales = codes + kTile * f.code_row();
     stage = (scales + kTile * f.scale_row() + 1023) / 1024 * 1024;
-    off_q = kStages * stage;
     q_bytes = nhp * 2 * (f.r + f.dr);
-    off_p = off_q + (q_bytes + 1023) / 1024 * 1024;
-    off_st = off_p + 2 * kTile * nhp * 2;
-    off_misc = off_st + kStages * f.scale_row() * kTile * 2;
+    const int q_room = (q_bytes + 1023) / 1024 * 1024, p_room = 2 * kTile * nhp * 2;
+    const int scale_room = f.scale_row() * kTile * 2;
+    const int fixed = q_room + p_room + 2048 + (batch + 1) * 4 + 1024;   // 1024: alignment of the base
+    // At least three (r 512, 32 heads, d_R 64: exactly), which the expansion's waits rely on; with one
+    // unit a tile (r <= 128) always four, as many as a tile's value operands may lag.
+    stages = (kSmemMax - fixed) / (stage + scale_room);
+    if (stages > kMaxStages) stages = kMaxStages;
+    off_q = stages * stage;
+    off_p = off_q + q_room;
+    off_st = off_p + p_room;
+    off_misc = off_st + stages * scale_room;
     off_prefix = off_misc + 2048;
-    total = off_prefix + (batch + 1) * 4 + 1024;         // slack for the alignment of the base
+    total = off_prefix + (batch + 1) * 4 + 1024;
   }
 };
 
@@ -178,26 +186,25 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   uint8_t* sm = smem_raw + (base - raw);
   Misc* misc = reinterpret_cast<Misc*>(sm + L.off_misc);
   int* prefix = reinterpret_cast<int*>(sm + L.off_prefix);
-  volatile int* abort_word = &misc->abort_word;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // warp: uniform
   auto bar = [&](unsigned long long& p) { return smem_u32(&p); };
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) {
+    for (int i = 0; i < L.stages; ++i) {
       mbar_init(bar(misc->raw_full[i]), 1);
-      mbar_init(bar(misc->raw_empty[i]), kScoreWarps + kValueWarps + 1);
-      mbar_init(bar(misc->scale_full[i]), kScoreWarps);
+      mbar_init(bar(misc->raw_empty[i]), 2 * NB * 4 + 1);        // a warp of each unit, the key products
+      mbar_init(bar(misc->scale_full[i]), NB * 4);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(misc->as_full[i]), kScoreWarps / 2);
-      mbar_init(bar(misc->as_empty[i]), 1);
       mbar_init(bar(misc->s_full[i]), 1);
       mbar_init(bar(misc->s_empty[i]), kSoftmaxWarps);
       mbar_init(bar(misc->p_full[i]), kSoftmaxWarps);
       mbar_init(bar(misc->p_empty[i]), 1);
     }
-    for (int i = 0; i < kMaxAv; ++i) {
-      mbar_init(bar(misc->av_full[i]), kValueWarps);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(bar(misc->as_full[i]), 4);
+      mbar_init(bar(misc->as_empty[i]), 1);
+      mbar_init(bar(misc->av_full[i]), 4);
       mbar_init(bar(misc->av_empty[i]), 1);
     }
     for (int i = 0; i < kInfo; ++i) mbar_init(bar(misc->info_full[i]), 1);
@@ -210,7 +217,9 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tmem = misc->tmem_base;
+  // All 512 columns are this CTA's, so they start at column 0: a constant that the addresses of the
+  // matrix instructions are formed with (anything else would be an allocator's error, told as such).
+  constexpr uint32_t tmem = 0;
   grid_launch_dependents();      // this CTA owns its TMEM columns (see decode_attn_tc.cuh)
   grid_dependency_wait();
 
@@ -221,19 +230,21 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     g0 = share_begin(blockIdx.x, total, ctas);
     g1 = share_begin(blockIdx.x + 1, total, ctas);
   }
-  const int n_tiles = g1 - g0;
+  const int n_tiles = __shfl_sync(0xffffffffu, g1 - g0, 0);      // uniform
   const uint32_t q_u32 = base + L.off_q, p_u32 = base + L.off_p, st_u32 = base + L.off_st;
-  auto wait = [&](unsigned long long& b, int phase, int code) {
-    return mbar_wait_compact(bar(b), phase & 1, abort_word, a.error_word, code);
+  auto wait = [&](unsigned long long& b, int phase) { return mbar_wait_compact(bar(b), phase & 1); };
+  auto wait_warp = [&](unsigned long long& b, int phase) {                 // one answer for the warp
+    return __all_sync(0xffffffffu, wait(b, phase)) != 0;
   };
-  auto wait_warp = [&](unsigned long long& b, int phase, int code) {       // one answer for the warp
-    return __all_sync(0xffffffffu, wait(b, phase, code)) != 0;
-  };
+  bool ok = true;                // false once a wait of this thread has given up
+  if (threadIdx.x == 0 && misc->tmem_base != 0) {
+    misc->abort_word = 1;
+    atomicCAS(a.error_word, 0, 100);
+  }
 
   if (n_tiles == 0) {
     // nothing to do; the CTA falls through to the common end
-  } else if (warp < kScoreWarp0) {
-    reg_dealloc<kRegsControl>();
+  } else if (warp < kExpandWarp0) {
     if (warp == kProducerWarp && lane == 0) {
       // ---------------------------------------------------------------- producer
       int b = find_seq(prefix, a.batch, g0), seg = 0, st = 0, round = 0;
@@ -249,7 +260,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           page[i] = have > 0 && t < a.width ? __ldg(a.table + (long long)b * a.width + t) : -1;
           rows[i] = page[i] >= 0 && page[i] < a.n_pages ? min(have, kPageRows) : 0;
         }
-        if (!wait(misc->raw_empty[st], round + 1, 1)) break;
+        ok = wait(misc->raw_empty[st], round + 1);
+        if (!ok) break;
         TileInfo& info = misc->info[n % kInfo];
         info.b = b;
         info.flags = (first ? 1 : 0) | (last ? 2 : 0);
@@ -273,12 +285,13 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         }
         if (first) {
           // The segment's queries, once the score products of the segment before are done.
-          if (!wait(misc->q_empty, seg + 1, 2)) break;
+          ok = wait(misc->q_empty, seg + 1);
+          if (!ok) break;
           mbar_arrive_expect_tx(bar(misc->q_full), L.q_bytes);
           bulk_load(q_u32, a.q_image + (long long)b * L.q_bytes, L.q_bytes, bar(misc->q_full));
           ++seg;
         }
-        if (++st == kStages) { st = 0; ++round; }
+        if (++st == L.stages) { st = 0; ++round; }
       }
     } else if (warp == kScoreIssuer) {
       // ---------------------------------------------------------------- score products (whole warp, uniform)
@@ -287,17 +300,16 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       const uint64_t q_desc = make_smem_desc(q_u32, 16, 1024, kSwizzle128B);
       const uint64_t qk_desc = make_smem_desc(q_u32 + NHP * 2 * r, 16, key_sbo, mode);
       int seg = 0, st = 0, round = 0;
-      bool ok = true;
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = wait_warp(misc->raw_full[st], round, 3);
+        ok = wait_warp(misc->raw_full[st], round);
         if (!ok) break;
         const int flags = misc->info[n % kInfo].flags;
         if (flags & 1) {
-          ok = wait_warp(misc->q_full, seg, 4);
+          ok = wait_warp(misc->q_full, seg);
           if (!ok) break;
           ++seg;
         }
-        ok = wait_warp(misc->s_empty[n & 1], (n >> 1) + 1, 5);
+        ok = wait_warp(misc->s_empty[n & 1], (n >> 1) + 1);
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t d = tmem + kColS + (n & 1) * 32;
@@ -313,21 +325,21 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         __syncwarp();
 #pragma unroll 1
         for (int kq = 0; kq < NB; ++kq) {
-          const int k = n * NB + kq, sb = k & 1;
-          ok = wait_warp(misc->as_full[sb], k >> 1, 6);
+          const int k = n * NB + kq;
+          ok = wait_warp(misc->as_full[k & 3], k >> 2);
           if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t at = tmem + COL_AS + sb * 64;
-          const uint64_t panel = q_desc + (uint64_t)(kq * 2 * NHP * 8);
+          const uint32_t at = tmem + COL_AS + (k & 1) * 64;
+          const uint32_t panel = (uint32_t)q_desc + kq * 2 * NHP * 8, hi = (uint32_t)(q_desc >> 32);
           if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) mma_f16_ts(d, at + ks * 8, panel + ks * 2, IDESC_S, 1u);
+            for (int ks = 0; ks < 4; ++ks) mma_f16_ts(d, at + ks * 8, panel + ks * 2, hi, IDESC_S, 1u);
             if (kq * 128 + 64 < r) {
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks)
-                mma_f16_ts(d, at + 32 + ks * 8, panel + NHP * 8 + ks * 2, IDESC_S, 1u);
+                mma_f16_ts(d, at + 32 + ks * 8, panel + NHP * 8 + ks * 2, hi, IDESC_S, 1u);
             }
-            mma_commit(bar(misc->as_empty[sb]));
+            mma_commit(bar(misc->as_empty[k & 3]));
           }
           __syncwarp();
         }
@@ -338,86 +350,94 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           if (flags & 2) mma_commit(bar(misc->q_empty));
         }
         __syncwarp();
-        if (++st == kStages) { st = 0; ++round; }
+        if (++st == L.stages) { st = 0; ++round; }
       }
     } else if (warp == kValueIssuer) {
       // ---------------------------------------------------------------- value products (whole warp, uniform)
       const uint64_t p_desc = make_smem_desc(p_u32, 128, P_SBO, kSwizzleNone);
-      int vb = 0, round = 0;
-      bool ok = true;
+      int vb = 0;
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = wait_warp(misc->p_full[n & 1], n >> 1, 7);
+        ok = wait_warp(misc->p_full[n & 1], n >> 1);
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t fresh = misc->info[n % kInfo].flags & 1;
-        const uint64_t pd = p_desc + (uint64_t)((n & 1) * (P_BYTES / 16));
+        const uint32_t pd = (uint32_t)p_desc + (n & 1) * (P_BYTES / 16), hi = (uint32_t)(p_desc >> 32);
 #pragma unroll 1
         for (int mb = 0; mb < NB; ++mb) {
-          ok = wait_warp(misc->av_full[vb], round, 8);
+          const int k = n * NB + mb;
+          ok = wait_warp(misc->av_full[k & 3], k >> 2);
           if (!ok) break;
           tc_fence_after_sync();
           const uint32_t d = tmem + kColO + mb * NHP, at = tmem + COL_AV + vb * 64;
           if (elect_one()) {
-            mma_f16_ts(d, at, pd, IDESC_V, fresh ^ 1u);
+            mma_f16_ts(d, at, pd, hi, IDESC_V, fresh ^ 1u);
 #pragma unroll
-            for (int ks = 1; ks < kTile / 16; ++ks) mma_f16_ts(d, at + ks * 8, pd + ks * 16, IDESC_V, 1u);
-            mma_commit(bar(misc->av_empty[vb]));
+            for (int ks = 1; ks < kTile / 16; ++ks) mma_f16_ts(d, at + ks * 8, pd + ks * 16, hi, IDESC_V, 1u);
+            mma_commit(bar(misc->av_empty[k & 3]));
           }
           __syncwarp();
-          if (++vb == AVB) { vb = 0; ++round; }
+          if (++vb == AVB) vb = 0;
         }
         if (ok && elect_one()) mma_commit(bar(misc->p_empty[n & 1]));
         __syncwarp();
       }
     }
-  } else if (warp < kValueWarp0) {
-    // ------------------------------------------------------------------ expansion for the scores
-    // Two groups of four warps; a group fills every other operand buffer.
-    reg_alloc<kRegsWorker>();
-    const int q = warp & 3, grp = (warp - kScoreWarp0) >> 2, slot = q * 32 + lane, row = slot & 63;
-    const int cmask = f.code_mask(), chunks = r / kGroup;
-    const uint32_t lane_as = tmem + ((uint32_t)(q * 32) << 16) + COL_AS + grp * 64;
-    const uint32_t twist = (uint32_t)(row & cmask) * 16;
-    int st = 0, round = 0;
-    bool ok = true;
-    // One warp of a group polls, the others wait in a hardware barrier: polling takes issue slots.
-    auto any_bad = [&](bool bad) { return grp ? named_sync_or<5, 128>(bad) : named_sync_or<2, 128>(bad); };
-    for (int n = 0; n < n_tiles; ++n) {
-      if (q == 0) ok = wait(misc->raw_full[st], round, 9);
-      if (any_bad(!ok)) break;
-      const TileInfo& info = misc->info[n % kInfo];
-      const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
-      const uint32_t stage = base + st * L.stage;
-      const uint32_t codes = stage + L.codes + slot * f.code_row();
-      uint32_t scales = stage + L.scales + slot * f.scale_row();
-      // The scales also go out as half precision, a group's 128 slots in a row, for the value warps;
-      // zero where there is no slot, so that whatever its codes are, the product is zero.
-      uint32_t st_out = st_u32 + st * f.scale_row() * kTile * 2 + slot * 2;
+  } else if (warp < kSoftmaxWarp0) {
+    // ------------------------------------------------------------------ expansion
+    // Four groups of four warps take the units in turn, a group expanding unit k for the scores and then
+    // unit k - NB, the same quarter of the tile before, for the values: the work is even whatever
+    // r is, and a tile's probabilities are usually there when its value units are wanted.
+    const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2, t = lane & 3;
+    const int slot = q * 32 + lane, row = slot & 63;
+    const int cmask = f.code_mask(), chunks = r / kGroup, code_row = f.code_row();
+    const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16);
+    const uint32_t twist = (uint32_t)(lane & cmask) * 16;       // rows lane, lane + 32, ... twist alike
+    const int n_units = n_tiles * NB;
+    // Tile n, quarter kq of unit k, the stage of tile n and how often the ring has come round; the
+    // value unit is the same quarter of tile n - 1.
+    int n = 0, kq = grp, st = 0, round = 0;
+    auto next_tile = [&]() {
+      ++n;
+      if (++st == L.stages) { st = 0; ++round; }
+    };
 #pragma unroll 1
-      for (int kq = (n * NB + grp) & 1; kq < NB; kq += 2) {
-        const int k = n * NB + kq;                       // k mod 2 = grp
-        if (q == 0) ok = wait(misc->as_empty[grp], (k >> 1) + 1, 10);
-        if (any_bad(!ok)) {
-          ok = false;
-          break;
-        }
+    while (kq >= NB) { kq -= NB; next_tile(); }
+    // One warp of a group polls, the others wait in a hardware barrier: polling takes issue slots.  The
+    // pollers keep off the schedulers (warp mod 4) of the two issuing warps.
+    const bool poller = q == (grp < 2 ? 3 : 2);
+    auto any_bad = [&](bool bad) { return named_sync_or<128>(2 + grp, bad); };
+#pragma unroll 1
+    for (int k = grp; k < n_units + NB; k += kExpandGroups) {
+      if (k < n_units) {
+        if (poller)
+          // The buffer first: that unit k - 2 has been used also tells that the stage's phase is the one
+          // before this tile's or later, which its parity alone would not.
+          ok = (k < 2 || wait(misc->as_empty[(k - 2) & 3], (k - 2) >> 2)) && wait(misc->raw_full[st], round);
+        if (any_bad(!ok)) break;
         tc_fence_after_sync();
+        const TileInfo& info = misc->info[n % kInfo];
+        const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
+        const uint32_t stage = base + st * L.stage;
+        const uint32_t codes = stage + L.codes + slot * code_row, scales = stage + L.scales + slot * f.scale_row();
+        // The scales also go out as half precision, a group's 128 slots in a row, for the value units;
+        // zero where there is no slot, so that whatever its codes are, the product is zero.
+        const uint32_t st_out = st_u32 + st * f.scale_row() * kTile * 2 + slot * 2;
         const int c_end = min(chunks, kq * 4 + 4);
+        uint32_t at = lane_tm + COL_AS + (k & 1) * 64;
 #pragma unroll 1
-        for (int c = kq * 4; c < c_end; c += 2) {
+        for (int c = kq * 4; c < c_end; c += 2, at += 32) {
           // Two chunks at a time: their loads overlap, and a row of scales is a multiple of 2 bytes.
           const uint4 w0 = lds128(codes + ((uint32_t)(c * 16) ^ twist));
           const uint4 w1 = lds128(codes + ((uint32_t)(c * 16 + 16) ^ twist));
           uint32_t two;
           asm volatile("{\n\t.reg .u16 x;\n\tld.shared.u16 x, [%1];\n\tcvt.u32.u16 %0, x;\n\t}"
                        : "=r"(two) : "r"(scales + c));
-          const uint32_t s0 = (two & 0xffu) << 7, s1 = (two >> 8) << 7;
-          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + c * (kTile * 2)), "h"((uint16_t)(s0 & live)) : "memory");
-          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + (c + 1) * (kTile * 2)), "h"((uint16_t)(s1 & live))
+          const uint32_t s01 = __byte_perm(two, 0, 0x4140) << 7, out = s01 & live;      // both as half precision
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + c * (kTile * 2)), "h"((uint16_t)out) : "memory");
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + (c + 1) * (kTile * 2)), "h"((uint16_t)(out >> 16))
                        : "memory");
-          const uint32_t sc0 = s0 | (s0 << 16), sc1 = s1 | (s1 << 16);
+          const uint32_t sc0 = __byte_perm(s01, 0, 0x1010), sc1 = __byte_perm(s01, 0, 0x3232);
           const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-          const uint32_t at = lane_as + (c & 3) * 16;
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
             uint32_t v[16];
@@ -434,81 +454,77 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc->as_full[grp]));
-      }
-      if (!ok) break;
-      if (lane == 0) {
-        mbar_arrive(bar(misc->scale_full[st]));
-        mbar_arrive(bar(misc->raw_empty[st]));
-      }
-      if (++st == kStages) { st = 0; ++round; }
-    }
-  } else if (warp < kSoftmaxWarp0) {
-    // ------------------------------------------------------------------ expansion for the values
-    reg_alloc<kRegsWorker>();
-    const int q = warp & 3, half = (warp - kValueWarp0) >> 2, t = lane & 3;
-    const int cmask = f.code_mask(), chunks = r / kGroup;
-    const uint32_t lane_av = tmem + ((uint32_t)(q * 32) << 16) + COL_AV + half * 32;
-    const uint32_t twist = (uint32_t)(lane & cmask) * 16;      // rows lane and lane + 32 twist alike
-    const uint32_t step = 32 * f.code_row();
-    int st = 0, round = 0, vb = 0, av_round = 0;
-    bool ok = true;
-    // One of a page's four warps polls (see above).
-    auto any_bad = [&](bool bad) { return half ? named_sync_or<4, 128>(bad) : named_sync_or<3, 128>(bad); };
-    for (int n = 0; n < n_tiles; ++n) {
-      if (q == 0) ok = wait(misc->raw_full[st], round, 11) && wait(misc->scale_full[st], round, 12);
-      if (any_bad(!ok)) break;
-      const uint32_t codes = base + st * L.stage + L.codes + (half * kPageRows + lane) * f.code_row();
-      const uint32_t sts = st_u32 + st * f.scale_row() * kTile * 2 + (half * kPageRows + 2 * t) * 2;
-#pragma unroll 1
-      for (int mb = 0; mb < NB; ++mb) {
-        const int c = mb * 4 + q;
-        if (q == 0) ok = wait(misc->av_empty[vb], av_round + 1, 13);
-        if (any_bad(!ok)) {
-          ok = false;
-          break;
+        if (lane == 0) {
+          mbar_arrive(bar(misc->as_full[k & 3]));
+          if (NB != kExpandGroups) mbar_arrive(bar(misc->scale_full[st]));
+          mbar_arrive(bar(misc->raw_empty[st]));
         }
+      }
+      const int kv = k - NB;
+      if (kv >= 0) {
+        const int c = kq * 4 + q, stv = st == 0 ? L.stages - 1 : st - 1, roundv = st == 0 ? round - 1 : round;
+        if (poller)
+          // With four units a tile this group has itself expanded this very quarter for the scores: it
+          // has waited for the tile and written the scales.
+          ok = (kv < AVB || wait(misc->av_empty[(kv - AVB) & 3], (kv - AVB) >> 2)) &&
+               (NB == kExpandGroups || (wait(misc->raw_full[stv], roundv) && wait(misc->scale_full[stv], roundv)));
+        if (any_bad(!ok)) break;
         tc_fence_after_sync();
         if (c < chunks) {
-          const uint32_t at = codes + ((uint32_t)(c * 16) ^ twist), sc_at = sts + c * (kTile * 2);
+          uint32_t from = base + stv * L.stage + L.codes + lane * code_row + ((uint32_t)(c * 16) ^ twist);
+          uint32_t sc_at = st_u32 + (stv * f.scale_row() + c) * (kTile * 2) + 4 * t;
+          uint32_t col = lane_tm + COL_AV + (kv % AVB) * 64;
 #pragma unroll 1
-          for (int h = 0; h < 2; ++h) {
-            uint32_t w[4], v[4][4];
-            ldsm_x4_trans(at + h * step, w);
+          for (int h = 0; h < 2; ++h) {                        // 64 slots each
+            uint32_t w[2][4];
+            ldsm_x4_trans(from, w[0]);
+            ldsm_x4_trans(from + 32 * code_row, w[1]);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-              uint32_t sc;
-              asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sc_at + (h * 32 + m * 8) * 2));
-              decode_pairs(w[m], v[m]);
+            for (int i2 = 0; i2 < 2; ++i2) {
+              uint32_t v[4][4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) v[m][i] = mul_h2(v[m][i], sc);
+              for (int m = 0; m < 4; ++m) {
+                uint32_t sc;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sc_at + i2 * 64 + m * 16));
+                decode_pairs(w[i2][m], v[m]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[m][i] = mul_h2(v[m][i], sc);
+              }
+              const uint32_t to = col + i2 * 16;
+              tmem_st_16x128_x4(to, v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]);
+              tmem_st_16x128_x4(to + (16u << 16), v[0][2], v[0][3], v[1][2], v[1][3], v[2][2], v[2][3], v[3][2],
+                                v[3][3]);
             }
-            const uint32_t col = lane_av + vb * 64 + h * 16;
-            tmem_st_16x128_x4(col, v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]);
-            tmem_st_16x128_x4(col + (16u << 16), v[0][2], v[0][3], v[1][2], v[1][3], v[2][2], v[2][3], v[3][2], v[3][3]);
+            from += 64 * code_row;
+            sc_at += 128;
+            col += 32;
           }
         }
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc->av_full[vb]));
-        if (++vb == AVB) { vb = 0; ++av_round; }
+        if (lane == 0) {
+          mbar_arrive(bar(misc->av_full[kv & 3]));
+          mbar_arrive(bar(misc->raw_empty[stv]));
+        }
       }
-      if (!ok) break;
-      if (lane == 0) mbar_arrive(bar(misc->raw_empty[st]));
-      if (++st == kStages) { st = 0; ++round; }
+      if (NB == 4) {
+        next_tile();
+      } else {
+        kq += kExpandGroups;
+#pragma unroll 1
+        while (kq >= NB) { kq -= NB; next_tile(); }
+      }
     }
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
     // Two groups of four warps: group gr owns heads [gr * NHH, (gr + 1) * NHH) of the tile's 128
     // slots, a slot per thread.  They leave the loop together (they agree on it once a tile, before
     // anything that depends on the tile's description), so the hardware barrier always completes.
-    reg_alloc<kRegsWorker>();
     constexpr int NHH = NHP / 2;
     const int sw = warp - kSoftmaxWarp0, gr = sw >> 2, q = warp & 3, HO = gr * NHH;
     const int sidx = sw * 32 + lane, slot = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + HO;
-    bool ok = true;
     auto group_sync = [&]() { named_sync<1, kSoftmaxThreads>(); };
     auto ld_cols = [&](uint32_t addr, uint32_t (&v)[16]) {
       if (NHH == 16) tmem_ld_x16(addr, v); else tmem_ld_x8(addr, v);
@@ -541,8 +557,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     uint8_t* const p_row = sm + L.off_p + (HO / 8) * P_SBO + slot * 16;
     float l_acc[NHH];
     for (int n = 0; n < n_tiles; ++n) {
-      if (ok && sw == 0) ok = wait(misc->info_full[n % kInfo], n / kInfo, 15) && wait(misc->s_full[n & 1], n >> 1, 16);
-      if (named_sync_or<1, kSoftmaxThreads>(!ok)) break;
+      if (ok && sw == 3) ok = wait(misc->info_full[n % kInfo], n / kInfo) && wait(misc->s_full[n & 1], n >> 1);
+      if (named_sync_or<kSoftmaxThreads>(1, !ok)) break;
       const int flags = misc->info[n % kInfo].flags;
       const int rows = slot < 64 ? misc->info[n % kInfo].rows0 : misc->info[n % kInfo].rows1;
       if (flags & 1) {
@@ -607,8 +623,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           *reinterpret_cast<uint4*>(p_row + (n & 1) * P_BYTES + i * P_SBO) =
               make_uint4(pb[4 * i], pb[4 * i + 1], pb[4 * i + 2], pb[4 * i + 3]);
       };
-      if (sw == 0 && ok) ok = wait(misc->p_empty[n & 1], (n >> 1) + 1, 17);    // value products of tile n - 2
-      if (named_sync_or<1, kSoftmaxThreads>(top > kShift + kRescale)) {
+      if (sw == 3 && ok) ok = wait(misc->p_empty[n & 1], (n >> 1) + 1);    // value products of tile n - 2
+      if (named_sync_or<kSoftmaxThreads>(1, top > kShift + kRescale)) {
         // Rare: some reference has to rise (always at a segment's first tile).
         {
           float x[NHH];
@@ -629,7 +645,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         for (int i = 0; i < NHH; ++i) l_acc[i] *= misc->fac[HO + i];
         if (!(flags & 1)) {
           // O is scaled to the old references: wait for the previous tile's products, rescale.
-          if (ok) ok = wait(misc->p_empty[(n - 1) & 1], (n - 1) >> 1, 19);
+          if (ok) ok = wait(misc->p_empty[(n - 1) & 1], (n - 1) >> 1);
           ok = __all_sync(0xffffffffu, ok);              // TMEM accesses are whole-warp operations
           if (ok) {
             tc_fence_after_sync();
@@ -679,7 +695,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       if (ok && sidx == 0 && g + 1 == prefix[b + 1])
         a.seq_parts[b] = whole ? make_int2(0, 0) : make_int2(c0 + b, (int)blockIdx.x - c0 + 1);
       group_sync();
-      if (ok) ok = wait(misc->p_empty[n & 1], n >> 1, 20);           // the last value products
+      if (ok) ok = wait(misc->p_empty[n & 1], n >> 1);           // the last value products
       ok = __all_sync(0xffffffffu, ok);
       if (ok) {
         tc_fence_after_sync();
@@ -707,8 +723,12 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     }
   }
 
+  if (!ok) {
+    misc->abort_word = 1;
+    atomicCAS(a.error_word, 0, 1 + warp);
+  }
   __syncthreads();
-  if (*abort_word) {
+  if (misc->abort_word) {
     // Give copies that may still be in flight time to land before the CTA's memory is reused.
     const uint64_t t0 = global_timer_ns();
     while (global_timer_ns() - t0 < 100000ull) __nanosleep(1000);
@@ -716,7 +736,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   if (warp == kProducerWarp) {
     __syncwarp();
     tc_fence_after_sync();
-    tmem_dealloc(tmem, kTmemCols);
+    tmem_dealloc(misc->tmem_base, kTmemCols);
   }
 }
 

@@ -83,23 +83,27 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return mbar_wait_for(bar, parity, abort_word, error_word, code, kWaitBudgetNs);
 }
 
-// The same wait as few instructions, for kernels whose roles would otherwise not fit the
-// instruction cache together: one polling loop, the clock read on every 256th poll only.
-__device__ __forceinline__ bool mbar_wait_compact(uint32_t bar, uint32_t parity, volatile int* abort_word,
-                                                  int* error_word, int code) {
-  uint32_t polls = 0, t0 = 0;
-  while (!mbar_try_wait(bar, parity)) {
-    if ((++polls & 255u) == 0u) {
-      const uint32_t now = (uint32_t)(global_timer_ns() >> 20);          // about milliseconds
-      if (polls == 256u) t0 = now;
-      if (*abort_word || now - t0 > (uint32_t)(kWaitBudgetNs >> 20)) {
-        *abort_word = 1;
-        atomicCAS(error_word, 0, code);
-        return false;
-      }
-    }
-  }
-  return true;
+// A bounded wait in as few instructions as it takes, for kernels whose roles would otherwise not fit the
+// instruction cache together: gives up 2^31 cycles (about a second) after it began and says so;
+// reporting is left to the caller.
+__device__ __forceinline__ bool mbar_wait_compact(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .u32 t0, t;\n\t"
+      "mov.u32 t0, %clock;\n"
+      "POLL:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "@p bra DONE;\n\t"
+      "mov.u32 t, %clock;\n\t"
+      "sub.u32 t, t, t0;\n\t"
+      "setp.lt.u32 q, t, 0x7fffffff;\n\t"
+      "@q bra POLL;\n"
+      "DONE:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(kSuspendHintNs)
+      : "memory");
+  return ok != 0;
 }
 
 // 2^x by the special-function unit (about 2 ulp; flushes denormals): enough for probabilities
@@ -138,8 +142,8 @@ template <int ID, int THREADS>
 __device__ __forceinline__ void named_sync() {
   asm volatile("barrier.cta.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory");
 }
-template <int ID, int THREADS>
-__device__ __forceinline__ bool named_sync_or(bool p) {
+template <int THREADS>
+__device__ __forceinline__ bool named_sync_or(int id, bool p) {
   int r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
@@ -147,7 +151,7 @@ __device__ __forceinline__ bool named_sync_or(bool p) {
       "barrier.cta.red.or.pred q, %2, %3, p;\n\t"
       "selp.b32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"((int)p), "n"(ID), "n"(THREADS)
+      : "r"((int)p), "r"(id), "n"(THREADS)
       : "memory");
   return r != 0;
 }
@@ -379,6 +383,19 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uin
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// The same with the B descriptor as its two words: only the low one (the address) changes between the
+// instructions of a loop, so advancing it is one 32-bit addition.
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi,
+                                           uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 b, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 
