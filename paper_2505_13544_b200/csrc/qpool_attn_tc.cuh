@@ -236,6 +236,9 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   auto wait_warp = [&](unsigned long long& b, int phase) {                 // one answer for the warp
     return __all_sync(0xffffffffu, wait(b, phase)) != 0;
   };
+  // Asks without waiting.  While the expanding warps keep the memory instruction queues full an answer
+  // takes some 300 cycles, so the issuing warps ask for what comes next before they issue what is there.
+  auto ask = [&](unsigned long long& b, int phase) { return mbar_test(bar(b), phase & 1); };
   bool ok = true;                // false once a wait of this thread has given up
   if (threadIdx.x == 0 && misc->tmem_base != 0) {
     misc->abort_word = 1;
@@ -300,8 +303,9 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       const uint64_t q_desc = make_smem_desc(q_u32, 16, 1024, kSwizzle128B);
       const uint64_t qk_desc = make_smem_desc(q_u32 + NHP * 2 * r, 16, key_sbo, mode);
       int seg = 0, st = 0, round = 0;
+      bool unit_there = false, raw_there = false, room_there = false;
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = wait_warp(misc->raw_full[st], round);
+        ok = __all_sync(0xffffffffu, raw_there) || wait_warp(misc->raw_full[st], round);
         if (!ok) break;
         const int flags = misc->info[n % kInfo].flags;
         if (flags & 1) {
@@ -309,7 +313,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           if (!ok) break;
           ++seg;
         }
-        ok = wait_warp(misc->s_empty[n & 1], (n >> 1) + 1);
+        ok = __all_sync(0xffffffffu, room_there) || wait_warp(misc->s_empty[n & 1], (n >> 1) + 1);
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t d = tmem + kColS + (n & 1) * 32;
@@ -326,8 +330,14 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
 #pragma unroll 1
         for (int kq = 0; kq < NB; ++kq) {
           const int k = n * NB + kq;
-          ok = wait_warp(misc->as_full[k & 3], k >> 2);
+          ok = __all_sync(0xffffffffu, unit_there) || wait_warp(misc->as_full[k & 3], k >> 2);
           if (!ok) break;
+          unit_there = ask(misc->as_full[(k + 1) & 3], (k + 1) >> 2);
+          if (kq + 1 == NB) {
+            const bool wrap = st + 1 == L.stages;
+            raw_there = ask(misc->raw_full[wrap ? 0 : st + 1], wrap ? round + 1 : round);
+            room_there = ask(misc->s_empty[(n + 1) & 1], ((n + 1) >> 1) + 1);
+          }
           tc_fence_after_sync();
           const uint32_t at = tmem + COL_AS + (k & 1) * 64;
           const uint32_t panel = (uint32_t)q_desc + kq * 2 * NHP * 8, hi = (uint32_t)(q_desc >> 32);
@@ -356,6 +366,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       // ---------------------------------------------------------------- value products (whole warp, uniform)
       const uint64_t p_desc = make_smem_desc(p_u32, 128, P_SBO, kSwizzleNone);
       int vb = 0;
+      bool unit_there = false;
       for (int n = 0; n < n_tiles && ok; ++n) {
         ok = wait_warp(misc->p_full[n & 1], n >> 1);
         if (!ok) break;
@@ -365,8 +376,9 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
 #pragma unroll 1
         for (int mb = 0; mb < NB; ++mb) {
           const int k = n * NB + mb;
-          ok = wait_warp(misc->av_full[k & 3], k >> 2);
+          ok = __all_sync(0xffffffffu, unit_there) || wait_warp(misc->av_full[k & 3], k >> 2);
           if (!ok) break;
+          unit_there = ask(misc->av_full[(k + 1) & 3], (k + 1) >> 2);
           tc_fence_after_sync();
           const uint32_t d = tmem + kColO + mb * NHP, at = tmem + COL_AV + vb * 64;
           if (elect_one()) {
@@ -402,18 +414,14 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     };
 #pragma unroll 1
     while (kq >= NB) { kq -= NB; next_tile(); }
-    // One warp of a group polls, the others wait in a hardware barrier: polling takes issue slots.  The
-    // pollers keep off the schedulers (warp mod 4) of the two issuing warps.
-    const bool poller = q == (grp < 2 ? 3 : 2);
-    auto any_bad = [&](bool bad) { return named_sync_or<128>(2 + grp, bad); };
 #pragma unroll 1
     for (int k = grp; k < n_units + NB; k += kExpandGroups) {
       if (k < n_units) {
-        if (poller)
-          // The buffer first: that unit k - 2 has been used also tells that the stage's phase is the one
-          // before this tile's or later, which its parity alone would not.
-          ok = (k < 2 || wait(misc->as_empty[(k - 2) & 3], (k - 2) >> 2)) && wait(misc->raw_full[st], round);
-        if (any_bad(!ok)) break;
+        // The buffer first: that unit k - 2 has been used also tells that the stage's phase is the one
+        // before this tile's or later, which its parity alone would not.
+        ok = (k < 2 || wait(misc->as_empty[(k - 2) & 3], (k - 2) >> 2)) && wait(misc->raw_full[st], round);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
         tc_fence_after_sync();
         const TileInfo& info = misc->info[n % kInfo];
         const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
@@ -463,12 +471,12 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       const int kv = k - NB;
       if (kv >= 0) {
         const int c = kq * 4 + q, stv = st == 0 ? L.stages - 1 : st - 1, roundv = st == 0 ? round - 1 : round;
-        if (poller)
-          // With four units a tile this group has itself expanded this very quarter for the scores: it
+        // With four units a tile this group has itself expanded this very quarter for the scores: it
           // has waited for the tile and written the scales.
           ok = (kv < AVB || wait(misc->av_empty[(kv - AVB) & 3], (kv - AVB) >> 2)) &&
                (NB == kExpandGroups || (wait(misc->raw_full[stv], roundv) && wait(misc->scale_full[stv], roundv)));
-        if (any_bad(!ok)) break;
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
         tc_fence_after_sync();
         if (c < chunks) {
           uint32_t from = base + stv * L.stage + L.codes + lane * code_row + ((uint32_t)(c * 16) ^ twist);

@@ -57,6 +57,19 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 
+// The same question without ever suspending the thread.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Every wait in these kernels is bounded: it gives up after kWaitBudgetNs of wall time (or
 // as soon as another thread of the CTA has given up), raises the CTA-wide abort word and
 // records a code in the global error word.  Callers unwind without touching the barrier again.
@@ -94,6 +107,7 @@ __device__ __forceinline__ bool mbar_wait_compact(uint32_t bar, uint32_t parity)
       "POLL:\n\t"
       "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
       "@p bra DONE;\n\t"
+      "nanosleep.u32 64;\n\t"
       "mov.u32 t, %clock;\n\t"
       "sub.u32 t, t, t0;\n\t"
       "setp.lt.u32 q, t, 0x7fffffff;\n\t"
