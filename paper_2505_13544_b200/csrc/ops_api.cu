@@ -137,8 +137,10 @@ int launch_dependent(K* kernel, dim3 grid, int threads, size_t smem, cudaStream_
 
 template <typename T>
 int launch_combine(const qp::AttnArgs& a, cudaStream_t st) {
-  const int pieces = ceil_div(a.n_heads * a.f.r, qp::kCombineThreads * 4);
-  return launch_dependent(qp::qpool_combine_kernel<T>, dim3(pieces, a.batch), qp::kCombineThreads, 0, st, a);
+  // As many CTAs as there can be pieces of split or empty sequences, six per SM at most.
+  const long long pieces = (long long)a.batch * a.n_heads * ceil_div(a.f.r, qp::kCombineCols), most = 6 * kPlanSms;
+  return launch_dependent(qp::qpool_combine_kernel<T>, dim3((unsigned)(pieces < most ? pieces : most)),
+                          qp::kCombineThreads, (size_t)a.batch * 4, st, a);
 }
 
 template <typename T, int MH>
@@ -217,12 +219,16 @@ int mtla_slot_map(const int32_t* held, const int32_t* fresh, int32_t B, int32_t 
   a.n_free = n_free;
   a.n_tokens = n_tokens;
   a.vec = aligned(out->seq, 16) && aligned(out->position, 16) && aligned(out->slot, 16) && aligned(out->store, 16);
-  const size_t smem = 2 * ((size_t)B + 1) * 4;
-  if (!raise_smem<sm::slot_map_kernel>(dev.device())) return MTLA_ERR_CUDA;
-  const int work = sm::kThreads * sm::kPerThread;
-  const int ctas = (int)(((long long)n_tokens + work - 1) / work), most = 2 * dev.sm_count();
-  const cudaError_t e = launch_kernel(sm::slot_map_kernel, dim3(ctas < 1 ? 1 : ctas < most ? ctas : most),
-                                      dim3(sm::kThreads), smem, static_cast<cudaStream_t>(stream), true, a);
+  const size_t smem = (3 * (size_t)B + 2) * 4;
+  // Four tokens a thread once that still gives every SM a CTA.
+  const bool four = n_tokens >= 4 * sm::kThreads * dev.sm_count();
+  if (!(four ? raise_smem<sm::slot_map_kernel<4>>(dev.device()) : raise_smem<sm::slot_map_kernel<1>>(dev.device())))
+    return MTLA_ERR_CUDA;
+  const int work = sm::kThreads * (four ? 4 : 1);
+  const int ctas = (int)(((long long)n_tokens + work - 1) / work), most = 4 * dev.sm_count();
+  const cudaError_t e = launch_kernel(four ? sm::slot_map_kernel<4> : sm::slot_map_kernel<1>,
+                                      dim3(ctas < 1 ? 1 : ctas < most ? ctas : most), dim3(sm::kThreads), smem,
+                                      static_cast<cudaStream_t>(stream), true, a);
   if (e != cudaSuccess) cudaGetLastError();
   return e == cudaSuccess ? MTLA_OK : MTLA_ERR_CUDA;
 }
@@ -290,7 +296,7 @@ int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int3
               aligned(t.x, 16) && aligned(t.y, 16);
   }
   if (n_tokens == 0) return MTLA_OK;
-  long long elements = 0;
+  long long units = 0;
   for (int n = 0; n < n_tensors; ++n) {
     const mtla_rope_tensor& t = tensors[n];
     const int v = use_vec ? vec : 1;
@@ -301,13 +307,14 @@ int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int3
     q.x_head = t.x_head_stride;
     q.y_token = t.y_token_stride;
     q.y_head = t.y_head_stride;
-    q.heads = t.n_heads;
-    q.width = t.width;
     q.first = t.first;
-    q.copy_units = (t.width - d) / v;
-    q.units = q.copy_units + (half ? d / 2 / v : (use_vec ? d / v : d / 2));
-    elements += (long long)t.n_heads * t.width;
+    q.copy_units = t.x == t.y ? 0 : (t.width - d) / v;
+    q.units.set(q.copy_units + (half ? d / 2 / v : (use_vec ? d / v : d / 2)));
+    q.all_units = t.n_heads * (int)q.units.d;
+    units += q.all_units;
   }
+  if (units > (1 << 26)) return MTLA_ERR_UNSUPPORTED_SHAPE;        // 8 tokens of it have to stay below 2^31
+  a.per_token.set((int)units);
   a.positions = positions;
   a.magnitude = magnitude;
   a.n_tensors = n_tensors;
@@ -316,10 +323,10 @@ int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int3
   a.inverse = inverse != 0;
   OnDeviceOf dev(tensors[0].y);
   if (dev.status() != MTLA_OK) return dev.status();
-  // Tokens per CTA: enough for two 16-byte units per thread, as long as every SM keeps several CTAs.
+  // Tokens per CTA: enough for four units per thread twice over, as long as every SM keeps several CTAs.
   int per = 1;
-  while (per < rp::kMaxTokens && per * elements < 2ll * rp::kThreads * vec &&
-         (n_tokens + 2 * per - 1) / (2 * per) >= 4 * dev.sm_count())
+  while (per < rp::kMaxTokens && per * units < 8ll * rp::kThreads &&
+         (n_tokens + 2 * per - 1) / (2 * per) >= 8 * dev.sm_count())
     per *= 2;
   a.tokens_per_cta = per;
   const dim3 grid(ceil_div(n_tokens, per));

@@ -488,53 +488,169 @@ __global__ void __launch_bounds__(kAttnThreads) qpool_attend_kernel(AttnArgs a) 
 }
 
 // Joins the partials of sequences that several CTAs worked on, and answers for sequences without a
-// slot: zeros and a logarithm of minus infinity.  Grid (pieces of n_heads * r, batch).
-constexpr int kCombineThreads = 256;
+// slot: zeros and a logarithm of minus infinity.  Every CTA lists these sequences (the others are
+// finished) and takes pieces of them in turn.  With few parts (a large batch: two parts for most
+// sequences) a piece is 1024 elements, four a thread, which weighs the parts itself.  With many (a
+// few long sequences over every SM) a piece is 128 columns of one head, eight groups of parts
+// by 32 threads of four columns, so that many loads are in flight: one way for both cost 68 us for 148
+// parts of one sequence, the other 190 us for 128 sequences of two (16 and 32 heads, r 512).  Parts
+// are added in a fixed order.
+constexpr int kCombineThreads = 256, kCombineCols = 128, kCombineGroups = 8;
+constexpr int kFewParts = 8;
+constexpr int kMaxParts = 512;                       // more than CTAs of any attention launch
+__device__ __forceinline__ void store4(float* p, const float (&v)[4]) { store_vec(p, v); }
+__device__ __forceinline__ void store4(bf16* p, const float (&v)[4]) {
+  const __nv_bfloat162 x0 = __floats2bfloat162_rn(v[0], v[1]), x1 = __floats2bfloat162_rn(v[2], v[3]);
+  *reinterpret_cast<uint2*>(p) =
+      make_uint2(*reinterpret_cast<const uint32_t*>(&x0), *reinterpret_cast<const uint32_t*>(&x1));
+}
 template <typename T>
 __global__ void __launch_bounds__(kCombineThreads) qpool_combine_kernel(AttnArgs a) {
-  const int b = blockIdx.y, r = a.f.r;
-  const int e = (blockIdx.x * kCombineThreads + threadIdx.x) * 4;
+  extern __shared__ int listed[];                    // [batch]
+  __shared__ int2 warp_count[kCombineThreads / 32];
+  __shared__ float weight[kMaxParts], red[kCombineThreads / 32], total[1];
+  __shared__ float4 sums[kCombineGroups][kCombineCols / 4];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = a.f.r, heads = a.n_heads;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  if (a.error_word && *a.error_word) {   // a bounded wait gave up: no result that looks like one
-    if (e < a.n_heads * r)
-      for (int i = 0; i < 4; ++i)
-        static_cast<T*>(a.out)[(long long)b * a.n_heads * r + e + i] = Elem<T>::from_float(NAN);
-    return;
-  }
-  const bool empty = a.slots[b] <= 0;
-  const int2 parts = empty ? make_int2(0, 1) : a.seq_parts[b];
-  if (parts.y == 0 || e >= a.n_heads * r) return;
-  const int h = e / r;
-  T* out = static_cast<T*>(a.out) + (long long)b * a.n_heads * r + e;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  float lse = -INFINITY;
-  if (!empty) {
-    const float* ml = a.ml_part + ((long long)parts.x * a.n_heads + h) * 2;
-    const float* o = a.o_part + (long long)parts.x * a.n_heads * r + e;
-    const long long ml_step = 2ll * a.n_heads, o_step = (long long)a.n_heads * r;
-    float m = -INFINITY;
-    for (int p = 0; p < parts.y; ++p) m = fmaxf(m, ml[p * ml_step]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int p = 0; p < parts.y; ++p) {
-      const float w = exp2f(ml[p * ml_step] - ref);
-      const float4 x = *reinterpret_cast<const float4*>(o + p * o_step);
-      l += w * ml[p * ml_step + 1];
-      v[0] += w * x.x; v[1] += w * x.y; v[2] += w * x.z; v[3] += w * x.w;
+  const bool failed = a.error_word && *a.error_word; // a bounded wait gave up: no result that looks like one
+  // Sequences with few parts (or none, or no result) from the front of the list, the others from its
+  // end, both in order: every CTA has the same list.
+  int n_few = 0, n_many = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kCombineThreads) {
+    const int b = b0 + tid;
+    int kind = 0;                                    // 1 few, 2 many
+    if (b < a.batch) {
+      if (failed || a.slots[b] <= 0) {
+        kind = 1;
+      } else {
+        const int n = a.seq_parts[b].y;
+        kind = n == 0 ? 0 : n <= kFewParts ? 1 : 2;
+      }
     }
+    const uint32_t few = __ballot_sync(0xffffffffu, kind == 1), many = __ballot_sync(0xffffffffu, kind == 2);
+    if (lane == 0) warp_count[warp] = make_int2(__popc(few), __popc(many));
+    __syncthreads();
+    const uint32_t below = (1u << lane) - 1u;
+    int at_few = n_few + __popc(few & below), at_many = n_many + __popc(many & below);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] /= l;
-    lse = (m + log2f(l)) * 0.69314718055994531f;
+    for (int i = 0; i < kCombineThreads / 32; ++i) {
+      const int2 c = warp_count[i];
+      if (i < warp) { at_few += c.x; at_many += c.y; }
+      n_few += c.x;
+      n_many += c.y;
+    }
+    if (kind == 1) listed[at_few] = b;
+    if (kind == 2) listed[a.batch - 1 - at_many] = b;
+    __syncthreads();
   }
-  if constexpr (sizeof(T) == 4) {
-    store_vec(out, v);
-  } else {
-    const __nv_bfloat162 x0 = __floats2bfloat162_rn(v[0], v[1]), x1 = __floats2bfloat162_rn(v[2], v[3]);
-    *reinterpret_cast<uint2*>(out) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&x0), *reinterpret_cast<const uint32_t*>(&x1));
+
+  const int seq_pieces = (heads * r + 4 * kCombineThreads - 1) / (4 * kCombineThreads);
+  for (long long w = blockIdx.x; w < (long long)n_few * seq_pieces; w += gridDim.x) {
+    const int b = listed[w / seq_pieces], e = ((int)(w % seq_pieces) * kCombineThreads + tid) * 4;
+    if (e >= heads * r) continue;
+    const int h = e / r;
+    const float fill = failed ? NAN : 0.f;
+    float v[4] = {fill, fill, fill, fill};
+    float lse = failed ? NAN : -INFINITY;
+    if (!failed && a.slots[b] > 0) {
+      const int2 parts = a.seq_parts[b];
+      const float2* ml = reinterpret_cast<const float2*>(a.ml_part) + (long long)parts.x * heads + h;
+      const float* o = a.o_part + (long long)parts.x * heads * r + e;
+      const long long o_step = (long long)heads * r;
+      float2 s[kFewParts];
+      float4 x[kFewParts];
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int p = 0; p < kFewParts; ++p)
+        if (p < parts.y) {
+          s[p] = ml[p * heads];
+          x[p] = *reinterpret_cast<const float4*>(o + p * o_step);
+        }
+#pragma unroll
+      for (int p = 0; p < kFewParts; ++p)
+        if (p < parts.y) m = fmaxf(m, s[p].x);
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int p = 0; p < kFewParts; ++p)
+        if (p < parts.y) {
+          const float f = exp2f(s[p].x - ref);
+          l += f * s[p].y;
+          v[0] += f * x[p].x; v[1] += f * x[p].y; v[2] += f * x[p].z; v[3] += f * x[p].w;
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] /= l;
+      lse = (m + log2f(l)) * 0.69314718055994531f;
+    }
+    store4(static_cast<T*>(a.out) + (long long)b * heads * r + e, v);
+    if (a.lse && e % r == 0) a.lse[(long long)b * heads + h] = lse;
   }
-  if (a.lse && e % r == 0) a.lse[(long long)b * a.n_heads + h] = lse;
+
+  const int col_blocks = (r + kCombineCols - 1) / kCombineCols;
+  for (long long w = blockIdx.x; w < (long long)n_many * heads * col_blocks; w += gridDim.x) {
+    const int cb = (int)(w % col_blocks), bh = (int)(w / col_blocks), h = bh % heads;
+    const int b = listed[a.batch - 1 - bh / heads], col = cb * kCombineCols + lane * 4;
+    float lse;
+    float4 sum;
+    {
+      const int2 parts = a.seq_parts[b];
+      const float* ml = a.ml_part + ((long long)parts.x * heads + h) * 2;
+      const float* o = a.o_part + ((long long)parts.x * heads + h) * r + col;
+      const long long ml_step = 2ll * heads, o_step = (long long)heads * r;
+      float m = -INFINITY;
+      for (int p = tid; p < parts.y; p += kCombineThreads) m = fmaxf(m, ml[p * ml_step]);
+      m = warp_max(m);
+      if (lane == 0) red[warp] = m;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kCombineThreads / 32; ++i) m = fmaxf(m, red[i]);
+      const float ref = m == -INFINITY ? 0.f : m;
+      for (int p = tid; p < parts.y; p += kCombineThreads) weight[p] = exp2f(ml[p * ml_step] - ref);
+      __syncthreads();
+      // The denominator: warp 0, a lane's parts in order, then the lanes in order.
+      if (warp == 0) {
+        float l = 0.f;
+        for (int p = lane; p < parts.y; p += 32) l += weight[p] * ml[p * ml_step + 1];
+        l = warp_sum(l);
+        if (lane == 0) total[0] = l;
+      }
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (col < r) {
+        constexpr int kU = 4;
+        for (int p0 = warp; p0 < parts.y; p0 += kU * kCombineGroups) {
+          float4 x[kU];
+#pragma unroll
+          for (int u = 0; u < kU; ++u) {
+            const int p = p0 + u * kCombineGroups;
+            x[u] = p < parts.y ? *reinterpret_cast<const float4*>(o + p * o_step) : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+#pragma unroll
+          for (int u = 0; u < kU; ++u) {
+            const int p = p0 + u * kCombineGroups;
+            const float f = p < parts.y ? weight[p] : 0.f;
+            v.x += f * x[u].x; v.y += f * x[u].y; v.z += f * x[u].z; v.w += f * x[u].w;
+          }
+        }
+      }
+      sums[warp][lane] = v;
+      __syncthreads();
+      sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kCombineGroups; ++i) {
+        const float4 x = sums[i][lane];
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+      }
+      const float l = total[0];
+      sum.x /= l; sum.y /= l; sum.z /= l; sum.w /= l;
+      lse = (m + log2f(l)) * 0.69314718055994531f;
+    }
+    if (warp == 0 && col < r) {
+      const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+      store4(static_cast<T*>(a.out) + ((long long)b * heads + h) * r + col, v);
+      if (a.lse && cb == 0 && lane == 0) a.lse[(long long)b * heads + h] = lse;
+    }
+    __syncthreads();                                 // the shared sums may be rewritten
+  }
 }
 
 }  // namespace qp

@@ -115,9 +115,58 @@ __device__ __forceinline__ void store16(T* p, const float (&x)[16]) {
   }
 }
 
-// Rows into the pool.  The code of x at scale s is the nearest one, the even one on a tie, found by
-// comparing |x| with the borders 0.25 s .. 5 s, which are exact in fp32: no quotient, hence no
-// rounding that could move a value across a border.  A group with an infinity or a NaN gets a NaN scale.
+// Eight values -> eight codes, nearest, the even one on a tie, saturating.
+__device__ __forceinline__ uint32_t encode8(const float (&y)[8]) {
+  uint32_t o;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(o)
+      : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+  return o;
+}
+// The same from the definition, by comparing |x| with the borders 0.25 s .. 5 s, which are exact in
+// fp32: no quotient, hence no rounding that could move a value across a border.
+__device__ __noinline__ uint32_t encode8_exact(const float* x, float s) {
+  uint32_t code = 0;
+  for (int i = 0; i < 8; ++i) {
+    const float v = fabsf(x[i]);
+    uint32_t c = (v > 0.25f * s) + (v >= 0.75f * s) + (v > 1.25f * s) + (v >= 1.75f * s) + (v > 2.5f * s) +
+                 (v >= 3.5f * s) + (v > 5.f * s);
+    c |= (__float_as_uint(x[i]) >> 28) & 8u;
+    code |= c << (4 * i);
+  }
+  return code;
+}
+// Eight elements at scale s > 0, inv = 1 / s.  The product x * inv is off by 2^-23 at most.  An element
+// that came from bf16 has 8 significant bits and a border 7, so unless the element is a border it is
+// 2^-8 away from it: rounding the product to 12 bits restores every border and moves nothing else
+// across.  An fp32 element may be next to a border: if the codes of the product made slightly
+// smaller and slightly larger agree they are right, else the definition decides.
+template <typename T>
+__device__ __forceinline__ uint32_t encode_group8(const float* x, float s, float inv) {
+  float y[8];
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __uint_as_float((__float_as_uint(x[i] * inv) + 0x800u) & 0xfffff000u);
+    return encode8(y);
+  } else {
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p = x[i] * inv;
+      y[i] = p * (1.f - 0x1p-20f);
+      z[i] = p * (1.f + 0x1p-20f);
+    }
+    const uint32_t lo = encode8(y), hi = encode8(z);
+    return lo == hi ? lo : encode8_exact(x, s);
+  }
+}
+
+// Rows into the pool.  A group with an infinity or a NaN gets a NaN scale.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) qpool_write_kernel(RowArgs a) {
   const int units = (a.f.r + a.f.dr) / 16, lat_units = a.f.r / 16;
@@ -142,17 +191,11 @@ __global__ void __launch_bounds__(kRowThreads) qpool_write_kernel(RowArgs a) {
     if (u < lat_units) {
       const bool finite = top < 0x7f800000u;
       const float s = finite ? pick_scale(__uint_as_float(top)) : 0.f;
-      const float b0 = 0.25f * s, b1 = 0.75f * s, b2 = 1.25f * s, b3 = 1.75f * s, b4 = 2.5f * s, b5 = 3.5f * s,
-                  b6 = 5.f * s;
       uint32_t code[2] = {0u, 0u};
       if (s > 0.f) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float v = fabsf(x[i]);
-          uint32_t c = (v > b0) + (v >= b1) + (v > b2) + (v >= b3) + (v > b4) + (v >= b5) + (v > b6);
-          c |= (__float_as_uint(x[i]) >> 28) & 8u;
-          code[i >> 3] |= c << (4 * (i & 7));
-        }
+        const float inv = 1.f / s;
+        code[0] = encode_group8<T>(x, s, inv);
+        code[1] = encode_group8<T>(x + 8, s, inv);
       }
       const int chunk = (u >> 1) ^ (row & a.f.code_mask());
       *reinterpret_cast<uint2*>(page + row * a.f.code_row() + chunk * 16 + (u & 1) * 8) = make_uint2(code[0], code[1]);

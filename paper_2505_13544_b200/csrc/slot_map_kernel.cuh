@@ -15,9 +15,8 @@ namespace mtla {
 namespace sm {
 
 constexpr int kThreads = 256;
-constexpr int kMaxBatch = 16384;       // two prefix sums in shared memory
+constexpr int kMaxBatch = 16384;       // lengths and two prefix sums in shared memory
 constexpr int kPage = 64;
-constexpr int kPerThread = 4;          // consecutive tokens of a thread: 16-byte stores
 
 struct Args {
   const int* held;
@@ -31,15 +30,23 @@ struct Args {
   int vec;                   // the token arrays are 16-byte aligned
 };
 
-// Pages that hold `tokens` tokens (64-bit: counts go up to 2^31 - 1).
-__device__ __forceinline__ int pages_of(long long tokens, int stride) {
-  return (int)(((tokens + stride - 1) / stride + kPage - 1) / kPage);
+// Slots and pages of `tokens` tokens, 0 .. 2^31 - 1, in 32-bit arithmetic that cannot overflow.
+__device__ __forceinline__ uint32_t slots_of(uint32_t tokens, uint32_t stride) {
+  return tokens ? (tokens - 1) / stride + 1 : 0;
+}
+__device__ __forceinline__ int pages_of(uint32_t tokens, uint32_t stride) {
+  return (int)((slots_of(tokens, stride) + kPage - 1) / kPage);
 }
 
+// PER: consecutive tokens of a thread.  Four give 16-byte stores where there are tokens for every SM;
+// with fewer, one token a thread keeps the chain of dependent loads short (128 tokens: 11.0 us with
+// four, see below for one).
+template <int PER>
 __global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
   extern __shared__ int smem[];
   int* s_start = smem;                   // [batch + 1] first token of every request
   int* s_page = smem + a.batch + 1;      // [batch + 1] first new page of every request
+  int* s_held = s_page + a.batch + 1;    // [batch]
   __shared__ long long warp_tok[kThreads / 32], warp_page[kThreads / 32];
   __shared__ int s_bad;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -55,8 +62,9 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
   for (int b = lo; b < hi; ++b) {
     const long long h = a.held[b], f = a.fresh[b];
     const bool ok = h >= 0 && f >= 0 && h + f <= 0x7fffffffll;
-    const int have = ok ? pages_of(h, a.stride) : 0;
-    const int want = ok ? pages_of(h + f, a.stride) : 0;
+    const int have = ok ? pages_of((uint32_t)h, a.stride) : 0;
+    const int want = ok ? pages_of((uint32_t)(h + f), a.stride) : 0;
+    s_held[b] = h > 0 ? (int)h : 0;
     bad |= !ok || want > a.width;
     s_start[b] = ok ? (int)f : 0;        // for now the counts
     s_page[b] = want - have;
@@ -97,11 +105,11 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
 
   // Per request: offsets, slot counts, the new entries of its table row (a warp per request).
   for (int b = blockIdx.x * (kThreads / 32) + warp; b < a.batch; b += gridDim.x * (kThreads / 32)) {
-    const int h = max(a.held[b], 0);
+    const int h = s_held[b];
     const int have = pages_of(h, a.stride), p0 = s_page[b], n_new = s_page[b + 1] - p0;
     if (lane == 0) {
       a.starts[b] = s_start[b];
-      a.slots[b] = (int)(((long long)h + (s_start[b + 1] - s_start[b]) + a.stride - 1) / a.stride);
+      a.slots[b] = (int)slots_of((uint32_t)h + (s_start[b + 1] - s_start[b]), a.stride);
     }
     for (int i = lane; i < n_new; i += 32) a.table[(long long)b * a.width + have + i] = a.free_pages[p0 + i];
   }
@@ -111,10 +119,10 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
   }
 
   // Per token.
-  for (long long t0 = ((long long)blockIdx.x * kThreads + tid) * kPerThread; t0 < a.n_tokens;
-       t0 += (long long)gridDim.x * kThreads * kPerThread) {
-    int seq[kPerThread], pos[kPerThread];
-    long long slot[kPerThread], store[kPerThread];
+  for (long long t0 = ((long long)blockIdx.x * kThreads + tid) * PER; t0 < a.n_tokens;
+       t0 += (long long)gridDim.x * kThreads * PER) {
+    int seq[PER], pos[PER];
+    long long slot[PER], store[PER];
     int b = 0;
     if (t0 < total) {                              // the last request that starts at or before t0
       int lo_b = 0, hi_b = a.batch;
@@ -124,20 +132,20 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
       }
       b = lo_b;
     }
-    int held = t0 < total ? a.held[b] : 0, page_of = -1;
+    int held = t0 < total ? s_held[b] : 0, page_of = -1;
     long long page = 0;
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
+    for (int i = 0; i < PER; ++i) {
       const long long t = t0 + i;
       seq[i] = -1; pos[i] = 0; slot[i] = -1; store[i] = -1;
       if (t >= total) continue;
       while (s_start[b + 1] <= t) {                // requests without new tokens are stepped over
         ++b;
-        held = a.held[b];
+        held = s_held[b];
         page_of = -1;
       }
       const int p = held + (int)(t - s_start[b]);
-      const int j = p / a.stride;
+      const int j = (int)((uint32_t)p / (uint32_t)a.stride);
       if (page_of != j >> 6) {
         page_of = j >> 6;
         const int have = pages_of(held, a.stride);
@@ -149,15 +157,15 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
       const bool last = p - j * a.stride == a.stride - 1 || t + 1 == s_start[b + 1];
       store[i] = last ? slot[i] : -1;
     }
-    if (a.vec && t0 + kPerThread <= a.n_tokens) {
-      *reinterpret_cast<int4*>(a.seq + t0) = make_int4(seq[0], seq[1], seq[2], seq[3]);
-      *reinterpret_cast<int4*>(a.position + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-      *reinterpret_cast<longlong2*>(a.slot + t0) = make_longlong2(slot[0], slot[1]);
-      *reinterpret_cast<longlong2*>(a.slot + t0 + 2) = make_longlong2(slot[2], slot[3]);
-      *reinterpret_cast<longlong2*>(a.store + t0) = make_longlong2(store[0], store[1]);
-      *reinterpret_cast<longlong2*>(a.store + t0 + 2) = make_longlong2(store[2], store[3]);
+    if (PER == 4 && a.vec && t0 + PER <= a.n_tokens) {
+      *reinterpret_cast<int4*>(a.seq + t0) = make_int4(seq[0], seq[1 % PER], seq[2 % PER], seq[3 % PER]);
+      *reinterpret_cast<int4*>(a.position + t0) = make_int4(pos[0], pos[1 % PER], pos[2 % PER], pos[3 % PER]);
+      *reinterpret_cast<longlong2*>(a.slot + t0) = make_longlong2(slot[0], slot[1 % PER]);
+      *reinterpret_cast<longlong2*>(a.slot + t0 + 2) = make_longlong2(slot[2 % PER], slot[3 % PER]);
+      *reinterpret_cast<longlong2*>(a.store + t0) = make_longlong2(store[0], store[1 % PER]);
+      *reinterpret_cast<longlong2*>(a.store + t0 + 2) = make_longlong2(store[2 % PER], store[3 % PER]);
     } else {
-      for (int i = 0; i < kPerThread && t0 + i < a.n_tokens; ++i) {
+      for (int i = 0; i < PER && t0 + i < a.n_tokens; ++i) {
         a.seq[t0 + i] = seq[i];
         a.position[t0 + i] = pos[i];
         a.slot[t0 + i] = slot[i];
