@@ -8,6 +8,7 @@ raises, and every non-zero status raises MTLAError.
 from __future__ import annotations
 
 import ctypes
+import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -190,7 +191,7 @@ def load_library() -> ctypes.CDLL:
         "mtla_selftest_wait_timeout": (ctypes.c_int, [vp, i32, vp]),
         "mtla_slot_map": (ctypes.c_int, [vp, vp, i32, i32, vp, i32, vp, i32, ctypes.POINTER(mtla_slot_map_out),
                                          i32, vp]),
-        "mtla_rope": (ctypes.c_int, [ctypes.POINTER(mtla_rope_config), ctypes.POINTER(mtla_rope_tensor), i32, i32,
+        "mtla_rope": (ctypes.c_int, [ctypes.POINTER(mtla_rope_config), vp, i32, i32,
                                      vp, i32, i32, vp]),
         "mtla_qpool_page_bytes": (sz, [qp_p]),
         "mtla_qpool_write": (ctypes.c_int, [qp_p, vp, vp, ctypes.c_int64, i32, vp, i32, vp]),
@@ -739,20 +740,29 @@ def mtla_train_backward(h: Handle, x: torch.Tensor, dy: torch.Tensor, stream=Non
 
 _ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
 _ROPE_SCALINGS = {"none": 0, "linear": 1, "ramp": 2}
+_ROPE_TENSOR = struct.Struct("@QQqqqqiii4x")          # mtla_rope_tensor
+assert _ROPE_TENSOR.size == ctypes.sizeof(mtla_rope_tensor)
 
 
-def _stream_of(t: torch.Tensor, stream) -> int:
-    """The given stream, or the current one of the GPU that holds `t`."""
-    return (torch.cuda.current_stream(t.device) if stream is None else stream).cuda_stream
+def _gpu_of(t: torch.Tensor, name: str) -> int:
+    """Index of the GPU that holds `t`: the call's GPU."""
+    dev = t.get_device()
+    if dev < 0:
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    return dev
 
 
-def _expect_on(t: torch.Tensor, like: torch.Tensor | None, dtype, shape, name: str) -> int:
-    """data_ptr() of a contiguous CUDA tensor of that type and shape on the GPU of `like`."""
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-        raise TypeError(f"{name}: expected contiguous {dtype} tensor of shape {tuple(shape)}")
-    if not t.is_cuda or (like is not None and t.device != like.device):
-        raise TypeError(f"{name}: expected a CUDA tensor on the call's GPU")
-    return t.data_ptr()
+def _stream_on(dev: int, stream) -> int:
+    """The given stream, or the current one of GPU `dev` (asked for without building a Stream
+    object, which would cost as much as the rest of a small call's checks)."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _ptr(t: torch.Tensor, dtype, shape, dev: int, name: str) -> int:
+    """data_ptr() of a contiguous tensor of that type and shape on the call's GPU."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise TypeError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the call's GPU ({dev})")
 
 
 @dataclass
@@ -787,20 +797,19 @@ def mtla_slot_map(held: torch.Tensor, fresh: torch.Tensor, free_pages: torch.Ten
         if n_tokens is None:
             raise TypeError("n_tokens: needed when no buffers are given")
         out = make_slot_map(batch, n_tokens, table.device)
-    n = out.seq.shape[0]
+    n, n_free = out.seq.shape[0], free_pages.shape[0]
     if n_tokens is not None and n_tokens != n:
         raise TypeError("out: its token arrays differ from n_tokens")
-    i32, i64 = torch.int32, torch.int64
-    tp = _expect_on(table, None, i32, (batch, width), "table")
+    dev, i32, i64, per_seq, per_token = _gpu_of(table, "table"), torch.int32, torch.int64, (batch,), (n,)
     o = mtla_slot_map_out(
-        _expect_on(out.starts, table, i32, (batch + 1,), "starts"), _expect_on(out.seq, table, i32, (n,), "seq"),
-        _expect_on(out.position, table, i32, (n,), "position"), _expect_on(out.slot, table, i64, (n,), "slot"),
-        _expect_on(out.store, table, i64, (n,), "store"), _expect_on(out.slots, table, i32, (batch,), "slots"),
-        _expect_on(out.taken, table, i32, (1,), "taken"))
+        _ptr(out.starts, i32, (batch + 1,), dev, "starts"), _ptr(out.seq, i32, per_token, dev, "seq"),
+        _ptr(out.position, i32, per_token, dev, "position"), _ptr(out.slot, i64, per_token, dev, "slot"),
+        _ptr(out.store, i64, per_token, dev, "store"), _ptr(out.slots, i32, per_seq, dev, "slots"),
+        _ptr(out.taken, i32, (1,), dev, "taken"))
     _check(load_library().mtla_slot_map(
-        _expect_on(held, table, i32, (batch,), "held"), _expect_on(fresh, table, i32, (batch,), "fresh"), batch,
-        stride, tp, width, _expect_on(free_pages, table, i32, free_pages.shape, "free_pages"), free_pages.shape[0],
-        ctypes.byref(o), n, _stream_of(table, stream)), "mtla_slot_map")
+        _ptr(held, i32, per_seq, dev, "held"), _ptr(fresh, i32, per_seq, dev, "fresh"), batch, stride,
+        _ptr(table, i32, (batch, width), dev, "table"), width, _ptr(free_pages, i32, (n_free,), dev, "free_pages"),
+        n_free, ctypes.byref(o), n, _stream_on(dev, stream)), "mtla_slot_map")
     return out
 
 
@@ -821,23 +830,24 @@ def mtla_rope(cfg: mtla_rope_config, tensors, positions: torch.Tensor, *, first=
         out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in tensors]
     if count < 1 or len(out) != count or len(firsts) != count:
         raise TypeError("tensors, out and first: expected one entry per tensor")
-    dtype = tensors[0].dtype
+    dtype, dev = tensors[0].dtype, _gpu_of(positions, "positions")
     if dtype not in _DTYPES:
         raise TypeError(f"tensors: unsupported type {dtype}")
-    pp = _expect_on(positions, tensors[0], torch.int32, (n_tokens,), "positions")
-    arr = (mtla_rope_tensor * count)()
-    for i in range(count):
-        x, y = tensors[i], out[i]
-        for t in (x, y):
-            if t.dim() != 3 or t.dtype != dtype or t.shape != x.shape or t.shape[0] != n_tokens or (
-                    t.stride(2) != 1 and t.shape[2] > 1) or t.device != positions.device:
-                raise TypeError(f"tensor {i}: expected {dtype} [{n_tokens}][heads][width] on the call's GPU, "
-                                "consecutive elements in a head, and an output of the same shape")
-        xs, ys = x.stride(), y.stride()
-        arr[i] = mtla_rope_tensor(x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], x.shape[1], x.shape[2],
-                                  firsts[i])
-    _check(load_library().mtla_rope(ctypes.byref(cfg), arr, count, _DTYPES[dtype], pp, n_tokens, int(inverse),
-                                    _stream_of(positions, stream)), "mtla_rope")
+    pp = _ptr(positions, torch.int32, (n_tokens,), dev, "positions")
+    packed = b""
+    for x, y, at in zip(tensors, out, firsts):
+        if x.dim() != 3 or x.shape != y.shape:
+            raise TypeError(f"expected [{n_tokens}][heads][width] and an output of the same shape")
+        n, heads, width = x.shape
+        x0, x1, x2 = x.stride()
+        y0, y1, y2 = y.stride()
+        if (n != n_tokens or x.dtype is not dtype or y.dtype is not dtype or x.get_device() != dev
+                or y.get_device() != dev or (width > 1 and (x2 != 1 or y2 != 1))):
+            raise TypeError(f"expected {dtype} [{n_tokens}][heads][width] on the call's GPU, consecutive elements in "
+                            "a head")
+        packed += _ROPE_TENSOR.pack(x.data_ptr(), y.data_ptr(), x0, x1, y0, y1, heads, width, at)
+    _check(load_library().mtla_rope(ctypes.byref(cfg), packed, count, _DTYPES[dtype], pp, n_tokens, int(inverse),
+                                    _stream_on(dev, stream)), "mtla_rope")
     return out
 
 
@@ -849,9 +859,9 @@ def mtla_qpool_page_bytes(cfg: mtla_qpool_config) -> int:
     return load_library().mtla_qpool_page_bytes(ctypes.byref(cfg))
 
 
-def _qpool_pages(cfg: mtla_qpool_config, pages: torch.Tensor) -> int:
+def _qpool_pages(cfg: mtla_qpool_config, pages: torch.Tensor, dev: int) -> int:
     size = 34 * cfg.latent_rank + 128 * cfg.rope_dim        # mtla_qpool_page_bytes, without the call
-    return _expect_on(pages, None, torch.uint8, (cfg.n_pages, size), "pages")
+    return _ptr(pages, torch.uint8, (cfg.n_pages, size), dev, "pages")
 
 
 def make_qpool(cfg: mtla_qpool_config, device="cuda:0") -> torch.Tensor:
@@ -862,35 +872,33 @@ def make_qpool(cfg: mtla_qpool_config, device="cuda:0") -> torch.Tensor:
     return torch.empty(cfg.n_pages, size, dtype=torch.uint8, device=device)
 
 
-def _qpool_rows(cfg: mtla_qpool_config, rows: torch.Tensor, pages: torch.Tensor, n: int, name: str) -> int:
-    if (rows.dtype not in _DTYPES or rows.dim() != 2 or rows.shape != (n, cfg.latent_rank + cfg.rope_dim)
-            or rows.stride(1) != 1 or rows.device != pages.device):
-        raise TypeError(f"{name}: expected [{n}][r + d_R], fp32 or bf16, consecutive elements in a row, on the "
-                        "pool's GPU")
-    return rows.data_ptr()
+def _qpool_rows(cfg: mtla_qpool_config, rows: torch.Tensor, dev: int, n: int, name: str) -> int:
+    if (rows.dtype in _DTYPES and rows.shape == (n, cfg.latent_rank + cfg.rope_dim) and rows.stride(1) == 1
+            and rows.get_device() == dev):
+        return rows.data_ptr()
+    raise TypeError(f"{name}: expected [{n}][r + d_R], fp32 or bf16, consecutive elements in a row, on the pool's GPU")
 
 
 def mtla_qpool_write(cfg: mtla_qpool_config, pages: torch.Tensor, rows: torch.Tensor, index: torch.Tensor,
                      stream=None) -> None:
     """rows [n][r + d_R] (fp32 or bf16) into pool rows index (int64 [n]; outside the pool: skipped)."""
-    n = index.shape[0]
-    pp, rp = _qpool_pages(cfg, pages), _qpool_rows(cfg, rows, pages, n, "rows")
+    n, dev = index.shape[0], _gpu_of(pages, "pages")
+    pp, rp = _qpool_pages(cfg, pages, dev), _qpool_rows(cfg, rows, dev, n, "rows")
     _check(load_library().mtla_qpool_write(ctypes.byref(cfg), pp, rp, rows.stride(0), _DTYPES[rows.dtype],
-                                           _expect_on(index, pages, torch.int64, (n,), "index"), n,
-                                           _stream_of(pages, stream)), "mtla_qpool_write")
+                                           _ptr(index, torch.int64, (n,), dev, "index"), n, _stream_on(dev, stream)),
+           "mtla_qpool_write")
 
 
 def mtla_qpool_read(cfg: mtla_qpool_config, pages: torch.Tensor, index: torch.Tensor, *, dtype=torch.bfloat16,
                     out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Pool rows index (int64 [n]) as [n][r + d_R]; zeros where the index is outside the pool."""
-    n = index.shape[0]
-    pp = _qpool_pages(cfg, pages)
+    n, dev = index.shape[0], _gpu_of(pages, "pages")
+    pp = _qpool_pages(cfg, pages, dev)
     if out is None:
         out = torch.empty(n, cfg.latent_rank + cfg.rope_dim, dtype=dtype, device=pages.device)
-    rp = _qpool_rows(cfg, out, pages, n, "out")
-    _check(load_library().mtla_qpool_read(ctypes.byref(cfg), pp,
-                                          _expect_on(index, pages, torch.int64, (n,), "index"), n, rp,
-                                          out.stride(0), _DTYPES[out.dtype], _stream_of(pages, stream)),
+    rp = _qpool_rows(cfg, out, dev, n, "out")
+    _check(load_library().mtla_qpool_read(ctypes.byref(cfg), pp, _ptr(index, torch.int64, (n,), dev, "index"), n, rp,
+                                          out.stride(0), _DTYPES[out.dtype], _stream_on(dev, stream)),
            "mtla_qpool_read")
     return out
 
@@ -908,20 +916,19 @@ def mtla_qpool_attend(cfg: mtla_qpool_config, pages: torch.Tensor, table: torch.
     if q.dim() != 3 or table.dim() != 2 or q.dtype not in _DTYPES:
         raise TypeError("q: expected fp32 or bf16 [B][n_heads][r + d_R]; table: expected [B][width]")
     batch, width = table.shape
-    heads, r = cfg.n_heads, cfg.latent_rank
-    pp = _qpool_pages(cfg, pages)
+    heads, r, dev, dtype = cfg.n_heads, cfg.latent_rank, _gpu_of(pages, "pages"), q.dtype
     if out is None:
-        out = torch.empty(batch, heads, r, dtype=q.dtype, device=q.device)
+        out = torch.empty(batch, heads, r, dtype=dtype, device=q.device)
     if lse is None:
         lse = torch.empty(batch, heads, dtype=torch.float32, device=q.device)
     if workspace is None:
         workspace = torch.empty(mtla_qpool_workspace_bytes(cfg, batch), dtype=torch.uint8, device=q.device)
+    ws_shape = workspace.shape
     _check(load_library().mtla_qpool_attend(
-        ctypes.byref(cfg), pp, _expect_on(table, pages, torch.int32, (batch, width), "table"), width,
-        _expect_on(slots, pages, torch.int32, (batch,), "slots"), batch,
-        _expect_on(q, pages, q.dtype, (batch, heads, r + cfg.rope_dim), "q"), _DTYPES[q.dtype], scale,
-        _expect_on(out, pages, q.dtype, (batch, heads, r), "out"),
-        _expect_on(lse, pages, torch.float32, (batch, heads), "lse"),
-        _expect_on(workspace, pages, torch.uint8, workspace.shape, "workspace"), workspace.numel(),
-        _stream_of(pages, stream)), "mtla_qpool_attend")
+        ctypes.byref(cfg), _qpool_pages(cfg, pages, dev), _ptr(table, torch.int32, (batch, width), dev, "table"), width,
+        _ptr(slots, torch.int32, (batch,), dev, "slots"), batch,
+        _ptr(q, dtype, (batch, heads, r + cfg.rope_dim), dev, "q"), _DTYPES[dtype], scale,
+        _ptr(out, dtype, (batch, heads, r), dev, "out"), _ptr(lse, torch.float32, (batch, heads), dev, "lse"),
+        _ptr(workspace, torch.uint8, ws_shape, dev, "workspace"), ws_shape.numel(), _stream_on(dev, stream)),
+        "mtla_qpool_attend")
     return out, lse

@@ -45,8 +45,12 @@ class OnDeviceOf {
   ~OnDeviceOf() { if (switched_) cudaSetDevice(old_); }
   int status() const { return status_; }
   int sm_count() const {
-    int n = 0;
-    return cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device_) == cudaSuccess && n > 0 ? n : 1;
+    static std::atomic<int> known[64];       // per GPU, 0 until asked
+    int n = device_ < 64 ? known[device_].load(std::memory_order_relaxed) : 0;
+    if (n > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device_) != cudaSuccess || n < 1) return 1;
+    if (device_ < 64) known[device_].store(n, std::memory_order_relaxed);
+    return n;
   }
   int device() const { return device_; }
 
@@ -97,11 +101,13 @@ int row_call(const mtla_qpool_config* cfg, const void* pages, const void* rows, 
   a.pool_rows = (long long)cfg->n_pages * qp::kPageRows;
   a.n = n;
   a.f = format_of(cfg);
-  const long long units = (long long)n * (width / 16);
-  const long long ctas = (units + qp::kRowThreads - 1) / qp::kRowThreads, most = 16ll * dev.sm_count();
+  // Rows of a CTA: those that its threads hold at once when there are few, more as the SMs fill up.
+  const int at_once = qp::kRowThreads / (width / (write ? 16 : 8)), even = ceil_div(n, 8 * dev.sm_count());
+  a.chunk = even < at_once ? at_once : even < qp::kMaxChunk ? even : qp::kMaxChunk;
+  const int ctas = ceil_div(n, a.chunk);
   auto kernel = dtype == MTLA_DTYPE_BF16 ? (write ? qp::qpool_write_kernel<bf16> : qp::qpool_read_kernel<bf16>)
                                          : (write ? qp::qpool_write_kernel<float> : qp::qpool_read_kernel<float>);
-  kernel<<<(unsigned)(ctas < most ? ctas : most), qp::kRowThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  kernel<<<(unsigned)ctas, qp::kRowThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
   return launched();
 }
 
@@ -309,12 +315,11 @@ int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int3
     q.y_head = t.y_head_stride;
     q.first = t.first;
     q.copy_units = t.x == t.y ? 0 : (t.width - d) / v;
-    q.units.set(q.copy_units + (half ? d / 2 / v : (use_vec ? d / v : d / 2)));
-    q.all_units = t.n_heads * (int)q.units.d;
+    q.units = q.copy_units + (half ? d / 2 / v : (use_vec ? d / v : d / 2));
+    q.all_units = t.n_heads * q.units;
     units += q.all_units;
   }
-  if (units > (1 << 26)) return MTLA_ERR_UNSUPPORTED_SHAPE;        // 8 tokens of it have to stay below 2^31
-  a.per_token.set((int)units);
+  a.per_token = (int)units;
   a.positions = positions;
   a.magnitude = magnitude;
   a.n_tensors = n_tensors;
@@ -323,20 +328,26 @@ int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int3
   a.inverse = inverse != 0;
   OnDeviceOf dev(tensors[0].y);
   if (dev.status() != MTLA_OK) return dev.status();
-  // Tokens per CTA: enough for four units per thread twice over, as long as every SM keeps several CTAs.
+  // A token's units over as few rounds of the CTA's threads as they take, evenly; as many tokens side by
+  // side as then fit.
+  const int rounds = ceil_div(a.per_token, rp::kThreads);
+  a.lanes = ceil_div(a.per_token, rounds);
+  a.rows = rp::kThreads / a.lanes;
+  // Tokens per CTA: four in flight for every thread, as long as every SM keeps several CTAs.
   int per = 1;
-  while (per < rp::kMaxTokens && per * units < 8ll * rp::kThreads &&
-         (n_tokens + 2 * per - 1) / (2 * per) >= 8 * dev.sm_count())
+  while (per < rp::kMaxTokens && per < 4 * a.rows && (n_tokens + 2 * per - 1) / (2 * per) >= 4 * dev.sm_count())
     per *= 2;
   a.tokens_per_cta = per;
-  const dim3 grid(ceil_div(n_tokens, per));
+  // With few tokens the rounds run as CTAs of their own instead of one after the other.
+  const dim3 grid(ceil_div(n_tokens, per), per == 1 && rounds < 65536 ? rounds : 1);
   auto pick = [&](auto bf, auto fp) { return dtype == MTLA_DTYPE_BF16 ? bf : fp; };
   auto kernel = use_vec ? (half ? pick(rp::rope_kernel<bf16, true, true>, rp::rope_kernel<float, true, true>)
                                 : pick(rp::rope_kernel<bf16, true, false>, rp::rope_kernel<float, true, false>))
                         : (half ? pick(rp::rope_kernel<bf16, false, true>, rp::rope_kernel<float, false, true>)
                                 : pick(rp::rope_kernel<bf16, false, false>, rp::rope_kernel<float, false, false>));
   const cudaError_t e =
-      launch_kernel(kernel, grid, dim3(rp::kThreads), (size_t)0, static_cast<cudaStream_t>(stream), true, a);
+      launch_kernel(kernel, grid, dim3(rp::kThreads), (size_t)per * a.pairs * 8, static_cast<cudaStream_t>(stream),
+                    true, a);
   if (e != cudaSuccess) cudaGetLastError();
   return e == cudaSuccess ? MTLA_OK : MTLA_ERR_CUDA;
 }

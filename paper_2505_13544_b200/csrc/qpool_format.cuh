@@ -84,14 +84,18 @@ struct RowArgs {
   void* rows;                // [n][r + d_R], row_stride elements apart
   long long row_stride;
   long long pool_rows;
-  int n;
+  int n, chunk;              // rows; rows of a CTA, at most kMaxChunk
   Format f;
 };
 
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 256, kMaxChunk = 256;
 
 // A unit is 16 elements: half a group, so the two threads of a group are neighbours (a row has an
-// even number of units).  Both kernels are bound by the bytes of the wide rows.
+// even number of units).  A CTA reads the indices of its rows at once, a thread then keeps its place in
+// the row and walks over rows, two or four in flight; the write walks over the rows that are kept
+// only.  Both kernels should be bound by the bytes of the wide rows; what the write had to lose for
+// that was instructions (131071 rows of r 512, half of them kept: 87 us comparing with all borders and
+// with 64-bit index arithmetic, 51 us with threads idle at every skipped row).
 template <typename T>
 __device__ __forceinline__ void load16(const T* p, float (&x)[16]) {
   constexpr int V = Elem<T>::kVec;
@@ -103,18 +107,6 @@ __device__ __forceinline__ void load16(const T* p, float (&x)[16]) {
     for (int j = 0; j < V; ++j) x[i * V + j] = v[j];
   }
 }
-template <typename T>
-__device__ __forceinline__ void store16(T* p, const float (&x)[16]) {
-  constexpr int V = Elem<T>::kVec;
-#pragma unroll
-  for (int i = 0; i < 16 / V; ++i) {
-    float v[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = x[i * V + j];
-    store_vec(p + i * V, v);
-  }
-}
-
 // Eight values -> eight codes, nearest, the even one on a tie, saturating.
 __device__ __forceinline__ uint32_t encode8(const float (&y)[8]) {
   uint32_t o;
@@ -141,17 +133,19 @@ __device__ __noinline__ uint32_t encode8_exact(const float* x, float s) {
   }
   return code;
 }
-// Eight elements at scale s > 0, inv = 1 / s.  The product x * inv is off by 2^-23 at most.  An element
-// that came from bf16 has 8 significant bits and a border 7, so unless the element is a border it is
-// 2^-8 away from it: rounding the product to 12 bits restores every border and moves nothing else
-// across.  An fp32 element may be next to a border: if the codes of the product made slightly
-// smaller and slightly larger agree they are right, else the definition decides.
+// Eight elements at scale s > 0, inv = 1 / s (off by 2^-24 at most).  An element that came from bf16
+// has 8 significant bits and a border 7, so unless x / s is a border it is 2^-8 of one away from
+// it, 2^-10 at least: rounding the quotient to steps of 2^-13 (by adding a number whose last bit that
+// is) restores every border and moves nothing else across.  An fp32 element may be next to a
+// border: if the codes of the quotient made slightly smaller and slightly larger agree they are right,
+// else the definition decides.
 template <typename T>
 __device__ __forceinline__ uint32_t encode_group8(const float* x, float s, float inv) {
   float y[8];
   if constexpr (sizeof(T) == 2) {
+    constexpr float kRound = 1536.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __uint_as_float((__float_as_uint(x[i] * inv) + 0x800u) & 0xfffff000u);
+    for (int i = 0; i < 8; ++i) y[i] = copysignf(fmaf(x[i], inv, kRound) - kRound, x[i]);   // -0 keeps its sign
     return encode8(y);
   } else {
     float z[8];
@@ -169,28 +163,27 @@ __device__ __forceinline__ uint32_t encode_group8(const float* x, float s, float
 // Rows into the pool.  A group with an infinity or a NaN gets a NaN scale.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) qpool_write_kernel(RowArgs a) {
-  const int units = (a.f.r + a.f.dr) / 16, lat_units = a.f.r / 16;
-  const long long total = (long long)a.n * units;
-  for (long long w = (long long)blockIdx.x * kRowThreads + threadIdx.x; w - (threadIdx.x & 31) < total;
-       w += (long long)gridDim.x * kRowThreads) {
-    const bool in = w < total;
-    const int n = in ? (int)(w / units) : 0, u = in ? (int)(w - (long long)n * units) : 0;
-    const long long at = in ? a.index[n] : -1;
-    const bool keep = at >= 0 && at < a.pool_rows;
-    float x[16];
+  const int units = (a.f.r + a.f.dr) / 16, lat_units = a.f.r / 16, rows = kRowThreads / units;
+  const int lane_row = threadIdx.x / units, u = threadIdx.x - lane_row * units;
+  const bool works = lane_row < rows;
+  // One row's unit: x into the pool row `at` (outside the pool: nowhere, but the neighbour's exchange is joined).
+  auto put = [&](float (&x)[16], long long at) {
+    const bool keep = at >= 0;
+    // The largest magnitude; a sum of x * 0 tells whether an infinity or a NaN is among them.
+    float top = 0.f, odd = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    if (keep) load16(static_cast<const T*>(a.rows) + n * a.row_stride + u * 16, x);
-    uint32_t top = 0;                              // magnitudes order like their bits; NaN on top
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    if (!keep) continue;
+    for (int i = 0; i < 16; ++i) {
+      top = fmaxf(top, fabsf(x[i]));
+      odd = fmaf(x[i], 0.f, odd);
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    odd += __shfl_xor_sync(0xffffffffu, odd, 1);
+    if (!keep) return;
     uint8_t* page = a.pages + (at >> 6) * a.f.page_bytes();
     const int row = (int)(at & 63);
     if (u < lat_units) {
-      const bool finite = top < 0x7f800000u;
-      const float s = finite ? pick_scale(__uint_as_float(top)) : 0.f;
+      const bool finite = odd == 0.f;
+      const float s = finite ? pick_scale(top) : 0.f;
       uint32_t code[2] = {0u, 0u};
       if (s > 0.f) {
         const float inv = 1.f / s;
@@ -213,54 +206,105 @@ __global__ void __launch_bounds__(kRowThreads) qpool_write_kernel(RowArgs a) {
         store_vec(reinterpret_cast<bf16*>(keys + ((c0 + h) ^ sw) * 16), v);
       }
     }
+  };
+  __shared__ long long at_s[kMaxChunk];
+  __shared__ int row_s[kMaxChunk], warp_kept[kRowThreads / 32];
+  const int first = blockIdx.x * a.chunk, chunk = min(a.chunk, a.n - first), lane = threadIdx.x & 31,
+            warp = threadIdx.x >> 5;
+  const long long mine = (int)threadIdx.x < chunk ? a.index[first + threadIdx.x] : -1;
+  const bool kept = mine >= 0 && mine < a.pool_rows;
+  const uint32_t votes = __ballot_sync(0xffffffffu, kept);
+  if (lane == 0) warp_kept[warp] = __popc(votes);
+  __syncthreads();
+  int place = __popc(votes & ((1u << lane) - 1u)), n_kept = 0;
+#pragma unroll
+  for (int i = 0; i < kRowThreads / 32; ++i) {
+    if (i < warp) place += warp_kept[i];
+    n_kept += warp_kept[i];
+  }
+  if (kept) {
+    at_s[place] = mine;
+    row_s[place] = first + threadIdx.x;
+  }
+  __syncthreads();
+  for (int i0 = 0; i0 < n_kept; i0 += 2 * rows) {    // two rows of a thread in flight
+    long long at[2];
+    float x[2][16];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k = i0 + i * rows + lane_row;
+      at[i] = -1;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[i][j] = 0.f;
+      if (works && k < n_kept) {
+        at[i] = at_s[k];
+        load16(static_cast<const T*>(a.rows) + row_s[k] * a.row_stride + u * 16, x[i]);
+      }
+    }
+    put(x[0], at[0]);
+    put(x[1], at[1]);
   }
 }
 
 // Rows out of the pool, widened to T (exact in both types); zeros where the index is outside the pool.
+// Eight elements a thread: a bf16 row is then written in full 16-byte steps by neighbouring threads
+// (sixteen, in two steps each, took 44 us for 131071 rows of r 512, see below for eight).
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) qpool_read_kernel(RowArgs a) {
-  const int units = (a.f.r + a.f.dr) / 16, lat_units = a.f.r / 16;
-  const long long total = (long long)a.n * units;
-  for (long long w = (long long)blockIdx.x * kRowThreads + threadIdx.x; w < total;
-       w += (long long)gridDim.x * kRowThreads) {
-    const int n = (int)(w / units), u = (int)(w - (long long)n * units);
-    const long long at = a.index[n];
-    float x[16];
+  const int units = (a.f.r + a.f.dr) / 8, lat_units = a.f.r / 8, rows = kRowThreads / units;
+  const int lane_row = threadIdx.x / units, u = threadIdx.x - lane_row * units;
+  constexpr int kU = 4;                              // rows of a thread in flight
+  __shared__ long long at_s[kMaxChunk];
+  const int first = blockIdx.x * a.chunk, chunk = min(a.chunk, a.n - first);
+  if ((int)threadIdx.x < chunk) at_s[threadIdx.x] = a.index[first + threadIdx.x];
+  __syncthreads();
+  if (lane_row >= rows) return;
+  T* out = static_cast<T*>(a.rows) + first * a.row_stride + u * 8;
+  for (int i0 = lane_row; i0 < chunk; i0 += kU * rows) {
+    uint4 data[kU];                                  // a word of codes and its scale, or eight keys
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    if (at >= 0 && at < a.pool_rows) {
+    for (int i = 0; i < kU; ++i) {
+      data[i] = make_uint4(0, 0, 0, 0);
+      const long long at = i0 + i * rows < chunk ? at_s[i0 + i * rows] : -1;
+      if (at < 0 || at >= a.pool_rows) continue;
       const uint8_t* page = a.pages + (at >> 6) * a.f.page_bytes();
       const int row = (int)(at & 63);
       if (u < lat_units) {
-        const int chunk = (u >> 1) ^ (row & a.f.code_mask());
-        const uint2 code = *reinterpret_cast<const uint2*>(page + row * a.f.code_row() + chunk * 16 + (u & 1) * 8);
-        const uint32_t s = scale_pair(page[a.f.off_scales() + row * a.f.scale_row() + (u >> 1)]);
-        const uint32_t words[2] = {code.x, code.y};
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          uint32_t o[4];
-          decode8(words[k], o);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t v = mul_h2(o[i], s);
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
-            x[k * 8 + 2 * i] = f.x;
-            x[k * 8 + 2 * i + 1] = f.y;
-          }
-        }
+        const int chunk_at = (u >> 2) ^ (row & a.f.code_mask());
+        data[i].x = *reinterpret_cast<const uint32_t*>(page + row * a.f.code_row() + chunk_at * 16 + (u & 3) * 4);
+        data[i].y = page[a.f.off_scales() + row * a.f.scale_row() + (u >> 2)];
       } else {
-        const int c0 = (u - lat_units) * 2, sw = a.f.key_swizzle(row);
-        const uint8_t* keys = page + a.f.off_keys() + row * a.f.key_row();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[8];
-          load_vec(reinterpret_cast<const bf16*>(keys + ((c0 + h) ^ sw) * 16), v);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[h * 8 + j] = v[j];
-        }
+        const int k = (u - lat_units) ^ a.f.key_swizzle(row);
+        data[i] = *reinterpret_cast<const uint4*>(page + a.f.off_keys() + row * a.f.key_row() + k * 16);
       }
     }
-    store16(static_cast<T*>(a.rows) + n * a.row_stride + u * 16, x);
+#pragma unroll
+    for (int i = 0; i < kU; ++i) {
+      if (i0 + i * rows >= chunk) break;
+      float x[8];
+      if (u < lat_units) {
+        uint32_t o[4];
+        decode8(data[i].x, o);
+        const uint32_t sc = scale_pair(data[i].y);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t v = mul_h2(o[j], sc);
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
+          x[2 * j] = f.x;
+          x[2 * j + 1] = f.y;
+        }
+      } else {
+        load_vec(reinterpret_cast<const bf16*>(&data[i]), x);
+      }
+      T* d = out + (long long)(i0 + i * rows) * a.row_stride;
+      if constexpr (sizeof(T) == 2) {
+        store_vec(d, x);
+      } else {
+        const float x0[4] = {x[0], x[1], x[2], x[3]}, x1[4] = {x[4], x[5], x[6], x[7]};
+        store_vec(d, x0);
+        store_vec(d + 4, x1);
+      }
+    }
   }
 }
 

@@ -17,6 +17,7 @@ namespace sm {
 constexpr int kThreads = 256;
 constexpr int kMaxBatch = 16384;       // lengths and two prefix sums in shared memory
 constexpr int kPage = 64;
+constexpr int kFewPages = 2;           // new pages of a request that one thread enters by itself
 
 struct Args {
   const int* held;
@@ -103,15 +104,30 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
   __syncthreads();
   const int total = s_start[a.batch];
 
-  // Per request: offsets, slot counts, the new entries of its table row (a warp per request).
-  for (int b = blockIdx.x * (kThreads / 32) + warp; b < a.batch; b += gridDim.x * (kThreads / 32)) {
-    const int h = s_held[b];
-    const int have = pages_of(h, a.stride), p0 = s_page[b], n_new = s_page[b + 1] - p0;
-    if (lane == 0) {
-      a.starts[b] = s_start[b];
-      a.slots[b] = (int)slots_of((uint32_t)h + (s_start[b + 1] - s_start[b]), a.stride);
+  // Per request, a thread each: offsets, slot counts, the new entries of its table row; rows with more
+  // than a few new entries are written by the whole warp.
+  // Consecutive requests go to different CTAs.
+  for (int i0 = warp * 32; (long long)i0 * gridDim.x + blockIdx.x < a.batch; i0 += kThreads) {
+    const int b = (int)min((long long)a.batch, (long long)(i0 + lane) * gridDim.x + blockIdx.x);
+    int have = 0, p0 = 0, n_new = 0;
+    if (b < a.batch) {
+      const int h = s_held[b], first = s_start[b];
+      have = pages_of(h, a.stride);
+      p0 = s_page[b];
+      n_new = s_page[b + 1] - p0;
+      a.starts[b] = first;
+      a.slots[b] = (int)slots_of((uint32_t)h + (s_start[b + 1] - first), a.stride);
+      if (n_new <= kFewPages)
+        for (int i = 0; i < n_new; ++i) a.table[(long long)b * a.width + have + i] = a.free_pages[p0 + i];
     }
-    for (int i = lane; i < n_new; i += 32) a.table[(long long)b * a.width + have + i] = a.free_pages[p0 + i];
+    uint32_t big = __ballot_sync(0xffffffffu, n_new > kFewPages);
+    while (big) {
+      const int src = __ffs(big) - 1;
+      big &= big - 1;
+      const int bb = __shfl_sync(0xffffffffu, b, src), hh = __shfl_sync(0xffffffffu, have, src), pp = __shfl_sync(0xffffffffu, p0, src),
+                nn = __shfl_sync(0xffffffffu, n_new, src);
+      for (int i = lane; i < nn; i += 32) a.table[(long long)bb * a.width + hh + i] = a.free_pages[pp + i];
+    }
   }
   if (blockIdx.x == 0 && tid == 0) {
     a.starts[a.batch] = total;
