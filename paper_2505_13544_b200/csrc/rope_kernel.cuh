@@ -46,7 +46,7 @@ struct Args {
 // A unit of work is, with VEC, 16 bytes (interleaved pairs and plain elements) or two runs of 16
 // bytes, one from each half (half layout); without VEC, one pair or one plain element.
 template <typename T, bool VEC, bool HALF>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 4) rope_kernel(const __grid_constant__ Args a) {
   constexpr int V = VEC ? Elem<T>::kVec : 1;
   constexpr int kU = 4;                         // tokens of a thread in flight
   extern __shared__ __align__(16) float2 cs[];  // [tokens_per_cta][pairs]
