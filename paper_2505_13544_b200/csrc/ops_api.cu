@@ -63,11 +63,11 @@ int launched() { return cudaGetLastError() == cudaSuccess ? MTLA_OK : MTLA_ERR_C
 
 // Raises a kernel's dynamic shared-memory limit to what one CTA may have, once per device.
 template <auto Kernel>
-bool raise_smem(int device) {
+bool raise_smem(int device, int bytes = 227 * 1024 - 1024) {
   static std::atomic<uint64_t> done{0};
   const uint64_t bit = device < 64 ? 1ull << device : 0;
   if (bit && (done.load(std::memory_order_acquire) & bit)) return true;
-  if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024) != cudaSuccess)
+  if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
     return false;
   done.fetch_or(bit, std::memory_order_release);
   return true;
@@ -142,11 +142,12 @@ int launch_dependent(K* kernel, dim3 grid, int threads, size_t smem, cudaStream_
 }
 
 template <typename T>
-int launch_combine(const qp::AttnArgs& a, cudaStream_t st) {
+int launch_combine(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
+  if (!raise_smem<qp::qpool_combine_kernel<T>>(dev.device(), qp::kMaxBatch * 16)) return MTLA_ERR_CUDA;
   // As many CTAs as there can be pieces of split or empty sequences, six per SM at most.
   const long long pieces = (long long)a.batch * a.n_heads * ceil_div(a.f.r, qp::kCombineCols), most = 6 * kPlanSms;
   return launch_dependent(qp::qpool_combine_kernel<T>, dim3((unsigned)(pieces < most ? pieces : most)),
-                          qp::kCombineThreads, (size_t)a.batch * 4, st, a);
+                          qp::kCombineThreads, (size_t)a.batch * 16, st, a);
 }
 
 template <typename T, int MH>
@@ -160,7 +161,7 @@ int launch_attend(qp::AttnArgs a, const OnDeviceOf& dev, cudaStream_t st) {
   const long long most = (long long)a.batch * a.width;
   const int ctas = (int)(most < (long long)per_sm * sms ? most : (long long)per_sm * sms);
   const int status = launch_dependent(qp::qpool_attend_kernel<T, MH>, dim3(ctas), qp::kAttnThreads, smem, st, a);
-  return status == MTLA_OK ? launch_combine<T>(a, st) : status;
+  return status == MTLA_OK ? launch_combine<T>(a, dev, st) : status;
 }
 
 template <int NHP, int NB>
@@ -174,7 +175,7 @@ int launch_attend_tc(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t 
                                 qp::kQueryThreads, 0, st, a);
   if (status == MTLA_OK)
     status = launch_dependent(qp::qpool_attend_tc_kernel<NHP, NB>, dim3(ctas), qp::tc::kThreads, l.total, st, a);
-  return status == MTLA_OK ? launch_combine<bf16>(a, st) : status;
+  return status == MTLA_OK ? launch_combine<bf16>(a, dev, st) : status;
 }
 template <int NHP>
 int launch_attend_tc(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
@@ -409,7 +410,12 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
   a.q_unit = reinterpret_cast<float*>(ws + p.q_unit);
   a.error_word = reinterpret_cast<int*>(ws + p.error_word);
   const bool wide = cfg->n_heads > 16;
-  if (dtype == MTLA_DTYPE_BF16 && B <= qp::tc::kMaxBatch)
+  // The tensor-core kernel, except where its longer set-up shows: at most a page per SM of up to 256
+  // latents (8 heads, r 64, one slot tile: 9.0 us against 7.2; 64 sequences of two pages, r 256: 13.9
+  // against 12.1; but 8 sequences of two pages, r 512: 14.3 against 15.6).  fp32 queries, and batches
+  // whose prefix sums outgrow its shared memory, also take the other one.
+  const bool small = (long long)B * table_width <= kPlanSms && cfg->latent_rank <= 256;
+  if (dtype == MTLA_DTYPE_BF16 && B <= qp::tc::kMaxBatch && !small)
     return wide ? launch_attend_tc<32>(a, dev, st) : launch_attend_tc<16>(a, dev, st);
   if (dtype == MTLA_DTYPE_BF16)
     return wide ? launch_attend<bf16, 2>(a, dev, st) : launch_attend<bf16, 1>(a, dev, st);

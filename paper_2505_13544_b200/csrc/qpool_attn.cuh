@@ -118,8 +118,10 @@ __device__ __forceinline__ void decode_pairs(uint32_t w, uint32_t (&o)[4]) {
 }
 
 // Prefix sums of the sequences' tile counts (PAGES pages each) into prefix[0 .. batch]; returns the total.
+// With `slots` the (non-negative) slot counts are left there for whoever needs them later.
 template <int PAGES>
-__device__ inline long long tile_prefix(const AttnArgs& a, int* prefix, int* warp_sums, int threads) {
+__device__ inline long long tile_prefix(const AttnArgs& a, int* prefix, int* warp_sums, int threads,
+                                        int* slots = nullptr) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = ceil_div(a.batch, threads);
   const int lo = min(a.batch, tid * per), hi = min(a.batch, lo + per);
@@ -129,6 +131,7 @@ __device__ inline long long tile_prefix(const AttnArgs& a, int* prefix, int* war
     const int n = max(a.slots[b], 0);
     const int pages = min(n / kPageRows + (n % kPageRows != 0), a.width), t = (pages + PAGES - 1) / PAGES;
     prefix[b + 1] = t;
+    if (slots) slots[b] = n;
     sum += t;
   }
   int incl = sum;
@@ -139,11 +142,13 @@ __device__ inline long long tile_prefix(const AttnArgs& a, int* prefix, int* war
   }
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
-  int run = incl - sum;
-  for (int w = 0; w < warp; ++w) run += warp_sums[w];
-  for (int b = lo; b < hi; ++b) {
-    run += prefix[b + 1];
-    prefix[b + 1] = run;
+  if (lo < hi) {                       // most warps of a small batch have nothing to add up
+    int run = incl - sum;
+    for (int w = 0; w < warp; ++w) run += warp_sums[w];
+    for (int b = lo; b < hi; ++b) {
+      run += prefix[b + 1];
+      prefix[b + 1] = run;
+    }
   }
   if (tid == 0) prefix[0] = 0;
   __syncthreads();
@@ -506,27 +511,28 @@ __device__ __forceinline__ void store4(bf16* p, const float (&v)[4]) {
 }
 template <typename T>
 __global__ void __launch_bounds__(kCombineThreads) qpool_combine_kernel(AttnArgs a) {
-  extern __shared__ int listed[];                    // [batch]
+  extern __shared__ int4 listed[];                   // [batch] sequence, first part, parts (0: no slot)
   __shared__ int2 warp_count[kCombineThreads / 32];
-  __shared__ float weight[kMaxParts], red[kCombineThreads / 32], total[1];
+  __shared__ float weight[kMaxParts], red[kCombineThreads / 32], total[kCombineThreads / 32];
   __shared__ float4 sums[kCombineGroups][kCombineCols / 4];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = a.f.r, heads = a.n_heads;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const bool failed = a.error_word && *a.error_word; // a bounded wait gave up: no result that looks like one
+  const int* error = a.error_word;
+  // A bounded wait gave up: no result that looks like one.
+  const bool failed = error != nullptr && *error != 0;
   // Sequences with few parts (or none, or no result) from the front of the list, the others from its
   // end, both in order: every CTA has the same list.
   int n_few = 0, n_many = 0;
   for (int b0 = 0; b0 < a.batch; b0 += kCombineThreads) {
     const int b = b0 + tid;
     int kind = 0;                                    // 1 few, 2 many
+    int2 parts = make_int2(0, 0);
     if (b < a.batch) {
-      if (failed || a.slots[b] <= 0) {
-        kind = 1;
-      } else {
-        const int n = a.seq_parts[b].y;
-        kind = n == 0 ? 0 : n <= kFewParts ? 1 : 2;
-      }
+      const int n = a.slots[b];
+      parts = a.seq_parts[b];                        // (not set for a sequence without slots)
+      if (n <= 0) parts.y = 0;
+      kind = failed || n <= 0 ? 1 : parts.y == 0 ? 0 : parts.y <= kFewParts ? 1 : 2;
     }
     const uint32_t few = __ballot_sync(0xffffffffu, kind == 1), many = __ballot_sync(0xffffffffu, kind == 2);
     if (lane == 0) warp_count[warp] = make_int2(__popc(few), __popc(many));
@@ -540,21 +546,22 @@ __global__ void __launch_bounds__(kCombineThreads) qpool_combine_kernel(AttnArgs
       n_few += c.x;
       n_many += c.y;
     }
-    if (kind == 1) listed[at_few] = b;
-    if (kind == 2) listed[a.batch - 1 - at_many] = b;
+    if (kind == 1) listed[at_few] = make_int4(b, parts.x, parts.y, 0);
+    if (kind == 2) listed[a.batch - 1 - at_many] = make_int4(b, parts.x, parts.y, 0);
     __syncthreads();
   }
 
   const int seq_pieces = (heads * r + 4 * kCombineThreads - 1) / (4 * kCombineThreads);
   for (long long w = blockIdx.x; w < (long long)n_few * seq_pieces; w += gridDim.x) {
-    const int b = listed[w / seq_pieces], e = ((int)(w % seq_pieces) * kCombineThreads + tid) * 4;
+    const int4 seq = listed[w / seq_pieces];
+    const int b = seq.x, e = ((int)(w % seq_pieces) * kCombineThreads + tid) * 4;
     if (e >= heads * r) continue;
     const int h = e / r;
     const float fill = failed ? NAN : 0.f;
     float v[4] = {fill, fill, fill, fill};
     float lse = failed ? NAN : -INFINITY;
-    if (!failed && a.slots[b] > 0) {
-      const int2 parts = a.seq_parts[b];
+    if (!failed && seq.z > 0) {
+      const int2 parts = make_int2(seq.y, seq.z);
       const float2* ml = reinterpret_cast<const float2*>(a.ml_part) + (long long)parts.x * heads + h;
       const float* o = a.o_part + (long long)parts.x * heads * r + e;
       const long long o_step = (long long)heads * r;
@@ -589,48 +596,61 @@ __global__ void __launch_bounds__(kCombineThreads) qpool_combine_kernel(AttnArgs
   const int col_blocks = (r + kCombineCols - 1) / kCombineCols;
   for (long long w = blockIdx.x; w < (long long)n_many * heads * col_blocks; w += gridDim.x) {
     const int cb = (int)(w % col_blocks), bh = (int)(w / col_blocks), h = bh % heads;
-    const int b = listed[a.batch - 1 - bh / heads], col = cb * kCombineCols + lane * 4;
+    const int4 seq = listed[a.batch - 1 - bh / heads];
+    const int b = seq.x, n_parts = seq.z, col = cb * kCombineCols + lane * 4;
     float lse;
     float4 sum;
     {
-      const int2 parts = a.seq_parts[b];
-      const float* ml = a.ml_part + ((long long)parts.x * heads + h) * 2;
-      const float* o = a.o_part + ((long long)parts.x * heads + h) * r + col;
-      const long long ml_step = 2ll * heads, o_step = (long long)heads * r;
+      const float2* ml = reinterpret_cast<const float2*>(a.ml_part) + (long long)seq.y * heads + h;
+      const float* o = a.o_part + ((long long)seq.y * heads + h) * r + col;
+      const long long o_step = (long long)heads * r;
+      // The first loads of the sums do not wait for the weights.
+      constexpr int kU = 4;
+      float4 x[kU];
+      auto load = [&](int p0) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int p = p0 + u * kCombineGroups;
+          x[u] = col < r && p < n_parts ? *reinterpret_cast<const float4*>(o + p * o_step)
+                                        : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      };
+      load(warp);
+      // A thread's parts: at most two (kMaxParts over the threads).
+      float2 mine[2];
       float m = -INFINITY;
-      for (int p = tid; p < parts.y; p += kCombineThreads) m = fmaxf(m, ml[p * ml_step]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int p = tid + i * kCombineThreads;
+        mine[i] = p < n_parts ? ml[(long long)p * heads] : make_float2(-INFINITY, 0.f);
+        m = fmaxf(m, mine[i].x);
+      }
       m = warp_max(m);
       if (lane == 0) red[warp] = m;
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < kCombineThreads / 32; ++i) m = fmaxf(m, red[i]);
       const float ref = m == -INFINITY ? 0.f : m;
-      for (int p = tid; p < parts.y; p += kCombineThreads) weight[p] = exp2f(ml[p * ml_step] - ref);
-      __syncthreads();
-      // The denominator: warp 0, a lane's parts in order, then the lanes in order.
-      if (warp == 0) {
-        float l = 0.f;
-        for (int p = lane; p < parts.y; p += 32) l += weight[p] * ml[p * ml_step + 1];
-        l = warp_sum(l);
-        if (lane == 0) total[0] = l;
+      float l = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int p = tid + i * kCombineThreads;
+        const float f = p < n_parts ? exp2f(mine[i].x - ref) : 0.f;
+        if (p < n_parts) weight[p] = f;
+        l += p < n_parts ? f * mine[i].y : 0.f;
       }
+      l = warp_sum(l);
+      if (lane == 0) total[warp] = l;
+      __syncthreads();
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (col < r) {
-        constexpr int kU = 4;
-        for (int p0 = warp; p0 < parts.y; p0 += kU * kCombineGroups) {
-          float4 x[kU];
+      for (int p0 = warp; p0 < n_parts; p0 += kU * kCombineGroups) {
 #pragma unroll
-          for (int u = 0; u < kU; ++u) {
-            const int p = p0 + u * kCombineGroups;
-            x[u] = p < parts.y ? *reinterpret_cast<const float4*>(o + p * o_step) : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
-#pragma unroll
-          for (int u = 0; u < kU; ++u) {
-            const int p = p0 + u * kCombineGroups;
-            const float f = p < parts.y ? weight[p] : 0.f;
-            v.x += f * x[u].x; v.y += f * x[u].y; v.z += f * x[u].z; v.w += f * x[u].w;
-          }
+        for (int u = 0; u < kU; ++u) {
+          const int p = p0 + u * kCombineGroups;
+          const float f = p < n_parts ? weight[p] : 0.f;
+          v.x += f * x[u].x; v.y += f * x[u].y; v.z += f * x[u].z; v.w += f * x[u].w;
         }
+        load(p0 + kU * kCombineGroups);
       }
       sums[warp][lane] = v;
       __syncthreads();
@@ -640,7 +660,9 @@ __global__ void __launch_bounds__(kCombineThreads) qpool_combine_kernel(AttnArgs
         const float4 x = sums[i][lane];
         sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
       }
-      const float l = total[0];
+      l = 0.f;
+#pragma unroll
+      for (int i = 0; i < kCombineThreads / 32; ++i) l += total[i];
       sum.x /= l; sum.y /= l; sum.z /= l; sum.w /= l;
       lse = (m + log2f(l)) * 0.69314718055994531f;
     }

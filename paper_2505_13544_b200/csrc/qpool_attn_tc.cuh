@@ -92,7 +92,7 @@ static_assert(sizeof(Misc) <= 2048, "misc region too small");
 struct Layout {
   int codes, scales, keys;                  // offsets in a stage
   int stage, stages;
-  int off_q, q_bytes, off_p, off_st, off_misc, off_prefix, total;
+  int off_q, q_bytes, off_p, off_st, off_misc, off_prefix, off_slots, total;
   __host__ __device__ Layout(const Format& f, int nhp, int batch) {
     keys = 0;                                            // swizzled operand: 1024-byte aligned
     codes = kTile * f.key_row();
@@ -101,7 +101,7 @@ struct Layout {
     q_bytes = nhp * 2 * (f.r + f.dr);
     const int q_room = (q_bytes + 1023) / 1024 * 1024, p_room = 2 * kTile * nhp * 2;
     const int scale_room = f.scale_row() * kTile * 2;
-    const int fixed = q_room + p_room + 2048 + (batch + 1) * 4 + 1024;   // 1024: alignment of the base
+    const int fixed = q_room + p_room + 2048 + (2 * batch + 1) * 4 + 1024;   // 1024: alignment of the base
     // At least three (r 512, 32 heads, d_R 64: exactly), which the expansion's waits rely on; with one
     // unit a tile (r <= 128) always four, as many as a tile's value operands may lag.
     stages = (kSmemMax - fixed) / (stage + scale_room);
@@ -111,7 +111,8 @@ struct Layout {
     off_st = off_p + p_room;
     off_misc = off_st + stages * scale_room;
     off_prefix = off_misc + 2048;
-    total = off_prefix + (batch + 1) * 4 + 1024;
+    off_slots = off_prefix + (batch + 1) * 4;
+    total = off_slots + batch * 4 + 1024;
   }
 };
 
@@ -186,6 +187,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   uint8_t* sm = smem_raw + (base - raw);
   Misc* misc = reinterpret_cast<Misc*>(sm + L.off_misc);
   int* prefix = reinterpret_cast<int*>(sm + L.off_prefix);
+  int* slots_s = reinterpret_cast<int*>(sm + L.off_slots);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // warp: uniform
   auto bar = [&](unsigned long long& p) { return smem_u32(&p); };
 
@@ -223,7 +225,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   grid_launch_dependents();      // this CTA owns its TMEM columns (see decode_attn_tc.cuh)
   grid_dependency_wait();
 
-  const long long total = tile_prefix<2>(a, prefix, misc->warp_sums, kThreads);
+  const long long total = tile_prefix<2>(a, prefix, misc->warp_sums, kThreads, slots_s);
   const int ctas = (int)(total < gridDim.x ? total : gridDim.x);
   int g0 = 0, g1 = 0;
   if ((int)blockIdx.x < ctas) {
@@ -254,7 +256,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       for (int n = 0; n < n_tiles; ++n) {
         const int g = g0 + n;
         while (prefix[b + 1] <= g) ++b;
-        const int tile = g - prefix[b], slots = a.slots[b];
+        const int tile = g - prefix[b], slots = slots_s[b];
         const bool first = n == 0 || tile == 0, last = n + 1 == n_tiles || g + 1 == prefix[b + 1];
         int page[2], rows[2];
 #pragma unroll
@@ -710,19 +712,25 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         // Lane 8j + g of a quarter holds latent 4g + j.
         const int lat = q * 32 + 4 * (lane & 7) + (lane >> 3);
         const long long at = (long long)(whole ? b : part) * a.n_heads * r + lat;
+        constexpr int STEP = NB > 1 ? 2 : 1;             // blocks whose loads are in flight together
 #pragma unroll 1
-        for (int mb = 0; mb < NB; ++mb) {
-          uint32_t ov[16];
-          ld_cols(lane_base + kColO + mb * NHP, ov);
-          tmem_wait_ld();
-          if (mb * 128 + lat >= r) continue;
+        for (int mb = 0; mb < NB; mb += STEP) {
+          uint32_t ov[STEP][16];
 #pragma unroll
-          for (int i = 0; i < NHH; ++i) {
-            if (HO + i >= a.n_heads) break;
-            const long long e = at + (HO + i) * r + mb * 128;
-            const float v = __uint_as_float(ov[i]);
-            if (whole) static_cast<bf16*>(a.out)[e] = __float2bfloat16_rn(v * misc->unit[HO + i]);
-            else a.o_part[e] = v;
+          for (int j = 0; j < STEP; ++j)
+            if (mb + j < NB) ld_cols(lane_base + kColO + (mb + j) * NHP, ov[j]);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < STEP; ++j) {
+            if (mb + j >= NB || (mb + j) * 128 + lat >= r) continue;
+#pragma unroll
+            for (int i = 0; i < NHH; ++i) {
+              if (HO + i >= a.n_heads) break;
+              const long long e = at + (HO + i) * r + (mb + j) * 128;
+              const float v = __uint_as_float(ov[j][i]);
+              if (whole) static_cast<bf16*>(a.out)[e] = __float2bfloat16_rn(v * misc->unit[HO + i]);
+              else a.o_part[e] = v;
+            }
           }
         }
         tc_fence_before_sync();
