@@ -64,6 +64,23 @@ def test_slot_map(stride, batch, held_max, fresh_max, pad):
     check_map(m, t, want, table, sum(fresh), pad)
 
 
+def test_slot_map_of_the_largest_batch():
+    rng = np.random.default_rng(1)
+    held = [int(v) for v in rng.integers(0, 300, 16384)]
+    fresh = [int(v) for v in rng.integers(0, 3, 16384)]
+    m, t, table, free = run_map(held, fresh, 2, 4, 5)
+    want = Q.slot_map(held, fresh, 2, table, free)
+    check_map(m, t, want, table, sum(fresh), 5)
+
+
+def test_slot_map_of_positions_near_the_integer_limit():
+    """One request with almost 2^31 tokens at a stride that leaves few slots."""
+    held, fresh, stride = [2 ** 31 - 5], [4], 1 << 26
+    m, t, table, free = run_map(held, fresh, stride, 2)
+    want = Q.slot_map(held, fresh, stride, table, free)
+    check_map(m, t, want, table, 4, 0)
+
+
 def test_slot_map_without_tokens_and_misaligned_outputs():
     m, t, table, free = run_map([5, 0, 64], [0, 0, 0], 1, 2)
     want = Q.slot_map([5, 0, 64], [0, 0, 0], 1, table, free)
@@ -180,6 +197,21 @@ def test_rope_of_queries_and_shared_key_in_one_launch():
         assert (np.abs(host(y) - want) <= rope_bound(x, want, first, 32, "interleaved", 1.0, "fp32")).all()
 
 
+@pytest.mark.parametrize("n,heads,width,first,dim", [(1, 600, 80, 16, 64), (40000, 1, 16, 0, 16), (700, 33, 8, 0, 8)])
+def test_rope_shapes_of_work(n, heads, width, first, dim):
+    """One token of many heads (several rounds of a CTA's threads), many short tokens side by side."""
+    case = ("bf16", n, heads, width, first, dim, "half" if n == 1 else "interleaved", "linear")
+    x, pos, cfg, f, mag = rope_setup(case, 2)
+    rows = np.unique(np.linspace(0, n - 1, 60).astype(int))
+    (y,) = M.mtla_rope(cfg, [x.cuda()], pos.cuda(), first=first)
+    y = y.cpu()
+    want = Q.rope(host(x[rows]), pos[rows].tolist(), f, case[6], first, mag)
+    assert (np.abs(host(y[rows]) - want) <= rope_bound(x[rows], want, first, dim, case[6], mag, "bf16")).all()
+    # Rows that were not computed by the oracle keep their length, pair by pair.
+    norm = lambda v: v.double().square().sum(-1).sqrt()
+    assert (torch.abs(norm(y) - norm(x)) <= norm(x) * 2 * half_step(torch.bfloat16) + 1e-6).all()
+
+
 def test_rope_gradient_is_the_formula_and_the_difference_quotient():
     """For L = <w, rope(x)> the gradient is the inverse applied to w; L is linear, so a difference
     quotient of the forward call has no truncation error, only the roundings of two sums of 32-bit
@@ -275,6 +307,26 @@ def test_pool_write_and_read(dtype, r, dr, n):
         value = np.concatenate([Q.dequantise(byte, code), host(x[:, r:].bfloat16())], 1)
         value[(index < 0) | (index >= n_pages * 64)] = 0
         assert np.array_equal(host(got), value, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_pool_rows_of_a_long_prompt(dtype):
+    """More rows than one round of CTAs holds at once, most of them skipped."""
+    r, dr, n = 128, 32, 70000
+    cfg, pages = pool(r, dr, 300)
+    x = torch.randn(n, r + dr, generator=torch.Generator().manual_seed(4)).to(DT[dtype])
+    index = torch.full((n,), -1, dtype=torch.int64)
+    kept = torch.arange(3, n, 5)
+    index[kept] = torch.randperm(300 * 64, generator=torch.Generator().manual_seed(5))[:len(kept)]
+    M.mtla_qpool_write(cfg, pages, x.cuda(), index.cuda())
+    got = M.mtla_qpool_read(cfg, pages, index.cuda(), dtype=torch.float32).cpu()
+    skipped = torch.ones(n, dtype=torch.bool)
+    skipped[kept] = False
+    assert (got[skipped] == 0).all()
+    some = kept[::37]
+    byte, code = Q.quantise(host(x[some])[:, :r])
+    assert np.array_equal(host(got[some])[:, :r], Q.dequantise(byte, code))
+    assert torch.equal(got[kept][:, r:], x[kept][:, r:].bfloat16().float())
 
 
 def test_pool_read_into_strided_rows_leaves_the_rest():
@@ -382,6 +434,46 @@ def test_attend_more_tiles_than_one_share(dtype):
     lens = [int(v) for v in rng.integers(0, 130, 500)] + [9000, 0, 3000]
     s = attend_setup(lens, 6, 64, 32, dtype, 8)
     check_attend(*s, 0.2, dtype, lens)
+
+
+@pytest.mark.parametrize("extra", [0, 200])
+@pytest.mark.parametrize("lens,heads,r,dr", [([1, 64, 65, 130, 0, 7], 8, 64, 64), ([257], 32, 256, 32), ([90, 33], 20, 192, 64)])
+def test_attend_both_kernels_on_one_batch(lens, heads, r, dr, extra):
+    """A wide table sends the same bf16 batch to the tensor-core kernel, a narrow one to the other."""
+    cfg, pages, table, slots, q, seqs = attend_setup(lens, heads, r, dr, "bf16", 40)
+    wide = torch.full((len(lens), table.shape[1] + extra), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    check_attend(cfg, pages, wide, slots, q, seqs, 0.125, "bf16", lens)
+
+
+def test_attend_batch_beyond_the_tensor_core_kernels_lists():
+    rng = np.random.default_rng(7)
+    lens = [int(v) for v in rng.integers(0, 90, 1100)]
+    s = attend_setup(lens, 3, 64, 32, "bf16", 41)
+    check_attend(*s, 0.2, "bf16", lens)
+
+
+@pytest.mark.parametrize("r,dr,heads", [(64, 32, 8), (128, 64, 32), (256, 32, 16), (320, 64, 17), (384, 64, 32), (448, 32, 4),
+                                        (512, 64, 32), (512, 64, 9)])
+def test_attend_many_tiles_and_segments_per_cta(r, dr, heads):
+    """Every CTA walks several tiles of several sequences: rings and phases wrap around more than once."""
+    rng = np.random.default_rng(r)
+    lens = [int(v) for v in rng.integers(0, 1500, 300)] + [0, 1, 128, 129, 5000]
+    s = attend_setup(lens, heads, r, dr, "bf16", 42)
+    cfg, pages, table, slots, q, seqs = s
+    out, lse = M.mtla_qpool_attend(cfg, pages, table, slots, q.cuda(), scale=0.125)
+    assert torch.isfinite(out.float()).all()
+    again, _ = M.mtla_qpool_attend(cfg, pages, table, slots, q.cuda(), scale=0.125)
+    assert torch.equal(out, again)
+    got, got_lse = host(out), host(lse)
+    for b in list(range(0, 305, 17)) + [300, 301, 302, 303, 304]:
+        want, want_lse, mean_abs = Q.attend(host(q[b]), seqs[b][:, :r], seqs[b][:, r:], 0.125)
+        if lens[b] == 0:
+            assert (got[b] == 0).all() and np.isneginf(got_lse[b]).all()
+            continue
+        tol, tol_lse = bound(host(q[b]), seqs[b], 0.125, mean_abs, want, "bf16", r)
+        assert (np.abs(got[b] - want) <= tol).all(), (b, lens[b])
+        assert (np.abs(got_lse[b] - want_lse) <= tol_lse + 2.0 ** -23 * np.abs(want_lse)).all(), b
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
