@@ -24,7 +24,7 @@
 // Queries arrive as an image of the B operand that qpool_query_kernel has written (half precision
 // scaled by a power of two per head, swizzled), so that a segment's query is one bulk copy.
 //
-// Roles (28 warps): warp 0 issues the score products, warp 1 the value products, warp 2 is the
+// Roles (28 warps): warps 0 and 3 issue the score products, warp 1 the value products, warp 2 is the
 // producer; warps 4-19 expand, in four groups that take turns (see there); warps 20-27 are softmax
 // and epilogue.  The hot loops are short on purpose: with several kinds of code on every scheduler,
 // fetching unrolled instructions was the longest stall (107 KB of them: 517 us at 128 x 16384
@@ -46,7 +46,7 @@ constexpr int kTile = 128;                  // slots per tile: two pages
 constexpr int kThreads = 896;
 constexpr int kMaxStages = 4;
 constexpr int kMaxBatch = 1022;             // prefix sums kept in shared memory
-constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2;
+constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kScoreIssuer2 = 3;
 constexpr int kExpandWarp0 = 4, kExpandGroups = 4;
 constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
 constexpr int kInfo = 16;                   // ring of tile descriptions, deeper than any role's lag
@@ -72,9 +72,10 @@ struct TileInfo {
 struct Misc {
   unsigned long long raw_full[kMaxStages], raw_empty[kMaxStages], scale_full[kMaxStages];
   // Operand units (a quarter of r of one tile) are numbered through; unit k's barriers are those of k
-  // mod 4, its buffer is shared with fewer units.  Who fills unit k waits for the unit that had the
-  // buffer before, and sees every phase of that unit's barrier.
-  unsigned long long as_full[4], as_empty[4], av_full[4], av_empty[4];
+  // mod 8 (scores) or 4 (values), its buffer is shared with fewer units.  Who fills unit k waits for the
+  // unit that had the buffer before, and who reads it waits for it; both see every phase of the
+  // barriers they wait for.
+  unsigned long long as_full[8], as_empty[8], av_full[4], av_empty[4];
   unsigned long long s_full[2], s_empty[2], p_full[2], p_empty[2], q_full, q_empty;
   unsigned long long info_full[kInfo];
   uint32_t tmem_base;
@@ -178,6 +179,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   constexpr uint32_t IDESC_S = make_idesc_f16(128, NHP, 0, 0), IDESC_K = make_idesc_bf16(128, NHP, 0, 0);
   constexpr uint32_t IDESC_V = make_idesc_f16(128, NHP, 0, 1);
   constexpr uint32_t P_BYTES = kTile * NHP * 2, P_SBO = kTile * 16;   // bytes between groups of 8 heads
+  constexpr int SI = NB == 3 ? 1 : 2;           // score issuers (see there)
   constexpr int AVB = av_buffers(NHP), COL_AS = col_as(NHP), COL_AV = col_av(NHP);
   extern __shared__ uint8_t smem_raw[];
   const Format f = a.f;
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   if (threadIdx.x == 0) {
     for (int i = 0; i < L.stages; ++i) {
       mbar_init(bar(misc->raw_full[i]), 1);
-      mbar_init(bar(misc->raw_empty[i]), 2 * NB * 4 + 1);        // a warp of each unit, the key products
+      mbar_init(bar(misc->raw_empty[i]), 2 * NB * 4 + SI);       // a warp of each unit, the score issuers
       mbar_init(bar(misc->scale_full[i]), NB * 4);
     }
     for (int i = 0; i < 2; ++i) {
@@ -203,15 +205,17 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       mbar_init(bar(misc->p_full[i]), kSoftmaxWarps);
       mbar_init(bar(misc->p_empty[i]), 1);
     }
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
       mbar_init(bar(misc->as_full[i]), 4);
       mbar_init(bar(misc->as_empty[i]), 1);
+    }
+    for (int i = 0; i < 4; ++i) {
       mbar_init(bar(misc->av_full[i]), 4);
       mbar_init(bar(misc->av_empty[i]), 1);
     }
     for (int i = 0; i < kInfo; ++i) mbar_init(bar(misc->info_full[i]), 1);
     mbar_init(bar(misc->q_full), 1);
-    mbar_init(bar(misc->q_empty), 1);
+    mbar_init(bar(misc->q_empty), SI);
     misc->abort_word = 0;
     mbar_fence_init();
   }
@@ -298,16 +302,21 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         }
         if (++st == L.stages) { st = 0; ++round; }
       }
-    } else if (warp == kScoreIssuer) {
+    } else if (warp == kScoreIssuer || (SI == 2 && warp == kScoreIssuer2)) {
       // ---------------------------------------------------------------- score products (whole warp, uniform)
+      // Two warps issue them, a tile each in turn (the tiles' accumulators alternate anyway): with the
+      // memory instruction queues full of the expansion's traffic a wait, even for what is there,
+      // takes some 300 cycles, and one warp's waits took all of a tile's time.  Each still looks at
+      // every tile, so that it sees every phase of the barriers.  (With three units a tile the units'
+      // barriers would change hands between the two, so there one warp does it all.)
+      const int mine = warp == kScoreIssuer ? 0 : 1;
       const uint64_t mode = dr == 64 ? kSwizzle128B : kSwizzle64B;
       const uint32_t key_sbo = 8 * f.key_row();
       const uint64_t q_desc = make_smem_desc(q_u32, 16, 1024, kSwizzle128B);
       const uint64_t qk_desc = make_smem_desc(q_u32 + NHP * 2 * r, 16, key_sbo, mode);
       int seg = 0, st = 0, round = 0;
-      bool unit_there = false, raw_there = false, room_there = false;
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = __all_sync(0xffffffffu, raw_there) || wait_warp(misc->raw_full[st], round);
+        ok = wait_warp(misc->raw_full[st], round);
         if (!ok) break;
         const int flags = misc->info[n % kInfo].flags;
         if (flags & 1) {
@@ -315,50 +324,49 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           if (!ok) break;
           ++seg;
         }
-        ok = __all_sync(0xffffffffu, room_there) || wait_warp(misc->s_empty[n & 1], (n >> 1) + 1);
-        if (!ok) break;
-        tc_fence_after_sync();
-        const uint32_t d = tmem + kColS + (n & 1) * 32;
-        const uint64_t key_desc = make_smem_desc(base + st * L.stage + L.keys, 16, key_sbo, mode);
-        if (elect_one()) {                               // RoPE part: d_R / 16 is 2 or 4
-          mma_bf16_ss(d, key_desc, qk_desc, IDESC_K, 0u);
-          mma_bf16_ss(d, key_desc + 2, qk_desc + 2, IDESC_K, 1u);
-          if (dr == 64) {
-            mma_bf16_ss(d, key_desc + 4, qk_desc + 4, IDESC_K, 1u);
-            mma_bf16_ss(d, key_desc + 6, qk_desc + 6, IDESC_K, 1u);
-          }
-        }
-        __syncwarp();
-#pragma unroll 1
-        for (int kq = 0; kq < NB; ++kq) {
-          const int k = n * NB + kq;
-          ok = __all_sync(0xffffffffu, unit_there) || wait_warp(misc->as_full[k & 3], k >> 2);
+        if (SI == 1 || (n & 1) == mine) {
+          ok = wait_warp(misc->s_empty[n & 1], (n >> 1) + 1);
           if (!ok) break;
-          unit_there = ask(misc->as_full[(k + 1) & 3], (k + 1) >> 2);
-          if (kq + 1 == NB) {
-            const bool wrap = st + 1 == L.stages;
-            raw_there = ask(misc->raw_full[wrap ? 0 : st + 1], wrap ? round + 1 : round);
-            room_there = ask(misc->s_empty[(n + 1) & 1], ((n + 1) >> 1) + 1);
-          }
           tc_fence_after_sync();
-          const uint32_t at = tmem + COL_AS + (k & 1) * 64;
-          const uint32_t panel = (uint32_t)q_desc + kq * 2 * NHP * 8, hi = (uint32_t)(q_desc >> 32);
-          if (elect_one()) {
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) mma_f16_ts(d, at + ks * 8, panel + ks * 2, hi, IDESC_S, 1u);
-            if (kq * 128 + 64 < r) {
-#pragma unroll
-              for (int ks = 0; ks < 4; ++ks)
-                mma_f16_ts(d, at + 32 + ks * 8, panel + NHP * 8 + ks * 2, hi, IDESC_S, 1u);
+          const uint32_t d = tmem + kColS + (n & 1) * 32;
+          const uint64_t key_desc = make_smem_desc(base + st * L.stage + L.keys, 16, key_sbo, mode);
+          if (elect_one()) {                             // RoPE part: d_R / 16 is 2 or 4
+            mma_bf16_ss(d, key_desc, qk_desc, IDESC_K, 0u);
+            mma_bf16_ss(d, key_desc + 2, qk_desc + 2, IDESC_K, 1u);
+            if (dr == 64) {
+              mma_bf16_ss(d, key_desc + 4, qk_desc + 4, IDESC_K, 1u);
+              mma_bf16_ss(d, key_desc + 6, qk_desc + 6, IDESC_K, 1u);
             }
-            mma_commit(bar(misc->as_empty[k & 3]));
           }
           __syncwarp();
-        }
-        if (!ok) break;
-        if (elect_one()) {
-          mma_commit(bar(misc->s_full[n & 1]));
-          mma_commit(bar(misc->raw_empty[st]));
+#pragma unroll 1
+          for (int kq = 0; kq < NB; ++kq) {
+            const int k = n * NB + kq;
+            ok = wait_warp(misc->as_full[k & 7], k >> 3);
+            if (!ok) break;
+            tc_fence_after_sync();
+            const uint32_t at = tmem + COL_AS + (k & 1) * 64;
+            const uint32_t panel = (uint32_t)q_desc + kq * 2 * NHP * 8, hi = (uint32_t)(q_desc >> 32);
+            if (elect_one()) {
+#pragma unroll
+              for (int ks = 0; ks < 4; ++ks) mma_f16_ts(d, at + ks * 8, panel + ks * 2, hi, IDESC_S, 1u);
+              if (kq * 128 + 64 < r) {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                  mma_f16_ts(d, at + 32 + ks * 8, panel + NHP * 8 + ks * 2, hi, IDESC_S, 1u);
+              }
+              mma_commit(bar(misc->as_empty[k & 7]));
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
+          if (elect_one()) {
+            mma_commit(bar(misc->s_full[n & 1]));
+            mma_commit(bar(misc->raw_empty[st]));
+            if (flags & 2) mma_commit(bar(misc->q_empty));
+          }
+        } else if (elect_one()) {
+          mbar_arrive(bar(misc->raw_empty[st]));
           if (flags & 2) mma_commit(bar(misc->q_empty));
         }
         __syncwarp();
@@ -421,7 +429,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       if (k < n_units) {
         // The buffer first: that unit k - 2 has been used also tells that the stage's phase is the one
         // before this tile's or later, which its parity alone would not.
-        ok = (k < 2 || wait(misc->as_empty[(k - 2) & 3], (k - 2) >> 2)) && wait(misc->raw_full[st], round);
+        ok = (k < 2 || wait(misc->as_empty[(k - 2) & 7], (k - 2) >> 3)) && wait(misc->raw_full[st], round);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after_sync();
@@ -465,7 +473,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(bar(misc->as_full[k & 3]));
+          mbar_arrive(bar(misc->as_full[k & 7]));
           if (NB != kExpandGroups) mbar_arrive(bar(misc->scale_full[st]));
           mbar_arrive(bar(misc->raw_empty[st]));
         }
