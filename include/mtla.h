@@ -393,6 +393,8 @@ int mtla_qpool_read(const mtla_qpool_config* cfg, const void* pages, const int64
  * dtype is that of q and out; sums, maxima and denominators are fp32.  A sequence without slots
  * (slots[b] <= 0) gives zeros and minus infinity.  slots[b] past 64 * table_width counts as that
  * many; slots of a page number outside the pool are left out, and a sequence with no other gives NaN.
+ * (Should a bounded wait inside the kernel give up, which nothing in a correct program leads to, all
+ * of out and lse is NaN.)
  * workspace: device, 256-byte aligned, mtla_qpool_workspace_bytes(cfg, B) bytes (0 if invalid); its
  * contents need no preparation, but two calls that may run at the same time need one each (graphs
  * that may overlap included).  B <= 4096. */

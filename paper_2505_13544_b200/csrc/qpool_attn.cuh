@@ -7,7 +7,12 @@
 // a sequence; such segments leave a partial (reference maximum, denominator, unnormalised output)
 // that qpool_combine_kernel joins in share order; a sequence that lies in one share is finished at once.
 //
-// The kernel of this file runs on the warp-level matrix instructions (m16n8k16), with the codes
+// The kernel of this file serves fp32 queries and the smallest batches (the other one is in
+// qpool_attn_tc.cuh; its rule is beside the launch).  Its
+// warps expand, multiply and reduce by turns, so it is bound by instruction issue: 1220 us at
+// 128 x 16384 slots, 32 heads, r 512, bf16, where the other takes 270.
+//
+// It runs on the warp-level matrix instructions (m16n8k16), with the codes
 // expanded from shared memory into registers in both fragment layouts:
 //   scores  S[heads x slots]   = Q[heads x r] . C^T   B fragment: a thread owns one slot and reads 16
 //                                                     bytes = 32 latents; the order of the latents in

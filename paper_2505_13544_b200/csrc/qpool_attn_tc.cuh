@@ -15,8 +15,19 @@
 //                                                               Lane 8j + g of a 32-lane quarter therefore
 //                                                               holds latent 4g + j; the output undoes it.
 // Shared memory then carries only the raw pages (three tiles of 128 slots deep), the queries and the
-// probabilities, and the kernel is bound by the instructions of the expansion (conversion, scale, and
-// for the values the pairing): about 60 per slot and warp lane, against 8 of matrix work.
+// probabilities.
+//
+// Measured at 128 sequences of 16384 slots, 32 heads, r 512, d_R 64: 270 us, 3.1 TB/s of pool, 48 % of
+// the measured copy bandwidth; the bytes alone would take 130 us.  Per tile of 128 slots that is about
+// 4500 cycles.  The expansion's conversions and scalings, which share a rate of 1.25 pairs of latents
+// per cycle and SM (measured), need 2300 of them, the matrix instructions 1100, the bytes 2100.  What
+// is between is the hand-over of the operand units: a unit's buffer goes from the expanding warps
+// through an mbarrier to the issuing warp, through the matrix unit and back in some 2200 cycles, since
+// with the memory instruction queues full of operand stores a wait takes 300 even for what is there.
+// Tensor memory has room for two units of the scores and three of the values beside the two
+// accumulators (three and two: 281 us).  At 32 sequences, 91 us with one score issuer, leaving out the
+// softmax gave 90 us, the matrix instructions 78, the operand stores 73, loads, arithmetic and
+// stores together 76, all of it 52.
 //
 // A head count of 16 or 32 is the matrix instructions' N, so heads are not padded further.  The RoPE
 // keys go from the pool to the score product as they are (bf16, shared memory, hardware swizzle).
@@ -28,7 +39,8 @@
 // producer; warps 4-19 expand, in four groups that take turns (see there); warps 20-27 are softmax
 // and epilogue.  The hot loops are short on purpose: with several kinds of code on every scheduler,
 // fetching unrolled instructions was the longest stall (107 KB of them: 517 us at 128 x 16384
-// slots, 61 KB: 362 us).
+// slots, 61 KB: 362 us), then the issuing threads' scalar descriptors (a uniform warp: 331), the sharing
+// out of the expansion (282) and a single score issuer (270 with two; a second value issuer adds nothing).
 // The online softmax raises a head's reference only when a tile exceeds it by 2^8.  Probabilities
 // are kept times 2^7: with the 2^8 they stay inside half precision.
 //

@@ -40,8 +40,8 @@ __device__ __forceinline__ int pages_of(uint32_t tokens, uint32_t stride) {
 }
 
 // PER: consecutive tokens of a thread.  Four give 16-byte stores where there are tokens for every SM;
-// with fewer, one token a thread keeps the chain of dependent loads short (128 tokens: 11.0 us with
-// four, see below for one).
+// with fewer, one token a thread keeps the chain of dependent loads short (128 requests of one token: 8.3
+// us with four, 3.1 us so; 400000 tokens: 7.0 us, of which the bytes are 1.5).
 template <int PER>
 __global__ void __launch_bounds__(kThreads) slot_map_kernel(Args a) {
   extern __shared__ int smem[];
