@@ -301,7 +301,8 @@ int mtla_train_backward(mtla_handle* h, const void* x, const void* dy, int32_t B
  * buffer, whichever GPU is current; all buffers of a call are that GPU's, and `stream` is one of
  * its streams.  All of them may be captured into CUDA graphs.  Errors are as for the handle calls;
  * what only the GPU can see (lengths, page numbers, indices) never leads outside the buffers, each
- * call says what becomes of it. */
+ * call says what becomes of it.  Calls for no tokens or rows do nothing; their token and row
+ * buffers may then be NULL. */
 
 /* Block tables and slot maps from request lengths.  Request b holds held[b] tokens and gets
  * fresh[b] new ones (either may be 0); with stride s (s tokens share a slot) it then has
@@ -377,7 +378,7 @@ typedef struct {
 size_t mtla_qpool_page_bytes(const mtla_qpool_config* cfg);
 
 /* Rows of r + d_R elements (the layout of mtla_cache_export; row_stride elements apart, a multiple
- * of 16 bytes, 16-byte aligned) into the pool rows index[0 .. n-1] (device), and back.  write skips
+ * of 16 bytes unless there is one row only, 16-byte aligned) into the pool rows index[0 .. n-1] (device), and back.  write skips
  * rows whose index is outside the pool (-1 in a slot map); apart from those no index may occur
  * twice, since the rows would be stored into each other.  read fills rows of such an index with
  * zeros; values are exact in both types. */

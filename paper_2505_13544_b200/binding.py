@@ -7,6 +7,7 @@ raises, and every non-zero status raises MTLAError.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import struct
 from dataclasses import dataclass
@@ -755,7 +756,17 @@ def _gpu_of(t: torch.Tensor, name: str) -> int:
 def _stream_on(dev: int, stream) -> int:
     """The given stream, or the current one of GPU `dev` (asked for without building a Stream
     object, which would cost as much as the rest of a small call's checks)."""
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise TypeError(f"stream: of GPU {stream.device_index}, the call's buffers are on GPU {dev}")
+    return stream.cuda_stream
+
+
+def _buffers_on(stream):
+    """Context for allocating a call's own buffers: memory that the given stream may use at once and,
+    once freed, only reuses behind the call (the allocator keeps its memory per stream)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 def _ptr(t: torch.Tensor, dtype, shape, dev: int, name: str) -> int:
@@ -796,7 +807,8 @@ def mtla_slot_map(held: torch.Tensor, fresh: torch.Tensor, free_pages: torch.Ten
     if out is None:
         if n_tokens is None:
             raise TypeError("n_tokens: needed when no buffers are given")
-        out = make_slot_map(batch, n_tokens, table.device)
+        with _buffers_on(stream):
+            out = make_slot_map(batch, n_tokens, table.device)
     n, n_free = out.seq.shape[0], free_pages.shape[0]
     if n_tokens is not None and n_tokens != n:
         raise TypeError("out: its token arrays differ from n_tokens")
@@ -827,7 +839,8 @@ def mtla_rope(cfg: mtla_rope_config, tensors, positions: torch.Tensor, *, first=
     count, n_tokens = len(tensors), positions.shape[0]
     firsts = first if isinstance(first, (list, tuple)) else [first] * count
     if out is None:
-        out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in tensors]
+        with _buffers_on(stream):
+            out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in tensors]
     if count < 1 or len(out) != count or len(firsts) != count:
         raise TypeError("tensors, out and first: expected one entry per tensor")
     dtype, dev = tensors[0].dtype, _gpu_of(positions, "positions")
@@ -895,7 +908,8 @@ def mtla_qpool_read(cfg: mtla_qpool_config, pages: torch.Tensor, index: torch.Te
     n, dev = index.shape[0], _gpu_of(pages, "pages")
     pp = _qpool_pages(cfg, pages, dev)
     if out is None:
-        out = torch.empty(n, cfg.latent_rank + cfg.rope_dim, dtype=dtype, device=pages.device)
+        with _buffers_on(stream):
+            out = torch.empty(n, cfg.latent_rank + cfg.rope_dim, dtype=dtype, device=pages.device)
     rp = _qpool_rows(cfg, out, dev, n, "out")
     _check(load_library().mtla_qpool_read(ctypes.byref(cfg), pp, _ptr(index, torch.int64, (n,), dev, "index"), n, rp,
                                           out.stride(0), _DTYPES[out.dtype], _stream_on(dev, stream)),
@@ -912,17 +926,20 @@ def mtla_qpool_attend(cfg: mtla_qpool_config, pages: torch.Tensor, table: torch.
                       lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
     """q [B][n_heads][r + d_R] over the first slots[b] slots of table row b; returns (out
     [B][n_heads][r], lse [B][n_heads] fp32).  workspace: uint8, see mtla_qpool_workspace_bytes; a
-    fresh one if None (a loop should keep one)."""
+    fresh one if None (a loop should keep one).  Results made on a given stream belong to that stream,
+    as with torch's own operations."""
     if q.dim() != 3 or table.dim() != 2 or q.dtype not in _DTYPES:
         raise TypeError("q: expected fp32 or bf16 [B][n_heads][r + d_R]; table: expected [B][width]")
     batch, width = table.shape
     heads, r, dev, dtype = cfg.n_heads, cfg.latent_rank, _gpu_of(pages, "pages"), q.dtype
-    if out is None:
-        out = torch.empty(batch, heads, r, dtype=dtype, device=q.device)
-    if lse is None:
-        lse = torch.empty(batch, heads, dtype=torch.float32, device=q.device)
-    if workspace is None:
-        workspace = torch.empty(mtla_qpool_workspace_bytes(cfg, batch), dtype=torch.uint8, device=q.device)
+    if out is None or lse is None or workspace is None:
+        with _buffers_on(stream):
+            if out is None:
+                out = torch.empty(batch, heads, r, dtype=dtype, device=q.device)
+            if lse is None:
+                lse = torch.empty(batch, heads, dtype=torch.float32, device=q.device)
+            if workspace is None:
+                workspace = torch.empty(mtla_qpool_workspace_bytes(cfg, batch), dtype=torch.uint8, device=q.device)
     ws_shape = workspace.shape
     _check(load_library().mtla_qpool_attend(
         ctypes.byref(cfg), _qpool_pages(cfg, pages, dev), _ptr(table, torch.int32, (batch, width), dev, "table"), width,

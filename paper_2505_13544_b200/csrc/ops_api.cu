@@ -85,10 +85,11 @@ qp::Format format_of(const mtla_qpool_config* c) { return qp::Format{c->latent_r
 
 int row_call(const mtla_qpool_config* cfg, const void* pages, const void* rows, int64_t row_stride, int32_t dtype,
              const int64_t* index, int32_t n, void* stream, bool write) {
-  if (!pages || !rows || !index || n < 0 || !good_dtype(dtype)) return MTLA_ERR_INVALID_ARG;
+  if (!pages || n < 0 || !good_dtype(dtype) || (n > 0 && (!rows || !index))) return MTLA_ERR_INVALID_ARG;
   if (!good_pool(cfg)) return MTLA_ERR_UNSUPPORTED_SHAPE;
   const int width = cfg->latent_rank + cfg->rope_dim, vec = dtype == MTLA_DTYPE_BF16 ? 8 : 4;
-  if (!aligned(pages, 16) || !aligned(rows, 16) || !aligned(index, 8) || row_stride < width || row_stride % vec)
+  if (!aligned(pages, 16) || !aligned(rows, 16) || !aligned(index, 8) ||
+      (n > 1 && (row_stride < width || row_stride % vec)))
     return MTLA_ERR_INVALID_ARG;
   if (n == 0) return MTLA_OK;
   OnDeviceOf dev(pages);
@@ -117,6 +118,8 @@ int row_call(const mtla_qpool_config* cfg, const void* pages, const void* rows, 
 constexpr int kAttnCtasPerSm = 2;
 constexpr int kPlanSms = 148;
 constexpr int kPlanCtas = kAttnCtasPerSm * kPlanSms;
+
+constexpr double kLog2e = 1.4426950408889634;
 
 struct AttnPlan { size_t o_part, ml_part, seq_parts, q_image, q_unit, error_word, total; };
 int padded_heads(int n) { return n <= 16 ? 16 : 32; }
@@ -244,7 +247,7 @@ int mtla_slot_map(const int32_t* held, const int32_t* fresh, int32_t B, int32_t 
 
 int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int32_t n_tensors, int32_t dtype,
               const int32_t* positions, int32_t n_tokens, int32_t inverse, void* stream) {
-  if (!cfg || !tensors || !positions || n_tensors < 1 || n_tokens < 0 || !good_dtype(dtype) ||
+  if (!cfg || !tensors || (n_tokens > 0 && !positions) || n_tensors < 1 || n_tokens < 0 || !good_dtype(dtype) ||
       !aligned(positions, 4))
     return MTLA_ERR_INVALID_ARG;
   if (n_tensors > rp::kMaxTensors) return MTLA_ERR_UNSUPPORTED_SHAPE;
@@ -283,7 +286,7 @@ int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int3
   bool use_vec = d % vec == 0 && (!half || (d / 2) % vec == 0);
   for (int n = 0; n < n_tensors; ++n) {
     const mtla_rope_tensor& t = tensors[n];
-    if (!t.x || !t.y || t.n_heads < 1 || t.width < 1 || t.first < 0 || !aligned(t.x, elem) || !aligned(t.y, elem))
+    if ((n_tokens > 0 && (!t.x || !t.y)) || t.n_heads < 1 || t.width < 1 || t.first < 0 || !aligned(t.x, elem) || !aligned(t.y, elem))
       return MTLA_ERR_INVALID_ARG;
     if (t.x_token_stride < 0 || t.x_head_stride < 0 || t.y_token_stride < 0 || t.y_head_stride < 0)
       return MTLA_ERR_INVALID_ARG;
@@ -295,7 +298,7 @@ int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int3
         (!one && t.n_heads > 1 && t.y_token_stride < t.y_head_stride * (t.n_heads - 1) + t.width &&
          t.y_head_stride < t.y_token_stride * ((long long)n_tokens - 1) + t.width))
       return MTLA_ERR_INVALID_ARG;
-    if (t.x == t.y && ((!one && t.x_token_stride != t.y_token_stride) ||
+    if (t.x && t.x == t.y && ((!one && t.x_token_stride != t.y_token_stride) ||
                        (t.n_heads > 1 && t.x_head_stride != t.y_head_stride)))
       return MTLA_ERR_INVALID_ARG;
     use_vec = use_vec && t.width % vec == 0 && t.first % vec == 0 && t.x_token_stride % vec == 0 &&
@@ -336,7 +339,7 @@ int mtla_rope(const mtla_rope_config* cfg, const mtla_rope_tensor* tensors, int3
   a.rows = rp::kThreads / a.lanes;
   // Tokens per CTA: four in flight for every thread, as long as every SM keeps several CTAs.
   int per = 1;
-  while (per < rp::kMaxTokens && per < 4 * a.rows && (n_tokens + 2 * per - 1) / (2 * per) >= 4 * dev.sm_count())
+  while (per < rp::kMaxTokens && per < 4 * a.rows && ((long long)n_tokens + 2 * per - 1) / (2 * per) >= 4 * dev.sm_count())
     per *= 2;
   a.tokens_per_cta = per;
   // With few tokens the rounds run as CTAs of their own instead of one after the other.
@@ -377,7 +380,7 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
                       const int32_t* slots, int32_t B, const void* q, int32_t dtype, float scale, void* out,
                       float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (!pages || !table || !slots || !q || !out || !workspace || B < 1 || table_width < 1 || !good_dtype(dtype) ||
-      !isfinite(scale))
+      !isfinite((float)((double)scale * kLog2e)))
     return MTLA_ERR_INVALID_ARG;
   if (!good_pool(cfg) || B > qp::kMaxBatch || (long long)B * table_width > 0x7fffffffll)
     return MTLA_ERR_UNSUPPORTED_SHAPE;
@@ -399,7 +402,7 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
   a.o_part = reinterpret_cast<float*>(ws + p.o_part);
   a.ml_part = reinterpret_cast<float*>(ws + p.ml_part);
   a.seq_parts = reinterpret_cast<int2*>(ws + p.seq_parts);
-  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.scale_log2 = (float)((double)scale * kLog2e);
   a.n_heads = cfg->n_heads;
   a.batch = B;
   a.width = table_width;

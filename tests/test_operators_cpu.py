@@ -191,3 +191,21 @@ def test_host_tensors_are_refused_by_the_binding():
         M.mtla_slot_map(torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32),
                         torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1, dtype=torch.int32), stride=1,
                         out=M.make_slot_map(1, 1, "cpu"))
+
+
+def test_calls_for_nothing_take_empty_buffers():
+    """An empty tensor's address is NULL."""
+    lib = M.load_library()
+    cfg, rope = pool_config(), M.make_rope_config(rope_dim=32)
+    for call in (lib.mtla_qpool_write, lambda c, p, r, s, d, i, n, st: lib.mtla_qpool_read(c, p, i, n, r, s, d, st)):
+        assert call(ctypes.byref(cfg), A, None, 288, 1, None, 0, None) == 0
+        assert call(ctypes.byref(cfg), None, None, 288, 1, None, 0, None) == -1
+    t = M.mtla_rope_tensor(None, None, 128, 64, 64, 64 * 7, 2, 64, 32)        # another order of the result
+    assert lib.mtla_rope(ctypes.byref(rope), ctypes.byref(t), 1, 1, None, 0, 0, None) == 0
+    assert lib.mtla_rope(ctypes.byref(rope), ctypes.byref(t), 1, 1, A, 1, 0, None) == -1
+
+
+def test_attend_refuses_a_scale_that_overflows_in_base_two():
+    cfg = pool_config()
+    need = M.mtla_qpool_workspace_bytes(cfg, 1)
+    assert M.load_library().mtla_qpool_attend(ctypes.byref(cfg), A, A, 1, A, 1, A, 1, 3e38, A, None, A, need, None) == -1

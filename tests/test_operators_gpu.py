@@ -340,6 +340,34 @@ def test_pool_read_into_strided_rows_leaves_the_rest():
     assert (wide[:, :8] == 9).all() and (wide[:, 104:] == 9).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_one_row_needs_no_row_stride(dtype):
+    cfg, pages = pool(64, 32, 2)
+    x = latent_rows(1, 64, 32, dtype, 6).cuda()
+    index = torch.tensor([77], device="cuda")
+    M.mtla_qpool_write(cfg, pages, x, index)
+    want, stored = M.mtla_qpool_read(cfg, pages, index, dtype=DT[dtype]), pages.clone()
+    for stride in (0, 1, 97):
+        one = x.as_strided((1, 96), (stride, 1))
+        pages.fill_(0xA5)
+        M.mtla_qpool_write(cfg, pages, one, index)
+        assert torch.equal(pages, stored)
+        out = torch.empty_like(want).as_strided((1, 96), (stride, 1))
+        M.mtla_qpool_read(cfg, pages, index, out=out)
+        assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(want))
+
+
+def test_calls_without_rows_or_tokens():
+    cfg, pages = pool(64, 32, 2)
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    before = pages.clone()
+    M.mtla_qpool_write(cfg, pages, torch.empty(0, 96, device="cuda"), none)
+    assert M.mtla_qpool_read(cfg, pages, none).shape == (0, 96) and torch.equal(pages, before)
+    x = torch.empty(0, 3, 48, device="cuda")
+    (y,) = M.mtla_rope(M.make_rope_config(rope_dim=16), [x], none.int())
+    assert y.shape == x.shape
+
+
 # ------------------------------------------------------------------------------ attention
 
 def attend_setup(lens, heads, r, dr, dtype, seed, junk=0xFF, size=1.0):
@@ -710,6 +738,27 @@ def test_two_streams_with_a_workspace_each():
     torch.cuda.synchronize()
     for o in outs:
         assert torch.equal(o, want)
+
+
+def test_buffers_of_a_call_come_from_its_stream(monkeypatch):
+    """Memory that a call allocates is the given stream's: freed at once (the workspace), it must not go to
+    work that another stream has queued."""
+    cfg, pages, table, slots, q, seqs = attend_setup([70, 3], 8, 64, 32, "bf16", 31)
+    qd, index = q.cuda(), torch.arange(4, device="cuda")
+    lens = torch.tensor([1, 2], dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    stream, made, empty = torch.cuda.Stream(), [], torch.empty
+    monkeypatch.setattr(M.torch, "empty", lambda *s, **kw: made.append(torch.cuda.current_stream()) or empty(*s, **kw))
+    M.mtla_qpool_attend(cfg, pages, table, slots, qd, scale=0.125, stream=stream)
+    assert len(made) == 3
+    M.mtla_qpool_read(cfg, pages, index, stream=stream)
+    M.mtla_rope(M.make_rope_config(rope_dim=16), [qd], lens, stream=stream)
+    M.mtla_slot_map(lens * 0, lens, lens, table.clone(), stride=1, n_tokens=3, stream=stream)
+    torch.cuda.synchronize()
+    assert len(made) == 12 and all(s == stream for s in made)
+    made.clear()
+    M.mtla_qpool_attend(cfg, pages, table, slots, qd, scale=0.125)
+    assert len(made) == 3 and all(s == torch.cuda.current_stream() for s in made)
 
 
 def test_page_numbers_past_32_bit_offsets():
