@@ -177,7 +177,7 @@ int launch_attend_tc(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t 
   int status = launch_dependent(qp::qpool_query_kernel<NHP>, dim3(NHP / (qp::kQueryThreads / 32), a.batch),
                                 qp::kQueryThreads, 0, st, a);
   if (status == MTLA_OK)
-    status = launch_dependent(qp::qpool_attend_tc_kernel<NHP, NB>, dim3(ctas), qp::tc::kThreads, l.total, st, a);
+    status = launch_dependent(qp::qpool_attend_tc_kernel<NHP, NB>, dim3(ctas), qp::tc::kThreads, l.total, st, a, l);
   return status == MTLA_OK ? launch_combine<bf16>(a, dev, st) : status;
 }
 template <int NHP>

@@ -56,7 +56,7 @@ namespace tc {
 
 constexpr int kTile = 128;                  // slots per tile: two pages
 constexpr int kThreads = 896;
-constexpr int kMaxStages = 4;
+constexpr int kMaxStages = 4;               // as many as value units' barriers
 constexpr int kMaxBatch = 1022;             // prefix sums kept in shared memory
 constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kScoreIssuer2 = 3;
 constexpr int kExpandWarp0 = 4, kExpandGroups = 4;
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kQueryThreads) qpool_query_kernel(AttnArgs a) 
 
 // NHP: heads padded to 16 or 32.  NB: ceil(r / 128).
 template <int NHP, int NB>
-__global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnArgs a, tc::Layout L) {
   using namespace tc;
   using namespace ptx;
   constexpr uint32_t IDESC_S = make_idesc_f16(128, NHP, 0, 0), IDESC_K = make_idesc_bf16(128, NHP, 0, 0);
@@ -196,7 +196,6 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   extern __shared__ uint8_t smem_raw[];
   const Format f = a.f;
   const int r = f.r, dr = f.dr;
-  const Layout L(f, NHP, a.batch);
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* sm = smem_raw + (base - raw);
   Misc* misc = reinterpret_cast<Misc*>(sm + L.off_misc);
@@ -205,30 +204,32 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // warp: uniform
   auto bar = [&](unsigned long long& p) { return smem_u32(&p); };
 
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < L.stages; ++i) {
+  // A thread per barrier of a kind: one thread for all of them would take 1000 cycles.
+  if (threadIdx.x < kInfo) {
+    const int i = threadIdx.x;
+    mbar_init(bar(misc->info_full[i]), 1);
+    if (i < 8) {
+      mbar_init(bar(misc->as_full[i]), 4);
+      mbar_init(bar(misc->as_empty[i]), 1);
+    }
+    if (i < 4) {
       mbar_init(bar(misc->raw_full[i]), 1);
       mbar_init(bar(misc->raw_empty[i]), 2 * NB * 4 + SI);       // a warp of each unit, the score issuers
       mbar_init(bar(misc->scale_full[i]), NB * 4);
+      mbar_init(bar(misc->av_full[i]), 4);
+      mbar_init(bar(misc->av_empty[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    if (i < 2) {
       mbar_init(bar(misc->s_full[i]), 1);
       mbar_init(bar(misc->s_empty[i]), kSoftmaxWarps);
       mbar_init(bar(misc->p_full[i]), kSoftmaxWarps);
       mbar_init(bar(misc->p_empty[i]), 1);
     }
-    for (int i = 0; i < 8; ++i) {
-      mbar_init(bar(misc->as_full[i]), 4);
-      mbar_init(bar(misc->as_empty[i]), 1);
+    if (i == 0) {
+      mbar_init(bar(misc->q_full), 1);
+      mbar_init(bar(misc->q_empty), SI);
+      misc->abort_word = 0;
     }
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(bar(misc->av_full[i]), 4);
-      mbar_init(bar(misc->av_empty[i]), 1);
-    }
-    for (int i = 0; i < kInfo; ++i) mbar_init(bar(misc->info_full[i]), 1);
-    mbar_init(bar(misc->q_full), 1);
-    mbar_init(bar(misc->q_empty), SI);
-    misc->abort_word = 0;
     mbar_fence_init();
   }
   if (warp == kProducerWarp) tmem_alloc(smem_u32(&misc->tmem_base), kTmemCols);
