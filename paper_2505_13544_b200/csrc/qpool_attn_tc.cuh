@@ -495,9 +495,11 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       if (kv >= 0) {
         const int c = kq * 4 + q, stv = st == 0 ? L.stages - 1 : st - 1, roundv = st == 0 ? round - 1 : round;
         // With four units a tile this group has itself expanded this very quarter for the scores: it
-          // has waited for the tile and written the scales.
+          // has waited for the tile, and that unit k - 2 has been used tells that its four warps have all
+        // written their scales of unit k - 4; behind the last tile only that unit's own barrier does.
           ok = (kv < AVB || wait(misc->av_empty[(kv - AVB) & 3], (kv - AVB) >> 2)) &&
-               (NB == kExpandGroups || (wait(misc->raw_full[stv], roundv) && wait(misc->scale_full[stv], roundv)));
+               (NB == kExpandGroups ? k < n_units || wait(misc->as_full[kv & 7], kv >> 3)
+                                    : wait(misc->raw_full[stv], roundv) && wait(misc->scale_full[stv], roundv));
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after_sync();
