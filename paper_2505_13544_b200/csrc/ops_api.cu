@@ -121,18 +121,15 @@ constexpr int kPlanCtas = kAttnCtasPerSm * kPlanSms;
 
 constexpr double kLog2e = 1.4426950408889634;
 
-struct AttnPlan { size_t o_part, ml_part, seq_parts, q_image, q_unit, error_word, total; };
-int padded_heads(int n) { return n <= 16 ? 16 : 32; }
+struct AttnPlan { size_t o_part, ml_part, seq_parts, error_words, total; };
 AttnPlan plan_attend(const mtla_qpool_config* c, int B) {
   AttnPlan p;
   const size_t parts = (size_t)B + kPlanCtas;
   p.o_part = 0;
   p.ml_part = align_up(parts * c->n_heads * c->latent_rank * 4, 256);
   p.seq_parts = p.ml_part + align_up(parts * c->n_heads * 8, 256);
-  p.q_image = p.seq_parts + align_up((size_t)B * 8, 256);
-  p.q_unit = p.q_image + align_up((size_t)B * padded_heads(c->n_heads) * 2 * (c->latent_rank + c->rope_dim), 256);
-  p.error_word = p.q_unit + align_up((size_t)B * 32 * 4, 256);
-  p.total = p.error_word + 256;
+  p.error_words = p.seq_parts + align_up((size_t)B * 8, 256);
+  p.total = p.error_words + align_up(kPlanSms * 4, 256);
   return p;
 }
 
@@ -157,7 +154,7 @@ template <typename T, int MH>
 int launch_attend(qp::AttnArgs a, const OnDeviceOf& dev, cudaStream_t st) {
   using L = qp::AttnLayout<MH, sizeof(T) == 2 ? 1 : 2>;
   if (!raise_smem<qp::qpool_attend_kernel<T, MH>>(dev.device())) return MTLA_ERR_CUDA;
-  a.error_word = nullptr;                    // this kernel has no wait that could run out
+  a.n_error_words = 0;                       // this kernel has no wait that could run out
   const int smem = L::bytes(a.f, a.batch);
   const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
   const int per_sm = smem <= 112 * 1024 ? kAttnCtasPerSm : 1;
@@ -168,16 +165,15 @@ int launch_attend(qp::AttnArgs a, const OnDeviceOf& dev, cudaStream_t st) {
 }
 
 template <int NHP, int NB>
-int launch_attend_tc(const qp::AttnArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
+int launch_attend_tc(qp::AttnArgs a, const OnDeviceOf& dev, cudaStream_t st) {
   if (!raise_smem<qp::qpool_attend_tc_kernel<NHP, NB>>(dev.device())) return MTLA_ERR_CUDA;
   const qp::tc::Layout l(a.f, NHP, a.batch);
   const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
   const long long most = (long long)a.batch * ceil_div(a.width, 2);
   const int ctas = (int)(most < sms ? most : sms);
-  int status = launch_dependent(qp::qpool_query_kernel<NHP>, dim3(NHP / (qp::kQueryThreads / 32), a.batch),
-                                qp::kQueryThreads, 0, st, a);
-  if (status == MTLA_OK)
-    status = launch_dependent(qp::qpool_attend_tc_kernel<NHP, NB>, dim3(ctas), qp::tc::kThreads, l.total, st, a, l);
+  a.n_error_words = ctas;
+  const int status =
+      launch_dependent(qp::qpool_attend_tc_kernel<NHP, NB>, dim3(ctas), qp::tc::kThreads, l.total, st, a, l);
   return status == MTLA_OK ? launch_combine<bf16>(a, dev, st) : status;
 }
 template <int NHP>
@@ -409,9 +405,7 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
   a.n_pages = cfg->n_pages;
   a.f = format_of(cfg);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  a.q_image = reinterpret_cast<uint8_t*>(ws + p.q_image);
-  a.q_unit = reinterpret_cast<float*>(ws + p.q_unit);
-  a.error_word = reinterpret_cast<int*>(ws + p.error_word);
+  a.error_words = reinterpret_cast<int*>(ws + p.error_words);
   const bool wide = cfg->n_heads > 16;
   // The tensor-core kernel, except where its longer set-up shows: at most a page per SM of up to 256
   // latents (8 heads, r 64, one slot tile: 9.0 us against 7.2; 64 sequences of two pages, r 256: 13.9

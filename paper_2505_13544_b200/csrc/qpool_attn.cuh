@@ -48,11 +48,9 @@ struct AttnArgs {
   float* o_part;             // [batch + ctas][n_heads][r]
   float* ml_part;            // [batch + ctas][n_heads][2]: reference (log2 units) of the sums, denominator
   int2* seq_parts;           // [batch] first part, number of parts (0: finished by one CTA)
-  uint8_t* q_image;          // tensor-core kernel: [batch] queries as its shared memory holds them
-  float* q_unit;             // tensor-core kernel: [batch][32] scale of a head's scores
-  int* error_word;           // tensor-core kernel: a bounded wait gave up
+  int* error_words;          // tensor-core kernel: [n_error_words] a CTA's bounded wait gave up
   float scale_log2;          // scale * log2(e)
-  int n_heads, batch, width, n_pages;
+  int n_heads, batch, width, n_pages, n_error_words;
   Format f;
 };
 
@@ -576,9 +574,8 @@ __global__ void __launch_bounds__(kCombineThreads) qpool_combine_kernel(AttnArgs
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = a.f.r, heads = a.n_heads;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const int* error = a.error_word;
   // A bounded wait gave up: no result that looks like one.
-  const bool failed = error != nullptr && *error != 0;
+  const bool failed = __syncthreads_or(tid < a.n_error_words && a.error_words[tid] != 0);
   // Sequences with few parts (or none, or no result) from the front of the list, the others from its
   // end, both in order: every CTA has the same list.
   int n_few = 0, n_many = 0;

@@ -32,9 +32,6 @@
 // A head count of 16 or 32 is the matrix instructions' N, so heads are not padded further.  The RoPE
 // keys go from the pool to the score product as they are (bf16, shared memory, hardware swizzle).
 //
-// Queries arrive as an image of the B operand that qpool_query_kernel has written (half precision
-// scaled by a power of two per head, swizzled), so that a segment's query is one bulk copy.
-//
 // Roles (28 warps): warps 0 and 3 issue the score products, warp 1 the value products, warp 2 is the
 // producer; warps 4-19 expand, in four groups that take turns (see there); warps 20-27 are softmax
 // and epilogue.  The hot loops are short on purpose: with several kinds of code on every scheduler,
@@ -61,6 +58,9 @@ constexpr int kMaxBatch = 1022;             // prefix sums kept in shared memory
 constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kScoreIssuer2 = 3;
 constexpr int kExpandWarp0 = 4, kExpandGroups = 4;
 constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
+// Queries and scales of segments: the expanding warps are at most two segments ahead of the softmax
+// (its tile has to leave the accumulator that the second next one takes), so four keep them apart.
+constexpr int kQRing = 4;
 constexpr int kInfo = 16;                   // ring of tile descriptions, deeper than any role's lag
 // TMEM columns: two score buffers, up to four output blocks of NHP columns, two operand
 // buffers of 64 columns for the scores and what is left, three (32 heads) or four, for the values.
@@ -77,7 +77,7 @@ constexpr int kSmemMax = 227 * 1024 - 1024;
 
 struct TileInfo {
   int b;
-  int flags;                 // 1: first tile of a segment, 2: last
+  int flags;                 // 1: first tile of a segment, 2: last; the segment's number times 4
   int rows0, rows1;          // slots of the tile's two pages
 };
 
@@ -88,7 +88,8 @@ struct Misc {
   // unit that had the buffer before, and who reads it waits for it; both see every phase of the
   // barriers they wait for.
   unsigned long long as_full[8], as_empty[8], av_full[4], av_empty[4];
-  unsigned long long s_full[2], s_empty[2], p_full[2], p_empty[2], q_full, q_empty;
+  unsigned long long s_full[2], s_empty[2], p_full[2], p_empty[2];
+  unsigned long long q_full[kQRing], q_empty[kQRing];        // segment s: those of s mod 4
   unsigned long long info_full[kInfo];
   uint32_t tmem_base;
   int abort_word;
@@ -97,10 +98,12 @@ struct Misc {
   float m_used[32];          // reference maximum (log2 units), minus infinity before the first score
   alignas(16) float neg_ref[32];   // shift - reference: what a score is offset by
   alignas(16) float unit[32];      // scale of the head's scores
+  float next_unit[kQRing][32];     // the same, as the queries' writers leave it
   float fac[32];
   float red[8][16];
 };
-static_assert(sizeof(Misc) <= 2048, "misc region too small");
+constexpr int kMiscBytes = 2560;
+static_assert(sizeof(Misc) <= kMiscBytes, "misc region too small");
 
 struct Layout {
   int codes, scales, keys;                  // offsets in a stage
@@ -114,7 +117,7 @@ struct Layout {
     q_bytes = nhp * 2 * (f.r + f.dr);
     const int q_room = (q_bytes + 1023) / 1024 * 1024, p_room = 2 * kTile * nhp * 2;
     const int scale_room = f.scale_row() * kTile * 2;
-    const int fixed = q_room + p_room + 2048 + (2 * batch + 1) * 4 + 1024;   // 1024: alignment of the base
+    const int fixed = q_room + p_room + kMiscBytes + (2 * batch + 1) * 4 + 1024;   // 1024: alignment of the base
     // At least three (r 512, 32 heads, d_R 64: exactly), which the expansion's waits rely on; with one
     // unit a tile (r <= 128) always four, as many as a tile's value operands may lag.
     stages = (kSmemMax - fixed) / (stage + scale_room);
@@ -123,7 +126,7 @@ struct Layout {
     off_p = off_q + q_room;
     off_st = off_p + p_room;
     off_misc = off_st + stages * scale_room;
-    off_prefix = off_misc + 2048;
+    off_prefix = off_misc + kMiscBytes;
     off_slots = off_prefix + (batch + 1) * 4;
     total = off_slots + batch * 4 + 1024;
   }
@@ -131,56 +134,79 @@ struct Layout {
 
 }  // namespace tc
 
-// Queries -> the image of the score product's B operand: per sequence r / 64 panels [NHP][64] half
-// precision with the 128-byte swizzle and one panel [NHP][d_R] bf16 (128- or 64-byte swizzle), a head's
-// row scaled by the power of two that brings its largest element into [2^14, 2^15); heads that do not
-// exist are zero.  A warp per head.
-constexpr int kQueryThreads = 256;
-template <int NHP>
-__global__ void __launch_bounds__(kQueryThreads) qpool_query_kernel(AttnArgs a) {
-  const int b = blockIdx.y, lane = threadIdx.x & 31, h = blockIdx.x * (kQueryThreads / 32) + (threadIdx.x >> 5);
-  const int r = a.f.r, dr = a.f.dr, n8 = (r + dr) / 8;
-  ptx::grid_launch_dependents();
-  ptx::grid_dependency_wait();
-  if (b == 0 && blockIdx.x == 0 && threadIdx.x == 0) *a.error_word = 0;
-  const bf16* q = static_cast<const bf16*>(a.q) + ((long long)b * a.n_heads + h) * (r + dr);
-  float v[3][8];                                  // up to 72 runs of eight over 32 lanes
-  uint32_t top = 0;
+// Queries of a segment -> the score product's B operand, by the QW warps that expand the units of its
+// first tile (two of the three with three), each some heads: r / 64 panels [NHP][64] half precision with
+// the 128-byte swizzle and one panel [NHP][d_R] bf16 (128- or 64-byte swizzle).  A head's row is scaled
+// by the power of two that brings its largest element into [2^14, 2^15); heads that do not exist are
+// zero.  As a kernel of its own in front, with the image loaded from memory, this took 1 to 2.5 us more of
+// a small batch's 15 to 19.  Not inlined: the loop that calls it once a segment is short of registers.
+template <int NHP, int QW, int QB, int QV>
+__device__ __noinline__ bool put_queries(const bf16* q, uint8_t* image, tc::Misc* misc, float scale_log2, int n_heads,
+                                         Format f, int seg, int first_head) {
+  using namespace tc;
+  const int r = f.r, dr = f.dr, lane = threadIdx.x & 31;
+  const int n8 = (r + dr) / 8;
+#pragma unroll 1
+  for (int h0 = first_head; h0 < NHP; h0 += QB * QW) {
+    uint4 w[QB][QV];
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int c = lane + 32 * i;
+    for (int j = 0; j < QB; ++j) {
+      const int h = h0 + j * QW;
+      const bf16* src = q + (long long)h * (r + dr);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-    if (c < n8 && h < a.n_heads) load_vec(q + 8 * c, v[i]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
-  }
-  top = __reduce_max_sync(0xffffffffu, top);
-  const bool fine = top > 0 && top < 0x7f800000u;
-  const int e = fine ? 14 - ilogbf(__uint_as_float(top)) : 0;
-  if (lane == 0) a.q_unit[b * 32 + h] = ldexpf(a.scale_log2, -e);
-  uint8_t* img = a.q_image + (long long)b * NHP * 2 * (r + dr);
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int c = lane + 32 * i;
-    if (c >= n8) break;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = ldexpf(v[i][j], e);
-    if (8 * c < r) {
-      uint32_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const __half2 x = __floats2half2_rn(v[i][2 * j], v[i][2 * j + 1]);
-        w[j] = *reinterpret_cast<const uint32_t*>(&x);
+      for (int i = 0; i < QV; ++i) {
+        const int c = lane + 32 * i;
+        w[j][i] = make_uint4(0u, 0u, 0u, 0u);
+        if (c < n8 && h < n_heads) w[j][i] = *reinterpret_cast<const uint4*>(src + 8 * c);
       }
-      *reinterpret_cast<uint4*>(img + (c >> 3) * NHP * 128 + h * 128 + ((c ^ h) & 7) * 16) =
-          make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-      const int k = c - r / 8;
-      uint8_t* p = img + NHP * 2 * r + h * 2 * dr + (k ^ a.f.key_swizzle(h)) * 16;
-      store_vec(reinterpret_cast<bf16*>(p), v[i]);
+    }
+    // The score products of the segment before are done.
+    const bool there = seg == 0 || ptx::mbar_wait_compact(ptx::smem_u32(&misc->q_empty[(seg - 1) % kQRing]),
+                                                          (seg - 1) / kQRing & 1);
+    if (!__all_sync(0xffffffffu, there)) return false;
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+      const int h = h0 + j * QW;                    // NHP is a multiple of QB * QW
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const uint32_t x[4] = {w[j][i].x, w[j][i].y, w[j][i].z, w[j][i].w};
+#pragma unroll
+        for (int m = 0; m < 4; ++m) top = max(top, max(x[m] & 0x7fff0000u, (x[m] << 16) & 0x7fff0000u));
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+      // Exponents -113 .. 140 (a row of subnormal numbers only reaches less); none for zeros and specials.
+      const bool fine = top > 0 && top < 0x7f800000u;
+      const int e = fine ? 141 - max((int)(top >> 23), 1) : 0, e1 = e / 2, e2 = e - e1;
+      const float f1 = __uint_as_float((127 + e1) << 23), f2 = __uint_as_float((127 + e2) << 23);
+      if (lane == 0)
+        misc->next_unit[seg % kQRing][h] =
+            scale_log2 * __uint_as_float((127 - e1) << 23) * __uint_as_float((127 - e2) << 23);
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const int c = lane + 32 * i;
+        if (c >= n8) break;
+        const uint32_t x[4] = {w[j][i].x, w[j][i].y, w[j][i].z, w[j][i].w};
+        const bool latent = 8 * c < r;
+        uint32_t y[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const float lo = __uint_as_float(x[m] << 16) * f1 * f2;
+          const float hi = __uint_as_float(x[m] & 0xffff0000u) * f1 * f2;
+          const __half2 l2 = __floats2half2_rn(lo, hi);
+          const __nv_bfloat162 k2 = __floats2bfloat162_rn(lo, hi);
+          y[m] = latent ? *reinterpret_cast<const uint32_t*>(&l2) : *reinterpret_cast<const uint32_t*>(&k2);
+        }
+        const int at = latent ? (c >> 3) * NHP * 128 + h * 128 + ((c ^ h) & 7) * 16
+                              : NHP * 2 * r + h * 2 * dr + ((c - r / 8) ^ f.key_swizzle(h)) * 16;
+        *reinterpret_cast<uint4*>(image + at) = make_uint4(y[0], y[1], y[2], y[3]);
+      }
     }
   }
+  ptx::fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&misc->q_full[seg % kQRing]));
+  return true;
 }
 
 // NHP: heads padded to 16 or 32.  NB: ceil(r / 128).
@@ -192,6 +218,9 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   constexpr uint32_t IDESC_V = make_idesc_f16(128, NHP, 0, 1);
   constexpr uint32_t P_BYTES = kTile * NHP * 2, P_SBO = kTile * 16;   // bytes between groups of 8 heads
   constexpr int SI = NB == 3 ? 1 : 2;           // score issuers (see there)
+  constexpr int QW = NB == 4 ? 16 : NB == 1 ? 4 : 8;                  // warps that write a segment's queries
+  constexpr int QB = NHP / QW < 2 ? 1 : NB == 1 ? 4 : 2;              // their heads loaded together
+  constexpr int QV = (NB * 16 + 8 + 31) / 32;   // runs of eight elements of a lane
   constexpr int AVB = av_buffers(NHP), COL_AS = col_as(NHP), COL_AV = col_av(NHP);
   extern __shared__ uint8_t smem_raw[];
   const Format f = a.f;
@@ -218,6 +247,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       mbar_init(bar(misc->scale_full[i]), NB * 4);
       mbar_init(bar(misc->av_full[i]), 4);
       mbar_init(bar(misc->av_empty[i]), 1);
+      mbar_init(bar(misc->q_full[i]), QW);
+      mbar_init(bar(misc->q_empty[i]), SI);
     }
     if (i < 2) {
       mbar_init(bar(misc->s_full[i]), 1);
@@ -225,11 +256,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       mbar_init(bar(misc->p_full[i]), kSoftmaxWarps);
       mbar_init(bar(misc->p_empty[i]), 1);
     }
-    if (i == 0) {
-      mbar_init(bar(misc->q_full), 1);
-      mbar_init(bar(misc->q_empty), SI);
-      misc->abort_word = 0;
-    }
+    if (i == 0) misc->abort_word = 0;
     mbar_fence_init();
   }
   if (warp == kProducerWarp) tmem_alloc(smem_u32(&misc->tmem_base), kTmemCols);
@@ -259,17 +286,14 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   // takes some 300 cycles, so the issuing warps ask for what comes next before they issue what is there.
   auto ask = [&](unsigned long long& b, int phase) { return mbar_test(bar(b), phase & 1); };
   bool ok = true;                // false once a wait of this thread has given up
-  if (threadIdx.x == 0 && misc->tmem_base != 0) {
-    misc->abort_word = 1;
-    atomicCAS(a.error_word, 0, 100);
-  }
+  if (threadIdx.x == 0 && misc->tmem_base != 0) misc->abort_word = 1;
 
   if (n_tiles == 0) {
     // nothing to do; the CTA falls through to the common end
   } else if (warp < kExpandWarp0) {
     if (warp == kProducerWarp && lane == 0) {
       // ---------------------------------------------------------------- producer
-      int b = find_seq(prefix, a.batch, g0), seg = 0, st = 0, round = 0;
+      int b = find_seq(prefix, a.batch, g0), seg = -1, st = 0, round = 0;
       for (int n = 0; n < n_tiles; ++n) {
         const int g = g0 + n;
         while (prefix[b + 1] <= g) ++b;
@@ -286,7 +310,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         if (!ok) break;
         TileInfo& info = misc->info[n % kInfo];
         info.b = b;
-        info.flags = (first ? 1 : 0) | (last ? 2 : 0);
+        seg += first;
+        info.flags = (first ? 1 : 0) | (last ? 2 : 0) | seg << 2;
         info.rows0 = rows[0];
         info.rows1 = rows[1];
         mbar_arrive(bar(misc->info_full[n % kInfo]));
@@ -305,14 +330,6 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           bulk_load(dst + L.codes + i * kPageRows * f.code_row(), src, rows[i] * f.code_row(), full);
           bulk_load(dst + L.keys + i * kPageRows * f.key_row(), src + f.off_keys(), rows[i] * f.key_row(), full);
         }
-        if (first) {
-          // The segment's queries, once the score products of the segment before are done.
-          ok = wait(misc->q_empty, seg + 1);
-          if (!ok) break;
-          mbar_arrive_expect_tx(bar(misc->q_full), L.q_bytes);
-          bulk_load(q_u32, a.q_image + (long long)b * L.q_bytes, L.q_bytes, bar(misc->q_full));
-          ++seg;
-        }
         if (++st == L.stages) { st = 0; ++round; }
       }
     } else if (warp == kScoreIssuer || (SI == 2 && warp == kScoreIssuer2)) {
@@ -327,15 +344,14 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       const uint32_t key_sbo = 8 * f.key_row();
       const uint64_t q_desc = make_smem_desc(q_u32, 16, 1024, kSwizzle128B);
       const uint64_t qk_desc = make_smem_desc(q_u32 + NHP * 2 * r, 16, key_sbo, mode);
-      int seg = 0, st = 0, round = 0;
+      int st = 0, round = 0;
       for (int n = 0; n < n_tiles && ok; ++n) {
         ok = wait_warp(misc->raw_full[st], round);
         if (!ok) break;
-        const int flags = misc->info[n % kInfo].flags;
+        const int flags = misc->info[n % kInfo].flags, seg = flags >> 2;
         if (flags & 1) {
-          ok = wait_warp(misc->q_full, seg);
+          ok = wait_warp(misc->q_full[seg % kQRing], seg / kQRing);
           if (!ok) break;
-          ++seg;
         }
         if (SI == 1 || (n & 1) == mine) {
           ok = wait_warp(misc->s_empty[n & 1], (n >> 1) + 1);
@@ -376,11 +392,11 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           if (elect_one()) {
             mma_commit(bar(misc->s_full[n & 1]));
             mma_commit(bar(misc->raw_empty[st]));
-            if (flags & 2) mma_commit(bar(misc->q_empty));
+            if (flags & 2) mma_commit(bar(misc->q_empty[seg % kQRing]));
           }
         } else if (elect_one()) {
           mbar_arrive(bar(misc->raw_empty[st]));
-          if (flags & 2) mma_commit(bar(misc->q_empty));
+          if (flags & 2) mma_commit(bar(misc->q_empty[seg % kQRing]));
         }
         __syncwarp();
         if (++st == L.stages) { st = 0; ++round; }
@@ -428,6 +444,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16);
     const uint32_t twist = (uint32_t)(lane & cmask) * 16;       // rows lane, lane + 32, ... twist alike
     const int n_units = n_tiles * NB;
+    // The segment that tile n is in, its sequence, and the tile at which the next one begins.
+    int seg = -1, b = find_seq(prefix, a.batch, g0), next_start = 0;
     // Tile n, quarter kq of unit k, the stage of tile n and how often the ring has come round; the
     // value unit is the same quarter of tile n - 1.
     int n = 0, kq = grp, st = 0, round = 0;
@@ -440,6 +458,21 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
 #pragma unroll 1
     for (int k = grp; k < n_units + NB; k += kExpandGroups) {
       if (k < n_units) {
+        if (__builtin_expect(n >= next_start, 0)) {
+          int start;
+          do {
+            start = next_start;
+            while (prefix[b + 1] <= g0 + start) ++b;
+            next_start = prefix[b + 1] - g0;
+            ++seg;
+          } while (n >= next_start);
+          if (n == start && kq < QW / 4) {
+            const int h0 = kq * 4 + q;
+            ok = put_queries<NHP, QW, QB, QV>(static_cast<const bf16*>(a.q) + (long long)b * a.n_heads * (r + dr),
+                                              sm + L.off_q, misc, a.scale_log2, a.n_heads, f, seg, h0);
+            if (!ok) break;
+          }
+        }
         // The buffer first: that unit k - 2 has been used also tells that the stage's phase is the one
         // before this tile's or later, which its parity alone would not.
         ok = (k < 2 || wait(misc->as_empty[(k - 2) & 7], (k - 2) >> 3)) && wait(misc->raw_full[st], round);
@@ -596,9 +629,11 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       const int rows = slot < 64 ? misc->info[n % kInfo].rows0 : misc->info[n % kInfo].rows1;
       if (flags & 1) {
         if (sidx < 32) {
+          const int seg = flags >> 2;
+          if (ok) ok = wait(misc->q_full[seg % kQRing], seg / kQRing);       // long since; for the scales
           misc->m_used[sidx] = -INFINITY;
           misc->neg_ref[sidx] = kUnset;
-          misc->unit[sidx] = sidx < NHP ? a.q_unit[misc->info[n % kInfo].b * 32 + sidx] : 0.f;
+          misc->unit[sidx] = sidx < NHP ? misc->next_unit[seg % kQRing][sidx] : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < NHH; ++i) l_acc[i] = 0.f;
@@ -762,11 +797,9 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
     }
   }
 
-  if (!ok) {
-    misc->abort_word = 1;
-    atomicCAS(a.error_word, 0, 1 + warp);
-  }
+  if (!ok) misc->abort_word = 1;
   __syncthreads();
+  if (threadIdx.x == 0) a.error_words[blockIdx.x] = misc->abort_word;
   if (misc->abort_word) {
     // Give copies that may still be in flight time to land before the CTA's memory is reused.
     const uint64_t t0 = global_timer_ns();
