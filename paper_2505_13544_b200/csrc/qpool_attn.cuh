@@ -10,7 +10,7 @@
 // The kernel of this file serves fp32 queries and the smallest batches (the other one is in
 // qpool_attn_tc.cuh; its rule is beside the launch).  Its
 // warps expand, multiply and reduce by turns, so it is bound by instruction issue: 1220 us at
-// 128 x 16384 slots, 32 heads, r 512, bf16, where the other takes 270.
+// 128 x 16384 slots, 32 heads, r 512, bf16, where the other takes 263.
 //
 // It runs on the warp-level matrix instructions (m16n8k16), with the codes
 // expanded from shared memory into registers in both fragment layouts:

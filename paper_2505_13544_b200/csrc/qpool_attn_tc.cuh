@@ -17,7 +17,7 @@
 // Shared memory then carries only the raw pages (three tiles of 128 slots deep), the queries and the
 // probabilities.
 //
-// Measured at 128 sequences of 16384 slots, 32 heads, r 512, d_R 64: 270 us, 3.1 TB/s of pool, 48 % of
+// Measured at 128 sequences of 16384 slots, 32 heads, r 512, d_R 64: 263 us, 3.2 TB/s of pool, 49 % of
 // the measured copy bandwidth; the bytes alone would take 130 us.  Per tile of 128 slots that is about
 // 4500 cycles.  The expansion's conversions and scalings, which share a rate of 1.25 pairs of latents
 // per cycle and SM (measured), need 2300 of them, the matrix instructions 1100, the bytes 2100.  What
@@ -25,7 +25,7 @@
 // through an mbarrier to the issuing warp, through the matrix unit and back in some 2200 cycles, since
 // with the memory instruction queues full of operand stores a wait takes 300 even for what is there.
 // Tensor memory has room for two units of the scores and three of the values beside the two
-// accumulators (three and two: 281 us).  At 32 sequences, 91 us with one score issuer, leaving out the
+// accumulators (three and two: 281 us beside 270).  At 32 sequences, 91 us with one score issuer, leaving out the
 // softmax gave 90 us, the matrix instructions 78, the operand stores 73, loads, arithmetic and
 // stores together 76, all of it 52.
 //
@@ -33,7 +33,7 @@
 // keys go from the pool to the score product as they are (bf16, shared memory, hardware swizzle).
 //
 // Roles (28 warps): warps 0 and 3 issue the score products, warp 1 the value products, warp 2 is the
-// producer; warps 4-19 expand, in four groups that take turns (see there); warps 20-27 are softmax
+// producer; warps 4-19 expand, in four groups that take turns (see there), and write the queries; warps 20-27 are softmax
 // and epilogue.  The hot loops are short on purpose: with several kinds of code on every scheduler,
 // fetching unrolled instructions was the longest stall (107 KB of them: 517 us at 128 x 16384
 // slots, 61 KB: 362 us), then the issuing threads' scalar descriptors (a uniform warp: 331), the sharing

@@ -504,6 +504,15 @@ def test_attend_many_tiles_and_segments_per_cta(r, dr, heads):
         assert (np.abs(got_lse[b] - want_lse) <= tol_lse + 2.0 ** -23 * np.abs(want_lse)).all(), b
 
 
+@pytest.mark.parametrize("heads", [16, 31, 32])
+@pytest.mark.parametrize("r", [448, 512])
+@pytest.mark.parametrize("lens", [[300] * 5, [128, 127, 1, 0, 256, 129] * 4])
+def test_attend_shares_of_a_tile_on_fresh_data(lens, r, heads):
+    """The first call on new pages: what a share's only tile needs comes late and unevenly."""
+    for seed in range(3):
+        check_attend(*attend_setup(lens, heads, r, 64, "bf16", 50 + seed), 0.125, "bf16", lens)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("scale,size", [(0.0, 1.0), (-0.3, 1.0), (4.0, 1.0), (0.125, 1e-4), (0.125, 300.0), (1e-9, 1e4)])
 def test_attend_scales(dtype, scale, size):
