@@ -33,8 +33,8 @@
 // keys go from the pool to the score product as they are (bf16, shared memory, hardware swizzle).
 //
 // Roles (28 warps): warps 0 and 3 issue the score products, warp 1 the value products, warp 2 is the
-// producer; warps 4-19 expand, in four groups that take turns (see there), and write the queries; warps 20-27 are softmax
-// and epilogue.  The hot loops are short on purpose: with several kinds of code on every scheduler,
+// producer; warps 4-19 expand, in four groups that take turns (see there), and write the queries;
+// warps 20-27 are softmax and epilogue.  The hot loops are short on purpose: with several kinds of code on every scheduler,
 // fetching unrolled instructions was the longest stall (107 KB of them: 517 us at 128 x 16384
 // slots, 61 KB: 362 us), then the issuing threads' scalar descriptors (a uniform warp: 331), the sharing
 // out of the expansion (282) and a single score issuer (270 with two; a second value issuer adds nothing).
