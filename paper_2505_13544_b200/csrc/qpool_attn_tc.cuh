@@ -41,6 +41,12 @@
 // The online softmax raises a head's reference only when a tile exceeds it by 2^8.  Probabilities
 // are kept times 2^7: with the 2^8 they stay inside half precision.
 //
+// The matrix unit cuts its running sums off instead of rounding them: every 16 slots the output loses part
+// of its last place, always towards zero (a segment of 2^18 slots came out 1.6e-3 too small, one of
+// 2^20 slots 6.6e-3, more than the rounding of the bf16 result).  So after kFoldTiles tiles the softmax warps
+// take the sums out of tensor memory and add them up, rounded, in the segment's place among the partials,
+// and 6e-5 is missing at any length (2^14 and 2^20 slots alike).
+//
 // Every wait is bounded; after a time-out the roles unwind, each when its own next wait runs out, and
 // qpool_combine_kernel answers with NaN.
 #pragma once
@@ -72,12 +78,16 @@ __host__ __device__ constexpr int av_buffers(int nhp) { return nhp == 32 ? 3 : 4
 static_assert(col_av(32) + 64 * av_buffers(32) <= kTmemCols && col_av(16) + 64 * av_buffers(16) <= kTmemCols,
               "tensor memory budget");
 constexpr float kShift = 7.f, kRescale = 8.f;
+constexpr int kFoldTiles = 128;             // tiles whose products are summed in tensor memory
 constexpr float kUnset = 3e38f;             // in the place of -reference: any score then exceeds it
 constexpr int kSmemMax = 227 * 1024 - 1024;
 
+// First and last tile of a segment; the sums of the tiles before it are set down first; sums have been set
+// down before this tile, or with it.
+constexpr int kFirst = 1, kLast = 2, kFold = 4, kFolded = 8, kFoldedNow = 16, kSegShift = 5;
 struct TileInfo {
   int b;
-  int flags;                 // 1: first tile of a segment, 2: last; the segment's number times 4
+  int flags;                 // the above; the segment's number times 32
   int rows0, rows1;          // slots of the tile's two pages
 };
 
@@ -101,8 +111,9 @@ struct Misc {
   float next_unit[kQRing][32];     // the same, as the queries' writers leave it
   float fac[32];
   float red[8][16];
+  float m_fold[32];          // reference of the sums that have been set down
 };
-constexpr int kMiscBytes = 2560;
+constexpr int kMiscBytes = 2688;
 static_assert(sizeof(Misc) <= kMiscBytes, "misc region too small");
 
 struct Layout {
@@ -209,6 +220,33 @@ __device__ __noinline__ bool put_queries(const bf16* q, uint8_t* image, tc::Misc
   return true;
 }
 
+// A softmax thread's output sums (of latent `lat` of every block, heads ho ..) out of tensor memory, added to
+// what the segment has set down in `part` (not yet anything without `add`), which is brought to the present
+// references by fac; into `part` again, or at the segment's end, divided, into `out`.  A whole-warp call.
+// Rarely reached, yet inlined: a call made the loop around it spill (128 sequences of r 384, 32 heads: 254 us,
+// so 251; with no folding at all 249).
+template <int NHP, int NB>
+__device__ __forceinline__ void fold_output(float* part, bf16* out, const tc::Misc* misc, uint32_t taddr, int ho, int n_heads,
+                                         int r, int lat, bool add) {
+  constexpr int NHH = NHP / 2;
+#pragma unroll 1
+  for (int mb = 0; mb < NB; ++mb) {
+    uint32_t ov[16];
+    if (NHH == 16) ptx::tmem_ld_x16(taddr + mb * NHP, ov); else ptx::tmem_ld_x8(taddr + mb * NHP, ov);
+    ptx::tmem_wait_ld();
+    if (mb * 128 + lat >= r) continue;
+#pragma unroll
+    for (int i = 0; i < NHH; ++i) {
+      if (ho + i >= n_heads) break;
+      const long long e = (long long)(ho + i) * r + mb * 128 + lat;
+      float v = __uint_as_float(ov[i]);
+      if (add) v = fmaf(part[e], misc->fac[ho + i], v);
+      if (out) out[e] = __float2bfloat16_rn(v * misc->unit[ho + i]);
+      else part[e] = v;
+    }
+  }
+}
+
 // NHP: heads padded to 16 or 32.  NB: ceil(r / 128).
 template <int NHP, int NB>
 __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnArgs a, tc::Layout L) {
@@ -293,7 +331,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   } else if (warp < kExpandWarp0) {
     if (warp == kProducerWarp && lane == 0) {
       // ---------------------------------------------------------------- producer
-      int b = find_seq(prefix, a.batch, g0), seg = -1, st = 0, round = 0;
+      int b = find_seq(prefix, a.batch, g0), seg = -1, st = 0, round = 0, begun = 0;
       for (int n = 0; n < n_tiles; ++n) {
         const int g = g0 + n;
         while (prefix[b + 1] <= g) ++b;
@@ -311,7 +349,10 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         TileInfo& info = misc->info[n % kInfo];
         info.b = b;
         seg += first;
-        info.flags = (first ? 1 : 0) | (last ? 2 : 0) | seg << 2;
+        if (first) begun = n;
+        const int before = n - begun;
+        info.flags = (first ? kFirst : 0) | (last ? kLast : 0) | (before && before % kFoldTiles == 0 ? kFold : 0) |
+                     (before > kFoldTiles ? kFolded : 0) | (before >= kFoldTiles ? kFoldedNow : 0) | seg << kSegShift;
         info.rows0 = rows[0];
         info.rows1 = rows[1];
         mbar_arrive(bar(misc->info_full[n % kInfo]));
@@ -348,8 +389,8 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       for (int n = 0; n < n_tiles && ok; ++n) {
         ok = wait_warp(misc->raw_full[st], round);
         if (!ok) break;
-        const int flags = misc->info[n % kInfo].flags, seg = flags >> 2;
-        if (flags & 1) {
+        const int flags = misc->info[n % kInfo].flags, seg = flags >> kSegShift;
+        if (flags & kFirst) {
           ok = wait_warp(misc->q_full[seg % kQRing], seg / kQRing);
           if (!ok) break;
         }
@@ -392,11 +433,11 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
           if (elect_one()) {
             mma_commit(bar(misc->s_full[n & 1]));
             mma_commit(bar(misc->raw_empty[st]));
-            if (flags & 2) mma_commit(bar(misc->q_empty[seg % kQRing]));
+            if (flags & kLast) mma_commit(bar(misc->q_empty[seg % kQRing]));
           }
         } else if (elect_one()) {
           mbar_arrive(bar(misc->raw_empty[st]));
-          if (flags & 2) mma_commit(bar(misc->q_empty[seg % kQRing]));
+          if (flags & kLast) mma_commit(bar(misc->q_empty[seg % kQRing]));
         }
         __syncwarp();
         if (++st == L.stages) { st = 0; ++round; }
@@ -410,7 +451,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         ok = wait_warp(misc->p_full[n & 1], n >> 1);
         if (!ok) break;
         tc_fence_after_sync();
-        const uint32_t fresh = misc->info[n % kInfo].flags & 1;
+        const uint32_t fresh = (misc->info[n % kInfo].flags & (kFirst | kFold)) != 0;
         const uint32_t pd = (uint32_t)p_desc + (n & 1) * (P_BYTES / 16), hi = (uint32_t)(p_desc >> 32);
 #pragma unroll 1
         for (int mb = 0; mb < NB; ++mb) {
@@ -627,9 +668,9 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       if (named_sync_or<kSoftmaxThreads>(1, !ok)) break;
       const int flags = misc->info[n % kInfo].flags;
       const int rows = slot < 64 ? misc->info[n % kInfo].rows0 : misc->info[n % kInfo].rows1;
-      if (flags & 1) {
+      if (flags & kFirst) {
         if (sidx < 32) {
-          const int seg = flags >> 2;
+          const int seg = flags >> kSegShift;
           if (ok) ok = wait(misc->q_full[seg % kQRing], seg / kQRing);       // long since; for the scales
           misc->m_used[sidx] = -INFINITY;
           misc->neg_ref[sidx] = kUnset;
@@ -638,6 +679,29 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
 #pragma unroll
         for (int i = 0; i < NHH; ++i) l_acc[i] = 0.f;
         group_sync();
+      }
+      // Output sums of the segment: this thread's latent (lane 8j + g of a quarter holds latent 4g + j).
+      auto fold = [&](bool whole, bool add) {
+        const int b = misc->info[n % kInfo].b, seq_out = a.n_heads * r;
+        fold_output<NHP, NB>(a.o_part + ((long long)blockIdx.x + b) * seq_out,
+                             whole ? static_cast<bf16*>(a.out) + (long long)b * seq_out : nullptr, misc, lane_base + kColO, HO,
+                             a.n_heads, r, q * 32 + 4 * (lane & 7) + (lane >> 3), add);
+      };
+      if (__builtin_expect(flags & kFold, 0)) {
+        // The sums so far are set down; this tile's products then begin new ones.
+        if (ok) ok = wait(misc->p_empty[(n - 1) & 1], (n - 1) >> 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (sidx < NHP) {
+          const float m = misc->m_used[sidx], m_old = misc->m_fold[sidx];
+          misc->fac[sidx] = m == m_old ? 1.f : exp2f(m_old - m);        // of use from the second time on
+          misc->m_fold[sidx] = m;
+        }
+        group_sync();
+        if (ok) {
+          tc_fence_after_sync();
+          fold(false, flags & kFolded);
+        }
+        group_sync();                                    // fac may be rewritten
       }
       float s[NHH];
       {
@@ -711,7 +775,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
         group_sync();
 #pragma unroll
         for (int i = 0; i < NHH; ++i) l_acc[i] *= misc->fac[HO + i];
-        if (!(flags & 1)) {
+        if (!(flags & (kFirst | kFold))) {
           // O is scaled to the old references: wait for the previous tile's products, rescale.
           if (ok) ok = wait(misc->p_empty[(n - 1) & 1], (n - 1) >> 1);
           ok = __all_sync(0xffffffffu, ok);              // TMEM accesses are whole-warp operations
@@ -740,7 +804,7 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(misc->p_full[n & 1]));
-      if (!(flags & 2)) continue;
+      if (!(flags & kLast)) continue;
 
       // ---- end of a segment
       const int b = misc->info[n % kInfo].b, g = g0 + n;
@@ -752,6 +816,10 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       group_sync();
       if (ok && sidx < a.n_heads) {
         const float l = misc->fac[sidx], m = misc->m_used[sidx] - kShift;
+        if (flags & kFoldedNow) {
+          const float m_set = misc->m_fold[sidx], m_now = misc->m_used[sidx];
+          misc->fac[sidx] = m_set == m_now ? 1.f : exp2f(m_set - m_now);
+        }
         misc->unit[sidx] = 1.f / l;                      // the units have done their work in this segment
         if (whole) {
           if (a.lse) a.lse[(long long)b * a.n_heads + sidx] = (m + log2f(l)) * 0.69314718055994531f;
@@ -765,7 +833,11 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
       group_sync();
       if (ok) ok = wait(misc->p_empty[n & 1], n >> 1);           // the last value products
       ok = __all_sync(0xffffffffu, ok);
-      if (ok) {
+      if (ok && __builtin_expect(flags & kFoldedNow, 0)) {
+        tc_fence_after_sync();
+        fold(whole, true);
+        tc_fence_before_sync();
+      } else if (ok) {
         tc_fence_after_sync();
         // Lane 8j + g of a quarter holds latent 4g + j.
         const int lat = q * 32 + 4 * (lane & 7) + (lane >> 3);
