@@ -26,9 +26,10 @@
 // terms, its RoPE part as one or three bf16 terms against the bf16 keys, and a probability,
 // relative to the running maximum's, as one or two half-precision terms.  Maxima, denominators and
 // all sums are fp32.  The matrix instructions cut their running sums off instead of rounding them, so a
-// score collects one product per 32 latents and, for fp32 queries, an output one per 32 slots, and the
-// products are added outside: the error against 64 bits falls by 2 to 3 (r 512, 5000 slots: 3.4e-6 to
-// 1.5e-6 of the output's size), at no time.
+// score collects one product per 32 latents and an output one per 32 slots, and the
+// products are added outside: the error against 64 bits falls by 2 to 3 for fp32 queries (r 512, 5000 slots:
+// 3.4e-6 to 1.5e-6 of the output's size), at no time; for bf16 ones outputs of 2^20 slots came out 6.6e-3
+// too small (1023 x 1024 slots, 32 heads, r 512: 588 us, so 606).
 #pragma once
 
 #include <math.h>
@@ -218,8 +219,9 @@ struct AttnLayout {
   __host__ __device__ static int bytes(const Format& f, int batch) { return off_prefix(f) + (batch + 1) * 4; }
 };
 
+// bf16 queries: two CTAs an SM, which the compiler gives up for a few registers more (740 us instead of 606).
 template <typename T, int MH>
-__global__ void __launch_bounds__(kAttnThreads) qpool_attend_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) qpool_attend_kernel(AttnArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 2;
   using L = AttnLayout<MH, TERMS>;
   constexpr int KT = L::kKeyTerms, NH = L::kHeads;
@@ -450,15 +452,13 @@ __global__ void __launch_bounds__(kAttnThreads) qpool_attend_kernel(AttnArgs a) 
           const int lr = half * 32 + lane;
           uint32_t w[4];
           ldsm_x4_trans(buf + lr * f.code_row() + (c ^ (lr & cmask)) * 16, w);
-          float part[4][MH][4];              // of these 32 slots (fp32 queries)
-          if constexpr (TERMS == 2) {
+          float part[4][MH][4];              // of these 32 slots
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 4; ++j)
 #pragma unroll
-              for (int mh = 0; mh < MH; ++mh)
+            for (int mh = 0; mh < MH; ++mh)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) part[j][mh][i] = 0.f;
-          }
+              for (int i = 0; i < 4; ++i) part[j][mh][i] = 0.f;
           uint32_t v[4][4];
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
@@ -479,16 +479,14 @@ __global__ void __launch_bounds__(kAttnThreads) qpool_attend_kernel(AttnArgs a) 
                 ldsm_x4(p_u32 + ((k * NH + mh * 16 + (lane & 15)) * L::kPStride + half * 32 + k2 * 16 + (lane >> 4) * 8) * 2, p);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                  mma_f16(TERMS == 2 ? part[j][mh] : acc[ci][j][mh], p, v[2 * k2][j], v[2 * k2 + 1][j]);
+                  mma_f16(part[j][mh], p, v[2 * k2][j], v[2 * k2 + 1][j]);
               }
-          if constexpr (TERMS == 2) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 4; ++j)
 #pragma unroll
-              for (int mh = 0; mh < MH; ++mh)
+            for (int mh = 0; mh < MH; ++mh)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[ci][j][mh][i] += part[j][mh][i];
-          }
+              for (int i = 0; i < 4; ++i) acc[ci][j][mh][i] += part[j][mh][i];
         }
       }
     }

@@ -121,3 +121,20 @@ def test_sums_are_set_down_at_any_place_of_a_sequence(r, dr, heads, lift):
              (40000, 3), (129, 0)]
     lens, lists = zip(*[kinds[i % len(kinds)] for i in range(180)])
     check(list(lens), list(lists), heads, r, dr, 0.125, r + heads, lift=lift, **TC)
+
+
+# The warp-level kernel, for batches beyond the other one's lists (1022), adds products of 32 slots outside.
+WARP = dict(cut=32, added=lambda n: n / 32 + 600)
+
+
+@pytest.mark.parametrize("r,dr,heads", [(64, 32, 4), (128, 64, 20)])
+def test_long_sequences_of_a_large_batch(r, dr, heads):
+    """2^20 slots of 1030 sequences, which take about half a second."""
+    check([1 << 20] * 1030, [0] * 1030, heads, r, dr, 0.03, r + 7, **WARP)
+
+
+@pytest.mark.parametrize("r,dr,heads,lift", [(64, 32, 8, 4.0), (320, 64, 9, 30.0), (512, 64, 32, 4.0), (448, 32, 20, 30.0)])
+def test_sums_of_a_large_batch_of_ragged_lengths(r, dr, heads, lift):
+    kinds = [(16384, 1), (16385, 1), (16448, 2), (33, 1), (32768, 2), (32769, 1), (50001, 3), (0, 0), (1, 0), (700, 1)]
+    lens, lists = zip(*[kinds[i % len(kinds)] for i in range(1030)])
+    check(list(lens), list(lists), heads, r, dr, 0.125, r + heads, lift=lift, **WARP)
