@@ -319,7 +319,7 @@ int mtla_train_backward(mtla_handle* h, const void* x, const void* dy, int32_t B
  * A batch that does not fit (too few free pages, a row wider than the table, more tokens than
  * n_tokens, a negative or overflowing length) is refused as a whole on the device: taken is -1, all
  * tokens read as behind the last one, starts is 0, slots[b] = ceil(held / s), the table is left.
- * B <= 16384. */
+ * B 1 .. 16384 (the Python binding answers for no requests by itself). */
 typedef struct {
   int32_t *starts, *seq, *position;
   int64_t *slot, *store;
@@ -398,7 +398,7 @@ int mtla_qpool_read(const mtla_qpool_config* cfg, const void* pages, const int64
  * of out and lse is NaN.)
  * workspace: device, 256-byte aligned, mtla_qpool_workspace_bytes(cfg, B) bytes (0 if invalid); its
  * contents need no preparation, but two calls that may run at the same time need one each (graphs
- * that may overlap included).  B <= 4096. */
+ * that may overlap included).  B 1 .. 4096 (the Python binding answers for no sequences by itself). */
 size_t mtla_qpool_workspace_bytes(const mtla_qpool_config* cfg, int32_t B);
 int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
                       const int32_t* slots, int32_t B, const void* q, int32_t dtype, float scale, void* out,

@@ -800,7 +800,8 @@ def make_slot_map(batch: int, n_tokens: int, device="cuda:0") -> SlotMap:
 def mtla_slot_map(held: torch.Tensor, fresh: torch.Tensor, free_pages: torch.Tensor, table: torch.Tensor, *,
                   stride: int, n_tokens: int | None = None, out: SlotMap | None = None, stream=None) -> SlotMap:
     """held, fresh [B], free_pages [F], table [B][width] (updated in place): int32 on the GPU.
-    n_tokens: entries of the token arrays; taken from `out` if that is given."""
+    n_tokens: entries of the token arrays; taken from `out` if that is given.  A batch of no requests takes
+    no pages; all its tokens read as behind the last one."""
     if table.dim() != 2 or held.dim() != 1 or free_pages.dim() != 1:
         raise TypeError("table: expected [B][width]; held and free_pages: one-dimensional")
     batch, width = table.shape
@@ -818,10 +819,18 @@ def mtla_slot_map(held: torch.Tensor, fresh: torch.Tensor, free_pages: torch.Ten
         _ptr(out.position, i32, per_token, dev, "position"), _ptr(out.slot, i64, per_token, dev, "slot"),
         _ptr(out.store, i64, per_token, dev, "store"), _ptr(out.slots, i32, per_seq, dev, "slots"),
         _ptr(out.taken, i32, (1,), dev, "taken"))
-    _check(load_library().mtla_slot_map(
-        _ptr(held, i32, per_seq, dev, "held"), _ptr(fresh, i32, per_seq, dev, "fresh"), batch, stride,
-        _ptr(table, i32, (batch, width), dev, "table"), width, _ptr(free_pages, i32, (n_free,), dev, "free_pages"),
-        n_free, ctypes.byref(o), n, _stream_on(dev, stream)), "mtla_slot_map")
+    args = (_ptr(held, i32, per_seq, dev, "held"), _ptr(fresh, i32, per_seq, dev, "fresh"), batch, stride,
+            _ptr(table, i32, (batch, width), dev, "table"), width,
+            _ptr(free_pages, i32, (n_free,), dev, "free_pages"), n_free, ctypes.byref(o), n, _stream_on(dev, stream))
+    if batch == 0:                       # the C call wants a request
+        if stride < 1 or width < 1:
+            raise MTLAError(-1, "mtla_slot_map")
+        with _buffers_on(stream):
+            for t, value in ((out.starts, 0), (out.taken, 0), (out.position, 0), (out.seq, -1), (out.slot, -1),
+                             (out.store, -1)):
+                t.fill_(value)
+        return out
+    _check(load_library().mtla_slot_map(*args), "mtla_slot_map")
     return out
 
 
@@ -927,7 +936,7 @@ def mtla_qpool_attend(cfg: mtla_qpool_config, pages: torch.Tensor, table: torch.
     """q [B][n_heads][r + d_R] over the first slots[b] slots of table row b; returns (out
     [B][n_heads][r], lse [B][n_heads] fp32).  workspace: uint8, see mtla_qpool_workspace_bytes; a
     fresh one if None (a loop should keep one).  Results made on a given stream belong to that stream,
-    as with torch's own operations."""
+    as with torch's own operations.  No sequences: nothing is launched."""
     if q.dim() != 3 or table.dim() != 2 or q.dtype not in _DTYPES:
         raise TypeError("q: expected fp32 or bf16 [B][n_heads][r + d_R]; table: expected [B][width]")
     batch, width = table.shape
@@ -941,11 +950,14 @@ def mtla_qpool_attend(cfg: mtla_qpool_config, pages: torch.Tensor, table: torch.
             if workspace is None:
                 workspace = torch.empty(mtla_qpool_workspace_bytes(cfg, batch), dtype=torch.uint8, device=q.device)
     ws_shape = workspace.shape
-    _check(load_library().mtla_qpool_attend(
-        ctypes.byref(cfg), _qpool_pages(cfg, pages, dev), _ptr(table, torch.int32, (batch, width), dev, "table"), width,
-        _ptr(slots, torch.int32, (batch,), dev, "slots"), batch,
-        _ptr(q, dtype, (batch, heads, r + cfg.rope_dim), dev, "q"), _DTYPES[dtype], scale,
-        _ptr(out, dtype, (batch, heads, r), dev, "out"), _ptr(lse, torch.float32, (batch, heads), dev, "lse"),
-        _ptr(workspace, torch.uint8, ws_shape, dev, "workspace"), ws_shape.numel(), _stream_on(dev, stream)),
-        "mtla_qpool_attend")
+    args = (ctypes.byref(cfg), _qpool_pages(cfg, pages, dev), _ptr(table, torch.int32, (batch, width), dev, "table"),
+            width, _ptr(slots, torch.int32, (batch,), dev, "slots"), batch,
+            _ptr(q, dtype, (batch, heads, r + cfg.rope_dim), dev, "q"), _DTYPES[dtype], scale,
+            _ptr(out, dtype, (batch, heads, r), dev, "out"), _ptr(lse, torch.float32, (batch, heads), dev, "lse"),
+            _ptr(workspace, torch.uint8, ws_shape, dev, "workspace"), ws_shape.numel(), _stream_on(dev, stream))
+    if batch == 0:                       # the C call wants a sequence
+        if mtla_qpool_page_bytes(cfg) == 0:
+            raise MTLAError(-2, "mtla_qpool_attend")
+        return out, lse
+    _check(load_library().mtla_qpool_attend(*args), "mtla_qpool_attend")
     return out, lse
