@@ -389,19 +389,8 @@ __host__ __device__ constexpr uint32_t make_idesc_f16(int m, int n, int a_mn_maj
 }
 
 // D[tmem] (+)= A[tmem] * B[smem]; issued by ONE thread.  A row of A is a TMEM lane, a column holds two
-// consecutive 16-bit elements along K.
-__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                           uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
-// The same with the B descriptor as its two words: only the low one (the address) changes between the
-// instructions of a loop, so advancing it is one 32-bit addition.
+// consecutive 16-bit elements along K.  The B descriptor comes as its two words: only the low one (the
+// address) changes between the instructions of a loop, so advancing it is one 32-bit addition.
 __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi,
                                            uint32_t idesc, uint32_t accumulate) {
   asm volatile(
