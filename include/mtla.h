@@ -404,6 +404,12 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
                       const int32_t* slots, int32_t B, const void* q, int32_t dtype, float scale, void* out,
                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Diagnostics: a kernel whose only wait (on a barrier nobody arrives at) runs out after about a
+ * millisecond and tells so as the attention's kernel would, and then the attention's last kernel, which
+ * answers with NaN in all of out and lse.  Arguments as for mtla_qpool_attend; nothing is left behind. */
+int mtla_selftest_qpool_timeout(const mtla_qpool_config* cfg, const int32_t* slots, int32_t B, int32_t dtype, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Bytes of cache in use: B * ceil(tokens/s) * (r + d_R) * sizeof(element)  (Sections 4, 4.3);
  * with per-sequence token counts, the sum over the sequences. */
 size_t mtla_cache_bytes(const mtla_handle* h);

@@ -42,7 +42,7 @@ EXPORTED_SYMBOLS = (
     "mtla_stack_check", "mtla_stack_launch_count", "mtla_stack_destroy",
     "mtla_train_workspace_bytes", "mtla_train_backward", "mtla_slot_map", "mtla_rope",
     "mtla_qpool_page_bytes", "mtla_qpool_write", "mtla_qpool_read", "mtla_qpool_workspace_bytes",
-    "mtla_qpool_attend")
+    "mtla_qpool_attend", "mtla_selftest_qpool_timeout")
 
 PAGE_SLOTS = 64
 
@@ -200,6 +200,7 @@ def load_library() -> ctypes.CDLL:
         "mtla_qpool_workspace_bytes": (sz, [qp_p, i32]),
         "mtla_qpool_attend": (ctypes.c_int, [qp_p, vp, vp, i32, vp, i32, vp, i32, ctypes.c_float, vp, vp, vp, sz,
                                              vp]),
+        "mtla_selftest_qpool_timeout": (ctypes.c_int, [qp_p, vp, i32, i32, vp, vp, vp, sz, vp]),
         "mtla_clear_error": (ctypes.c_int, [vp, vp]),
     }
     for name, (res, args) in sigs.items():
@@ -961,3 +962,16 @@ def mtla_qpool_attend(cfg: mtla_qpool_config, pages: torch.Tensor, table: torch.
         return out, lse
     _check(load_library().mtla_qpool_attend(*args), "mtla_qpool_attend")
     return out, lse
+
+
+def mtla_selftest_qpool_timeout(cfg: mtla_qpool_config, slots: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                                workspace: torch.Tensor, stream=None) -> None:
+    """Runs a bounded wait out and lets the attention's last kernel answer: all of out and lse is NaN."""
+    batch, heads, r = out.shape
+    dev = _gpu_of(out, "out")
+    _check(load_library().mtla_selftest_qpool_timeout(
+        ctypes.byref(cfg), _ptr(slots, torch.int32, (batch,), dev, "slots"), batch, _DTYPES[out.dtype],
+        _ptr(out, out.dtype, (batch, cfg.n_heads, cfg.latent_rank), dev, "out"),
+        _ptr(lse, torch.float32, (batch, heads), dev, "lse"),
+        _ptr(workspace, torch.uint8, workspace.shape, dev, "workspace"), workspace.numel(), _stream_on(dev, stream)),
+        "mtla_selftest_qpool_timeout")

@@ -419,4 +419,33 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
   return wide ? launch_attend<float, 2>(a, dev, st) : launch_attend<float, 1>(a, dev, st);
 }
 
+int mtla_selftest_qpool_timeout(const mtla_qpool_config* cfg, const int32_t* slots, int32_t B, int32_t dtype, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!slots || !out || !workspace || B < 1 || !good_dtype(dtype) || !aligned(slots, 4) || !aligned(out, 16) ||
+      !aligned(lse, 4) || !aligned(workspace, 256))
+    return MTLA_ERR_INVALID_ARG;
+  if (!good_pool(cfg) || B > qp::kMaxBatch) return MTLA_ERR_UNSUPPORTED_SHAPE;
+  const AttnPlan p = plan_attend(cfg, B);
+  if (workspace_bytes < p.total) return MTLA_ERR_ARENA_TOO_SMALL;
+  OnDeviceOf dev(out);
+  if (dev.status() != MTLA_OK) return dev.status();
+  char* ws = static_cast<char*>(workspace);
+  qp::AttnArgs a = {};
+  a.slots = slots;
+  a.out = out;
+  a.lse = lse;
+  a.o_part = reinterpret_cast<float*>(ws + p.o_part);
+  a.ml_part = reinterpret_cast<float*>(ws + p.ml_part);
+  a.seq_parts = reinterpret_cast<int2*>(ws + p.seq_parts);
+  a.error_words = reinterpret_cast<int*>(ws + p.error_words);
+  a.n_error_words = 1;
+  a.n_heads = cfg->n_heads;
+  a.batch = B;
+  a.f = format_of(cfg);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  qp::wait_timeout_selftest_kernel<<<1, 64, 0, st>>>(a.error_words);
+  if (launched() != MTLA_OK) return MTLA_ERR_CUDA;
+  return dtype == MTLA_DTYPE_BF16 ? launch_combine<bf16>(a, dev, st) : launch_combine<float>(a, dev, st);
+}
+
 }  // extern "C"

@@ -884,5 +884,20 @@ __global__ void __launch_bounds__(tc::kThreads, 1) qpool_attend_tc_kernel(AttnAr
   }
 }
 
+// Self-test of the bounded wait: one CTA whose only wait, on a barrier that expects an arrival which never
+// comes, gives up after 2^21 cycles (about a millisecond) instead of 2^31, and what became of it in the error
+// word that the combine reads.
+__global__ void __launch_bounds__(64) wait_timeout_selftest_kernel(int* error_word) {
+  __shared__ unsigned long long bar;
+  if (threadIdx.x == 0) {
+    ptx::mbar_init(ptx::smem_u32(&bar), 1);
+    ptx::mbar_fence_init();
+  }
+  __syncthreads();
+  const bool ok = ptx::mbar_wait_compact<1u << 21>(ptx::smem_u32(&bar), 0);
+  const bool failed = __syncthreads_or(!ok);
+  if (threadIdx.x == 0) *error_word = failed;
+}
+
 }  // namespace qp
 }  // namespace mtla

@@ -97,8 +97,9 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 }
 
 // A bounded wait in as few instructions as it takes, for kernels whose roles would otherwise not fit the
-// instruction cache together: gives up 2^31 cycles (about a second) after it began and says so;
+// instruction cache together: gives up CYCLES (2^31: about a second) after it began and says so;
 // reporting is left to the caller.
+template <uint32_t CYCLES = 0x7fffffffu>
 __device__ __forceinline__ bool mbar_wait_compact(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -110,12 +111,12 @@ __device__ __forceinline__ bool mbar_wait_compact(uint32_t bar, uint32_t parity)
       "nanosleep.u32 64;\n\t"
       "mov.u32 t, %clock;\n\t"
       "sub.u32 t, t, t0;\n\t"
-      "setp.lt.u32 q, t, 0x7fffffff;\n\t"
+      "setp.lt.u32 q, t, %4;\n\t"
       "@q bra POLL;\n"
       "DONE:\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(kSuspendHintNs)
+      : "r"(bar), "r"(parity), "r"(kSuspendHintNs), "n"(CYCLES)
       : "memory");
   return ok != 0;
 }
