@@ -117,3 +117,42 @@ def test_a_captured_step_follows_the_lengths():
             tol, tol_lse = bound(host(q[b]), seq, 0.125, mean_abs, exact, "bf16", r)
             assert (np.abs(host(out[b]) - exact) <= tol).all(), (lens, b)
             assert (np.abs(host(lse[b]) - exact_lse) <= tol_lse + 2.0 ** -23 * np.abs(exact_lse)).all(), (lens, b)
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_two_streams_with_a_workspace_each_and_different_batches(captured):
+    """Calls that overlap on two streams, each with its own workspace, kept until the end, and its own lengths and
+    queries, so that partials of one that reached the other would change a result."""
+    cfg, pages, table, slots, q, _ = attend_setup([5000, 40, 700, 0], 8, 256, 32, "bf16", 80)
+    calls = []
+    for i, lens in enumerate(([5000, 40, 700, 0], [3, 0, 1, 0])):
+        t, n, x = table.clone(), torch.tensor(lens, dtype=torch.int32, device="cuda"), (q.cuda() * (1 + i)).contiguous()
+        ws = torch.empty(M.mtla_qpool_workspace_bytes(cfg, 4), dtype=torch.uint8, device="cuda")
+        want = M.mtla_qpool_attend(cfg, pages, t, n, x, scale=0.125, workspace=ws)
+        results = [tuple(torch.full_like(w, 9.0) for w in want) for _ in range(20)]
+        calls.append((t, n, x, ws, want, results, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+
+    def run(i, k):
+        t, n, x, ws, _, results, stream = calls[i]
+        M.mtla_qpool_attend(cfg, pages, t, n, x, scale=0.125, workspace=ws, out=results[k][0], lse=results[k][1],
+                            stream=torch.cuda.current_stream() if captured else stream)
+
+    if captured:
+        graphs = []
+        for i in range(2):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[i]):
+                for k in range(20):
+                    run(i, k)
+        for i in range(2):
+            with torch.cuda.stream(calls[i][6]):
+                graphs[i].replay()
+    else:
+        for k in range(20):
+            for i in range(2):
+                run(i, k)
+    torch.cuda.synchronize()
+    for _, _, _, _, want, results, _ in calls:
+        for out, lse in results:
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
