@@ -219,9 +219,11 @@ struct AttnLayout {
   __host__ __device__ static int bytes(const Format& f, int batch) { return off_prefix(f) + (batch + 1) * 4; }
 };
 
-// bf16 queries: two CTAs an SM, which the compiler gives up for a few registers more (740 us instead of 606).
+// Two CTAs an SM where the registers allow it (not for fp32 queries of over 16 heads); left to itself the
+// compiler takes a few registers more (1023 x 1024 slots, 32 heads, bf16: 740 us for 606; 8 x 4112 slots, 16 heads,
+// fp32: 41 for 34).
 template <typename T, int MH>
-__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) qpool_attend_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 1) qpool_attend_kernel(AttnArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 2;
   using L = AttnLayout<MH, TERMS>;
   constexpr int KT = L::kKeyTerms, NH = L::kHeads;
