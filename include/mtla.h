@@ -292,7 +292,9 @@ int mtla_train_backward(mtla_handle* h, const void* x, const void* dy, int32_t B
 /* ---- operators around a paged latent cache held in 4 bits ----
  *
  * For serving loops that keep their own requests and page lists: what they run next to a layer's
- * products when the latent cache is to take about a third of its bf16 bytes.  A step is
+ * products when the latent cache is to take about a third of its bf16 bytes.  The products themselves
+ * (projections, absorbed queries, the gate and the slots' running states) are the caller's; the handles
+ * above keep theirs to themselves and do not use these pools.  Around them a step is
  *     mtla_slot_map      which slot and page every new token goes to,
  *     mtla_rope          the RoPE parts of its queries and of the shared key (Section 4.3),
  *     mtla_qpool_write   the slots' running states (Section 4.1) into the pool,
@@ -391,14 +393,16 @@ int mtla_qpool_read(const mtla_qpool_config* cfg, const void* pages, const int64
  * RoPE query), out device [B][n_heads][r] = softmax(scale q [c ; k]^T) c over the first slots[b]
  * slots of the pages in row b of `table` (device [B][table_width]); lse (device [B][n_heads], fp32,
  * may be NULL) receives the natural logarithm of the denominator, for joining with other slots.
- * dtype is that of q and out; sums, maxima and denominators are fp32.  A sequence without slots
+ * dtype is that of q and out; sums, maxima and denominators are fp32; probabilities are rounded to 11
+ * bits (bf16) or 22 bits (fp32, as are the queries' latents) for the products.  A sequence without slots
  * (slots[b] <= 0) gives zeros and minus infinity.  slots[b] past 64 * table_width counts as that
  * many; slots of a page number outside the pool are left out, and a sequence with no other gives NaN.
  * (Should a bounded wait inside the kernel give up, which nothing in a correct program leads to, all
  * of out and lse is NaN.)
  * workspace: device, 256-byte aligned, mtla_qpool_workspace_bytes(cfg, B) bytes (0 if invalid); its
  * contents need no preparation, but two calls that may run at the same time need one each (graphs
- * that may overlap included).  B 1 .. 4096 (the Python binding answers for no sequences by itself). */
+ * that may overlap included).  bf16 queries of more than 1022 sequences go to the fp32 queries' kernel, which
+ * takes about three times as long.  B 1 .. 4096 (the Python binding answers for no sequences by itself). */
 size_t mtla_qpool_workspace_bytes(const mtla_qpool_config* cfg, int32_t B);
 int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
                       const int32_t* slots, int32_t B, const void* q, int32_t dtype, float scale, void* out,

@@ -409,8 +409,9 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
   const bool wide = cfg->n_heads > 16;
   // The tensor-core kernel, except where its longer set-up shows: at most a page per SM of 64 latents
   // (4 heads, 20 slots: 7.5 us against 6.9; 3 x 200 slots: 8.8 against 8.6; but 8 heads of r 256, 512
-  // slots: 9.8 against 10.3; 64 sequences of two pages: 10.8 against 12.4).  fp32 queries, and batches
-  // whose prefix sums outgrow its shared memory, also take the other one.
+  // slots: 9.8 against 10.3; 64 sequences of two pages: 10.8 against 12.4).  fp32 queries, and batches of
+  // more sequences than it keeps lists of, also take the other one (1023 x 1024 slots, 32 heads, r 512: 605
+  // us, where 1022 take 193).
   const bool small = (long long)B * table_width <= kPlanSms && cfg->latent_rank <= 64;
   if (dtype == MTLA_DTYPE_BF16 && B <= qp::tc::kMaxBatch && !small)
     return wide ? launch_attend_tc<32>(a, dev, st) : launch_attend_tc<16>(a, dev, st);

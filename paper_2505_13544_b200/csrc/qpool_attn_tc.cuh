@@ -17,11 +17,12 @@
 // Shared memory then carries only the raw pages (three tiles of 128 slots deep), the queries and the
 // probabilities.
 //
-// Measured at 128 sequences of 16384 slots, 32 heads, r 512, d_R 64: 263 us, 3.2 TB/s of pool, 49 % of
-// the measured copy bandwidth; the bytes alone would take 130 us.  Per tile of 128 slots that is about
-// 4500 cycles.  The expansion's conversions and scalings, which share a rate of 1.25 pairs of latents
-// per cycle and SM (measured), need 2300 of them, the matrix instructions 1100, the bytes 2100.  What
-// is between is the hand-over of the operand units: a unit's buffer goes from the expanding warps
+// Measured at 128 sequences of 16384 slots, 32 heads, r 512, d_R 64: 267 us at 1965 MHz (295 us once the
+// power cap holds the clock at 1.78 GHz), 3.1 TB/s of pool, 49 % of the measured copy bandwidth; the bytes
+// alone would take 130 us.  Per tile of 128 slots that is 4740 cycles, start and join included.  The
+// expansion's conversions and scalings need 1900 of them (46.7 pairs of latents per cycle and SM for the
+// scores, 27.1 for the values, whose codes have to be paired first; measured from registers, 16 warps an
+// SM), the matrix instructions 1100, the bytes 2300.  What is between is the hand-over of the operand units: a unit's buffer goes from the expanding warps
 // through an mbarrier to the issuing warp, through the matrix unit and back in some 2200 cycles, since
 // with the memory instruction queues full of operand stores a wait takes 300 even for what is there.
 // Tensor memory has room for two units of the scores and three of the values beside the two
@@ -39,7 +40,9 @@
 // slots, 61 KB: 362 us), then the issuing threads' scalar descriptors (a uniform warp: 331), the sharing
 // out of the expansion (282) and a single score issuer (270 with two; a second value issuer adds nothing).
 // The online softmax raises a head's reference only when a tile exceeds it by 2^8.  Probabilities
-// are kept times 2^7: with the 2^8 they stay inside half precision.
+// are kept times 2^7: with the 2^8 they stay inside half precision.  For the value product they are rounded
+// to it, 2^-11 at most, an eighth of what the bf16 output is rounded by (a second term would double that
+// product and its buffers); the denominators add the unrounded ones in 32 bits.
 //
 // The matrix unit cuts its running sums off instead of rounding them: every 16 slots the output loses part
 // of its last place, always towards zero (a segment of 2^18 slots came out 1.6e-3 too small, one of
@@ -60,7 +63,9 @@ namespace tc {
 constexpr int kTile = 128;                  // slots per tile: two pages
 constexpr int kThreads = 896;
 constexpr int kMaxStages = 4;               // as many as value units' barriers
-constexpr int kMaxBatch = 1022;             // prefix sums kept in shared memory
+// Sequences whose prefix sums and slot counts every CTA keeps in shared memory: as many as fit beside three
+// stages in the largest shape (r 512, d_R 64, 32 heads).
+constexpr int kMaxBatch = 1022;
 constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kScoreIssuer2 = 3;
 constexpr int kExpandWarp0 = 4, kExpandGroups = 4;
 constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
