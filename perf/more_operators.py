@@ -6,7 +6,7 @@ one step.  Next to the 4-bit latent pool it then runs
   tree     positions of the nodes, and what each of them sees        (mtla_tree_map)
   attend   every node's query over its request's 4-bit slots and the drafted rows it sees
                                                                      (mtla_qpool_attend_tree)
-  w4       products of the step's few rows with 4-bit weights        (mtla_w4_product)
+  w4       products of the step's few rows with 4-bit weights        (mtla_qweight_product)
 
 Trees: node i of a request has a parent among the nodes before it, or -1: it follows the last token held.
 With `held` tokens it stands at position held + depth.  With stride s a node's row is the running state of its
@@ -397,7 +397,7 @@ def run(state):
                             out=M.TreeMap(**state["buf"]))
         return dict(seq=m.seq, position=m.position, seen=m.seen, slots=m.slots)
     if op == "w4":
-        return M.mtla_w4_product(state["packed"], state["x"], case["n_out"], out=state["y"])
+        return M.mtla_qweight_product(state["packed"], state["x"], case["n_out"], out=state["y"])
     cfg = M.make_qpool_config(n_heads=case["heads"], latent_rank=case["rank"], rope_dim=case["rope"],
                               n_pages=state["n_pages"])
     return list(M.mtla_qpool_attend_tree(cfg, state["pages"], state["table"], state["slots"], state["starts"],
