@@ -414,6 +414,72 @@ int mtla_qpool_attend(const mtla_qpool_config* cfg, const void* pages, const int
 int mtla_selftest_qpool_timeout(const mtla_qpool_config* cfg, const int32_t* slots, int32_t B, int32_t dtype, void* out,
                                 float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- operators of a verification step over drafted trees ----
+ *
+ * A serving loop that lets a small model draft a tree of tokens for every request verifies all nodes in one
+ * step over the 4-bit pool.  The nodes of all requests form one flat list; request b has nodes
+ * starts[b] .. starts[b + 1] - 1 (starts device [B + 1], ascending within 0 .. n_nodes; entries in front of starts[0]
+ * and behind starts[B] belong to no request).  Conventions are those of the operators above; B 1 .. 4096.  Around
+ * the loop's own model code a step is
+ *     mtla_tree_map           positions of the nodes and what each of them sees,
+ *     mtla_qweight_product    products of the step's few rows with weights in 4 bits,
+ *     mtla_rope               the RoPE parts at those positions,
+ *     mtla_qpool_attend_tree  every node's query over its request's slots and the drafted rows that it sees,
+ *     mtla_qpool_write        the rows of the accepted path into the pool (index -1 for the others). */
+
+/* Positions and masks from the trees' parents.  Request b holds held[b] tokens; node i of it (counted within the
+ * request) follows node parents[.] < i of the request, or with -1 the last token held, and stands at position
+ * held + depth.  With stride s a node's row is the running state of its chunk (Section 4.1), so it sees
+ * the closed slots of the context, slots[b] = floor(held / s) of them (an open one is continued by every
+ * path and lives on in the nodes' rows), those of its ancestors that close a chunk ((position + 1) mod s = 0), and
+ * itself: bit j of `seen` is node j of the request.  Outputs (device): seq, position, seen [n_nodes], slots [B].
+ * Nodes of no request get seq -1, position 0, seen 0; so do, refused on the device, those of a request with more
+ * than 64 nodes, a parent out of order, a negative `held` or a position past 2^31 - 1, and all nodes of a
+ * batch whose `starts` are out of order.  Requests without nodes may occur. */
+typedef struct {
+  int32_t *seq, *position;
+  int64_t* seen;
+  int32_t* slots;
+} mtla_tree_map_out;
+int mtla_tree_map(const int32_t* held, const int32_t* starts, const int32_t* parents, int32_t B, int32_t stride,
+                  const mtla_tree_map_out* out, int32_t n_nodes, void* stream);
+
+/* Attention of drafted trees: q device [n_nodes][n_heads][r + d_R] (absorbed and rotated queries), rows device
+ * [n_nodes][r + d_R], row_stride elements apart (the nodes' own latents and rotated keys, not in the pool yet;
+ * a multiple of 16 bytes unless there is one node only), out device [n_nodes][n_heads][r] =
+ * softmax(scale q [c ; k]^T) c over the first slots[b] slots of the pages in row b of `table` (as for
+ * mtla_qpool_attend) and the rows of the request's nodes j < 64 whose bit j of seen[node] is set (bits behind its nodes
+ * are ignored).  lse (device [n_nodes][n_heads], fp32, may be NULL) as there.  dtype is that of q, rows and out; sums are
+ * fp32 and probabilities of slots rounded as there, drafted rows are multiplied in fp32.  A row that a node does
+ * not see never reaches its result, whatever it holds.  A node that sees nothing (slots of page numbers outside the
+ * pool are left out) gives zeros and minus infinity.  Nodes of no request are left as they were; a batch whose
+ * `starts` are out of order gives NaN for all n_nodes.
+ * workspace: device, 256-byte aligned, mtla_qpool_tree_workspace_bytes(cfg, B, n_nodes) bytes (0 if invalid),
+ * otherwise as for mtla_qpool_attend. */
+size_t mtla_qpool_tree_workspace_bytes(const mtla_qpool_config* cfg, int32_t B, int32_t n_nodes);
+int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
+                           const int32_t* slots, const int32_t* starts, int32_t B, const void* rows, int64_t row_stride,
+                           const int64_t* seen, const void* q, int32_t n_nodes, int32_t dtype, float scale, void* out,
+                           float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Weights in 4 bits, for the projections around the pool: a matrix w device [n_in][n_out] (w_stride elements apart,
+ * fp32 or bf16) is kept as e2m1 codes with a scale per 32 inputs of an output, codes and scales as in the pool
+ * (see above; a group with an infinity or a NaN reads back as NaN), 4.25 bits a weight, in blocks of 128 inputs by 16
+ * outputs filled up with zeros.  packed: device, 16-byte aligned, mtla_qweight_bytes(n_in, n_out) bytes (0 if
+ * invalid).  n_in a multiple of 8, n_in and n_out up to 2^22.  unpack is exact in both types. */
+size_t mtla_qweight_bytes(int32_t n_in, int32_t n_out);
+int mtla_qweight_pack(const void* w, int64_t w_stride, int32_t dtype, int32_t n_in, int32_t n_out, void* packed,
+                      void* stream);
+int mtla_qweight_unpack(const void* packed, int32_t n_in, int32_t n_out, void* w, int64_t w_stride, int32_t dtype,
+                        void* stream);
+
+/* y[n][n_out] = x[n][n_in] W for the rows of a step, n up to 2^19: x device, 16-byte aligned, x_stride elements
+ * apart (a multiple of 16 bytes unless n is 1), y device, y_stride elements apart (any, at least n_out); they must not
+ * overlap.  dtype is that of x and y.  Weights enter exactly, sums are fp32.  Every row's result is independent
+ * of the others' values. */
+int mtla_qweight_product(const void* packed, int32_t n_in, int32_t n_out, const void* x, int64_t x_stride, int32_t n,
+                         void* y, int64_t y_stride, int32_t dtype, void* stream);
+
 /* Bytes of cache in use: B * ceil(tokens/s) * (r + d_R) * sizeof(element)  (Sections 4, 4.3);
  * with per-sequence token counts, the sum over the sequences. */
 size_t mtla_cache_bytes(const mtla_handle* h);

@@ -42,7 +42,9 @@ EXPORTED_SYMBOLS = (
     "mtla_stack_check", "mtla_stack_launch_count", "mtla_stack_destroy",
     "mtla_train_workspace_bytes", "mtla_train_backward", "mtla_slot_map", "mtla_rope",
     "mtla_qpool_page_bytes", "mtla_qpool_write", "mtla_qpool_read", "mtla_qpool_workspace_bytes",
-    "mtla_qpool_attend", "mtla_selftest_qpool_timeout")
+    "mtla_qpool_attend", "mtla_selftest_qpool_timeout", "mtla_tree_map", "mtla_qpool_tree_workspace_bytes",
+    "mtla_qpool_attend_tree", "mtla_qweight_bytes", "mtla_qweight_pack", "mtla_qweight_unpack",
+    "mtla_qweight_product")
 
 PAGE_SLOTS = 64
 
@@ -99,6 +101,10 @@ class mtla_stack_config(ctypes.Structure):
 
 class mtla_slot_map_out(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("starts", "seq", "position", "slot", "store", "slots", "taken")]
+
+
+class mtla_tree_map_out(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("seq", "position", "seen", "slots")]
 
 
 class mtla_rope_config(ctypes.Structure):
@@ -202,6 +208,14 @@ def load_library() -> ctypes.CDLL:
                                              vp]),
         "mtla_selftest_qpool_timeout": (ctypes.c_int, [qp_p, vp, i32, i32, vp, vp, vp, sz, vp]),
         "mtla_clear_error": (ctypes.c_int, [vp, vp]),
+        "mtla_tree_map": (ctypes.c_int, [vp, vp, vp, i32, i32, ctypes.POINTER(mtla_tree_map_out), i32, vp]),
+        "mtla_qpool_tree_workspace_bytes": (sz, [qp_p, i32, i32]),
+        "mtla_qpool_attend_tree": (ctypes.c_int, [qp_p, vp, vp, i32, vp, vp, i32, vp, ctypes.c_int64, vp, vp, i32, i32,
+                                                  ctypes.c_float, vp, vp, vp, sz, vp]),
+        "mtla_qweight_bytes": (sz, [i32, i32]),
+        "mtla_qweight_pack": (ctypes.c_int, [vp, ctypes.c_int64, i32, i32, i32, vp, vp]),
+        "mtla_qweight_unpack": (ctypes.c_int, [vp, i32, i32, vp, ctypes.c_int64, i32, vp]),
+        "mtla_qweight_product": (ctypes.c_int, [vp, i32, i32, vp, ctypes.c_int64, i32, vp, ctypes.c_int64, i32, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -975,3 +989,145 @@ def mtla_selftest_qpool_timeout(cfg: mtla_qpool_config, slots: torch.Tensor, out
         _ptr(lse, torch.float32, (batch, heads), dev, "lse"),
         _ptr(workspace, torch.uint8, workspace.shape, dev, "workspace"), workspace.numel(), _stream_on(dev, stream)),
         "mtla_selftest_qpool_timeout")
+
+
+# --------------------------------------------------------------------------- drafted trees, 4-bit weights
+
+@dataclass
+class TreeMap:
+    """Outputs of mtla_tree_map (see include/mtla.h); keep one to reuse its buffers."""
+    seq: torch.Tensor        # int32 [n_nodes]
+    position: torch.Tensor   # int32 [n_nodes]
+    seen: torch.Tensor       # int64 [n_nodes]
+    slots: torch.Tensor      # int32 [B]
+
+
+def make_tree_map(batch: int, n_nodes: int, device="cuda:0") -> TreeMap:
+    """Buffers for a batch and a number of nodes."""
+    i32 = dict(dtype=torch.int32, device=device)
+    return TreeMap(torch.empty(n_nodes, **i32), torch.empty(n_nodes, **i32),
+                   torch.empty(n_nodes, dtype=torch.int64, device=device), torch.empty(batch, **i32))
+
+
+def mtla_tree_map(held: torch.Tensor, starts: torch.Tensor, parents: torch.Tensor, *, stride: int,
+                  out: TreeMap | None = None, stream=None) -> TreeMap:
+    """held [B], starts [B + 1], parents [n_nodes]: int32 on the GPU.  Without requests all nodes are of none."""
+    if held.dim() != 1 or starts.dim() != 1 or parents.dim() != 1:
+        raise TypeError("held, starts and parents: expected one dimension")
+    batch, n = held.shape[0], parents.shape[0]
+    if out is None:
+        with _buffers_on(stream):
+            out = make_tree_map(batch, n, held.device)
+    dev, i32, per_seq, per_node = _gpu_of(held, "held"), torch.int32, (batch,), (n,)
+    o = mtla_tree_map_out(
+        _ptr(out.seq, i32, per_node, dev, "seq"), _ptr(out.position, i32, per_node, dev, "position"),
+        _ptr(out.seen, torch.int64, per_node, dev, "seen"), _ptr(out.slots, i32, per_seq, dev, "slots"))
+    args = (_ptr(held, i32, per_seq, dev, "held"), _ptr(starts, i32, (batch + 1,), dev, "starts"),
+            _ptr(parents, i32, per_node, dev, "parents"), batch, stride, ctypes.byref(o), n, _stream_on(dev, stream))
+    if batch == 0:                       # the C call wants a request
+        if stride < 1:
+            raise MTLAError(-1, "mtla_tree_map")
+        with _buffers_on(stream):
+            for t, value in ((out.seq, -1), (out.position, 0), (out.seen, 0)):
+                t.fill_(value)
+        return out
+    _check(load_library().mtla_tree_map(*args), "mtla_tree_map")
+    return out
+
+
+def mtla_qpool_tree_workspace_bytes(cfg: mtla_qpool_config, batch: int, n_nodes: int) -> int:
+    return load_library().mtla_qpool_tree_workspace_bytes(ctypes.byref(cfg), batch, n_nodes)
+
+
+def mtla_qpool_attend_tree(cfg: mtla_qpool_config, pages: torch.Tensor, table: torch.Tensor, slots: torch.Tensor,
+                           starts: torch.Tensor, rows: torch.Tensor, seen: torch.Tensor, q: torch.Tensor, *,
+                           scale: float, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                           workspace: torch.Tensor | None = None, stream=None):
+    """q [n_nodes][n_heads][r + d_R] over the first slots[b] slots of table row b and the rows [n_nodes][r + d_R] of
+    the node's request (starts int32 [B + 1]) that seen (int64 [n_nodes]) names; returns (out [n_nodes][n_heads][r],
+    lse [n_nodes][n_heads] fp32).  workspace: uint8, see mtla_qpool_tree_workspace_bytes; a fresh one if
+    None (a loop should keep one).  Results made on a given stream belong to that stream, as with torch's own operations."""
+    if q.dim() != 3 or table.dim() != 2 or q.dtype not in _DTYPES:
+        raise TypeError("q: expected fp32 or bf16 [n_nodes][n_heads][r + d_R]; table: expected [B][width]")
+    batch, width = table.shape
+    n, heads, r, dev, dtype = q.shape[0], cfg.n_heads, cfg.latent_rank, _gpu_of(pages, "pages"), q.dtype
+    if rows.dtype is not dtype:
+        raise TypeError(f"rows: expected {dtype}, as q")
+    if out is None or lse is None or workspace is None:
+        with _buffers_on(stream):
+            if out is None:
+                out = torch.empty(n, heads, r, dtype=dtype, device=q.device)
+            if lse is None:
+                lse = torch.empty(n, heads, dtype=torch.float32, device=q.device)
+            if workspace is None:
+                workspace = torch.empty(mtla_qpool_tree_workspace_bytes(cfg, max(batch, 1), n), dtype=torch.uint8,
+                                        device=q.device)
+    ws_shape = workspace.shape
+    args = (ctypes.byref(cfg), _qpool_pages(cfg, pages, dev), _ptr(table, torch.int32, (batch, width), dev, "table"),
+            width, _ptr(slots, torch.int32, (batch,), dev, "slots"),
+            _ptr(starts, torch.int32, (batch + 1,), dev, "starts"), batch, _qpool_rows(cfg, rows, dev, n, "rows"),
+            rows.stride(0), _ptr(seen, torch.int64, (n,), dev, "seen"),
+            _ptr(q, dtype, (n, heads, r + cfg.rope_dim), dev, "q"), n, _DTYPES[dtype], scale,
+            _ptr(out, dtype, (n, heads, r), dev, "out"), _ptr(lse, torch.float32, (n, heads), dev, "lse"),
+            _ptr(workspace, torch.uint8, ws_shape, dev, "workspace"), ws_shape.numel(), _stream_on(dev, stream))
+    if batch == 0 or n == 0:             # nothing to do, but for the configuration's check
+        if mtla_qpool_page_bytes(cfg) == 0:
+            raise MTLAError(-2, "mtla_qpool_attend_tree")
+        return out, lse
+    _check(load_library().mtla_qpool_attend_tree(*args), "mtla_qpool_attend_tree")
+    return out, lse
+
+
+def mtla_qweight_bytes(n_in: int, n_out: int) -> int:
+    return load_library().mtla_qweight_bytes(n_in, n_out)
+
+
+def _qweight_buffer(packed: torch.Tensor, n_in: int, n_out: int, dev: int) -> int:
+    size = (n_in + 127) // 128 * ((n_out + 15) // 16) * 1088     # mtla_qweight_bytes, without the call
+    return _ptr(packed, torch.uint8, (size,), dev, "packed")
+
+
+def mtla_qweight_pack(w: torch.Tensor, packed: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """w [n_in][n_out] (fp32 or bf16, consecutive elements in a row) in 4 bits: uint8 [mtla_qweight_bytes]."""
+    if w.dim() != 2 or w.dtype not in _DTYPES or (w.shape[1] > 1 and w.stride(1) != 1):
+        raise TypeError("w: expected fp32 or bf16 [n_in][n_out], consecutive elements in a row")
+    (n_in, n_out), dev = w.shape, _gpu_of(w, "w")
+    size = mtla_qweight_bytes(n_in, n_out)
+    if size == 0:
+        raise MTLAError(-2, "mtla_qweight_bytes")
+    if packed is None:
+        with _buffers_on(stream):
+            packed = torch.empty(size, dtype=torch.uint8, device=w.device)
+    _check(load_library().mtla_qweight_pack(w.data_ptr(), w.stride(0), _DTYPES[w.dtype], n_in, n_out,
+                                            _qweight_buffer(packed, n_in, n_out, dev), _stream_on(dev, stream)),
+           "mtla_qweight_pack")
+    return packed
+
+
+def mtla_qweight_unpack(packed: torch.Tensor, n_in: int, n_out: int, *, dtype=torch.bfloat16, stream=None):
+    """The weights [n_in][n_out] that a packed buffer stands for."""
+    dev = _gpu_of(packed, "packed")
+    pp = _qweight_buffer(packed, n_in, n_out, dev)
+    with _buffers_on(stream):
+        w = torch.empty(n_in, n_out, dtype=dtype, device=packed.device)
+    _check(load_library().mtla_qweight_unpack(pp, n_in, n_out, w.data_ptr(), n_out, _DTYPES[dtype],
+                                              _stream_on(dev, stream)), "mtla_qweight_unpack")
+    return w
+
+
+def mtla_qweight_product(packed: torch.Tensor, x: torch.Tensor, n_out: int, out: torch.Tensor | None = None,
+                         stream=None) -> torch.Tensor:
+    """x [n][n_in] (fp32 or bf16, any row stride of whole 16 bytes) times packed weights [n_in][n_out]: [n][n_out]."""
+    if x.dim() != 2 or x.dtype not in _DTYPES or x.stride(1) != 1:
+        raise TypeError("x: expected fp32 or bf16 [n][n_in], consecutive elements in a row")
+    (n, n_in), dev = x.shape, _gpu_of(x, "x")
+    if out is None:
+        with _buffers_on(stream):
+            out = torch.empty(n, n_out, dtype=x.dtype, device=x.device)
+    if out.dtype is not x.dtype or out.shape != (n, n_out) or out.get_device() != dev or (
+            n_out > 1 and out.stride(1) != 1):
+        raise TypeError(f"out: expected {x.dtype} [{n}][{n_out}] on the call's GPU, consecutive elements in a row")
+    _check(load_library().mtla_qweight_product(_qweight_buffer(packed, n_in, n_out, dev), n_in, n_out, x.data_ptr(),
+                                               x.stride(0), n, out.data_ptr(), out.stride(0), _DTYPES[x.dtype],
+                                               _stream_on(dev, stream)), "mtla_qweight_product")
+    return out

@@ -9,7 +9,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "libmtla.so")
-SOURCES = ["mtla_api.cu", "ops_api.cu"]
+SOURCES = ["mtla_api.cu", "ops_api.cu", "tree_api.cu", "qweight_api.cu"]
 OBJ_DIR = os.path.join(PKG_DIR, "_build")
 
 

@@ -55,6 +55,12 @@ struct AttnArgs {
   float scale_log2;          // scale * log2(e)
   int n_heads, batch, width, n_pages, n_error_words;
   Format f;
+  // Column groups of drafted trees (tree_kernels.cuh) in the place of sequences: how many there are, the tiles before
+  // each, and its request, first column, columns and slots.  Their results are always parts, of `cols` columns.
+  const int* n_groups;
+  const int* prefix;
+  const int4* groups;
+  int cols;
 };
 
 constexpr int kAttnThreads = 256;
@@ -182,6 +188,19 @@ __device__ inline long long tile_prefix(const AttnArgs& a, int* prefix, int* war
   __syncthreads();
   return prefix[a.batch];
 }
+// Largest b with list[b] <= i in ascending global memory list[0 .. n], by a whole warp.
+__device__ __forceinline__ int find_wide(const int* list, int n, int i) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const uint32_t below = __ballot_sync(0xffffffffu, at < hi && list[at < hi ? at : lo] <= i);
+    const int k = max(1, __popc(below));             // the first ones, lane 0's among them
+    lo += (k - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
 __device__ __forceinline__ int find_seq(const int* prefix, int batch, int g) {   // largest b with prefix[b] <= g
   int lo = 0, hi = batch;
   while (hi - lo > 1) {
@@ -224,7 +243,8 @@ struct AttnLayout {
 // Two CTAs an SM where the registers allow it (not for fp32 queries of over 16 heads); left to itself the
 // compiler takes a few registers more (1023 x 1024 slots, 32 heads, bf16: 740 us for 606; 8 x 4112 slots, 16 heads,
 // fp32: 41 for 34).
-template <typename T, int MH>
+// TREE: over column groups instead of sequences.
+template <typename T, int MH, bool TREE = false>
 __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 1) qpool_attend_kernel(AttnArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 2;
   using L = AttnLayout<MH, TERMS>;
@@ -234,7 +254,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const Format f = a.f;
   const int r = f.r, dr = f.dr, page_bytes = f.page_bytes();
-  int* prefix = reinterpret_cast<int*>(smem + L::off_prefix(f));
+  int* own_prefix = reinterpret_cast<int*>(smem + L::off_prefix(f));
   __half* qs = reinterpret_cast<__half*>(smem + L::off_q(f));
   bf16* ks = reinterpret_cast<bf16*>(smem + L::off_k(f));
   float* ss = reinterpret_cast<float*>(smem + L::off_s(f));
@@ -247,7 +267,9 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
 
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const long long total = tile_prefix<1>(a, prefix, warp_sums, kAttnThreads);
+  const int* const prefix = TREE ? a.prefix : own_prefix;
+  const int n_seqs = TREE ? max(*a.n_groups, 0) : a.batch;
+  const long long total = TREE ? prefix[n_seqs] : tile_prefix<1>(a, own_prefix, warp_sums, kAttnThreads);
   if (total == 0) return;
   // With fewer tiles than CTAs the rest stays out, so that every share has a tile and the parts of
   // a sequence follow one another without a gap.
@@ -257,13 +279,14 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
 
   // Tile n of the list into its buffer; rows past the sequence's end (and pages outside the pool)
   // are filled with zeros, so that nothing behind the last slot enters a product.
+  auto page_of = [&](int b, int tile) { return a.table[(long long)(TREE ? a.groups[b].x : b) * a.width + tile]; };
   auto tile_rows = [&](int b, int tile) {
-    const int page = a.table[(long long)b * a.width + tile];
-    return page < 0 || page >= a.n_pages ? 0 : min(kPageRows, a.slots[b] - tile * kPageRows);
+    const int page = page_of(b, tile);
+    return page < 0 || page >= a.n_pages ? 0 : min(kPageRows, (TREE ? a.groups[b].w : a.slots[b]) - tile * kPageRows);
   };
   auto load_tile = [&](int n, int b) {
     const int tile = n - prefix[b], rows = tile_rows(b, tile);
-    const uint8_t* src = a.pages + (rows ? (long long)a.table[(long long)b * a.width + tile] * page_bytes : 0);
+    const uint8_t* src = a.pages + (rows ? (long long)page_of(b, tile) * page_bytes : 0);
     const uint32_t dst = raw_u32 + ((n - g0) % L::kStages) * page_bytes;
     const int c_bytes = f.off_scales(), s_bytes = f.off_keys();
     for (int o = tid * 16; o < page_bytes; o += kAttnThreads * 16) {
@@ -277,7 +300,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
     }
   };
 
-  int b = find_seq(prefix, a.batch, g0), b_load = b;
+  int b = TREE ? find_wide(prefix, n_seqs, g0) : find_seq(prefix, n_seqs, g0), b_load = b;
   load_tile(g0, b);
   cp_async_commit();
 
@@ -297,10 +320,12 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
     if (seg_first) {
       // The sequence's query: a warp per head.  The row is scaled by a power of two so that its
       // largest element lies in [2^14, 2^15).
+      const long long col0 = TREE ? (long long)a.groups[b].y : (long long)b * a.n_heads;
+      const int n_cols = TREE ? a.groups[b].z : a.n_heads;
       for (int h = warp; h < NH; h += kAttnWarps) {
-        const T* q = static_cast<const T*>(a.q) + ((long long)b * a.n_heads + h) * (r + dr);
+        const T* q = static_cast<const T*>(a.q) + (col0 + h) * (r + dr);
         float top = 0.f;
-        if (h < a.n_heads)
+        if (h < n_cols)
           for (int i = lane; i < r + dr; i += 32) top = fmaxf(top, fabsf(Elem<T>::to_float(q[i])));
         top = warp_max(top);
         const bool fine = top > 0.f && top < INFINITY;
@@ -311,7 +336,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
           unit_s[h] = ldexpf(a.scale_log2, -e);
         }
         for (int i = lane; i < r; i += 32) {
-          float v = h < a.n_heads ? ldexpf(Elem<T>::to_float(q[i]), e) : 0.f;
+          float v = h < n_cols ? ldexpf(Elem<T>::to_float(q[i]), e) : 0.f;
 #pragma unroll
           for (int k = 0; k < TERMS; ++k) {
             const __half x = __float2half_rn(v);
@@ -320,7 +345,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
           }
         }
         for (int i = lane; i < dr; i += 32) {
-          float v = h < a.n_heads ? ldexpf(Elem<T>::to_float(q[r + i]), e) : 0.f;
+          float v = h < n_cols ? ldexpf(Elem<T>::to_float(q[r + i]), e) : 0.f;
 #pragma unroll
           for (int k = 0; k < KT; ++k) {
             const bf16 x = __float2bfloat16_rn(v);
@@ -496,7 +521,8 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
     }
     if (seg_last) {
       // ---- end of a segment: the finished output, or a partial
-      const bool whole = prefix[b] >= g0 && tile + 1 == seq_tiles;
+      const int n_cols = TREE ? a.groups[b].z : a.n_heads, stride = TREE ? a.cols : a.n_heads;
+      const bool whole = !TREE && prefix[b] >= g0 && tile + 1 == seq_tiles;
       const int c0 = share_owner(prefix[b], total, ctas);
       const int part = blockIdx.x + b;                     // unique per (CTA, sequence), parts of a sequence in a row
       if (tid == 0 && tile + 1 == seq_tiles)
@@ -510,7 +536,7 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
             const int h = mh * 16 + hh * 8 + g;
-            if (h >= a.n_heads) continue;
+            if (h >= n_cols) continue;
             // Fragment column 2t is latent 8t + j, column 2t + 1 latent 8t + 4 + j: eight in a row.
             float v[8];
 #pragma unroll
@@ -531,18 +557,18 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
                 store_vec(d + 4, v1);
               }
             } else {
-              float* d = a.o_part + ((long long)part * a.n_heads + h) * r + c * kGroup + 8 * t;
+              float* d = a.o_part + ((long long)part * stride + h) * r + c * kGroup + 8 * t;
               *reinterpret_cast<float4*>(d) = make_float4(v[0], v[1], v[2], v[3]);
               *reinterpret_cast<float4*>(d + 4) = make_float4(v[4], v[5], v[6], v[7]);
             }
           }
       }
-      if (tid < a.n_heads) {
+      if (tid < n_cols) {
         if (whole) {
           if (a.lse) a.lse[(long long)b * a.n_heads + tid] = (m_s[tid] - kProbShift + log2f(l_s[tid])) * 0.69314718055994531f;
         } else {
-          a.ml_part[((long long)part * a.n_heads + tid) * 2] = m_s[tid] - kProbShift;
-          a.ml_part[((long long)part * a.n_heads + tid) * 2 + 1] = l_s[tid];
+          a.ml_part[((long long)part * stride + tid) * 2] = m_s[tid] - kProbShift;
+          a.ml_part[((long long)part * stride + tid) * 2 + 1] = l_s[tid];
         }
       }
     }

@@ -122,7 +122,7 @@ __device__ __forceinline__ uint32_t encode8(const float (&y)[8]) {
 }
 // The same from the definition, by comparing |x| with the borders 0.25 s .. 5 s, which are exact in
 // fp32: no quotient, hence no rounding that could move a value across a border.
-__device__ __noinline__ uint32_t encode8_exact(const float* x, float s) {
+inline __device__ __noinline__ uint32_t encode8_exact(const float* x, float s) {
   uint32_t code = 0;
   for (int i = 0; i < 8; ++i) {
     const float v = fabsf(x[i]);
