@@ -6,6 +6,7 @@
 #include "common.cuh"
 #include "ops_common.cuh"
 #include "qpool_attn.cuh"
+#include "tree_attn_tc.cuh"
 #include "tree_kernels.cuh"
 
 using namespace mtla;
@@ -14,7 +15,7 @@ using namespace mtla::ops;
 namespace {
 
 constexpr int kMostCtas = 2 * kPlanSms;          // of the launch over the context
-constexpr int kLeastCols = 16, kMostCols = 32;   // of a group
+constexpr int kLeastCols = 16, kMostCols = 64;   // of a group
 
 // Sized for any group width, so that the choice between the kernels stays the call's.
 struct TreePlan { size_t o_part, ml_part, parts, groups, prefix, first, n_groups, error_words, total; };
@@ -53,6 +54,42 @@ int launch_context(qp::AttnArgs a, long long tiles, const OnDeviceOf& dev, cudaS
   const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms, per_sm = smem <= 112 * 1024 ? 2 : 1;
   const int ctas = (int)(tiles < (long long)per_sm * sms ? tiles : (long long)per_sm * sms);
   return launch_dependent(qp::qpool_attend_kernel<T, MH, true>, dim3(ctas), qp::kAttnThreads, smem, st, a);
+}
+
+// The roles' registers come out of what the kernel is launched with; an increase that this does not cover would wait
+// for ever, so nothing is launched then.  Asked once.
+template <auto Kernel>
+bool registers_suffice() {
+  static std::atomic<int> known{0};                // 0 not asked, 1 yes, 2 no
+  int state = known.load(std::memory_order_relaxed);
+  if (state == 0) {
+    cudaFuncAttributes attr;
+    if (cudaFuncGetAttributes(&attr, Kernel) != cudaSuccess) return false;
+    constexpr int kWarps = tree::kThreads / 32;
+    state = (attr.numRegs + 7) / 8 * 8 * kWarps >= tree::kRoleRegisters ? 1 : 2;
+    known.store(state, std::memory_order_relaxed);
+  }
+  return state == 1;
+}
+
+template <int NC, int NB>
+int launch_context_tc(const qp::AttnArgs& a, long long tiles, const OnDeviceOf& dev, cudaStream_t st) {
+  if (!raise_smem<tree::tree_attend_tc_kernel<NC, NB>>(dev.device()) ||
+      !registers_suffice<tree::tree_attend_tc_kernel<NC, NB>>())
+    return MTLA_ERR_CUDA;
+  const tree::Layout l(a.f, NC);
+  const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
+  return launch_dependent(tree::tree_attend_tc_kernel<NC, NB>, dim3(tiles < sms ? (int)tiles : sms), tree::kThreads,
+                          l.total, st, a, l);
+}
+template <int NC>
+int launch_context_tc(const qp::AttnArgs& a, long long tiles, const OnDeviceOf& dev, cudaStream_t st) {
+  switch (ceil_div(a.f.r, 128)) {
+    case 1: return launch_context_tc<NC, 1>(a, tiles, dev, st);
+    case 2: return launch_context_tc<NC, 2>(a, tiles, dev, st);
+    case 3: return launch_context_tc<NC, 3>(a, tiles, dev, st);
+    default: return launch_context_tc<NC, 4>(a, tiles, dev, st);
+  }
 }
 
 template <typename T>
@@ -122,7 +159,9 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   char* ws = static_cast<char*>(workspace);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
 
-  const int cols = (long long)n_nodes * cfg->n_heads > 16ll * B ? 32 : 16;
+  const long long all_cols = (long long)n_nodes * cfg->n_heads;
+  const bool tensor = dtype == MTLA_DTYPE_BF16;
+  const int cols = tensor ? (all_cols > 32ll * B ? 64 : 32) : (all_cols > 16ll * B ? 32 : 16);
   tree::PlanArgs pa;
   pa.slots = slots;
   pa.starts = starts;
@@ -135,7 +174,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   pa.heads = cfg->n_heads;
   pa.width = table_width;
   pa.cols = cols;
-  pa.tile_pages = 1;
+  pa.tile_pages = tensor ? 2 : 1;
   int status = launch_dependent(tree::tree_plan_kernel, dim3(1), tree::kPlanThreads, 0, st, pa);
   if (status != MTLA_OK) return status;
 
@@ -156,9 +195,10 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   a.prefix = pa.prefix;
   a.groups = pa.groups;
   a.cols = cols;
-  const long long tiles = most_groups(cfg, B, n_nodes, cols) * table_width;
-  if (dtype == MTLA_DTYPE_BF16)
-    status = cols == 32 ? launch_context<bf16, 2>(a, tiles, dev, st) : launch_context<bf16, 1>(a, tiles, dev, st);
+  const long long tiles = most_groups(cfg, B, n_nodes, cols) * ceil_div(table_width, pa.tile_pages);
+  const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
+  if (tensor)
+    status = cols == 64 ? launch_context_tc<64>(a, tiles, dev, st) : launch_context_tc<32>(a, tiles, dev, st);
   else
     status = cols == 32 ? launch_context<float, 2>(a, tiles, dev, st) : launch_context<float, 1>(a, tiles, dev, st);
   if (status != MTLA_OK) return status;
@@ -183,7 +223,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   j.n_nodes = n_nodes;
   j.heads = cfg->n_heads;
   j.cols = cols;
-  j.n_error_words = 0;
+  j.n_error_words = tensor ? (int)(tiles < sms ? tiles : sms) : 0;
   j.f = a.f;
   return dtype == MTLA_DTYPE_BF16 ? launch_join<bf16>(j, dev, st) : launch_join<float>(j, dev, st);
 }

@@ -1,0 +1,707 @@
+// Attention of drafted trees' columns over the 4-bit pool on the fifth-generation tensor cores (bf16 queries).
+//
+// The mathematics, the orientation of both products and the expansion of the codes into tensor memory are those of
+// qpool_attn_tc.cuh; what differs is that a tree brings many columns (nodes times heads) to the same slots, so that
+// an expanded tile is used by NC = 64 of them instead of one sequence's heads.  The bound then is arithmetic: per
+// tile of 128 slots and r 512 the matrix unit needs 68 x 32 = 2180 cycles, the expansion of both operands about 1900 of
+// the issue slots, the softmax of 128 x 64 scores about 500.
+//
+// Tensor memory holds the output sums (r / 128 blocks of NC columns), one or two score tiles and operand units of 32
+// columns: 64 latents of the 128 slots for the scores, or 64 slots of 128 latents for the values.  Units half as wide as
+// there leave three buffers for each product beside 64 columns of r 512.
+//
+// Groups of columns take the place of sequences; a group's result is always a part (reference, denominator, sums in 32
+// bits) that tree_join_kernel joins with the drafted rows.  Roles (28 warps): warp 0 issues the score products, warp 1
+// the value products, warp 2 is the producer; warps 4-19 expand in four groups that take units in turn and write the
+// queries; warps 20-27 are softmax and epilogue.  Every wait is bounded as there.
+#pragma once
+
+#include "qpool_attn_tc.cuh"
+
+namespace mtla {
+namespace tree {
+
+constexpr int kTile = 128, kThreads = 896;
+constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kExpandWarp0 = 4, kExpandGroups = 4;
+constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
+// Registers of a thread of the issuing, expanding and softmax warps, and of all warps together.
+constexpr int kIssueRegs = 40, kExpandRegs = 64, kSoftmaxRegs = 104;
+constexpr int kRoleRegisters = 4 * kIssueRegs + 16 * kExpandRegs + 8 * kSoftmaxRegs;
+static_assert(kRoleRegisters <= 72 * (kThreads / 32), "more than 72 registers a thread are not there for 896 threads");
+constexpr int kQRing = qp::tc::kQRing, kInfo = 16, kUnitRing = 8, kMaxStages = 4;
+constexpr float kShift = qp::tc::kShift, kRescale = qp::tc::kRescale, kUnset = qp::tc::kUnset;
+constexpr int kFoldTiles = qp::tc::kFoldTiles;
+constexpr int kFirst = 1, kLast = 2, kFold = 4, kFolded = 8, kFoldedNow = 16, kEnds = 32, kSegShift = 6;
+
+// Tensor memory for NC columns and NB blocks of 128 latents.
+template <int NC, int NB>
+struct Tmem {
+  static constexpr int kScores = (2 + NB) * NC + 6 * 32 <= 512 ? 2 : 1;        // score tiles
+  static constexpr int kLeft = (512 - (kScores + NB) * NC) / 64;
+  static constexpr int kUnits = kLeft < 4 ? kLeft : 4;                         // buffers for each product
+  static constexpr int kColS = 0, kColO = kScores * NC, kColAs = kColO + NB * NC, kColAv = kColAs + 32 * kUnits;
+  static_assert(kUnits >= 3 && kColAv + 32 * kUnits <= 512, "tensor memory budget");
+};
+
+struct TileInfo {
+  int group, flags;          // flags: the above; the segment's number times 64
+  int rows0, rows1;          // slots of the tile's two pages
+  int cols, owner;           // columns of the group, the CTA of its first tile
+};
+
+struct Misc {
+  unsigned long long code_full[kMaxStages], code_empty[kMaxStages], scale_full[kMaxStages];
+  unsigned long long key_full[2], key_empty[2];
+  unsigned long long as_full[kUnitRing], as_empty[kUnitRing], av_full[kUnitRing], av_empty[kUnitRing];
+  unsigned long long s_full[2], s_empty[2], p_full[2], p_empty[2];
+  unsigned long long q_full[kQRing], q_empty[kQRing];
+  unsigned long long info_full[kInfo];
+  uint32_t tmem_base;
+  int abort_word;
+  TileInfo info[kInfo];
+  float m_used[64];
+  alignas(16) float neg_ref[64];
+  alignas(16) float unit[64];
+  float next_unit[kQRing][64];
+  float fac[64];
+  float red[8][32];
+  float m_fold[64];
+};
+constexpr int kMiscBytes = 5120;
+static_assert(sizeof(Misc) <= kMiscBytes, "misc region too small");
+
+struct Layout {
+  int scales, stage, stages, key_stage, key_stages, p_bytes, p_stages, scale_room;
+  int off_codes, off_keys, off_q, off_p, off_st, off_misc, total;
+  __host__ __device__ Layout(const qp::Format& f, int nc) {
+    scales = kTile * f.code_row();
+    stage = (scales + kTile * f.scale_row() + 127) / 128 * 128;
+    key_stage = kTile * f.key_row();
+    scale_room = f.scale_row() * kTile * 2;
+    p_bytes = kTile * nc * 2;
+    const int q_room = (nc * 2 * (f.r + f.dr) + 1023) / 1024 * 1024;
+    const int room = qp::tc::kSmemMax - kMiscBytes - 1024 - q_room;
+    // Three stages of codes in any shape (the expansion's waits rely on them), then a second key stage and
+    // probability tile, then the fourth.
+    key_stages = p_stages = 1;
+    stages = 3;
+    auto used = [&]() { return stages * (stage + scale_room) + key_stages * key_stage + p_stages * p_bytes; };
+    if (used() + key_stage <= room) key_stages = 2;
+    if (used() + p_bytes <= room) p_stages = 2;
+    if (used() + stage + scale_room <= room) stages = 4;
+    off_keys = 0;                                           // swizzled operands: 1024-byte aligned
+    off_q = off_keys + key_stages * key_stage;
+    off_p = off_q + q_room;
+    off_codes = off_p + p_stages * p_bytes;
+    off_st = off_codes + stages * stage;
+    off_misc = (off_st + stages * scale_room + 15) / 16 * 16;
+    total = off_misc + kMiscBytes + 1024;
+  }
+};
+
+template <int NC, int NB>
+__global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArgs a, Layout L) {
+  using namespace ptx;
+  using T = Tmem<NC, NB>;
+  constexpr uint32_t IDESC_S = make_idesc_f16(128, NC, 0, 0), IDESC_K = make_idesc_bf16(128, NC, 0, 0);
+  constexpr uint32_t IDESC_V = make_idesc_f16(128, NC, 0, 1);
+  constexpr uint32_t P_SBO = kTile * 16;        // bytes between groups of 8 columns of a probability tile
+  constexpr int U = 2 * NB, SB = T::kScores, BUFS = T::kUnits;
+  constexpr int QW = NB == 1 ? 8 : 16, QB = 2, QV = (NB * 16 + 8 + 31) / 32;
+  extern __shared__ uint8_t smem_raw[];
+  const qp::Format f = a.f;
+  const int r = f.r, dr = f.dr;
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* sm = smem_raw + (base - raw);
+  Misc* misc = reinterpret_cast<Misc*>(sm + L.off_misc);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // warp: uniform
+  auto bar = [&](unsigned long long& p) { return smem_u32(&p); };
+
+  if (threadIdx.x < kInfo) {
+    const int i = threadIdx.x;
+    mbar_init(bar(misc->info_full[i]), 1);
+    if (i < kUnitRing) {
+      mbar_init(bar(misc->as_full[i]), 4);
+      mbar_init(bar(misc->as_empty[i]), 1);
+      mbar_init(bar(misc->av_full[i]), 4);
+      mbar_init(bar(misc->av_empty[i]), 1);
+    }
+    if (i < kMaxStages) {
+      mbar_init(bar(misc->code_full[i]), 1);
+      mbar_init(bar(misc->code_empty[i]), 2 * U * 4);            // a warp of every unit
+      mbar_init(bar(misc->scale_full[i]), U * 4);
+      mbar_init(bar(misc->q_full[i]), QW);
+      mbar_init(bar(misc->q_empty[i]), 1);
+    }
+    if (i < 2) {
+      mbar_init(bar(misc->key_full[i]), 1);
+      mbar_init(bar(misc->key_empty[i]), 1);
+      mbar_init(bar(misc->s_full[i]), 1);
+      mbar_init(bar(misc->s_empty[i]), kSoftmaxWarps);
+      mbar_init(bar(misc->p_full[i]), kSoftmaxWarps);
+      mbar_init(bar(misc->p_empty[i]), 1);
+    }
+    if (i == 0) misc->abort_word = 0;
+    mbar_fence_init();
+  }
+  if (warp == kProducerWarp) tmem_alloc(smem_u32(&misc->tmem_base), 512);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  constexpr uint32_t tmem = 0;                  // all columns are this CTA's
+  grid_launch_dependents();
+  grid_dependency_wait();
+
+  const int* const prefix = a.prefix;
+  const int n_groups = max(*a.n_groups, 0);
+  const long long total = prefix[n_groups];
+  const int ctas = (int)(total < gridDim.x ? total : gridDim.x);
+  int g0 = 0, g1 = 0;
+  if ((int)blockIdx.x < ctas) {
+    g0 = qp::share_begin(blockIdx.x, total, ctas);
+    g1 = qp::share_begin(blockIdx.x + 1, total, ctas);
+  }
+  const int n_tiles = __shfl_sync(0xffffffffu, g1 - g0, 0);      // uniform
+  const uint32_t q_u32 = base + L.off_q, p_u32 = base + L.off_p, st_u32 = base + L.off_st;
+  auto wait = [&](unsigned long long& b, int phase) { return mbar_wait_compact(bar(b), phase & 1); };
+  auto wait_warp = [&](unsigned long long& b, int phase) {                 // one answer for the warp
+    return __all_sync(0xffffffffu, wait(b, phase)) != 0;
+  };
+  bool ok = true;                // false once a wait of this thread has given up
+  if (threadIdx.x == 0 && misc->tmem_base != 0) misc->abort_word = 1;
+
+  if (n_tiles == 0) {
+    // nothing to do; the CTA falls through to the common end
+  } else if (warp < kExpandWarp0) {
+    reg_dealloc<kIssueRegs>();
+    if (warp == kProducerWarp) {
+      // ---------------------------------------------------------------- producer
+      int v = qp::find_wide(prefix, n_groups, g0), seg = -1, st = 0, round = 0, begun = 0;
+      if (lane == 0) {
+        int v_begin = prefix[v], v_end = prefix[v + 1];
+        int4 group = a.groups[v];
+        for (int n = 0; n < n_tiles; ++n) {
+          const int g = g0 + n;
+          while (v_end <= g) {
+            ++v;
+            v_begin = v_end;
+            v_end = prefix[v + 1];
+            group = a.groups[v];
+          }
+          const int tile = g - v_begin;
+          const bool first = n == 0 || tile == 0, ends = g + 1 == v_end, last = n + 1 == n_tiles || ends;
+          int page[2], rows[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int t = 2 * tile + i, have = group.w - t * qp::kPageRows;
+            page[i] = have > 0 && t < a.width ? __ldg(a.table + (long long)group.x * a.width + t) : -1;
+            rows[i] = page[i] >= 0 && page[i] < a.n_pages ? min(have, qp::kPageRows) : 0;
+          }
+          ok = wait(misc->code_empty[st], round + 1);
+          if (!ok) break;
+          TileInfo& info = misc->info[n % kInfo];
+          seg += first;
+          if (first) begun = n;
+          const int before = n - begun;
+          info.group = v;
+          info.flags = (first ? kFirst : 0) | (last ? kLast : 0) | (ends ? kEnds : 0) |
+                       (before && before % kFoldTiles == 0 ? kFold : 0) | (before > kFoldTiles ? kFolded : 0) |
+                       (before >= kFoldTiles ? kFoldedNow : 0) | seg << kSegShift;
+          info.rows0 = rows[0];
+          info.rows1 = rows[1];
+          info.cols = group.z;
+          info.owner = qp::share_owner(v_begin, total, ctas);
+          mbar_arrive(bar(misc->info_full[n % kInfo]));
+          const uint32_t full = bar(misc->code_full[st]), dst = base + L.off_codes + st * L.stage;
+          const uint8_t* src[2];
+          uint32_t bytes = 0;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            src[i] = a.pages + (rows[i] ? (long long)page[i] * f.page_bytes() : 0);
+            bytes += rows[i] * f.code_row() + (rows[i] * f.scale_row() + 15) / 16 * 16;
+          }
+          mbar_arrive_expect_tx(full, bytes);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (rows[i] == 0) continue;
+            bulk_load(dst + L.scales + i * qp::kPageRows * f.scale_row(), src[i] + f.off_scales(),
+                      (rows[i] * f.scale_row() + 15) / 16 * 16, full);
+            bulk_load(dst + i * qp::kPageRows * f.code_row(), src[i], rows[i] * f.code_row(), full);
+          }
+          const int ks = L.key_stages == 2 ? n & 1 : 0, key_round = L.key_stages == 2 ? n >> 1 : n;
+          ok = wait(misc->key_empty[ks], key_round + 1);
+          if (!ok) break;
+          const uint32_t key_bar = bar(misc->key_full[ks]), key_dst = base + L.off_keys + ks * L.key_stage;
+          mbar_arrive_expect_tx(key_bar, (rows[0] + rows[1]) * f.key_row());
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (rows[i]) bulk_load(key_dst + i * qp::kPageRows * f.key_row(), src[i] + f.off_keys(), rows[i] * f.key_row(), key_bar);
+          if (++st == L.stages) { st = 0; ++round; }
+        }
+      }
+    } else if (warp == kScoreIssuer) {
+      // ---------------------------------------------------------------- score products (whole warp, uniform)
+      const uint64_t mode = dr == 64 ? kSwizzle128B : kSwizzle64B;
+      const uint32_t key_sbo = 8 * f.key_row();
+      const uint64_t q_desc = make_smem_desc(q_u32, 16, 1024, kSwizzle128B);
+      const uint64_t qk_desc = make_smem_desc(q_u32 + NC * 2 * r, 16, key_sbo, mode);
+      int buf = 0;
+      for (int n = 0; n < n_tiles && ok; ++n) {
+        const int ks = L.key_stages == 2 ? n & 1 : 0, key_round = L.key_stages == 2 ? n >> 1 : n;
+        ok = wait_warp(misc->key_full[ks], key_round);
+        if (!ok) break;
+        const int flags = misc->info[n % kInfo].flags, seg = flags >> kSegShift;
+        if (flags & kFirst) {
+          ok = wait_warp(misc->q_full[seg % kQRing], seg / kQRing);
+          if (!ok) break;
+        }
+        ok = wait_warp(misc->s_empty[n % SB], n / SB + 1);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t d = tmem + T::kColS + (n % SB) * NC;
+        const uint64_t key_desc = make_smem_desc(base + L.off_keys + ks * L.key_stage, 16, key_sbo, mode);
+        if (elect_one()) {                               // RoPE part: d_R / 16 is 2 or 4
+          mma_bf16_ss(d, key_desc, qk_desc, IDESC_K, 0u);
+          mma_bf16_ss(d, key_desc + 2, qk_desc + 2, IDESC_K, 1u);
+          if (dr == 64) {
+            mma_bf16_ss(d, key_desc + 4, qk_desc + 4, IDESC_K, 1u);
+            mma_bf16_ss(d, key_desc + 6, qk_desc + 6, IDESC_K, 1u);
+          }
+          mma_commit(bar(misc->key_empty[ks]));
+        }
+        __syncwarp();
+#pragma unroll 1
+        for (int p = 0; p < U; ++p) {
+          const int k = n * U + p, s = U == 8 ? 2 * (p & 3) + (p >> 2) : p;
+          ok = wait_warp(misc->as_full[k % kUnitRing], k / kUnitRing);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t at = tmem + T::kColAs + buf * 32;
+          const uint32_t panel = (uint32_t)q_desc + s * NC * 8, hi = (uint32_t)(q_desc >> 32);
+          if (elect_one()) {
+            if (s * 64 < r) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) mma_f16_ts(d, at + i * 8, panel + i * 2, hi, IDESC_S, 1u);
+            }
+            mma_commit(bar(misc->as_empty[k % kUnitRing]));
+          }
+          __syncwarp();
+          if (++buf == BUFS) buf = 0;
+        }
+        if (!ok) break;
+        if (elect_one()) {
+          mma_commit(bar(misc->s_full[n % SB]));
+          if (flags & kLast) mma_commit(bar(misc->q_empty[seg % kQRing]));
+        }
+        __syncwarp();
+      }
+    } else if (warp == kValueIssuer) {
+      // ---------------------------------------------------------------- value products (whole warp, uniform)
+      const uint64_t p_desc = make_smem_desc(p_u32, 128, P_SBO, kSwizzleNone);
+      int buf = 0;
+      for (int n = 0; n < n_tiles && ok; ++n) {
+        const int ps = L.p_stages == 2 ? n & 1 : 0, p_round = L.p_stages == 2 ? n >> 1 : n;
+        ok = wait_warp(misc->p_full[ps], p_round);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t fresh = (misc->info[n % kInfo].flags & (kFirst | kFold)) != 0;
+        const uint32_t pd = (uint32_t)p_desc + ps * (L.p_bytes / 16), hi = (uint32_t)(p_desc >> 32);
+#pragma unroll 1
+        for (int p = 0; p < U; ++p) {
+          const int k = n * U + p, mb = U == 8 ? p & 3 : p >> 1, h = U == 8 ? p >> 2 : p & 1;
+          ok = wait_warp(misc->av_full[k % kUnitRing], k / kUnitRing);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t d = tmem + T::kColO + mb * NC, at = tmem + T::kColAv + buf * 32;
+          if (elect_one()) {
+            mma_f16_ts(d, at, pd + h * 64, hi, IDESC_V, h ? 1u : fresh ^ 1u);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) mma_f16_ts(d, at + i * 8, pd + h * 64 + i * 16, hi, IDESC_V, 1u);
+            mma_commit(bar(misc->av_empty[k % kUnitRing]));
+          }
+          __syncwarp();
+          if (++buf == BUFS) buf = 0;
+        }
+        if (ok && elect_one()) mma_commit(bar(misc->p_empty[ps]));
+        __syncwarp();
+      }
+    }
+  } else if (warp < kSoftmaxWarp0) {
+    // ------------------------------------------------------------------ expansion
+    // Four groups of four warps take the units in turn, a group expanding unit k for the scores and then
+    // unit k - U, the same place of the tile before, for the values.  With eight units a tile their order makes both a
+    // group's score units cover the 128 latents of its value units, so that it waits for no other group's scales.
+    reg_dealloc<kExpandRegs>();
+    const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2, t = lane & 3;
+    const int slot = q * 32 + lane, row = slot & 63;
+    const int cmask = f.code_mask(), chunks = r / qp::kGroup, code_row = f.code_row();
+    const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16);
+    const uint32_t twist = (uint32_t)(lane & cmask) * 16;       // rows lane, lane + 32, ... twist alike
+    const int n_units = n_tiles * U;
+    int seg = -1, v = qp::find_wide(prefix, n_groups, g0), next_start = 0;
+    int n = 0, p = grp, st = 0, round = 0, buf = grp % BUFS;
+    auto next_tile = [&]() {
+      ++n;
+      if (++st == L.stages) { st = 0; ++round; }
+    };
+#pragma unroll 1
+    while (p >= U) { p -= U; next_tile(); }
+#pragma unroll 1
+    for (int k = grp; k < n_units + U; k += kExpandGroups) {
+      if (k < n_units) {
+        if (__builtin_expect(n >= next_start, 0)) {
+          int start;
+          do {
+            start = next_start;
+            while (prefix[v + 1] <= g0 + start) ++v;
+            next_start = prefix[v + 1] - g0;
+            ++seg;
+          } while (n >= next_start);
+          if (n == start && p < QW / 4) {
+            const int4 group = a.groups[v];
+            ok = qp::put_queries<NC, QW, QB, QV>(static_cast<const bf16*>(a.q) + (long long)group.y * (r + dr),
+                                                 sm + L.off_q, misc, a.scale_log2, group.z, f, seg, p * 4 + q);
+            if (!ok) break;
+          }
+        }
+        // The buffer first: that the unit which had it has been used also tells that the stage's phase is the
+        // one before this tile's or later, which its parity alone would not.
+        ok = (k < BUFS || wait(misc->as_empty[(k - BUFS) % kUnitRing], (k - BUFS) / kUnitRing)) &&
+             wait(misc->code_full[st], round);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const int s = U == 8 ? 2 * (p & 3) + (p >> 2) : p, c = 2 * s;
+        if (c < chunks) {
+          const TileInfo& info = misc->info[n % kInfo];
+          const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
+          const uint32_t stage = base + L.off_codes + st * L.stage;
+          const uint32_t codes = stage + slot * code_row, scales = stage + L.scales + slot * f.scale_row();
+          // The scales also go out as half precision, a group's 128 slots in a row, for the value units;
+          // zero where there is no slot, so that whatever its codes are, the product is zero.
+          const uint32_t st_out = st_u32 + st * L.scale_room + slot * 2 + c * (kTile * 2);
+          const uint32_t at = lane_tm + T::kColAs + buf * 32;
+          const uint4 w0 = qp::lds128(codes + ((uint32_t)(c * 16) ^ twist));
+          const uint4 w1 = qp::lds128(codes + ((uint32_t)(c * 16 + 16) ^ twist));
+          uint32_t two;
+          asm volatile("{\n\t.reg .u16 x;\n\tld.shared.u16 x, [%1];\n\tcvt.u32.u16 %0, x;\n\t}"
+                       : "=r"(two) : "r"(scales + c));
+          const uint32_t s01 = __byte_perm(two, 0, 0x4140) << 7, out = s01 & live;        // both as half precision
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out), "h"((uint16_t)out) : "memory");
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + kTile * 2), "h"((uint16_t)(out >> 16)) : "memory");
+          const uint32_t sc0 = __byte_perm(s01, 0, 0x1010), sc1 = __byte_perm(s01, 0, 0x3232);
+          const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t x[16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t o[4];
+              qp::decode8(word[4 * half + i], o);
+#pragma unroll
+              for (int m = 0; m < 4; ++m) x[4 * i + m] = qp::mul_h2(o[m], half ? sc1 : sc0);
+            }
+            tmem_st_x16(at + half * 16, x);
+          }
+        }
+        tmem_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar(misc->as_full[k % kUnitRing]));
+          if (U != 8) mbar_arrive(bar(misc->scale_full[st]));
+          mbar_arrive(bar(misc->code_empty[st]));
+        }
+      }
+      const int kv = k - U;
+      if (kv >= 0) {
+        const int mb = U == 8 ? p & 3 : p >> 1, h = U == 8 ? p >> 2 : p & 1, c = mb * 4 + q;
+        const int stv = st == 0 ? L.stages - 1 : st - 1, roundv = st == 0 ? round - 1 : round;
+        // With eight units a tile the scales are this group's own: that unit k - BUFS has been used tells that its
+        // four warps have written those of unit k - 4 and before; behind the last tile only the units' own
+        // barriers do.
+        ok = kv < BUFS || wait(misc->av_empty[(kv - BUFS) % kUnitRing], (kv - BUFS) / kUnitRing);
+        if (U == 8) {
+          if (k >= n_units && p < 4)
+            ok = ok && wait(misc->as_full[kv % kUnitRing], kv / kUnitRing) &&
+                 wait(misc->as_full[(kv + 4) % kUnitRing], (kv + 4) / kUnitRing);
+        } else {
+          ok = ok && wait(misc->code_full[stv], roundv) && wait(misc->scale_full[stv], roundv);
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after_sync();
+        if (c < chunks) {
+          const uint32_t from = base + L.off_codes + stv * L.stage + (h * 64 + lane) * code_row + ((uint32_t)(c * 16) ^ twist);
+          const uint32_t sc_at = st_u32 + stv * L.scale_room + c * (kTile * 2) + h * 128 + 4 * t;
+          // Value units are numbered from the tile before, so their buffer is that of unit kv.
+          const uint32_t col = lane_tm + T::kColAv + (kv % BUFS) * 32;
+          uint32_t w[2][4];
+          qp::ldsm_x4_trans(from, w[0]);
+          qp::ldsm_x4_trans(from + 32 * code_row, w[1]);
+#pragma unroll
+          for (int i2 = 0; i2 < 2; ++i2) {
+            uint32_t x[4][4];
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+              uint32_t sc;
+              asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sc_at + i2 * 64 + m * 16));
+              qp::decode_pairs(w[i2][m], x[m]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[m][i] = qp::mul_h2(x[m][i], sc);
+            }
+            const uint32_t to = col + i2 * 16;
+            tmem_st_16x128_x4(to, x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]);
+            tmem_st_16x128_x4(to + (16u << 16), x[0][2], x[0][3], x[1][2], x[1][3], x[2][2], x[2][3], x[3][2], x[3][3]);
+          }
+        }
+        tmem_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar(misc->av_full[kv % kUnitRing]));
+          mbar_arrive(bar(misc->code_empty[stv]));
+        }
+      }
+      p += kExpandGroups;
+#pragma unroll 1
+      while (p >= U) { p -= U; next_tile(); }
+      buf += kExpandGroups % BUFS;
+      if (buf >= BUFS) buf -= BUFS;
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax and epilogue
+    // Two groups of four warps: group gr owns columns [gr * NHH, (gr + 1) * NHH) of the tile's 128 slots, a slot per
+    // thread.  They leave the loop together (they agree on it once a tile, before anything that depends on
+    // the tile's description), so the hardware barrier always completes.
+    reg_alloc<kSoftmaxRegs>();
+    constexpr int NHH = NC / 2;
+    const int sw = warp - kSoftmaxWarp0, gr = sw >> 2, q = warp & 3, HO = gr * NHH;
+    const int sidx = sw * 32 + lane, slot = q * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + HO;
+    auto group_sync = [&]() { named_sync<1, kSoftmaxThreads>(); };
+    // One value per column over the warp's 32 slots, left in red[sw][i]: halving exchanges, in each of
+    // which a lane keeps half of its columns and adds the partner's share of them.
+    auto reduce_columns = [&](float (&x)[NHH], bool is_max) {
+      auto join = [&](float c, float d) { return is_max ? fmaxf(c, d) : c + d; };
+#pragma unroll
+      for (int n = NHH, o = 16; n > 1; n >>= 1, o >>= 1) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) {
+          const float keep = upper ? x[i + n / 2] : x[i], give = upper ? x[i] : x[i + n / 2];
+          x[i] = join(keep, __shfl_xor_sync(0xffffffffu, give, o));
+        }
+      }
+      float y = x[0];                                    // column (lane / (32 / NHH)) of the group
+#pragma unroll
+      for (int o = 16 / NHH; o >= 1; o >>= 1) y = join(y, __shfl_xor_sync(0xffffffffu, y, o));
+      if ((lane & (32 / NHH - 1)) == 0) misc->red[sw][lane / (32 / NHH)] = y;
+    };
+    auto reduced = [&](int h, bool is_max) {
+      const float* x = &misc->red[(h / NHH) * 4][h % NHH];
+      return is_max ? fmaxf(fmaxf(x[0], x[32]), fmaxf(x[64], x[96])) : (x[0] + x[32]) + (x[64] + x[96]);
+    };
+    auto load_scores = [&](int n, float (&x)[NHH]) {
+      uint32_t s[NHH / 16][16];
+#pragma unroll
+      for (int i = 0; i < NHH / 16; ++i) tmem_ld_x16(lane_base + T::kColS + (n % SB) * NC + i * 16, s[i]);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < NHH; ++i) x[i] = __uint_as_float(s[i / 16][i % 16]);
+    };
+    uint8_t* const p_row = sm + L.off_p + (HO / 8) * P_SBO + slot * 16;
+    float l_acc[NHH];
+    for (int n = 0; n < n_tiles; ++n) {
+      if (ok && sw == 3) ok = wait(misc->info_full[n % kInfo], n / kInfo) && wait(misc->s_full[n % SB], n / SB);
+      if (named_sync_or<kSoftmaxThreads>(1, !ok)) break;
+      const TileInfo& info = misc->info[n % kInfo];
+      const int flags = info.flags;
+      const int rows = slot < 64 ? info.rows0 : info.rows1;
+      const int ps = L.p_stages == 2 ? n & 1 : 0, p_round = L.p_stages == 2 ? n >> 1 : n;
+      const int ps1 = L.p_stages == 2 ? (n - 1) & 1 : 0, p_round1 = L.p_stages == 2 ? (n - 1) >> 1 : n - 1;
+      if (flags & kFirst) {
+        if (sidx < 64) {
+          const int seg = flags >> kSegShift;
+          if (ok) ok = wait(misc->q_full[seg % kQRing], seg / kQRing);       // long since; for the scales
+          misc->m_used[sidx] = -INFINITY;
+          misc->neg_ref[sidx] = kUnset;
+          misc->unit[sidx] = sidx < NC ? misc->next_unit[seg % kQRing][sidx] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < NHH; ++i) l_acc[i] = 0.f;
+        group_sync();
+      }
+      // Output sums of the segment, this thread's latent of every block (lane 8j + g of a quarter holds latent
+      // 4g + j), into the segment's part: added to what has been set down there, which fac brings to the
+      // present references, or without `add` as they are.
+      auto set_down = [&](bool add) {
+        const int lat = q * 32 + 4 * (lane & 7) + (lane >> 3), cols = info.cols;
+        float* part = a.o_part + ((long long)blockIdx.x + info.group) * a.cols * r;
+#pragma unroll 1
+        for (int i = 0; i < NB * (NHH / 16); ++i) {
+          const int mb = i % NB, ho = HO + i / NB * 16;
+          uint32_t o[16];
+          tmem_ld_x16(lane_base + T::kColO + mb * NC + i / NB * 16, o);
+          tmem_wait_ld();
+          if (mb * 128 + lat >= r) continue;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            if (ho + j >= cols) break;
+            const long long e = (long long)(ho + j) * r + mb * 128 + lat;
+            float x = __uint_as_float(o[j]);
+            if (add) x = fmaf(part[e], misc->fac[ho + j], x);
+            part[e] = x;
+          }
+        }
+      };
+      if (__builtin_expect(flags & kFold, 0)) {
+        // The sums so far are set down; this tile's products then begin new ones.
+        if (ok) ok = wait(misc->p_empty[ps1], p_round1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (sidx < NC) {
+          const float m = misc->m_used[sidx], m_old = misc->m_fold[sidx];
+          misc->fac[sidx] = m == m_old ? 1.f : exp2f(m_old - m);        // of use from the second time on
+          misc->m_fold[sidx] = m;
+        }
+        group_sync();
+        if (ok) {
+          tc_fence_after_sync();
+          set_down(flags & kFolded);
+          tc_fence_before_sync();
+        }
+        group_sync();                                    // fac may be rewritten
+      }
+      float x[NHH];
+      tc_fence_after_sync();
+      load_scores(n, x);
+      const bool live = (slot & 63) < rows, full = __all_sync(0xffffffffu, live);
+      // x = score - reference + shift in log2 units.
+      auto offset_scores = [&]() {
+#pragma unroll
+        for (int i = 0; i < NHH; i += 4) {
+          const float4 u = *reinterpret_cast<const float4*>(&misc->unit[HO + i]);
+          const float4 o = *reinterpret_cast<const float4*>(&misc->neg_ref[HO + i]);
+          x[i] = fmaf(x[i], u.x, o.x);
+          x[i + 1] = fmaf(x[i + 1], u.y, o.y);
+          x[i + 2] = fmaf(x[i + 2], u.z, o.z);
+          x[i + 3] = fmaf(x[i + 3], u.w, o.w);
+        }
+        if (!full) {                                     // only a sequence's last tile
+#pragma unroll
+          for (int i = 0; i < NHH; ++i) x[i] = live ? x[i] : -INFINITY;
+        }
+      };
+      offset_scores();
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < NHH; ++i) top = fmaxf(top, x[i]);
+      if (sw == 3 && ok) ok = wait(misc->p_empty[ps], p_round + 1);    // value products of the tile that had it
+      if (named_sync_or<kSoftmaxThreads>(1, top > kShift + kRescale)) {
+        // Rare: some reference has to rise (always at a segment's first tile).
+        load_scores(n, x);
+#pragma unroll
+        for (int i = 0; i < NHH; ++i) x[i] = live ? x[i] * misc->unit[HO + i] : -INFINITY;
+        reduce_columns(x, true);
+        group_sync();
+        if (sidx < NC) {
+          const float mt = reduced(sidx, true), m_old = misc->m_used[sidx];
+          const float m_new = mt > m_old + kRescale ? mt : m_old;
+          misc->m_used[sidx] = m_new;
+          misc->neg_ref[sidx] = m_new == -INFINITY ? kUnset : kShift - m_new;
+          misc->fac[sidx] = m_new == m_old ? 1.f : exp2f(m_old - m_new);       // 0 from minus infinity
+        }
+        group_sync();
+#pragma unroll
+        for (int i = 0; i < NHH; ++i) l_acc[i] *= misc->fac[HO + i];
+        if (!(flags & (kFirst | kFold))) {
+          // O is scaled to the old references: wait for the previous tile's products, rescale.
+          if (ok) ok = wait(misc->p_empty[ps1], p_round1);
+          ok = __all_sync(0xffffffffu, ok);              // TMEM accesses are whole-warp operations
+          if (ok) {
+            tc_fence_after_sync();
+#pragma unroll 1
+            for (int i = 0; i < NB * (NHH / 16); ++i) {
+              const uint32_t at = lane_base + T::kColO + (i % NB) * NC + i / NB * 16;
+              uint32_t o[16];
+              tmem_ld_x16(at, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                o[j] = __float_as_uint(__uint_as_float(o[j]) * misc->fac[HO + i / NB * 16 + j]);
+              tmem_st_x16(at, o);
+            }
+            tmem_wait_st();
+          }
+        }
+        load_scores(n, x);
+        offset_scores();
+        group_sync();                                    // fac / red may be rewritten
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(misc->s_empty[n % SB]));
+      // P as the MN-major, un-swizzled B operand: eight columns of a slot are 16 bytes, eight slots
+      // follow one another, groups of eight columns are P_SBO apart.
+#pragma unroll
+      for (int i = 0; i < NHH / 8; ++i) {
+        uint32_t pb[4];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const float e0 = ex2_approx(x[8 * i + j]), e1 = ex2_approx(x[8 * i + j + 1]);
+          l_acc[8 * i + j] += e0;
+          l_acc[8 * i + j + 1] += e1;
+          const __half2 y = __floats2half2_rn(e0, e1);
+          pb[j / 2] = *reinterpret_cast<const uint32_t*>(&y);
+        }
+        if (ok) *reinterpret_cast<uint4*>(p_row + ps * L.p_bytes + i * P_SBO) = make_uint4(pb[0], pb[1], pb[2], pb[3]);
+      }
+      fence_proxy_async_smem();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(misc->p_full[ps]));
+      if (!(flags & kLast)) continue;
+
+      // ---- end of a segment
+      const int v = info.group, part = (int)blockIdx.x + v;
+      reduce_columns(l_acc, false);
+      group_sync();
+      if (ok && sidx < info.cols) {
+        const float m = misc->m_used[sidx];
+        *reinterpret_cast<float2*>(a.ml_part + ((long long)part * a.cols + sidx) * 2) =
+            make_float2(m - kShift, reduced(sidx, false));
+        if (flags & kFoldedNow) {
+          const float m_set = misc->m_fold[sidx];
+          misc->fac[sidx] = m_set == m ? 1.f : exp2f(m_set - m);
+        }
+      }
+      if (ok && sidx == 0 && (flags & kEnds)) a.seq_parts[v] = make_int2(info.owner + v, (int)blockIdx.x - info.owner + 1);
+      group_sync();
+      if (ok) ok = wait(misc->p_empty[ps], p_round);             // the last value products
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok) {
+        tc_fence_after_sync();
+        set_down(flags & kFoldedNow);
+        tc_fence_before_sync();
+      }
+      group_sync();                                      // fac, unit and the references may be rewritten
+    }
+  }
+
+  if (!ok) misc->abort_word = 1;
+  __syncthreads();
+  if (threadIdx.x == 0) a.error_words[blockIdx.x] = misc->abort_word;
+  if (misc->abort_word) {
+    // Give copies that may still be in flight time to land before the CTA's memory is reused.
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 100000ull) __nanosleep(1000);
+  }
+  if (warp == kProducerWarp) {
+    __syncwarp();
+    tc_fence_after_sync();
+    tmem_dealloc(misc->tmem_base, 512);
+  }
+}
+
+}  // namespace tree
+}  // namespace mtla
