@@ -22,7 +22,8 @@ namespace mtla {
 namespace tree {
 
 constexpr int kTile = 128, kThreads = 896;
-constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kExpandWarp0 = 4, kExpandGroups = 4;
+constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kExpandWarp0 = 4;
+constexpr int kExpandGroups = 4, kScoreGroups = 2;
 constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
 // Registers of a thread of the issuing, expanding and softmax warps, and of all warps together.
 constexpr int kIssueRegs = 40, kExpandRegs = 64, kSoftmaxRegs = 104;
@@ -107,7 +108,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
   constexpr uint32_t IDESC_V = make_idesc_f16(128, NC, 0, 1);
   constexpr uint32_t P_SBO = kTile * 16;        // bytes between groups of 8 columns of a probability tile
   constexpr int U = 2 * NB, SB = T::kScores, BUFS = T::kUnits;
-  constexpr int QW = NB == 1 ? 8 : 16, QB = 2, QV = (NB * 16 + 8 + 31) / 32;
+  constexpr int QW = 4 * kScoreGroups, QB = 2, QV = (NB * 16 + 8 + 31) / 32;
   extern __shared__ uint8_t smem_raw[];
   const qp::Format f = a.f;
   const int r = f.r, dr = f.dr;
@@ -272,14 +273,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         __syncwarp();
 #pragma unroll 1
         for (int p = 0; p < U; ++p) {
-          const int k = n * U + p, s = U == 8 ? 2 * (p & 3) + (p >> 2) : p;
+          const int k = n * U + p;
           ok = wait_warp(misc->as_full[k % kUnitRing], k / kUnitRing);
           if (!ok) break;
           tc_fence_after_sync();
           const uint32_t at = tmem + T::kColAs + buf * 32;
-          const uint32_t panel = (uint32_t)q_desc + s * NC * 8, hi = (uint32_t)(q_desc >> 32);
+          const uint32_t panel = (uint32_t)q_desc + p * NC * 8, hi = (uint32_t)(q_desc >> 32);
           if (elect_one()) {
-            if (s * 64 < r) {
+            if (p * 64 < r) {
 #pragma unroll
               for (int i = 0; i < 4; ++i) mma_f16_ts(d, at + i * 8, panel + i * 2, hi, IDESC_S, 1u);
             }
@@ -308,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         const uint32_t pd = (uint32_t)p_desc + ps * (L.p_bytes / 16), hi = (uint32_t)(p_desc >> 32);
 #pragma unroll 1
         for (int p = 0; p < U; ++p) {
-          const int k = n * U + p, mb = U == 8 ? p & 3 : p >> 1, h = U == 8 ? p >> 2 : p & 1;
+          const int k = n * U + p, mb = p % NB, h = p / NB;
           ok = wait_warp(misc->av_full[k % kUnitRing], k / kUnitRing);
           if (!ok) break;
           tc_fence_after_sync();
@@ -328,27 +329,41 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     }
   } else if (warp < kSoftmaxWarp0) {
     // ------------------------------------------------------------------ expansion
-    // Four groups of four warps take the units in turn, a group expanding unit k for the scores and then
-    // unit k - U, the same place of the tile before, for the values.  With eight units a tile their order makes both a
-    // group's score units cover the 128 latents of its value units, so that it waits for no other group's scales.
+    // Groups of four warps, kScoreGroups for the scores' operand, the others for the values', each kind taking its
+    // units in turn: the scores' units then never wait behind a value unit whose buffer waits for the probabilities.
     reg_dealloc<kExpandRegs>();
     const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2, t = lane & 3;
-    const int slot = q * 32 + lane, row = slot & 63;
     const int cmask = f.code_mask(), chunks = r / qp::kGroup, code_row = f.code_row();
     const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16);
     const uint32_t twist = (uint32_t)(lane & cmask) * 16;       // rows lane, lane + 32, ... twist alike
     const int n_units = n_tiles * U;
-    int seg = -1, v = qp::find_wide(prefix, n_groups, g0), next_start = 0;
-    int n = 0, p = grp, st = 0, round = 0, buf = grp % BUFS;
-    auto next_tile = [&]() {
-      ++n;
-      if (++st == L.stages) { st = 0; ++round; }
+    const bool scores_role = grp < kScoreGroups;
+    const int step = scores_role ? kScoreGroups : kExpandGroups - kScoreGroups;
+    // Unit k: place p of tile n, in stage st, whose ring has come round `round` times; its buffer.
+    int k = scores_role ? grp : grp - kScoreGroups;
+    int n = 0, p = k, st = 0, round = 0, buf = k % BUFS;
+    auto settle = [&]() {
+#pragma unroll 1
+      while (p >= U) {
+        p -= U;
+        ++n;
+        if (++st == L.stages) { st = 0; ++round; }
+      }
     };
+    auto advance = [&]() {
+      k += step;
+      p += step;
+      settle();
+      buf += step;
 #pragma unroll 1
-    while (p >= U) { p -= U; next_tile(); }
+      while (buf >= BUFS) buf -= BUFS;
+    };
+    settle();
+    if (scores_role) {
+      const int slot = q * 32 + lane, row = slot & 63;
+      int seg = -1, v = qp::find_wide(prefix, n_groups, g0), next_start = 0;
 #pragma unroll 1
-    for (int k = grp; k < n_units + U; k += kExpandGroups) {
-      if (k < n_units) {
+      for (; k < n_units; advance()) {
         if (__builtin_expect(n >= next_start, 0)) {
           int start;
           do {
@@ -357,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
             next_start = prefix[v + 1] - g0;
             ++seg;
           } while (n >= next_start);
-          if (n == start && p < QW / 4) {
+          if (n == start && p < kScoreGroups) {
             const int4 group = a.groups[v];
             ok = qp::put_queries<NC, QW, QB, QV>(static_cast<const bf16*>(a.q) + (long long)group.y * (r + dr),
                                                  sm + L.off_q, misc, a.scale_log2, group.z, f, seg, p * 4 + q);
@@ -371,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after_sync();
-        const int s = U == 8 ? 2 * (p & 3) + (p >> 2) : p, c = 2 * s;
+        const int c = 2 * p;
         if (c < chunks) {
           const TileInfo& info = misc->info[n % kInfo];
           const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
@@ -409,33 +424,23 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(bar(misc->as_full[k % kUnitRing]));
-          if (U != 8) mbar_arrive(bar(misc->scale_full[st]));
+          mbar_arrive(bar(misc->scale_full[st]));
           mbar_arrive(bar(misc->code_empty[st]));
         }
       }
-      const int kv = k - U;
-      if (kv >= 0) {
-        const int mb = U == 8 ? p & 3 : p >> 1, h = U == 8 ? p >> 2 : p & 1, c = mb * 4 + q;
-        const int stv = st == 0 ? L.stages - 1 : st - 1, roundv = st == 0 ? round - 1 : round;
-        // With eight units a tile the scales are this group's own: that unit k - BUFS has been used tells that its
-        // four warps have written those of unit k - 4 and before; behind the last tile only the units' own
-        // barriers do.
-        ok = kv < BUFS || wait(misc->av_empty[(kv - BUFS) % kUnitRing], (kv - BUFS) / kUnitRing);
-        if (U == 8) {
-          if (k >= n_units && p < 4)
-            ok = ok && wait(misc->as_full[kv % kUnitRing], kv / kUnitRing) &&
-                 wait(misc->as_full[(kv + 4) % kUnitRing], (kv + 4) / kUnitRing);
-        } else {
-          ok = ok && wait(misc->code_full[stv], roundv) && wait(misc->scale_full[stv], roundv);
-        }
+    } else {
+#pragma unroll 1
+      for (; k < n_units; advance()) {
+        const int mb = p % NB, h = p / NB, c = mb * 4 + q;
+        ok = (k < BUFS || wait(misc->av_empty[(k - BUFS) % kUnitRing], (k - BUFS) / kUnitRing)) &&
+             wait(misc->scale_full[st], round);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after_sync();
         if (c < chunks) {
-          const uint32_t from = base + L.off_codes + stv * L.stage + (h * 64 + lane) * code_row + ((uint32_t)(c * 16) ^ twist);
-          const uint32_t sc_at = st_u32 + stv * L.scale_room + c * (kTile * 2) + h * 128 + 4 * t;
-          // Value units are numbered from the tile before, so their buffer is that of unit kv.
-          const uint32_t col = lane_tm + T::kColAv + (kv % BUFS) * 32;
+          const uint32_t from = base + L.off_codes + st * L.stage + (h * 64 + lane) * code_row + ((uint32_t)(c * 16) ^ twist);
+          const uint32_t sc_at = st_u32 + st * L.scale_room + c * (kTile * 2) + h * 128 + 4 * t;
+          const uint32_t col = lane_tm + T::kColAv + buf * 32;
           uint32_t w[2][4];
           qp::ldsm_x4_trans(from, w[0]);
           qp::ldsm_x4_trans(from + 32 * code_row, w[1]);
@@ -459,15 +464,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(bar(misc->av_full[kv % kUnitRing]));
-          mbar_arrive(bar(misc->code_empty[stv]));
+          mbar_arrive(bar(misc->av_full[k % kUnitRing]));
+          mbar_arrive(bar(misc->code_empty[st]));
         }
       }
-      p += kExpandGroups;
-#pragma unroll 1
-      while (p >= U) { p -= U; next_tile(); }
-      buf += kExpandGroups % BUFS;
-      if (buf >= BUFS) buf -= BUFS;
     }
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
