@@ -235,6 +235,11 @@ __device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void* src, ui
       : "memory");
 }
 
+// Asks for a run of bytes to be brought into L2; address and size multiples of 16.
+__device__ __forceinline__ void prefetch_l2(const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(src)), "r"(bytes) : "memory");
+}
+
 // ---- tensor memory ---------------------------------------------------------------------
 
 // Whole-warp calls.  `columns` is a power of two >= 32; the base address lands in *dst_smem.

@@ -30,7 +30,7 @@ constexpr int kIssueRegs = 40, kExpandRegs = 64, kSoftmaxRegs = 104;
 constexpr int kRoleRegisters = 4 * kIssueRegs + 16 * kExpandRegs + 8 * kSoftmaxRegs;
 static_assert(kRoleRegisters <= 72 * (kThreads / 32), "more than 72 registers a thread are not there for 896 threads");
 constexpr int kQRing = qp::tc::kQRing, kInfo = 16, kUnitRing = 8, kMaxStages = 4;
-constexpr float kShift = qp::tc::kShift, kRescale = qp::tc::kRescale, kUnset = qp::tc::kUnset;
+constexpr float kShift = qp::tc::kShift, kRescale = qp::tc::kRescale;
 constexpr int kFoldTiles = qp::tc::kFoldTiles;
 constexpr int kFirst = 1, kLast = 2, kFold = 4, kFolded = 8, kFoldedNow = 16, kEnds = 32, kSegShift = 6;
 
@@ -64,7 +64,7 @@ struct Misc {
   alignas(16) float neg_ref[64];
   alignas(16) float unit[64];
   float next_unit[kQRing][64];
-  float fac[64];
+  float fac[64], down[64];
   float red[8][32];
   float m_fold[64];
 };
@@ -202,7 +202,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           if (!ok) break;
           TileInfo& info = misc->info[n % kInfo];
           seg += first;
-          if (first) begun = n;
+          if (first) {
+            begun = n;
+            if (v_end < g1) {                            // the next group's queries, into L2
+              const int4 next = a.groups[v + 1];
+              prefetch_l2(static_cast<const bf16*>(a.q) + (long long)next.y * (r + dr), next.z * (r + dr) * 2);
+            }
+          }
           const int before = n - begun;
           info.group = v;
           info.flags = (first ? kFirst : 0) | (last ? kLast : 0) | (ends ? kEnds : 0) |
@@ -379,14 +385,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
             if (!ok) break;
           }
         }
-        // The buffer first: that the unit which had it has been used also tells that the stage's phase is the
-        // one before this tile's or later, which its parity alone would not.
-        ok = (k < BUFS || wait(misc->as_empty[(k - BUFS) % kUnitRing], (k - BUFS) / kUnitRing)) &&
-             wait(misc->code_full[st], round);
-        ok = __all_sync(0xffffffffu, ok);
+        // The unit is decoded into registers before its buffer is waited for.  (The stage's phase is the one before
+        // this tile's or later, which its parity alone would not tell: the wait for the buffer of this group's
+        // unit before has seen a unit used that is at most three tiles older than this one, and there are four
+        // stages wherever a tile has fewer than six units.)
+        ok = __all_sync(0xffffffffu, wait(misc->code_full[st], round));
         if (!ok) break;
-        tc_fence_after_sync();
         const int c = 2 * p;
+        uint32_t x[32];
         if (c < chunks) {
           const TileInfo& info = misc->info[n % kInfo];
           const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
@@ -395,7 +401,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           // The scales also go out as half precision, a group's 128 slots in a row, for the value units;
           // zero where there is no slot, so that whatever its codes are, the product is zero.
           const uint32_t st_out = st_u32 + st * L.scale_room + slot * 2 + c * (kTile * 2);
-          const uint32_t at = lane_tm + T::kColAs + buf * 32;
           const uint4 w0 = qp::lds128(codes + ((uint32_t)(c * 16) ^ twist));
           const uint4 w1 = qp::lds128(codes + ((uint32_t)(c * 16 + 16) ^ twist));
           uint32_t two;
@@ -407,66 +412,74 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           const uint32_t sc0 = __byte_perm(s01, 0, 0x1010), sc1 = __byte_perm(s01, 0, 0x3232);
           const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t x[16];
+          for (int i = 0; i < 8; ++i) {
+            uint32_t o[4];
+            qp::decode8(word[i], o);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t o[4];
-              qp::decode8(word[4 * half + i], o);
-#pragma unroll
-              for (int m = 0; m < 4; ++m) x[4 * i + m] = qp::mul_h2(o[m], half ? sc1 : sc0);
-            }
-            tmem_st_x16(at + half * 16, x);
+            for (int m = 0; m < 4; ++m) x[4 * i + m] = qp::mul_h2(o[m], i < 4 ? sc0 : sc1);
           }
         }
-        tmem_wait_st();
-        tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(bar(misc->as_full[k % kUnitRing]));
           mbar_arrive(bar(misc->scale_full[st]));
           mbar_arrive(bar(misc->code_empty[st]));
         }
+        if (k >= BUFS) {
+          ok = __all_sync(0xffffffffu, wait(misc->as_empty[(k - BUFS) % kUnitRing], (k - BUFS) / kUnitRing));
+          if (!ok) break;
+          tc_fence_after_sync();
+        }
+        if (c < chunks) tmem_st_x32(lane_tm + T::kColAs + buf * 32, x);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(misc->as_full[k % kUnitRing]));
       }
     } else {
 #pragma unroll 1
       for (; k < n_units; advance()) {
         const int mb = p % NB, h = p / NB, c = mb * 4 + q;
-        ok = (k < BUFS || wait(misc->av_empty[(k - BUFS) % kUnitRing], (k - BUFS) / kUnitRing)) &&
-             wait(misc->scale_full[st], round);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, wait(misc->scale_full[st], round));
         if (!ok) break;
-        tc_fence_after_sync();
+        uint32_t x[2][4][4];
         if (c < chunks) {
           const uint32_t from = base + L.off_codes + st * L.stage + (h * 64 + lane) * code_row + ((uint32_t)(c * 16) ^ twist);
           const uint32_t sc_at = st_u32 + st * L.scale_room + c * (kTile * 2) + h * 128 + 4 * t;
-          const uint32_t col = lane_tm + T::kColAv + buf * 32;
           uint32_t w[2][4];
           qp::ldsm_x4_trans(from, w[0]);
           qp::ldsm_x4_trans(from + 32 * code_row, w[1]);
 #pragma unroll
-          for (int i2 = 0; i2 < 2; ++i2) {
-            uint32_t x[4][4];
+          for (int i2 = 0; i2 < 2; ++i2)
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
               uint32_t sc;
               asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sc_at + i2 * 64 + m * 16));
-              qp::decode_pairs(w[i2][m], x[m]);
+              qp::decode_pairs(w[i2][m], x[i2][m]);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) x[m][i] = qp::mul_h2(x[m][i], sc);
+              for (int i = 0; i < 4; ++i) x[i2][m][i] = qp::mul_h2(x[i2][m][i], sc);
             }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(misc->code_empty[st]));
+        if (k >= BUFS) {
+          ok = __all_sync(0xffffffffu, wait(misc->av_empty[(k - BUFS) % kUnitRing], (k - BUFS) / kUnitRing));
+          if (!ok) break;
+          tc_fence_after_sync();
+        }
+        if (c < chunks) {
+          const uint32_t col = lane_tm + T::kColAv + buf * 32;
+#pragma unroll
+          for (int i2 = 0; i2 < 2; ++i2) {
+            const uint32_t(&y)[4][4] = x[i2];
             const uint32_t to = col + i2 * 16;
-            tmem_st_16x128_x4(to, x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]);
-            tmem_st_16x128_x4(to + (16u << 16), x[0][2], x[0][3], x[1][2], x[1][3], x[2][2], x[2][3], x[3][2], x[3][3]);
+            tmem_st_16x128_x4(to, y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]);
+            tmem_st_16x128_x4(to + (16u << 16), y[0][2], y[0][3], y[1][2], y[1][3], y[2][2], y[2][3], y[3][2], y[3][3]);
           }
         }
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(bar(misc->av_full[k % kUnitRing]));
-          mbar_arrive(bar(misc->code_empty[st]));
-        }
+        if (lane == 0) mbar_arrive(bar(misc->av_full[k % kUnitRing]));
       }
     }
   } else {
@@ -512,6 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     };
     uint8_t* const p_row = sm + L.off_p + (HO / 8) * P_SBO + slot * 16;
     float l_acc[NHH];
+    bool unset = true;                                   // no slot of the segment yet, hence no reference
     for (int n = 0; n < n_tiles; ++n) {
       if (ok && sw == 3) ok = wait(misc->info_full[n % kInfo], n / kInfo) && wait(misc->s_full[n % SB], n / SB);
       if (named_sync_or<kSoftmaxThreads>(1, !ok)) break;
@@ -525,11 +539,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           const int seg = flags >> kSegShift;
           if (ok) ok = wait(misc->q_full[seg % kQRing], seg / kQRing);       // long since; for the scales
           misc->m_used[sidx] = -INFINITY;
-          misc->neg_ref[sidx] = kUnset;
+          misc->neg_ref[sidx] = 0.f;
           misc->unit[sidx] = sidx < NC ? misc->next_unit[seg % kQRing][sidx] : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < NHH; ++i) l_acc[i] = 0.f;
+        unset = true;
         group_sync();
       }
       // Output sums of the segment, this thread's latent of every block (lane 8j + g of a quarter holds latent
@@ -572,49 +587,59 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         }
         group_sync();                                    // fac may be rewritten
       }
+      // The scores leave tensor memory at once, so that the next tile's products may begin.
       float x[NHH];
       tc_fence_after_sync();
       load_scores(n, x);
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(misc->s_empty[n % SB]));
       const bool live = (slot & 63) < rows, full = __all_sync(0xffffffffu, live);
-      // x = score - reference + shift in log2 units.
-      auto offset_scores = [&]() {
+      // x = score - reference + shift in log2 units; the bare score as long as there is no reference, which the
+      // segment's first slots set.
 #pragma unroll
-        for (int i = 0; i < NHH; i += 4) {
-          const float4 u = *reinterpret_cast<const float4*>(&misc->unit[HO + i]);
-          const float4 o = *reinterpret_cast<const float4*>(&misc->neg_ref[HO + i]);
-          x[i] = fmaf(x[i], u.x, o.x);
-          x[i + 1] = fmaf(x[i + 1], u.y, o.y);
-          x[i + 2] = fmaf(x[i + 2], u.z, o.z);
-          x[i + 3] = fmaf(x[i + 3], u.w, o.w);
-        }
-        if (!full) {                                     // only a sequence's last tile
+      for (int i = 0; i < NHH; i += 4) {
+        const float4 u = *reinterpret_cast<const float4*>(&misc->unit[HO + i]);
+        const float4 o = *reinterpret_cast<const float4*>(&misc->neg_ref[HO + i]);
+        x[i] = fmaf(x[i], u.x, o.x);
+        x[i + 1] = fmaf(x[i + 1], u.y, o.y);
+        x[i + 2] = fmaf(x[i + 2], u.z, o.z);
+        x[i + 3] = fmaf(x[i + 3], u.w, o.w);
+      }
+      if (!full) {                                       // only a sequence's last tile
 #pragma unroll
-          for (int i = 0; i < NHH; ++i) x[i] = live ? x[i] : -INFINITY;
-        }
-      };
-      offset_scores();
+        for (int i = 0; i < NHH; ++i) x[i] = live ? x[i] : -INFINITY;
+      }
       float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < NHH; ++i) top = fmaxf(top, x[i]);
       if (sw == 3 && ok) ok = wait(misc->p_empty[ps], p_round + 1);    // value products of the tile that had it
-      if (named_sync_or<kSoftmaxThreads>(1, top > kShift + kRescale)) {
-        // Rare: some reference has to rise (always at a segment's first tile).
-        load_scores(n, x);
+      if (named_sync_or<kSoftmaxThreads>(1, unset || top > kShift + kRescale)) {
+        // Some reference has to rise: always at a segment's first slots, else rarely.
+        {
+          float y[NHH];
 #pragma unroll
-        for (int i = 0; i < NHH; ++i) x[i] = live ? x[i] * misc->unit[HO + i] : -INFINITY;
-        reduce_columns(x, true);
+          for (int i = 0; i < NHH; ++i) y[i] = x[i];
+          reduce_columns(y, true);
+        }
         group_sync();
         if (sidx < NC) {
-          const float mt = reduced(sidx, true), m_old = misc->m_used[sidx];
-          const float m_new = mt > m_old + kRescale ? mt : m_old;
-          misc->m_used[sidx] = m_new;
-          misc->neg_ref[sidx] = m_new == -INFINITY ? kUnset : kShift - m_new;
-          misc->fac[sidx] = m_new == m_old ? 1.f : exp2f(m_old - m_new);       // 0 from minus infinity
+          // What the column's largest score is above its reference by (from the bare scores: itself).
+          const float mt = reduced(sidx, true) - (unset ? 0.f : kShift), m_old = unset ? 0.f : misc->m_used[sidx];
+          const bool rise = unset ? mt > -INFINITY : mt > kRescale;
+          const float by = rise ? mt : 0.f;
+          misc->m_used[sidx] = unset && !rise ? -INFINITY : m_old + by;
+          misc->neg_ref[sidx] = unset && !rise ? 0.f : kShift - (m_old + by);
+          misc->fac[sidx] = unset ? 0.f : exp2f(-by);
+          misc->down[sidx] = unset ? kShift - by : -by;
         }
         group_sync();
 #pragma unroll
-        for (int i = 0; i < NHH; ++i) l_acc[i] *= misc->fac[HO + i];
-        if (!(flags & (kFirst | kFold))) {
+        for (int i = 0; i < NHH; ++i) {
+          l_acc[i] *= misc->fac[HO + i];
+          x[i] += misc->down[HO + i];
+        }
+        if (!unset && !(flags & kFold)) {
           // O is scaled to the old references: wait for the previous tile's products, rescale.
           if (ok) ok = wait(misc->p_empty[ps1], p_round1);
           ok = __all_sync(0xffffffffu, ok);              // TMEM accesses are whole-warp operations
@@ -634,13 +659,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
             tmem_wait_st();
           }
         }
-        load_scores(n, x);
-        offset_scores();
-        group_sync();                                    // fac / red may be rewritten
+        unset = unset && (info.rows0 | info.rows1) == 0;
+        group_sync();                                    // fac / down / red may be rewritten
       }
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(misc->s_empty[n % SB]));
       // P as the MN-major, un-swizzled B operand: eight columns of a slot are 16 bytes, eight slots
       // follow one another, groups of eight columns are P_SBO apart.
 #pragma unroll
