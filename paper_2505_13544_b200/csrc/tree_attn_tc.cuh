@@ -23,7 +23,6 @@ namespace tree {
 
 constexpr int kTile = 128, kThreads = 896;
 constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kExpandWarp0 = 4;
-constexpr int kExpandGroups = 4, kScoreGroups = 2;
 constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
 // Registers of a thread of the issuing, expanding and softmax warps, and of all warps together.
 constexpr int kIssueRegs = 40, kExpandRegs = 64, kSoftmaxRegs = 104;
@@ -108,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
   constexpr uint32_t IDESC_V = make_idesc_f16(128, NC, 0, 1);
   constexpr uint32_t P_SBO = kTile * 16;        // bytes between groups of 8 columns of a probability tile
   constexpr int U = 2 * NB, SB = T::kScores, BUFS = T::kUnits;
-  constexpr int QW = 4 * kScoreGroups, QB = 2, QV = (NB * 16 + 8 + 31) / 32;
+  constexpr int QW = 8, QB = 2, QV = (NB * 16 + 8 + 31) / 32;
   extern __shared__ uint8_t smem_raw[];
   const qp::Format f = a.f;
   const int r = f.r, dr = f.dr;
@@ -129,8 +128,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     }
     if (i < kMaxStages) {
       mbar_init(bar(misc->code_full[i]), 1);
-      mbar_init(bar(misc->code_empty[i]), 2 * U * 4);            // a warp of every unit
-      mbar_init(bar(misc->scale_full[i]), U * 4);
+      mbar_init(bar(misc->code_empty[i]), 16);                   // the expanding warps
+      mbar_init(bar(misc->scale_full[i]), 8);
       mbar_init(bar(misc->q_full[i]), QW);
       mbar_init(bar(misc->q_empty[i]), 1);
     }
@@ -335,151 +334,139 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     }
   } else if (warp < kSoftmaxWarp0) {
     // ------------------------------------------------------------------ expansion
-    // Groups of four warps, kScoreGroups for the scores' operand, the others for the values', each kind taking its
-    // units in turn: the scores' units then never wait behind a value unit whose buffer waits for the probabilities.
+    // Two groups of four warps for the scores' operand, two for the values', so that the scores' units never wait
+    // behind a value unit whose buffer waits for the probabilities.  Group grp has the units grp, grp + 2, ... of every
+    // tile.  A unit is decoded into registers before its buffer is waited for.  Every wait, arrival and index that
+    // a tile needs once is outside the units' loop: it was a third of all instructions inside (...).
     reg_dealloc<kExpandRegs>();
-    const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2, t = lane & 3;
+    const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2 & 1, t = lane & 3;
     const int cmask = f.code_mask(), chunks = r / qp::kGroup, code_row = f.code_row();
     const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16);
     const uint32_t twist = (uint32_t)(lane & cmask) * 16;       // rows lane, lane + 32, ... twist alike
-    const int n_units = n_tiles * U;
-    const bool scores_role = grp < kScoreGroups;
-    const int step = scores_role ? kScoreGroups : kExpandGroups - kScoreGroups;
-    // Unit k: place p of tile n, in stage st, whose ring has come round `round` times; its buffer.
-    int k = scores_role ? grp : grp - kScoreGroups;
-    int n = 0, p = k, st = 0, round = 0, buf = k % BUFS;
-    auto settle = [&]() {
-#pragma unroll 1
-      while (p >= U) {
-        p -= U;
-        ++n;
-        if (++st == L.stages) { st = 0; ++round; }
-      }
+    int st = 0, round = 0, buf = grp, k = grp;
+    auto next_unit = [&]() {
+      k += 2;
+      buf += 2;
+      if (buf >= BUFS) buf -= BUFS;
     };
-    auto advance = [&]() {
-      k += step;
-      p += step;
-      settle();
-      buf += step;
-#pragma unroll 1
-      while (buf >= BUFS) buf -= BUFS;
+    // The unit that had unit k's buffer has been used; a whole-warp answer.
+    auto buffer_free = [&](unsigned long long* empty) {
+      const int u = k - BUFS;
+      const bool there = u < 0 || mbar_wait_compact(smem_u32(empty) + (u % kUnitRing) * 8, u / kUnitRing & 1);
+      return __all_sync(0xffffffffu, there) != 0;
     };
-    settle();
-    if (scores_role) {
+    if (warp < kExpandWarp0 + 8) {
       const int slot = q * 32 + lane, row = slot & 63;
       int seg = -1, v = qp::find_wide(prefix, n_groups, g0), next_start = 0;
 #pragma unroll 1
-      for (; k < n_units; advance()) {
-        if (__builtin_expect(n >= next_start, 0)) {
-          int start;
-          do {
-            start = next_start;
-            while (prefix[v + 1] <= g0 + start) ++v;
-            next_start = prefix[v + 1] - g0;
-            ++seg;
-          } while (n >= next_start);
-          if (n == start && p < kScoreGroups) {
-            const int4 group = a.groups[v];
-            ok = qp::put_queries<NC, QW, QB, QV>(static_cast<const bf16*>(a.q) + (long long)group.y * (r + dr),
-                                                 sm + L.off_q, misc, a.scale_log2, group.z, f, seg, p * 4 + q);
-            if (!ok) break;
-          }
+      for (int n = 0; n < n_tiles && ok; ++n) {
+        if (n == next_start) {
+          while (prefix[v + 1] <= g0 + n) ++v;
+          next_start = prefix[v + 1] - g0;
+          ++seg;
+          const int4 group = a.groups[v];
+          ok = qp::put_queries<NC, QW, QB, QV>(static_cast<const bf16*>(a.q) + (long long)group.y * (r + dr), sm + L.off_q,
+                                               misc, a.scale_log2, group.z, f, seg, grp * 4 + q);
+          if (!ok) break;
         }
-        // The unit is decoded into registers before its buffer is waited for.  (The stage's phase is the one before
-        // this tile's or later, which its parity alone would not tell: the wait for the buffer of this group's
-        // unit before has seen a unit used that is at most three tiles older than this one, and there are four
-        // stages wherever a tile has fewer than six units.)
         ok = __all_sync(0xffffffffu, wait(misc->code_full[st], round));
         if (!ok) break;
-        const int c = 2 * p;
-        uint32_t x[32];
-        if (c < chunks) {
-          const TileInfo& info = misc->info[n % kInfo];
-          const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
-          const uint32_t stage = base + L.off_codes + st * L.stage;
-          const uint32_t codes = stage + slot * code_row, scales = stage + L.scales + slot * f.scale_row();
-          // The scales also go out as half precision, a group's 128 slots in a row, for the value units;
-          // zero where there is no slot, so that whatever its codes are, the product is zero.
-          const uint32_t st_out = st_u32 + st * L.scale_room + slot * 2 + c * (kTile * 2);
-          const uint4 w0 = qp::lds128(codes + ((uint32_t)(c * 16) ^ twist));
-          const uint4 w1 = qp::lds128(codes + ((uint32_t)(c * 16 + 16) ^ twist));
-          uint32_t two;
-          asm volatile("{\n\t.reg .u16 x;\n\tld.shared.u16 x, [%1];\n\tcvt.u32.u16 %0, x;\n\t}"
-                       : "=r"(two) : "r"(scales + c));
-          const uint32_t s01 = __byte_perm(two, 0, 0x4140) << 7, out = s01 & live;        // both as half precision
-          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out), "h"((uint16_t)out) : "memory");
-          asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + kTile * 2), "h"((uint16_t)(out >> 16)) : "memory");
-          const uint32_t sc0 = __byte_perm(s01, 0, 0x1010), sc1 = __byte_perm(s01, 0, 0x3232);
-          const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+        const TileInfo& info = misc->info[n % kInfo];
+        const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
+        const uint32_t stage = base + L.off_codes + st * L.stage, codes = stage + slot * code_row;
+        uint32_t scale_at = stage + L.scales + slot * f.scale_row() + 2 * grp;
+        uint32_t st_out = st_u32 + st * L.scale_room + slot * 2 + 2 * grp * (kTile * 2);
+        uint32_t code_at = 32 * grp;
+#pragma unroll 1
+        for (int i = 0; i < NB; ++i, next_unit(), scale_at += 4, st_out += 8 * kTile, code_at += 64) {
+          const bool there = code_at < (uint32_t)code_row;       // the last unit of a half block is empty
+          uint32_t x[32];
+          if (there) {
+            const uint4 w0 = qp::lds128(codes + (code_at ^ twist)), w1 = qp::lds128(codes + ((code_at + 16) ^ twist));
+            uint32_t two;
+            asm volatile("{\n\t.reg .u16 x;\n\tld.shared.u16 x, [%1];\n\tcvt.u32.u16 %0, x;\n\t}"
+                         : "=r"(two) : "r"(scale_at));
+            // The scales also go out as half precision, a group's 128 slots in a row, for the value units;
+            // zero where there is no slot, so that whatever its codes are, the product is zero.
+            const uint32_t s01 = __byte_perm(two, 0, 0x4140) << 7, out = s01 & live;      // both as half precision
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out), "h"((uint16_t)out) : "memory");
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(st_out + kTile * 2), "h"((uint16_t)(out >> 16)) : "memory");
+            const uint32_t sc0 = __byte_perm(s01, 0, 0x1010), sc1 = __byte_perm(s01, 0, 0x3232);
+            const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            uint32_t o[4];
-            qp::decode8(word[i], o);
+            for (int e = 0; e < 8; ++e) {
+              uint32_t o[4];
+              qp::decode8(word[e], o);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) x[4 * i + m] = qp::mul_h2(o[m], i < 4 ? sc0 : sc1);
+              for (int m = 0; m < 4; ++m) x[4 * e + m] = qp::mul_h2(o[m], e < 4 ? sc0 : sc1);
+            }
           }
+          ok = buffer_free(misc->as_empty);
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (there) tmem_st_x32(lane_tm + T::kColAs + buf * 32, x);
+          tmem_wait_st();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(misc->as_full) + k % kUnitRing * 8);
         }
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(bar(misc->scale_full[st]));
           mbar_arrive(bar(misc->code_empty[st]));
         }
-        if (k >= BUFS) {
-          ok = __all_sync(0xffffffffu, wait(misc->as_empty[(k - BUFS) % kUnitRing], (k - BUFS) / kUnitRing));
-          if (!ok) break;
-          tc_fence_after_sync();
-        }
-        if (c < chunks) tmem_st_x32(lane_tm + T::kColAs + buf * 32, x);
-        tmem_wait_st();
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc->as_full[k % kUnitRing]));
+        if (++st == L.stages) { st = 0; ++round; }
       }
     } else {
+      // Place p of a tile: block p % NB of 128 latents, half p / NB of the slots.
 #pragma unroll 1
-      for (; k < n_units; advance()) {
-        const int mb = p % NB, h = p / NB, c = mb * 4 + q;
+      for (int n = 0; n < n_tiles && ok; ++n) {
         ok = __all_sync(0xffffffffu, wait(misc->scale_full[st], round));
         if (!ok) break;
-        uint32_t x[2][4][4];
-        if (c < chunks) {
-          const uint32_t from = base + L.off_codes + st * L.stage + (h * 64 + lane) * code_row + ((uint32_t)(c * 16) ^ twist);
-          const uint32_t sc_at = st_u32 + st * L.scale_room + c * (kTile * 2) + h * 128 + 4 * t;
-          uint32_t w[2][4];
-          qp::ldsm_x4_trans(from, w[0]);
-          qp::ldsm_x4_trans(from + 32 * code_row, w[1]);
+        const uint32_t rows_at = base + L.off_codes + st * L.stage + lane * code_row;
+        const uint32_t scale_at = st_u32 + st * L.scale_room + 4 * t;
+#pragma unroll 1
+        for (int i = 0; i < NB; ++i, next_unit()) {
+          const int p = 2 * i + grp, h = p >= NB ? 1 : 0, c = (p - h * NB) * 4 + q;
+          uint32_t x[2][4][4];
+          if (c < chunks) {
+            const uint32_t from = rows_at + h * 64 * code_row + ((uint32_t)(c * 16) ^ twist);
+            const uint32_t sc_at = scale_at + c * (kTile * 2) + h * 128;
+            uint32_t w[2][4];
+            qp::ldsm_x4_trans(from, w[0]);
+            qp::ldsm_x4_trans(from + 32 * code_row, w[1]);
 #pragma unroll
-          for (int i2 = 0; i2 < 2; ++i2)
+            for (int i2 = 0; i2 < 2; ++i2)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-              uint32_t sc;
-              asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sc_at + i2 * 64 + m * 16));
-              qp::decode_pairs(w[i2][m], x[i2][m]);
+              for (int m = 0; m < 4; ++m) {
+                uint32_t sc;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sc_at + i2 * 64 + m * 16));
+                qp::decode_pairs(w[i2][m], x[i2][m]);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) x[i2][m][i] = qp::mul_h2(x[i2][m][i], sc);
+                for (int e = 0; e < 4; ++e) x[i2][m][e] = qp::mul_h2(x[i2][m][e], sc);
+              }
+          }
+          ok = buffer_free(misc->av_empty);
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (c < chunks) {
+            const uint32_t col = lane_tm + T::kColAv + buf * 32;
+#pragma unroll
+            for (int i2 = 0; i2 < 2; ++i2) {
+              const uint32_t(&y)[4][4] = x[i2];
+              const uint32_t to = col + i2 * 16;
+              tmem_st_16x128_x4(to, y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]);
+              tmem_st_16x128_x4(to + (16u << 16), y[0][2], y[0][3], y[1][2], y[1][3], y[2][2], y[2][3], y[3][2], y[3][3]);
             }
+          }
+          tmem_wait_st();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(misc->av_full) + k % kUnitRing * 8);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(misc->code_empty[st]));
-        if (k >= BUFS) {
-          ok = __all_sync(0xffffffffu, wait(misc->av_empty[(k - BUFS) % kUnitRing], (k - BUFS) / kUnitRing));
-          if (!ok) break;
-          tc_fence_after_sync();
-        }
-        if (c < chunks) {
-          const uint32_t col = lane_tm + T::kColAv + buf * 32;
-#pragma unroll
-          for (int i2 = 0; i2 < 2; ++i2) {
-            const uint32_t(&y)[4][4] = x[i2];
-            const uint32_t to = col + i2 * 16;
-            tmem_st_16x128_x4(to, y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]);
-            tmem_st_16x128_x4(to + (16u << 16), y[0][2], y[0][3], y[1][2], y[1][3], y[2][2], y[2][3], y[3][2], y[3][3]);
-          }
-        }
-        tmem_wait_st();
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc->av_full[k % kUnitRing]));
+        if (++st == L.stages) { st = 0; ++round; }
       }
     }
   } else {
