@@ -60,6 +60,7 @@ struct AttnArgs {
   const int* n_groups;
   const int* prefix;
   const int4* groups;
+  const uint8_t* image;      // the groups' queries as the tensor-core kernel wants them
   int cols;
 };
 

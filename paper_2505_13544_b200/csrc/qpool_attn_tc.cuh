@@ -156,8 +156,8 @@ struct Layout {
 // by the power of two that brings its largest element into [2^14, 2^15); heads that do not exist are
 // zero.  As a kernel of its own in front, with the image loaded from memory, this took 1 to 2.5 us more of
 // a small batch's 15 to 19.  Not inlined: the loop that calls it once a segment is short of registers.
-template <int NHP, int QW, int QB, int QV, typename Misc>
-__device__ __noinline__ bool put_queries(const bf16* q, uint8_t* image, Misc* misc, float scale_log2, int n_heads,
+template <int NHP, int QW, int QB, int QV>
+__device__ __noinline__ bool put_queries(const bf16* q, uint8_t* image, tc::Misc* misc, float scale_log2, int n_heads,
                                          Format f, int seg, int first_head) {
   using namespace tc;
   const int r = f.r, dr = f.dr, lane = threadIdx.x & 31;

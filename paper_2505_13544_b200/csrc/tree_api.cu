@@ -6,8 +6,8 @@
 #include "common.cuh"
 #include "ops_common.cuh"
 #include "qpool_attn.cuh"
-#include "tree_attn_tc.cuh"
 #include "tree_kernels.cuh"
+#include "tree_attn_tc.cuh"
 
 using namespace mtla;
 using namespace mtla::ops;
@@ -18,7 +18,7 @@ constexpr int kMostCtas = 2 * kPlanSms;          // of the launch over the conte
 constexpr int kLeastCols = 16, kMostCols = 64;   // of a group
 
 // Sized for any group width, so that the choice between the kernels stays the call's.
-struct TreePlan { size_t o_part, ml_part, parts, groups, prefix, first, n_groups, error_words, total; };
+struct TreePlan { size_t o_part, ml_part, parts, groups, prefix, first, n_groups, error_words, image, total; };
 long long most_groups(const mtla_qpool_config* c, int B, int n_nodes, int cols) {
   return (long long)n_nodes * c->n_heads / cols + (B < n_nodes ? B : n_nodes);
 }
@@ -42,7 +42,13 @@ TreePlan plan_tree(const mtla_qpool_config* c, int B, int n_nodes) {
   p.first = p.prefix + align_up((groups + 1) * 4, 256);
   p.n_groups = p.first + align_up(((size_t)B + 1) * 4, 256);
   p.error_words = p.n_groups + 256;
-  p.total = p.error_words + align_up(kPlanSms * 4, 256);
+  p.image = p.error_words + align_up(kPlanSms * 4, 256);
+  size_t image = 0;
+  for (int w = 32; w <= kMostCols; w *= 2) {
+    const size_t n = (size_t)most_groups(c, B, n_nodes, w) * tree::image_bytes(w, format_of(c));
+    if (n > image) image = n;
+  }
+  p.total = p.image + align_up(image, 256);
   return p;
 }
 
@@ -175,7 +181,14 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   pa.width = table_width;
   pa.cols = cols;
   pa.tile_pages = tensor ? 2 : 1;
-  int status = launch_dependent(tree::tree_plan_kernel, dim3(1), tree::kPlanThreads, 0, st, pa);
+  pa.q = static_cast<const bf16*>(q);
+  pa.image = tensor ? reinterpret_cast<uint8_t*>(ws + p.image) : nullptr;
+  pa.scale_log2 = (float)((double)scale * kLog2e);
+  pa.f = format_of(cfg);
+  const long long groups = most_groups(cfg, B, n_nodes, cols), images = tensor ? groups : 0;
+  const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
+  int status = launch_dependent(tree::tree_plan_kernel, dim3(1 + (unsigned)(images < 2 * sms ? images : 2 * sms)),
+                                tree::kPlanThreads, 0, st, pa);
   if (status != MTLA_OK) return status;
 
   qp::AttnArgs a = {};
@@ -186,17 +199,17 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   a.ml_part = reinterpret_cast<float*>(ws + p.ml_part);
   a.seq_parts = reinterpret_cast<int2*>(ws + p.parts);
   a.error_words = reinterpret_cast<int*>(ws + p.error_words);
-  a.scale_log2 = (float)((double)scale * kLog2e);
+  a.scale_log2 = pa.scale_log2;
   a.n_heads = cfg->n_heads;
   a.width = table_width;
   a.n_pages = cfg->n_pages;
-  a.f = format_of(cfg);
+  a.f = pa.f;
+  a.image = pa.image;
   a.n_groups = pa.n_groups;
   a.prefix = pa.prefix;
   a.groups = pa.groups;
   a.cols = cols;
-  const long long tiles = most_groups(cfg, B, n_nodes, cols) * ceil_div(table_width, pa.tile_pages);
-  const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
+  const long long tiles = groups * ceil_div(table_width, pa.tile_pages);
   if (tensor)
     status = cols == 64 ? launch_context_tc<64>(a, tiles, dev, st) : launch_context_tc<32>(a, tiles, dev, st);
   else

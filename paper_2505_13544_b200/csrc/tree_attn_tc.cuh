@@ -12,22 +12,24 @@
 //
 // Groups of columns take the place of sequences; a group's result is always a part (reference, denominator, sums in 32
 // bits) that tree_join_kernel joins with the drafted rows.  Roles (28 warps): warp 0 issues the score products, warp 1
-// the value products, warp 2 is the producer; warps 4-19 expand in four groups that take units in turn and write the
-// queries; warps 20-27 are softmax and epilogue.  Every wait is bounded as there.
+// the value products, warp 2 is the producer; warp 3 fetches the queries; warps 4-11
+// expand for the scores, warps 12-19 for the values (and write the results); warps 20-27 are softmax.  Every wait is bounded as there.
 #pragma once
 
 #include "qpool_attn_tc.cuh"
+#include "tree_kernels.cuh"
 
 namespace mtla {
 namespace tree {
 
 constexpr int kTile = 128, kThreads = 896;
-constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kExpandWarp0 = 4;
+constexpr int kScoreIssuer = 0, kValueIssuer = 1, kProducerWarp = 2, kQueryWarp = 3;
+constexpr int kScoreWarp0 = 4, kScoreWarps = 8, kValueWarp0 = 12, kValueWarps = 8;
 constexpr int kSoftmaxWarp0 = 20, kSoftmaxThreads = 256, kSoftmaxWarps = 8;
 // Registers of a thread of the issuing, expanding and softmax warps, and of all warps together.
 constexpr int kIssueRegs = 40, kExpandRegs = 64, kSoftmaxRegs = 104;
-constexpr int kRoleRegisters = 4 * kIssueRegs + 16 * kExpandRegs + 8 * kSoftmaxRegs;
-static_assert(kRoleRegisters <= 72 * (kThreads / 32), "more than 72 registers a thread are not there for 896 threads");
+constexpr int kRoleRegisters = 4 * kIssueRegs + (kScoreWarps + kValueWarps) * kExpandRegs + 8 * kSoftmaxRegs;
+static_assert(kRoleRegisters <= 72 * (kThreads / 32), "there are 72 registers for each of 896 threads");
 constexpr int kQRing = qp::tc::kQRing, kInfo = 16, kUnitRing = 8, kMaxStages = 4;
 constexpr float kShift = qp::tc::kShift, kRescale = qp::tc::kRescale;
 constexpr int kFoldTiles = qp::tc::kFoldTiles;
@@ -53,8 +55,9 @@ struct Misc {
   unsigned long long code_full[kMaxStages], code_empty[kMaxStages], scale_full[kMaxStages];
   unsigned long long key_full[2], key_empty[2];
   unsigned long long as_full[kUnitRing], as_empty[kUnitRing], av_full[kUnitRing], av_empty[kUnitRing];
-  unsigned long long s_full[2], s_empty[2], p_full[2], p_empty[2];
+  unsigned long long s_full[2], s_empty[2], p_full[4], p_empty[4];       // a probability tile: each half of the slots
   unsigned long long q_full[kQRing], q_empty[kQRing];
+  unsigned long long end_full[2], o_full[2], o_empty;
   unsigned long long info_full[kInfo];
   uint32_t tmem_base;
   int abort_word;
@@ -62,12 +65,12 @@ struct Misc {
   float m_used[64];
   alignas(16) float neg_ref[64];
   alignas(16) float unit[64];
-  float next_unit[kQRing][64];
+  alignas(16) float next_unit[kQRing][64];
   float fac[64], down[64];
   float red[8][32];
-  float m_fold[64];
+  float m_fold[64], end_fac[2][64];
 };
-constexpr int kMiscBytes = 5120;
+constexpr int kMiscBytes = 5632;
 static_assert(sizeof(Misc) <= kMiscBytes, "misc region too small");
 
 struct Layout {
@@ -99,6 +102,31 @@ struct Layout {
   }
 };
 
+// A segment's output sums, this thread's latent of every block (lane 8j + g of a quarter holds latent 4g + j), into
+// the segment's part [NC][r], shared out among STEP groups of four warps in pieces of 16 columns of a block: added to
+// what has been set down there, which `fac` brings to the present references, or without `add` as they are.
+template <int NC, int NB, int STEP>
+__device__ __forceinline__ void set_down(float* part, uint32_t taddr, const float* fac, bool add, int cols, int r, int lat,
+                                         int grp) {
+#pragma unroll 1
+  for (int i = grp; i < NB * (NC / 16); i += STEP) {
+    const int mb = i / (NC / 16), c0 = i % (NC / 16) * 16, row = mb * 128 + lat;
+    uint32_t o[16];
+    ptx::tmem_ld_x16(taddr + mb * NC + c0, o);
+    ptx::tmem_wait_ld();
+    if (row >= r) continue;
+    float* dst = part + c0 * r + row;
+    if (add) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (c0 + j < cols) o[j] = __float_as_uint(fmaf(dst[j * r], fac[c0 + j], __uint_as_float(o[j])));
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j, dst += r)
+      if (c0 + j < cols) *dst = __uint_as_float(o[j]);
+  }
+}
+
 template <int NC, int NB>
 __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArgs a, Layout L) {
   using namespace ptx;
@@ -107,7 +135,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
   constexpr uint32_t IDESC_V = make_idesc_f16(128, NC, 0, 1);
   constexpr uint32_t P_SBO = kTile * 16;        // bytes between groups of 8 columns of a probability tile
   constexpr int U = 2 * NB, SB = T::kScores, BUFS = T::kUnits;
-  constexpr int QW = 8, QB = 2, QV = (NB * 16 + 8 + 31) / 32;
   extern __shared__ uint8_t smem_raw[];
   const qp::Format f = a.f;
   const int r = f.r, dr = f.dr;
@@ -127,10 +154,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       mbar_init(bar(misc->av_empty[i]), 1);
     }
     if (i < kMaxStages) {
+      mbar_init(bar(misc->p_full[i]), kSoftmaxWarps / 2);
+      mbar_init(bar(misc->p_empty[i]), 1);
       mbar_init(bar(misc->code_full[i]), 1);
-      mbar_init(bar(misc->code_empty[i]), 16);                   // the expanding warps
-      mbar_init(bar(misc->scale_full[i]), 8);
-      mbar_init(bar(misc->q_full[i]), QW);
+      mbar_init(bar(misc->code_empty[i]), kScoreWarps + kValueWarps);
+      mbar_init(bar(misc->scale_full[i]), kScoreWarps);
+      mbar_init(bar(misc->q_full[i]), 1);
       mbar_init(bar(misc->q_empty[i]), 1);
     }
     if (i < 2) {
@@ -138,9 +167,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       mbar_init(bar(misc->key_empty[i]), 1);
       mbar_init(bar(misc->s_full[i]), 1);
       mbar_init(bar(misc->s_empty[i]), kSoftmaxWarps);
-      mbar_init(bar(misc->p_full[i]), kSoftmaxWarps);
-      mbar_init(bar(misc->p_empty[i]), 1);
+      mbar_init(bar(misc->end_full[i]), kSoftmaxWarps);
+      mbar_init(bar(misc->o_full[i]), 1);
     }
+    if (i == 0) mbar_init(bar(misc->o_empty), kValueWarps);
     if (i == 0) misc->abort_word = 0;
     mbar_fence_init();
   }
@@ -172,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
 
   if (n_tiles == 0) {
     // nothing to do; the CTA falls through to the common end
-  } else if (warp < kExpandWarp0) {
+  } else if (warp < kScoreWarp0) {
     reg_dealloc<kIssueRegs>();
     if (warp == kProducerWarp) {
       // ---------------------------------------------------------------- producer
@@ -201,13 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           if (!ok) break;
           TileInfo& info = misc->info[n % kInfo];
           seg += first;
-          if (first) {
-            begun = n;
-            if (v_end < g1) {                            // the next group's queries, into L2
-              const int4 next = a.groups[v + 1];
-              prefetch_l2(static_cast<const bf16*>(a.q) + (long long)next.y * (r + dr), next.z * (r + dr) * 2);
-            }
-          }
+          if (first) begun = n;
           const int before = n - begun;
           info.group = v;
           info.flags = (first ? kFirst : 0) | (last ? kLast : 0) | (ends ? kEnds : 0) |
@@ -243,6 +267,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           for (int i = 0; i < 2; ++i)
             if (rows[i]) bulk_load(key_dst + i * qp::kPageRows * f.key_row(), src[i] + f.off_keys(), rows[i] * f.key_row(), key_bar);
           if (++st == L.stages) { st = 0; ++round; }
+        }
+      }
+    } else if (warp == kQueryWarp) {
+      // ---------------------------------------------------------------- queries of every segment
+      int v = qp::find_wide(prefix, n_groups, g0);
+      if (lane == 0) {
+        for (int seg = 0, g = g0; g < g1; ++seg) {
+          while (prefix[v + 1] <= g) ++v;
+          ok = seg == 0 || wait(misc->q_empty[(seg - 1) % kQRing], (seg - 1) / kQRing);
+          if (!ok) break;
+          const uint8_t* src = a.image + (long long)v * image_bytes(NC, f);
+          const uint32_t full = bar(misc->q_full[seg % kQRing]), rows = NC * 2 * (r + dr);
+          mbar_arrive_expect_tx(full, rows + NC * 4);
+          bulk_load(q_u32, src, rows, full);
+          bulk_load(smem_u32(misc->next_unit[seg % kQRing]), src + rows, NC * 4, full);
+          g = prefix[v + 1];
         }
       }
     } else if (warp == kScoreIssuer) {
@@ -307,14 +347,26 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       int buf = 0;
       for (int n = 0; n < n_tiles && ok; ++n) {
         const int ps = L.p_stages == 2 ? n & 1 : 0, p_round = L.p_stages == 2 ? n >> 1 : n;
-        ok = wait_warp(misc->p_full[ps], p_round);
+        ok = wait_warp(misc->p_full[2 * ps], p_round);
         if (!ok) break;
         tc_fence_after_sync();
-        const uint32_t fresh = (misc->info[n % kInfo].flags & (kFirst | kFold)) != 0;
+        const int flags = misc->info[n % kInfo].flags, seg = flags >> kSegShift;
+        const uint32_t fresh = (flags & (kFirst | kFold)) != 0;
+        if ((flags & kFirst) && seg > 0) {               // the segment before has left the accumulators
+          ok = wait_warp(misc->o_empty, seg - 1);
+          if (!ok) break;
+          tc_fence_after_sync();
+        }
         const uint32_t pd = (uint32_t)p_desc + ps * (L.p_bytes / 16), hi = (uint32_t)(p_desc >> 32);
 #pragma unroll 1
         for (int p = 0; p < U; ++p) {
-          const int k = n * U + p, mb = p % NB, h = p / NB;
+          const int k = n * U + p, h = p >= NB ? 1 : 0, mb = p - h * NB;
+          if (p == NB) {                                 // the first half's products are issued
+            if (elect_one()) mma_commit(bar(misc->p_empty[2 * ps]));
+            __syncwarp();
+            ok = wait_warp(misc->p_full[2 * ps + 1], p_round);
+            if (!ok) break;
+          }
           ok = wait_warp(misc->av_full[k % kUnitRing], k / kUnitRing);
           if (!ok) break;
           tc_fence_after_sync();
@@ -328,47 +380,42 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           __syncwarp();
           if (++buf == BUFS) buf = 0;
         }
-        if (ok && elect_one()) mma_commit(bar(misc->p_empty[ps]));
+        if (ok && elect_one()) {
+          mma_commit(bar(misc->p_empty[2 * ps + 1]));
+          if (flags & kLast) mma_commit(bar(misc->o_full[seg & 1]));
+        }
         __syncwarp();
       }
     }
   } else if (warp < kSoftmaxWarp0) {
     // ------------------------------------------------------------------ expansion
-    // Two groups of four warps for the scores' operand, two for the values', so that the scores' units never wait
-    // behind a value unit whose buffer waits for the probabilities.  Group grp has the units grp, grp + 2, ... of every
-    // tile.  A unit is decoded into registers before its buffer is waited for.  Every wait, arrival and index that
-    // a tile needs once is outside the units' loop: it was a third of all instructions inside (...).
+    // Groups of four warps, two for the scores' operand and three for the values', which takes longer, so that the
+    // scores' units never wait behind a value unit whose buffer waits for the probabilities.  A group takes every second
+    // (third) unit; it is decoded into registers before its buffer is waited for.  What a tile needs once, waits,
+    // arrivals and addresses, is outside the units' loop: inside, it was a third of all instructions.
     reg_dealloc<kExpandRegs>();
-    const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2 & 1, t = lane & 3;
-    const int cmask = f.code_mask(), chunks = r / qp::kGroup, code_row = f.code_row();
+    constexpr int VG = kValueWarps / 4;
+    const bool scores_role = warp < kValueWarp0;
+    const int q = warp & 3, grp = (warp - (scores_role ? kScoreWarp0 : kValueWarp0)) >> 2, t = lane & 3;
+    const int chunks = r / qp::kGroup, code_row = f.code_row();
     const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16);
-    const uint32_t twist = (uint32_t)(lane & cmask) * 16;       // rows lane, lane + 32, ... twist alike
-    int st = 0, round = 0, buf = grp, k = grp;
-    auto next_unit = [&]() {
-      k += 2;
-      buf += 2;
-      if (buf >= BUFS) buf -= BUFS;
-    };
+    const uint32_t twist = (uint32_t)(lane & f.code_mask()) * 16;     // rows lane, lane + 32, ... twist alike
+    int st = 0, round = 0, buf = grp % BUFS, k = grp;
     // The unit that had unit k's buffer has been used; a whole-warp answer.
     auto buffer_free = [&](unsigned long long* empty) {
       const int u = k - BUFS;
       const bool there = u < 0 || mbar_wait_compact(smem_u32(empty) + (u % kUnitRing) * 8, u / kUnitRing & 1);
       return __all_sync(0xffffffffu, there) != 0;
     };
-    if (warp < kExpandWarp0 + 8) {
+    auto next_unit = [&](int step) {
+      k += step;
+      buf += step;
+      if (buf >= BUFS) buf -= BUFS;
+    };
+    if (scores_role) {
       const int slot = q * 32 + lane, row = slot & 63;
-      int seg = -1, v = qp::find_wide(prefix, n_groups, g0), next_start = 0;
 #pragma unroll 1
       for (int n = 0; n < n_tiles && ok; ++n) {
-        if (n == next_start) {
-          while (prefix[v + 1] <= g0 + n) ++v;
-          next_start = prefix[v + 1] - g0;
-          ++seg;
-          const int4 group = a.groups[v];
-          ok = qp::put_queries<NC, QW, QB, QV>(static_cast<const bf16*>(a.q) + (long long)group.y * (r + dr), sm + L.off_q,
-                                               misc, a.scale_log2, group.z, f, seg, grp * 4 + q);
-          if (!ok) break;
-        }
         ok = __all_sync(0xffffffffu, wait(misc->code_full[st], round));
         if (!ok) break;
         const TileInfo& info = misc->info[n % kInfo];
@@ -378,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         uint32_t st_out = st_u32 + st * L.scale_room + slot * 2 + 2 * grp * (kTile * 2);
         uint32_t code_at = 32 * grp;
 #pragma unroll 1
-        for (int i = 0; i < NB; ++i, next_unit(), scale_at += 4, st_out += 8 * kTile, code_at += 64) {
+        for (int i = 0; i < NB; ++i, next_unit(2), scale_at += 4, st_out += 8 * kTile, code_at += 64) {
           const bool there = code_at < (uint32_t)code_row;       // the last unit of a half block is empty
           uint32_t x[32];
           if (there) {
@@ -419,6 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       }
     } else {
       // Place p of a tile: block p % NB of 128 latents, half p / NB of the slots.
+      int p = grp;
 #pragma unroll 1
       for (int n = 0; n < n_tiles && ok; ++n) {
         ok = __all_sync(0xffffffffu, wait(misc->scale_full[st], round));
@@ -426,8 +474,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         const uint32_t rows_at = base + L.off_codes + st * L.stage + lane * code_row;
         const uint32_t scale_at = st_u32 + st * L.scale_room + 4 * t;
 #pragma unroll 1
-        for (int i = 0; i < NB; ++i, next_unit()) {
-          const int p = 2 * i + grp, h = p >= NB ? 1 : 0, c = (p - h * NB) * 4 + q;
+        for (; p < U; p += VG, next_unit(VG)) {
+          const int h = p >= NB ? 1 : 0, c = (p - h * NB) * 4 + q;
           uint32_t x[2][4][4];
           if (c < chunks) {
             const uint32_t from = rows_at + h * 64 * code_row + ((uint32_t)(c * 16) ^ twist);
@@ -464,9 +512,25 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(misc->av_full) + k % kUnitRing * 8);
         }
+        if (!ok) break;
+        p -= U;
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(misc->code_empty[st]));
         if (++st == L.stages) { st = 0; ++round; }
+        const TileInfo& info = misc->info[n % kInfo];
+        if (info.flags & kLast) {
+          // A segment's sums leave tensor memory, while the softmax warps go on.
+          const int seg = info.flags >> kSegShift;
+          ok = __all_sync(0xffffffffu, wait(misc->end_full[seg & 1], seg >> 1) && wait(misc->o_full[seg & 1], seg >> 1));
+          if (!ok) break;
+          tc_fence_after_sync();
+          set_down<NC, NB, VG>(a.o_part + ((long long)blockIdx.x + info.group) * NC * r, lane_tm + T::kColO,
+                               misc->end_fac[seg & 1], info.flags & kFoldedNow, info.cols, r,
+                               q * 32 + 4 * (lane & 7) + (lane >> 3), grp);
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(misc->o_empty));
+        }
       }
     }
   } else {
@@ -480,23 +544,27 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     const int sidx = sw * 32 + lane, slot = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + HO;
     auto group_sync = [&]() { named_sync<1, kSoftmaxThreads>(); };
-    // One value per column over the warp's 32 slots, left in red[sw][i]: halving exchanges, in each of
-    // which a lane keeps half of its columns and adds the partner's share of them.
-    auto reduce_columns = [&](float (&x)[NHH], bool is_max) {
+    // One value per column over the warp's 32 slots, left in red[sw][i], 16 columns at a time: halving exchanges, in
+    // each of which a lane keeps half of its columns and adds the partner's share of them.
+    auto reduce_columns = [&](const float (&x)[NHH], bool is_max) {
       auto join = [&](float c, float d) { return is_max ? fmaxf(c, d) : c + d; };
 #pragma unroll
-      for (int n = NHH, o = 16; n > 1; n >>= 1, o >>= 1) {
-        const bool upper = lane & o;
+      for (int c0 = 0; c0 < NHH; c0 += 16) {
+        float y[16];
 #pragma unroll
-        for (int i = 0; i < n / 2; ++i) {
-          const float keep = upper ? x[i + n / 2] : x[i], give = upper ? x[i] : x[i + n / 2];
-          x[i] = join(keep, __shfl_xor_sync(0xffffffffu, give, o));
+        for (int i = 0; i < 16; ++i) y[i] = x[c0 + i];
+#pragma unroll
+        for (int n = 16, o = 16; n > 1; n >>= 1, o >>= 1) {
+          const bool upper = lane & o;
+#pragma unroll
+          for (int i = 0; i < n / 2; ++i) {
+            const float keep = upper ? y[i + n / 2] : y[i], give = upper ? y[i] : y[i + n / 2];
+            y[i] = join(keep, __shfl_xor_sync(0xffffffffu, give, o));
+          }
         }
+        const float z = join(y[0], __shfl_xor_sync(0xffffffffu, y[0], 1));
+        if (!(lane & 1)) misc->red[sw][c0 + (lane >> 1)] = z;
       }
-      float y = x[0];                                    // column (lane / (32 / NHH)) of the group
-#pragma unroll
-      for (int o = 16 / NHH; o >= 1; o >>= 1) y = join(y, __shfl_xor_sync(0xffffffffu, y, o));
-      if ((lane & (32 / NHH - 1)) == 0) misc->red[sw][lane / (32 / NHH)] = y;
     };
     auto reduced = [&](int h, bool is_max) {
       const float* x = &misc->red[(h / NHH) * 4][h % NHH];
@@ -534,32 +602,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         unset = true;
         group_sync();
       }
-      // Output sums of the segment, this thread's latent of every block (lane 8j + g of a quarter holds latent
-      // 4g + j), into the segment's part: added to what has been set down there, which fac brings to the
-      // present references, or without `add` as they are.
-      auto set_down = [&](bool add) {
-        const int lat = q * 32 + 4 * (lane & 7) + (lane >> 3), cols = info.cols;
-        float* part = a.o_part + ((long long)blockIdx.x + info.group) * a.cols * r;
-#pragma unroll 1
-        for (int i = 0; i < NB * (NHH / 16); ++i) {
-          const int mb = i % NB, ho = HO + i / NB * 16;
-          uint32_t o[16];
-          tmem_ld_x16(lane_base + T::kColO + mb * NC + i / NB * 16, o);
-          tmem_wait_ld();
-          if (mb * 128 + lat >= r) continue;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            if (ho + j >= cols) break;
-            const long long e = (long long)(ho + j) * r + mb * 128 + lat;
-            float x = __uint_as_float(o[j]);
-            if (add) x = fmaf(part[e], misc->fac[ho + j], x);
-            part[e] = x;
-          }
-        }
-      };
       if (__builtin_expect(flags & kFold, 0)) {
         // The sums so far are set down; this tile's products then begin new ones.
-        if (ok) ok = wait(misc->p_empty[ps1], p_round1);
+        if (ok) ok = wait(misc->p_empty[2 * ps1 + 1], p_round1);
         ok = __all_sync(0xffffffffu, ok);
         if (sidx < NC) {
           const float m = misc->m_used[sidx], m_old = misc->m_fold[sidx];
@@ -569,7 +614,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         group_sync();
         if (ok) {
           tc_fence_after_sync();
-          set_down(flags & kFolded);
+          set_down<NC, NB, 2>(a.o_part + ((long long)blockIdx.x + info.group) * NC * r,
+                              tmem + ((uint32_t)(q * 32) << 16) + T::kColO, misc->fac, flags & kFolded, info.cols, r,
+                              q * 32 + 4 * (lane & 7) + (lane >> 3), gr);
           tc_fence_before_sync();
         }
         group_sync();                                    // fac may be rewritten
@@ -600,15 +647,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < NHH; ++i) top = fmaxf(top, x[i]);
-      if (sw == 3 && ok) ok = wait(misc->p_empty[ps], p_round + 1);    // value products of the tile that had it
       if (named_sync_or<kSoftmaxThreads>(1, unset || top > kShift + kRescale)) {
         // Some reference has to rise: always at a segment's first slots, else rarely.
-        {
-          float y[NHH];
-#pragma unroll
-          for (int i = 0; i < NHH; ++i) y[i] = x[i];
-          reduce_columns(y, true);
-        }
+        reduce_columns(x, true);
         group_sync();
         if (sidx < NC) {
           // What the column's largest score is above its reference by (from the bare scores: itself).
@@ -628,7 +669,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         }
         if (!unset && !(flags & kFold)) {
           // O is scaled to the old references: wait for the previous tile's products, rescale.
-          if (ok) ok = wait(misc->p_empty[ps1], p_round1);
+          if (ok) ok = wait(misc->p_empty[2 * ps1 + 1], p_round1);
           ok = __all_sync(0xffffffffu, ok);              // TMEM accesses are whole-warp operations
           if (ok) {
             tc_fence_after_sync();
@@ -649,6 +690,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         unset = unset && (info.rows0 | info.rows1) == 0;
         group_sync();                                    // fac / down / red may be rewritten
       }
+      // The value products of the tile that had this half's place are done.
+      if (ok) ok = wait(misc->p_empty[2 * ps + (q >> 1)], p_round + 1);
       // P as the MN-major, un-swizzled B operand: eight columns of a slot are 16 bytes, eight slots
       // follow one another, groups of eight columns are P_SBO apart.
 #pragma unroll
@@ -667,7 +710,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       fence_proxy_async_smem();
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(misc->p_full[ps]));
+      if (lane == 0) mbar_arrive(bar(misc->p_full[2 * ps + (q >> 1)]));
       if (!(flags & kLast)) continue;
 
       // ---- end of a segment
@@ -680,19 +723,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
             make_float2(m - kShift, reduced(sidx, false));
         if (flags & kFoldedNow) {
           const float m_set = misc->m_fold[sidx];
-          misc->fac[sidx] = m_set == m ? 1.f : exp2f(m_set - m);
+          misc->end_fac[flags >> kSegShift & 1][sidx] = m_set == m ? 1.f : exp2f(m_set - m);
         }
       }
       if (ok && sidx == 0 && (flags & kEnds)) a.seq_parts[v] = make_int2(info.owner + v, (int)blockIdx.x - info.owner + 1);
-      group_sync();
-      if (ok) ok = wait(misc->p_empty[ps], p_round);             // the last value products
-      ok = __all_sync(0xffffffffu, ok);
-      if (ok) {
-        tc_fence_after_sync();
-        set_down(flags & kFoldedNow);
-        tc_fence_before_sync();
-      }
-      group_sync();                                      // fac, unit and the references may be rewritten
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(misc->end_full[flags >> kSegShift & 1]));
+      group_sync();                                      // red, unit and the references may be rewritten
     }
   }
 

@@ -123,14 +123,69 @@ struct PlanArgs {
   int* prefix;               // [groups + 1] tiles before every group
   int* first;                // [batch + 1] first group of every request
   int* n_groups;
+  const bf16* q;             // [n_nodes][heads][r + d_R]
+  uint8_t* image;            // [groups] of image_bytes, or nullptr
+  float scale_log2;
   int batch, n_nodes, heads, width, cols, tile_pages;
+  qp::Format f;
 };
 
 constexpr int kPlanThreads = 1024;
 constexpr int kMaxRequests = 4096;
 
-// One CTA: two prefix sums over the requests (groups, tiles), then a warp per request enters its groups.  A batch
-// whose `starts` do not ascend inside the nodes gets no groups and a count of -1.
+// A group's queries for the tensor-core kernel, as they lie in its shared memory: r / 64 panels [cols][64] half
+// precision with the 128-byte swizzle, one panel [cols][d_R] bf16 (128- or 64-byte swizzle), and what a column's scores
+// are to be multiplied by.
+__host__ __device__ inline int image_bytes(int cols, const qp::Format& f) { return cols * (2 * (f.r + f.dr) + 4); }
+
+// One column into its group's image, by a warp.  The row is scaled by the power of two that brings its largest
+// element into [2^14, 2^15), exactly down to 2^-39 of that; a column that does not exist is zero.
+__device__ __forceinline__ void put_column(const bf16* q, bool there, uint8_t* image, int col, int cols, float scale_log2,
+                                           const qp::Format& f) {
+  const int lane = threadIdx.x & 31, r = f.r, dr = f.dr, n8 = (r + dr) / 8;
+  uint4 w[3];                                    // r + d_R is 576 at most
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int c = lane + 32 * i;
+    w[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (there && c < n8) w[i] = *reinterpret_cast<const uint4*>(q + 8 * c);
+    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+    for (int m = 0; m < 4; ++m) top = max(top, max(x[m] & 0x7fff0000u, (x[m] << 16) & 0x7fff0000u));
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  // Exponents -113 .. 140 (a row of subnormal numbers only reaches less); none for zeros and specials.
+  const bool fine = top > 0 && top < 0x7f800000u;
+  const int e = fine ? 141 - max((int)(top >> 23), 1) : 0, e1 = e / 2, e2 = e - e1;
+  const float f1 = __uint_as_float((127 + e1) << 23), f2 = __uint_as_float((127 + e2) << 23);
+  if (lane == 0)
+    reinterpret_cast<float*>(image + (long long)cols * 2 * (r + dr))[col] =
+        scale_log2 * __uint_as_float((127 - e1) << 23) * __uint_as_float((127 - e2) << 23);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int c = lane + 32 * i;
+    if (c >= n8) break;
+    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+    const bool latent = 8 * c < r;
+    uint32_t y[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const float lo = __uint_as_float(x[m] << 16) * f1 * f2, hi = __uint_as_float(x[m] & 0xffff0000u) * f1 * f2;
+      const __half2 l2 = __floats2half2_rn(lo, hi);
+      const __nv_bfloat162 k2 = __floats2bfloat162_rn(lo, hi);
+      y[m] = latent ? *reinterpret_cast<const uint32_t*>(&l2) : *reinterpret_cast<const uint32_t*>(&k2);
+    }
+    const int at = latent ? (c >> 3) * cols * 128 + col * 128 + ((c ^ col) & 7) * 16
+                          : cols * 2 * r + col * 2 * dr + ((c - r / 8) ^ f.key_swizzle(col)) * 16;
+    *reinterpret_cast<uint4*>(image + at) = make_uint4(y[0], y[1], y[2], y[3]);
+  }
+}
+
+// Two prefix sums over the requests (groups, tiles) in every CTA; the first enters the list, a warp per request, the
+// others (of bf16 queries) write the groups' images, a group each in turn.  A batch whose `starts` do not ascend inside
+// the nodes gets no groups and a count of -1.  As a part of the attention, each CTA writing the image of its next
+// group itself when the last one's products are done, the images took 13000 cycles of every change between groups.
 __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(PlanArgs a) {
   __shared__ int s_first[kMaxRequests + 1], s_tile[kMaxRequests + 1];
   __shared__ int warp_g[32], warp_t[32];
@@ -146,17 +201,17 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(PlanArgs a) {
   bool wrong = a.starts[0] < 0;
   for (int b = lo; b < hi; ++b) wrong |= a.starts[b] > a.starts[b + 1] || a.starts[b + 1] > a.n_nodes;
   if (__syncthreads_or(wrong)) {
-    if (tid == 0) {
+    if (blockIdx.x == 0 && tid == 0) {
       *a.n_groups = -1;
       a.prefix[0] = 0;
     }
     return;
   }
-  // Ascending requests have at most max_groups groups, whose tiles the host has found to fit 32 bits.
-  auto groups_of = [&](int b) { return ceil_div((a.starts[b + 1] - a.starts[b]) * a.heads, a.cols); };
+  // Ascending requests have at most as many groups as there is room for, and tiles that the host has found to fit
+  // 32 bits.
   int sum_g = 0, sum_t = 0;
   for (int b = lo; b < hi; ++b) {
-    const int g = groups_of(b);
+    const int g = ceil_div((a.starts[b + 1] - a.starts[b]) * a.heads, a.cols);
     s_first[b] = sum_g;
     s_tile[b] = sum_t;
     sum_g += g;
@@ -175,19 +230,35 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(PlanArgs a) {
   for (int b = lo; b < hi; ++b) { s_first[b] += base_g; s_tile[b] += base_t; }
   if (hi == a.batch && lo < hi) { s_first[a.batch] = base_g + sum_g; s_tile[a.batch] = base_t + sum_t; }
   __syncthreads();
-  for (int b = tid; b <= a.batch; b += kPlanThreads) a.first[b] = s_first[b];
-  for (int b = warp; b < a.batch; b += kPlanThreads / 32) {
-    const int col0 = a.starts[b] * a.heads, cols = a.starts[b + 1] * a.heads - col0, tiles = tiles_of(b);
-    const int slots = min(max(a.slots[b], 0), (int)min((long long)a.width * qp::kPageRows, 0x7fffffffll));
-    const int g0 = s_first[b], n = s_first[b + 1] - g0;
-    for (int i = lane; i < n; i += 32) {
-      a.groups[g0 + i] = make_int4(b, col0 + i * a.cols, min(a.cols, cols - i * a.cols), slots);
-      a.prefix[g0 + i] = s_tile[b] + i * tiles;
+  const int total = s_first[a.batch];
+  if (blockIdx.x == 0) {
+    for (int b = tid; b <= a.batch; b += kPlanThreads) a.first[b] = s_first[b];
+    for (int b = warp; b < a.batch; b += kPlanThreads / 32) {
+      const int col0 = a.starts[b] * a.heads, cols = a.starts[b + 1] * a.heads - col0, tiles = tiles_of(b);
+      const int slots = min(max(a.slots[b], 0), (int)min((long long)a.width * qp::kPageRows, 0x7fffffffll));
+      const int g0 = s_first[b], n = s_first[b + 1] - g0;
+      for (int i = lane; i < n; i += 32) {
+        a.groups[g0 + i] = make_int4(b, col0 + i * a.cols, min(a.cols, cols - i * a.cols), slots);
+        a.prefix[g0 + i] = s_tile[b] + i * tiles;
+      }
     }
+    if (tid == 0) {
+      *a.n_groups = total;
+      a.prefix[total] = s_tile[a.batch];
+    }
+    return;
   }
-  if (tid == 0) {
-    *a.n_groups = s_first[a.batch];
-    a.prefix[s_first[a.batch]] = s_tile[a.batch];
+  for (int v = blockIdx.x - 1; v < total; v += gridDim.x - 1) {
+    int b = 0, end = a.batch;                          // the request: the last one that begins at v or before it
+    while (end - b > 1) {
+      const int mid = (b + end) >> 1;
+      if (s_first[mid] <= v) b = mid; else end = mid;
+    }
+    const int skip = (v - s_first[b]) * a.cols, col0 = a.starts[b] * a.heads + skip;
+    const int cols = a.starts[b + 1] * a.heads - col0;
+    for (int c = warp; c < a.cols; c += kPlanThreads / 32)
+      put_column(a.q + (long long)(col0 + c) * (a.f.r + a.f.dr), c < cols, a.image + (long long)v * image_bytes(a.cols, a.f),
+                 c, a.cols, a.scale_log2, a.f);
   }
 }
 
