@@ -100,13 +100,14 @@ int launch_context_tc(const qp::AttnArgs& a, long long tiles, const OnDeviceOf& 
 
 template <typename T>
 int launch_join(const tree::JoinArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
-  // Four heads a warp share the loads of a drafted row; where that leaves SMs idle, one.
-  const long long warps4 = (long long)a.n_nodes * ceil_div(a.heads, 4);
-  const bool four = warps4 >= 8ll * dev.sm_count();
-  const long long units = four ? warps4 : (long long)a.n_nodes * a.heads;
+  // A CTA per column as long as all of them run at once, four on an SM; then a warp per two heads of a node.
+  const long long columns = (long long)a.n_nodes * a.heads, at_once = 4ll * dev.sm_count();
+  if (columns <= at_once)
+    return launch_dependent(tree::tree_join_split_kernel<T>, dim3((unsigned)columns), tree::kSplitThreads, 0, st, a);
+  const long long units = (long long)a.n_nodes * ceil_div(a.heads, 2);
   const long long ctas = (units + tree::kJoinWarps - 1) / tree::kJoinWarps, most = 16ll * dev.sm_count();
-  return launch_dependent(four ? tree::tree_join_kernel<T, 4> : tree::tree_join_kernel<T, 1>,
-                          dim3((unsigned)(ctas < most ? ctas : most)), tree::kJoinThreads, 0, st, a);
+  return launch_dependent(tree::tree_join_kernel<T>, dim3((unsigned)(ctas < most ? ctas : most)), tree::kJoinThreads, 0, st,
+                          a);
 }
 
 }  // namespace
@@ -185,9 +186,9 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   pa.image = tensor ? reinterpret_cast<uint8_t*>(ws + p.image) : nullptr;
   pa.scale_log2 = (float)((double)scale * kLog2e);
   pa.f = format_of(cfg);
-  const long long groups = most_groups(cfg, B, n_nodes, cols), images = tensor ? groups : 0;
+  const long long groups = most_groups(cfg, B, n_nodes, cols), images = tensor ? 2 * groups : 0;
   const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
-  int status = launch_dependent(tree::tree_plan_kernel, dim3(1 + (unsigned)(images < 2 * sms ? images : 2 * sms)),
+  int status = launch_dependent(tree::tree_plan_kernel, dim3(1 + (unsigned)(images < 3 * sms ? images : 3 * sms)),
                                 tree::kPlanThreads, 0, st, pa);
   if (status != MTLA_OK) return status;
 

@@ -130,7 +130,7 @@ struct PlanArgs {
   qp::Format f;
 };
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 512;
 constexpr int kMaxRequests = 4096;
 
 // A group's queries for the tensor-core kernel, as they lie in its shared memory: r / 64 panels [cols][64] half
@@ -183,12 +183,12 @@ __device__ __forceinline__ void put_column(const bf16* q, bool there, uint8_t* i
 }
 
 // Two prefix sums over the requests (groups, tiles) in every CTA; the first enters the list, a warp per request, the
-// others (of bf16 queries) write the groups' images, a group each in turn.  A batch whose `starts` do not ascend inside
+// others (of bf16 queries) write the groups' images, half a group each in turn.  A batch whose `starts` do not ascend inside
 // the nodes gets no groups and a count of -1.  As a part of the attention, each CTA writing the image of its next
 // group itself when the last one's products are done, the images took 13000 cycles of every change between groups.
-__global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(PlanArgs a) {
+__global__ void __launch_bounds__(kPlanThreads, 3) tree_plan_kernel(PlanArgs a) {
   __shared__ int s_first[kMaxRequests + 1], s_tile[kMaxRequests + 1];
-  __shared__ int warp_g[32], warp_t[32];
+  __shared__ int warp_g[kPlanThreads / 32], warp_t[kPlanThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
@@ -248,7 +248,8 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(PlanArgs a) {
     }
     return;
   }
-  for (int v = blockIdx.x - 1; v < total; v += gridDim.x - 1) {
+  for (int u = blockIdx.x - 1; u < 2 * total; u += gridDim.x - 1) {
+    const int v = u >> 1, half = a.cols / 2;
     int b = 0, end = a.batch;                          // the request: the last one that begins at v or before it
     while (end - b > 1) {
       const int mid = (b + end) >> 1;
@@ -256,7 +257,7 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(PlanArgs a) {
     }
     const int skip = (v - s_first[b]) * a.cols, col0 = a.starts[b] * a.heads + skip;
     const int cols = a.starts[b + 1] * a.heads - col0;
-    for (int c = warp; c < a.cols; c += kPlanThreads / 32)
+    for (int c = (u & 1) * half + warp; c < ((u & 1) + 1) * half; c += kPlanThreads / 32)
       put_column(a.q + (long long)(col0 + c) * (a.f.r + a.f.dr), c < cols, a.image + (long long)v * image_bytes(a.cols, a.f),
                  c, a.cols, a.scale_log2, a.f);
   }
@@ -283,145 +284,258 @@ struct JoinArgs {
   qp::Format f;
 };
 
-constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32;
+// What has been joined of one column: reference (log2 units), denominator, sums; a lane holds E latents.
+template <typename T>
+struct Running {
+  static constexpr int V = Elem<T>::kVec, R = 512 / (32 * V), E = R * V;       // runs of 16 bytes of a row
+  float m, l, acc[E];
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  }
+  // Sums x with the denominator and reference of their own; minus infinity: nothing.
+  __device__ __forceinline__ void add(float mx, float lx, const float (&x)[E]) {
+    const float top = fmaxf(m, mx), ref = top == -INFINITY ? 0.f : top, al = exp2f(m - ref), p = exp2f(mx - ref);
+    m = top;
+    l = l * al + p * lx;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = fmaf(p, x[e], acc[e] * al);
+  }
+};
+// A row's latents (16 bytes a lane and run) and key (d_R / 32 elements a lane).
+template <typename T>
+__device__ __forceinline__ void load_row(const T* src, const qp::Format& f, float (&x)[Running<T>::E], float (&k)[2]) {
+  constexpr int V = Running<T>::V, R = Running<T>::R;
+  const int lane = threadIdx.x & 31, kd = f.dr / 32;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+    if ((j * 32 + lane) * V < f.r) load_vec(src + (j * 32 + lane) * V, v);
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[j * V + e] = v[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) k[e] = e < kd ? Elem<T>::to_float(src[f.r + lane * kd + e]) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void load_part(const float* src, int r, float (&x)[Running<T>::E]) {
+  constexpr int V = Running<T>::V, R = Running<T>::R;
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int j = 0; j < R; ++j)
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+      float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+      if ((j * 32 + lane) * V < r) w = *reinterpret_cast<const float4*>(src + (j * 32 + lane) * V + e);
+      x[j * V + e] = w.x;
+      x[j * V + e + 1] = w.y;
+      x[j * V + e + 2] = w.z;
+      x[j * V + e + 3] = w.w;
+    }
+}
+template <typename T>
+__device__ __forceinline__ float dot_row(const float (&q)[Running<T>::E], const float (&qk)[2],
+                                         const float (&x)[Running<T>::E], const float (&k)[2]) {
+  float s = qk[0] * k[0] + qk[1] * k[1];
+#pragma unroll
+  for (int e = 0; e < Running<T>::E; ++e) s = fmaf(q[e], x[e], s);
+  return warp_sum(s);
+}
 
-// A warp per node and HB of its heads: the online softmax over the drafted rows that the node sees, row after row
-// (a lane keeps 16 of the 512 latents of every head, a row is loaded once for all of them), and then
-// the parts that the attention over the context has left for its columns.  Masked rows are never read, so what
-// they hold cannot reach a result; sums, maxima and products are fp32.
-// A row's latents are loaded 16 bytes a lane, V elements, in R rounds; its key as d_R / 32 elements a lane.
-template <typename T, int HB>
+// Where a node stands: its request's first node, the drafted rows that it sees, and its columns' groups.
+struct Place {
+  bool fine;                 // in a request (or the batch is refused: nothing is seen)
+  int lo, first_group;
+  unsigned long long seen;
+};
+__device__ __forceinline__ Place place_of(const JoinArgs& a, int node, bool refused) {
+  Place p = {true, 0, 0, 0};
+  if (refused) return p;
+  const unsigned long long seen = (unsigned long long)a.seen[node];
+  const int b = qp::find_wide(a.starts, a.batch, node), hi = a.starts[b + 1];
+  p.lo = a.starts[b];
+  p.first_group = a.first[b];
+  p.fine = node >= p.lo;                               // else in front of the first request
+  p.seen = hi - p.lo < kMaxNodes ? seen & ((1ull << (hi - p.lo)) - 1) : seen;
+  return p;
+}
+// The parts of a column: x first, y number; z the column inside its group.
+__device__ __forceinline__ int3 parts_of(const JoinArgs& a, const Place& p, int node, int h, bool refused) {
+  if (refused) return make_int3(0, 0, 0);
+  const int local = (node - p.lo) * a.heads + h, v = p.first_group + local / a.cols;
+  const int2 parts = a.parts[v];                       // (not set for a group without tiles)
+  return make_int3(parts.x, a.groups[v].w > 0 ? parts.y : 0, local % a.cols);
+}
+template <typename T>
+__device__ __forceinline__ void store_column(const JoinArgs& a, long long column, float m, float l, bool failed,
+                                             const float (&acc)[Running<T>::E]) {
+  constexpr int V = Running<T>::V, R = Running<T>::R;
+  const int lane = threadIdx.x & 31;
+  // A node that sees nothing: zeros and minus infinity.
+  const float inv = failed ? NAN : l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    if ((j * 32 + lane) * V >= a.f.r) continue;
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = acc[j * V + e] * inv;
+    store_vec(static_cast<T*>(a.out) + column * a.f.r + (j * 32 + lane) * V, v);
+  }
+  if (a.lse && lane == 0) a.lse[column] = failed ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// The join: the online softmax over the drafted rows that a node sees, row after row, and the parts that the attention
+// over the context has left for its columns.  Masked rows are never read, so what they hold cannot reach a
+// result; sums, maxima and products are fp32.  Bound by the parts' bytes when there are many columns, else by the chain
+// of loads.  Two forms:
+//   a warp per node and two heads, which share the rows' loads, for many columns;
+//   with SPLIT a CTA per column, whose warps share rows and parts out, for few: one request of 112 columns in 74 parts
+//   each took 53 us with a warp per column.
+constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kSplitThreads = 256, kSplitWarps = kSplitThreads / 32;
+
+template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(JoinArgs a) {
-  constexpr int V = Elem<T>::kVec, R = 512 / (32 * V), E = R * V;
-  __shared__ int s_failed;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = a.f.r, dr = a.f.dr, kd = dr / 32;
-  const int blocks = ceil_div(a.heads, HB);
-  if (threadIdx.x == 0) s_failed = 0;
-  __syncthreads();
+  using Run = Running<T>;
+  constexpr int E = Run::E, HB = 2;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = a.f.r, blocks = ceil_div(a.heads, HB);
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  for (int i = threadIdx.x; i < a.n_error_words; i += kJoinThreads)
-    if (a.error_words[i]) s_failed = 1;
-  __syncthreads();
-  const bool refused = *a.n_groups < 0, failed = s_failed != 0 || refused;
+  bool failed = false;
+  for (int i = threadIdx.x; i < a.n_error_words; i += kJoinThreads) failed |= a.error_words[i] != 0;
+  const bool refused = *a.n_groups < 0;
+  failed = __syncthreads_or(failed) || refused;
   // Nodes behind the last request are left as they were; those of a refused batch all get NaN.
   const long long units = (long long)(refused ? a.n_nodes : a.starts[a.batch]) * blocks;
   for (long long u = (long long)blockIdx.x * kJoinWarps + warp; u < units; u += (long long)gridDim.x * kJoinWarps) {
     const int node = (int)(u / blocks), h0 = (int)(u % blocks) * HB;
-    const int b = refused ? 0 : qp::find_wide(a.starts, a.batch, node);
-    const int lo = refused ? 0 : a.starts[b], hi = refused ? 0 : a.starts[b + 1];
-    if (node < lo) continue;                              // in front of the first request
-    unsigned long long seen = refused ? 0 : (unsigned long long)a.seen[node];
-    if (hi - lo < kMaxNodes) seen &= (1ull << (hi - lo)) - 1;
-    float q[HB][E], qk[HB][2], acc[HB][E], m[HB], l[HB];
+    const bool two = h0 + 1 < a.heads;
+    float q[HB][E], qk[HB][2];
 #pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      const bool there = h0 + h < a.heads;
-      const T* src = static_cast<const T*>(a.q) + ((long long)node * a.heads + h0 + (there ? h : 0)) * (r + dr);
+    for (int h = 0; h < HB; ++h)
+      load_row<T>(static_cast<const T*>(a.q) + ((long long)node * a.heads + h0 + (two ? h : 0)) * (r + a.f.dr), a.f, q[h],
+                  qk[h]);
+    Place p = place_of(a, node, refused);
+    if (!p.fine) continue;
+    int3 parts[HB];
 #pragma unroll
-      for (int j = 0; j < R; ++j) {
-        float v[V];
+    for (int h = 0; h < HB; ++h) parts[h] = parts_of(a, p, node, h0 + (two ? h : 0), refused);
+    Run run[HB];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = 0.f;
-        if ((j * 32 + lane) * V < r) load_vec(src + (j * 32 + lane) * V, v);
+    for (int h = 0; h < HB; ++h) run[h].clear();
+    while (p.seen) {
+      const int at = __ffsll((long long)p.seen) - 1;
+      p.seen &= p.seen - 1;
+      float x[E], k[2];
+      load_row<T>(static_cast<const T*>(a.rows) + (p.lo + at) * a.row_stride, a.f, x, k);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          q[h][j * V + e] = v[e];
-          acc[h][j * V + e] = 0.f;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) qk[h][e] = e < kd ? Elem<T>::to_float(src[r + lane * kd + e]) : 0.f;
-      m[h] = -INFINITY;
-      l[h] = 0.f;
+      for (int h = 0; h < HB; ++h) run[h].add(dot_row<T>(q[h], qk[h], x, k) * a.scale_log2, 1.f, x);
     }
-    while (seen) {
-      const int at = __ffsll((long long)seen) - 1;
-      seen &= seen - 1;
-      const T* src = static_cast<const T*>(a.rows) + (lo + at) * a.row_stride;
-      float c[E], ck[2];
-#pragma unroll
-      for (int j = 0; j < R; ++j) {
-        float v[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = 0.f;
-        if ((j * 32 + lane) * V < r) load_vec(src + (j * 32 + lane) * V, v);
-#pragma unroll
-        for (int e = 0; e < V; ++e) c[j * V + e] = v[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) ck[e] = e < kd ? Elem<T>::to_float(src[r + lane * kd + e]) : 0.f;
+    // Both heads' parts together, as long as either has one.
+    const int most = max(parts[0].y, parts[1].y);
+    for (int n = 0; n < most; ++n) {
+      float2 ml[HB];
+      float x[HB][E];
 #pragma unroll
       for (int h = 0; h < HB; ++h) {
-        float s = qk[h][0] * ck[0] + qk[h][1] * ck[1];
-#pragma unroll
-        for (int e = 0; e < E; ++e) s = fmaf(q[h][e], c[e], s);
-        s = warp_sum(s) * a.scale_log2;
-        const float top = fmaxf(m[h], s), ref = top == -INFINITY ? 0.f : top;
-        const float al = exp2f(m[h] - ref), p = exp2f(s - ref);
-        m[h] = top;
-        l[h] = l[h] * al + p;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[h][e] = fmaf(p, c[e], acc[h][e] * al);
-      }
-    }
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      if (h0 + h >= a.heads) break;
-      int2 parts = make_int2(0, 0);
-      int col = 0;
-      if (!refused) {
-        const int local = (node - lo) * a.heads + h0 + h;      // column of the request
-        const int v = a.first[b] + local / a.cols;
-        col = local % a.cols;
-        if (a.groups[v].w > 0) parts = a.parts[v];
-      }
-      constexpr int U = 4;                              // parts whose loads are in flight together
-      for (int p0 = 0; p0 < parts.y; p0 += U) {
-        float2 ml[U];
-        float x[U][E];
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const long long at = (long long)(parts.x + min(p0 + i, parts.y - 1)) * a.cols + col;
-          ml[i] = reinterpret_cast<const float2*>(a.ml_part)[at];
-#pragma unroll
-          for (int j = 0; j < R; ++j)
-#pragma unroll
-            for (int e = 0; e < V; e += 4) {
-              float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-              if ((j * 32 + lane) * V < r)
-                w = *reinterpret_cast<const float4*>(a.o_part + at * r + (j * 32 + lane) * V + e);
-              x[i][j * V + e] = w.x;
-              x[i][j * V + e + 1] = w.y;
-              x[i][j * V + e + 2] = w.z;
-              x[i][j * V + e + 3] = w.w;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          if (p0 + i >= parts.y) break;
-          const float top = fmaxf(m[h], ml[i].x), ref = top == -INFINITY ? 0.f : top;
-          const float al = exp2f(m[h] - ref), p = exp2f(ml[i].x - ref);
-          m[h] = top;
-          l[h] = l[h] * al + p * ml[i].y;
-#pragma unroll
-          for (int e = 0; e < E; ++e) acc[h][e] = fmaf(p, x[i][e], acc[h][e] * al);
+        const long long at = (long long)(parts[h].x + min(n, max(parts[h].y, 1) - 1)) * a.cols + parts[h].z;
+        ml[h] = make_float2(-INFINITY, 0.f);
+        if (n < parts[h].y) {
+          ml[h] = reinterpret_cast<const float2*>(a.ml_part)[at];
+          load_part<T>(a.o_part + at * r, r, x[h]);
         }
       }
-      // A node that sees nothing: zeros and minus infinity.
-      const float inv = failed ? NAN : l[h] == 0.f ? 0.f : 1.f / l[h];
-      const long long column = (long long)node * a.heads + h0 + h;
 #pragma unroll
-      for (int j = 0; j < R; ++j) {
-        if ((j * 32 + lane) * V >= r) continue;
-        float v8[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) v8[e] = acc[h][j * V + e] * inv;
-        store_vec(static_cast<T*>(a.out) + column * r + (j * 32 + lane) * V, v8);
-      }
-      if (a.lse && lane == 0)
-        a.lse[column] = failed ? NAN : l[h] == 0.f ? -INFINITY : (m[h] + log2f(l[h])) * 0.69314718055994531f;
+      for (int h = 0; h < HB; ++h)
+        if (n < parts[h].y) run[h].add(ml[h].x, ml[h].y, x[h]);
     }
+#pragma unroll
+    for (int h = 0; h < HB; ++h)
+      if (h == 0 || two)
+        store_column<T>(a, (long long)node * a.heads + h0 + h, run[h].m, run[h].l, failed, run[h].acc);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSplitThreads) tree_join_split_kernel(JoinArgs a) {
+  using Run = Running<T>;
+  constexpr int E = Run::E;
+  __shared__ float s_m[kSplitWarps], s_l[kSplitWarps];
+  __shared__ float4 s_acc[kSplitWarps][E / 4][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = a.f.r;
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+  bool failed = false;
+  for (int i = threadIdx.x; i < a.n_error_words; i += kSplitThreads) failed |= a.error_words[i] != 0;
+  const bool refused = *a.n_groups < 0;
+  failed = __syncthreads_or(failed) || refused;
+  const long long columns = (long long)(refused ? a.n_nodes : a.starts[a.batch]) * a.heads;
+  for (long long column = blockIdx.x; column < columns; column += gridDim.x) {
+    const int node = (int)(column / a.heads), h = (int)(column % a.heads);
+    const Place p = place_of(a, node, refused);
+    if (!p.fine) continue;
+    const int3 parts = parts_of(a, p, node, h, refused);
+    Run run;
+    run.clear();
+    // Rows in turn: the warp's are the set bits number warp, warp + 8, ...
+    if (__popcll(p.seen) > warp) {
+      float q[E], qk[2];
+      load_row<T>(static_cast<const T*>(a.q) + column * (r + a.f.dr), a.f, q, qk);
+      unsigned long long seen = p.seen;
+      for (int n = 0; seen; ++n) {
+        const int at = __ffsll((long long)seen) - 1;
+        seen &= seen - 1;
+        if (n % kSplitWarps != warp) continue;
+        float x[E], k[2];
+        load_row<T>(static_cast<const T*>(a.rows) + (p.lo + at) * a.row_stride, a.f, x, k);
+        run.add(dot_row<T>(q, qk, x, k) * a.scale_log2, 1.f, x);
+      }
+    }
+    constexpr int U = 4;                                 // parts whose loads are in flight together
+    for (int n0 = warp; n0 < parts.y; n0 += U * kSplitWarps) {
+      float2 ml[U];
+      float x[U][E];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int n = n0 + i * kSplitWarps;
+        ml[i] = make_float2(-INFINITY, 0.f);
+        if (n >= parts.y) continue;
+        const long long at = (long long)(parts.x + n) * a.cols + parts.z;
+        ml[i] = reinterpret_cast<const float2*>(a.ml_part)[at];
+        load_part<T>(a.o_part + at * r, r, x[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (n0 + i * kSplitWarps < parts.y) run.add(ml[i].x, ml[i].y, x[i]);
+    }
+    if (lane == 0) {
+      s_m[warp] = run.m;
+      s_l[warp] = run.l;
+    }
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+      s_acc[warp][e / 4][lane] = make_float4(run.acc[e], run.acc[e + 1], run.acc[e + 2], run.acc[e + 3]);
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll 1
+      for (int w = 1; w < kSplitWarps; ++w) {            // in the warps' order
+        float x[E];
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+          const float4 v = s_acc[w][e / 4][lane];
+          x[e] = v.x;
+          x[e + 1] = v.y;
+          x[e + 2] = v.z;
+          x[e + 3] = v.w;
+        }
+        run.add(s_m[w], s_l[w], x);
+      }
+      store_column<T>(a, column, run.m, run.l, failed, run.acc);
+    }
+    __syncthreads();
   }
 }
 
