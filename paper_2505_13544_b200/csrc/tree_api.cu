@@ -99,13 +99,20 @@ int launch_context_tc(const qp::AttnArgs& a, long long tiles, const OnDeviceOf& 
 }
 
 template <typename T>
-int launch_join(const tree::JoinArgs& a, const OnDeviceOf& dev, cudaStream_t st) {
-  // A CTA per column as long as all of them run at once, four on an SM; then a warp per two heads of a node.
-  const long long columns = (long long)a.n_nodes * a.heads, at_once = 4ll * dev.sm_count();
-  if (columns <= at_once)
+int launch_join(const tree::JoinArgs& a, long long groups, const OnDeviceOf& dev, cudaStream_t st) {
+  // A CTA per column as long as all of them run at once, two on an SM.
+  const long long columns = (long long)a.n_nodes * a.heads, sms = dev.sm_count();
+  if (columns <= 2 * sms)
     return launch_dependent(tree::tree_join_split_kernel<T>, dim3((unsigned)columns), tree::kSplitThreads, 0, st, a);
-  const long long units = (long long)a.n_nodes * ceil_div(a.heads, 2);
-  const long long ctas = (units + tree::kJoinWarps - 1) / tree::kJoinWarps, most = 16ll * dev.sm_count();
+  if constexpr (sizeof(T) == 2) {
+    if (a.cols == 64 && groups >= sms) {         // a group for every SM
+      constexpr int kBytes = tree::Dense<64>::bytes(qp::Format{512, 64});
+      if (!raise_smem<tree::tree_join_dense_kernel<64>>(dev.device(), kBytes)) return MTLA_ERR_CUDA;
+      return launch_dependent(tree::tree_join_dense_kernel<64>, dim3((unsigned)groups), tree::Dense<64>::kThreads,
+                              tree::Dense<64>::bytes(a.f), st, a);
+    }
+  }
+  const long long ctas = (columns + tree::kJoinWarps - 1) / tree::kJoinWarps, most = 16 * sms;
   return launch_dependent(tree::tree_join_kernel<T>, dim3((unsigned)(ctas < most ? ctas : most)), tree::kJoinThreads, 0, st,
                           a);
 }
@@ -239,7 +246,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   j.cols = cols;
   j.n_error_words = tensor ? (int)(tiles < sms ? tiles : sms) : 0;
   j.f = a.f;
-  return dtype == MTLA_DTYPE_BF16 ? launch_join<bf16>(j, dev, st) : launch_join<float>(j, dev, st);
+  return dtype == MTLA_DTYPE_BF16 ? launch_join<bf16>(j, groups, dev, st) : launch_join<float>(j, groups, dev, st);
 }
 
 }  // extern "C"

@@ -9,6 +9,7 @@
 #pragma once
 
 #include "qpool_attn.cuh"
+#include "qweight_format.cuh"
 
 namespace mtla {
 namespace tree {
@@ -139,47 +140,51 @@ constexpr int kMaxRequests = 4096;
 __host__ __device__ inline int image_bytes(int cols, const qp::Format& f) { return cols * (2 * (f.r + f.dr) + 4); }
 
 // One column into its group's image, by a warp.  The row is scaled by the power of two that brings its largest
-// element into [2^14, 2^15), exactly down to 2^-39 of that; a column that does not exist is zero.
+// element into [2^14, 2^15), exactly down to 2^-39 of that; a column that does not exist is zero.  Magnitudes and scaling
+// work on pairs of bf16 numbers (a power of two in two factors, since one may be out of range).
 __device__ __forceinline__ void put_column(const bf16* q, bool there, uint8_t* image, int col, int cols, float scale_log2,
                                            const qp::Format& f) {
-  const int lane = threadIdx.x & 31, r = f.r, dr = f.dr, n8 = (r + dr) / 8;
-  uint4 w[3];                                    // r + d_R is 576 at most
-  uint32_t top = 0;
+  const int lane = threadIdx.x & 31, r = f.r, dr = f.dr;
+  uint4 w[2], key = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int c = lane + 32 * i;
+  for (int i = 0; i < 2; ++i) {
     w[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (there && c < n8) w[i] = *reinterpret_cast<const uint4*>(q + 8 * c);
-    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-    for (int m = 0; m < 4; ++m) top = max(top, max(x[m] & 0x7fff0000u, (x[m] << 16) & 0x7fff0000u));
+    if (there && (lane + 32 * i) * 8 < r) w[i] = *reinterpret_cast<const uint4*>(q + (lane + 32 * i) * 8);
   }
-  top = __reduce_max_sync(0xffffffffu, top);
+  if (there && lane * 8 < dr) key = *reinterpret_cast<const uint4*>(q + r + lane * 8);
+  uint32_t top = 0;
+  auto largest = [&](const uint4& v) {
+    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int m = 0; m < 4; ++m) top = __vmaxu2(top, x[m] & 0x7fff7fffu);
+  };
+  largest(w[0]);
+  largest(w[1]);
+  largest(key);
+  top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
   // Exponents -113 .. 140 (a row of subnormal numbers only reaches less); none for zeros and specials.
-  const bool fine = top > 0 && top < 0x7f800000u;
-  const int e = fine ? 141 - max((int)(top >> 23), 1) : 0, e1 = e / 2, e2 = e - e1;
-  const float f1 = __uint_as_float((127 + e1) << 23), f2 = __uint_as_float((127 + e2) << 23);
+  const bool fine = top > 0 && top < 0x7f80u;
+  const int e = fine ? 141 - max((int)(top >> 7), 1) : 0, e1 = e / 2, e2 = e - e1;
+  const uint32_t f1 = (uint32_t)(127 + e1) * 0x00800080u, f2 = (uint32_t)(127 + e2) * 0x00800080u;
   if (lane == 0)
     reinterpret_cast<float*>(image + (long long)cols * 2 * (r + dr))[col] =
         scale_log2 * __uint_as_float((127 - e1) << 23) * __uint_as_float((127 - e2) << 23);
+  auto scaled = [&](uint32_t x) { return qw::mul_b2(qw::mul_b2(x, f1), f2); };
+  auto half2_of = [&](uint32_t x) {
+    const uint32_t y = scaled(x);
+    const __half2 h = __floats2half2_rn(__uint_as_float(y << 16), __uint_as_float(y & 0xffff0000u));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  };
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < 2; ++i) {
     const int c = lane + 32 * i;
-    if (c >= n8) break;
-    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-    const bool latent = 8 * c < r;
-    uint32_t y[4];
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const float lo = __uint_as_float(x[m] << 16) * f1 * f2, hi = __uint_as_float(x[m] & 0xffff0000u) * f1 * f2;
-      const __half2 l2 = __floats2half2_rn(lo, hi);
-      const __nv_bfloat162 k2 = __floats2bfloat162_rn(lo, hi);
-      y[m] = latent ? *reinterpret_cast<const uint32_t*>(&l2) : *reinterpret_cast<const uint32_t*>(&k2);
-    }
-    const int at = latent ? (c >> 3) * cols * 128 + col * 128 + ((c ^ col) & 7) * 16
-                          : cols * 2 * r + col * 2 * dr + ((c - r / 8) ^ f.key_swizzle(col)) * 16;
-    *reinterpret_cast<uint4*>(image + at) = make_uint4(y[0], y[1], y[2], y[3]);
+    if (c * 8 < r)
+      *reinterpret_cast<uint4*>(image + (c >> 3) * cols * 128 + col * 128 + ((c ^ col) & 7) * 16) =
+          make_uint4(half2_of(w[i].x), half2_of(w[i].y), half2_of(w[i].z), half2_of(w[i].w));
   }
+  if (lane * 8 < dr)
+    *reinterpret_cast<uint4*>(image + cols * 2 * r + col * 2 * dr + (lane ^ f.key_swizzle(col)) * 16) =
+        make_uint4(scaled(key.x), scaled(key.y), scaled(key.z), scaled(key.w));
 }
 
 // Two prefix sums over the requests (groups, tiles) in every CTA; the first enters the list, a warp per request, the
@@ -284,29 +289,39 @@ struct JoinArgs {
   qp::Format f;
 };
 
-// What has been joined of one column: reference (log2 units), denominator, sums; a lane holds E latents.
+// What has been joined of one column: reference (log2 units), denominator, sums; a lane holds E latents, in pairs.
 template <typename T>
 struct Running {
   static constexpr int V = Elem<T>::kVec, R = 512 / (32 * V), E = R * V;       // runs of 16 bytes of a row
-  float m, l, acc[E];
+  float m, l;
+  uint64_t acc[E / 2];
   __device__ __forceinline__ void clear() {
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    for (int e = 0; e < E / 2; ++e) acc[e] = 0;
   }
   // Sums x with the denominator and reference of their own; minus infinity: nothing.
-  __device__ __forceinline__ void add(float mx, float lx, const float (&x)[E]) {
-    const float top = fmaxf(m, mx), ref = top == -INFINITY ? 0.f : top, al = exp2f(m - ref), p = exp2f(mx - ref);
-    m = top;
-    l = l * al + p * lx;
+  __device__ __forceinline__ void add(float mx, float lx, const uint64_t (&x)[E / 2]) {
+    const float top = fmaxf(m, mx), ref = top == -INFINITY ? 0.f : top, p = exp2f(mx - ref);
+    if (top != m) {
+      const float al = exp2f(m - ref);
+      l *= al;
+      const uint64_t al2 = ptx::pack2(al, al);
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(p, x[e], acc[e] * al);
+      for (int e = 0; e < E / 2; ++e) acc[e] = ptx::mul2(acc[e], al2);
+      m = top;
+    }
+    l += p * lx;
+    const uint64_t p2 = ptx::pack2(p, p);
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) acc[e] = ptx::fma2(p2, x[e], acc[e]);
   }
 };
 // A row's latents (16 bytes a lane and run) and key (d_R / 32 elements a lane).
 template <typename T>
-__device__ __forceinline__ void load_row(const T* src, const qp::Format& f, float (&x)[Running<T>::E], float (&k)[2]) {
+__device__ __forceinline__ void load_row(const T* src, const qp::Format& f, uint64_t (&x)[Running<T>::E / 2],
+                                         float (&k)[2]) {
   constexpr int V = Running<T>::V, R = Running<T>::R;
   const int lane = threadIdx.x & 31, kd = f.dr / 32;
 #pragma unroll
@@ -316,34 +331,35 @@ __device__ __forceinline__ void load_row(const T* src, const qp::Format& f, floa
     for (int e = 0; e < V; ++e) v[e] = 0.f;
     if ((j * 32 + lane) * V < f.r) load_vec(src + (j * 32 + lane) * V, v);
 #pragma unroll
-    for (int e = 0; e < V; ++e) x[j * V + e] = v[e];
+    for (int e = 0; e < V; e += 2) x[(j * V + e) / 2] = ptx::pack2(v[e], v[e + 1]);
   }
 #pragma unroll
   for (int e = 0; e < 2; ++e) k[e] = e < kd ? Elem<T>::to_float(src[f.r + lane * kd + e]) : 0.f;
 }
 template <typename T>
-__device__ __forceinline__ void load_part(const float* src, int r, float (&x)[Running<T>::E]) {
+__device__ __forceinline__ void load_part(const float* src, int r, uint64_t (&x)[Running<T>::E / 2]) {
   constexpr int V = Running<T>::V, R = Running<T>::R;
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int j = 0; j < R; ++j)
 #pragma unroll
     for (int e = 0; e < V; e += 4) {
-      float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-      if ((j * 32 + lane) * V < r) w = *reinterpret_cast<const float4*>(src + (j * 32 + lane) * V + e);
-      x[j * V + e] = w.x;
-      x[j * V + e + 1] = w.y;
-      x[j * V + e + 2] = w.z;
-      x[j * V + e + 3] = w.w;
+      ulonglong2 w = make_ulonglong2(0ull, 0ull);
+      if ((j * 32 + lane) * V < r) w = *reinterpret_cast<const ulonglong2*>(src + (j * 32 + lane) * V + e);
+      x[(j * V + e) / 2] = w.x;
+      x[(j * V + e) / 2 + 1] = w.y;
     }
 }
+// A lane's share of the product of a query and a drafted row.
 template <typename T>
-__device__ __forceinline__ float dot_row(const float (&q)[Running<T>::E], const float (&qk)[2],
-                                         const float (&x)[Running<T>::E], const float (&k)[2]) {
-  float s = qk[0] * k[0] + qk[1] * k[1];
+__device__ __forceinline__ float dot_share(const uint64_t (&q)[Running<T>::E / 2], const float (&qk)[2],
+                                           const uint64_t (&x)[Running<T>::E / 2], const float (&k)[2]) {
+  uint64_t s = ptx::pack2(qk[0] * k[0], qk[1] * k[1]);
 #pragma unroll
-  for (int e = 0; e < Running<T>::E; ++e) s = fmaf(q[e], x[e], s);
-  return warp_sum(s);
+  for (int e = 0; e < Running<T>::E / 2; ++e) s = ptx::fma2(q[e], x[e], s);
+  float lo, hi;
+  ptx::unpack2(s, lo, hi);
+  return lo + hi;
 }
 
 // Where a node stands: its request's first node, the drafted rows that it sees, and its columns' groups.
@@ -352,6 +368,7 @@ struct Place {
   int lo, first_group;
   unsigned long long seen;
 };
+// (Columns fit 31 bits, and a group has a power of two of them.)
 __device__ __forceinline__ Place place_of(const JoinArgs& a, int node, bool refused) {
   Place p = {true, 0, 0, 0};
   if (refused) return p;
@@ -366,13 +383,13 @@ __device__ __forceinline__ Place place_of(const JoinArgs& a, int node, bool refu
 // The parts of a column: x first, y number; z the column inside its group.
 __device__ __forceinline__ int3 parts_of(const JoinArgs& a, const Place& p, int node, int h, bool refused) {
   if (refused) return make_int3(0, 0, 0);
-  const int local = (node - p.lo) * a.heads + h, v = p.first_group + local / a.cols;
+  const int local = (node - p.lo) * a.heads + h, v = p.first_group + (local >> (31 - __clz(a.cols)));
   const int2 parts = a.parts[v];                       // (not set for a group without tiles)
-  return make_int3(parts.x, a.groups[v].w > 0 ? parts.y : 0, local % a.cols);
+  return make_int3(parts.x, a.groups[v].w > 0 ? parts.y : 0, local & (a.cols - 1));
 }
 template <typename T>
 __device__ __forceinline__ void store_column(const JoinArgs& a, long long column, float m, float l, bool failed,
-                                             const float (&acc)[Running<T>::E]) {
+                                             const uint64_t (&acc)[Running<T>::E / 2]) {
   constexpr int V = Running<T>::V, R = Running<T>::R;
   const int lane = threadIdx.x & 31;
   // A node that sees nothing: zeros and minus infinity.
@@ -382,26 +399,33 @@ __device__ __forceinline__ void store_column(const JoinArgs& a, long long column
     if ((j * 32 + lane) * V >= a.f.r) continue;
     float v[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = acc[j * V + e] * inv;
+    for (int e = 0; e < V; e += 2) {
+      ptx::unpack2(acc[(j * V + e) / 2], v[e], v[e + 1]);
+      v[e] *= inv;
+      v[e + 1] *= inv;
+    }
     store_vec(static_cast<T*>(a.out) + column * a.f.r + (j * 32 + lane) * V, v);
   }
   if (a.lse && lane == 0) a.lse[column] = failed ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
-// The join: the online softmax over the drafted rows that a node sees, row after row, and the parts that the attention
-// over the context has left for its columns.  Masked rows are never read, so what they hold cannot reach a
-// result; sums, maxima and products are fp32.  Bound by the parts' bytes when there are many columns, else by the chain
-// of loads.  Two forms:
-//   a warp per node and two heads, which share the rows' loads, for many columns;
-//   with SPLIT a CTA per column, whose warps share rows and parts out, for few: one request of 112 columns in 74 parts
-//   each took 53 us with a warp per column.
+// The join: the softmax over the drafted rows that a node sees, and the parts that the attention over the context has
+// left for its columns; sums, maxima and products are fp32.  Bound by the parts' bytes when there are many columns,
+// else by the chain of loads.  Three forms:
+//   tree_join_split_kernel   a CTA per column, whose warps share rows and parts out, for few columns (112 columns in 74
+//                            parts each: 53 us with a warp per column, 14 so);
+//   tree_join_kernel         a warp per column, row after row;
+//   tree_join_dense_kernel   a CTA per group of 64 columns, all its drafted rows by matrix products, for bf16 with a group
+//                            for every SM (16384 columns that see 6 of 64 rows each: 45 us with a warp per column, 36 so;
+//                            52 groups: 14 us and 25).
+// In the first two masked rows are never read, so what they hold cannot reach a result.
 constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kSplitThreads = 256, kSplitWarps = kSplitThreads / 32;
 
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(JoinArgs a) {
+__global__ void __launch_bounds__(kJoinThreads, 5) tree_join_kernel(JoinArgs a) {
   using Run = Running<T>;
-  constexpr int E = Run::E, HB = 2;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = a.f.r, blocks = ceil_div(a.heads, HB);
+  constexpr int E = Run::E;
+  const int warp = threadIdx.x >> 5, r = a.f.r;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
   bool failed = false;
@@ -409,62 +433,49 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(JoinArgs a) {
   const bool refused = *a.n_groups < 0;
   failed = __syncthreads_or(failed) || refused;
   // Nodes behind the last request are left as they were; those of a refused batch all get NaN.
-  const long long units = (long long)(refused ? a.n_nodes : a.starts[a.batch]) * blocks;
-  for (long long u = (long long)blockIdx.x * kJoinWarps + warp; u < units; u += (long long)gridDim.x * kJoinWarps) {
-    const int node = (int)(u / blocks), h0 = (int)(u % blocks) * HB;
-    const bool two = h0 + 1 < a.heads;
-    float q[HB][E], qk[HB][2];
-#pragma unroll
-    for (int h = 0; h < HB; ++h)
-      load_row<T>(static_cast<const T*>(a.q) + ((long long)node * a.heads + h0 + (two ? h : 0)) * (r + a.f.dr), a.f, q[h],
-                  qk[h]);
+  const uint32_t columns = (uint32_t)(refused ? a.n_nodes : a.starts[a.batch]) * a.heads;
+  for (uint32_t column = blockIdx.x * kJoinWarps + warp; column < columns; column += gridDim.x * kJoinWarps) {
+    const int node = (int)(column / (uint32_t)a.heads), h = (int)(column - (uint32_t)node * a.heads);
+    uint64_t q[E / 2];
+    float qk[2];
+    load_row<T>(static_cast<const T*>(a.q) + (long long)column * (r + a.f.dr), a.f, q, qk);
     Place p = place_of(a, node, refused);
     if (!p.fine) continue;
-    int3 parts[HB];
-#pragma unroll
-    for (int h = 0; h < HB; ++h) parts[h] = parts_of(a, p, node, h0 + (two ? h : 0), refused);
-    Run run[HB];
-#pragma unroll
-    for (int h = 0; h < HB; ++h) run[h].clear();
+    const int3 parts = parts_of(a, p, node, h, refused);
+    float2 ml;
+    uint64_t y[E / 2];
+    auto load_one = [&](int n) {
+      if (n >= parts.y) return;
+      const long long at = (long long)(parts.x + n) * a.cols + parts.z;
+      ml = reinterpret_cast<const float2*>(a.ml_part)[at];
+      load_part<T>(a.o_part + at * r, r, y);
+    };
+    load_one(0);
+    Run run;
+    run.clear();
+    const T* rows = static_cast<const T*>(a.rows) + p.lo * a.row_stride;
     while (p.seen) {
       const int at = __ffsll((long long)p.seen) - 1;
       p.seen &= p.seen - 1;
-      float x[E], k[2];
-      load_row<T>(static_cast<const T*>(a.rows) + (p.lo + at) * a.row_stride, a.f, x, k);
-#pragma unroll
-      for (int h = 0; h < HB; ++h) run[h].add(dot_row<T>(q[h], qk[h], x, k) * a.scale_log2, 1.f, x);
+      uint64_t x[E / 2];
+      float k[2];
+      load_row<T>(rows + at * a.row_stride, a.f, x, k);
+      run.add(warp_sum(dot_share<T>(q, qk, x, k)) * a.scale_log2, 1.f, x);
     }
-    // Both heads' parts together, as long as either has one.
-    const int most = max(parts[0].y, parts[1].y);
-    for (int n = 0; n < most; ++n) {
-      float2 ml[HB];
-      float x[HB][E];
-#pragma unroll
-      for (int h = 0; h < HB; ++h) {
-        const long long at = (long long)(parts[h].x + min(n, max(parts[h].y, 1) - 1)) * a.cols + parts[h].z;
-        ml[h] = make_float2(-INFINITY, 0.f);
-        if (n < parts[h].y) {
-          ml[h] = reinterpret_cast<const float2*>(a.ml_part)[at];
-          load_part<T>(a.o_part + at * r, r, x[h]);
-        }
-      }
-#pragma unroll
-      for (int h = 0; h < HB; ++h)
-        if (n < parts[h].y) run[h].add(ml[h].x, ml[h].y, x[h]);
+    for (int n = 0; n < parts.y; ++n) {
+      run.add(ml.x, ml.y, y);
+      load_one(n + 1);
     }
-#pragma unroll
-    for (int h = 0; h < HB; ++h)
-      if (h == 0 || two)
-        store_column<T>(a, (long long)node * a.heads + h0 + h, run[h].m, run[h].l, failed, run[h].acc);
+    store_column<T>(a, column, run.m, run.l, failed, run.acc);
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSplitThreads) tree_join_split_kernel(JoinArgs a) {
+__global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinArgs a) {
   using Run = Running<T>;
   constexpr int E = Run::E;
   __shared__ float s_m[kSplitWarps], s_l[kSplitWarps];
-  __shared__ float4 s_acc[kSplitWarps][E / 4][32];
+  __shared__ uint64_t s_acc[kSplitWarps][E / 2][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = a.f.r;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
@@ -472,9 +483,9 @@ __global__ void __launch_bounds__(kSplitThreads) tree_join_split_kernel(JoinArgs
   for (int i = threadIdx.x; i < a.n_error_words; i += kSplitThreads) failed |= a.error_words[i] != 0;
   const bool refused = *a.n_groups < 0;
   failed = __syncthreads_or(failed) || refused;
-  const long long columns = (long long)(refused ? a.n_nodes : a.starts[a.batch]) * a.heads;
-  for (long long column = blockIdx.x; column < columns; column += gridDim.x) {
-    const int node = (int)(column / a.heads), h = (int)(column % a.heads);
+  const uint32_t columns = (uint32_t)(refused ? a.n_nodes : a.starts[a.batch]) * a.heads;
+  for (uint32_t column = blockIdx.x; column < columns; column += gridDim.x) {
+    const int node = (int)(column / (uint32_t)a.heads), h = (int)(column - (uint32_t)node * a.heads);
     const Place p = place_of(a, node, refused);
     if (!p.fine) continue;
     const int3 parts = parts_of(a, p, node, h, refused);
@@ -482,27 +493,28 @@ __global__ void __launch_bounds__(kSplitThreads) tree_join_split_kernel(JoinArgs
     run.clear();
     // Rows in turn: the warp's are the set bits number warp, warp + 8, ...
     if (__popcll(p.seen) > warp) {
-      float q[E], qk[2];
-      load_row<T>(static_cast<const T*>(a.q) + column * (r + a.f.dr), a.f, q, qk);
+      uint64_t q[E / 2];
+      float qk[2];
+      load_row<T>(static_cast<const T*>(a.q) + (long long)column * (r + a.f.dr), a.f, q, qk);
       unsigned long long seen = p.seen;
       for (int n = 0; seen; ++n) {
         const int at = __ffsll((long long)seen) - 1;
         seen &= seen - 1;
         if (n % kSplitWarps != warp) continue;
-        float x[E], k[2];
+        uint64_t x[E / 2];
+        float k[2];
         load_row<T>(static_cast<const T*>(a.rows) + (p.lo + at) * a.row_stride, a.f, x, k);
-        run.add(dot_row<T>(q, qk, x, k) * a.scale_log2, 1.f, x);
+        run.add(warp_sum(dot_share<T>(q, qk, x, k)) * a.scale_log2, 1.f, x);
       }
     }
     constexpr int U = 4;                                 // parts whose loads are in flight together
     for (int n0 = warp; n0 < parts.y; n0 += U * kSplitWarps) {
       float2 ml[U];
-      float x[U][E];
+      uint64_t x[U][E / 2];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int n = n0 + i * kSplitWarps;
-        ml[i] = make_float2(-INFINITY, 0.f);
-        if (n >= parts.y) continue;
+        if (n >= parts.y) break;
         const long long at = (long long)(parts.x + n) * a.cols + parts.z;
         ml[i] = reinterpret_cast<const float2*>(a.ml_part)[at];
         load_part<T>(a.o_part + at * r, r, x[i]);
@@ -516,26 +528,304 @@ __global__ void __launch_bounds__(kSplitThreads) tree_join_split_kernel(JoinArgs
       s_l[warp] = run.l;
     }
 #pragma unroll
-    for (int e = 0; e < E; e += 4)
-      s_acc[warp][e / 4][lane] = make_float4(run.acc[e], run.acc[e + 1], run.acc[e + 2], run.acc[e + 3]);
+    for (int e = 0; e < E / 2; ++e) s_acc[warp][e][lane] = run.acc[e];
     __syncthreads();
     if (warp == 0) {
 #pragma unroll 1
       for (int w = 1; w < kSplitWarps; ++w) {            // in the warps' order
-        float x[E];
+        uint64_t x[E / 2];
 #pragma unroll
-        for (int e = 0; e < E; e += 4) {
-          const float4 v = s_acc[w][e / 4][lane];
-          x[e] = v.x;
-          x[e + 1] = v.y;
-          x[e + 2] = v.z;
-          x[e + 3] = v.w;
-        }
+        for (int e = 0; e < E / 2; ++e) x[e] = s_acc[w][e][lane];
         run.add(s_m[w], s_l[w], x);
       }
       store_column<T>(a, column, run.m, run.l, failed, run.acc);
     }
     __syncthreads();
+  }
+}
+
+// bf16, a CTA per group of NC columns, a warp per 16 columns and half of the rows (scores) or of the runs of 32 latents
+// (values); m16n8k16 instructions.  The request's rows lie in shared memory with the
+// pairs of every 32 latents transposed (pair 4 i + j at place 4 j + i): read as they are, they give lane (g, t) the
+// latents 8t .. 8t + 7 of row g, which it also reads of a query in one piece; read transposed, they give the output's
+// fragments eight latents in a row.  A probability enters as two bf16 terms, 2^-17 of it.  A matrix product
+// touches every row, so a row with an infinity or a NaN is taken as zeros, and columns that see it get NaN.
+template <int NC>
+struct Dense {
+  static constexpr int kThreads = NC * 4, kTiles = NC / 16;
+  __host__ __device__ static constexpr int row_bytes(const qp::Format& f) { return 2 * (f.r + f.dr) + 16; }
+  __host__ __device__ static constexpr int bytes(const qp::Format& f) { return kMaxNodes * row_bytes(f); }
+};
+
+template <int NC>
+__global__ void __launch_bounds__(NC * 4, 2) tree_join_dense_kernel(JoinArgs a) {
+  using D = Dense<NC>;
+  extern __shared__ __align__(128) uint8_t rows_s[];
+  __shared__ uint4 p_s[D::kTiles][4][2][32];          // A fragments of 16 columns by 16 rows, two terms
+  __shared__ unsigned long long seen_s[NC];
+  __shared__ float max_s[2][NC], sum_s[2][NC];
+  __shared__ unsigned int bad_s[2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int mt = warp >> 1, half = warp & 1, r = a.f.r, width = r + a.f.dr, stride = D::row_bytes(a.f);
+  if (tid < 2) bad_s[tid] = 0;
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+  bool failed = false;
+  for (int i = tid; i < a.n_error_words; i += D::kThreads) failed |= a.error_words[i] != 0;
+  failed = __syncthreads_or(failed);
+  const int n_groups = *a.n_groups, v = blockIdx.x;
+  bf16* out = static_cast<bf16*>(a.out);
+  if (n_groups < 0) {                                  // the batch is refused
+    const long long n = (long long)a.n_nodes * a.heads, step = (long long)gridDim.x * D::kThreads;
+    const long long first = (long long)v * D::kThreads + tid;
+    for (long long i = first; i < n * r; i += step) out[i] = __float2bfloat16_rn(NAN);
+    for (long long i = first; a.lse && i < n; i += step) a.lse[i] = NAN;
+    return;
+  }
+  if (v >= n_groups) return;
+  const int4 group = a.groups[v];
+  const int lo = a.starts[group.x], count = a.starts[group.x + 1] - lo, n_rows = min(count, kMaxNodes);
+  const int steps = (n_rows + 15) / 16;                // of 16 rows
+  const int2 parts = group.w > 0 ? a.parts[v] : make_int2(0, 0);
+  if (tid < NC) {
+    unsigned long long seen = 0;
+    if (tid < group.z) {
+      seen = (unsigned long long)a.seen[(group.y + tid) / a.heads];
+      if (count < kMaxNodes) seen &= (1ull << count) - 1;
+    }
+    seen_s[tid] = seen;
+  }
+  // ---- rows into shared memory: a warp per row, two in flight, 16 bytes a lane and up to three of those
+  {
+    constexpr int kWarps = D::kThreads / 32;
+    const int runs = width / 8;
+    const bf16* src = static_cast<const bf16*>(a.rows) + (long long)lo * a.row_stride;
+    for (int row0 = warp; row0 < steps * 16; row0 += 2 * kWarps) {
+      uint4 w[2][3];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          const int row = row0 + k * kWarps, c = lane + 32 * i;
+          w[k][i] = make_uint4(0u, 0u, 0u, 0u);
+          if (row < n_rows && c < runs) w[k][i] = *reinterpret_cast<const uint4*>(src + row * a.row_stride + c * 8);
+        }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int row = row0 + k * kWarps;
+        if (row >= steps * 16) break;
+        // A magnitude plus one in its exponent reaches the sign bit for an infinity or a NaN alone.
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          const uint32_t x[4] = {w[k][i].x, w[k][i].y, w[k][i].z, w[k][i].w};
+#pragma unroll
+          for (int m = 0; m < 4; ++m) odd |= (x[m] & 0x7fff7fffu) + 0x00800080u;
+        }
+        const bool bad = __any_sync(0xffffffffu, odd & 0x80008000u);
+        if (bad && lane == 0) atomicOr(&bad_s[row >> 5], 1u << (row & 31));
+        uint32_t* dst = reinterpret_cast<uint32_t*>(rows_s + row * stride + (lane >> 2) * 64) + (lane & 3);
+#pragma unroll
+        for (int i = 0; i < 3; ++i, dst += 128) {
+          if (lane + 32 * i >= runs) break;
+          dst[0] = bad ? 0u : w[k][i].x;
+          dst[4] = bad ? 0u : w[k][i].y;
+          dst[8] = bad ? 0u : w[k][i].z;
+          dst[12] = bad ? 0u : w[k][i].w;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const uint32_t rows_u32 = ptx::smem_u32(rows_s);
+  const int c0 = mt * 16 + g, c1 = c0 + 8;             // this lane's columns
+  // ---- scores of 16 columns by 32 rows
+  float s[4][4];
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
+  {
+    const bf16* q = static_cast<const bf16*>(a.q) + (long long)group.y * width + 8 * t;
+    const uint32_t at = rows_u32 + (half * 32 + (lane & 7)) * stride + (lane >> 3) * 16;
+    const int chunks = width / 32;
+    if (half * 32 < steps * 16) {
+      constexpr int F = 6;                               // runs of a query in flight; r + d_R has at most 18
+      for (int f0 = 0; f0 < chunks; f0 += F) {
+        uint4 q0[F], q1[F];
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+          const int c = f0 + f;
+          q0[f] = q1[f] = make_uint4(0u, 0u, 0u, 0u);
+          if (c < chunks && c0 < group.z) q0[f] = *reinterpret_cast<const uint4*>(q + (long long)c0 * width + c * 32);
+          if (c < chunks && c1 < group.z) q1[f] = *reinterpret_cast<const uint4*>(q + (long long)c1 * width + c * 32);
+        }
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+          if (f0 + f >= chunks) break;
+          const uint32_t a0[4] = {q0[f].x, q1[f].x, q0[f].y, q1[f].y}, a1[4] = {q0[f].z, q1[f].z, q0[f].w, q1[f].w};
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            if (half * 32 + n * 8 >= steps * 16) break;
+            uint32_t w[4];
+            qp::ldsm_x4(at + n * 8 * stride + (f0 + f) * 64, w);
+            qp::mma_bf16(s[n], a0, w[0], w[1]);
+            qp::mma_bf16(s[n], a1, w[2], w[3]);
+          }
+        }
+      }
+    }
+  }
+  // ---- softmax over the rows that each column sees: bits of row half * 32 + 8 n + 2 t + e
+  const uint32_t see0 = (uint32_t)(seen_s[c0] >> (32 * half)), see1 = (uint32_t)(seen_s[c1] >> (32 * half));
+  const unsigned long long bad = bad_s[0] | (unsigned long long)bad_s[1] << 32;
+  float top0 = -INFINITY, top1 = -INFINITY;
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t bit = 1u << (8 * n + 2 * t + e);
+      s[n][e] = see0 & bit ? s[n][e] * a.scale_log2 : -INFINITY;
+      s[n][2 + e] = see1 & bit ? s[n][2 + e] * a.scale_log2 : -INFINITY;
+      top0 = fmaxf(top0, s[n][e]);
+      top1 = fmaxf(top1, s[n][2 + e]);
+    }
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    top0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, o));
+    top1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, o));
+  }
+  if (t == 0) {
+    max_s[half][c0] = top0;
+    max_s[half][c1] = top1;
+  }
+  __syncthreads();
+  const float m0 = fmaxf(max_s[0][c0], max_s[1][c0]), m1 = fmaxf(max_s[0][c1], max_s[1][c1]);
+  const float ref0 = m0 == -INFINITY ? 0.f : m0, ref1 = m1 == -INFINITY ? 0.f : m1;
+  float sum0 = 0.f, sum1 = 0.f;
+  uint32_t hi[4][2], low[4][2];                        // [n-tile][column]
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const float p0 = exp2f(s[n][2 * c] - (c ? ref1 : ref0)), p1 = exp2f(s[n][2 * c + 1] - (c ? ref1 : ref0));
+      (c ? sum1 : sum0) += p0 + p1;
+      const __nv_bfloat162 x = __floats2bfloat162_rn(p0, p1);
+      const __nv_bfloat162 y = __floats2bfloat162_rn(p0 - __low2float(x), p1 - __high2float(x));
+      hi[n][c] = *reinterpret_cast<const uint32_t*>(&x);
+      low[n][c] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    sum0 += __shfl_xor_sync(0xffffffffu, sum0, o);
+    sum1 += __shfl_xor_sync(0xffffffffu, sum1, o);
+  }
+  if (t == 0) {
+    sum_s[half][c0] = sum0;
+    sum_s[half][c1] = sum1;
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    p_s[mt][half * 2 + k][0][lane] = make_uint4(hi[2 * k][0], hi[2 * k][1], hi[2 * k + 1][0], hi[2 * k + 1][1]);
+    p_s[mt][half * 2 + k][1][lane] = make_uint4(low[2 * k][0], low[2 * k][1], low[2 * k + 1][0], low[2 * k + 1][1]);
+  }
+  __syncthreads();
+  // ---- references and denominators of the whole, this lane's two columns
+  float whole_m[2] = {m0, m1}, whole_l[2] = {sum_s[0][c0] + sum_s[1][c0], sum_s[0][c1] + sum_s[1][c1]}, drafted[2];
+  const float2* ml = reinterpret_cast<const float2*>(a.ml_part) + (long long)parts.x * NC;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int col = c ? c1 : c0;
+    float m = whole_m[c];
+    if (col < group.z)
+#pragma unroll 4
+      for (int n = 0; n < parts.y; ++n) m = fmaxf(m, ml[n * NC + col].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    drafted[c] = exp2f(whole_m[c] - ref);
+    float l = whole_l[c] * drafted[c];
+    if (col < group.z)
+#pragma unroll 4
+      for (int n = 0; n < parts.y; ++n) {
+        const float2 x = ml[n * NC + col];
+        l += exp2f(x.x - ref) * x.y;
+      }
+    if (failed || (seen_s[col] & bad)) l = NAN;
+    whole_m[c] = ref;
+    whole_l[c] = l;
+    if (a.lse && half == 0 && t == 0 && col < group.z)
+      a.lse[group.y + col] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
+  }
+  // ---- values: runs of 32 latents, every second is this warp's
+  const float inv[2] = {whole_l[0] == 0.f ? 0.f : 1.f / whole_l[0], whole_l[1] == 0.f ? 0.f : 1.f / whole_l[1]};
+  for (int c = half; c < r / 32; c += 2) {
+    // The first parts' loads go ahead of the products.
+    constexpr int F = 2;
+    float4 x0[2][F], x1[2][F];
+    float w_part[2][F];
+    auto load_parts = [&](int n0) {
+#pragma unroll
+      for (int col2 = 0; col2 < 2; ++col2)
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+          const int col = col2 ? c1 : c0, n = n0 + f;
+          x0[col2][f] = x1[col2][f] = make_float4(0.f, 0.f, 0.f, 0.f);
+          w_part[col2][f] = 0.f;
+          if (n < parts.y && col < group.z) {
+            const float* part = a.o_part + ((long long)(parts.x + n) * NC + col) * r + c * 32 + 8 * t;
+            x0[col2][f] = *reinterpret_cast<const float4*>(part);
+            x1[col2][f] = *reinterpret_cast<const float4*>(part + 4);
+            w_part[col2][f] = exp2f(ml[n * NC + col].x - whole_m[col2]);
+          }
+        }
+    };
+    load_parts(0);
+    float o[4][4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
+    // Rows k * 16 + ..: matrices of rows 0 .. 7 and 8 .. 15 at places 8 n and 8 n + 8.
+    const uint32_t at = rows_u32 + (lane & 15) * stride + c * 64 + (lane >> 4) * 16;
+    for (int k = 0; k < steps; ++k) {
+      const uint4 x = p_s[mt][k][0][lane], y = p_s[mt][k][1][lane];
+      const uint32_t p0[4] = {x.x, x.y, x.z, x.w}, p1[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int n = 0; n < 4; n += 2) {
+        uint32_t w[4];
+        qp::ldsm_x4_trans(at + k * 16 * stride + n * 16, w);
+        qp::mma_bf16(o[n], p0, w[0], w[1]);
+        qp::mma_bf16(o[n + 1], p0, w[2], w[3]);
+        qp::mma_bf16(o[n], p1, w[0], w[1]);
+        qp::mma_bf16(o[n + 1], p1, w[2], w[3]);
+      }
+    }
+    // Fragment column 2t + e of tile n is latent 8t + 2n + e: eight in a row.
+    float y[2][8];
+#pragma unroll
+    for (int col2 = 0; col2 < 2; ++col2)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[col2][i] = o[i / 2][2 * col2 + i % 2] * drafted[col2];
+    for (int n0 = 0; n0 < parts.y; n0 += F) {
+#pragma unroll
+      for (int col2 = 0; col2 < 2; ++col2)
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+          const float w = w_part[col2][f];
+          const float4 u = x0[col2][f], v4 = x1[col2][f];
+          const float x[8] = {u.x, u.y, u.z, u.w, v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[col2][i] = fmaf(w, x[i], y[col2][i]);
+        }
+      if (n0 + F < parts.y) load_parts(n0 + F);
+    }
+#pragma unroll
+    for (int col2 = 0; col2 < 2; ++col2) {
+      const int col = col2 ? c1 : c0;
+      if (col >= group.z) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[col2][i] *= inv[col2];
+      store_vec(out + (long long)(group.y + col) * r + c * 32 + 8 * t, y[col2]);
+    }
   }
 }
 
