@@ -5,6 +5,7 @@
 #include "ops_common.cuh"
 #include "qweight_format.cuh"
 #include "qweight_kernels.cuh"
+#include "qweight_tc.cuh"
 
 using namespace mtla;
 using namespace mtla::ops;
@@ -39,6 +40,70 @@ template <typename T, int NT>
 int launch_product(const qw::ProductArgs& a, cudaStream_t st) {
   return launch_dependent(qw::qweight_product_kernel<T, NT>, dim3(a.s.out_blocks(), ceil_div(a.n, 8 * NT)), qw::kThreads,
                           0, st, a);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_tiled_fn() {
+  static std::atomic<EncodeTiledFn> known{nullptr};
+  EncodeTiledFn fn = known.load(std::memory_order_acquire);
+  if (fn) return fn;
+  void* p = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
+      found != cudaDriverEntryPointSuccess)
+    return nullptr;
+  fn = reinterpret_cast<EncodeTiledFn>(p);
+  known.store(fn, std::memory_order_release);
+  return fn;
+}
+
+// Rows of x in boxes of `box` rows by 64 inputs (the swizzle's span); zeros outside.
+bool make_x_map(CUtensorMap* map, const qw::ProductArgs& a, int box) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)a.s.n_in, (cuuint64_t)a.n}, strides[1] = {(cuuint64_t)a.x_stride * 2};
+  const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, steps[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, boxes, steps,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int BN, int MT>
+int launch_product_tc(const qw::ProductArgs& p, const OnDeviceOf& dev, cudaStream_t st) {
+  using C = qw::tc::Config<BN, MT>;
+  if (!raise_smem<qw::tc::qweight_tc_kernel<BN, MT>>(dev.device(), C::kBytes)) return MTLA_ERR_CUDA;
+  CUtensorMap map;
+  if (!make_x_map(&map, p, BN)) return MTLA_ERR_CUDA;
+  qw::tc::Args a;
+  a.packed = p.packed;
+  a.y = static_cast<bf16*>(p.y);
+  a.y_stride = p.y_stride;
+  a.n = p.n;
+  a.s = p.s;
+  const int tiles = ceil_div(p.s.n_out, MT * qw::tc::kTile), row_tiles = ceil_div(p.n, BN);
+  // The inputs are shared out, at least four blocks of 128 a CTA, as long as all CTAs run at once.
+  const long long at_once = (long long)dev.sm_count() * (C::kAlloc == 256 ? 2 : 1);
+  a.splits = 1;
+  while (a.splits < 8 && 2ll * a.splits * tiles * row_tiles <= at_once && p.s.in_blocks() >= 8 * a.splits) a.splits *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * a.splits), (unsigned)row_tiles);
+  cfg.blockDim = dim3(qw::tc::kThreads);
+  cfg.dynamicSmemBytes = C::kBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.splits;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.splits > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, qw::tc::qweight_tc_kernel<BN, MT>, map, a) == cudaSuccess) return MTLA_OK;
+  cudaGetLastError();
+  return MTLA_ERR_CUDA;
 }
 
 }  // namespace
@@ -79,9 +144,14 @@ int mtla_qweight_product(const void* packed, int32_t n_in, int32_t n_out, const 
   a.n = n;
   a.s = qw::Shape{n_in, n_out};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dtype == MTLA_DTYPE_BF16 && n > 16) {
+    if (n <= 32) return launch_product_tc<32, 1>(a, dev, st);
+    if (n <= 64) return launch_product_tc<64, 1>(a, dev, st);
+    if (n <= 128) return launch_product_tc<128, 1>(a, dev, st);
+    return launch_product_tc<128, 2>(a, dev, st);
+  }
   if (dtype == MTLA_DTYPE_BF16)
-    return n <= 8 ? launch_product<bf16, 1>(a, st) : n <= 16 ? launch_product<bf16, 2>(a, st)
-                                                              : launch_product<bf16, 4>(a, st);
+    return n <= 8 ? launch_product<bf16, 1>(a, st) : launch_product<bf16, 2>(a, st);
   return n <= 8 ? launch_product<float, 1>(a, st) : launch_product<float, 2>(a, st);
 }
 

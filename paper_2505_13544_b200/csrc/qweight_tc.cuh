@@ -1,0 +1,266 @@
+// Products of many bf16 rows with 4-bit weights on the fifth-generation tensor cores.
+//
+// A CTA has MT tiles of 128 outputs by BN rows of x and a share of the inputs.  The weights are the A operand: expanding
+// warps decode 64 inputs of a tile from the raw blocks in shared memory into bf16 (exactly, times 2^-13) and write them
+// to tensor memory, the rows of x are the B operand, which a tensor map brings into shared memory with its 128-byte
+// swizzle.  So the weights' 4 bits are all that travels of them, and x is what costs: a panel of BN rows is
+// read by every CTA along the outputs, hence two tiles of outputs per CTA where there are many rows.  Bound by the
+// matrix unit then (128 x BN x 16 in BN / 2 cycles), by the blocks' bytes with few rows; expanding a unit of 64 inputs
+// takes about 150 cycles of the issue slots, against 2 BN of the matrix unit.
+//
+// With few tiles of outputs the inputs are shared out among the CTAs of a cluster, which add their sums through
+// distributed shared memory in rank order.  Every wait is bounded; should one give up, the tile's results are NaN.
+//
+// Roles (12 warps): warp 0 fetches, warp 1 issues, warp 2 owns the tensor memory, warps 4-11 expand (two groups of
+// four) and then write the results.
+#pragma once
+
+#include "qpool_attn.cuh"
+#include "qweight_kernels.cuh"
+
+namespace mtla {
+namespace qw {
+namespace tc {
+
+constexpr int kThreads = 384, kExpandWarp0 = 4, kExpandThreads = 256;
+constexpr int kTile = 128;                         // outputs of a tile: eight blocks
+constexpr int kRawStages = 4;
+
+template <int BN, int MT>
+struct Config {
+  static constexpr int kCols = MT * BN;                             // tensor memory of the sums
+  static constexpr int kAlloc = kCols <= 128 ? 256 : 512;
+  static constexpr int kUnits = (kAlloc - kCols) / 32 < 8 ? (kAlloc - kCols) / 32 : 8;      // buffers of 64 inputs
+  static constexpr int kPanel = BN * 128;                           // 64 inputs of BN rows
+  static constexpr int kStages = kAlloc == 256 ? (BN == 128 ? 4 : 6) : 8;
+  static constexpr int kRaw = MT * 8 * kBlockBytes;
+  static constexpr int kSums = kCols * kTile * 4;                   // a cluster's sums lie where the panels were
+  static constexpr int kPanels = kStages * kPanel > kSums ? kStages * kPanel : kSums;
+  static constexpr int kBytes = kPanels + kRawStages * kRaw + 1024;
+  static_assert(kBytes <= (kAlloc == 256 ? 113 : 226) * 1024, "shared memory budget");
+};
+
+struct Args {
+  const uint8_t* packed;
+  bf16* y;
+  long long y_stride;
+  int n, splits;
+  Shape s;
+};
+
+struct Misc {
+  unsigned long long raw_full[kRawStages], raw_empty[kRawStages], b_full[8], b_empty[8], a_full[8], a_empty[8], done;
+  uint32_t tmem_base;
+  int failed;
+};
+
+__device__ __forceinline__ uint32_t load_cluster(uint32_t addr, uint32_t rank) {
+  uint32_t remote, v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int BN, int MT>
+__global__ void __launch_bounds__(kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 1)
+    qweight_tc_kernel(const __grid_constant__ CUtensorMap x_map, Args a) {
+  using namespace ptx;
+  using C = Config<BN, MT>;
+  constexpr uint32_t IDESC = make_idesc_bf16(128, BN, 0, 0);
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Misc misc;
+  const uint32_t raw_base = smem_u32(smem_raw), base = (raw_base + 1023u) & ~1023u;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  auto bar = [&](unsigned long long& p) { return smem_u32(&p); };
+  if (threadIdx.x < 8) {
+    const int i = threadIdx.x;
+    if (i < kRawStages) {
+      mbar_init(bar(misc.raw_full[i]), 1);
+      mbar_init(bar(misc.raw_empty[i]), kExpandThreads / 32);
+    }
+    mbar_init(bar(misc.b_full[i]), 1);
+    mbar_init(bar(misc.b_empty[i]), 1);
+    mbar_init(bar(misc.a_full[i]), 4);
+    mbar_init(bar(misc.a_empty[i]), 1);
+    if (i == 0) {
+      mbar_init(bar(misc.done), 1);
+      misc.failed = 0;
+    }
+    mbar_fence_init();
+  }
+  if (warp == 2) tmem_alloc(smem_u32(&misc.tmem_base), C::kAlloc);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = misc.tmem_base;
+  grid_launch_dependents();
+  grid_dependency_wait();
+
+  const int rank = a.splits > 1 ? (int)blockIdx.x % a.splits : 0, tile = (int)blockIdx.x / a.splits;
+  const int kbs = a.s.in_blocks(), ob0 = tile * MT * 8, obs = min(MT * 8, a.s.out_blocks() - ob0);
+  const int kb0 = (int)((long long)kbs * rank / a.splits), n_kb = (int)((long long)kbs * (rank + 1) / a.splits) - kb0;
+  const int n0 = blockIdx.y * BN, n_units = 2 * n_kb;              // of 64 inputs
+  const uint32_t raw_u32 = base + C::kPanels;
+  auto wait = [&](unsigned long long& b, int phase) { return mbar_wait_compact(bar(b), phase & 1); };
+  auto wait_warp = [&](unsigned long long& b, int phase) { return __all_sync(0xffffffffu, wait(b, phase)) != 0; };
+  bool ok = true;                    // false once a wait of this thread has given up
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- producer
+    if (lane == 0) {
+      for (int u = 0; u < n_units && ok; ++u) {
+        if (!(u & 1)) {
+          const int kb = u >> 1, st = kb % kRawStages;
+          ok = wait(misc.raw_empty[st], kb / kRawStages + 1);
+          if (!ok) break;
+          const uint32_t full = bar(misc.raw_full[st]);
+          mbar_arrive_expect_tx(full, obs * kBlockBytes);
+          for (int b = 0; b < obs; ++b)
+            bulk_load(raw_u32 + st * C::kRaw + b * kBlockBytes,
+                      a.packed + ((long long)(ob0 + b) * kbs + kb0 + kb) * kBlockBytes, kBlockBytes, full);
+        }
+        const int st = u % C::kStages;
+        ok = wait(misc.b_empty[st], u / C::kStages + 1);
+        if (!ok) break;
+        mbar_arrive_expect_tx(bar(misc.b_full[st]), C::kPanel);
+        tma_load_2d(base + st * C::kPanel, &x_map, bar(misc.b_full[st]), kb0 * kInputs + u * 64, n0);
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- issuer (whole warp, uniform)
+    const uint64_t b_desc = make_smem_desc(base, 16, 1024, kSwizzle128B);
+    int st = 0, st_round = 0, buf = 0, buf_round = 0;
+    for (int u = 0; u < n_units && ok; ++u) {
+      ok = wait_warp(misc.b_full[st], st_round);
+      if (!ok) break;
+      const uint32_t panel = (uint32_t)b_desc + st * (C::kPanel / 16), hi = (uint32_t)(b_desc >> 32);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        ok = wait_warp(misc.a_full[buf], buf_round);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t d = tmem + m * BN, at = tmem + C::kCols + buf * 32;
+        if (elect_one()) {
+          mma_f16_ts(d, at, panel, hi, IDESC, u > 0);
+#pragma unroll
+          for (int i = 1; i < 4; ++i) mma_f16_ts(d, at + i * 8, panel + i * 2, hi, IDESC, 1u);
+          mma_commit(bar(misc.a_empty[buf]));
+        }
+        __syncwarp();
+        if (++buf == C::kUnits) { buf = 0; ++buf_round; }
+      }
+      if (!ok) break;
+      if (elect_one()) mma_commit(bar(misc.b_empty[st]));
+      __syncwarp();
+      if (++st == C::kStages) { st = 0; ++st_round; }
+    }
+    if (ok && elect_one()) mma_commit(bar(misc.done));
+    __syncwarp();
+  } else if (warp >= kExpandWarp0) {
+    // ---------------------------------------------------------------- expansion
+    // Unit u of tile m has number u MT + m; group grp takes tile grp (MT = 2) or every second unit (MT = 1).
+    const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2, o = q * 32 + lane, i = o & 15;
+    const uint32_t block = raw_u32 + ((MT == 2 ? grp * 8 : 0) + (o >> 4)) * kBlockBytes;
+    const uint32_t twist = (uint32_t)(i >> 1 & 3) * 16, row = block + i * 64;
+    const uint32_t scales = block + kCodeBytes + 8 * (i & 7) + (i >> 3);
+    const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16) + C::kCols;
+    int st = 0, round = 0;
+    for (int kb = 0; kb < n_kb && ok; ++kb) {
+      ok = wait_warp(misc.raw_full[st], round);
+      if (!ok) break;
+#pragma unroll 1
+      for (int h = MT == 2 ? 0 : grp; h < 2; h += MT == 2 ? 1 : 2) {
+        const int k = MT == 2 ? (2 * kb + h) * 2 + grp : 2 * kb + h;     // the unit's number
+        const uint32_t at = st * C::kRaw;
+        const uint4 w0 = qp::lds128(row + at + ((uint32_t)(h * 32) ^ twist));
+        const uint4 w1 = qp::lds128(row + at + ((uint32_t)(h * 32 + 16) ^ twist));
+        const uint32_t s0 = scale_b2(qp::lds_u8(scales + at + 4 * h)), s1 = scale_b2(qp::lds_u8(scales + at + 4 * h + 2));
+        const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+        uint32_t x[32];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          uint32_t r[4];
+          decode8(word[e], r);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) x[4 * e + m] = mul_b2(r[m], e < 4 ? s0 : s1);
+        }
+        const int buf = k % C::kUnits;
+        if (k >= C::kUnits) {
+          ok = wait_warp(misc.a_empty[buf], k / C::kUnits + 1);
+          if (!ok) break;
+          tc_fence_after_sync();
+        }
+        tmem_st_x32(lane_tm + buf * 32, x);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(misc.a_full[buf]));
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(misc.raw_empty[st]));
+      if (++st == kRawStages) { st = 0; ++round; }
+    }
+    if (ok) ok = wait(misc.done, 0);
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) misc.failed = 1;
+    named_sync<1, kExpandThreads>();
+    const bool failed = *reinterpret_cast<volatile int*>(&misc.failed) != 0;
+    tc_fence_after_sync();
+    // ---------------------------------------------------------------- results: lane = output, columns = rows of x
+    for (int c0 = 0; c0 < MT * BN; c0 += 32) {
+      if ((c0 / 32 & 1) != grp) continue;                    // the groups take pieces of 32 columns in turn
+      uint32_t v[32];
+      tmem_ld_x32(tmem + ((uint32_t)(q * 32) << 16) + c0, v);
+      tmem_wait_ld();
+      if (a.splits > 1) {
+        float* sums = reinterpret_cast<float*>(smem_raw + (base - raw_base)) + (long long)c0 * kTile + o;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) sums[j * kTile] = __uint_as_float(v[j]);
+      } else {
+        const int out = (ob0 * kRows) + c0 / BN * kTile + o, n = n0 + c0 % BN;
+        bf16* dst = a.y + n * a.y_stride + out;
+        if (out < a.s.n_out) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (n + j < a.n) dst[j * a.y_stride] = __float2bfloat16_rn(failed ? NAN : __uint_as_float(v[j]) * kUnit);
+        }
+      }
+    }
+    tc_fence_before_sync();
+  }
+  if (!ok) misc.failed = 1;
+  __syncwarp();
+  if (a.splits > 1) {
+    cluster_sync();
+    // This CTA's share of the columns: all CTAs' sums in rank order.
+    const int lo = MT * BN * rank / a.splits, hi = MT * BN * (rank + 1) / a.splits;
+    bool failed = false;
+    for (int s = 0; s < a.splits; ++s) failed |= load_cluster(smem_u32(&misc.failed), s) != 0;
+    for (int e = lo * kTile + threadIdx.x; e < hi * kTile; e += kThreads) {
+      const int c = e / kTile, o = e % kTile, out = ob0 * kRows + c / BN * kTile + o, n = n0 + c % BN;
+      float v = 0.f;
+      for (int s = 0; s < a.splits; ++s) v += __uint_as_float(load_cluster(base + e * 4, s));
+      if (out < a.s.n_out && n < a.n) a.y[n * a.y_stride + out] = __float2bfloat16_rn(failed ? NAN : v * kUnit);
+    }
+    __syncwarp();
+    cluster_sync();                                          // the sums are read by others until here
+  }
+  __syncthreads();
+  if (*reinterpret_cast<volatile int*>(&misc.failed)) {
+    // Give copies that may still be in flight time to land before the CTA's memory is reused.
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 100000ull) __nanosleep(1000);
+  }
+  if (warp == 2) {
+    __syncwarp();
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, C::kAlloc);
+  }
+}
+
+}  // namespace tc
+}  // namespace qw
+}  // namespace mtla
