@@ -90,7 +90,7 @@ int launch_product_tc(const qw::ProductArgs& p, const OnDeviceOf& dev, cudaStrea
   while (a.splits < 8 && 2ll * a.splits * tiles * row_tiles <= at_once && p.s.in_blocks() >= 8 * a.splits) a.splits *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * a.splits), (unsigned)row_tiles);
-  cfg.blockDim = dim3(qw::tc::kThreads);
+  cfg.blockDim = dim3(C::kThreads);
   cfg.dynamicSmemBytes = C::kBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];

@@ -11,8 +11,10 @@
 // With few tiles of outputs the inputs are shared out among the CTAs of a cluster, which add their sums through
 // distributed shared memory in rank order.  Every wait is bounded; should one give up, the tile's results are NaN.
 //
-// Roles (12 warps): warp 0 fetches, warp 1 issues, warp 2 owns the tensor memory, warps 4-11 expand (two groups of
-// four) and then write the results.
+// Roles: warp 0 fetches x, warp 3 the weights (one thread for both took 1900 cycles to issue a block of 16 copies),
+// warp 1 issues, warp 2 owns the tensor memory, the others from warp 4 on expand, four for every
+// unit of a block (MT tiles by two halves of the inputs), and then write the results.  (Half as many for MT = 2: 48 us
+// for 512 rows of 4096 x 6720, each unit taking its warps some 1400 cycles.)
 #pragma once
 
 #include "qpool_attn.cuh"
@@ -22,12 +24,13 @@ namespace mtla {
 namespace qw {
 namespace tc {
 
-constexpr int kThreads = 384, kExpandWarp0 = 4, kExpandThreads = 256;
+constexpr int kExpandWarp0 = 4;
 constexpr int kTile = 128;                         // outputs of a tile: eight blocks
 constexpr int kRawStages = 4;
 
 template <int BN, int MT>
 struct Config {
+  static constexpr int kGroups = 2 * MT, kExpandThreads = kGroups * 128, kThreads = kExpandWarp0 * 32 + kExpandThreads;
   static constexpr int kCols = MT * BN;                             // tensor memory of the sums
   static constexpr int kAlloc = kCols <= 128 ? 256 : 512;
   static constexpr int kUnits = (kAlloc - kCols) / 32 < 8 ? (kAlloc - kCols) / 32 : 8;      // buffers of 64 inputs
@@ -65,7 +68,7 @@ __device__ __forceinline__ void cluster_sync() {
 }
 
 template <int BN, int MT>
-__global__ void __launch_bounds__(kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 1)
+__global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 1)
     qweight_tc_kernel(const __grid_constant__ CUtensorMap x_map, Args a) {
   using namespace ptx;
   using C = Config<BN, MT>;
@@ -79,7 +82,7 @@ __global__ void __launch_bounds__(kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 
     const int i = threadIdx.x;
     if (i < kRawStages) {
       mbar_init(bar(misc.raw_full[i]), 1);
-      mbar_init(bar(misc.raw_empty[i]), kExpandThreads / 32);
+      mbar_init(bar(misc.raw_empty[i]), C::kExpandThreads / 32);
     }
     mbar_init(bar(misc.b_full[i]), 1);
     mbar_init(bar(misc.b_empty[i]), 1);
@@ -109,25 +112,28 @@ __global__ void __launch_bounds__(kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 
   bool ok = true;                    // false once a wait of this thread has given up
 
   if (warp == 0) {
-    // ---------------------------------------------------------------- producer
+    // ---------------------------------------------------------------- rows of x
     if (lane == 0) {
       for (int u = 0; u < n_units && ok; ++u) {
-        if (!(u & 1)) {
-          const int kb = u >> 1, st = kb % kRawStages;
-          ok = wait(misc.raw_empty[st], kb / kRawStages + 1);
-          if (!ok) break;
-          const uint32_t full = bar(misc.raw_full[st]);
-          mbar_arrive_expect_tx(full, obs * kBlockBytes);
-          for (int b = 0; b < obs; ++b)
-            bulk_load(raw_u32 + st * C::kRaw + b * kBlockBytes,
-                      a.packed + ((long long)(ob0 + b) * kbs + kb0 + kb) * kBlockBytes, kBlockBytes, full);
-        }
         const int st = u % C::kStages;
         ok = wait(misc.b_empty[st], u / C::kStages + 1);
         if (!ok) break;
         mbar_arrive_expect_tx(bar(misc.b_full[st]), C::kPanel);
         tma_load_2d(base + st * C::kPanel, &x_map, bar(misc.b_full[st]), kb0 * kInputs + u * 64, n0);
       }
+    }
+  } else if (warp == 3) {
+    // ---------------------------------------------------------------- weights: a lane per block of outputs
+    const uint8_t* src = a.packed + ((long long)(ob0 + min(lane, obs - 1)) * kbs + kb0) * kBlockBytes;
+    int st = 0, round = 0;
+    for (int kb = 0; kb < n_kb && ok; ++kb, src += kBlockBytes) {
+      ok = wait_warp(misc.raw_empty[st], round + 1);
+      if (!ok) break;
+      const uint32_t full = bar(misc.raw_full[st]);
+      if (lane == 0) mbar_arrive_expect_tx(full, obs * kBlockBytes);
+      __syncwarp();
+      if (lane < obs) bulk_load(raw_u32 + st * C::kRaw + lane * kBlockBytes, src, kBlockBytes, full);
+      if (++st == kRawStages) { st = 0; ++round; }
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- issuer (whole warp, uniform)
@@ -161,23 +167,23 @@ __global__ void __launch_bounds__(kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 
     __syncwarp();
   } else if (warp >= kExpandWarp0) {
     // ---------------------------------------------------------------- expansion
-    // Unit u of tile m has number u MT + m; group grp takes tile grp (MT = 2) or every second unit (MT = 1).
+    // Unit u of tile m has number u MT + m; group grp has tile grp % MT and half grp / MT of every block.
     const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2, o = q * 32 + lane, i = o & 15;
-    const uint32_t block = raw_u32 + ((MT == 2 ? grp * 8 : 0) + (o >> 4)) * kBlockBytes;
+    const int h = grp / MT;
+    const uint32_t block = raw_u32 + (grp % MT * 8 + (o >> 4)) * kBlockBytes;
     const uint32_t twist = (uint32_t)(i >> 1 & 3) * 16, row = block + i * 64;
-    const uint32_t scales = block + kCodeBytes + 8 * (i & 7) + (i >> 3);
+    const uint32_t chunk0 = (uint32_t)(h * 32) ^ twist, chunk1 = (uint32_t)(h * 32 + 16) ^ twist;
+    const uint32_t scales = block + kCodeBytes + 8 * (i & 7) + (i >> 3) + 4 * h;
     const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16) + C::kCols;
     int st = 0, round = 0;
     for (int kb = 0; kb < n_kb && ok; ++kb) {
       ok = wait_warp(misc.raw_full[st], round);
       if (!ok) break;
-#pragma unroll 1
-      for (int h = MT == 2 ? 0 : grp; h < 2; h += MT == 2 ? 1 : 2) {
-        const int k = MT == 2 ? (2 * kb + h) * 2 + grp : 2 * kb + h;     // the unit's number
+      {
+        const int k = (2 * kb + h) * MT + grp % MT;      // the unit's number
         const uint32_t at = st * C::kRaw;
-        const uint4 w0 = qp::lds128(row + at + ((uint32_t)(h * 32) ^ twist));
-        const uint4 w1 = qp::lds128(row + at + ((uint32_t)(h * 32 + 16) ^ twist));
-        const uint32_t s0 = scale_b2(qp::lds_u8(scales + at + 4 * h)), s1 = scale_b2(qp::lds_u8(scales + at + 4 * h + 2));
+        const uint4 w0 = qp::lds128(row + at + chunk0), w1 = qp::lds128(row + at + chunk1);
+        const uint32_t s0 = scale_b2(qp::lds_u8(scales + at)), s1 = scale_b2(qp::lds_u8(scales + at + 2));
         const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
         uint32_t x[32];
 #pragma unroll
@@ -187,6 +193,8 @@ __global__ void __launch_bounds__(kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 
 #pragma unroll
           for (int m = 0; m < 4; ++m) x[4 * e + m] = mul_b2(r[m], e < 4 ? s0 : s1);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(misc.raw_empty[st]));
         const int buf = k % C::kUnits;
         if (k >= C::kUnits) {
           ok = wait_warp(misc.a_empty[buf], k / C::kUnits + 1);
@@ -199,19 +207,17 @@ __global__ void __launch_bounds__(kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(misc.a_full[buf]));
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(misc.raw_empty[st]));
       if (++st == kRawStages) { st = 0; ++round; }
     }
     if (ok) ok = wait(misc.done, 0);
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) misc.failed = 1;
-    named_sync<1, kExpandThreads>();
+    named_sync<1, C::kExpandThreads>();
     const bool failed = *reinterpret_cast<volatile int*>(&misc.failed) != 0;
     tc_fence_after_sync();
     // ---------------------------------------------------------------- results: lane = output, columns = rows of x
     for (int c0 = 0; c0 < MT * BN; c0 += 32) {
-      if ((c0 / 32 & 1) != grp) continue;                    // the groups take pieces of 32 columns in turn
+      if (c0 / 32 % C::kGroups != grp) continue;                    // the groups take pieces of 32 columns in turn
       uint32_t v[32];
       tmem_ld_x32(tmem + ((uint32_t)(q * 32) << 16) + c0, v);
       tmem_wait_ld();
@@ -239,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 
     const int lo = MT * BN * rank / a.splits, hi = MT * BN * (rank + 1) / a.splits;
     bool failed = false;
     for (int s = 0; s < a.splits; ++s) failed |= load_cluster(smem_u32(&misc.failed), s) != 0;
-    for (int e = lo * kTile + threadIdx.x; e < hi * kTile; e += kThreads) {
+    for (int e = lo * kTile + threadIdx.x; e < hi * kTile; e += C::kThreads) {
       const int c = e / kTile, o = e % kTile, out = ob0 * kRows + c / BN * kTile + o, n = n0 + c % BN;
       float v = 0.f;
       for (int s = 0; s < a.splits; ++s) v += __uint_as_float(load_cluster(base + e * 4, s));
