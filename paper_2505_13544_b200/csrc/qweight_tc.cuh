@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
   const int n0 = blockIdx.y * BN, n_units = 2 * n_kb;              // of 64 inputs
   const uint32_t raw_u32 = base + C::kPanels;
   auto wait = [&](unsigned long long& b, int phase) { return mbar_wait_compact(bar(b), phase & 1); };
-  auto wait_warp = [&](unsigned long long& b, int phase) { return __all_sync(0xffffffffu, wait(b, phase)) != 0; };
+  auto wait_warp = [&](unsigned long long& b, int phase) { return mbar_wait_eager(bar(b), phase & 1); };
   bool ok = true;                    // false once a wait of this thread has given up
 
   if (warp == 0) {
@@ -139,24 +139,26 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
     // ---------------------------------------------------------------- issuer (whole warp, uniform)
     const uint64_t b_desc = make_smem_desc(base, 16, 1024, kSwizzle128B);
     int st = 0, st_round = 0, buf = 0, buf_round = 0;
+    bool there = false;              // the next unit, asked for before the instructions in front of it are issued
     for (int u = 0; u < n_units && ok; ++u) {
       ok = wait_warp(misc.b_full[st], st_round);
       if (!ok) break;
       const uint32_t panel = (uint32_t)b_desc + st * (C::kPanel / 16), hi = (uint32_t)(b_desc >> 32);
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        ok = wait_warp(misc.a_full[buf], buf_round);
+        ok = __all_sync(0xffffffffu, there) || wait_warp(misc.a_full[buf], buf_round);
         if (!ok) break;
         tc_fence_after_sync();
-        const uint32_t d = tmem + m * BN, at = tmem + C::kCols + buf * 32;
+        const uint32_t d = tmem + m * BN, at = tmem + C::kCols + buf * 32, empty = bar(misc.a_empty[buf]);
+        if (++buf == C::kUnits) { buf = 0; ++buf_round; }
+        there = mbar_test(bar(misc.a_full[buf]), buf_round & 1);
         if (elect_one()) {
           mma_f16_ts(d, at, panel, hi, IDESC, u > 0);
 #pragma unroll
           for (int i = 1; i < 4; ++i) mma_f16_ts(d, at + i * 8, panel + i * 2, hi, IDESC, 1u);
-          mma_commit(bar(misc.a_empty[buf]));
+          mma_commit(empty);
         }
         __syncwarp();
-        if (++buf == C::kUnits) { buf = 0; ++buf_round; }
       }
       if (!ok) break;
       if (elect_one()) mma_commit(bar(misc.b_empty[st]));

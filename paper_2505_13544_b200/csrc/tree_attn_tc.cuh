@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
   const uint32_t q_u32 = base + L.off_q, p_u32 = base + L.off_p, st_u32 = base + L.off_st;
   auto wait = [&](unsigned long long& b, int phase) { return mbar_wait_compact(bar(b), phase & 1); };
   auto wait_warp = [&](unsigned long long& b, int phase) {                 // one answer for the warp
-    return __all_sync(0xffffffffu, wait(b, phase)) != 0;
+    return mbar_wait_eager(bar(b), phase & 1);
   };
   bool ok = true;                // false once a wait of this thread has given up
   if (threadIdx.x == 0 && misc->tmem_base != 0) misc->abort_word = 1;
@@ -292,6 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       const uint64_t q_desc = make_smem_desc(q_u32, 16, 1024, kSwizzle128B);
       const uint64_t qk_desc = make_smem_desc(q_u32 + NC * 2 * r, 16, key_sbo, mode);
       int buf = 0;
+      bool there = false;            // the next unit, asked for before the instructions in front of it are issued
       for (int n = 0; n < n_tiles && ok; ++n) {
         const int ks = L.key_stages == 2 ? n & 1 : 0, key_round = L.key_stages == 2 ? n >> 1 : n;
         ok = wait_warp(misc->key_full[ks], key_round);
@@ -319,8 +320,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
 #pragma unroll 1
         for (int p = 0; p < U; ++p) {
           const int k = n * U + p;
-          ok = wait_warp(misc->as_full[k % kUnitRing], k / kUnitRing);
+          ok = __all_sync(0xffffffffu, there) || wait_warp(misc->as_full[k % kUnitRing], k / kUnitRing);
           if (!ok) break;
+          there = mbar_test(bar(misc->as_full[(k + 1) % kUnitRing]), (k + 1) / kUnitRing & 1);
           tc_fence_after_sync();
           const uint32_t at = tmem + T::kColAs + buf * 32;
           const uint32_t panel = (uint32_t)q_desc + p * NC * 8, hi = (uint32_t)(q_desc >> 32);
@@ -345,6 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       // ---------------------------------------------------------------- value products (whole warp, uniform)
       const uint64_t p_desc = make_smem_desc(p_u32, 128, P_SBO, kSwizzleNone);
       int buf = 0;
+      bool there = false;
       for (int n = 0; n < n_tiles && ok; ++n) {
         const int ps = L.p_stages == 2 ? n & 1 : 0, p_round = L.p_stages == 2 ? n >> 1 : n;
         ok = wait_warp(misc->p_full[2 * ps], p_round);
@@ -367,8 +370,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
             ok = wait_warp(misc->p_full[2 * ps + 1], p_round);
             if (!ok) break;
           }
-          ok = wait_warp(misc->av_full[k % kUnitRing], k / kUnitRing);
+          ok = __all_sync(0xffffffffu, there) || wait_warp(misc->av_full[k % kUnitRing], k / kUnitRing);
           if (!ok) break;
+          there = mbar_test(bar(misc->av_full[(k + 1) % kUnitRing]), (k + 1) / kUnitRing & 1);
           tc_fence_after_sync();
           const uint32_t d = tmem + T::kColO + mb * NC, at = tmem + T::kColAv + buf * 32;
           if (elect_one()) {
@@ -404,8 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     // The unit that had unit k's buffer has been used; a whole-warp answer.
     auto buffer_free = [&](unsigned long long* empty) {
       const int u = k - BUFS;
-      const bool there = u < 0 || mbar_wait_compact(smem_u32(empty) + (u % kUnitRing) * 8, u / kUnitRing & 1);
-      return __all_sync(0xffffffffu, there) != 0;
+      return u < 0 || mbar_wait_eager<4>(smem_u32(empty) + (u % kUnitRing) * 8, u / kUnitRing & 1);
     };
     auto next_unit = [&](int step) {
       k += step;
@@ -416,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       const int slot = q * 32 + lane, row = slot & 63;
 #pragma unroll 1
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = __all_sync(0xffffffffu, wait(misc->code_full[st], round));
+        ok = mbar_wait_eager<4>(bar(misc->code_full[st]), round & 1);
         if (!ok) break;
         const TileInfo& info = misc->info[n % kInfo];
         const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
@@ -469,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       int p = grp;
 #pragma unroll 1
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = __all_sync(0xffffffffu, wait(misc->scale_full[st], round));
+        ok = mbar_wait_eager<4>(bar(misc->scale_full[st]), round & 1);
         if (!ok) break;
         const uint32_t rows_at = base + L.off_codes + st * L.stage + lane * code_row;
         const uint32_t scale_at = st_u32 + st * L.scale_room + 4 * t;
