@@ -83,6 +83,7 @@ int launch_product_tc(const qw::ProductArgs& p, const OnDeviceOf& dev, cudaStrea
   a.y_stride = p.y_stride;
   a.n = p.n;
   a.s = p.s;
+  a.pairs = p.s.n_out % 2 == 0 && p.y_stride % 2 == 0 && aligned(p.y, 4);
   const int tiles = ceil_div(p.s.n_out, MT * qw::tc::kTile), row_tiles = ceil_div(p.n, BN);
   // The inputs are shared out, at least four blocks of 128 a CTA, as long as all CTAs run at once.
   const long long at_once = (long long)dev.sm_count() * (C::kAlloc == 256 ? 2 : 1);

@@ -48,6 +48,7 @@ struct Args {
   bf16* y;
   long long y_stride;
   int n, splits;
+  int pairs;                 // two neighbouring outputs of a row are four aligned bytes, and n_out is even
   Shape s;
 };
 
@@ -61,6 +62,16 @@ __device__ __forceinline__ uint32_t load_cluster(uint32_t addr, uint32_t rank) {
   uint32_t remote, v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 load_cluster4(uint32_t addr, uint32_t rank) {
+  uint32_t remote;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(remote)
+               : "memory");
   return v;
 }
 __device__ __forceinline__ void cluster_sync() {
@@ -78,6 +89,7 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
   const uint32_t raw_base = smem_u32(smem_raw), base = (raw_base + 1023u) & ~1023u;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   auto bar = [&](unsigned long long& p) { return smem_u32(&p); };
+  if (threadIdx.x == 32) prefetch_tensormap(&x_map);
   if (threadIdx.x < 8) {
     const int i = threadIdx.x;
     if (i < kRawStages) {
@@ -177,39 +189,50 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
     const uint32_t chunk0 = (uint32_t)(h * 32) ^ twist, chunk1 = (uint32_t)(h * 32 + 16) ^ twist;
     const uint32_t scales = block + kCodeBytes + 8 * (i & 7) + (i >> 3) + 4 * h;
     const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16) + C::kCols;
+    // A unit's bytes are read while the one before is waiting for its buffer.
     int st = 0, round = 0;
-    for (int kb = 0; kb < n_kb && ok; ++kb) {
+    uint4 w0, w1;
+    uint32_t b0, b1;
+    auto read = [&]() {
       ok = wait_warp(misc.raw_full[st], round);
-      if (!ok) break;
-      {
-        const int k = (2 * kb + h) * MT + grp % MT;      // the unit's number
-        const uint32_t at = st * C::kRaw;
-        const uint4 w0 = qp::lds128(row + at + chunk0), w1 = qp::lds128(row + at + chunk1);
-        const uint32_t s0 = scale_b2(qp::lds_u8(scales + at)), s1 = scale_b2(qp::lds_u8(scales + at + 2));
-        const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-        uint32_t x[32];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          uint32_t r[4];
-          decode8(word[e], r);
-#pragma unroll
-          for (int m = 0; m < 4; ++m) x[4 * e + m] = mul_b2(r[m], e < 4 ? s0 : s1);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc.raw_empty[st]));
-        const int buf = k % C::kUnits;
-        if (k >= C::kUnits) {
-          ok = wait_warp(misc.a_empty[buf], k / C::kUnits + 1);
-          if (!ok) break;
-          tc_fence_after_sync();
-        }
-        tmem_st_x32(lane_tm + buf * 32, x);
-        tmem_wait_st();
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(misc.a_full[buf]));
-      }
+      if (!ok) return;
+      const uint32_t at = st * C::kRaw;
+      w0 = qp::lds128(row + at + chunk0);
+      w1 = qp::lds128(row + at + chunk1);
+      b0 = qp::lds_u8(scales + at);
+      b1 = qp::lds_u8(scales + at + 2);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(misc.raw_empty[st]));
       if (++st == kRawStages) { st = 0; ++round; }
+    };
+    read();
+#pragma unroll 1
+    for (int kb = 0; kb < n_kb && ok; ++kb) {
+      const int k = (2 * kb + h) * MT + grp % MT, buf = k % C::kUnits;       // the unit's number and buffer
+      const uint32_t s0 = scale_b2(b0), s1 = scale_b2(b1);
+      const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+      uint32_t x[32];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        uint32_t r[4];
+        decode8(word[e], r);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) x[4 * e + m] = mul_b2(r[m], e < 4 ? s0 : s1);
+      }
+      if (kb + 1 < n_kb) {
+        read();
+        if (!ok) break;
+      }
+      if (k >= C::kUnits) {
+        ok = wait_warp(misc.a_empty[buf], k / C::kUnits + 1);
+        if (!ok) break;
+        tc_fence_after_sync();
+      }
+      tmem_st_x32(lane_tm + buf * 32, x);
+      tmem_wait_st();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(misc.a_full[buf]));
     }
     if (ok) ok = wait(misc.done, 0);
     ok = __all_sync(0xffffffffu, ok);
@@ -229,11 +252,23 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
         for (int j = 0; j < 32; ++j) sums[j * kTile] = __uint_as_float(v[j]);
       } else {
         const int out = (ob0 * kRows) + c0 / BN * kTile + o, n = n0 + c0 % BN;
-        bf16* dst = a.y + n * a.y_stride + out;
-        if (out < a.s.n_out) {
+        const float unit = failed ? NAN : kUnit;
+        if (a.pairs) {
+          // Two outputs a lane: neighbours exchange, the even one has row n + j, the odd one the next.
+          const bool odd = lane & 1;
+          bf16* dst = a.y + (n + odd) * a.y_stride + (out & ~1);
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (n + j < a.n) dst[j * a.y_stride] = __float2bfloat16_rn(failed ? NAN : __uint_as_float(v[j]) * kUnit);
+          for (int j = 0; j < 32; j += 2, dst += 2 * a.y_stride) {
+            const float mine = __uint_as_float(odd ? v[j + 1] : v[j]);
+            const float got = __shfl_xor_sync(0xffffffffu, __uint_as_float(odd ? v[j] : v[j + 1]), 1);
+            const __nv_bfloat162 two = __floats2bfloat162_rn((odd ? got : mine) * unit, (odd ? mine : got) * unit);
+            if ((out | 1) < a.s.n_out && n + j + odd < a.n) *reinterpret_cast<__nv_bfloat162*>(dst) = two;
+          }
+        } else if (out < a.s.n_out) {
+          bf16* dst = a.y + n * a.y_stride + out;
+#pragma unroll
+          for (int j = 0; j < 32; ++j, dst += a.y_stride)
+            if (n + j < a.n) *dst = __float2bfloat16_rn(__uint_as_float(v[j]) * unit);
         }
       }
     }
@@ -247,11 +282,27 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
     const int lo = MT * BN * rank / a.splits, hi = MT * BN * (rank + 1) / a.splits;
     bool failed = false;
     for (int s = 0; s < a.splits; ++s) failed |= load_cluster(smem_u32(&misc.failed), s) != 0;
-    for (int e = lo * kTile + threadIdx.x; e < hi * kTile; e += C::kThreads) {
-      const int c = e / kTile, o = e % kTile, out = ob0 * kRows + c / BN * kTile + o, n = n0 + c % BN;
-      float v = 0.f;
-      for (int s = 0; s < a.splits; ++s) v += __uint_as_float(load_cluster(base + e * 4, s));
-      if (out < a.s.n_out && n < a.n) a.y[n * a.y_stride + out] = __float2bfloat16_rn(failed ? NAN : v * kUnit);
+    for (int e = (lo * kTile + 4 * threadIdx.x); e < hi * kTile; e += 4 * C::kThreads) {
+      float4 v[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        if (s < a.splits) v[s] = load_cluster4(base + e * 4, s);
+      float4 sum = v[0];
+#pragma unroll
+      for (int s = 1; s < 8; ++s)
+        if (s < a.splits) { sum.x += v[s].x; sum.y += v[s].y; sum.z += v[s].z; sum.w += v[s].w; }
+      const int c = e / kTile, out = ob0 * kRows + c / BN * kTile + e % kTile, n = n0 + c % BN;
+      if (n >= a.n) continue;
+      const float unit = failed ? NAN : kUnit, y[4] = {sum.x * unit, sum.y * unit, sum.z * unit, sum.w * unit};
+      bf16* dst = a.y + n * a.y_stride + out;
+      if (a.pairs && out + 3 < a.s.n_out) {
+        reinterpret_cast<__nv_bfloat162*>(dst)[0] = __floats2bfloat162_rn(y[0], y[1]);
+        reinterpret_cast<__nv_bfloat162*>(dst)[1] = __floats2bfloat162_rn(y[2], y[3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (out + i < a.s.n_out) dst[i] = __float2bfloat16_rn(y[i]);
+      }
     }
     __syncwarp();
     cluster_sync();                                          // the sums are read by others until here
