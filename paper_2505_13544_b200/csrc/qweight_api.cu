@@ -36,9 +36,9 @@ int pack_call(const void* w, int64_t stride, int32_t dtype, int32_t n_in, int32_
                           static_cast<cudaStream_t>(stream), a);
 }
 
-template <typename T, int NT>
+template <typename T, int NT, int U>
 int launch_product(const qw::ProductArgs& a, cudaStream_t st) {
-  return launch_dependent(qw::qweight_product_kernel<T, NT>, dim3(a.s.out_blocks(), ceil_div(a.n, 8 * NT)), qw::kThreads,
+  return launch_dependent(qw::qweight_product_kernel<T, NT, U>, dim3(a.s.out_blocks(), ceil_div(a.n, 8 * NT)), qw::kThreads,
                           0, st, a);
 }
 
@@ -145,15 +145,18 @@ int mtla_qweight_product(const void* packed, int32_t n_in, int32_t n_out, const 
   a.n = n;
   a.s = qw::Shape{n_in, n_out};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (dtype == MTLA_DTYPE_BF16 && n > 16) {
-    if (n <= 32) return launch_product_tc<32, 1>(a, dev, st);
-    if (n <= 64) return launch_product_tc<64, 1>(a, dev, st);
-    if (n <= 128) return launch_product_tc<128, 1>(a, dev, st);
-    return launch_product_tc<128, 2>(a, dev, st);
-  }
-  if (dtype == MTLA_DTYPE_BF16)
-    return n <= 8 ? launch_product<bf16, 1>(a, st) : launch_product<bf16, 2>(a, st);
-  return n <= 8 ? launch_product<float, 1>(a, st) : launch_product<float, 2>(a, st);
+  if (dtype == MTLA_DTYPE_FP32) return n <= 8 ? launch_product<float, 1, 1>(a, st) : launch_product<float, 2, 1>(a, st);
+  // Several blocks' loads ahead as long as all CTAs run at once all the same, two on an SM.
+  const bool ahead = a.s.out_blocks() <= 2 * dev.sm_count();
+  if (n <= 8) return ahead ? launch_product<bf16, 1, 4>(a, st) : launch_product<bf16, 1, 1>(a, st);
+  if (n <= 16) return ahead ? launch_product<bf16, 2, 2>(a, st) : launch_product<bf16, 2, 1>(a, st);
+  // More rows: the tensor cores' set-up and joining take 3 us longer, passes over the weights 2.2 us per 10^8
+  // products (64 rows of 1024 x 1024: 4.1 us and 6.6; 32 of 4096 x 4096: 12.4 and 9.2; 128 of 2048 x 512: 7.3 and 7.7).
+  if ((double)n * n_in * n_out <= 1.5e8) return launch_product<bf16, 4, 1>(a, st);
+  if (n <= 32) return launch_product_tc<32, 1>(a, dev, st);
+  if (n <= 64) return launch_product_tc<64, 1>(a, dev, st);
+  if (n <= 128) return launch_product_tc<128, 1>(a, dev, st);
+  return launch_product_tc<128, 2>(a, dev, st);
 }
 
 }  // extern "C"

@@ -30,31 +30,37 @@ struct Operand;
 template <>
 struct Operand<bf16> {
   static constexpr int kTerms = 1;
-  uint32_t p[1][4];
+  uint4 v;
   __device__ __forceinline__ void load(const bf16* src, bool there) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    v = make_uint4(0u, 0u, 0u, 0u);
     if (there) v = *reinterpret_cast<const uint4*>(src);
+  }
+  __device__ __forceinline__ void split(uint32_t (&p)[1][4]) const {
     p[0][0] = v.x; p[0][1] = v.y; p[0][2] = v.z; p[0][3] = v.w;
   }
 };
 template <>
 struct Operand<float> {
   static constexpr int kTerms = 3;
-  uint32_t p[3][4];
+  float v[8];
   __device__ __forceinline__ void load(const float* src, bool there) {
-    float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
     if (there) {
       float lo[4], hi[4];
       load_vec(src, lo);
       load_vec(src + 4, hi);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[i] = lo[i];
-        x[4 + i] = hi[i];
+        v[i] = lo[i];
+        v[4 + i] = hi[i];
       }
     }
+  }
+  __device__ __forceinline__ void split(uint32_t (&p)[3][4]) const {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = v[i];
 #pragma unroll
     for (int t = 0; t < 3; ++t)
 #pragma unroll
@@ -69,9 +75,12 @@ struct Operand<float> {
   }
 };
 
-// A CTA per 16 outputs and 8 NT rows; its warps share the input blocks out, sums are joined in the warps' order.
-template <typename T, int NT>
-__global__ void __launch_bounds__(kThreads) qweight_product_kernel(ProductArgs a) {
+// A CTA per 16 outputs and 8 NT rows; its warps share the input blocks out, sums are joined in the warps' order.  The
+// loads of U blocks (weights, scales and x) are issued before the first of them is used.  That takes registers: one row
+// of 4096 x 4096, where all CTAs run at once either way, takes 7.2 us with one block at a time and 5.1 with four; of
+// 8192 x 8192 it takes 14.7 and 15.8.
+template <typename T, int NT, int U>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && NT <= 2 && U == 1 ? 4 : 2) qweight_product_kernel(ProductArgs a) {
   constexpr int TERMS = Operand<T>::kTerms;
   __shared__ float red[kWarps][kRows][8 * NT + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -83,47 +92,63 @@ __global__ void __launch_bounds__(kThreads) qweight_product_kernel(ProductArgs a
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-  const int kb0 = (int)((long long)kbs * warp / kWarps), kb1 = (int)((long long)kbs * (warp + 1) / kWarps);
-  const uint8_t* block = a.packed + ((long long)ob * kbs + kb0) * kBlockBytes;
-  for (int kb = kb0; kb < kb1; ++kb, block += kBlockBytes) {
-    const uint8_t* codes = block + g * 64 + (t ^ (g >> 1 & 3)) * 16;
-    const uint4 w0 = *reinterpret_cast<const uint4*>(codes), w1 = *reinterpret_cast<const uint4*>(codes + 512);
-    const uint32_t two = *reinterpret_cast<const uint16_t*>(block + kCodeBytes + 2 * lane);
-    const uint32_t s0 = scale_b2(two & 255u), s1 = scale_b2(two >> 8);
-    const uint32_t word0[4] = {w0.x, w0.y, w0.z, w0.w}, word1[4] = {w1.x, w1.y, w1.z, w1.w};
-    const int k = kb * kInputs + t * kGroup;
-    float part[NT][4];                         // fp32: a block's products are added outside the matrix unit
+  const int kb0 = kbs * warp / kWarps, kb1 = kbs * (warp + 1) / kWarps;
+  const uint8_t* codes = a.packed + (long long)ob * kbs * kBlockBytes + g * 64 + (t ^ (g >> 1 & 3)) * 16;
+  const uint8_t* scales = a.packed + (long long)ob * kbs * kBlockBytes + kCodeBytes + 2 * lane;
+  for (int kb = kb0; kb < kb1; kb += U) {
+    uint4 w0[U], w1[U];
+    uint32_t two[U];
+    Operand<T> x[U][4][NT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int u = 0; u < U; ++u) {
+      const bool there = kb + u < kb1;
+      const long long at = (long long)(kb + (there ? u : 0)) * kBlockBytes;
+      w0[u] = *reinterpret_cast<const uint4*>(codes + at);
+      w1[u] = *reinterpret_cast<const uint4*>(codes + at + 512);
+      two[u] = *reinterpret_cast<const uint16_t*>(scales + at);
+      const int k = (kb + u) * kInputs + t * kGroup;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) part[j][i] = TERMS == 1 ? acc[j][i] : 0.f;
+      for (int m = 0; m < 4; ++m)
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      uint32_t r0[4], r1[4];
-      decode8(word0[m], r0);
-      decode8(word1[m], r1);
+        for (int j = 0; j < NT; ++j) {
+          const int row = n0 + 8 * j + g;
+          x[u][m][j].load(static_cast<const T*>(a.x) + row * a.x_stride + k + 8 * m,
+                          there && row < a.n && k + 8 * m < a.s.n_in);
+        }
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        r0[i] = mul_b2(r0[i], s0);
-        r1[i] = mul_b2(r1[i], s1);
-      }
-      const uint32_t a0[4] = {r0[0], r1[0], r0[1], r1[1]}, a1[4] = {r0[2], r1[2], r0[3], r1[3]};
+    for (int u = 0; u < U; ++u) {
+      if (kb + u >= kb1) break;
+      const uint32_t s0 = scale_b2(two[u] & 255u), s1 = scale_b2(two[u] >> 8);
+      const uint32_t word0[4] = {w0[u].x, w0[u].y, w0[u].z, w0[u].w}, word1[4] = {w1[u].x, w1[u].y, w1[u].z, w1[u].w};
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        Operand<T> x;
-        const int row = n0 + 8 * j + g;
-        x.load(static_cast<const T*>(a.x) + row * a.x_stride + k + 8 * m, row < a.n && k + 8 * m < a.s.n_in);
+      for (int m = 0; m < 4; ++m) {
+        uint32_t r0[4], r1[4];
+        decode8(word0[m], r0);
+        decode8(word1[m], r1);
 #pragma unroll
-        for (int e = 0; e < TERMS; ++e) {
-          qp::mma_bf16(part[j], a0, x.p[e][0], x.p[e][1]);
-          qp::mma_bf16(part[j], a1, x.p[e][2], x.p[e][3]);
+        for (int i = 0; i < 4; ++i) {
+          r0[i] = mul_b2(r0[i], s0);
+          r1[i] = mul_b2(r1[i], s1);
+        }
+        const uint32_t a0[4] = {r0[0], r1[0], r0[1], r1[1]}, a1[4] = {r0[2], r1[2], r0[3], r1[3]};
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          uint32_t p[TERMS][4];
+          x[u][m][j].split(p);
+          float part[4];                       // fp32: products of 32 inputs are added outside the matrix unit
+#pragma unroll
+          for (int i = 0; i < 4; ++i) part[i] = TERMS == 1 ? acc[j][i] : 0.f;
+#pragma unroll
+          for (int e = TERMS - 1; e >= 0; --e) {
+            qp::mma_bf16(part, a0, p[e][0], p[e][1]);
+            qp::mma_bf16(part, a1, p[e][2], p[e][3]);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[j][i] = TERMS == 1 ? part[i] : acc[j][i] + part[i];
         }
       }
     }
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[j][i] = TERMS == 1 ? part[j][i] : acc[j][i] + part[j][i];
   }
   // Fragment: outputs g and g + 8, rows 2t and 2t + 1.
 #pragma unroll
