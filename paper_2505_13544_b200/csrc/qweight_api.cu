@@ -71,10 +71,10 @@ bool make_x_map(CUtensorMap* map, const qw::ProductArgs& a, int box) {
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN, int MT>
+template <int BN>
 int launch_product_tc(const qw::ProductArgs& p, const OnDeviceOf& dev, cudaStream_t st) {
-  using C = qw::tc::Config<BN, MT>;
-  if (!raise_smem<qw::tc::qweight_tc_kernel<BN, MT>>(dev.device(), C::kBytes)) return MTLA_ERR_CUDA;
+  using C = qw::tc::Config<BN>;
+  if (!raise_smem<qw::tc::qweight_tc_kernel<BN>>(dev.device(), C::kBytes)) return MTLA_ERR_CUDA;
   CUtensorMap map;
   if (!make_x_map(&map, p, BN)) return MTLA_ERR_CUDA;
   qw::tc::Args a;
@@ -84,14 +84,14 @@ int launch_product_tc(const qw::ProductArgs& p, const OnDeviceOf& dev, cudaStrea
   a.n = p.n;
   a.s = p.s;
   a.pairs = p.s.n_out % 2 == 0 && p.y_stride % 2 == 0 && aligned(p.y, 4);
-  const int tiles = ceil_div(p.s.n_out, MT * qw::tc::kTile), row_tiles = ceil_div(p.n, BN);
+  const int tiles = ceil_div(p.s.n_out, qw::tc::kTile), row_tiles = ceil_div(p.n, BN);
   // The inputs are shared out, at least four blocks of 128 a CTA, as long as all CTAs run at once.
-  const long long at_once = (long long)dev.sm_count() * (C::kAlloc == 256 ? 2 : 1);
+  const long long at_once = 2ll * dev.sm_count();
   a.splits = 1;
   while (a.splits < 8 && 2ll * a.splits * tiles * row_tiles <= at_once && p.s.in_blocks() >= 8 * a.splits) a.splits *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * a.splits), (unsigned)row_tiles);
-  cfg.blockDim = dim3(C::kThreads);
+  cfg.blockDim = dim3(qw::tc::kThreads);
   cfg.dynamicSmemBytes = C::kBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -102,7 +102,7 @@ int launch_product_tc(const qw::ProductArgs& p, const OnDeviceOf& dev, cudaStrea
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.splits > 1 ? 2 : 1;
-  if (cudaLaunchKernelEx(&cfg, qw::tc::qweight_tc_kernel<BN, MT>, map, a) == cudaSuccess) return MTLA_OK;
+  if (cudaLaunchKernelEx(&cfg, qw::tc::qweight_tc_kernel<BN>, map, a) == cudaSuccess) return MTLA_OK;
   cudaGetLastError();
   return MTLA_ERR_CUDA;
 }
@@ -149,14 +149,13 @@ int mtla_qweight_product(const void* packed, int32_t n_in, int32_t n_out, const 
   // Several blocks' loads ahead as long as all CTAs run at once all the same, two on an SM.
   const bool ahead = a.s.out_blocks() <= 2 * dev.sm_count();
   if (n <= 8) return ahead ? launch_product<bf16, 1, 4>(a, st) : launch_product<bf16, 1, 1>(a, st);
-  if (n <= 16) return ahead ? launch_product<bf16, 2, 2>(a, st) : launch_product<bf16, 2, 1>(a, st);
+  if (n <= 16 && (double)n_in * n_out <= 2e7)        // 16 rows of 8192 x 8192: 23.6 us, on the tensor cores 16.6
+    return ahead ? launch_product<bf16, 2, 2>(a, st) : launch_product<bf16, 2, 1>(a, st);
   // More rows: the tensor cores' set-up and joining take 3 us longer, passes over the weights 2.2 us per 10^8
   // products (64 rows of 1024 x 1024: 4.1 us and 6.6; 32 of 4096 x 4096: 12.4 and 9.2; 128 of 2048 x 512: 7.3 and 7.7).
   if ((double)n * n_in * n_out <= 1.5e8) return launch_product<bf16, 4, 1>(a, st);
-  if (n <= 32) return launch_product_tc<32, 1>(a, dev, st);
-  if (n <= 64) return launch_product_tc<64, 1>(a, dev, st);
-  if (n <= 128) return launch_product_tc<128, 1>(a, dev, st);
-  return launch_product_tc<128, 2>(a, dev, st);
+  if (n <= 32) return launch_product_tc<32>(a, dev, st);
+  return n <= 64 ? launch_product_tc<64>(a, dev, st) : launch_product_tc<128>(a, dev, st);
 }
 
 }  // extern "C"

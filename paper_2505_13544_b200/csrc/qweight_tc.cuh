@@ -1,20 +1,19 @@
 // Products of many bf16 rows with 4-bit weights on the fifth-generation tensor cores.
 //
-// A CTA has MT tiles of 128 outputs by BN rows of x and a share of the inputs.  The weights are the A operand: expanding
-// warps decode 64 inputs of a tile from the raw blocks in shared memory into bf16 (exactly, times 2^-13) and write them
+// A CTA has a tile of 128 outputs by BN rows of x and a share of the inputs.  The weights are the A operand: expanding
+// warps decode 64 inputs of the tile from the raw blocks in shared memory into bf16 (exactly, times 2^-13) and write them
 // to tensor memory, the rows of x are the B operand, which a tensor map brings into shared memory with its 128-byte
-// swizzle.  So the weights' 4 bits are all that travels of them, and x is what costs: a panel of BN rows is
-// read by every CTA along the outputs, hence two tiles of outputs per CTA where there are many rows.  Bound by the
-// matrix unit then (128 x BN x 16 in BN / 2 cycles), by the blocks' bytes with few rows; expanding a unit of 64 inputs
-// takes about 150 cycles of the issue slots, against 2 BN of the matrix unit.
+// swizzle.  So the weights' 4 bits are all that travels of them.  Bound by the matrix unit with many rows (128 x BN x 16
+// in BN / 2 cycles; 2048 rows through 4096 x 6720: 90 us, 1.25 PFLOP/s), by the length of the chain with few (load,
+// decode, multiply, join: 9 us for 32 rows through 4096 x 4096).  Two CTAs an SM hide each other's starts and ends: with
+// 256 outputs a CTA, which halves the reads of x, 512 rows took 33 us, so 28.
 //
-// With few tiles of outputs the inputs are shared out among the CTAs of a cluster, which add their sums through
-// distributed shared memory in rank order.  Every wait is bounded; should one give up, the tile's results are NaN.
+// With few tiles the inputs are shared out among the CTAs of a cluster, which add their sums through distributed shared
+// memory in rank order (read by the CTA that needs them, four at a time: sending them took twice as long).  Every
+// wait is bounded; should one give up, the tile's results are NaN.
 //
-// Roles: warp 0 fetches x, warp 3 the weights (one thread for both took 1900 cycles to issue a block of 16 copies),
-// warp 1 issues, warp 2 owns the tensor memory, the others from warp 4 on expand, four for every
-// unit of a block (MT tiles by two halves of the inputs), and then write the results.  (Half as many for MT = 2: 48 us
-// for 512 rows of 4096 x 6720, each unit taking its warps some 1400 cycles.)
+// Roles (12 warps): warp 0 fetches x, warp 3 the weights (one thread for both took 1900 cycles to issue 16 copies), warp 1
+// issues, warp 2 owns the tensor memory; warps 4-11 expand, four for each half of a block's inputs, and write the results.
 #pragma once
 
 #include "qpool_attn.cuh"
@@ -24,23 +23,21 @@ namespace mtla {
 namespace qw {
 namespace tc {
 
-constexpr int kExpandWarp0 = 4;
+constexpr int kExpandWarp0 = 4, kGroups = 2, kExpandThreads = kGroups * 128, kThreads = kExpandWarp0 * 32 + kExpandThreads;
 constexpr int kTile = 128;                         // outputs of a tile: eight blocks
 constexpr int kRawStages = 4;
 
-template <int BN, int MT>
+template <int BN>
 struct Config {
-  static constexpr int kGroups = 2 * MT, kExpandThreads = kGroups * 128, kThreads = kExpandWarp0 * 32 + kExpandThreads;
-  static constexpr int kCols = MT * BN;                             // tensor memory of the sums
-  static constexpr int kAlloc = kCols <= 128 ? 256 : 512;
-  static constexpr int kUnits = (kAlloc - kCols) / 32 < 8 ? (kAlloc - kCols) / 32 : 8;      // buffers of 64 inputs
+  static constexpr int kAlloc = 256;                                // tensor memory columns: two CTAs an SM
+  static constexpr int kUnits = (kAlloc - BN) / 32 < 8 ? (kAlloc - BN) / 32 : 8;            // buffers of 64 inputs
   static constexpr int kPanel = BN * 128;                           // 64 inputs of BN rows
-  static constexpr int kStages = kAlloc == 256 ? (BN == 128 ? 4 : 6) : 8;
-  static constexpr int kRaw = MT * 8 * kBlockBytes;
-  static constexpr int kSums = kCols * kTile * 4;                   // a cluster's sums lie where the panels were
+  static constexpr int kStages = BN == 128 ? 4 : 6;
+  static constexpr int kRaw = 8 * kBlockBytes;
+  static constexpr int kSums = BN * kTile * 4;                      // a cluster's sums lie where the panels were
   static constexpr int kPanels = kStages * kPanel > kSums ? kStages * kPanel : kSums;
   static constexpr int kBytes = kPanels + kRawStages * kRaw + 1024;
-  static_assert(kBytes <= (kAlloc == 256 ? 113 : 226) * 1024, "shared memory budget");
+  static_assert(kBytes <= 113 * 1024, "shared memory of half an SM");
 };
 
 struct Args {
@@ -78,11 +75,10 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int BN, int MT>
-__global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAlloc == 256 ? 2 : 1)
-    qweight_tc_kernel(const __grid_constant__ CUtensorMap x_map, Args a) {
+template <int BN>
+__global__ void __launch_bounds__(kThreads, 2) qweight_tc_kernel(const __grid_constant__ CUtensorMap x_map, Args a) {
   using namespace ptx;
-  using C = Config<BN, MT>;
+  using C = Config<BN>;
   constexpr uint32_t IDESC = make_idesc_bf16(128, BN, 0, 0);
   extern __shared__ uint8_t smem_raw[];
   __shared__ Misc misc;
@@ -94,7 +90,7 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
     const int i = threadIdx.x;
     if (i < kRawStages) {
       mbar_init(bar(misc.raw_full[i]), 1);
-      mbar_init(bar(misc.raw_empty[i]), C::kExpandThreads / 32);
+      mbar_init(bar(misc.raw_empty[i]), kExpandThreads / 32);
     }
     mbar_init(bar(misc.b_full[i]), 1);
     mbar_init(bar(misc.b_empty[i]), 1);
@@ -115,7 +111,7 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
   grid_dependency_wait();
 
   const int rank = a.splits > 1 ? (int)blockIdx.x % a.splits : 0, tile = (int)blockIdx.x / a.splits;
-  const int kbs = a.s.in_blocks(), ob0 = tile * MT * 8, obs = min(MT * 8, a.s.out_blocks() - ob0);
+  const int kbs = a.s.in_blocks(), ob0 = tile * 8, obs = min(8, a.s.out_blocks() - ob0);
   const int kb0 = (int)((long long)kbs * rank / a.splits), n_kb = (int)((long long)kbs * (rank + 1) / a.splits) - kb0;
   const int n0 = blockIdx.y * BN, n_units = 2 * n_kb;              // of 64 inputs
   const uint32_t raw_u32 = base + C::kPanels;
@@ -156,24 +152,19 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
       ok = wait_warp(misc.b_full[st], st_round);
       if (!ok) break;
       const uint32_t panel = (uint32_t)b_desc + st * (C::kPanel / 16), hi = (uint32_t)(b_desc >> 32);
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        ok = __all_sync(0xffffffffu, there) || wait_warp(misc.a_full[buf], buf_round);
-        if (!ok) break;
-        tc_fence_after_sync();
-        const uint32_t d = tmem + m * BN, at = tmem + C::kCols + buf * 32, empty = bar(misc.a_empty[buf]);
-        if (++buf == C::kUnits) { buf = 0; ++buf_round; }
-        there = mbar_test(bar(misc.a_full[buf]), buf_round & 1);
-        if (elect_one()) {
-          mma_f16_ts(d, at, panel, hi, IDESC, u > 0);
-#pragma unroll
-          for (int i = 1; i < 4; ++i) mma_f16_ts(d, at + i * 8, panel + i * 2, hi, IDESC, 1u);
-          mma_commit(empty);
-        }
-        __syncwarp();
-      }
+      ok = __all_sync(0xffffffffu, there) || wait_warp(misc.a_full[buf], buf_round);
       if (!ok) break;
-      if (elect_one()) mma_commit(bar(misc.b_empty[st]));
+      tc_fence_after_sync();
+      const uint32_t at = tmem + BN + buf * 32, empty = bar(misc.a_empty[buf]);
+      if (++buf == C::kUnits) { buf = 0; ++buf_round; }
+      there = mbar_test(bar(misc.a_full[buf]), buf_round & 1);
+      if (elect_one()) {
+        mma_f16_ts(tmem, at, panel, hi, IDESC, u > 0);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) mma_f16_ts(tmem, at + i * 8, panel + i * 2, hi, IDESC, 1u);
+        mma_commit(empty);
+        mma_commit(bar(misc.b_empty[st]));
+      }
       __syncwarp();
       if (++st == C::kStages) { st = 0; ++st_round; }
     }
@@ -181,14 +172,13 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
     __syncwarp();
   } else if (warp >= kExpandWarp0) {
     // ---------------------------------------------------------------- expansion
-    // Unit u of tile m has number u MT + m; group grp has tile grp % MT and half grp / MT of every block.
+    // Group grp has half grp of every block.
     const int q = warp & 3, grp = (warp - kExpandWarp0) >> 2, o = q * 32 + lane, i = o & 15;
-    const int h = grp / MT;
-    const uint32_t block = raw_u32 + (grp % MT * 8 + (o >> 4)) * kBlockBytes;
+    const uint32_t block = raw_u32 + (o >> 4) * kBlockBytes;
     const uint32_t twist = (uint32_t)(i >> 1 & 3) * 16, row = block + i * 64;
-    const uint32_t chunk0 = (uint32_t)(h * 32) ^ twist, chunk1 = (uint32_t)(h * 32 + 16) ^ twist;
-    const uint32_t scales = block + kCodeBytes + 8 * (i & 7) + (i >> 3) + 4 * h;
-    const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16) + C::kCols;
+    const uint32_t chunk0 = (uint32_t)(grp * 32) ^ twist, chunk1 = (uint32_t)(grp * 32 + 16) ^ twist;
+    const uint32_t scales = block + kCodeBytes + 8 * (i & 7) + (i >> 3) + 4 * grp;
+    const uint32_t lane_tm = tmem + ((uint32_t)(q * 32) << 16) + BN;
     // A unit's bytes are read while the one before is waiting for its buffer.
     int st = 0, round = 0;
     uint4 w0, w1;
@@ -208,7 +198,7 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
     read();
 #pragma unroll 1
     for (int kb = 0; kb < n_kb && ok; ++kb) {
-      const int k = (2 * kb + h) * MT + grp % MT, buf = k % C::kUnits;       // the unit's number and buffer
+      const int k = 2 * kb + grp, buf = k % C::kUnits;       // the unit's number and buffer
       const uint32_t s0 = scale_b2(b0), s1 = scale_b2(b1);
       const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
       uint32_t x[32];
@@ -237,12 +227,11 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
     if (ok) ok = wait(misc.done, 0);
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) misc.failed = 1;
-    named_sync<1, C::kExpandThreads>();
+    named_sync<1, kExpandThreads>();
     const bool failed = *reinterpret_cast<volatile int*>(&misc.failed) != 0;
     tc_fence_after_sync();
     // ---------------------------------------------------------------- results: lane = output, columns = rows of x
-    for (int c0 = 0; c0 < MT * BN; c0 += 32) {
-      if (c0 / 32 % C::kGroups != grp) continue;                    // the groups take pieces of 32 columns in turn
+    for (int c0 = 32 * grp; c0 < BN; c0 += 32 * kGroups) {
       uint32_t v[32];
       tmem_ld_x32(tmem + ((uint32_t)(q * 32) << 16) + c0, v);
       tmem_wait_ld();
@@ -251,7 +240,7 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
 #pragma unroll
         for (int j = 0; j < 32; ++j) sums[j * kTile] = __uint_as_float(v[j]);
       } else {
-        const int out = (ob0 * kRows) + c0 / BN * kTile + o, n = n0 + c0 % BN;
+        const int out = ob0 * kRows + o, n = n0 + c0;
         const float unit = failed ? NAN : kUnit;
         if (a.pairs) {
           // Two outputs a lane: neighbours exchange, the even one has row n + j, the odd one the next.
@@ -279,10 +268,10 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
   if (a.splits > 1) {
     cluster_sync();
     // This CTA's share of the columns: all CTAs' sums in rank order.
-    const int lo = MT * BN * rank / a.splits, hi = MT * BN * (rank + 1) / a.splits;
+    const int lo = BN * rank / a.splits, hi = BN * (rank + 1) / a.splits;
     bool failed = false;
     for (int s = 0; s < a.splits; ++s) failed |= load_cluster(smem_u32(&misc.failed), s) != 0;
-    for (int e = (lo * kTile + 4 * threadIdx.x); e < hi * kTile; e += 4 * C::kThreads) {
+    for (int e = (lo * kTile + 4 * threadIdx.x); e < hi * kTile; e += 4 * kThreads) {
       float4 v[8];
 #pragma unroll
       for (int s = 0; s < 8; ++s)
@@ -291,7 +280,7 @@ __global__ void __launch_bounds__(Config<BN, MT>::kThreads, Config<BN, MT>::kAll
 #pragma unroll
       for (int s = 1; s < 8; ++s)
         if (s < a.splits) { sum.x += v[s].x; sum.y += v[s].y; sum.z += v[s].z; sum.w += v[s].w; }
-      const int c = e / kTile, out = ob0 * kRows + c / BN * kTile + e % kTile, n = n0 + c % BN;
+      const int out = ob0 * kRows + e % kTile, n = n0 + e / kTile;
       if (n >= a.n) continue;
       const float unit = failed ? NAN : kUnit, y[4] = {sum.x * unit, sum.y * unit, sum.z * unit, sum.w * unit};
       bf16* dst = a.y + n * a.y_stride + out;
