@@ -636,12 +636,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       // segment's first slots set.
 #pragma unroll
       for (int i = 0; i < NHH; i += 4) {
-        const float4 u = *reinterpret_cast<const float4*>(&misc->unit[HO + i]);
-        const float4 o = *reinterpret_cast<const float4*>(&misc->neg_ref[HO + i]);
-        x[i] = fmaf(x[i], u.x, o.x);
-        x[i + 1] = fmaf(x[i + 1], u.y, o.y);
-        x[i + 2] = fmaf(x[i + 2], u.z, o.z);
-        x[i + 3] = fmaf(x[i + 3], u.w, o.w);
+        const ulonglong2 u = *reinterpret_cast<const ulonglong2*>(&misc->unit[HO + i]);
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&misc->neg_ref[HO + i]);
+        unpack2(fma2(pack2(x[i], x[i + 1]), u.x, o.x), x[i], x[i + 1]);
+        unpack2(fma2(pack2(x[i + 2], x[i + 3]), u.y, o.y), x[i + 2], x[i + 3]);
       }
       if (!full) {                                       // only a sequence's last tile
 #pragma unroll
