@@ -102,6 +102,23 @@ struct Layout {
   }
 };
 
+// Codes of four latents of two neighbouring slots -> a pair (slot, next slot) of each latent: a thread's register of the
+// transposing load holds codes (4g .. 4g + 3) of slot 2t in its low half and of slot 2t + 1 in its high half.
+__device__ __forceinline__ void decode_pairs(uint32_t w, uint32_t (&o)[4]) {
+  uint32_t e, d;                               // latents 0, 2 and 1, 3 in the two low bytes, the next slot's above
+  asm("lop3.b32 %0, %1, %2, %3, 0xe4;" : "=r"(e) : "r"(w), "r"(w >> 12), "n"(0x0f0f));
+  asm("lop3.b32 %0, %1, %2, %3, 0xe4;" : "=r"(d) : "r"(w >> 4), "r"(w >> 16), "n"(0x0f0f));
+  asm("{\n\t.reg .b8 a, b, c, d, x, y;\n\t"
+      "mov.b32 {a, b, x, y}, %4;\n\t"
+      "mov.b32 {c, d, x, y}, %5;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
+      : "r"(e), "r"(d));
+}
+
 // A segment's output sums, this thread's latent of every block (lane 8j + g of a quarter holds latent 4g + j), into
 // the segment's part [NC][r], shared out among STEP groups of four warps in pieces of 16 columns of a block: added to
 // what has been set down there, which `fac` brings to the present references, or without `add` as they are.
@@ -408,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     // The unit that had unit k's buffer has been used; a whole-warp answer.
     auto buffer_free = [&](unsigned long long* empty) {
       const int u = k - BUFS;
-      return u < 0 || mbar_wait_eager<4>(smem_u32(empty) + (u % kUnitRing) * 8, u / kUnitRing & 1);
+      return u < 0 || mbar_wait_eager<1>(smem_u32(empty) + (u % kUnitRing) * 8, u / kUnitRing & 1);
     };
     auto next_unit = [&](int step) {
       k += step;
@@ -419,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       const int slot = q * 32 + lane, row = slot & 63;
 #pragma unroll 1
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = mbar_wait_eager<4>(bar(misc->code_full[st]), round & 1);
+        ok = mbar_wait_eager<1>(bar(misc->code_full[st]), round & 1);
         if (!ok) break;
         const TileInfo& info = misc->info[n % kInfo];
         const uint32_t live = row < (slot < 64 ? info.rows0 : info.rows1) ? 0xffffffffu : 0u;
@@ -472,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       int p = grp;
 #pragma unroll 1
       for (int n = 0; n < n_tiles && ok; ++n) {
-        ok = mbar_wait_eager<4>(bar(misc->scale_full[st]), round & 1);
+        ok = mbar_wait_eager<1>(bar(misc->scale_full[st]), round & 1);
         if (!ok) break;
         const uint32_t rows_at = base + L.off_codes + st * L.stage + lane * code_row;
         const uint32_t scale_at = st_u32 + st * L.scale_room + 4 * t;
@@ -492,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
               for (int m = 0; m < 4; ++m) {
                 uint32_t sc;
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc) : "r"(sc_at + i2 * 64 + m * 16));
-                qp::decode_pairs(w[i2][m], x[i2][m]);
+                decode_pairs(w[i2][m], x[i2][m]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[i2][m][e] = qp::mul_h2(x[i2][m][e], sc);
               }
