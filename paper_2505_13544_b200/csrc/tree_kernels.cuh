@@ -139,59 +139,71 @@ constexpr int kMaxRequests = 4096;
 // are to be multiplied by.
 __host__ __device__ inline int image_bytes(int cols, const qp::Format& f) { return cols * (2 * (f.r + f.dr) + 4); }
 
-// One column into its group's image, by a warp.  The row is scaled by the power of two that brings its largest
-// element into [2^14, 2^15), exactly down to 2^-39 of that; a column that does not exist is zero.  Magnitudes and scaling
-// work on pairs of bf16 numbers (a power of two in two factors, since one may be out of range).
-__device__ __forceinline__ void put_column(const bf16* q, bool there, uint8_t* image, int col, int cols, float scale_log2,
-                                           const qp::Format& f) {
+// Columns col, col + step, ... (N of them, whose loads are issued together) into their group's image, by a warp; `q`
+// is the group's first column.  A row is scaled by the power of two that brings its largest element into [2^14, 2^15),
+// exactly down to 2^-39 of that; a column that does not exist is zero.  Magnitudes and scaling work on pairs of bf16
+// numbers (a power of two in two factors, since one may be out of range).
+template <int N>
+__device__ __forceinline__ void put_columns(const bf16* q, int there, uint8_t* image, int col0, int step, int cols,
+                                            float scale_log2, const qp::Format& f) {
   const int lane = threadIdx.x & 31, r = f.r, dr = f.dr;
-  uint4 w[2], key = make_uint4(0u, 0u, 0u, 0u);
+  uint4 w[N][2], key[N];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    w[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (there && (lane + 32 * i) * 8 < r) w[i] = *reinterpret_cast<const uint4*>(q + (lane + 32 * i) * 8);
+  for (int n = 0; n < N; ++n) {
+    const int col = col0 + n * step;
+    const bf16* src = q + (long long)col * (r + dr);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      w[n][i] = make_uint4(0u, 0u, 0u, 0u);
+      if (col < there && (lane + 32 * i) * 8 < r) w[n][i] = *reinterpret_cast<const uint4*>(src + (lane + 32 * i) * 8);
+    }
+    key[n] = make_uint4(0u, 0u, 0u, 0u);
+    if (col < there && lane * 8 < dr) key[n] = *reinterpret_cast<const uint4*>(src + r + lane * 8);
   }
-  if (there && lane * 8 < dr) key = *reinterpret_cast<const uint4*>(q + r + lane * 8);
-  uint32_t top = 0;
-  auto largest = [&](const uint4& v) {
-    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int m = 0; m < 4; ++m) top = __vmaxu2(top, x[m] & 0x7fff7fffu);
-  };
-  largest(w[0]);
-  largest(w[1]);
-  largest(key);
-  top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-  // Exponents -113 .. 140 (a row of subnormal numbers only reaches less); none for zeros and specials.
-  const bool fine = top > 0 && top < 0x7f80u;
-  const int e = fine ? 141 - max((int)(top >> 7), 1) : 0, e1 = e / 2, e2 = e - e1;
-  const uint32_t f1 = (uint32_t)(127 + e1) * 0x00800080u, f2 = (uint32_t)(127 + e2) * 0x00800080u;
-  if (lane == 0)
-    reinterpret_cast<float*>(image + (long long)cols * 2 * (r + dr))[col] =
-        scale_log2 * __uint_as_float((127 - e1) << 23) * __uint_as_float((127 - e2) << 23);
-  auto scaled = [&](uint32_t x) { return qw::mul_b2(qw::mul_b2(x, f1), f2); };
-  auto half2_of = [&](uint32_t x) {
-    const uint32_t y = scaled(x);
-    const __half2 h = __floats2half2_rn(__uint_as_float(y << 16), __uint_as_float(y & 0xffff0000u));
-    return *reinterpret_cast<const uint32_t*>(&h);
-  };
+  for (int n = 0; n < N; ++n) {
+    const int col = col0 + n * step;
+    uint32_t top = 0;
+    auto largest = [&](const uint4& v) {
+      const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int c = lane + 32 * i;
-    if (c * 8 < r)
-      *reinterpret_cast<uint4*>(image + (c >> 3) * cols * 128 + col * 128 + ((c ^ col) & 7) * 16) =
-          make_uint4(half2_of(w[i].x), half2_of(w[i].y), half2_of(w[i].z), half2_of(w[i].w));
+      for (int m = 0; m < 4; ++m) top = __vmaxu2(top, x[m] & 0x7fff7fffu);
+    };
+    largest(w[n][0]);
+    largest(w[n][1]);
+    largest(key[n]);
+    top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+    // Exponents -113 .. 140 (a row of subnormal numbers only reaches less); none for zeros and specials.
+    const bool fine = top > 0 && top < 0x7f80u;
+    const int e = fine ? 141 - max((int)(top >> 7), 1) : 0, e1 = e / 2, e2 = e - e1;
+    const uint32_t f1 = (uint32_t)(127 + e1) * 0x00800080u, f2 = (uint32_t)(127 + e2) * 0x00800080u;
+    if (lane == 0)
+      reinterpret_cast<float*>(image + (long long)cols * 2 * (r + dr))[col] =
+          scale_log2 * __uint_as_float((127 - e1) << 23) * __uint_as_float((127 - e2) << 23);
+    auto scaled = [&](uint32_t x) { return qw::mul_b2(qw::mul_b2(x, f1), f2); };
+    auto half2_of = [&](uint32_t x) {
+      const uint32_t y = scaled(x);
+      const __half2 h = __floats2half2_rn(__uint_as_float(y << 16), __uint_as_float(y & 0xffff0000u));
+      return *reinterpret_cast<const uint32_t*>(&h);
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = lane + 32 * i;
+      if (c * 8 < r)
+        *reinterpret_cast<uint4*>(image + (c >> 3) * cols * 128 + col * 128 + ((c ^ col) & 7) * 16) =
+            make_uint4(half2_of(w[n][i].x), half2_of(w[n][i].y), half2_of(w[n][i].z), half2_of(w[n][i].w));
+    }
+    if (lane * 8 < dr)
+      *reinterpret_cast<uint4*>(image + cols * 2 * r + col * 2 * dr + (lane ^ f.key_swizzle(col)) * 16) =
+          make_uint4(scaled(key[n].x), scaled(key[n].y), scaled(key[n].z), scaled(key[n].w));
   }
-  if (lane * 8 < dr)
-    *reinterpret_cast<uint4*>(image + cols * 2 * r + col * 2 * dr + (lane ^ f.key_swizzle(col)) * 16) =
-        make_uint4(scaled(key.x), scaled(key.y), scaled(key.z), scaled(key.w));
 }
 
 // Two prefix sums over the requests (groups, tiles) in every CTA; the first enters the list, a warp per request, the
 // others (of bf16 queries) write the groups' images, half a group each in turn.  A batch whose `starts` do not ascend inside
 // the nodes gets no groups and a count of -1.  As a part of the attention, each CTA writing the image of its next
 // group itself when the last one's products are done, the images took 13000 cycles of every change between groups.
-__global__ void __launch_bounds__(kPlanThreads, 3) tree_plan_kernel(PlanArgs a) {
+__global__ void __launch_bounds__(kPlanThreads, 2) tree_plan_kernel(PlanArgs a) {
   __shared__ int s_first[kMaxRequests + 1], s_tile[kMaxRequests + 1];
   __shared__ int warp_g[kPlanThreads / 32], warp_t[kPlanThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -262,9 +274,14 @@ __global__ void __launch_bounds__(kPlanThreads, 3) tree_plan_kernel(PlanArgs a) 
     }
     const int skip = (v - s_first[b]) * a.cols, col0 = a.starts[b] * a.heads + skip;
     const int cols = a.starts[b + 1] * a.heads - col0;
-    for (int c = (u & 1) * half + warp; c < ((u & 1) + 1) * half; c += kPlanThreads / 32)
-      put_column(a.q + (long long)(col0 + c) * (a.f.r + a.f.dr), c < cols, a.image + (long long)v * image_bytes(a.cols, a.f),
-                 c, a.cols, a.scale_log2, a.f);
+    const bf16* q = a.q + (long long)col0 * (a.f.r + a.f.dr);
+    uint8_t* image = a.image + (long long)v * image_bytes(a.cols, a.f);
+    // Half a group: two columns a warp of 64, one of 32.
+    constexpr int kWarps = kPlanThreads / 32;
+    if (a.cols == 64)
+      put_columns<2>(q, cols, image, (u & 1) * half + warp, kWarps, a.cols, a.scale_log2, a.f);
+    else
+      put_columns<1>(q, cols, image, (u & 1) * half + warp, kWarps, a.cols, a.scale_log2, a.f);
   }
 }
 
@@ -587,6 +604,7 @@ __global__ void __launch_bounds__(NC * 4, 2) tree_join_dense_kernel(JoinArgs a) 
   const int lo = a.starts[group.x], count = a.starts[group.x + 1] - lo, n_rows = min(count, kMaxNodes);
   const int steps = (n_rows + 15) / 16;                // of 16 rows
   const int2 parts = group.w > 0 ? a.parts[v] : make_int2(0, 0);
+  static_assert(kPlanThreads / 32 == 16, "half a group is one or two columns of every warp");
   if (tid < NC) {
     unsigned long long seen = 0;
     if (tid < group.z) {
@@ -756,10 +774,18 @@ __global__ void __launch_bounds__(NC * 4, 2) tree_join_dense_kernel(JoinArgs a) 
       a.lse[group.y + col] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
   }
   // ---- values: runs of 32 latents, every second is this warp's
+  constexpr int F = 2;                                 // parts in flight
+  float w_first[2][F];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int n = 0; n < F; ++n) {
+      const int col = c ? c1 : c0;
+      w_first[c][n] = n < parts.y && col < group.z ? exp2f(ml[n * NC + col].x - whole_m[c]) : 0.f;
+    }
   const float inv[2] = {whole_l[0] == 0.f ? 0.f : 1.f / whole_l[0], whole_l[1] == 0.f ? 0.f : 1.f / whole_l[1]};
   for (int c = half; c < r / 32; c += 2) {
     // The first parts' loads go ahead of the products.
-    constexpr int F = 2;
     float4 x0[2][F], x1[2][F];
     float w_part[2][F];
     auto load_parts = [&](int n0) {
@@ -774,7 +800,7 @@ __global__ void __launch_bounds__(NC * 4, 2) tree_join_dense_kernel(JoinArgs a) 
             const float* part = a.o_part + ((long long)(parts.x + n) * NC + col) * r + c * 32 + 8 * t;
             x0[col2][f] = *reinterpret_cast<const float4*>(part);
             x1[col2][f] = *reinterpret_cast<const float4*>(part + 4);
-            w_part[col2][f] = exp2f(ml[n * NC + col].x - whole_m[col2]);
+            w_part[col2][f] = n0 == 0 ? w_first[col2][f] : exp2f(ml[n * NC + col].x - whole_m[col2]);
           }
         }
     };
