@@ -35,7 +35,7 @@ TreePlan plan_tree(const mtla_qpool_config* c, int B, int n_nodes) {
     if (n > cols) cols = n;
   }
   p.o_part = 0;
-  p.ml_part = align_up(cols * c->latent_rank * 4, 256);
+  p.ml_part = align_up(cols * align_up(c->latent_rank, 128) * 4, 256);
   p.parts = p.ml_part + align_up(cols * 8, 256);
   p.groups = p.parts + align_up(groups * 8, 256);
   p.prefix = p.groups + align_up(groups * 16, 256);
@@ -244,6 +244,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   j.n_nodes = n_nodes;
   j.heads = cfg->n_heads;
   j.cols = cols;
+  j.part_row = tensor ? (cfg->latent_rank + 127) / 128 * 128 : cfg->latent_rank;
   j.n_error_words = tensor ? (int)(tiles < sms ? tiles : sms) : 0;
   j.f = a.f;
   return dtype == MTLA_DTYPE_BF16 ? launch_join<bf16>(j, groups, dev, st) : launch_join<float>(j, groups, dev, st);

@@ -120,7 +120,7 @@ __device__ __forceinline__ void decode_pairs(uint32_t w, uint32_t (&o)[4]) {
 }
 
 // A segment's output sums, this thread's latent of every block (lane 8j + g of a quarter holds latent 4g + j), into
-// the segment's part [NC][r], shared out among STEP groups of four warps in pieces of 16 columns of a block: added to
+// the segment's part [NC][128 NB], shared out among STEP groups of four warps in pieces of 16 columns of a block: added to
 // what has been set down there, which `fac` brings to the present references, or without `add` as they are.
 template <int NC, int NB, int STEP>
 __device__ __forceinline__ void set_down(float* part, uint32_t taddr, const float* fac, bool add, int cols, int r, int lat,
@@ -132,15 +132,21 @@ __device__ __forceinline__ void set_down(float* part, uint32_t taddr, const floa
     ptx::tmem_ld_x16(taddr + mb * NC + c0, o);
     ptx::tmem_wait_ld();
     if (row >= r) continue;
-    float* dst = part + c0 * r + row;
+    constexpr int kRow = 128 * NB;             // a column's place in a part: every store has a constant offset
+    float* dst = part + c0 * kRow + row;
     if (add) {
 #pragma unroll
       for (int j = 0; j < 16; ++j)
-        if (c0 + j < cols) o[j] = __float_as_uint(fmaf(dst[j * r], fac[c0 + j], __uint_as_float(o[j])));
+        if (c0 + j < cols) o[j] = __float_as_uint(fmaf(dst[j * kRow], fac[c0 + j], __uint_as_float(o[j])));
     }
+    if (c0 + 16 <= cols) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j, dst += r)
-      if (c0 + j < cols) *dst = __uint_as_float(o[j]);
+      for (int j = 0; j < 16; ++j) dst[j * kRow] = __uint_as_float(o[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (c0 + j < cols) dst[j * kRow] = __uint_as_float(o[j]);
+    }
   }
 }
 
@@ -544,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           ok = __all_sync(0xffffffffu, wait(misc->end_full[seg & 1], seg >> 1) && wait(misc->o_full[seg & 1], seg >> 1));
           if (!ok) break;
           tc_fence_after_sync();
-          set_down<NC, NB, VG>(a.o_part + ((long long)blockIdx.x + info.group) * NC * r, lane_tm + T::kColO,
+          set_down<NC, NB, VG>(a.o_part + ((long long)blockIdx.x + info.group) * (NC * 128 * NB), lane_tm + T::kColO,
                                misc->end_fac[seg & 1], info.flags & kFoldedNow, info.cols, r,
                                q * 32 + 4 * (lane & 7) + (lane >> 3), grp);
           tc_fence_before_sync();
@@ -634,7 +640,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
         group_sync();
         if (ok) {
           tc_fence_after_sync();
-          set_down<NC, NB, 2>(a.o_part + ((long long)blockIdx.x + info.group) * NC * r,
+          set_down<NC, NB, 2>(a.o_part + ((long long)blockIdx.x + info.group) * (NC * 128 * NB),
                               tmem + ((uint32_t)(q * 32) << 16) + T::kColO, misc->fac, flags & kFolded, info.cols, r,
                               q * 32 + 4 * (lane & 7) + (lane >> 3), gr);
           tc_fence_before_sync();

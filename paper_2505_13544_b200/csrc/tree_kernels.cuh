@@ -295,14 +295,14 @@ struct JoinArgs {
   const int4* groups;
   const int *first, *n_groups;
   const int2* parts;         // [groups] first part, number of parts
-  const float* o_part;       // [parts][cols][r]
+  const float* o_part;       // [parts][cols][part_row], r of each row used
   const float* ml_part;      // [parts][cols][2]
   const int* error_words;
   void* out;
   float* lse;
   long long row_stride;
   float scale_log2;
-  int batch, n_nodes, heads, cols, n_error_words;
+  int batch, n_nodes, heads, cols, part_row, n_error_words;
   qp::Format f;
 };
 
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(kJoinThreads, 5) tree_join_kernel(JoinArgs a) 
       if (n >= parts.y) return;
       const long long at = (long long)(parts.x + n) * a.cols + parts.z;
       ml = reinterpret_cast<const float2*>(a.ml_part)[at];
-      load_part<T>(a.o_part + at * r, r, y);
+      load_part<T>(a.o_part + at * a.part_row, r, y);
     };
     load_one(0);
     Run run;
@@ -534,7 +534,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
         if (n >= parts.y) break;
         const long long at = (long long)(parts.x + n) * a.cols + parts.z;
         ml[i] = reinterpret_cast<const float2*>(a.ml_part)[at];
-        load_part<T>(a.o_part + at * r, r, x[i]);
+        load_part<T>(a.o_part + at * a.part_row, r, x[i]);
       }
 #pragma unroll
       for (int i = 0; i < U; ++i)
@@ -797,7 +797,7 @@ __global__ void __launch_bounds__(NC * 4, 2) tree_join_dense_kernel(JoinArgs a) 
           x0[col2][f] = x1[col2][f] = make_float4(0.f, 0.f, 0.f, 0.f);
           w_part[col2][f] = 0.f;
           if (n < parts.y && col < group.z) {
-            const float* part = a.o_part + ((long long)(parts.x + n) * NC + col) * r + c * 32 + 8 * t;
+            const float* part = a.o_part + ((long long)(parts.x + n) * NC + col) * a.part_row + c * 32 + 8 * t;
             x0[col2][f] = *reinterpret_cast<const float4*>(part);
             x1[col2][f] = *reinterpret_cast<const float4*>(part + 4);
             w_part[col2][f] = n0 == 0 ? w_first[col2][f] : exp2f(ml[n * NC + col].x - whole_m[col2]);
