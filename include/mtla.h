@@ -450,9 +450,10 @@ int mtla_tree_map(const int32_t* held, const int32_t* starts, const int32_t* par
  * softmax(scale q [c ; k]^T) c over the first slots[b] slots of the pages in row b of `table` (as for
  * mtla_qpool_attend) and the rows of the request's nodes j < 64 whose bit j of seen[node] is set (bits behind its nodes
  * are ignored).  lse (device [n_nodes][n_heads], fp32, may be NULL) as there.  dtype is that of q, rows and out; sums are
- * fp32 and probabilities of slots rounded as there, drafted rows are multiplied in fp32.  A row that a node does
- * not see never reaches its result, whatever it holds.  A node that sees nothing (slots of page numbers outside the
- * pool are left out) gives zeros and minus infinity.  Nodes of no request are left as they were; a batch whose
+ * fp32, probabilities of slots are rounded as there, those of drafted rows to 16 bits (bf16 with many columns, nodes times
+ * heads) or not at all.  A row that a node does not see never reaches its result, whatever it holds; one with an
+ * infinity or a NaN may give NaN to all of a node that sees it.  A node that sees nothing (slots of page numbers
+ * outside the pool are left out) gives zeros and minus infinity.  Nodes of no request are left as they were; a batch whose
  * `starts` are out of order gives NaN for all n_nodes.
  * workspace: device, 256-byte aligned, mtla_qpool_tree_workspace_bytes(cfg, B, n_nodes) bytes (0 if invalid),
  * otherwise as for mtla_qpool_attend. */

@@ -209,30 +209,30 @@ __global__ void __launch_bounds__(kPlanThreads, 2) tree_plan_kernel(PlanArgs a) 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  auto tiles_of = [&](int b) {
-    const int n = max(a.slots[b], 0);
+  auto tiles_of = [&](int slots) {
+    const int n = max(slots, 0);
     const int pages = min(n / qp::kPageRows + (n % qp::kPageRows != 0), a.width);
     return (pages + a.tile_pages - 1) / a.tile_pages;
   };
   const int per = ceil_div(a.batch, kPlanThreads), lo = min(a.batch, tid * per), hi = min(a.batch, lo + per);
   bool wrong = a.starts[0] < 0;
-  for (int b = lo; b < hi; ++b) wrong |= a.starts[b] > a.starts[b + 1] || a.starts[b + 1] > a.n_nodes;
+  // (Lengths that the host has found to fit 32 bits only if the batch is in order.)
+  int sum_g = 0, sum_t = 0;
+  for (int b = lo; b < hi; ++b) {
+    const int begin = a.starts[b], end = a.starts[b + 1], tiles = tiles_of(a.slots[b]);
+    wrong |= begin > end || end > a.n_nodes || begin < 0;
+    const int g = wrong ? 0 : ceil_div((end - begin) * a.heads, a.cols);
+    s_first[b] = sum_g;
+    s_tile[b] = sum_t;
+    sum_g += g;
+    sum_t += g * tiles;
+  }
   if (__syncthreads_or(wrong)) {
     if (blockIdx.x == 0 && tid == 0) {
       *a.n_groups = -1;
       a.prefix[0] = 0;
     }
     return;
-  }
-  // Ascending requests have at most as many groups as there is room for, and tiles that the host has found to fit
-  // 32 bits.
-  int sum_g = 0, sum_t = 0;
-  for (int b = lo; b < hi; ++b) {
-    const int g = ceil_div((a.starts[b + 1] - a.starts[b]) * a.heads, a.cols);
-    s_first[b] = sum_g;
-    s_tile[b] = sum_t;
-    sum_g += g;
-    sum_t += g * tiles_of(b);
   }
   int in_g = sum_g, in_t = sum_t;
 #pragma unroll
@@ -251,8 +251,8 @@ __global__ void __launch_bounds__(kPlanThreads, 2) tree_plan_kernel(PlanArgs a) 
   if (blockIdx.x == 0) {
     for (int b = tid; b <= a.batch; b += kPlanThreads) a.first[b] = s_first[b];
     for (int b = warp; b < a.batch; b += kPlanThreads / 32) {
-      const int col0 = a.starts[b] * a.heads, cols = a.starts[b + 1] * a.heads - col0, tiles = tiles_of(b);
-      const int slots = min(max(a.slots[b], 0), (int)min((long long)a.width * qp::kPageRows, 0x7fffffffll));
+      const int col0 = a.starts[b] * a.heads, cols = a.starts[b + 1] * a.heads - col0, n_slots = a.slots[b];
+      const int tiles = tiles_of(n_slots), slots = min(max(n_slots, 0), (int)min((long long)a.width * qp::kPageRows, 0x7fffffffll));
       const int g0 = s_first[b], n = s_first[b + 1] - g0;
       for (int i = lane; i < n; i += 32) {
         a.groups[g0 + i] = make_int4(b, col0 + i * a.cols, min(a.cols, cols - i * a.cols), slots);

@@ -143,3 +143,84 @@ def test_a_captured_product_and_other_streams(n):
     torch.cuda.synchronize()
     for z in got:
         assert torch.equal(z, -y)
+
+
+# Over 1.5 10^8 products of weights and rows: the tensor-core kernel, with and without shares of the inputs.
+MANY = [(9, 8192, 2600), (16, 4104, 5001), (17, 4104, 2200), (32, 4096, 1300), (33, 2056, 2300), (64, 2048, 1201),
+        (65, 1032, 2400), (128, 1024, 1160), (129, 1000, 1250), (300, 712, 777), (513, 520, 600), (700, 136, 1700),
+        (2000, 8, 9500)]
+
+
+@pytest.mark.parametrize("n,n_in,n_out", MANY)
+def test_product_of_many_rows(n, n_in, n_out):
+    check_product(n, n_in, n_out, "bf16", size=3.0)
+
+
+def test_many_rows_with_strides_and_specials():
+    n, n_in, n_out = 200, 1000, 801
+    packed, x, y = check_product(n, n_in, n_out, "bf16")
+    wide = torch.full((n, 1040), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[:, 8:1008] = x
+    for width, at in ((900, 2), (901, 3), (802, 0)):       # pairs of outputs aligned or not
+        out = torch.full((n + 1, width), 7.0, dtype=torch.bfloat16, device="cuda")
+        got = out[:n, at:at + n_out]
+        M.mtla_qweight_product(packed, wide[:, 8:1008], n_out, out=got)
+        assert torch.equal(got, y)
+        got.fill_(7)
+        assert (out == 7).all()
+    bad = x.clone()
+    bad[2], bad[130], bad[130, 9] = float("nan"), 0, float("-inf")
+    z = M.mtla_qweight_product(packed, bad, n_out)
+    keep = [i for i in range(n) if i not in (2, 130)]
+    assert torch.equal(z[keep], y[keep]) and torch.isnan(z[2]).all()
+    w = M.mtla_qweight_unpack(packed, n_in, n_out, dtype=torch.float32)[9]
+    assert torch.isnan(z[130][w == 0]).all() and torch.equal(z[130].float()[w != 0], -torch.inf * w[w != 0].sign())
+
+
+def test_every_code_and_scale_of_many_rows():
+    from oracle import qpool_oracle as Q
+    w = np.zeros((32, len(Q.SCALES) - 1))
+    w[:16] = np.concatenate([Q.MAGNITUDES, -Q.MAGNITUDES])[:, None] * Q.SCALES[1:][None]
+    w[16] = 6 * Q.SCALES[1:]
+    packed = M.mtla_qweight_pack(torch.from_numpy(w).float().cuda())
+    rows = 32 * 800
+    y = M.mtla_qweight_product(packed, torch.eye(32, dtype=torch.bfloat16, device="cuda").repeat(800, 1), w.shape[1])
+    assert np.array_equal(host(y[:64]), np.tile(w, (2, 1))) and np.array_equal(host(y[rows - 32:]), w)
+
+
+@pytest.mark.parametrize("n", [24, 256])
+def test_many_rows_captured_and_on_other_streams(n):
+    packed, x, y = check_product(n, 4096, 2000, "bf16")
+    out = torch.empty_like(y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        M.mtla_qweight_product(packed, x, 2000, out=out)
+    for _ in range(3):
+        out.fill_(5)
+        graph.replay()
+        assert torch.equal(out, y)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = [M.mtla_qweight_product(packed, x, 2000, stream=s) for _ in range(6) for s in streams]
+    torch.cuda.synchronize()
+    for z in got:
+        assert torch.equal(z, y)
+
+
+def test_products_that_follow_one_another():
+    """Two layers' products in a row on one stream, each reading what the one before has written."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    w1, w2 = (torch.randn(1024, 1024, device="cuda", generator=g) / 32 for _ in range(2))
+    p1, p2 = M.mtla_qweight_pack(w1), M.mtla_qweight_pack(w2)
+    u1, u2 = (M.mtla_qweight_unpack(p, 1024, 1024, dtype=torch.float32).double() for p in (p1, p2))
+    for n in (1, 12, 40, 400):
+        x = torch.randn(n, 1024, device="cuda", generator=g).bfloat16()
+        for _ in range(20):
+            h = M.mtla_qweight_product(p1, x, 1024)
+            y = M.mtla_qweight_product(p2, h, 1024)
+        for a, u, z in ((x, u1, h), (h, u2, y)):
+            want, mag = a.double() @ u, a.double().abs() @ u.abs()
+            tol = 2.0 ** -8 * want.abs() + mag * (1024 * 2.0 ** -23 + 2.0 ** -24)
+            assert ((z.double() - want).abs() <= tol).all()

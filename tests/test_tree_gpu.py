@@ -339,3 +339,113 @@ def test_on_another_gpu_than_the_current_one():
         got = M.mtla_qpool_attend_tree(*args, scale=1.0)
     torch.cuda.synchronize(0)
     assert torch.equal(want[0], got[0])
+
+
+# ------------------------------------------------------------------------------ many columns, long contexts
+
+def pool_of(rows, heads, r, dr, junk=0xFF):
+    """A pool of one sequence's rows (as stored) and its table row."""
+    n = rows.shape[0]
+    n_pages = -(-n // 64) + 1
+    cfg = M.make_qpool_config(n_heads=heads, latent_rank=r, rope_dim=dr, n_pages=n_pages)
+    pages = torch.full((n_pages, M.mtla_qpool_page_bytes(cfg)), junk, dtype=torch.uint8, device="cuda")
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(n))[:-(-n // 64)].int().cuda()
+    j = torch.arange(n, device="cuda")
+    index = order[j // 64].long() * 64 + j % 64
+    M.mtla_qpool_write(cfg, pages, rows, index)
+    return cfg, pages, order, host(M.mtla_qpool_read(cfg, pages, index, dtype=torch.float32))
+
+
+@pytest.mark.parametrize("masks", ["tree", "any"])
+@pytest.mark.parametrize("r,dr", [(64, 32), (192, 64), (512, 32)])
+def test_many_columns(r, dr, masks):
+    """More than 148 groups of columns: the drafted rows go through matrix products."""
+    lens, counts = [130, 0, 64, 1, 300], [64, 63, 80, 64, 65]
+    s = tree_setup(lens, counts, 32, r, dr, "bf16", r, masks=masks, front=3, pad=2)
+    out = torch.full((sum(counts) + 5, 32, r), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((sum(counts) + 5, 32), 7.0, device="cuda")
+    nodes = {*range(3, 3 + sum(counts), 13), 66, 67, 129, 130, 2 + sum(counts)}
+    check_tree(s, 0.125, "bf16", lens, nodes=nodes, out=out, lse=lse)
+    for t in (out, lse):
+        assert (t[:3] == 7).all() and (t[-2:] == 7).all() and torch.isfinite(t).all()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_many_columns_and_rows_that_hold_anything(bad):
+    """Whoever sees such a row gets NaN, the others are as they were without it, bit by bit."""
+    lens, counts = [130, 0, 64, 1, 300], [64, 64, 64, 64, 64]
+    s = list(tree_setup(lens, counts, 32, 128, 32, "bf16", 2))
+    args = lambda rows: (*s[:5], rows.cuda(), dev(s[6], torch.int64), s[7].cuda())
+    clean, clean_lse = M.mtla_qpool_attend_tree(*args(s[5]), scale=0.125)
+    rows = s[5].clone()
+    rows[5, 3], rows[64 + 17, 130], rows[256] = bad, bad, bad
+    out, lse = M.mtla_qpool_attend_tree(*args(rows), scale=0.125)
+    sees = torch.tensor([bool((i // 64 == 0 and s[6][i] >> 5 & 1) or (i // 64 == 1 and s[6][i] >> 17 & 1)
+                              or (i // 64 == 4 and s[6][i] & 1)) for i in range(320)], device="cuda")
+    assert sees.any() and torch.isnan(out[sees]).all() and torch.isnan(lse[sees]).all()
+    # (Zeros in the place of the row's numbers: nothing else of a sum changes.)
+    assert torch.equal(out[~sees], clean[~sees]) and torch.equal(lse[~sees], clean_lse[~sees])
+
+
+def test_many_columns_that_see_nothing_and_a_refused_batch():
+    lens, counts = [0] * 5, [64] * 5
+    s = list(tree_setup(lens, counts, 32, 64, 32, "bf16", 2))
+    s[6] = [0 if i % 3 else s[6][i] for i in range(320)]
+    check_tree(s, 0.125, "bf16", lens, nodes=set(range(0, 320, 7)))
+    out, lse = M.mtla_qpool_attend_tree(*s[:4], dev([0, 64, 32, 192, 256, 320]), s[5].cuda(), dev(s[6], torch.int64),
+                                        s[7].cuda(), scale=1.0)
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+def test_sums_over_many_tiles():
+    """Segments of more than 128 tiles, latents of one sign: the sums leave tensor memory in between, so what the matrix
+    unit cuts off does not grow with the length.  Five requests share the pages."""
+    n, heads, r, dr = 25600 + 77, 32, 64, 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows = torch.randn(n, r + dr, device="cuda", generator=g)
+    rows[:, :r] = rows[:, :r].abs() + 0.5
+    cfg, pages, order, seq = pool_of(rows, heads, r, dr)
+    counts, lens = [64] * 5, [n, n - 5, 25600, 20000, n]
+    q = (torch.randn(320, heads, r + dr, device="cuda", generator=g) * 0.3).bfloat16()
+    mine = torch.randn(320, r + dr, device="cuda", generator=g).bfloat16()
+    seen = [1 << (i % 64) for i in range(320)]
+    s = (cfg, pages, order[None].repeat(5, 1).contiguous(), dev(lens), dev(starts_of(counts)), mine.cpu(),
+         [v - (1 << 64) if v >> 63 else v for v in seen], q.cpu(), [seq] * 5, starts_of(counts))
+    check_tree(s, 0.125, "bf16", lens, nodes={0, 63, 64, 130, 200, 319})
+
+
+@pytest.mark.parametrize("heads,count", [(4, 3), (32, 7)])
+def test_scores_that_rise_from_tile_to_tile(heads, count):
+    """Every tile's largest score exceeds the one before by more than 2^8: references rise and sums are rescaled, in one
+    CTA's share and across shares; then the drafted rows exceed them again, or fall far short."""
+    n, r, dr = 700, 128, 32
+    g = torch.Generator().manual_seed(4)
+    q = torch.randn(count, heads, r + dr, generator=g).bfloat16()
+    rows = torch.randn(n, r + dr, generator=g) * 0.1
+    rows[::50] += q[0, 0].float()[None] * torch.linspace(0.05, 1.0, len(rows[::50]))[:, None]
+    cfg, pages, order, seq = pool_of(rows.cuda(), heads, r, dr)
+    mine = torch.stack([q[i, 0].float() * f for i, f in zip(range(count), [1.2, 0.01, 0.5, 1.5, 1.0, 0.7, 0.1])]).bfloat16()
+    for batch in (1, 200):                             # few and many tiles in a share
+        counts, lens = [count] * batch, [n - 3 * (i % 60) for i in range(batch)]
+        s = (cfg, pages, order[None].repeat(batch, 1).contiguous(), dev(lens), dev(starts_of(counts)),
+             mine.repeat(batch, 1), [(1 << (i % count)) | 1 for i in range(count * batch)], q.repeat(batch, 1, 1),
+             [seq] * batch, starts_of(counts))
+        check_tree(s, 2.0, "bf16", lens, nodes={*range(count), count * batch - 1, count * batch // 2})
+
+
+def test_many_requests_and_few_slots():
+    """A segment every tile, groups of all widths, requests without slots or nodes between them."""
+    rng = np.random.default_rng(8)
+    lens = [int(v) for v in rng.choice([0, 1, 70, 128, 129, 200], 300)]
+    counts = [int(v) for v in rng.choice([0, 1, 2, 5, 9], 300)]
+    for heads, r in ((8, 64), (31, 128), (16, 256)):
+        s = tree_setup(lens, counts, heads, r, 32, "bf16", heads)
+        check_tree(s, 0.125, "bf16", lens, nodes=set(range(0, sum(counts), 9)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_the_most_requests(dtype):
+    """4096 requests of one node."""
+    lens, counts = [3] * 4096, [1] * 4096
+    s = tree_setup(lens, counts, 2, 64, 32, dtype, 5)
+    check_tree(s, 0.125, dtype, lens, nodes={0, 1, 31, 32, 2047, 4095})
