@@ -55,9 +55,10 @@ struct AttnArgs {
   float scale_log2;          // scale * log2(e)
   int n_heads, batch, width, n_pages, n_error_words;
   Format f;
-  // Column groups of drafted trees (tree_kernels.cuh) in the place of sequences: how many there are, the tiles before
-  // each, and its request, first column, columns and slots.  Their results are always parts, of `cols` columns.
-  const int* n_groups;
+  // Column groups of drafted trees (tree_kernels.cuh) in the place of sequences: how many there are and their tiles, the
+  // tiles before each, and its request, first column, columns and slots.  Their results are always parts, of `cols`
+  // columns.
+  const int2* listed;
   const int* prefix;
   const int4* groups;
   const uint8_t* image;      // the groups' queries as the tensor-core kernel wants them
@@ -269,8 +270,9 @@ __global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
   const int* const prefix = TREE ? a.prefix : own_prefix;
-  const int n_seqs = TREE ? max(*a.n_groups, 0) : a.batch;
-  const long long total = TREE ? prefix[n_seqs] : tile_prefix<1>(a, own_prefix, warp_sums, kAttnThreads);
+  const int2 listed = TREE ? *a.listed : make_int2(a.batch, 0);
+  const int n_seqs = TREE ? max(listed.x, 0) : a.batch;
+  const long long total = TREE ? listed.y : tile_prefix<1>(a, own_prefix, warp_sums, kAttnThreads);
   if (total == 0) return;
   // With fewer tiles than CTAs the rest stays out, so that every share has a tile and the parts of
   // a sequence follow one another without a gap.

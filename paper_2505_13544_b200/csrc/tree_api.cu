@@ -18,7 +18,7 @@ constexpr int kMostCtas = 2 * kPlanSms;          // of the launch over the conte
 constexpr int kLeastCols = 16, kMostCols = 64;   // of a group
 
 // Sized for any group width, so that the choice between the kernels stays the call's.
-struct TreePlan { size_t o_part, ml_part, parts, groups, prefix, first, n_groups, error_words, image, total; };
+struct TreePlan { size_t o_part, ml_part, parts, groups, prefix, first, listed, error_words, image, total; };
 long long most_groups(const mtla_qpool_config* c, int B, int n_nodes, int cols) {
   return (long long)n_nodes * c->n_heads / cols + (B < n_nodes ? B : n_nodes);
 }
@@ -40,8 +40,8 @@ TreePlan plan_tree(const mtla_qpool_config* c, int B, int n_nodes) {
   p.groups = p.parts + align_up(groups * 8, 256);
   p.prefix = p.groups + align_up(groups * 16, 256);
   p.first = p.prefix + align_up((groups + 1) * 4, 256);
-  p.n_groups = p.first + align_up(((size_t)B + 1) * 4, 256);
-  p.error_words = p.n_groups + 256;
+  p.listed = p.first + align_up(((size_t)B + 1) * 4, 256);
+  p.error_words = p.listed + 256;
   p.image = p.error_words + align_up(kPlanSms * 4, 256);
   size_t image = 0;
   for (int w = 32; w <= kMostCols; w *= 2) {
@@ -182,7 +182,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   pa.groups = reinterpret_cast<int4*>(ws + p.groups);
   pa.prefix = reinterpret_cast<int*>(ws + p.prefix);
   pa.first = reinterpret_cast<int*>(ws + p.first);
-  pa.n_groups = reinterpret_cast<int*>(ws + p.n_groups);
+  pa.listed = reinterpret_cast<int2*>(ws + p.listed);
   pa.batch = B;
   pa.n_nodes = n_nodes;
   pa.heads = cfg->n_heads;
@@ -213,7 +213,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   a.n_pages = cfg->n_pages;
   a.f = pa.f;
   a.image = pa.image;
-  a.n_groups = pa.n_groups;
+  a.listed = pa.listed;
   a.prefix = pa.prefix;
   a.groups = pa.groups;
   a.cols = cols;
@@ -231,7 +231,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   j.starts = starts;
   j.groups = pa.groups;
   j.first = pa.first;
-  j.n_groups = pa.n_groups;
+  j.listed = pa.listed;
   j.parts = a.seq_parts;
   j.o_part = a.o_part;
   j.ml_part = a.ml_part;

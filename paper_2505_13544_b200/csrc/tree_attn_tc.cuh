@@ -206,8 +206,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
   grid_dependency_wait();
 
   const int* const prefix = a.prefix;
-  const int n_groups = max(*a.n_groups, 0);
-  const long long total = prefix[n_groups];
+  const int2 listed = *a.listed;
+  const int n_groups = max(listed.x, 0);
+  const long long total = listed.y;
   const int ctas = (int)(total < gridDim.x ? total : gridDim.x);
   int g0 = 0, g1 = 0;
   if ((int)blockIdx.x < ctas) {

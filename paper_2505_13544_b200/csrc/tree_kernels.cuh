@@ -123,7 +123,7 @@ struct PlanArgs {
   int4* groups;              // request, first column, columns, slots
   int* prefix;               // [groups + 1] tiles before every group
   int* first;                // [batch + 1] first group of every request
-  int* n_groups;
+  int2* listed;              // groups (-1: the batch is refused), their tiles
   const bf16* q;             // [n_nodes][heads][r + d_R]
   uint8_t* image;            // [groups] of image_bytes, or nullptr
   float scale_log2;
@@ -229,8 +229,7 @@ __global__ void __launch_bounds__(kPlanThreads, 2) tree_plan_kernel(PlanArgs a) 
   }
   if (__syncthreads_or(wrong)) {
     if (blockIdx.x == 0 && tid == 0) {
-      *a.n_groups = -1;
-      a.prefix[0] = 0;
+      *a.listed = make_int2(-1, 0);
     }
     return;
   }
@@ -260,7 +259,7 @@ __global__ void __launch_bounds__(kPlanThreads, 2) tree_plan_kernel(PlanArgs a) 
       }
     }
     if (tid == 0) {
-      *a.n_groups = total;
+      *a.listed = make_int2(total, s_tile[a.batch]);
       a.prefix[total] = s_tile[a.batch];
     }
     return;
@@ -293,7 +292,8 @@ struct JoinArgs {
   const long long* seen;     // [n_nodes]
   const int* starts;
   const int4* groups;
-  const int *first, *n_groups;
+  const int* first;
+  const int2* listed;
   const int2* parts;         // [groups] first part, number of parts
   const float* o_part;       // [parts][cols][part_row], r of each row used
   const float* ml_part;      // [parts][cols][2]
@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(kJoinThreads, 5) tree_join_kernel(JoinArgs a) 
   ptx::grid_dependency_wait();
   bool failed = false;
   for (int i = threadIdx.x; i < a.n_error_words; i += kJoinThreads) failed |= a.error_words[i] != 0;
-  const bool refused = *a.n_groups < 0;
+  const bool refused = a.listed->x < 0;
   failed = __syncthreads_or(failed) || refused;
   // Nodes behind the last request are left as they were; those of a refused batch all get NaN.
   const uint32_t columns = (uint32_t)(refused ? a.n_nodes : a.starts[a.batch]) * a.heads;
@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
   ptx::grid_dependency_wait();
   bool failed = false;
   for (int i = threadIdx.x; i < a.n_error_words; i += kSplitThreads) failed |= a.error_words[i] != 0;
-  const bool refused = *a.n_groups < 0;
+  const bool refused = a.listed->x < 0;
   failed = __syncthreads_or(failed) || refused;
   const uint32_t columns = (uint32_t)(refused ? a.n_nodes : a.starts[a.batch]) * a.heads;
   for (uint32_t column = blockIdx.x; column < columns; column += gridDim.x) {
@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(NC * 4, 2) tree_join_dense_kernel(JoinArgs a) 
   bool failed = false;
   for (int i = tid; i < a.n_error_words; i += D::kThreads) failed |= a.error_words[i] != 0;
   failed = __syncthreads_or(failed);
-  const int n_groups = *a.n_groups, v = blockIdx.x;
+  const int n_groups = a.listed->x, v = blockIdx.x;
   bf16* out = static_cast<bf16*>(a.out);
   if (n_groups < 0) {                                  // the batch is refused
     const long long n = (long long)a.n_nodes * a.heads, step = (long long)gridDim.x * D::kThreads;
