@@ -2,18 +2,25 @@
 //
 // The mathematics, the orientation of both products and the expansion of the codes into tensor memory are those of
 // qpool_attn_tc.cuh; what differs is that a tree brings many columns (nodes times heads) to the same slots, so that
-// an expanded tile is used by NC = 64 of them instead of one sequence's heads.  The bound then is arithmetic: per
-// tile of 128 slots and r 512 the matrix unit needs 68 x 32 = 2180 cycles, the expansion of both operands about 1900 of
-// the issue slots, the softmax of 128 x 64 scores about 500.
+// an expanded tile is used by NC = 64 of them instead of one sequence's heads (32 where a request has no more).  Per tile
+// of 128 slots and r 512 the matrix unit needs 68 x 32 = 2180 cycles; what bounds the kernel is the issue of
+// instructions: 16100 a tile (expansion, softmax, the bookkeeping of both) are 4000 cycles of the four schedulers, and
+// a tile takes about 5400.  Eight requests of 64 nodes and 32 heads over 4096 slots: 204 us by itself, cold (the whole
+// call takes 226, its launches overlap), where products at the measured rate of large ones would take 88.
 //
 // Tensor memory holds the output sums (r / 128 blocks of NC columns), one or two score tiles and operand units of 32
 // columns: 64 latents of the 128 slots for the scores, or 64 slots of 128 latents for the values.  Units half as wide as
 // there leave three buffers for each product beside 64 columns of r 512.
 //
 // Groups of columns take the place of sequences; a group's result is always a part (reference, denominator, sums in 32
-// bits) that tree_join_kernel joins with the drafted rows.  Roles (28 warps): warp 0 issues the score products, warp 1
-// the value products, warp 2 is the producer; warp 3 fetches the queries; warps 4-11
-// expand for the scores, warps 12-19 for the values (and write the results); warps 20-27 are softmax.  Every wait is bounded as there.
+// bits) that the join kernels put together with the drafted rows.  Roles (28 warps): warp 0 issues the score products,
+// warp 1 the value products, warp 2 fetches the pages, warp 3 the queries; warps 4-11 expand for the scores, warps 12-19
+// for the values, and write the results; warps 20-27 are softmax.  Measured on the way (the same eight requests): expanding
+// warps of their own for either product 246 -> 237 us of this kernel; waits and indices of a tile outside the units'
+// loop 238 -> 221; probabilities handed over in halves, queries laid out ahead and results written by the value
+// warps 221 -> 212; issuing warps that ask before they wait 254 -> 245 of the whole call.  Twelve value warps instead
+// of eight leave 56 registers a thread and spill (232 us for 221); reading a unit's bytes ahead costs more instructions
+// than it hides (256 for 243).  Every wait is bounded as there.
 #pragma once
 
 #include "qpool_attn_tc.cuh"
@@ -417,9 +424,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     }
   } else if (warp < kSoftmaxWarp0) {
     // ------------------------------------------------------------------ expansion
-    // Groups of four warps, two for the scores' operand and three for the values', which takes longer, so that the
-    // scores' units never wait behind a value unit whose buffer waits for the probabilities.  A group takes every second
-    // (third) unit; it is decoded into registers before its buffer is waited for.  What a tile needs once, waits,
+    // Groups of four warps, two for either operand, so that the scores' units never wait behind a value unit whose
+    // buffer waits for the probabilities.  A group takes every second unit; it is decoded into registers before its buffer is waited for.  What a tile needs once, waits,
     // arrivals and addresses, is outside the units' loop: inside, it was a third of all instructions.
     reg_dealloc<kExpandRegs>();
     constexpr int VG = kValueWarps / 4;
