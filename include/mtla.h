@@ -467,7 +467,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
  * fp32 or bf16) is kept as e2m1 codes with a scale per 32 inputs of an output, codes and scales as in the pool
  * (see above; a group with an infinity or a NaN reads back as NaN), 4.25 bits a weight, in blocks of 128 inputs by 16
  * outputs filled up with zeros.  packed: device, 16-byte aligned, mtla_qweight_bytes(n_in, n_out) bytes (0 if
- * invalid).  n_in a multiple of 8, n_in and n_out up to 2^22.  unpack is exact in both types. */
+ * invalid).  n_in a multiple of 8 up to 2^16, n_out up to 2^22.  unpack is exact in both types. */
 size_t mtla_qweight_bytes(int32_t n_in, int32_t n_out);
 int mtla_qweight_pack(const void* w, int64_t w_stride, int32_t dtype, int32_t n_in, int32_t n_out, void* packed,
                       void* stream);

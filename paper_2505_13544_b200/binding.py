@@ -1106,6 +1106,8 @@ def mtla_qweight_pack(w: torch.Tensor, packed: torch.Tensor | None = None, strea
 
 def mtla_qweight_unpack(packed: torch.Tensor, n_in: int, n_out: int, *, dtype=torch.bfloat16, stream=None):
     """The weights [n_in][n_out] that a packed buffer stands for."""
+    if dtype not in _DTYPES:
+        raise TypeError("dtype: expected fp32 or bf16")
     dev = _gpu_of(packed, "packed")
     pp = _qweight_buffer(packed, n_in, n_out, dev)
     with _buffers_on(stream):

@@ -12,10 +12,13 @@ using namespace mtla::ops;
 
 namespace {
 
-constexpr int kMostSize = 1 << 22;               // inputs or outputs (2^19 / 8 grid rows)
+constexpr int kMostSize = 1 << 22;               // outputs (2^19 / 8 grid rows)
+// The matrix unit cuts its running sums off instead of rounding them, so a sum of one sign falls short in proportion to its
+// length: by 3.6e-4 after the 4096 steps of 2^16 inputs in one CTA, a tenth of the result's rounding to bf16.
+constexpr int kMostInputs = 1 << 16;
 
 bool good_shape(int n_in, int n_out) {
-  return n_in >= 8 && n_in % 8 == 0 && n_in <= kMostSize && n_out >= 1 && n_out <= kMostSize;
+  return n_in >= 8 && n_in % 8 == 0 && n_in <= kMostInputs && n_out >= 1 && n_out <= kMostSize;
 }
 
 int pack_call(const void* w, int64_t stride, int32_t dtype, int32_t n_in, int32_t n_out, const void* packed, void* stream,

@@ -425,8 +425,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
   } else if (warp < kSoftmaxWarp0) {
     // ------------------------------------------------------------------ expansion
     // Groups of four warps, two for either operand, so that the scores' units never wait behind a value unit whose
-    // buffer waits for the probabilities.  A group takes every second unit; it is decoded into registers before its buffer is waited for.  What a tile needs once, waits,
-    // arrivals and addresses, is outside the units' loop: inside, it was a third of all instructions.
+    // buffer waits for the probabilities.  A group takes every second unit, decoded into registers before its buffer is
+    // waited for.  What a tile needs once, waits, arrivals and addresses, is outside the units' loop: inside, it was a
+    // third of all instructions.
     reg_dealloc<kExpandRegs>();
     constexpr int VG = kValueWarps / 4;
     const bool scores_role = warp < kValueWarp0;

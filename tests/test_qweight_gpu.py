@@ -224,3 +224,19 @@ def test_products_that_follow_one_another():
             want, mag = a.double() @ u, a.double().abs() @ u.abs()
             tol = 2.0 ** -8 * want.abs() + mag * (1024 * 2.0 ** -23 + 2.0 ** -24)
             assert ((z.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("n,n_out", [(1, 33), (16, 33), (40, 200), (2048, 1280)])
+def test_the_most_inputs(n, n_out):
+    """65536 products of one sign.  The matrix unit cuts a running sum off at every step of 16 inputs, by less than two
+    units of the last of its 24 bits; the results are rounded to bf16.  2048 x 1280 is one CTA for all inputs."""
+    n_in = 1 << 16
+    g = torch.Generator(device="cuda").manual_seed(n)
+    packed = M.mtla_qweight_pack(torch.rand(n_in, n_out, device="cuda", generator=g).add_(0.1).bfloat16())
+    x = torch.rand(n, n_in, device="cuda", generator=g).add_(0.1).bfloat16()
+    y = M.mtla_qweight_product(packed, x, n_out)
+    w64 = M.mtla_qweight_unpack(packed, n_in, n_out, dtype=torch.float32).double()
+    rows = sorted({0, n // 3, n // 2, n - 1})
+    want = x[rows].double() @ w64
+    off = ((y[rows].double() - want) / want).abs().max().item()
+    assert off <= half_step(torch.bfloat16) + n_in / 16 * 2.0 ** -22, off

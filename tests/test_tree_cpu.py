@@ -91,7 +91,7 @@ def test_attend_tree_refuses():
 
 def test_qweight_refuses():
     lib = M.load_library()
-    for n_in, n_out in ((0, 1), (7, 1), (12, 4), (8, 0), (-8, 4), ((1 << 22) + 8, 1), (8, (1 << 22) + 1)):
+    for n_in, n_out in ((0, 1), (7, 1), (12, 4), (8, 0), (-8, 4), ((1 << 16) + 8, 1), ((1 << 22) + 8, 1), (8, (1 << 22) + 1)):
         assert M.mtla_qweight_bytes(n_in, n_out) == 0
         assert lib.mtla_qweight_pack(A, 1 << 23, 1, n_in, n_out, A, None) == -2
         assert lib.mtla_qweight_unpack(A, n_in, n_out, A, 1 << 23, 1, None) == -2
@@ -128,5 +128,7 @@ def test_host_tensors_are_refused_by_the_binding():
                                  torch.zeros(1, 288), torch.zeros(1, dtype=torch.int64), torch.zeros(1, 8, 288), scale=1.0)
     with pytest.raises(TypeError):
         M.mtla_qweight_pack(torch.zeros(128, 16))
+    with pytest.raises(TypeError):
+        M.mtla_qweight_unpack(torch.zeros(1088, dtype=torch.uint8), 128, 16, dtype=torch.float16)
     with pytest.raises(TypeError):
         M.mtla_qweight_product(torch.zeros(1088, dtype=torch.uint8), torch.zeros(1, 128), 16)

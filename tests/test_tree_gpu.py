@@ -10,7 +10,7 @@ import torch
 
 from oracle import tree_oracle as T
 from paper_2505_13544_b200 import binding as M
-from tests.test_operators_gpu import DT, attend_setup, bound, host
+from tests.test_operators_gpu import DT, attend_setup, bound, half_step, host
 
 pytestmark = pytest.mark.gpu
 
@@ -449,3 +449,66 @@ def test_the_most_requests(dtype):
     lens, counts = [3] * 4096, [1] * 4096
     s = tree_setup(lens, counts, 2, 64, 32, dtype, 5)
     check_tree(s, 0.125, dtype, lens, nodes={0, 1, 31, 32, 2047, 4095})
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("dtype,count,heads", [("bf16", 3, 5), ("bf16", 64, 32), ("fp32", 20, 16)])
+def test_a_query_that_is_not_finite_reaches_no_other(dtype, count, heads, bad):
+    lens, counts = [300, 65, 200, 1, 130], [count] * 5
+    s = list(tree_setup(lens, counts, heads, 128, 32, dtype, 21))
+    whole, _ = M.mtla_qpool_attend_tree(*s[:4], s[4], s[5].cuda(), dev(s[6], torch.int64), s[7].cuda(), scale=0.125)
+    s[7][1, 2, 7], s[7][count, 0, 130] = bad, bad
+    out, lse = M.mtla_qpool_attend_tree(*s[:4], s[4], s[5].cuda(), dev(s[6], torch.int64), s[7].cuda(), scale=0.125)
+    keep = torch.ones(5 * count, heads, dtype=torch.bool)
+    keep[1, 2] = keep[count, 0] = False
+    assert torch.isfinite(lse.cpu()[keep]).all() and torch.isnan(out.cpu()[~keep]).any(-1).all()
+    # Rescaling of sums goes by what a warp's columns need together, so the others may move by a few roundings.
+    d = (out.cpu()[keep].double() - whole.cpu()[keep].double()).abs().max().item()
+    assert d <= 2 * whole.abs().max().item() * (half_step(DT[dtype]) + 2.0 ** -11)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_offsets_past_32_bits(dtype):
+    """More than 2^31 elements in the queries, the results and the parts; the requests share their pages."""
+    heads, r, dr, batch = 32, 512, 64, 2055
+    n = batch * 64
+    assert n * heads * r > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(6)
+    cfg, pages, order, seq = pool_of(torch.randn(65, r + dr, device="cuda", generator=g), heads, r, dr)
+    lens = [65 - i % 3 for i in range(batch)]
+    q = torch.empty(n, heads, r + dr, dtype=DT[dtype], device="cuda").normal_(generator=g)
+    rows = torch.randn(n, r + dr, device="cuda", generator=g).to(DT[dtype])
+    seen = [(1 << i % 64) | 1 for i in range(n)]
+    seen = torch.tensor([v - (1 << 64) if v >> 63 else v for v in seen], device="cuda")
+    starts = starts_of([64] * batch)
+    out, lse = M.mtla_qpool_attend_tree(cfg, pages, order[None].repeat(batch, 1).contiguous(), dev(lens), dev(starts),
+                                        rows, seen, q, scale=0.125)
+    for i in (0, 63, 64, n // 2 - 1, 2 ** 31 // (heads * (r + dr)), 2 ** 31 // (heads * r) + 1, n - 64, n - 1):
+        b = i // 64
+        q64, mine, context = host(q[i]), host(rows[64 * b:64 * b + 64]), seq[:lens[b]]
+        bits = int(seen[i])
+        want, want_lse, mean_abs = T.attend_node(q64, context, mine, bits, 0.125, r)
+        both = np.concatenate([context, mine[[j for j in range(64) if bits >> j & 1]]])
+        tol, tol_lse = tree_bound(q64, both, 0.125, mean_abs, want, dtype, r, 5)
+        assert (np.abs(host(out[i]) - want) <= tol).all(), i
+        assert (np.abs(host(lse[i]) - want_lse) <= tol_lse + 2.0 ** -23 * np.abs(want_lse)).all(), i
+    assert all(torch.isfinite(out[i:i + 4096]).all() for i in range(0, n, 4096))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_pages_past_32_bits(dtype):
+    heads, r, dr, n = 8, 512, 64, 200
+    size = M.mtla_qpool_page_bytes(M.make_qpool_config(n_heads=heads, latent_rank=r, rope_dim=dr, n_pages=1))
+    n_pages = 2 ** 31 // size + 9
+    cfg = M.make_qpool_config(n_heads=heads, latent_rank=r, rope_dim=dr, n_pages=n_pages)
+    pages = torch.full((n_pages, size), 0xFF, dtype=torch.uint8, device="cuda")
+    order = torch.tensor([n_pages - 1, 3, n_pages - 7, n_pages - 2], dtype=torch.int32, device="cuda")
+    j = torch.arange(n, device="cuda")
+    index = order[j // 64].long() * 64 + j % 64
+    g = torch.Generator(device="cuda").manual_seed(9)
+    M.mtla_qpool_write(cfg, pages, torch.randn(n, r + dr, device="cuda", generator=g), index)
+    seq = host(M.mtla_qpool_read(cfg, pages, index, dtype=torch.float32))
+    q = torch.randn(7, heads, r + dr, device="cuda", generator=g).to(DT[dtype])
+    rows = torch.randn(7, r + dr, device="cuda", generator=g).to(DT[dtype])
+    check_tree((cfg, pages, order[None].repeat(2, 1).contiguous(), dev([n, 65]), dev([0, 4, 7]), rows.cpu(),
+                [1, 2, 5, 9, 1, 3, 7], q.cpu(), [seq, seq], [0, 4, 7]), 0.125, dtype, [n, 65])
