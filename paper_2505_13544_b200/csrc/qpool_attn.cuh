@@ -61,6 +61,7 @@ struct AttnArgs {
   const int2* listed;
   const int* prefix;
   const int4* groups;
+  const int4* shares;        // the CTAs' shares of the tiles (tensor-core kernel)
   const uint8_t* image;      // the groups' queries as the tensor-core kernel wants them
   int cols;
 };

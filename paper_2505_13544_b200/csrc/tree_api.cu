@@ -18,7 +18,7 @@ constexpr int kMostCtas = 2 * kPlanSms;          // of the launch over the conte
 constexpr int kLeastCols = 16, kMostCols = 64;   // of a group
 
 // Sized for any group width, so that the choice between the kernels stays the call's.
-struct TreePlan { size_t o_part, ml_part, parts, groups, prefix, first, listed, error_words, image, total; };
+struct TreePlan { size_t o_part, ml_part, parts, groups, prefix, first, listed, shares, error_words, image, total; };
 long long most_groups(const mtla_qpool_config* c, int B, int n_nodes, int cols) {
   return (long long)n_nodes * c->n_heads / cols + (B < n_nodes ? B : n_nodes);
 }
@@ -41,7 +41,8 @@ TreePlan plan_tree(const mtla_qpool_config* c, int B, int n_nodes) {
   p.prefix = p.groups + align_up(groups * 16, 256);
   p.first = p.prefix + align_up((groups + 1) * 4, 256);
   p.listed = p.first + align_up(((size_t)B + 1) * 4, 256);
-  p.error_words = p.listed + 256;
+  p.shares = p.listed + 256;
+  p.error_words = p.shares + align_up(kPlanSms * 16, 256);
   p.image = p.error_words + align_up(kPlanSms * 4, 256);
   size_t image = 0;
   for (int w = 32; w <= kMostCols; w *= 2) {
@@ -79,22 +80,21 @@ bool registers_suffice() {
 }
 
 template <int NC, int NB>
-int launch_context_tc(const qp::AttnArgs& a, long long tiles, const OnDeviceOf& dev, cudaStream_t st) {
+int launch_context_tc(const qp::AttnArgs& a, int ctas, const OnDeviceOf& dev, cudaStream_t st) {
   if (!raise_smem<tree::tree_attend_tc_kernel<NC, NB>>(dev.device()) ||
       !registers_suffice<tree::tree_attend_tc_kernel<NC, NB>>())
     return MTLA_ERR_CUDA;
   const tree::Layout l(a.f, NC);
-  const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
-  return launch_dependent(tree::tree_attend_tc_kernel<NC, NB>, dim3(tiles < sms ? (int)tiles : sms), tree::kThreads,
+  return launch_dependent(tree::tree_attend_tc_kernel<NC, NB>, dim3(ctas), tree::kThreads,
                           l.total, st, a, l);
 }
 template <int NC>
-int launch_context_tc(const qp::AttnArgs& a, long long tiles, const OnDeviceOf& dev, cudaStream_t st) {
+int launch_context_tc(const qp::AttnArgs& a, int ctas, const OnDeviceOf& dev, cudaStream_t st) {
   switch (ceil_div(a.f.r, 128)) {
-    case 1: return launch_context_tc<NC, 1>(a, tiles, dev, st);
-    case 2: return launch_context_tc<NC, 2>(a, tiles, dev, st);
-    case 3: return launch_context_tc<NC, 3>(a, tiles, dev, st);
-    default: return launch_context_tc<NC, 4>(a, tiles, dev, st);
+    case 1: return launch_context_tc<NC, 1>(a, ctas, dev, st);
+    case 2: return launch_context_tc<NC, 2>(a, ctas, dev, st);
+    case 3: return launch_context_tc<NC, 3>(a, ctas, dev, st);
+    default: return launch_context_tc<NC, 4>(a, ctas, dev, st);
   }
 }
 
@@ -183,6 +183,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   pa.prefix = reinterpret_cast<int*>(ws + p.prefix);
   pa.first = reinterpret_cast<int*>(ws + p.first);
   pa.listed = reinterpret_cast<int2*>(ws + p.listed);
+  pa.shares = reinterpret_cast<int4*>(ws + p.shares);
   pa.batch = B;
   pa.n_nodes = n_nodes;
   pa.heads = cfg->n_heads;
@@ -195,6 +196,8 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   pa.f = format_of(cfg);
   const long long groups = most_groups(cfg, B, n_nodes, cols), images = tensor ? 2 * groups : 0;
   const int sms = dev.sm_count() < kPlanSms ? dev.sm_count() : kPlanSms;
+  const long long tiles = groups * ceil_div(table_width, pa.tile_pages);
+  pa.ctas = !tensor ? 0 : tiles < sms ? (int)tiles : sms;
   int status = launch_dependent(tree::tree_plan_kernel, dim3(1 + (unsigned)(images < 3 * sms ? images : 3 * sms)),
                                 tree::kPlanThreads, 0, st, pa);
   if (status != MTLA_OK) return status;
@@ -213,13 +216,13 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   a.n_pages = cfg->n_pages;
   a.f = pa.f;
   a.image = pa.image;
+  a.shares = pa.shares;
   a.listed = pa.listed;
   a.prefix = pa.prefix;
   a.groups = pa.groups;
   a.cols = cols;
-  const long long tiles = groups * ceil_div(table_width, pa.tile_pages);
   if (tensor)
-    status = cols == 64 ? launch_context_tc<64>(a, tiles, dev, st) : launch_context_tc<32>(a, tiles, dev, st);
+    status = cols == 64 ? launch_context_tc<64>(a, pa.ctas, dev, st) : launch_context_tc<32>(a, pa.ctas, dev, st);
   else
     status = cols == 32 ? launch_context<float, 2>(a, tiles, dev, st) : launch_context<float, 1>(a, tiles, dev, st);
   if (status != MTLA_OK) return status;
@@ -245,7 +248,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   j.heads = cfg->n_heads;
   j.cols = cols;
   j.part_row = tensor ? (cfg->latent_rank + 127) / 128 * 128 : cfg->latent_rank;
-  j.n_error_words = tensor ? (int)(tiles < sms ? tiles : sms) : 0;
+  j.n_error_words = pa.ctas;
   j.f = a.f;
   return dtype == MTLA_DTYPE_BF16 ? launch_join<bf16>(j, groups, dev, st) : launch_join<float>(j, groups, dev, st);
 }

@@ -213,16 +213,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
   grid_dependency_wait();
 
   const int* const prefix = a.prefix;
-  const int2 listed = *a.listed;
-  const int n_groups = max(listed.x, 0);
-  const long long total = listed.y;
-  const int ctas = (int)(total < gridDim.x ? total : gridDim.x);
-  int g0 = 0, g1 = 0;
-  if ((int)blockIdx.x < ctas) {
-    g0 = qp::share_begin(blockIdx.x, total, ctas);
-    g1 = qp::share_begin(blockIdx.x + 1, total, ctas);
-  }
-  const int n_tiles = __shfl_sync(0xffffffffu, g1 - g0, 0);      // uniform
+  const int4 share = a.shares[blockIdx.x];      // first tile, tiles, the first one's group, that group's first CTA
+  const int g0 = share.x, g1 = share.x + share.y;
+  const int n_tiles = __shfl_sync(0xffffffffu, share.y, 0);      // uniform
   const uint32_t q_u32 = base + L.off_q, p_u32 = base + L.off_p, st_u32 = base + L.off_st;
   auto wait = [&](unsigned long long& b, int phase) { return mbar_wait_compact(bar(b), phase & 1); };
   auto wait_warp = [&](unsigned long long& b, int phase) {                 // one answer for the warp
@@ -237,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
     reg_dealloc<kIssueRegs>();
     if (warp == kProducerWarp) {
       // ---------------------------------------------------------------- producer
-      int v = qp::find_wide(prefix, n_groups, g0), seg = -1, st = 0, round = 0, begun = 0;
+      int v = share.z, seg = -1, st = 0, round = 0, begun = 0;
       if (lane == 0) {
         int v_begin = prefix[v], v_end = prefix[v + 1];
         int4 group = a.groups[v];
@@ -271,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
           info.rows0 = rows[0];
           info.rows1 = rows[1];
           info.cols = group.z;
-          info.owner = qp::share_owner(v_begin, total, ctas);
+          info.owner = v == share.z ? share.w : (int)blockIdx.x;
           mbar_arrive(bar(misc->info_full[n % kInfo]));
           const uint32_t full = bar(misc->code_full[st]), dst = base + L.off_codes + st * L.stage;
           const uint8_t* src[2];
@@ -302,10 +295,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArg
       }
     } else if (warp == kQueryWarp) {
       // ---------------------------------------------------------------- queries of every segment
-      int v = qp::find_wide(prefix, n_groups, g0);
+      int v = share.z;
       if (lane == 0) {
         for (int seg = 0, g = g0; g < g1; ++seg) {
-          while (prefix[v + 1] <= g) ++v;
+          if (seg > 0)
+            while (prefix[v + 1] <= g) ++v;
           ok = seg == 0 || wait(misc->q_empty[(seg - 1) % kQRing], (seg - 1) / kQRing);
           if (!ok) break;
           const uint8_t* src = a.image + (long long)v * image_bytes(NC, f);

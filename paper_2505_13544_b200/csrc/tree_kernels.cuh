@@ -124,10 +124,11 @@ struct PlanArgs {
   int* prefix;               // [groups + 1] tiles before every group
   int* first;                // [batch + 1] first group of every request
   int2* listed;              // groups (-1: the batch is refused), their tiles
+  int4* shares;              // [ctas]: first tile, tiles, the first one's group, the CTA that begins that group
   const bf16* q;             // [n_nodes][heads][r + d_R]
   uint8_t* image;            // [groups] of image_bytes, or nullptr
   float scale_log2;
-  int batch, n_nodes, heads, width, cols, tile_pages;
+  int batch, n_nodes, heads, width, cols, tile_pages, ctas;
   qp::Format f;
 };
 
@@ -228,8 +229,9 @@ __global__ void __launch_bounds__(kPlanThreads, 2) tree_plan_kernel(PlanArgs a) 
     sum_t += g * tiles;
   }
   if (__syncthreads_or(wrong)) {
-    if (blockIdx.x == 0 && tid == 0) {
-      *a.listed = make_int2(-1, 0);
+    if (blockIdx.x == 0) {
+      if (tid == 0) *a.listed = make_int2(-1, 0);
+      for (int c = tid; c < a.ctas; c += kPlanThreads) a.shares[c] = make_int4(0, 0, 0, 0);
     }
     return;
   }
@@ -248,6 +250,25 @@ __global__ void __launch_bounds__(kPlanThreads, 2) tree_plan_kernel(PlanArgs a) 
   __syncthreads();
   const int total = s_first[a.batch];
   if (blockIdx.x == 0) {
+    // The shares of the tensor-core kernel's CTAs: found here once, they need not be found there by everyone before the
+    // first page is asked for (2600 cycles of a CTA's start).
+    const int all = s_tile[a.batch], ctas = min(a.ctas, all);
+    for (int c = tid; c < a.ctas; c += kPlanThreads) {
+      int4 share = make_int4(0, 0, 0, 0);
+      if (c < ctas) {
+        share.x = qp::share_begin(c, all, ctas);
+        share.y = qp::share_begin(c + 1, all, ctas) - share.x;
+        int b = 0, end = a.batch;                        // the last request that begins at this tile or before it
+        while (end - b > 1) {
+          const int mid = (b + end) >> 1;
+          if (s_tile[mid] <= share.x) b = mid; else end = mid;
+        }
+        const int tiles = tiles_of(a.slots[b]), i = (share.x - s_tile[b]) / tiles;
+        share.z = s_first[b] + i;
+        share.w = qp::share_owner(s_tile[b] + i * tiles, all, ctas);
+      }
+      a.shares[c] = share;
+    }
     for (int b = tid; b <= a.batch; b += kPlanThreads) a.first[b] = s_first[b];
     for (int b = warp; b < a.batch; b += kPlanThreads / 32) {
       const int col0 = a.starts[b] * a.heads, cols = a.starts[b + 1] * a.heads - col0, n_slots = a.slots[b];
@@ -426,6 +447,26 @@ __device__ __forceinline__ void store_column(const JoinArgs& a, long long column
   if (a.lse && lane == 0) a.lse[column] = failed ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
+// Pair number e of this lane's.
+template <typename T>
+__device__ __forceinline__ void store_pair(const JoinArgs& a, long long column, int e, float m, float l, bool failed,
+                                           uint64_t sum) {
+  constexpr int V = Running<T>::V;
+  const int lane = threadIdx.x & 31, at = (2 * e / V * 32 + lane) * V + 2 * e % V;
+  const float inv = failed ? NAN : l == 0.f ? 0.f : 1.f / l;
+  if (at < a.f.r) {
+    float x, y;
+    ptx::unpack2(sum, x, y);
+    T* out = static_cast<T*>(a.out) + column * a.f.r + at;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<__nv_bfloat162*>(out) = __floats2bfloat162_rn(x * inv, y * inv);
+    else
+      *reinterpret_cast<float2*>(out) = make_float2(x * inv, y * inv);
+  }
+  if (a.lse && lane == 0 && e == 0)
+    a.lse[column] = failed ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
 // The join: the softmax over the drafted rows that a node sees, and the parts that the attention over the context has
 // left for its columns; sums, maxima and products are fp32.  Bound by the parts' bytes when there are many columns,
 // else by the chain of loads.  Three forms:
@@ -493,6 +534,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
   constexpr int E = Run::E;
   __shared__ float s_m[kSplitWarps], s_l[kSplitWarps];
   __shared__ uint64_t s_acc[kSplitWarps][E / 2][32];
+  static_assert(kSplitWarps == E / 2, "a warp joins one pair of every lane's latents");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = a.f.r;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
@@ -547,16 +589,19 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
 #pragma unroll
     for (int e = 0; e < E / 2; ++e) s_acc[warp][e][lane] = run.acc[e];
     __syncthreads();
-    if (warp == 0) {
-#pragma unroll 1
-      for (int w = 1; w < kSplitWarps; ++w) {            // in the warps' order
-        uint64_t x[E / 2];
+    float top = s_m[0];
 #pragma unroll
-        for (int e = 0; e < E / 2; ++e) x[e] = s_acc[w][e][lane];
-        run.add(s_m[w], s_l[w], x);
-      }
-      store_column<T>(a, column, run.m, run.l, failed, run.acc);
+    for (int w = 1; w < kSplitWarps; ++w) top = fmaxf(top, s_m[w]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float l = 0.f;
+    uint64_t sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSplitWarps; ++w) {              // in the warps' order
+      const float p = exp2f(s_m[w] - ref);
+      l = fmaf(p, s_l[w], l);
+      sum = ptx::fma2(ptx::pack2(p, p), s_acc[w][warp][lane], sum);
     }
+    store_pair<T>(a, column, warp, top, l, failed, sum);
     __syncthreads();
   }
 }
