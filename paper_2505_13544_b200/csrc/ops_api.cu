@@ -86,7 +86,8 @@ int launch_attend(qp::AttnArgs a, const OnDeviceOf& dev, cudaStream_t st) {
   const int per_sm = smem <= 112 * 1024 ? kAttnCtasPerSm : 1;
   const long long most = (long long)a.batch * a.width;
   const int ctas = (int)(most < (long long)per_sm * sms ? most : (long long)per_sm * sms);
-  const int status = launch_dependent(qp::qpool_attend_kernel<T, MH>, dim3(ctas), qp::kAttnThreads, smem, st, a);
+  const int status = launch_dependent(qp::qpool_attend_kernel<T, MH>, dim3(ctas), qp::kAttnThreads, smem, st,
+                                      qp::KernelArgs<false>{a});
   return status == MTLA_OK ? launch_combine<T>(a, dev, st) : status;
 }
 

@@ -55,9 +55,21 @@ struct AttnArgs {
   float scale_log2;          // scale * log2(e)
   int n_heads, batch, width, n_pages, n_error_words;
   Format f;
-  // Column groups of drafted trees (tree_kernels.cuh) in the place of sequences: how many there are and their tiles, the
-  // tiles before each, and its request, first column, columns and slots.  Their results are always parts, of `cols`
-  // columns.
+};
+
+// Column groups of drafted trees (tree_kernels.cuh) in the place of sequences: how many there are and their tiles, the
+// tiles before each, and its request, first column, columns and slots.  Their results are always parts, of `cols`
+// columns.  A type of its own: as fields of all kernels' arguments these cost the tensor-core kernel over sequences
+// 1.4 % (128 x 16384 slots: 268 -> 272 us).
+template <bool TREE>
+struct KernelArgs : AttnArgs {
+  static constexpr const int2* listed = nullptr;
+  static constexpr const int* prefix = nullptr;
+  static constexpr const int4* groups = nullptr;
+  static constexpr int cols = 0;
+};
+template <>
+struct KernelArgs<true> : AttnArgs {
   const int2* listed;
   const int* prefix;
   const int4* groups;
@@ -65,6 +77,7 @@ struct AttnArgs {
   const uint8_t* image;      // the groups' queries as the tensor-core kernel wants them
   int cols;
 };
+using GroupArgs = KernelArgs<true>;
 
 constexpr int kAttnThreads = 256;
 constexpr int kAttnWarps = kAttnThreads / 32;
@@ -248,7 +261,7 @@ struct AttnLayout {
 // fp32: 41 for 34).
 // TREE: over column groups instead of sequences.
 template <typename T, int MH, bool TREE = false>
-__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 1) qpool_attend_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kAttnThreads, sizeof(T) == 2 || MH == 1 ? 2 : 1) qpool_attend_kernel(KernelArgs<TREE> a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 2;
   using L = AttnLayout<MH, TERMS>;
   constexpr int KT = L::kKeyTerms, NH = L::kHeads;

@@ -54,7 +54,7 @@ TreePlan plan_tree(const mtla_qpool_config* c, int B, int n_nodes) {
 }
 
 template <typename T, int MH>
-int launch_context(qp::AttnArgs a, long long tiles, const OnDeviceOf& dev, cudaStream_t st) {
+int launch_context(const qp::GroupArgs& a, long long tiles, const OnDeviceOf& dev, cudaStream_t st) {
   using L = qp::AttnLayout<MH, sizeof(T) == 2 ? 1 : 2>;
   if (!raise_smem<qp::qpool_attend_kernel<T, MH, true>>(dev.device())) return MTLA_ERR_CUDA;
   const int smem = L::bytes(a.f, 0);
@@ -80,7 +80,7 @@ bool registers_suffice() {
 }
 
 template <int NC, int NB>
-int launch_context_tc(const qp::AttnArgs& a, int ctas, const OnDeviceOf& dev, cudaStream_t st) {
+int launch_context_tc(const qp::GroupArgs& a, int ctas, const OnDeviceOf& dev, cudaStream_t st) {
   if (!raise_smem<tree::tree_attend_tc_kernel<NC, NB>>(dev.device()) ||
       !registers_suffice<tree::tree_attend_tc_kernel<NC, NB>>())
     return MTLA_ERR_CUDA;
@@ -89,7 +89,7 @@ int launch_context_tc(const qp::AttnArgs& a, int ctas, const OnDeviceOf& dev, cu
                           l.total, st, a, l);
 }
 template <int NC>
-int launch_context_tc(const qp::AttnArgs& a, int ctas, const OnDeviceOf& dev, cudaStream_t st) {
+int launch_context_tc(const qp::GroupArgs& a, int ctas, const OnDeviceOf& dev, cudaStream_t st) {
   switch (ceil_div(a.f.r, 128)) {
     case 1: return launch_context_tc<NC, 1>(a, ctas, dev, st);
     case 2: return launch_context_tc<NC, 2>(a, ctas, dev, st);
@@ -202,7 +202,7 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
                                 tree::kPlanThreads, 0, st, pa);
   if (status != MTLA_OK) return status;
 
-  qp::AttnArgs a = {};
+  qp::GroupArgs a = {};
   a.pages = static_cast<const uint8_t*>(pages);
   a.table = table;
   a.q = q;

@@ -158,7 +158,7 @@ __device__ __forceinline__ void set_down(float* part, uint32_t taddr, const floa
 }
 
 template <int NC, int NB>
-__global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::AttnArgs a, Layout L) {
+__global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupArgs a, Layout L) {
   using namespace ptx;
   using T = Tmem<NC, NB>;
   constexpr uint32_t IDESC_S = make_idesc_f16(128, NC, 0, 0), IDESC_K = make_idesc_bf16(128, NC, 0, 0);
