@@ -1120,16 +1120,17 @@ def mtla_qweight_unpack(packed: torch.Tensor, n_in: int, n_out: int, *, dtype=to
 def mtla_qweight_product(packed: torch.Tensor, x: torch.Tensor, n_out: int, out: torch.Tensor | None = None,
                          stream=None) -> torch.Tensor:
     """x [n][n_in] (fp32 or bf16, any row stride of whole 16 bytes) times packed weights [n_in][n_out]: [n][n_out]."""
-    if x.dim() != 2 or x.dtype not in _DTYPES or x.stride(1) != 1:
+    dtype, xs = x.dtype, x.stride()
+    if len(xs) != 2 or dtype not in _DTYPES or xs[1] != 1:
         raise TypeError("x: expected fp32 or bf16 [n][n_in], consecutive elements in a row")
     (n, n_in), dev = x.shape, _gpu_of(x, "x")
     if out is None:
         with _buffers_on(stream):
-            out = torch.empty(n, n_out, dtype=x.dtype, device=x.device)
-    if out.dtype is not x.dtype or out.shape != (n, n_out) or out.get_device() != dev or (
-            n_out > 1 and out.stride(1) != 1):
-        raise TypeError(f"out: expected {x.dtype} [{n}][{n_out}] on the call's GPU, consecutive elements in a row")
+            out = torch.empty(n, n_out, dtype=dtype, device=x.device)
+    ys = out.stride()
+    if out.dtype is not dtype or out.shape != (n, n_out) or out.get_device() != dev or (n_out > 1 and ys[1] != 1):
+        raise TypeError(f"out: expected {dtype} [{n}][{n_out}] on the call's GPU, consecutive elements in a row")
     _check(load_library().mtla_qweight_product(_qweight_buffer(packed, n_in, n_out, dev), n_in, n_out, x.data_ptr(),
-                                               x.stride(0), n, out.data_ptr(), out.stride(0), _DTYPES[x.dtype],
+                                               xs[0], n, out.data_ptr(), ys[0], _DTYPES[dtype],
                                                _stream_on(dev, stream)), "mtla_qweight_product")
     return out
