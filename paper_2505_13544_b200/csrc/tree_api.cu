@@ -100,10 +100,14 @@ int launch_context_tc(const qp::GroupArgs& a, int ctas, const OnDeviceOf& dev, c
 
 template <typename T>
 int launch_join(const tree::JoinArgs& a, long long groups, const OnDeviceOf& dev, cudaStream_t st) {
-  // A CTA per column as long as all of them run at once, two on an SM.
+  // A CTA per column, of eight warps as long as all of them run at once (two on an SM), of four up to twice what runs at
+  // once (four on an SM): 400 columns of 32773 slots 86 us with a warp per column, 69 so; 768 of 9000 57 and 50; but
+  // 1536 of 1024 slots 26.5 and 29.5.
   const long long columns = (long long)a.n_nodes * a.heads, sms = dev.sm_count();
   if (columns <= 2 * sms)
-    return launch_dependent(tree::tree_join_split_kernel<T>, dim3((unsigned)columns), tree::kSplitThreads, 0, st, a);
+    return launch_dependent(tree::tree_join_split_kernel<T, 8>, dim3((unsigned)columns), 256, 0, st, a);
+  if (columns <= 8 * sms)
+    return launch_dependent(tree::tree_join_split_kernel<T, 4>, dim3((unsigned)columns), 128, 0, st, a);
   if constexpr (sizeof(T) == 2) {
     if (a.cols == 64 && groups >= sms) {         // a group for every SM
       constexpr int kBytes = tree::Dense<64>::bytes(qp::Format{512, 64});

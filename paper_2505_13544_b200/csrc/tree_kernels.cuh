@@ -470,14 +470,14 @@ __device__ __forceinline__ void store_pair(const JoinArgs& a, long long column, 
 // The join: the softmax over the drafted rows that a node sees, and the parts that the attention over the context has
 // left for its columns; sums, maxima and products are fp32.  Bound by the parts' bytes when there are many columns,
 // else by the chain of loads.  Three forms:
-//   tree_join_split_kernel   a CTA per column, whose warps share rows and parts out, for few columns (112 columns in 74
+//   tree_join_split_kernel   a CTA per column, whose W warps share rows and parts out, for few columns (112 columns in 74
 //                            parts each: 53 us with a warp per column, 14 so);
 //   tree_join_kernel         a warp per column, row after row;
 //   tree_join_dense_kernel   a CTA per group of 64 columns, all its drafted rows by matrix products, for bf16 with a group
 //                            for every SM (16384 columns that see 6 of 64 rows each: 45 us with a warp per column, 36 so;
 //                            52 groups: 14 us and 25).
 // In the first two masked rows are never read, so what they hold cannot reach a result.
-constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kSplitThreads = 256, kSplitWarps = kSplitThreads / 32;
+constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32;
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads, 5) tree_join_kernel(JoinArgs a) {
@@ -528,18 +528,17 @@ __global__ void __launch_bounds__(kJoinThreads, 5) tree_join_kernel(JoinArgs a) 
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinArgs a) {
+template <typename T, int W>
+__global__ void __launch_bounds__(32 * W, 16 / W) tree_join_split_kernel(JoinArgs a) {
   using Run = Running<T>;
   constexpr int E = Run::E;
-  __shared__ float s_m[kSplitWarps], s_l[kSplitWarps];
-  __shared__ uint64_t s_acc[kSplitWarps][E / 2][32];
-  static_assert(kSplitWarps == E / 2, "a warp joins one pair of every lane's latents");
+  __shared__ float s_m[W], s_l[W];
+  __shared__ uint64_t s_acc[W][E / 2][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = a.f.r;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
   bool failed = false;
-  for (int i = threadIdx.x; i < a.n_error_words; i += kSplitThreads) failed |= a.error_words[i] != 0;
+  for (int i = threadIdx.x; i < a.n_error_words; i += 32 * W) failed |= a.error_words[i] != 0;
   const bool refused = a.listed->x < 0;
   failed = __syncthreads_or(failed) || refused;
   const uint32_t columns = (uint32_t)(refused ? a.n_nodes : a.starts[a.batch]) * a.heads;
@@ -550,7 +549,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
     const int3 parts = parts_of(a, p, node, h, refused);
     Run run;
     run.clear();
-    // Rows in turn: the warp's are the set bits number warp, warp + 8, ...
+    // Rows in turn: the warp's are the set bits number warp, warp + W, ...
     if (__popcll(p.seen) > warp) {
       uint64_t q[E / 2];
       float qk[2];
@@ -559,7 +558,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
       for (int n = 0; seen; ++n) {
         const int at = __ffsll((long long)seen) - 1;
         seen &= seen - 1;
-        if (n % kSplitWarps != warp) continue;
+        if (n % W != warp) continue;
         uint64_t x[E / 2];
         float k[2];
         load_row<T>(static_cast<const T*>(a.rows) + (p.lo + at) * a.row_stride, a.f, x, k);
@@ -567,12 +566,12 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
       }
     }
     constexpr int U = 4;                                 // parts whose loads are in flight together
-    for (int n0 = warp; n0 < parts.y; n0 += U * kSplitWarps) {
+    for (int n0 = warp; n0 < parts.y; n0 += U * W) {
       float2 ml[U];
       uint64_t x[U][E / 2];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const int n = n0 + i * kSplitWarps;
+        const int n = n0 + i * W;
         if (n >= parts.y) break;
         const long long at = (long long)(parts.x + n) * a.cols + parts.z;
         ml[i] = reinterpret_cast<const float2*>(a.ml_part)[at];
@@ -580,7 +579,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
       }
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (n0 + i * kSplitWarps < parts.y) run.add(ml[i].x, ml[i].y, x[i]);
+        if (n0 + i * W < parts.y) run.add(ml[i].x, ml[i].y, x[i]);
     }
     if (lane == 0) {
       s_m[warp] = run.m;
@@ -591,17 +590,20 @@ __global__ void __launch_bounds__(kSplitThreads, 2) tree_join_split_kernel(JoinA
     __syncthreads();
     float top = s_m[0];
 #pragma unroll
-    for (int w = 1; w < kSplitWarps; ++w) top = fmaxf(top, s_m[w]);
+    for (int w = 1; w < W; ++w) top = fmaxf(top, s_m[w]);
     const float ref = top == -INFINITY ? 0.f : top;
-    float l = 0.f;
-    uint64_t sum = 0;
+    float l = 0.f, share[W];
 #pragma unroll
-    for (int w = 0; w < kSplitWarps; ++w) {              // in the warps' order
-      const float p = exp2f(s_m[w] - ref);
-      l = fmaf(p, s_l[w], l);
-      sum = ptx::fma2(ptx::pack2(p, p), s_acc[w][warp][lane], sum);
+    for (int w = 0; w < W; ++w) {                        // in the warps' order
+      share[w] = exp2f(s_m[w] - ref);
+      l = fmaf(share[w], s_l[w], l);
     }
-    store_pair<T>(a, column, warp, top, l, failed, sum);
+    for (int e = warp; e < E / 2; e += W) {              // a pair of every lane's latents
+      uint64_t sum = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) sum = ptx::fma2(ptx::pack2(share[w], share[w]), s_acc[w][e][lane], sum);
+      store_pair<T>(a, column, e, top, l, failed, sum);
+    }
     __syncthreads();
   }
 }
