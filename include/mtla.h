@@ -463,6 +463,15 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
                            const int64_t* seen, const void* q, int32_t n_nodes, int32_t dtype, float scale, void* out,
                            float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Diagnostics, as mtla_selftest_qpool_timeout: a wait that runs out in the place of the attention over the context, and
+ * then the attention's last kernel, which answers with NaN for every node of a request.  Arguments as for
+ * mtla_qpool_attend_tree. */
+int mtla_selftest_tree_timeout(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
+                               const int32_t* slots, const int32_t* starts, int32_t B, const void* rows,
+                               int64_t row_stride, const int64_t* seen, const void* q, int32_t n_nodes, int32_t dtype,
+                               float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
 /* Weights in 4 bits, for the projections around the pool: a matrix w device [n_in][n_out] (w_stride elements apart,
  * fp32 or bf16) is kept as e2m1 codes with a scale per 32 inputs of an output, codes and scales as in the pool
  * (see above; a group with an infinity or a NaN reads back as NaN), 4.25 bits a weight, in blocks of 128 inputs by 16

@@ -43,8 +43,8 @@ EXPORTED_SYMBOLS = (
     "mtla_train_workspace_bytes", "mtla_train_backward", "mtla_slot_map", "mtla_rope",
     "mtla_qpool_page_bytes", "mtla_qpool_write", "mtla_qpool_read", "mtla_qpool_workspace_bytes",
     "mtla_qpool_attend", "mtla_selftest_qpool_timeout", "mtla_tree_map", "mtla_qpool_tree_workspace_bytes",
-    "mtla_qpool_attend_tree", "mtla_qweight_bytes", "mtla_qweight_pack", "mtla_qweight_unpack",
-    "mtla_qweight_product")
+    "mtla_qpool_attend_tree", "mtla_selftest_tree_timeout", "mtla_qweight_bytes", "mtla_qweight_pack",
+    "mtla_qweight_unpack", "mtla_qweight_product")
 
 PAGE_SLOTS = 64
 
@@ -212,6 +212,8 @@ def load_library() -> ctypes.CDLL:
         "mtla_qpool_tree_workspace_bytes": (sz, [qp_p, i32, i32]),
         "mtla_qpool_attend_tree": (ctypes.c_int, [qp_p, vp, vp, i32, vp, vp, i32, vp, ctypes.c_int64, vp, vp, i32, i32,
                                                   ctypes.c_float, vp, vp, vp, sz, vp]),
+        "mtla_selftest_tree_timeout": (ctypes.c_int, [qp_p, vp, vp, i32, vp, vp, i32, vp, ctypes.c_int64, vp, vp, i32, i32,
+                                                      ctypes.c_float, vp, vp, vp, sz, vp]),
         "mtla_qweight_bytes": (sz, [i32, i32]),
         "mtla_qweight_pack": (ctypes.c_int, [vp, ctypes.c_int64, i32, i32, i32, vp, vp]),
         "mtla_qweight_unpack": (ctypes.c_int, [vp, i32, i32, vp, ctypes.c_int64, i32, vp]),
@@ -1042,7 +1044,7 @@ def mtla_qpool_tree_workspace_bytes(cfg: mtla_qpool_config, batch: int, n_nodes:
 def mtla_qpool_attend_tree(cfg: mtla_qpool_config, pages: torch.Tensor, table: torch.Tensor, slots: torch.Tensor,
                            starts: torch.Tensor, rows: torch.Tensor, seen: torch.Tensor, q: torch.Tensor, *,
                            scale: float, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-                           workspace: torch.Tensor | None = None, stream=None):
+                           workspace: torch.Tensor | None = None, stream=None, _call="mtla_qpool_attend_tree"):
     """q [n_nodes][n_heads][r + d_R] over the first slots[b] slots of table row b and the rows [n_nodes][r + d_R] of
     the node's request (starts int32 [B + 1]) that seen (int64 [n_nodes]) names; returns (out [n_nodes][n_heads][r],
     lse [n_nodes][n_heads] fp32).  workspace: uint8, see mtla_qpool_tree_workspace_bytes; a fresh one if
@@ -1072,10 +1074,16 @@ def mtla_qpool_attend_tree(cfg: mtla_qpool_config, pages: torch.Tensor, table: t
             _ptr(workspace, torch.uint8, ws_shape, dev, "workspace"), ws_shape.numel(), _stream_on(dev, stream))
     if batch == 0 or n == 0:             # nothing to do, but for the configuration's check
         if mtla_qpool_page_bytes(cfg) == 0:
-            raise MTLAError(-2, "mtla_qpool_attend_tree")
+            raise MTLAError(-2, _call)
         return out, lse
-    _check(load_library().mtla_qpool_attend_tree(*args), "mtla_qpool_attend_tree")
+    _check(getattr(load_library(), _call)(*args), _call)
     return out, lse
+
+
+def mtla_selftest_tree_timeout(*args, **kw):
+    """Arguments as for mtla_qpool_attend_tree: runs a bounded wait out in the place of the attention over the context and
+    lets the last kernel answer: NaN for every node of a request."""
+    return mtla_qpool_attend_tree(*args, **kw, _call="mtla_selftest_tree_timeout")
 
 
 def mtla_qweight_bytes(n_in: int, n_out: int) -> int:

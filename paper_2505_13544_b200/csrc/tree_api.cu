@@ -121,44 +121,11 @@ int launch_join(const tree::JoinArgs& a, long long groups, const OnDeviceOf& dev
                           a);
 }
 
-}  // namespace
-
-extern "C" {
-
-int mtla_tree_map(const int32_t* held, const int32_t* starts, const int32_t* parents, int32_t B, int32_t stride,
-                  const mtla_tree_map_out* out, int32_t n_nodes, void* stream) {
-  if (!held || !starts || !out || !out->slots || B < 1 || stride < 1 || n_nodes < 0) return MTLA_ERR_INVALID_ARG;
-  if (n_nodes > 0 && (!parents || !out->seq || !out->position || !out->seen)) return MTLA_ERR_INVALID_ARG;
-  const void* words[] = {held, starts, parents, out->seq, out->position, out->slots};
-  for (const void* p : words)
-    if (!aligned(p, 4)) return MTLA_ERR_INVALID_ARG;
-  if (!aligned(out->seen, 8)) return MTLA_ERR_INVALID_ARG;
-  if (B > tree::kMaxRequests) return MTLA_ERR_UNSUPPORTED_SHAPE;
-  OnDeviceOf dev(out->slots);
-  if (dev.status() != MTLA_OK) return dev.status();
-  tree::MapArgs a;
-  a.held = held;
-  a.starts = starts;
-  a.parents = parents;
-  a.seq = out->seq;
-  a.position = out->position;
-  a.slots = out->slots;
-  a.seen = reinterpret_cast<unsigned long long*>(out->seen);
-  a.batch = B;
-  a.n_nodes = n_nodes;
-  a.stride = stride;
-  return launch_dependent(tree::tree_map_kernel, dim3(ceil_div(B, tree::kMapThreads / 32)), tree::kMapThreads, 0,
-                          static_cast<cudaStream_t>(stream), a);
-}
-
-size_t mtla_qpool_tree_workspace_bytes(const mtla_qpool_config* cfg, int32_t B, int32_t n_nodes) {
-  return good_tree(cfg, B, n_nodes) ? plan_tree(cfg, B, n_nodes).total : 0;
-}
-
-int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
-                           const int32_t* slots, const int32_t* starts, int32_t B, const void* rows, int64_t row_stride,
-                           const int64_t* seen, const void* q, int32_t n_nodes, int32_t dtype, float scale, void* out,
-                           float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+// `run_out`: the self-test, in which a wait that runs out takes the place of the attention over the context.
+int attend_tree(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
+                const int32_t* slots, const int32_t* starts, int32_t B, const void* rows, int64_t row_stride,
+                const int64_t* seen, const void* q, int32_t n_nodes, int32_t dtype, float scale, void* out, float* lse,
+                void* workspace, size_t workspace_bytes, void* stream, bool run_out) {
   if (!pages || !table || !slots || !starts || !workspace || B < 1 || n_nodes < 0 || table_width < 1 ||
       !good_dtype(dtype) || !isfinite((float)((double)scale * kLog2e)) || (n_nodes > 0 && (!rows || !seen || !q || !out)))
     return MTLA_ERR_INVALID_ARG;
@@ -225,7 +192,10 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   a.prefix = pa.prefix;
   a.groups = pa.groups;
   a.cols = cols;
-  if (tensor)
+  if (run_out) {
+    qp::wait_timeout_selftest_kernel<<<1, 64, 0, st>>>(a.error_words);
+    status = launched();
+  } else if (tensor)
     status = cols == 64 ? launch_context_tc<64>(a, pa.ctas, dev, st) : launch_context_tc<32>(a, pa.ctas, dev, st);
   else
     status = cols == 32 ? launch_context<float, 2>(a, tiles, dev, st) : launch_context<float, 1>(a, tiles, dev, st);
@@ -252,9 +222,60 @@ int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, cons
   j.heads = cfg->n_heads;
   j.cols = cols;
   j.part_row = tensor ? (cfg->latent_rank + 127) / 128 * 128 : cfg->latent_rank;
-  j.n_error_words = pa.ctas;
+  j.n_error_words = run_out ? 1 : pa.ctas;
   j.f = a.f;
   return dtype == MTLA_DTYPE_BF16 ? launch_join<bf16>(j, groups, dev, st) : launch_join<float>(j, groups, dev, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int mtla_tree_map(const int32_t* held, const int32_t* starts, const int32_t* parents, int32_t B, int32_t stride,
+                  const mtla_tree_map_out* out, int32_t n_nodes, void* stream) {
+  if (!held || !starts || !out || !out->slots || B < 1 || stride < 1 || n_nodes < 0) return MTLA_ERR_INVALID_ARG;
+  if (n_nodes > 0 && (!parents || !out->seq || !out->position || !out->seen)) return MTLA_ERR_INVALID_ARG;
+  const void* words[] = {held, starts, parents, out->seq, out->position, out->slots};
+  for (const void* p : words)
+    if (!aligned(p, 4)) return MTLA_ERR_INVALID_ARG;
+  if (!aligned(out->seen, 8)) return MTLA_ERR_INVALID_ARG;
+  if (B > tree::kMaxRequests) return MTLA_ERR_UNSUPPORTED_SHAPE;
+  OnDeviceOf dev(out->slots);
+  if (dev.status() != MTLA_OK) return dev.status();
+  tree::MapArgs a;
+  a.held = held;
+  a.starts = starts;
+  a.parents = parents;
+  a.seq = out->seq;
+  a.position = out->position;
+  a.slots = out->slots;
+  a.seen = reinterpret_cast<unsigned long long*>(out->seen);
+  a.batch = B;
+  a.n_nodes = n_nodes;
+  a.stride = stride;
+  return launch_dependent(tree::tree_map_kernel, dim3(ceil_div(B, tree::kMapThreads / 32)), tree::kMapThreads, 0,
+                          static_cast<cudaStream_t>(stream), a);
+}
+
+size_t mtla_qpool_tree_workspace_bytes(const mtla_qpool_config* cfg, int32_t B, int32_t n_nodes) {
+  return good_tree(cfg, B, n_nodes) ? plan_tree(cfg, B, n_nodes).total : 0;
+}
+
+int mtla_qpool_attend_tree(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
+                           const int32_t* slots, const int32_t* starts, int32_t B, const void* rows, int64_t row_stride,
+                           const int64_t* seen, const void* q, int32_t n_nodes, int32_t dtype, float scale, void* out,
+                           float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  return attend_tree(cfg, pages, table, table_width, slots, starts, B, rows, row_stride, seen, q, n_nodes, dtype, scale, out,
+                     lse, workspace, workspace_bytes, stream, false);
+}
+
+int mtla_selftest_tree_timeout(const mtla_qpool_config* cfg, const void* pages, const int32_t* table, int32_t table_width,
+                               const int32_t* slots, const int32_t* starts, int32_t B, const void* rows,
+                               int64_t row_stride, const int64_t* seen, const void* q, int32_t n_nodes, int32_t dtype,
+                               float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  return attend_tree(cfg, pages, table, table_width, slots, starts, B, rows, row_stride, seen, q, n_nodes, dtype, scale, out,
+                     lse, workspace, workspace_bytes, stream, true);
 }
 
 }  // extern "C"

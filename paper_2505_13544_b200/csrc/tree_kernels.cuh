@@ -315,7 +315,7 @@ struct JoinArgs {
   const int4* groups;
   const int* first;
   const int2* listed;
-  const int2* parts;         // [groups] first part, number of parts
+  const int2* parts;         // [groups] first part, number of parts; not to be read once an error word is set
   const float* o_part;       // [parts][cols][part_row], r of each row used
   const float* ml_part;      // [parts][cols][2]
   const int* error_words;
@@ -418,9 +418,10 @@ __device__ __forceinline__ Place place_of(const JoinArgs& a, int node, bool refu
   p.seen = hi - p.lo < kMaxNodes ? seen & ((1ull << (hi - p.lo)) - 1) : seen;
   return p;
 }
-// The parts of a column: x first, y number; z the column inside its group.
-__device__ __forceinline__ int3 parts_of(const JoinArgs& a, const Place& p, int node, int h, bool refused) {
-  if (refused) return make_int3(0, 0, 0);
+// The parts of a column: x first, y number; z the column inside its group.  None after a failure: a group's entry is
+// written by the CTA that ends the group, so where that one has given up it holds whatever the workspace held.
+__device__ __forceinline__ int3 parts_of(const JoinArgs& a, const Place& p, int node, int h, bool failed) {
+  if (failed) return make_int3(0, 0, 0);
   const int local = (node - p.lo) * a.heads + h, v = p.first_group + (local >> (31 - __clz(a.cols)));
   const int2 parts = a.parts[v];                       // (not set for a group without tiles)
   return make_int3(parts.x, a.groups[v].w > 0 ? parts.y : 0, local & (a.cols - 1));
@@ -499,7 +500,7 @@ __global__ void __launch_bounds__(kJoinThreads, 5) tree_join_kernel(JoinArgs a) 
     load_row<T>(static_cast<const T*>(a.q) + (long long)column * (r + a.f.dr), a.f, q, qk);
     Place p = place_of(a, node, refused);
     if (!p.fine) continue;
-    const int3 parts = parts_of(a, p, node, h, refused);
+    const int3 parts = parts_of(a, p, node, h, failed);
     float2 ml;
     uint64_t y[E / 2];
     auto load_one = [&](int n) {
@@ -546,7 +547,7 @@ __global__ void __launch_bounds__(32 * W, 16 / W) tree_join_split_kernel(JoinArg
     const int node = (int)(column / (uint32_t)a.heads), h = (int)(column - (uint32_t)node * a.heads);
     const Place p = place_of(a, node, refused);
     if (!p.fine) continue;
-    const int3 parts = parts_of(a, p, node, h, refused);
+    const int3 parts = parts_of(a, p, node, h, failed);
     Run run;
     run.clear();
     // Rows in turn: the warp's are the set bits number warp, warp + W, ...
@@ -650,7 +651,7 @@ __global__ void __launch_bounds__(NC * 4, 2) tree_join_dense_kernel(JoinArgs a) 
   const int4 group = a.groups[v];
   const int lo = a.starts[group.x], count = a.starts[group.x + 1] - lo, n_rows = min(count, kMaxNodes);
   const int steps = (n_rows + 15) / 16;                // of 16 rows
-  const int2 parts = group.w > 0 ? a.parts[v] : make_int2(0, 0);
+  const int2 parts = !failed && group.w > 0 ? a.parts[v] : make_int2(0, 0);      // see parts_of
   static_assert(kPlanThreads / 32 == 16, "half a group is one or two columns of every warp");
   if (tid < NC) {
     unsigned long long seen = 0;

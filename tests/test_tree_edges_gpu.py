@@ -1,0 +1,47 @@
+"""Drafted trees over the 4-bit pool: what a failure inside leaves, and calls at the edges of what their documentation
+allows.  Oracle and tolerances are those of test_tree_gpu.py."""
+import time
+
+import pytest
+import torch
+
+from paper_2505_13544_b200 import binding as M
+from tests.test_operators_gpu import DT
+from tests.test_tree_gpu import check_tree, dev, tree_setup
+
+pytestmark = pytest.mark.gpu
+
+
+def call_args(s):
+    return (*s[:5], s[5].cuda(), dev(s[6], torch.int64), s[7].cuda())
+
+
+# slots, nodes, heads, r, type: up to 2 columns an SM, up to 8, more; more than 148 groups of 64 columns.
+JOINS = [([300, 0], [3, 2], 4, 128, "bf16"), ([300, 0, 70], [20, 9, 4], 16, 192, "bf16"),
+         ([300, 0, 70], [20, 9, 16], 31, 256, "bf16"), ([130, 0, 64, 1, 300], [64] * 5, 32, 64, "bf16"),
+         ([300, 0], [3, 2], 4, 128, "fp32"), ([300, 0, 70], [20, 9, 4], 16, 192, "fp32"),
+         ([300, 0, 70], [20, 9, 16], 31, 256, "fp32")]
+
+
+@pytest.mark.parametrize("case", range(len(JOINS)))
+def test_a_wait_that_runs_out_gives_no_result(case):
+    """A bounded wait that gives up leaves the list of parts unwritten.  Here it says that every group has 200 parts (which
+    the workspace does have room for): all nodes get NaN whatever it says, nodes of no request stay as they were, and
+    the next call on the same workspace is an ordinary one."""
+    lens, counts, heads, r, dtype = JOINS[case]
+    s = tree_setup(lens, counts, heads, r, 32, dtype, case, front=1, pad=2)
+    args, n = call_args(s), sum(counts)
+    ws = torch.zeros(M.mtla_qpool_tree_workspace_bytes(s[0], len(lens), n + 3), dtype=torch.uint8, device="cuda")
+    out = torch.full((n + 3, heads, r), 7.0, dtype=DT[dtype], device="cuda")
+    lse = torch.full((n + 3, heads), 7.0, device="cuda")
+    for parts in (0, 200 << 32):                             # none; the first 200
+        ws.view(torch.int64).fill_(parts)
+        out.fill_(7), lse.fill_(7)
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        M.mtla_selftest_tree_timeout(*args, scale=0.125, out=out, lse=lse, workspace=ws)
+        torch.cuda.synchronize()
+        assert time.perf_counter() - t0 < 1.0
+        for t in (out, lse):
+            assert torch.isnan(t[1:n + 1]).all() and (t[:1] == 7).all() and (t[n + 1:] == 7).all()
+    check_tree(s, 0.125, dtype, lens, nodes=set(range(0, n + 3, 5)), workspace=ws)
