@@ -38,6 +38,11 @@ constexpr int kIssueRegs = 40, kExpandRegs = 64, kSoftmaxRegs = 104;
 constexpr int kRoleRegisters = 4 * kIssueRegs + (kScoreWarps + kValueWarps) * kExpandRegs + 8 * kSoftmaxRegs;
 static_assert(kRoleRegisters <= 72 * (kThreads / 32), "there are 72 registers for each of 896 threads");
 constexpr int kQRing = qp::tc::kQRing, kInfo = 16, kUnitRing = 8, kMaxStages = 4;
+// Barriers for the ends of segments: a phase must not complete twice before the value warps have looked at it.  When the
+// softmax warps end segment s, products of the tile two before its last one have been issued; that is a tile of segment
+// s - 2 or later, for which the value warps had to be done with the segment in front of it: of segments of one
+// tile s - 3, and no later one.  So three at least.  (end_fac is used by segments of over 128 tiles only.)
+constexpr int kEndRing = 4;
 constexpr float kShift = qp::tc::kShift, kRescale = qp::tc::kRescale;
 constexpr int kFoldTiles = qp::tc::kFoldTiles;
 constexpr int kFirst = 1, kLast = 2, kFold = 4, kFolded = 8, kFoldedNow = 16, kEnds = 32, kSegShift = 6;
@@ -64,7 +69,7 @@ struct Misc {
   unsigned long long as_full[kUnitRing], as_empty[kUnitRing], av_full[kUnitRing], av_empty[kUnitRing];
   unsigned long long s_full[2], s_empty[2], p_full[4], p_empty[4];       // a probability tile: each half of the slots
   unsigned long long q_full[kQRing], q_empty[kQRing];
-  unsigned long long end_full[2], o_full[2], o_empty;
+  unsigned long long end_full[kEndRing], o_full[2], o_empty;
   unsigned long long info_full[kInfo];
   uint32_t tmem_base;
   int abort_word;
@@ -78,6 +83,7 @@ struct Misc {
   float m_fold[64], end_fac[2][64];
 };
 constexpr int kMiscBytes = 5632;
+static_assert(kEndRing <= kMaxStages && kQRing <= kMaxStages, "barriers that are set up side by side");
 static_assert(sizeof(Misc) <= kMiscBytes, "misc region too small");
 
 struct Layout {
@@ -189,6 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupAr
       mbar_init(bar(misc->code_full[i]), 1);
       mbar_init(bar(misc->code_empty[i]), kScoreWarps + kValueWarps);
       mbar_init(bar(misc->scale_full[i]), kScoreWarps);
+      mbar_init(bar(misc->end_full[i]), kSoftmaxWarps);
       mbar_init(bar(misc->q_full[i]), 1);
       mbar_init(bar(misc->q_empty[i]), 1);
     }
@@ -197,7 +204,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupAr
       mbar_init(bar(misc->key_empty[i]), 1);
       mbar_init(bar(misc->s_full[i]), 1);
       mbar_init(bar(misc->s_empty[i]), kSoftmaxWarps);
-      mbar_init(bar(misc->end_full[i]), kSoftmaxWarps);
       mbar_init(bar(misc->o_full[i]), 1);
     }
     if (i == 0) mbar_init(bar(misc->o_empty), kValueWarps);
@@ -549,7 +555,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupAr
         if (info.flags & kLast) {
           // A segment's sums leave tensor memory, while the softmax warps go on.
           const int seg = info.flags >> kSegShift;
-          ok = __all_sync(0xffffffffu, wait(misc->end_full[seg & 1], seg >> 1) && wait(misc->o_full[seg & 1], seg >> 1));
+          ok = __all_sync(0xffffffffu, wait(misc->end_full[seg % kEndRing], seg / kEndRing) &&
+                                           wait(misc->o_full[seg & 1], seg >> 1));
           if (!ok) break;
           tc_fence_after_sync();
           set_down<NC, NB, VG>(a.o_part + ((long long)blockIdx.x + info.group) * (NC * 128 * NB), lane_tm + T::kColO,
@@ -754,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupAr
       }
       if (ok && sidx == 0 && (flags & kEnds)) a.seq_parts[v] = make_int2(info.owner + v, (int)blockIdx.x - info.owner + 1);
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(misc->end_full[flags >> kSegShift & 1]));
+      if (lane == 0) mbar_arrive(bar(misc->end_full[(flags >> kSegShift) % kEndRing]));
       group_sync();                                      // red, unit and the references may be rewritten
     }
   }
