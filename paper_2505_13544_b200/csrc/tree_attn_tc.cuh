@@ -615,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupAr
     };
     uint8_t* const p_row = sm + L.off_p + (HO / 8) * P_SBO + slot * 16;
     float l_acc[NHH];
-    bool unset = true;                                   // no slot of the segment yet, hence no reference
+    bool unset = true;                                   // a column has no reference: no score above minus infinity yet
     for (int n = 0; n < n_tiles; ++n) {
       if (ok && sw == 3) ok = wait(misc->info_full[n % kInfo], n / kInfo) && wait(misc->s_full[n % SB], n / SB);
       if (named_sync_or<kSoftmaxThreads>(1, !ok)) break;
@@ -684,15 +684,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupAr
         // Some reference has to rise: always at a segment's first slots, else rarely.
         reduce_columns(x, true);
         group_sync();
+        bool none = false;                               // this thread's column has no reference after this tile either
         if (sidx < NC) {
-          // What the column's largest score is above its reference by (from the bare scores: itself).
-          const float mt = reduced(sidx, true) - (unset ? 0.f : kShift), m_old = unset ? 0.f : misc->m_used[sidx];
-          const bool rise = unset ? mt > -INFINITY : mt > kRescale;
+          // What the column's largest score is above its reference by; without one (its x are bare scores): itself.
+          const float m_used = misc->m_used[sidx];
+          const bool first = m_used == -INFINITY;
+          const float mt = reduced(sidx, true) - (first ? 0.f : kShift), m_old = first ? 0.f : m_used;
+          const bool rise = mt > (first ? -INFINITY : kRescale);
           const float by = rise ? mt : 0.f;
-          misc->m_used[sidx] = unset && !rise ? -INFINITY : m_old + by;
-          misc->neg_ref[sidx] = unset && !rise ? 0.f : kShift - (m_old + by);
-          misc->fac[sidx] = unset ? 0.f : exp2f(-by);
-          misc->down[sidx] = unset ? kShift - by : -by;
+          none = first && !rise;
+          misc->m_used[sidx] = none ? -INFINITY : m_old + by;
+          misc->neg_ref[sidx] = none ? 0.f : kShift - (m_old + by);
+          misc->fac[sidx] = first ? 0.f : exp2f(-by);
+          misc->down[sidx] = first ? kShift - by : -by;
         }
         group_sync();
 #pragma unroll
@@ -700,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupAr
           l_acc[i] *= misc->fac[HO + i];
           x[i] += misc->down[HO + i];
         }
-        if (!unset && !(flags & kFold)) {
+        if (!(flags & (kFirst | kFold))) {
           // O is scaled to the old references: wait for the previous tile's products, rescale.
           if (ok) ok = wait(misc->p_empty[2 * ps1 + 1], p_round1);
           ok = __all_sync(0xffffffffu, ok);              // TMEM accesses are whole-warp operations
@@ -720,8 +724,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attend_tc_kernel(qp::GroupAr
             tmem_wait_st();
           }
         }
-        unset = unset && (info.rows0 | info.rows1) == 0;
-        group_sync();                                    // fac / down / red may be rewritten
+        // fac / down / red may be rewritten from here.
+        unset = named_sync_or<kSoftmaxThreads>(1, none && sidx < info.cols);
       }
       // The value products of the tile that had this half's place are done.
       if (ok) ok = wait(misc->p_empty[2 * ps + (q >> 1)], p_round + 1);

@@ -45,3 +45,21 @@ def test_a_wait_that_runs_out_gives_no_result(case):
         for t in (out, lse):
             assert torch.isnan(t[1:n + 1]).all() and (t[:1] == 7).all() and (t[n + 1:] == 7).all()
     check_tree(s, 0.125, dtype, lens, nodes=set(range(0, n + 3, 5)), workspace=ws)
+
+
+@pytest.mark.parametrize("heads,count", [(4, 3), (32, 2), (16, 9)])
+def test_first_slots_whose_scores_are_minus_infinity(heads, count):
+    """Keys of minus infinity (of bf16 queries with a positive element there) take their slots out, also where a CTA's
+    share begins with whole tiles of them: the scores behind them set the references."""
+    r, dr, batch = 128, 32, 200
+    lens, hidden = [[500, 130, 700, 129][b % 4] for b in range(batch)], [[256, 129, 300, 128][b % 4] for b in range(batch)]
+    cfg, pages, table, slots, starts, rows, seen, q, seqs, host_starts = tree_setup(lens, [count] * batch, heads, r, dr, "bf16", 31)
+    q[..., r] = q[..., r].abs() + 0.5
+    q *= 4
+    table_h = table.cpu()
+    at = torch.cat([table_h[b, torch.arange(n) // 64].long() * 64 + torch.arange(n) % 64 for b, n in enumerate(hidden)])
+    holes = torch.cat([torch.from_numpy(v[:n]).float() for v, n in zip(seqs, hidden)])
+    holes[:, r] = -float("inf")
+    M.mtla_qpool_write(cfg, pages, holes.cuda(), at.cuda())
+    s = (cfg, pages, table, slots, starts, rows, seen, q, [v[n:] for v, n in zip(seqs, hidden)], host_starts)
+    check_tree(s, 0.125, "bf16", [n - h for n, h in zip(lens, hidden)], nodes=set(range(0, batch * count, 7)))
