@@ -25,7 +25,8 @@ struct ProductArgs {
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 
 // Eight consecutive elements of a row as B operands: bf16 as they are, fp32 as three bf16 terms that add up to it
-// exactly (cut off, 8 bits each; an infinity is the first term alone).
+// exactly (cut off, 8 bits each).  An infinity is the first term alone; a NaN may have its fraction in the lower half only,
+// so that its first term is an infinity, but then what is left of it is a NaN.
 template <typename T>
 struct Operand;
 template <>
@@ -70,7 +71,7 @@ struct Operand<float> {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float top = __uint_as_float(__float_as_uint(x[2 * i + h]) & 0xffff0000u);
-          x[2 * i + h] = fabsf(top) == INFINITY ? 0.f : x[2 * i + h] - top;
+          x[2 * i + h] = fabsf(x[2 * i + h]) == INFINITY ? 0.f : x[2 * i + h] - top;
         }
       }
   }
