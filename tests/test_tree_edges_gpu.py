@@ -2,12 +2,14 @@
 allows.  Oracle and tolerances are those of test_tree_gpu.py."""
 import time
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import tree_oracle as T
 from paper_2505_13544_b200 import binding as M
-from tests.test_operators_gpu import DT
-from tests.test_tree_gpu import check_tree, dev, tree_setup
+from tests.test_operators_gpu import DT, host
+from tests.test_tree_gpu import check_tree, dev, pool_of, starts_of, tree_setup
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +65,30 @@ def test_first_slots_whose_scores_are_minus_infinity(heads, count):
     M.mtla_qpool_write(cfg, pages, holes.cuda(), at.cuda())
     s = (cfg, pages, table, slots, starts, rows, seen, q, [v[n:] for v, n in zip(seqs, hidden)], host_starts)
     check_tree(s, 0.125, "bf16", [n - h for n, h in zip(lens, hidden)], nodes=set(range(0, batch * count, 7)))
+
+
+def test_sums_that_are_set_down_twice():
+    """344 tiles a group and 372 a CTA: segments of over 256 tiles, whose sums leave tensor memory twice and are added up.
+    At tile 250 the scores rise by 5.8, a little more than what a reference may stay behind (8 log 2 = 5.55), so that
+    the sums of the first 128 tiles have to be brought to another reference at the second time, and still weigh
+    128 e^-5.8 / (94 + 250 e^-5.8) = 0.4 % of the result.  Latents of one sign, so the mean of the relative errors shows what is lost or counted too much: a probability's rounding, 2^-11
+    at most; what the matrix unit cuts off in the 1024 products of 128 tiles, less than 2^-22 each (a quarter of 2^-10); the
+    results' rounding to bf16, which cancels out over 2048 of them (4 standard deviations are 4 * 2^-8 / sqrt(12 * 2048), a
+    quarter of 2^-10): together below 2^-10 + 2^-11."""
+    n, heads, r, dr, scale = 44000, 32, 64, 32, 0.5
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows = torch.randn(n, r + dr, device="cuda", generator=g)
+    rows[:, :r] = rows[:, :r].abs() + 0.5
+    rows[:, r] = 5.8 / scale * (torch.arange(n, device="cuda") // (250 * 128))
+    cfg, pages, order, seq = pool_of(rows, heads, r, dr)
+    counts, lens = [64] * 5, [n, n - 5, n - 700, n - 128, n]
+    q = torch.randn(320, heads, r + dr, device="cuda", generator=g) * 0.01
+    q[..., r] = 1.0
+    mine = torch.randn(320, r + dr, device="cuda", generator=g).bfloat16()
+    s = (cfg, pages, order[None].repeat(5, 1).contiguous(), dev(lens), dev(starts_of(counts)), mine.cpu(), [0] * 320,
+         q.bfloat16().cpu(), [seq] * 5, starts_of(counts))
+    nodes = {0, 20, 63, 64, 130, 200, 319}
+    out, _ = check_tree(s, scale, "bf16", lens, nodes=nodes)
+    for i in nodes:
+        want, _, _ = T.attend_node(host(s[7][i]), seq[:lens[i // 64]], np.zeros((0, r + dr)), 0, scale, r)
+        assert abs((host(out[i]) / want - 1).mean()) <= 2.0 ** -10 + 2.0 ** -11, i
