@@ -435,7 +435,9 @@ int mtla_selftest_qpool_timeout(const mtla_qpool_config* cfg, const int32_t* slo
  * itself: bit j of `seen` is node j of the request.  Outputs (device): seq, position, seen [n_nodes], slots [B].
  * Nodes of no request get seq -1, position 0, seen 0; so do, refused on the device, those of a request with more
  * than 64 nodes, a parent out of order, a negative `held` or a position past 2^31 - 1, and all nodes of a
- * batch whose `starts` are out of order.  Requests without nodes may occur. */
+ * batch whose `starts` are out of order.  seq is what tells: a refused request keeps its slots[b] (0 for a negative
+ * `held`), so that a plain step still finds its context, and mtla_qpool_attend_tree, which does not look at seq,
+ * gives its nodes the softmax over that context alone.  Requests without nodes may occur. */
 typedef struct {
   int32_t *seq, *position;
   int64_t* seen;

@@ -1047,7 +1047,9 @@ def mtla_qpool_attend_tree(cfg: mtla_qpool_config, pages: torch.Tensor, table: t
                            workspace: torch.Tensor | None = None, stream=None, _call="mtla_qpool_attend_tree"):
     """q [n_nodes][n_heads][r + d_R] over the first slots[b] slots of table row b and the rows [n_nodes][r + d_R] of
     the node's request (starts int32 [B + 1]) that seen (int64 [n_nodes]) names; returns (out [n_nodes][n_heads][r],
-    lse [n_nodes][n_heads] fp32).  workspace: uint8, see mtla_qpool_tree_workspace_bytes; a fresh one if
+    lse [n_nodes][n_heads] fp32).  Nodes of no request (a batch padded to a fixed size) are not written: with buffers made
+    here their entries are whatever the memory held.  A node that mtla_tree_map has refused (seq -1) sees its
+    request's context alone.  workspace: uint8, see mtla_qpool_tree_workspace_bytes; a fresh one if
     None (a loop should keep one).  Results made on a given stream belong to that stream, as with torch's own operations."""
     if q.dim() != 3 or table.dim() != 2 or q.dtype not in _DTYPES:
         raise TypeError("q: expected fp32 or bf16 [n_nodes][n_heads][r + d_R]; table: expected [B][width]")
