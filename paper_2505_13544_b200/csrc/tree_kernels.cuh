@@ -4,7 +4,7 @@
 // A request's columns are its nodes times the heads; a column is a query row [r + d_R] and an output row [r],
 // both at index column of the flat tensors.  All nodes of a request see the same context slots (a path continues
 // the open slot, so only closed ones are left, and those are common), which makes the context's part the attention
-// of `columns` queries over one list of pages without any mask.  Groups of up to kCols columns take the place that
+// of `columns` queries over one list of pages without any mask.  Groups of up to 64 columns take the place that
 // sequences have in qpool_attn.cuh.
 #pragma once
 
@@ -298,6 +298,7 @@ __global__ void __launch_bounds__(kPlanThreads, 2) tree_plan_kernel(PlanArgs a) 
     uint8_t* image = a.image + (long long)v * image_bytes(a.cols, a.f);
     // Half a group: two columns a warp of 64, one of 32.
     constexpr int kWarps = kPlanThreads / 32;
+    static_assert(kWarps == 16, "half a group is one or two columns of every warp");
     if (a.cols == 64)
       put_columns<2>(q, cols, image, (u & 1) * half + warp, kWarps, a.cols, a.scale_log2, a.f);
     else
@@ -652,7 +653,6 @@ __global__ void __launch_bounds__(NC * 4, 2) tree_join_dense_kernel(JoinArgs a) 
   const int lo = a.starts[group.x], count = a.starts[group.x + 1] - lo, n_rows = min(count, kMaxNodes);
   const int steps = (n_rows + 15) / 16;                // of 16 rows
   const int2 parts = !failed && group.w > 0 ? a.parts[v] : make_int2(0, 0);      // see parts_of
-  static_assert(kPlanThreads / 32 == 16, "half a group is one or two columns of every warp");
   if (tid < NC) {
     unsigned long long seen = 0;
     if (tid < group.z) {
