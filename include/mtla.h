@@ -487,10 +487,18 @@ int mtla_qweight_unpack(const void* packed, int32_t n_in, int32_t n_out, void* w
 
 /* y[n][n_out] = x[n][n_in] W for the rows of a step, n up to 2^19: x device, 16-byte aligned, x_stride elements
  * apart (a multiple of 16 bytes unless n is 1), y device, y_stride elements apart (any, at least n_out); they must not
- * overlap.  dtype is that of x and y.  Weights enter exactly, sums are fp32.  Every row's result is independent
- * of the others' values. */
+ * overlap.  dtype is that of x and y.  Weights enter exactly; sums are fp32, but of bf16 rows the matrix unit cuts its running
+ * sums off instead of rounding them: a sum of one sign comes out short, by up to 3.6e-4 of it at 2^16 inputs and
+ * in proportion at fewer (fp32 rows: sums of 32 inputs only).  Every row's result is independent of the others' values.
+ * (Should a bounded wait inside the kernel give up, which nothing in a correct program leads to, the results of its
+ * tile are NaN.) */
 int mtla_qweight_product(const void* packed, int32_t n_in, int32_t n_out, const void* x, int64_t x_stride, int32_t n,
                          void* y, int64_t y_stride, int32_t dtype, void* stream);
+
+/* Diagnostics: the tensor-core kernel for up to 32 bf16 rows a tile, whose rows never arrive; its waits run out after about a
+ * millisecond, and all of y is NaN.  Arguments as for mtla_qweight_product with bf16 rows; nothing is left behind. */
+int mtla_selftest_qweight_timeout(const void* packed, int32_t n_in, int32_t n_out, const void* x, int64_t x_stride,
+                                  int32_t n, void* y, int64_t y_stride, void* stream);
 
 /* Bytes of cache in use: B * ceil(tokens/s) * (r + d_R) * sizeof(element)  (Sections 4, 4.3);
  * with per-sequence token counts, the sum over the sequences. */

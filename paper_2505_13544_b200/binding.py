@@ -44,7 +44,7 @@ EXPORTED_SYMBOLS = (
     "mtla_qpool_page_bytes", "mtla_qpool_write", "mtla_qpool_read", "mtla_qpool_workspace_bytes",
     "mtla_qpool_attend", "mtla_selftest_qpool_timeout", "mtla_tree_map", "mtla_qpool_tree_workspace_bytes",
     "mtla_qpool_attend_tree", "mtla_selftest_tree_timeout", "mtla_qweight_bytes", "mtla_qweight_pack",
-    "mtla_qweight_unpack", "mtla_qweight_product")
+    "mtla_qweight_unpack", "mtla_qweight_product", "mtla_selftest_qweight_timeout")
 
 PAGE_SLOTS = 64
 
@@ -218,6 +218,7 @@ def load_library() -> ctypes.CDLL:
         "mtla_qweight_pack": (ctypes.c_int, [vp, ctypes.c_int64, i32, i32, i32, vp, vp]),
         "mtla_qweight_unpack": (ctypes.c_int, [vp, i32, i32, vp, ctypes.c_int64, i32, vp]),
         "mtla_qweight_product": (ctypes.c_int, [vp, i32, i32, vp, ctypes.c_int64, i32, vp, ctypes.c_int64, i32, vp]),
+        "mtla_selftest_qweight_timeout": (ctypes.c_int, [vp, i32, i32, vp, ctypes.c_int64, i32, vp, ctypes.c_int64, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -1144,3 +1145,11 @@ def mtla_qweight_product(packed: torch.Tensor, x: torch.Tensor, n_out: int, out:
                                                xs[0], n, out.data_ptr(), ys[0], _DTYPES[dtype],
                                                _stream_on(dev, stream)), "mtla_qweight_product")
     return out
+
+
+def mtla_selftest_qweight_timeout(packed: torch.Tensor, x: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """The tensor-core product of bf16 rows whose waits run out: all of out [n][n_out] is NaN."""
+    (n, n_in), n_out, dev = x.shape, out.shape[1], _gpu_of(x, "x")
+    _check(load_library().mtla_selftest_qweight_timeout(
+        _qweight_buffer(packed, n_in, n_out, dev), n_in, n_out, _ptr(x, torch.bfloat16, (n, n_in), dev, "x"), n_in, n,
+        _ptr(out, torch.bfloat16, (n, n_out), dev, "out"), n_out, _stream_on(dev, stream)), "mtla_selftest_qweight_timeout")

@@ -74,10 +74,10 @@ bool make_x_map(CUtensorMap* map, const qw::ProductArgs& a, int box) {
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN>
+template <int BN, bool RUN_OUT = false>
 int launch_product_tc(const qw::ProductArgs& p, const OnDeviceOf& dev, cudaStream_t st) {
   using C = qw::tc::Config<BN>;
-  if (!raise_smem<qw::tc::qweight_tc_kernel<BN>>(dev.device(), C::kBytes)) return MTLA_ERR_CUDA;
+  if (!raise_smem<qw::tc::qweight_tc_kernel<BN, RUN_OUT>>(dev.device(), C::kBytes)) return MTLA_ERR_CUDA;
   CUtensorMap map;
   if (!make_x_map(&map, p, BN)) return MTLA_ERR_CUDA;
   qw::tc::Args a;
@@ -105,9 +105,28 @@ int launch_product_tc(const qw::ProductArgs& p, const OnDeviceOf& dev, cudaStrea
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.splits > 1 ? 2 : 1;
-  if (cudaLaunchKernelEx(&cfg, qw::tc::qweight_tc_kernel<BN>, map, a) == cudaSuccess) return MTLA_OK;
+  if (cudaLaunchKernelEx(&cfg, qw::tc::qweight_tc_kernel<BN, RUN_OUT>, map, a) == cudaSuccess) return MTLA_OK;
   cudaGetLastError();
   return MTLA_ERR_CUDA;
+}
+
+// What a call is refused for; fills in the kernels' arguments.
+int product_args(qw::ProductArgs& a, const void* packed, int32_t n_in, int32_t n_out, const void* x, int64_t x_stride, int32_t n,
+                 void* y, int64_t y_stride, int32_t dtype) {
+  if (!packed || n < 0 || !good_dtype(dtype) || (n > 0 && (!x || !y))) return MTLA_ERR_INVALID_ARG;
+  if (!good_shape(n_in, n_out) || n > kMostSize / 8) return MTLA_ERR_UNSUPPORTED_SHAPE;
+  const int vec = dtype == MTLA_DTYPE_BF16 ? 8 : 4;
+  if (!aligned(packed, 16) || !aligned(x, 16) || !aligned(y, 16 / vec) ||
+      (n > 1 && (x_stride < n_in || x_stride % vec || y_stride < n_out)))
+    return MTLA_ERR_INVALID_ARG;
+  a.packed = static_cast<const uint8_t*>(packed);
+  a.x = x;
+  a.y = y;
+  a.x_stride = x_stride;
+  a.y_stride = y_stride;
+  a.n = n;
+  a.s = qw::Shape{n_in, n_out};
+  return MTLA_OK;
 }
 
 }  // namespace
@@ -130,23 +149,11 @@ int mtla_qweight_unpack(const void* packed, int32_t n_in, int32_t n_out, void* w
 
 int mtla_qweight_product(const void* packed, int32_t n_in, int32_t n_out, const void* x, int64_t x_stride, int32_t n,
                          void* y, int64_t y_stride, int32_t dtype, void* stream) {
-  if (!packed || n < 0 || !good_dtype(dtype) || (n > 0 && (!x || !y))) return MTLA_ERR_INVALID_ARG;
-  if (!good_shape(n_in, n_out) || n > kMostSize / 8) return MTLA_ERR_UNSUPPORTED_SHAPE;
-  const int vec = dtype == MTLA_DTYPE_BF16 ? 8 : 4;
-  if (!aligned(packed, 16) || !aligned(x, 16) || !aligned(y, 16 / vec) ||
-      (n > 1 && (x_stride < n_in || x_stride % vec || y_stride < n_out)))
-    return MTLA_ERR_INVALID_ARG;
-  if (n == 0) return MTLA_OK;
+  qw::ProductArgs a;
+  const int status = product_args(a, packed, n_in, n_out, x, x_stride, n, y, y_stride, dtype);
+  if (status != MTLA_OK || n == 0) return status;
   OnDeviceOf dev(packed);
   if (dev.status() != MTLA_OK) return dev.status();
-  qw::ProductArgs a;
-  a.packed = static_cast<const uint8_t*>(packed);
-  a.x = x;
-  a.y = y;
-  a.x_stride = x_stride;
-  a.y_stride = y_stride;
-  a.n = n;
-  a.s = qw::Shape{n_in, n_out};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (dtype == MTLA_DTYPE_FP32) return n <= 8 ? launch_product<float, 1, 1>(a, st) : launch_product<float, 2, 1>(a, st);
   // Several blocks' loads ahead as long as all CTAs run at once all the same, two on an SM.
@@ -159,6 +166,16 @@ int mtla_qweight_product(const void* packed, int32_t n_in, int32_t n_out, const 
   if ((double)n * n_in * n_out <= 1.5e8) return launch_product<bf16, 4, 1>(a, st);
   if (n <= 32) return launch_product_tc<32>(a, dev, st);
   return n <= 64 ? launch_product_tc<64>(a, dev, st) : launch_product_tc<128>(a, dev, st);
+}
+
+int mtla_selftest_qweight_timeout(const void* packed, int32_t n_in, int32_t n_out, const void* x, int64_t x_stride, int32_t n,
+                                  void* y, int64_t y_stride, void* stream) {
+  qw::ProductArgs a;
+  const int status = product_args(a, packed, n_in, n_out, x, x_stride, n, y, y_stride, MTLA_DTYPE_BF16);
+  if (status != MTLA_OK || n == 0) return status;
+  OnDeviceOf dev(packed);
+  if (dev.status() != MTLA_OK) return dev.status();
+  return launch_product_tc<32, true>(a, dev, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

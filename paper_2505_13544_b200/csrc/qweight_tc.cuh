@@ -75,7 +75,8 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int BN>
+// RUN_OUT, the self-test: no row of x is ever fetched, and the waits give up after 2^21 cycles (about a millisecond).
+template <int BN, bool RUN_OUT = false>
 __global__ void __launch_bounds__(kThreads, 2) qweight_tc_kernel(const __grid_constant__ CUtensorMap x_map, Args a) {
   using namespace ptx;
   using C = Config<BN>;
@@ -120,13 +121,14 @@ __global__ void __launch_bounds__(kThreads, 2) qweight_tc_kernel(const __grid_co
 
   const int n0 = blockIdx.y * BN, n_units = 2 * n_kb;              // of 64 inputs
   const uint32_t raw_u32 = base + C::kPanels;
-  auto wait = [&](unsigned long long& b, int phase) { return mbar_wait_compact(bar(b), phase & 1); };
-  auto wait_warp = [&](unsigned long long& b, int phase) { return mbar_wait_eager(bar(b), phase & 1); };
+  constexpr uint32_t CYCLES = RUN_OUT ? 1u << 21 : 0x7fffffffu;
+  auto wait = [&](unsigned long long& b, int phase) { return mbar_wait_compact<CYCLES>(bar(b), phase & 1); };
+  auto wait_warp = [&](unsigned long long& b, int phase) { return mbar_wait_eager<32, CYCLES>(bar(b), phase & 1); };
   bool ok = true;                    // false once a wait of this thread has given up
 
   if (warp == 0) {
     // ---------------------------------------------------------------- rows of x
-    if (lane == 0) {
+    if (lane == 0 && !RUN_OUT) {
       for (int u = 0; u < n_units && ok; ++u) {
         const int st = u % C::kStages;
         ok = wait(misc.b_empty[st], u / C::kStages + 1);

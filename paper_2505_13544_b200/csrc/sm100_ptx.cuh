@@ -124,12 +124,12 @@ __device__ __forceinline__ bool mbar_wait_compact(uint32_t bar, uint32_t parity)
 // The same for a whole warp, which asks a few times without being suspended before it settles down to wait: to be told
 // of what is there takes some 40 cycles then instead of 140, which is what a warp that issues matrix instructions
 // loses between two runs of them (four of 128 x 64 x 16 take 128 cycles).
-template <int ASK = 32>
+template <int ASK = 32, uint32_t CYCLES = 0x7fffffffu>
 __device__ __forceinline__ bool mbar_wait_eager(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
   for (int i = 0; i < ASK; ++i)
     if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-  return __all_sync(0xffffffffu, mbar_wait_compact(bar, parity));
+  return __all_sync(0xffffffffu, mbar_wait_compact<CYCLES>(bar, parity));
 }
 
 // 2^x by the special-function unit (about 2 ulp; flushes denormals): enough for probabilities

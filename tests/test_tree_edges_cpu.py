@@ -1,5 +1,5 @@
-"""Drafted trees: what the self-test of a wait refuses, and the order of the attention's roles at the ends of segments
-(host checks only)."""
+"""Drafted trees and 4-bit weights: what the self-tests of waits refuse, and the order in which the attention's roles may
+come to the ends of segments (host checks only)."""
 import ctypes
 import os
 import re
@@ -25,6 +25,15 @@ def test_selftest_of_the_tree_attentions_wait_refuses():
     for bad in BAD_POOLS + (dict(B=4097),):
         assert call(**bad) == -2, bad
     assert call(ws_bytes=need - 1) == -3
+
+
+def test_selftest_of_the_products_wait_refuses():
+    lib = M.load_library()
+    for bad in (dict(p=None), dict(x=None), dict(y=None), dict(n=-1), dict(p=A + 8), dict(x=A + 8), dict(y=A + 1),
+                dict(xs=120), dict(xs=132), dict(ys=15)):
+        a = {**dict(p=A, x=A, xs=128, n=2, y=A, ys=16), **bad}
+        assert lib.mtla_selftest_qweight_timeout(a["p"], 128, 16, a["x"], a["xs"], a["n"], a["y"], a["ys"], None) == -1, bad
+    assert lib.mtla_selftest_qweight_timeout(A, 12, 16, A, 128, 1, A, 16, None) == -2
 
 
 # ------------------------------------------------------------------------------ ends of segments
