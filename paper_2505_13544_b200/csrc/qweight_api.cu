@@ -162,7 +162,9 @@ int mtla_qweight_product(const void* packed, int32_t n_in, int32_t n_out, const 
   if (n <= 16 && (double)n_in * n_out <= 2e7)        // 16 rows of 8192 x 8192: 23.6 us, on the tensor cores 16.6
     return ahead ? launch_product<bf16, 2, 2>(a, st) : launch_product<bf16, 2, 1>(a, st);
   // More rows: the tensor cores' set-up and joining take 3 us longer, passes over the weights 2.2 us per 10^8
-  // products (64 rows of 1024 x 1024: 4.1 us and 6.6; 32 of 4096 x 4096: 12.4 and 9.2; 128 of 2048 x 512: 7.3 and 7.7).
+  // products (on the tensor cores and here, 64 rows of 1024 x 1024: 6.5 us and 4.6; 32 of 4096 x 4096: 9.2 and 12.3; 128 of
+  // 2048 x 512: 7.6 and 6.9).  A pass is longer with many inputs and few outputs, which the rule does not see: 17 rows
+  // of 4096 x 1024 take 7.1 us here where the tensor cores need 6.3, 24 rows 8.5 and 6.3, 32 rows of 2048 x 2048 7.0 and 6.1.
   if ((double)n * n_in * n_out <= 1.5e8) return launch_product<bf16, 4, 1>(a, st);
   if (n <= 32) return launch_product_tc<32>(a, dev, st);
   return n <= 64 ? launch_product_tc<64>(a, dev, st) : launch_product_tc<128>(a, dev, st);

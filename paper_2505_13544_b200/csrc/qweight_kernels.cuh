@@ -1,7 +1,7 @@
 // Products of a few rows with 4-bit weights: y[n][out] = x[n][in] . W[in][out].
 //
 // The weights' bytes bound the product as long as there are few rows: 4.25 bits each, 1.4 us for 4096 x 4096, behind
-// some 2 us of launch and first loads (one row takes 4.8 us).  This kernel keeps everything in registers: a lane's 16
+// some 2 us of launch and first loads (one row takes 4.5 us).  This kernel keeps everything in registers: a lane's 16
 // bytes of a block are 32 inputs of one output, decoded to bf16 pairs in place as the A operand of the warp-level matrix
 // instruction (m16n8k16: 16 outputs by 8 rows of x).  The order of the inputs inside a block of 128 is permuted alike
 // on both sides: lane (g, t) multiplies group t, so that it also reads x 16 bytes at a time.
@@ -79,8 +79,9 @@ struct Operand<float> {
 
 // A CTA per 16 outputs and 8 NT rows; its warps share the input blocks out, sums are joined in the warps' order.  The
 // loads of U blocks (weights, scales and x) are issued before the first of them is used.  That takes registers: one row
-// of 4096 x 4096, where all CTAs run at once either way, takes 7.2 us with one block at a time and 5.1 with four; of
-// 8192 x 8192 it takes 14.7 and 15.8.
+// of 4096 x 4096, where all CTAs run at once either way, takes 5.9 us with one block at a time and 4.5 with four; of
+// 8192 x 8192 it takes 12.4 and 14.2 (bytes: 5.5).  fp32 rows pass over the weights once for every 16 rows, with three
+// products each: 512 rows of 4096 x 6720 take 867 us (bf16 rows on the tensor cores: 28).
 template <typename T, int NT, int U>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && NT <= 2 && U == 1 ? 4 : 2) qweight_product_kernel(ProductArgs a) {
   constexpr int TERMS = Operand<T>::kTerms;

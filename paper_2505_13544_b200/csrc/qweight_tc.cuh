@@ -4,7 +4,7 @@
 // warps decode 64 inputs of the tile from the raw blocks in shared memory into bf16 (exactly, times 2^-13) and write them
 // to tensor memory, the rows of x are the B operand, which a tensor map brings into shared memory with its 128-byte
 // swizzle.  So the weights' 4 bits are all that travels of them.  Bound by the matrix unit with many rows (128 x BN x 16
-// in BN / 2 cycles; 2048 rows through 4096 x 6720: 90 us, 1.25 PFLOP/s), by the length of the chain with few (load,
+// in BN / 2 cycles; 2048 rows through 4096 x 6720: 92 us, 1.23 PFLOP/s), by the length of the chain with few (load,
 // decode, multiply, join: 9 us for 32 rows through 4096 x 4096).  Two CTAs an SM hide each other's starts and ends: with
 // 256 outputs a CTA, which halves the reads of x, 512 rows took 33 us, so 28.
 //

@@ -19,7 +19,7 @@
 // warps of their own for either product 246 -> 237 us of this kernel; waits and indices of a tile outside the units'
 // loop 238 -> 221; probabilities handed over in halves, queries laid out ahead and results written by the value
 // warps 221 -> 212; issuing warps that ask before they wait 254 -> 245 of the whole call.  Twelve value warps instead
-// of eight leave 56 registers a thread and spill (232 us for 221); reading a unit's bytes ahead costs more instructions
+// of eight leave 56 registers a thread and spill more (232 us for 221; as it is, 64 columns spill 84 to 168 bytes a thread); reading a unit's bytes ahead costs more instructions
 // than it hides (256 for 243).  Every wait is bounded as there.
 #pragma once
 

@@ -1,5 +1,6 @@
 """Drafted trees over the 4-bit pool: what a failure inside leaves, and calls at the edges of what their documentation
 allows.  Oracle and tolerances are those of test_tree_gpu.py."""
+import ctypes
 import time
 
 import numpy as np
@@ -92,3 +93,22 @@ def test_sums_that_are_set_down_twice():
     for i in nodes:
         want, _, _ = T.attend_node(host(s[7][i]), seq[:lens[i // 64]], np.zeros((0, r + dr)), 0, scale, r)
         assert abs((host(out[i]) / want - 1).mean()) <= 2.0 ** -10 + 2.0 ** -11, i
+
+
+@pytest.mark.parametrize("case", range(len(JOINS)))
+def test_attend_tree_without_the_logarithm(case):
+    """A NULL lse: the same outputs, through each of the joins."""
+    lens, counts, heads, r, dtype = JOINS[case]
+    args = call_args(tree_setup(lens, counts, heads, r, 32, dtype, case, front=1, pad=2))
+    cfg, pages, table, slots, starts, rows, seen, q = args
+    n = sum(counts)
+    want, _ = M.mtla_qpool_attend_tree(*args, scale=0.125)
+    out = torch.full((n + 3, heads, r), 7.0, dtype=DT[dtype], device="cuda")
+    ws = torch.empty(M.mtla_qpool_tree_workspace_bytes(cfg, len(lens), n + 3), dtype=torch.uint8, device="cuda")
+    status = M.load_library().mtla_qpool_attend_tree(
+        ctypes.byref(cfg), pages.data_ptr(), table.data_ptr(), table.shape[1], slots.data_ptr(), starts.data_ptr(), len(lens),
+        rows.data_ptr(), r + 32, seen.data_ptr(), q.data_ptr(), n + 3, 1 if dtype == "bf16" else 0, 0.125, out.data_ptr(), None,
+        ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert status == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out[1:n + 1], want[1:n + 1]) and (out[:1] == 7).all() and (out[n + 1:] == 7).all()
