@@ -421,11 +421,11 @@ __device__ __forceinline__ Place place_of(const JoinArgs& a, int node, bool refu
 }
 // The parts of a column: x first, y number; z the column inside its group.  None after a failure: a group's entry is
 // written by the CTA that ends the group, so where that one has given up it holds whatever the workspace held.
-__device__ __forceinline__ int3 parts_of(const JoinArgs& a, const Place& p, int node, int h, bool failed) {
-  if (failed) return make_int3(0, 0, 0);
+__device__ __forceinline__ int3 parts_of(const JoinArgs& a, const Place& p, int node, int h, bool refused, bool failed) {
+  if (refused) return make_int3(0, 0, 0);
   const int local = (node - p.lo) * a.heads + h, v = p.first_group + (local >> (31 - __clz(a.cols)));
   const int2 parts = a.parts[v];                       // (not set for a group without tiles)
-  return make_int3(parts.x, a.groups[v].w > 0 ? parts.y : 0, local & (a.cols - 1));
+  return make_int3(parts.x, !failed && a.groups[v].w > 0 ? parts.y : 0, local & (a.cols - 1));
 }
 template <typename T>
 __device__ __forceinline__ void store_column(const JoinArgs& a, long long column, float m, float l, bool failed,
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(kJoinThreads, 5) tree_join_kernel(JoinArgs a) 
     load_row<T>(static_cast<const T*>(a.q) + (long long)column * (r + a.f.dr), a.f, q, qk);
     Place p = place_of(a, node, refused);
     if (!p.fine) continue;
-    const int3 parts = parts_of(a, p, node, h, failed);
+    const int3 parts = parts_of(a, p, node, h, refused, failed);
     float2 ml;
     uint64_t y[E / 2];
     auto load_one = [&](int n) {
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(32 * W, 16 / W) tree_join_split_kernel(JoinArg
     const int node = (int)(column / (uint32_t)a.heads), h = (int)(column - (uint32_t)node * a.heads);
     const Place p = place_of(a, node, refused);
     if (!p.fine) continue;
-    const int3 parts = parts_of(a, p, node, h, failed);
+    const int3 parts = parts_of(a, p, node, h, refused, failed);
     Run run;
     run.clear();
     // Rows in turn: the warp's are the set bits number warp, warp + W, ...
